@@ -384,6 +384,127 @@ vqc_status vqc_plan_export(const vqc_plan* plan, void* buf, size_t* inout_bytes)
  * in vqc_plan_export.  The records are those of this build, not a stable format. */
 vqc_status vqc_frames_export(const vqc_plan* plan, void* buf, size_t* inout_bytes);
 
+/* ---------------------------------------------------------------------------
+ * Classical operators of a hybrid model: what stands before and behind a
+ * circuit inside a network (features to angles, expectations back to features,
+ * normalisation and gated feed-forward blocks between them).  The paper has no
+ * counterpart; its circuits are trained inside such models.
+ *
+ * Conventions.  Matrices are row-major; a stride is the number of elements
+ * between the rows of an operand (>= its columns; elements of a row are
+ * adjacent).  Outputs are dense and 16-byte aligned; inputs may have any alignment.  `dtype`
+ * is the type of x, the weights, the biases and their gradients; sums, row
+ * statistics and saved pre-activations are float.  rows >= 0 (0 rows: outputs
+ * per row are empty, sums over rows zero), columns 1..2^31-1.  Calls are
+ * stream-ordered and use no memory but their arguments; results do not depend
+ * on timing (sums have a fixed order).  A call whose workspace size is 0 may
+ * be given NULL.  Buffers must not overlap. */
+typedef enum { VQC_F32 = 0, VQC_BF16 = 1, VQC_F16 = 2 } vqc_real;
+
+typedef enum {
+    VQC_ACT_NONE = 0,
+    VQC_ACT_RELU = 1,      /* max(z, 0) */
+    VQC_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function (error function form) */
+    VQC_ACT_SILU = 3,      /* z / (1 + exp(-z)) */
+    VQC_ACT_TANH = 4,
+    VQC_ACT_SIGMOID = 5    /* 1 / (1 + exp(-z)) */
+} vqc_activation;
+
+/* Layer norm over the columns of each row: y = (x - mean) * rstd * weight + bias
+ * with mean and rstd = 1 / sqrt(var + eps) of the row (var without Bessel's
+ * correction).
+ *   weight, bias  [cols] of dtype, or NULL (1 and 0).
+ *   y             [rows, cols] of dtype.
+ *   stats         [rows, 2] float: mean and rstd, for the backward; or NULL.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_CUDA. */
+vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, const void* x,
+                                  int64_t x_stride, const void* weight, const void* bias, double eps,
+                                  void* y, float* stats, void* stream);
+
+/* Gradients of a layer norm from its stats.  With h = (x - mean) * rstd and
+ * g = grad_y * weight:  grad_x = rstd (g - mean(g) - h mean(g h)) per row,
+ * grad_weight = sum over rows of grad_y * h, grad_bias = sum over rows of grad_y.
+ *   grad_x [rows, cols], grad_weight [cols], grad_bias [cols] of dtype, each or NULL.
+ *   workspace  vqc_layer_norm_workspace_bytes(rows, cols) bytes, 256-byte
+ *              aligned (not read before it is written); NULL where grad_weight
+ *              and grad_bias are NULL.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA. */
+size_t vqc_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, const void* grad_y,
+                                   int64_t grad_y_stride, const void* x, int64_t x_stride,
+                                   const void* weight, const float* stats, void* grad_x,
+                                   void* grad_weight, void* grad_bias, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* y = act(z) + residual, z = x weight^T + bias.
+ *   x         [rows, in], weight [out, in], bias [out] or NULL, of dtype.
+ *   out_dtype the type of y and residual: dtype; VQC_F32 from a 16-bit dtype (e.g.
+ *             the angles of a circuit); or a 16-bit type from VQC_F32 (e.g. a
+ *             circuit's expectations into a 16-bit residual stream).
+ *   residual  [rows, out] or NULL.
+ *   y         [rows, out].
+ *   saved     [rows, out] float: z, for the backward; or NULL.
+ *   workspace vqc_linear_workspace_bytes(0, ...) bytes, 256-byte aligned (not
+ *             read before it is written).
+ * 16-bit operands are multiplied on the tensor cores, sums in float; VQC_F32
+ * operands in float.  Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE,
+ * VQC_ERR_CUDA. */
+vqc_status vqc_linear_forward(vqc_real dtype, vqc_real out_dtype, int64_t rows, int64_t in, int64_t out,
+                              const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
+                              const void* bias, vqc_activation act, const void* residual,
+                              int64_t residual_stride, void* y, float* saved, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Gradients of vqc_linear_forward.  dz = grad_y * act'(z), rounded to dtype
+ * where that is a 16-bit type (the operand of the two products below);
+ * grad_x = dz weight, grad_weight = dz^T x, grad_bias = sum over rows of dz (summed
+ * before the rounding).  The residual's gradient is grad_y.
+ *   grad_y    [rows, out] of out_dtype.
+ *   saved     z of the forward (may be NULL for VQC_ACT_NONE).
+ *   grad_x [rows, in], grad_weight [out, in], grad_bias [out] of dtype, each or NULL.
+ *   workspace vqc_linear_workspace_bytes(1, ...) bytes, 256-byte aligned.
+ * Errors as vqc_linear_forward. */
+vqc_status vqc_linear_backward(vqc_real dtype, vqc_real out_dtype, int64_t rows, int64_t in, int64_t out,
+                               const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride,
+                               const void* weight, int64_t weight_stride, const float* saved,
+                               vqc_activation act, void* grad_x, void* grad_weight, void* grad_bias,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gated product of a feed-forward block, both projections in one kernel:
+ * h = act(g) * u, g = x weight_gate^T + bias_gate, u = x weight_up^T + bias_up.
+ *   x [rows, in]; weight_gate, weight_up [out, in] with one stride; bias_gate,
+ *   bias_up [out] or NULL; h [rows, out]; all of dtype.
+ *   saved     [2, rows, out] float: g and u, for the backward; or NULL.
+ *   workspace vqc_gated_workspace_bytes(0, ...) bytes.
+ * Errors as vqc_linear_forward. */
+vqc_status vqc_gated_forward(vqc_real dtype, int64_t rows, int64_t in, int64_t out, const void* x,
+                             int64_t x_stride, const void* weight_gate, const void* weight_up,
+                             int64_t weight_stride, const void* bias_gate, const void* bias_up,
+                             vqc_activation act, void* h, float* saved, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Gradients of vqc_gated_forward: dg = grad_h u act'(g), du = grad_h act(g), rounded
+ * to dtype as operands; grad_x = dg weight_gate + du weight_up, grad_weight_gate = dg^T x,
+ * grad_weight_up = du^T x, grad_bias_gate and grad_bias_up the sums of dg and du over
+ * the rows.  Each gradient or NULL; the two weight gradients both or neither, and
+ * the two bias gradients both or neither.  workspace:
+ * vqc_gated_workspace_bytes(1, ...) bytes.  Errors as vqc_linear_forward. */
+vqc_status vqc_gated_backward(vqc_real dtype, int64_t rows, int64_t in, int64_t out, const void* grad_h,
+                              int64_t grad_h_stride, const void* x, int64_t x_stride,
+                              const void* weight_gate, const void* weight_up, int64_t weight_stride,
+                              const float* saved, vqc_activation act, void* grad_x,
+                              void* grad_weight_gate, void* grad_weight_up, void* grad_bias_gate,
+                              void* grad_bias_up, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace: mode 0 forward, 1 backward (the three gradients).
+ * `aligned` is 1 where x, the weights and the incoming gradient lie on 16-byte
+ * boundaries, else 0.  (size_t)-1 for arguments that the call would refuse. */
+size_t vqc_linear_workspace_bytes(int32_t mode, vqc_real dtype, vqc_real out_dtype, int64_t rows,
+                                  int64_t in, int64_t out, int64_t x_stride, int64_t weight_stride,
+                                  int64_t grad_y_stride, vqc_activation act, int32_t aligned);
+size_t vqc_gated_workspace_bytes(int32_t mode, vqc_real dtype, int64_t rows, int64_t in, int64_t out,
+                                 int64_t x_stride, int64_t weight_stride, int32_t aligned);
+
 /* Synchronise `stream` and report any CUDA error, then read (and clear) the
  * error word of every plan of this process on the current device: each kernel
  * checks its launch geometry against the plan before touching memory and, on

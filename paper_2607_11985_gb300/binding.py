@@ -21,6 +21,8 @@ NUM_ANGLES = {"RX": 1, "RY": 1, "RZ": 1, "CRZ": 1, "RZZ": 1, "U3": 3}
 PKIND = {"c": 1, "x": 2, "w": 3}
 
 VQC_C64, VQC_C128, VQC_C128_DF = 0, 1, 2
+VQC_F32, VQC_BF16, VQC_F16 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 STATUS = {0: "VQC_OK", 1: "VQC_ERR_INVALID_ARG", 2: "VQC_ERR_UNSUPPORTED_GATE",
           3: "VQC_ERR_QUBIT_RANGE", 4: "VQC_ERR_TOO_MANY_QUBITS", 5: "VQC_ERR_PARAM_RANGE",
           6: "VQC_ERR_OUT_OF_MEMORY", 7: "VQC_ERR_CUDA", 8: "VQC_ERR_WORKSPACE",
@@ -60,7 +62,7 @@ class VQCError(RuntimeError):
 _lib = None
 
 # C entry points and their signatures: (name, restype, argtypes)
-_P, _I, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_P, _I, _S, _L, _D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64, ctypes.c_double
 SIGNATURES = [
     ("vqc_compile", _I, [ctypes.POINTER(vqc_gate), _I, _I, _I, _I, _I, ctypes.POINTER(_P)]),
     ("vqc_free", None, [_P]),
@@ -84,6 +86,16 @@ SIGNATURES = [
     ("vqc_host_direct", _I, [_I]),
     ("vqc_fma_peak", _I, [_I, ctypes.POINTER(ctypes.c_double)]),
     ("vqc_forward_backward", _I, [_P, _I, _P, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
+    ("vqc_layer_norm_forward", _I, [_I, _L, _L, _P, _L, _P, _P, _D, _P, _P, _P]),
+    ("vqc_layer_norm_workspace_bytes", _S, [_L, _L]),
+    ("vqc_layer_norm_backward", _I, [_I, _L, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _P, _S, _P]),
+    ("vqc_linear_forward", _I, [_I, _I, _L, _L, _L, _P, _L, _P, _L, _P, _I, _P, _L, _P, _P, _P, _S, _P]),
+    ("vqc_linear_backward", _I, [_I, _I, _L, _L, _L, _P, _L, _P, _L, _P, _L, _P, _I, _P, _P, _P, _P, _S, _P]),
+    ("vqc_linear_workspace_bytes", _S, [_I, _I, _I, _L, _L, _L, _L, _L, _L, _I, _I]),
+    ("vqc_gated_forward", _I, [_I, _L, _L, _L, _P, _L, _P, _P, _L, _P, _P, _I, _P, _P, _P, _S, _P]),
+    ("vqc_gated_backward", _I, [_I, _L, _L, _L, _P, _L, _P, _L, _P, _P, _L, _P, _I, _P, _P, _P, _P, _P, _P,
+                                _S, _P]),
+    ("vqc_gated_workspace_bytes", _S, [_I, _I, _L, _L, _L, _L, _L, _I]),
 ]
 
 
@@ -215,6 +227,57 @@ def vqc_fma_peak(dtype):
     out = ctypes.c_double(0.0)
     _check(lib().vqc_fma_peak(dtype, ctypes.byref(out)))
     return out.value
+
+
+def vqc_layer_norm_forward(dtype, rows, cols, x, x_stride, weight, bias, eps, y, stats, stream):
+    _check(lib().vqc_layer_norm_forward(dtype, rows, cols, x, x_stride, weight, bias, eps, y, stats, stream))
+
+
+def vqc_layer_norm_workspace_bytes(rows, cols):
+    return lib().vqc_layer_norm_workspace_bytes(rows, cols)
+
+
+def vqc_layer_norm_backward(dtype, rows, cols, grad_y, grad_y_stride, x, x_stride, weight, stats, grad_x,
+                            grad_weight, grad_bias, workspace, workspace_bytes, stream):
+    _check(lib().vqc_layer_norm_backward(dtype, rows, cols, grad_y, grad_y_stride, x, x_stride, weight, stats,
+                                         grad_x, grad_weight, grad_bias, workspace, workspace_bytes, stream))
+
+
+def vqc_linear_forward(dtype, out_dtype, rows, in_, out, x, x_stride, weight, weight_stride, bias, act, residual,
+                       residual_stride, y, saved, workspace, workspace_bytes, stream):
+    _check(lib().vqc_linear_forward(dtype, out_dtype, rows, in_, out, x, x_stride, weight, weight_stride, bias, act,
+                                    residual, residual_stride, y, saved, workspace, workspace_bytes, stream))
+
+
+def vqc_linear_backward(dtype, out_dtype, rows, in_, out, grad_y, grad_y_stride, x, x_stride, weight, weight_stride,
+                        saved, act, grad_x, grad_weight, grad_bias, workspace, workspace_bytes, stream):
+    _check(lib().vqc_linear_backward(dtype, out_dtype, rows, in_, out, grad_y, grad_y_stride, x, x_stride, weight,
+                                     weight_stride, saved, act, grad_x, grad_weight, grad_bias, workspace,
+                                     workspace_bytes, stream))
+
+
+def vqc_linear_workspace_bytes(mode, dtype, out_dtype, rows, in_, out, x_stride, weight_stride, grad_y_stride, act,
+                               aligned):
+    return lib().vqc_linear_workspace_bytes(mode, dtype, out_dtype, rows, in_, out, x_stride, weight_stride,
+                                            grad_y_stride, act, aligned)
+
+
+def vqc_gated_forward(dtype, rows, in_, out, x, x_stride, weight_gate, weight_up, weight_stride, bias_gate, bias_up,
+                      act, h, saved, workspace, workspace_bytes, stream):
+    _check(lib().vqc_gated_forward(dtype, rows, in_, out, x, x_stride, weight_gate, weight_up, weight_stride,
+                                   bias_gate, bias_up, act, h, saved, workspace, workspace_bytes, stream))
+
+
+def vqc_gated_backward(dtype, rows, in_, out, grad_h, grad_h_stride, x, x_stride, weight_gate, weight_up,
+                       weight_stride, saved, act, grad_x, grad_weight_gate, grad_weight_up, grad_bias_gate,
+                       grad_bias_up, workspace, workspace_bytes, stream):
+    _check(lib().vqc_gated_backward(dtype, rows, in_, out, grad_h, grad_h_stride, x, x_stride, weight_gate,
+                                    weight_up, weight_stride, saved, act, grad_x, grad_weight_gate, grad_weight_up,
+                                    grad_bias_gate, grad_bias_up, workspace, workspace_bytes, stream))
+
+
+def vqc_gated_workspace_bytes(mode, dtype, rows, in_, out, x_stride, weight_stride, aligned):
+    return lib().vqc_gated_workspace_bytes(mode, dtype, rows, in_, out, x_stride, weight_stride, aligned)
 
 
 def vqc_plan_info(plan, batch):

@@ -1,0 +1,81 @@
+// layers.h -- the classical operators around a circuit (layer norm, linear,
+// gated product): what their translation units share on the host.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+
+#include "vqc.h"
+
+namespace vqc {
+
+vqc_status set_error(vqc_status s, const std::string& msg);
+
+namespace layers {
+
+inline size_t elem_size(int dtype) { return dtype == VQC_F32 ? 4 : 2; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+vqc_status cuda_error(cudaError_t e, const char* what);
+int sm_count();   // of the current device (the GB300's 152 where there is none)
+
+// A matrix operand of a product: element (i, k) of the outer index i and the
+// contracted index k is p[i * ld + k], or p[k * ld + i] where k_outer is set.
+struct Operand {
+    const void* p;
+    int64_t ld;
+    bool k_outer;
+};
+
+enum Form {
+    PLAIN = 0,   // y0 = finish(a0 b0^T)
+    SUM = 1,     // y0 = finish(a0 b0^T + a1 b1^T)
+    PAIR = 2,    // y0 = a0 b0^T and y1 = a1 b1^T in one launch
+    GATED = 3    // y0 = act(a0 b0^T + bias0) * (a0 b1^T + bias1)
+};
+
+// What is done with the sums of a product before they are written.
+struct Finish {
+    const void* bias[2];   // per column, of the operands' type, or NULL
+    const void* res;       // added last, of y's type, or NULL
+    int64_t ld_res;
+    void* y[2];            // dense [m, n]
+    float* z[2];           // sums with their bias, dense [m, n], or NULL
+    int64_t m, n;
+    int32_t act, dtype, out_dtype, gated;
+};
+
+// m x n outputs, contraction over k; every matrix of one form has the same sizes.
+struct Product {
+    int form;
+    int64_t m, n, k;
+    Operand a[2], b[2];
+    Finish f;
+};
+
+// Bytes of workspace of a product.  `aligned`: the operands' addresses are
+// multiples of 16 bytes (their strides are looked at).
+size_t product_workspace(const Product& p, bool aligned);
+vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s);
+
+// dz = grad_y * act'(z) (gated: dg and du from grad_h, g and u) and the column sums.
+struct ActGrad {
+    const void* gy;          // [rows, n] of gy_dtype, rows ld_gy apart
+    int64_t ld_gy;
+    const float* z[2];       // dense [rows, n]; z[0] may be NULL without an activation
+    void* dz[2];             // of dtype, rows ld_dz apart, or NULL
+    int64_t ld_dz;
+    void* sum[2];            // [n] of dtype: column sums, or NULL
+    int64_t rows, n;
+    int32_t act, dtype, gy_dtype, gated;
+};
+size_t act_grad_workspace(int64_t rows, int64_t n, bool gated);
+vqc_status act_grad_run(const ActGrad& a, void* ws, size_t ws_bytes, cudaStream_t s);
+
+}  // namespace layers
+}  // namespace vqc

@@ -1,0 +1,84 @@
+// layers_elem.cuh -- element types, activations and the end of a product
+// (bias, activation, gate, residual, rounding), shared by the layer kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "layers.h"
+
+namespace vqc {
+namespace layers {
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half(v); }
+
+// element i of an array whose type is known at run time (one uniform branch)
+__device__ __forceinline__ float load_as(const void* p, int dtype, int64_t i) {
+    if (dtype == VQC_F32) return static_cast<const float*>(p)[i];
+    if (dtype == VQC_BF16) return to_f(static_cast<const __nv_bfloat16*>(p)[i]);
+    return to_f(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, int dtype, int64_t i, float v) {
+    if (dtype == VQC_F32) static_cast<float*>(p)[i] = v;
+    else if (dtype == VQC_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16(v);
+    else static_cast<__half*>(p)[i] = __float2half(v);
+}
+
+// act(z) in float.  A NaN stays one.
+__device__ __forceinline__ float act_value(int act, float z) {
+    switch (act) {
+        case VQC_ACT_RELU: return z < 0.f ? 0.f : z;
+        case VQC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case VQC_ACT_SILU: return z / (1.f + expf(-z));
+        case VQC_ACT_TANH: return tanhf(z);
+        case VQC_ACT_SIGMOID: return 1.f / (1.f + expf(-z));
+        default: return z;
+    }
+}
+
+// act(z) and act'(z)
+__device__ __forceinline__ float2 act_both(int act, float z) {
+    switch (act) {
+        case VQC_ACT_RELU: return z < 0.f ? make_float2(0.f, 0.f) : make_float2(z, z == 0.f ? 0.f : 1.f);
+        case VQC_ACT_GELU: {
+            const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+            return make_float2(z * p, p + z * (0.39894228040143268f * expf(-0.5f * z * z)));
+        }
+        case VQC_ACT_SILU: {
+            const float p = 1.f / (1.f + expf(-z));
+            return make_float2(z * p, p * (1.f + z * (1.f - p)));
+        }
+        case VQC_ACT_TANH: {
+            const float a = tanhf(z);
+            return make_float2(a, 1.f - a * a);
+        }
+        case VQC_ACT_SIGMOID: {
+            const float p = 1.f / (1.f + expf(-z));
+            return make_float2(p, p * (1.f - p));
+        }
+        default: return make_float2(z, 1.f);
+    }
+}
+
+// The end of a product for one element: v0 (and v1, gated) are its sums.
+__device__ __forceinline__ void finish_one(const Finish& f, int which, int64_t row, int64_t col, float v0, float v1) {
+    if (f.bias[which]) v0 += load_as(f.bias[which], f.dtype, col);
+    if (f.gated && f.bias[1]) v1 += load_as(f.bias[1], f.dtype, col);
+    const int64_t at = row * f.n + col;
+    if (f.z[which]) f.z[which][at] = v0;
+    if (f.gated && f.z[1]) f.z[1][at] = v1;
+    float r = act_value(f.act, v0);
+    if (f.gated) r *= v1;
+    if (f.res) r += load_as(f.res, f.out_dtype, row * f.ld_res + col);
+    store_as(f.y[which], f.out_dtype, at, r);
+}
+
+}  // namespace layers
+}  // namespace vqc
