@@ -1512,6 +1512,9 @@ vqc_status set_error(vqc_status s, const std::string& msg) { return fail(s, msg)
 // tc_stage.cu: the error word of vqc_stage_apply's kernels (read and cleared).
 vqc_status stage_error_check();
 
+// layers_tc.cu: the error word of the tensor-core products (read and cleared).
+vqc_status layers_error_check();
+
 // host_eval.cu: the per-plan arena of vqc_evaluate_host.
 void release_host_arena(const vqc_plan* plan);
 
@@ -2092,7 +2095,8 @@ vqc_status vqc_sync_check(void* stream) {
                         ((tripped & 1u) ? " resident sweep geometry" : "") +
                         ((tripped & 2u) ? " HBM pass geometry" : "") +
                         ((tripped & 4u) ? " cluster geometry" : "") + " (the work was skipped)");
-    return stage_error_check();   // vqc_stage_apply's tensor-core waits
+    const vqc_status st = stage_error_check();   // vqc_stage_apply's tensor-core waits
+    return st == VQC_OK ? layers_error_check() : st;   // those of the products
 }
 
 vqc_status vqc_frames_export(const vqc_plan* plan, void* buf, size_t* inout_bytes) {

@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "layers_elem.cuh"
+#include "layers_tc.h"
 
 namespace vqc {
 namespace layers {
@@ -184,13 +185,14 @@ vqc_status join_run(const Product& p, const float* part, int splits, cudaStream_
 }
 
 size_t product_workspace(const Product& p, bool aligned) {
-    (void)aligned;
     if (p.m == 0 || p.k == 0) return 0;
+    if (tc_takes(p)) return tc_workspace(p, aligned);
     return part_bytes(p, pick_splits(p, pick_tile(p)));
 }
 
 vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
     if (p.m == 0 || p.n == 0) return VQC_OK;
+    if (tc_takes(p)) return tc_run(p, ws, ws_bytes, s);
     const Tile t = pick_tile(p);
     ProductArgs a{};
     for (int i = 0; i < 2; ++i) { a.a[i] = p.a[i]; a.b[i] = p.b[i]; }

@@ -1,0 +1,21 @@
+// layers_tc.h -- products on the tensor cores and the join of cut products.
+#pragma once
+
+#include "layers.h"
+
+namespace vqc {
+namespace layers {
+
+bool tc_takes(const Product& p);
+size_t tc_workspace(const Product& p, bool aligned);
+vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s);
+
+// Sums of a contraction that was cut, [splits][one or two products][m][n], joined
+// in the order of the cuts and finished.
+vqc_status join_run(const Product& p, const float* part, int splits, cudaStream_t s);
+
+}  // namespace layers
+
+vqc_status layers_error_check();
+
+}  // namespace vqc
