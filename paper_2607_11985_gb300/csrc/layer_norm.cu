@@ -1,7 +1,14 @@
 // layer_norm.cu -- layer norm over the columns of each row, forward and backward.
 //
-// Statistics in float: the mean first, then the sum of squared differences from
-// it, so that rows with a large mean lose nothing.
+// A row stays in registers between its statistics and its result: x is read
+// once (forward), x and grad_y once (backward), each result written once, which
+// is all that bounds these kernels.  Statistics in float: the mean first, then
+// the sum of squared differences from it, so that rows with a large mean lose
+// nothing.  The backward's column sums (gradients of weight and bias) stay in
+// registers over all rows of a CTA: a thread owns the same columns of every
+// row; the CTAs' sums are joined by sum_run in a fixed order.
+//
+// Rows longer than the registers hold take kernels that read their row again.
 #include <algorithm>
 
 #include "layers_elem.cuh"
@@ -9,11 +16,7 @@
 namespace vqc {
 namespace layers {
 
-vqc_status sum_run(const float* part, int64_t count, int64_t n, void* out0, void* out1, int dtype, cudaStream_t s);
-
 namespace {
-
-constexpr int kNormThreads = 256;
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -21,16 +24,22 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// sum over the CTA, the same value in every thread
-__device__ __forceinline__ float cta_sum(float v, float* buf) {
-    v = warp_sum(v);
+// Sums of s and t over the WARPS warps of a row, the same value in every thread.  `buf`
+// is one of two buffers used in turn, so that one barrier per sum is enough.
+template <int WARPS> __device__ __forceinline__ float2 row_sum(float s, float t, float2* buf) {
+    s = warp_sum(s);
+    t = warp_sum(t);
+    if (WARPS == 1) return make_float2(s, t);
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float2(s, t);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
+    s = t = 0.f;
 #pragma unroll
-    for (int i = 0; i < kNormThreads / 32; ++i) v += buf[i];
-    return v;
+    for (int i = 0; i < WARPS; ++i) {
+        const float2 p = buf[i];
+        s += p.x;
+        t += p.y;
+    }
+    return make_float2(s, t);
 }
 
 struct NormArgs {
@@ -38,30 +47,195 @@ struct NormArgs {
     void *y, *gx;
     const float* stats_in;
     float* stats;
-    float* part;         // [2][CTAs][cols] column sums of the backward
+    float* part;         // [2][CTAs][cols] column sums of the backward, or NULL
     int64_t rows, cols, ld_x, ld_gy;
     float eps;
 };
 
-template <typename T> __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid_constant__ NormArgs A) {
-    __shared__ float buf[kNormThreads / 32];
+// VEC neighbouring elements, read at once
+template <typename T, int VEC> struct Pack {
+    T e[VEC];
+};
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_pack(const T* p) {
+    Pack<T, VEC> r;
+    if constexpr (VEC * sizeof(T) == 16) *reinterpret_cast<uint4*>(r.e) = *reinterpret_cast<const uint4*>(p);
+    else r.e[0] = *p;
+    return r;
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* p, const Pack<T, VEC>& v) {
+    if constexpr (VEC * sizeof(T) == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v.e);
+    else *p = v.e[0];
+}
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> fill_pack(float f) {
+    Pack<T, VEC> r;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) r.e[e] = from_f<T>(f);
+    return r;
+}
+
+// WARPS warps per row, NV packs of VEC elements per thread: pack i of thread t holds the
+// columns (i * threads + t) * VEC + [0, VEC).  With one warp per row a CTA has 8 rows.
+template <typename T, int VEC, int WARPS> struct Row {
+    static constexpr int kThreads = WARPS * 32, kCta = WARPS == 1 ? 256 : kThreads;
+    static __device__ __forceinline__ int64_t column(int i) {
+        return ((int64_t)i * kThreads + (WARPS == 1 ? threadIdx.x & 31 : threadIdx.x)) * VEC;
+    }
+    static __device__ __forceinline__ int64_t first() { return WARPS == 1 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : blockIdx.x; }
+    static __device__ __forceinline__ int64_t step() { return WARPS == 1 ? gridDim.x * 8ll : gridDim.x; }
+};
+
+template <typename T, int VEC, int WARPS, int NV>
+__global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_forward_kernel(const __grid_constant__ NormArgs A) {
+    using R = Row<T, VEC, WARPS>;
+    __shared__ float2 buf[2][WARPS];
+    const float inv = 1.f / (float)A.cols;
+    for (int64_t r = R::first(); r < A.rows; r += R::step()) {
+        const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
+        Pack<T, VEC> v[NV];
+        float s = 0.f, q = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = fill_pack<T, VEC>(0.f);
+            if (R::column(i) < A.cols) v[i] = load_pack<T, VEC>(x + R::column(i));
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += to_f(v[i].e[e]);
+        const float mean = row_sum<WARPS>(s, 0.f, buf[0]).x * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (R::column(i) < A.cols)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = to_f(v[i].e[e]) - mean;
+                    q = fmaf(d, d, q);
+                }
+        const float rstd = 1.f / sqrtf(row_sum<WARPS>(q, 0.f, buf[1]).x * inv + A.eps);
+        if (A.stats && R::column(0) == 0) *reinterpret_cast<float2*>(A.stats + 2 * r) = make_float2(mean, rstd);
+        T* y = static_cast<T*>(A.y) + r * A.cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t c = R::column(i);
+            if (c >= A.cols) continue;
+            Pack<T, VEC> w = fill_pack<T, VEC>(1.f), b = fill_pack<T, VEC>(0.f), o;
+            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + c);
+            if (A.bias) b = load_pack<T, VEC>(static_cast<const T*>(A.bias) + c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o.e[e] = from_f<T>(fmaf((to_f(v[i].e[e]) - mean) * rstd, to_f(w.e[e]), to_f(b.e[e])));
+            store_pack<T, VEC>(y + c, o);
+        }
+    }
+}
+
+template <typename T, int VEC, int WARPS, int NV>
+__global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
+    using R = Row<T, VEC, WARPS>;
+    __shared__ float2 buf[2][WARPS];
+    const float inv = 1.f / (float)A.cols;
+    float gw[NV][VEC], gb[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) gw[i][e] = gb[i][e] = 0.f;
+    int turn = 0;
+    for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
+        const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
+        const T* gy = static_cast<const T*>(A.gy) + r * A.ld_gy;
+        const float2 st = *reinterpret_cast<const float2*>(A.stats_in + 2 * r);
+        Pack<T, VEC> v[NV], g[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = g[i] = fill_pack<T, VEC>(0.f);
+            if (R::column(i) < A.cols) {
+                v[i] = load_pack<T, VEC>(x + R::column(i));
+                g[i] = load_pack<T, VEC>(gy + R::column(i));
+            }
+        }
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (R::column(i) >= A.cols) continue;
+            Pack<T, VEC> w = fill_pack<T, VEC>(1.f);
+            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + R::column(i));
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float h = (to_f(v[i].e[e]) - st.x) * st.y, d = to_f(g[i].e[e]);
+                gw[i][e] = fmaf(d, h, gw[i][e]);
+                gb[i][e] += d;
+                const float k = d * to_f(w.e[e]);
+                s += k;
+                t = fmaf(k, h, t);
+            }
+        }
+        if (!A.gx) continue;
+        const float2 sum = row_sum<WARPS>(s, t, buf[turn]);
+        const float ms = sum.x * inv, mt = sum.y * inv;
+        T* gx = static_cast<T*>(A.gx) + r * A.cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t c = R::column(i);
+            if (c >= A.cols) continue;
+            Pack<T, VEC> w = fill_pack<T, VEC>(1.f), o;
+            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float h = (to_f(v[i].e[e]) - st.x) * st.y;
+                o.e[e] = from_f<T>(st.y * (to_f(g[i].e[e]) * to_f(w.e[e]) - ms - h * mt));
+            }
+            store_pack<T, VEC>(gx + c, o);
+        }
+    }
+    if (!A.part) return;
+    if constexpr (WARPS == 1) {   // the CTA's 8 rows' sums in the order of the warps
+        __shared__ float sums[8][NV * VEC * 32];
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sums[threadIdx.x >> 5][R::column(i) + e] = which ? gb[i][e] : gw[i][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < A.cols; c += 256) {
+                float a = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a += sums[i][c];
+                A.part[((int64_t)which * gridDim.x + blockIdx.x) * A.cols + c] = a;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (R::column(i) < A.cols) {
+                    A.part[(int64_t)blockIdx.x * A.cols + R::column(i) + e] = gw[i][e];
+                    A.part[((int64_t)gridDim.x + blockIdx.x) * A.cols + R::column(i) + e] = gb[i][e];
+                }
+    }
+}
+
+// ------------------------------------------------------------ rows beyond the registers
+
+constexpr int kLong = 512;
+
+template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long(const __grid_constant__ NormArgs A) {
+    __shared__ float2 buf[2][kLong / 32];
     for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
         float s = 0.f;
-        for (int64_t c = threadIdx.x; c < A.cols; c += kNormThreads) s += to_f(x[c]);
-        const float mean = cta_sum(s, buf) / (float)A.cols;
+        for (int64_t c = threadIdx.x; c < A.cols; c += kLong) s += to_f(x[c]);
+        const float mean = row_sum<kLong / 32>(s, 0.f, buf[0]).x / (float)A.cols;
         s = 0.f;
-        for (int64_t c = threadIdx.x; c < A.cols; c += kNormThreads) {
+        for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
             const float d = to_f(x[c]) - mean;
             s = fmaf(d, d, s);
         }
-        const float rstd = 1.f / sqrtf(cta_sum(s, buf) / (float)A.cols + A.eps);
-        if (A.stats && threadIdx.x == 0) {
-            A.stats[2 * r] = mean;
-            A.stats[2 * r + 1] = rstd;
-        }
+        const float rstd = 1.f / sqrtf(row_sum<kLong / 32>(s, 0.f, buf[1]).x / (float)A.cols + A.eps);
+        if (A.stats && threadIdx.x == 0) *reinterpret_cast<float2*>(A.stats + 2 * r) = make_float2(mean, rstd);
         T* y = static_cast<T*>(A.y) + r * A.cols;
-        for (int64_t c = threadIdx.x; c < A.cols; c += kNormThreads) {
+        for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
             const float w = A.weight ? to_f(static_cast<const T*>(A.weight)[c]) : 1.f;
             const float b = A.bias ? to_f(static_cast<const T*>(A.bias)[c]) : 0.f;
             y[c] = from_f<T>(fmaf((to_f(x[c]) - mean) * rstd, w, b));
@@ -69,36 +243,38 @@ template <typename T> __global__ void __launch_bounds__(kNormThreads) norm_forwa
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const __grid_constant__ NormArgs A) {
-    __shared__ float buf[kNormThreads / 32];
-    for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_long(const __grid_constant__ NormArgs A) {
+    __shared__ float2 buf[2][kLong / 32];
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x, turn ^= 1) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
         const T* gy = static_cast<const T*>(A.gy) + r * A.ld_gy;
         const float mean = A.stats_in[2 * r], rstd = A.stats_in[2 * r + 1];
         float s = 0.f, t = 0.f;
-        for (int64_t c = threadIdx.x; c < A.cols; c += kNormThreads) {
+        for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
             const float g = to_f(gy[c]) * (A.weight ? to_f(static_cast<const T*>(A.weight)[c]) : 1.f);
             s += g;
             t = fmaf(g, (to_f(x[c]) - mean) * rstd, t);
         }
-        s = cta_sum(s, buf) / (float)A.cols;
-        t = cta_sum(t, buf) / (float)A.cols;
-        if (!A.gx) continue;
+        const float2 sum = row_sum<kLong / 32>(s, t, buf[turn]);
+        s = sum.x / (float)A.cols;
+        t = sum.y / (float)A.cols;
         T* gx = static_cast<T*>(A.gx) + r * A.cols;
-        for (int64_t c = threadIdx.x; c < A.cols; c += kNormThreads) {
+        for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
             const float g = to_f(gy[c]) * (A.weight ? to_f(static_cast<const T*>(A.weight)[c]) : 1.f);
             gx[c] = from_f<T>(rstd * (g - s - (to_f(x[c]) - mean) * rstd * t));
         }
     }
 }
 
-// Column sums over the rows of one CTA: thread = column.
-template <typename T> __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const __grid_constant__ NormArgs A, int64_t per) {
-    const int64_t across = (A.cols + kNormThreads - 1) / kNormThreads, block = blockIdx.x / across, blocks = gridDim.x / across;
-    const int64_t c = blockIdx.x % across * kNormThreads + threadIdx.x;
+// Column sums over `per` rows: thread = column.
+template <typename T> __global__ void __launch_bounds__(256) norm_columns_long(const __grid_constant__ NormArgs A, int64_t per) {
+    const int64_t across = (A.cols + 255) / 256, block = blockIdx.x / across, blocks = gridDim.x / across;
+    const int64_t c = blockIdx.x % across * 256 + threadIdx.x;
     if (c >= A.cols) return;
     float s = 0.f, t = 0.f;
     const int64_t r1 = min(A.rows, (block + 1) * per);
+#pragma unroll 4
     for (int64_t r = block * per; r < r1; ++r) {
         const float g = to_f(static_cast<const T*>(A.gy)[r * A.ld_gy + c]);
         s = fmaf(g, (to_f(static_cast<const T*>(A.x)[r * A.ld_x + c]) - A.stats_in[2 * r]) * A.stats_in[2 * r + 1], s);
@@ -108,20 +284,80 @@ template <typename T> __global__ void __launch_bounds__(kNormThreads) norm_colum
     A.part[(blocks + block) * A.cols + c] = t;
 }
 
-template <typename T> cudaError_t launch(int which, NormArgs a, int grid, int64_t per, cudaStream_t s) {
-    void* args[] = {&a, &per};
-    const void* fn = which == 0 ? (const void*)norm_forward_kernel<T>
-                     : which == 1 ? (const void*)norm_backward_kernel<T> : (const void*)norm_columns_kernel<T>;
-    return cudaLaunchKernel(fn, dim3(grid), dim3(kNormThreads), args, 0, s);
-}
-cudaError_t launch_as(int dtype, int which, const NormArgs& a, int64_t grid, int64_t per, cudaStream_t s) {
-    if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return dtype == VQC_F32    ? launch<float>(which, a, (int)grid, per, s)
-           : dtype == VQC_BF16 ? launch<__nv_bfloat16>(which, a, (int)grid, per, s)
-                               : launch<__half>(which, a, (int)grid, per, s);
+// ------------------------------------------------------------ choice and launch
+
+// Threads per row so that a thread holds 8 or 16 elements (backward; as many sums
+// twice) and up to 32 (forward); rows beyond 16 warps of these are `long`.
+constexpr int64_t kMostForward = 16384, kMostBackward = 8192;
+
+int64_t row_ctas(int warps, int64_t rows, int64_t most) {
+    const int64_t n = warps == 1 ? ceil_div(rows, 8) : rows;
+    return std::max<int64_t>(1, std::min<int64_t>(n, most));
 }
 
-constexpr int64_t kNormBlocks = 64;   // blocks of rows of the column sums
+struct Plan {
+    const void* fn;
+    int warps, threads;
+};
+template <typename T, int VEC, int WARPS, int NV> Plan forward_plan() {
+    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<T, VEC, WARPS>::kCta};
+}
+template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
+    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<T, VEC, WARPS>::kCta};
+}
+// E: elements per thread and step of the ladder
+template <typename T, int VEC> Plan forward_choice(int64_t cols) {
+    constexpr int N8 = 8 / VEC, N16 = 16 / VEC, N32 = 32 / VEC;
+    if (cols <= 256) return forward_plan<T, VEC, 1, N8>();
+    if (cols <= 512) return forward_plan<T, VEC, 1, N16>();
+    if (cols <= 1024) return forward_plan<T, VEC, 1, N32>();
+    if (cols <= 2048) return forward_plan<T, VEC, 4, N16>();
+    if (cols <= 4096) return forward_plan<T, VEC, 8, N16>();
+    if (cols <= 8192) return forward_plan<T, VEC, 16, N16>();
+    return forward_plan<T, VEC, 16, N32>();
+}
+template <typename T, int VEC> Plan backward_choice(int64_t cols) {
+    constexpr int N8 = 8 / VEC, N16 = 16 / VEC;
+    if (cols <= 256) return backward_plan<T, VEC, 1, N8>();
+    if (cols <= 512) return backward_plan<T, VEC, 2, N8>();
+    if (cols <= 1024) return backward_plan<T, VEC, 4, N8>();
+    if (cols <= 2048) return backward_plan<T, VEC, 8, N8>();
+    if (cols <= 4096) return backward_plan<T, VEC, 8, N16>();
+    return backward_plan<T, VEC, 16, N16>();
+}
+template <typename T> Plan choose_plan(bool forward, int64_t cols, bool vec) {
+    constexpr int V = 16 / sizeof(T);
+    if (forward) return vec ? forward_choice<T, V>(cols) : forward_choice<T, 1>(cols);
+    return vec ? backward_choice<T, V>(cols) : backward_choice<T, 1>(cols);
+}
+Plan choose_plan(int dtype, bool forward, int64_t cols, bool vec) {
+    return dtype == VQC_F32    ? choose_plan<float>(forward, cols, vec)
+           : dtype == VQC_BF16 ? choose_plan<__nv_bfloat16>(forward, cols, vec)
+                               : choose_plan<__half>(forward, cols, vec);
+}
+template <typename T> const void* long_kernel(int which) {
+    return which == 0 ? (const void*)norm_forward_long<T>
+           : which == 1 ? (const void*)norm_backward_long<T> : (const void*)norm_columns_long<T>;
+}
+const void* long_kernel(int dtype, int which) {
+    return dtype == VQC_F32 ? long_kernel<float>(which) : dtype == VQC_BF16 ? long_kernel<__nv_bfloat16>(which) : long_kernel<__half>(which);
+}
+
+// CTAs of the backward (partial column sums of each): two per SM
+int64_t backward_ctas(int warps, int64_t rows) { return row_ctas(warps, rows, 2LL * sm_count()); }
+constexpr int64_t kLongBlocks = 64;   // blocks of rows of norm_columns_long
+
+// rows and vectors on 16-byte boundaries
+bool packs(size_t e, int64_t cols, std::initializer_list<const void*> p, std::initializer_list<int64_t> strides) {
+    if (cols * e % 16) return false;
+    for (const void* q : p)
+        if (!aligned_to(q, 16)) return false;
+    for (int64_t s : strides)
+        if (s * e % 16) return false;
+    return true;
+}
+
+vqc_status launched(cudaError_t e) { return e == cudaSuccess ? VQC_OK : cuda_error(e, "layer norm launch"); }
 
 }  // namespace
 }  // namespace layers
@@ -145,8 +381,13 @@ vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, co
         NormArgs a{};
         a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.stats = stats;
         a.rows = rows; a.cols = cols; a.ld_x = x_stride; a.eps = (float)eps;
-        const cudaError_t err = launch_as(dtype, 0, a, std::min<int64_t>(rows, 8LL * sm_count()), 0, static_cast<cudaStream_t>(stream));
-        return err == cudaSuccess ? VQC_OK : cuda_error(err, "layer norm launch");
+        void* args[] = {&a};
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        if (cols > kMostForward)
+            return launched(cudaLaunchKernel(long_kernel(dtype, 0), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())),
+                                             dim3(kLong), args, 0, s));
+        const Plan p = choose_plan(dtype, true, cols, packs(e, cols, {x, weight, bias, y}, {x_stride}));
+        return launched(cudaLaunchKernel(p.fn, dim3((unsigned)row_ctas(p.warps, rows, 0x7fffffff)), dim3(p.threads), args, 0, s));
     } catch (...) {
         return VQC_ERR_OUT_OF_MEMORY;
     }
@@ -154,7 +395,8 @@ vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, co
 
 size_t vqc_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || cols > 0x7fffffff) return (size_t)-1;
-    return align256((size_t)2 * kNormBlocks * cols * 4);
+    const int64_t blocks = cols > kMostBackward ? kLongBlocks : backward_ctas(cols <= 256 ? 1 : 2, rows);
+    return align256((size_t)2 * blocks * cols * 4);
 }
 
 vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, const void* grad_y, int64_t grad_y_stride,
@@ -167,31 +409,41 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             return set_error(VQC_ERR_INVALID_ARG, "vqc_layer_norm_backward: bad type, size, stride or NULL pointer");
         const size_t e = elem_size(dtype);
         if (!aligned_to(x, e) || !aligned_to(grad_y, e) || !aligned_to(weight, e) || !aligned_to(grad_x, 16) ||
-            !aligned_to(grad_weight, e) || !aligned_to(grad_bias, e) || !aligned_to(stats, 4) || !aligned_to(workspace, 256))
+            !aligned_to(grad_weight, e) || !aligned_to(grad_bias, e) || !aligned_to(stats, 8) || !aligned_to(workspace, 256))
             return set_error(VQC_ERR_INVALID_ARG, "vqc_layer_norm_backward: misaligned operand, output or workspace");
         const bool columns = grad_weight || grad_bias;
         if (columns && (!workspace || workspace_bytes < vqc_layer_norm_workspace_bytes(rows, cols)))
             return set_error(VQC_ERR_WORKSPACE, "vqc_layer_norm_backward: workspace too small");
+        if (!columns && (!grad_x || rows == 0)) return VQC_OK;
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         NormArgs a{};
         a.x = x; a.weight = weight; a.gy = grad_y; a.gx = grad_x; a.stats_in = stats;
         a.rows = rows; a.cols = cols; a.ld_x = x_stride; a.ld_gy = grad_y_stride;
-        a.part = static_cast<float*>(workspace);
-        if (grad_x && rows > 0) {
-            const cudaError_t err = launch_as(dtype, 1, a, std::min<int64_t>(rows, 8LL * sm_count()), 0, s);
-            if (err != cudaSuccess) return cuda_error(err, "layer norm launch");
+        a.part = columns ? static_cast<float*>(workspace) : nullptr;
+        int64_t blocks = 0;
+        if (rows > 0 && cols > kMostBackward) {
+            int64_t per = ceil_div(rows, kLongBlocks);
+            void* args[] = {&a, &per};
+            if (grad_x) {
+                const cudaError_t err = cudaLaunchKernel(long_kernel(dtype, 1), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())),
+                                                         dim3(kLong), args, 0, s);
+                if (err != cudaSuccess) return launched(err);
+            }
+            if (columns) {
+                blocks = ceil_div(rows, per);
+                const int64_t grid = blocks * ceil_div(cols, 256);
+                if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "vqc_layer_norm_backward: too many columns");
+                const cudaError_t err = cudaLaunchKernel(long_kernel(dtype, 2), dim3((unsigned)grid), dim3(256), args, 0, s);
+                if (err != cudaSuccess) return launched(err);
+            }
+        } else if (rows > 0) {
+            const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
+            blocks = columns ? backward_ctas(p.warps, rows) : row_ctas(p.warps, rows, 0x7fffffff);
+            void* args[] = {&a};
+            const cudaError_t err = cudaLaunchKernel(p.fn, dim3((unsigned)blocks), dim3(p.threads), args, 0, s);
+            if (err != cudaSuccess) return launched(err);
         }
-        if (!columns) return VQC_OK;
-        const int64_t per = ceil_div(rows, kNormBlocks), blocks = rows ? ceil_div(rows, per) : 0;
-        if (blocks) {
-            const cudaError_t err = launch_as(dtype, 2, a, blocks * ceil_div(cols, kNormThreads), per, s);
-            if (err != cudaSuccess) return cuda_error(err, "layer norm launch");
-        }
-        if (grad_weight) {
-            const vqc_status st = sum_run(a.part, blocks, cols, grad_weight, nullptr, dtype, s);
-            if (st != VQC_OK) return st;
-        }
-        return grad_bias ? sum_run(a.part + blocks * cols, blocks, cols, grad_bias, nullptr, dtype, s) : VQC_OK;
+        return columns ? sum_run(a.part, blocks, cols, grad_weight, grad_bias, dtype, s) : VQC_OK;
     } catch (...) {
         return VQC_ERR_OUT_OF_MEMORY;
     }

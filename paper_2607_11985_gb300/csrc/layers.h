@@ -77,5 +77,9 @@ struct ActGrad {
 size_t act_grad_workspace(int64_t rows, int64_t n, bool gated);
 vqc_status act_grad_run(const ActGrad& a, void* ws, size_t ws_bytes, cudaStream_t s);
 
+// out[i][c] = sum over j of part[i][j][c] for i = 0, 1 ([count][n] each), in a fixed
+// order; either output may be NULL.
+vqc_status sum_run(const float* part, int64_t count, int64_t n, void* out0, void* out1, int dtype, cudaStream_t s);
+
 }  // namespace layers
 }  // namespace vqc

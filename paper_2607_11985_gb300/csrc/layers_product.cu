@@ -215,75 +215,140 @@ vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t
 
 namespace {
 
-constexpr int kGradRows = 64;   // rows of one CTA
-
-// A CTA takes 128 columns x kGradRows rows: warp w the rows w, w + 8, ..., lane l
-// the columns l + 32 i.  Column sums are joined over the warps in shared memory
+// One pass over grad_y and the saved pre-activations, bound by their bytes.  A CTA
+// takes 256 columns x `per` rows: a thread owns 8 columns (neighbours where
+// rows lie on 16-byte boundaries, else 32 apart) of every eighth row and keeps
+// their sums in registers; these are joined over the CTA in shared memory
 // and over the CTAs by sum_kernel, both in a fixed order.
-template <typename T>
-__global__ void __launch_bounds__(256) act_grad_kernel(const __grid_constant__ ActGrad A, float* part) {
-    __shared__ float sums[2][8][128];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t across = (A.n + 127) / 128, block = blockIdx.x / across, blocks = gridDim.x / across;
-    const int64_t c0 = blockIdx.x % across * 128, r0 = block * kGradRows;
-    float s0[4] = {}, s1[4] = {};
-    for (int i = warp; i < kGradRows; i += 8) {
-        const int64_t r = r0 + i;
-        if (r >= A.rows) break;
+constexpr int kGradCols = 256;
+
+template <bool VEC> __device__ __forceinline__ void load8(const void* p, int dtype, int64_t row, int64_t c, int64_t n, float (&v)[8]) {
+    if constexpr (VEC) {
+        if (dtype == VQC_F32) {
+            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
+            const float4 a = q[0], b = q[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = c0 + lane + 32 * j;
-            if (c >= A.n) continue;
-            const float gy = load_as(A.gy, A.gy_dtype, r * A.ld_gy + c);
-            float d0, d1 = 0.f;
-            if (A.gated) {
-                const float2 v = act_both(A.act, A.z[0][r * A.n + c]);
-                d0 = gy * A.z[1][r * A.n + c] * v.y;
-                d1 = gy * v.x;
-                if (A.dz[1]) static_cast<T*>(A.dz[1])[r * A.ld_dz + c] = from_f<T>(d1);
-            } else {
-                d0 = A.act == VQC_ACT_NONE ? gy : gy * act_both(A.act, A.z[0][r * A.n + c]).y;
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = dtype == VQC_BF16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]))
+                                                   : __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
             }
-            if (A.dz[0]) static_cast<T*>(A.dz[0])[r * A.ld_dz + c] = from_f<T>(d0);
-            s0[j] += d0;
-            s1[j] += d1;
         }
-    }
-    if (!part) return;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        sums[0][warp][lane + 32 * j] = s0[j];
-        sums[1][warp][lane + 32 * j] = s1[j];
+        for (int i = 0; i < 8; ++i) v[i] = c + 32 * i < n ? load_as(p, dtype, row + c + 32 * i) : 0.f;
     }
-    __syncthreads();
-    const int c = threadIdx.x & 127, w = threadIdx.x >> 7;
-    if (c0 + c < A.n && (w == 0 || A.gated)) {
-        float v = 0.f;
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, int64_t row, int64_t c, int64_t n, const float (&v)[8]) {
+    T o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v += sums[w][i][c];
-        part[(w * blocks + block) * A.n + c0 + c] = v;
+    for (int i = 0; i < 8; ++i) o[i] = from_f<T>(v[i]);
+    T* q = static_cast<T*>(p) + row + c;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(q)[i] = reinterpret_cast<const uint4*>(o)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + 32 * i < n) q[32 * i] = o[i];
     }
 }
 
-// out[c] = sum over i of part[i][c], in the order of i: 32 columns per CTA, warp w
-// adds the rows w, w + 8, ..., then the eight sums.
-__global__ void __launch_bounds__(256) sum_kernel(const float* part, int64_t count, int64_t n, void* out0, void* out1,
-                                                  int dtype) {
-    __shared__ float sums[8][32];
+template <typename T, bool VEC, int ACT, bool GATE>
+__device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
+#pragma unroll 2
+    for (int64_t r = r0; r < r1; r += 8) {
+        float gy[8], z[8], u[8], d[8];
+        load8<VEC>(A.gy, A.gy_dtype, r * A.ld_gy, c, A.n, gy);
+        if (ACT != VQC_ACT_NONE || GATE) load8<VEC>(A.z[0], VQC_F32, r * A.n, c, A.n, z);
+        if (GATE) load8<VEC>(A.z[1], VQC_F32, r * A.n, c, A.n, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (GATE) {
+                const float2 v = act_both(ACT, z[i]);
+                d[i] = gy[i] * u[i] * v.y;
+                u[i] = gy[i] * v.x;
+                s1[i] += u[i];
+            } else {
+                d[i] = ACT == VQC_ACT_NONE ? gy[i] : gy[i] * act_both(ACT, z[i]).y;
+            }
+            s0[i] += d[i];
+        }
+        if (A.dz[0]) store8<T, VEC>(A.dz[0], r * A.ld_dz, c, A.n, d);
+        if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], r * A.ld_dz, c, A.n, u);
+    }
+}
+template <typename T, bool VEC, bool GATE>
+__device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
+    switch (A.act) {
+        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE>(A, r0, r1, c, s0, s1);
+        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE>(A, r0, r1, c, s0, s1);
+        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE>(A, r0, r1, c, s0, s1);
+        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE>(A, r0, r1, c, s0, s1);
+        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE>(A, r0, r1, c, s0, s1);
+        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE>(A, r0, r1, c, s0, s1);
+    }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
+    __shared__ float sums[8][kGradCols];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across, blocks = gridDim.x / across;
+    const int64_t c0 = blockIdx.x % across * kGradCols, c = c0 + (VEC ? 8 * lane : lane);
+    float s0[8] = {}, s1[8] = {};
+    if (c < A.n) {
+        const int64_t r0 = block * per + warp, r1 = min(A.rows, (block + 1) * per);
+        if (A.gated) act_grad_as<T, VEC, true>(A, r0, r1, c, s0, s1);
+        else act_grad_as<T, VEC, false>(A, r0, r1, c, s0, s1);
+    }
+    if (!part) return;
+    for (int w = 0; w < (A.gated ? 2 : 1); ++w) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[warp][VEC ? 8 * lane + i : lane + 32 * i] = w ? s1[i] : s0[i];
+        __syncthreads();
+        if (c0 + threadIdx.x < A.n) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += sums[i][threadIdx.x];
+            part[(w * blocks + block) * A.n + c0 + threadIdx.x] = v;
+        }
+    }
+}
+
+// 32 columns per CTA: warp w adds the rows w, w + 32, ..., then the 32 sums are added.
+__global__ void __launch_bounds__(1024) sum_kernel(const float* part, int64_t count, int64_t n, void* out0, void* out1,
+                                                   int dtype) {
+    __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    void* out = blockIdx.y ? out1 : out0;
+    if (!out) return;
     part += (int64_t)blockIdx.y * count * n;
     float v = 0.f;
     if (c < n)
-        for (int64_t i = warp; i < count; i += 8) v += part[i * n + c];
+#pragma unroll 4
+        for (int64_t i = warp; i < count; i += 32) v += part[i * n + c];
     sums[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && c < n) {
-        v = 0.f;
+    // transposed, so that a warp joins the sums of one column
+    v = sums[lane][warp];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v += sums[i][lane];
-        store_as(blockIdx.y ? out1 : out0, dtype, c, v);
-    }
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (lane == 0 && (int64_t)blockIdx.x * 32 + warp < n) store_as(out, dtype, (int64_t)blockIdx.x * 32 + warp, v);
+}
+
+// Rows of a CTA: enough CTAs for four per SM, at least 16 rows, at most 256
+int64_t grad_rows(int64_t rows, int64_t n) {
+    const int64_t want = ceil_div(rows * ceil_div(n, kGradCols), 4LL * sm_count());
+    return std::min<int64_t>(256, std::max<int64_t>(16, (want + 7) / 8 * 8));
 }
 
 }  // namespace
@@ -291,12 +356,12 @@ __global__ void __launch_bounds__(256) sum_kernel(const float* part, int64_t cou
 vqc_status sum_run(const float* part, int64_t count, int64_t n, void* out0, void* out1, int dtype, cudaStream_t s) {
     void* args[] = {&part, &count, &n, &out0, &out1, &dtype};
     const cudaError_t e = cudaLaunchKernel((const void*)sum_kernel, dim3((unsigned)ceil_div(n, 32), out1 ? 2 : 1),
-                                           dim3(256), args, 0, s);
+                                           dim3(1024), args, 0, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "sum launch");
 }
 
 size_t act_grad_workspace(int64_t rows, int64_t n, bool gated) {
-    return align256((size_t)std::max<int64_t>(1, ceil_div(rows, kGradRows)) * n * (gated ? 2 : 1) * 4);
+    return align256((size_t)std::max<int64_t>(1, ceil_div(rows, grad_rows(rows, n))) * n * (gated ? 2 : 1) * 4);
 }
 
 vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, cudaStream_t s) {
@@ -305,14 +370,16 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, cudaStream
     float* part = sums ? static_cast<float*>(ws) : nullptr;
     if (sums && (!ws || ws_bytes < act_grad_workspace(a.rows, a.n, a.gated)))
         return set_error(VQC_ERR_WORKSPACE, "column sums: workspace too small");
-    const int64_t blocks = ceil_div(a.rows, kGradRows);
-    const int64_t grid = blocks * ceil_div(a.n, 128);
+    int64_t per = grad_rows(a.rows, a.n);
+    const int64_t blocks = ceil_div(a.rows, per), grid = blocks * ceil_div(a.n, kGradCols);
     if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "too many rows times columns");
     if (grid > 0) {
-        void* args[] = {&a, &part};
-        const void* fn = a.dtype == VQC_F32    ? (const void*)act_grad_kernel<float>
-                         : a.dtype == VQC_BF16 ? (const void*)act_grad_kernel<__nv_bfloat16>
-                                               : (const void*)act_grad_kernel<__half>;
+        // whole packs of 8 elements on 16-byte boundaries (z is dense, dz the library's own)
+        const bool vec = a.n % 8 == 0 && a.ld_gy % 8 == 0 && aligned_to(a.gy, 16) && aligned_to(a.z[0], 16) && aligned_to(a.z[1], 16);
+        void* args[] = {&a, &part, &per};
+        const void* fn = a.dtype == VQC_F32 ? (vec ? (const void*)act_grad_kernel<float, true> : (const void*)act_grad_kernel<float, false>)
+                         : a.dtype == VQC_BF16 ? (vec ? (const void*)act_grad_kernel<__nv_bfloat16, true> : (const void*)act_grad_kernel<__nv_bfloat16, false>)
+                                               : (vec ? (const void*)act_grad_kernel<__half, true> : (const void*)act_grad_kernel<__half, false>);
         const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(256), args, 0, s);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
