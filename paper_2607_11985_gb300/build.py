@@ -29,7 +29,7 @@ UNITS = ["compiler.cpp", "frames.cpp", "qasm.cpp", "capi.cu", "noalloc.cu", "hos
          "kernels_dd_fwd.cu", "kernels_dd_bwd.cu", "kernels_dd_fused.cu", "kernels_dd_hbm.cu",
          "tc_stage.cu", "kernels_f32_fwd_nph.cu", "kernels_f32_bwd_nph.cu", "kernels_hbm_nph.cu",
          "kernels_f32_fused_nph.cu", "kernels_cluster_bwd.cu",
-         "layers.cu", "layers_tc.cu", "layers_product.cu", "layer_norm.cu"]
+         "layers.cu", "layers_tc.cu", "layers_rows.cu", "layers_product.cu", "layer_norm.cu"]
 
 
 def nvcc() -> str:

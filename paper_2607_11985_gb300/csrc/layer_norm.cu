@@ -24,20 +24,32 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// Sums of s and t over the WARPS warps of a row, the same value in every thread.  `buf`
-// is one of two buffers used in turn, so that one barrier per sum is enough.
+// Sums over the WARPS warps of a row, the same value in every thread: over the lanes, then
+// (through `buf`) over the warps by every warp for itself.  Two buffers are used in
+// turn, so that one barrier per sum is enough.
+template <int WARPS> __device__ __forceinline__ float row_sum(float s, float* buf) {
+    s = warp_sum(s);
+    if (WARPS == 1) return s;
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = buf[threadIdx.x & (WARPS - 1)];
+#pragma unroll
+    for (int o = WARPS / 2; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+    return s;
+}
 template <int WARPS> __device__ __forceinline__ float2 row_sum(float s, float t, float2* buf) {
     s = warp_sum(s);
     t = warp_sum(t);
     if (WARPS == 1) return make_float2(s, t);
     if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float2(s, t);
     __syncthreads();
-    s = t = 0.f;
+    const float2 p = buf[threadIdx.x & (WARPS - 1)];
+    s = p.x;
+    t = p.y;
 #pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
-        const float2 p = buf[i];
-        s += p.x;
-        t += p.y;
+    for (int o = WARPS / 2; o; o >>= 1) {
+        s += __shfl_xor_sync(~0u, s, o);
+        t += __shfl_xor_sync(~0u, t, o);
     }
     return make_float2(s, t);
 }
@@ -52,138 +64,172 @@ struct NormArgs {
     float eps;
 };
 
-// VEC neighbouring elements, read at once
+// VEC neighbouring elements as they lie in memory: one element, or 16 bytes
 template <typename T, int VEC> struct Pack {
-    T e[VEC];
+    uint32_t w[VEC == 1 ? 1 : 4];
 };
 template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_pack(const T* p) {
     Pack<T, VEC> r;
-    if constexpr (VEC * sizeof(T) == 16) *reinterpret_cast<uint4*>(r.e) = *reinterpret_cast<const uint4*>(p);
-    else r.e[0] = *p;
+    if constexpr (VEC > 1) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
+    } else if constexpr (sizeof(T) == 4) {
+        r.w[0] = __float_as_uint(*p);
+    } else {
+        r.w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
     return r;
 }
-template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* p, const Pack<T, VEC>& v) {
-    if constexpr (VEC * sizeof(T) == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v.e);
-    else *p = v.e[0];
-}
-template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> fill_pack(float f) {
-    Pack<T, VEC> r;
+template <typename T, int VEC> __device__ __forceinline__ void unpack(const Pack<T, VEC>& p, float (&v)[VEC]) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) r.e[e] = from_f<T>(f);
-    return r;
+        for (int e = 0; e < VEC; ++e) v[e] = __uint_as_float(p.w[e]);
+    } else if constexpr (VEC == 1) {
+        v[0] = unpack2<T>(p.w[0]).x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+            const float2 f = unpack2<T>(p.w[e / 2]);
+            v[e] = f.x;
+            v[e + 1] = f.y;
+        }
+    }
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1) *p = from_f<T>(v[0]);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+template <typename T, int VEC> __device__ __forceinline__ void load_param(const void* p, int c, float other, float (&v)[VEC]) {
+    if (p) {
+        unpack<T, VEC>(load_pack<T, VEC>(static_cast<const T*>(p) + c), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = other;
+    }
 }
 
 // WARPS warps per row, NV packs of VEC elements per thread: pack i of thread t holds the
 // columns (i * threads + t) * VEC + [0, VEC).  With one warp per row a CTA has 8 rows.
-template <typename T, int VEC, int WARPS> struct Row {
+template <int VEC, int WARPS> struct Row {
     static constexpr int kThreads = WARPS * 32, kCta = WARPS == 1 ? 256 : kThreads;
-    static __device__ __forceinline__ int64_t column(int i) {
-        return ((int64_t)i * kThreads + (WARPS == 1 ? threadIdx.x & 31 : threadIdx.x)) * VEC;
+    static __device__ __forceinline__ int column(int i) {
+        return (i * kThreads + (int)(WARPS == 1 ? threadIdx.x & 31 : threadIdx.x)) * VEC;
     }
     static __device__ __forceinline__ int64_t first() { return WARPS == 1 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : blockIdx.x; }
     static __device__ __forceinline__ int64_t step() { return WARPS == 1 ? gridDim.x * 8ll : gridDim.x; }
 };
 
+// A thread's packs of row r; zeros beyond the columns, nothing beyond the rows.
 template <typename T, int VEC, int WARPS, int NV>
-__global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_forward_kernel(const __grid_constant__ NormArgs A) {
-    using R = Row<T, VEC, WARPS>;
-    __shared__ float2 buf[2][WARPS];
-    const float inv = 1.f / (float)A.cols;
+__device__ __forceinline__ void load_row(const NormArgs& A, const void* p, int64_t ld, int64_t r, Pack<T, VEC> (&v)[NV]) {
+    using R = Row<VEC, WARPS>;
+    if (r >= A.rows) return;
+    const T* x = static_cast<const T*>(p) + r * ld;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        v[i] = Pack<T, VEC>{};
+        if (R::column(i) < (int)A.cols) v[i] = load_pack<T, VEC>(x + R::column(i));
+    }
+}
+
+// 8192 x 4096 bfloat16: see the table of the operators' cases; instructions count here as
+// much as bytes, so elements are converted once and kept as floats.
+template <typename T, int VEC, int WARPS, int NV>
+__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, 1024 / Row<VEC, WARPS>::kCta)
+norm_forward_kernel(const __grid_constant__ NormArgs A) {
+    using R = Row<VEC, WARPS>;
+    __shared__ float buf[2][WARPS];
+    const int cols = (int)A.cols;
+    const float inv = 1.f / (float)cols;
     for (int64_t r = R::first(); r < A.rows; r += R::step()) {
-        const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
-        Pack<T, VEC> v[NV];
-        float s = 0.f, q = 0.f;
+        Pack<T, VEC> raw[NV];
+        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r, raw);
+        float v[NV][VEC], s = 0.f, q = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            v[i] = fill_pack<T, VEC>(0.f);
-            if (R::column(i) < A.cols) v[i] = load_pack<T, VEC>(x + R::column(i));
+            unpack<T, VEC>(raw[i], v[i]);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += v[i][e];
         }
+        const float mean = row_sum<WARPS>(s, buf[0]) * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s += to_f(v[i].e[e]);
-        const float mean = row_sum<WARPS>(s, 0.f, buf[0]).x * inv;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (R::column(i) < A.cols)
+            if (R::column(i) < cols)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float d = to_f(v[i].e[e]) - mean;
-                    q = fmaf(d, d, q);
+                    v[i][e] -= mean;
+                    q = fmaf(v[i][e], v[i][e], q);
                 }
-        const float rstd = 1.f / sqrtf(row_sum<WARPS>(q, 0.f, buf[1]).x * inv + A.eps);
+        const float rstd = rsqrtf(row_sum<WARPS>(q, buf[1]) * inv + A.eps);
         if (A.stats && R::column(0) == 0) *reinterpret_cast<float2*>(A.stats + 2 * r) = make_float2(mean, rstd);
-        T* y = static_cast<T*>(A.y) + r * A.cols;
+        T* y = static_cast<T*>(A.y) + r * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t c = R::column(i);
-            if (c >= A.cols) continue;
-            Pack<T, VEC> w = fill_pack<T, VEC>(1.f), b = fill_pack<T, VEC>(0.f), o;
-            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + c);
-            if (A.bias) b = load_pack<T, VEC>(static_cast<const T*>(A.bias) + c);
+            const int c = R::column(i);
+            if (c >= cols) continue;
+            float w[VEC], b[VEC];
+            load_param<T, VEC>(A.weight, c, 1.f, w);
+            load_param<T, VEC>(A.bias, c, 0.f, b);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) o.e[e] = from_f<T>(fmaf((to_f(v[i].e[e]) - mean) * rstd, to_f(w.e[e]), to_f(b.e[e])));
-            store_pack<T, VEC>(y + c, o);
+            for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[e], b[e]);
+            store_pack<T, VEC>(y + c, v[i]);
         }
     }
 }
 
+// Loads run a row ahead, so that they are in flight during the sums of the row before.
 template <typename T, int VEC, int WARPS, int NV>
-__global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
-    using R = Row<T, VEC, WARPS>;
+__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
+    using R = Row<VEC, WARPS>;
     __shared__ float2 buf[2][WARPS];
-    const float inv = 1.f / (float)A.cols;
+    const int cols = (int)A.cols;
+    const float inv = 1.f / (float)cols;
     float gw[NV][VEC], gb[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) gw[i][e] = gb[i][e] = 0.f;
     int turn = 0;
+    Pack<T, VEC> nx[NV], ng[NV];
+    load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
+    load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
     for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
-        const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
-        const T* gy = static_cast<const T*>(A.gy) + r * A.ld_gy;
         const float2 st = *reinterpret_cast<const float2*>(A.stats_in + 2 * r);
-        Pack<T, VEC> v[NV], g[NV];
+        float h[NV][VEC], k[NV][VEC];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            v[i] = g[i] = fill_pack<T, VEC>(0.f);
-            if (R::column(i) < A.cols) {
-                v[i] = load_pack<T, VEC>(x + R::column(i));
-                g[i] = load_pack<T, VEC>(gy + R::column(i));
-            }
+            unpack<T, VEC>(nx[i], h[i]);
+            unpack<T, VEC>(ng[i], k[i]);
         }
+        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
+        load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (R::column(i) >= A.cols) continue;
-            Pack<T, VEC> w = fill_pack<T, VEC>(1.f);
-            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + R::column(i));
+            if (R::column(i) >= cols) continue;
+            float w[VEC];
+            load_param<T, VEC>(A.weight, R::column(i), 1.f, w);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float h = (to_f(v[i].e[e]) - st.x) * st.y, d = to_f(g[i].e[e]);
-                gw[i][e] = fmaf(d, h, gw[i][e]);
-                gb[i][e] += d;
-                const float k = d * to_f(w.e[e]);
-                s += k;
-                t = fmaf(k, h, t);
+                h[i][e] = (h[i][e] - st.x) * st.y;
+                gw[i][e] = fmaf(k[i][e], h[i][e], gw[i][e]);
+                gb[i][e] += k[i][e];
+                k[i][e] *= w[e];
+                s += k[i][e];
+                t = fmaf(k[i][e], h[i][e], t);
             }
         }
         if (!A.gx) continue;
         const float2 sum = row_sum<WARPS>(s, t, buf[turn]);
         const float ms = sum.x * inv, mt = sum.y * inv;
-        T* gx = static_cast<T*>(A.gx) + r * A.cols;
+        T* gx = static_cast<T*>(A.gx) + r * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t c = R::column(i);
-            if (c >= A.cols) continue;
-            Pack<T, VEC> w = fill_pack<T, VEC>(1.f), o;
-            if (A.weight) w = load_pack<T, VEC>(static_cast<const T*>(A.weight) + c);
+            if (R::column(i) >= cols) continue;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float h = (to_f(v[i].e[e]) - st.x) * st.y;
-                o.e[e] = from_f<T>(st.y * (to_f(g[i].e[e]) * to_f(w.e[e]) - ms - h * mt));
-            }
-            store_pack<T, VEC>(gx + c, o);
+            for (int e = 0; e < VEC; ++e) k[i][e] = st.y * fmaf(-h[i][e], mt, k[i][e] - ms);
+            store_pack<T, VEC>(gx + R::column(i), k[i]);
         }
     }
     if (!A.part) return;
@@ -197,22 +243,25 @@ __global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_backward_kernel
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sums[threadIdx.x >> 5][R::column(i) + e] = which ? gb[i][e] : gw[i][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < A.cols; c += 256) {
+            for (int c = threadIdx.x; c < cols; c += 256) {
                 float a = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) a += sums[i][c];
-                A.part[((int64_t)which * gridDim.x + blockIdx.x) * A.cols + c] = a;
+                A.part[((int64_t)which * gridDim.x + blockIdx.x) * cols + c] = a;
             }
         }
     } else {
+        float* pw = A.part + (int64_t)blockIdx.x * cols;
+        float* pb = pw + (int64_t)gridDim.x * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
+            if (R::column(i) < cols) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (R::column(i) < A.cols) {
-                    A.part[(int64_t)blockIdx.x * A.cols + R::column(i) + e] = gw[i][e];
-                    A.part[((int64_t)gridDim.x + blockIdx.x) * A.cols + R::column(i) + e] = gb[i][e];
+                for (int e = 0; e < VEC; ++e) {
+                    pw[R::column(i) + e] = gw[i][e];
+                    pb[R::column(i) + e] = gb[i][e];
                 }
+            }
     }
 }
 
@@ -221,18 +270,18 @@ __global__ void __launch_bounds__(Row<T, VEC, WARPS>::kCta) norm_backward_kernel
 constexpr int kLong = 512;
 
 template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long(const __grid_constant__ NormArgs A) {
-    __shared__ float2 buf[2][kLong / 32];
+    __shared__ float buf[2][kLong / 32];
     for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
         float s = 0.f;
         for (int64_t c = threadIdx.x; c < A.cols; c += kLong) s += to_f(x[c]);
-        const float mean = row_sum<kLong / 32>(s, 0.f, buf[0]).x / (float)A.cols;
+        const float mean = row_sum<kLong / 32>(s, buf[0]) / (float)A.cols;
         s = 0.f;
         for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
             const float d = to_f(x[c]) - mean;
             s = fmaf(d, d, s);
         }
-        const float rstd = 1.f / sqrtf(row_sum<kLong / 32>(s, 0.f, buf[1]).x / (float)A.cols + A.eps);
+        const float rstd = rsqrtf(row_sum<kLong / 32>(s, buf[1]) / (float)A.cols + A.eps);
         if (A.stats && threadIdx.x == 0) *reinterpret_cast<float2*>(A.stats + 2 * r) = make_float2(mean, rstd);
         T* y = static_cast<T*>(A.y) + r * A.cols;
         for (int64_t c = threadIdx.x; c < A.cols; c += kLong) {
@@ -300,10 +349,10 @@ struct Plan {
     int warps, threads;
 };
 template <typename T, int VEC, int WARPS, int NV> Plan forward_plan() {
-    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<T, VEC, WARPS>::kCta};
+    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
 }
 template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
-    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<T, VEC, WARPS>::kCta};
+    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
 }
 // E: elements per thread and step of the ladder
 template <typename T, int VEC> Plan forward_choice(int64_t cols) {
@@ -322,7 +371,7 @@ template <typename T, int VEC> Plan backward_choice(int64_t cols) {
     if (cols <= 512) return backward_plan<T, VEC, 2, N8>();
     if (cols <= 1024) return backward_plan<T, VEC, 4, N8>();
     if (cols <= 2048) return backward_plan<T, VEC, 8, N8>();
-    if (cols <= 4096) return backward_plan<T, VEC, 8, N16>();
+    if (cols <= 4096) return backward_plan<T, VEC, 16, N8>();
     return backward_plan<T, VEC, 16, N16>();
 }
 template <typename T> Plan choose_plan(bool forward, int64_t cols, bool vec) {
@@ -343,8 +392,11 @@ const void* long_kernel(int dtype, int which) {
     return dtype == VQC_F32 ? long_kernel<float>(which) : dtype == VQC_BF16 ? long_kernel<__nv_bfloat16>(which) : long_kernel<__half>(which);
 }
 
-// CTAs of the backward (partial column sums of each): two per SM
-int64_t backward_ctas(int warps, int64_t rows) { return row_ctas(warps, rows, 2LL * sm_count()); }
+// CTAs of the backward (each with its column sums): 1024 threads per SM
+int64_t backward_ctas(int64_t cols, int64_t rows) {
+    const int warps = cols <= 256 ? 1 : cols <= 512 ? 2 : cols <= 1024 ? 4 : cols <= 2048 ? 8 : 16;
+    return row_ctas(warps, rows, (int64_t)sm_count() * (warps == 1 ? 4 : 32 / warps));
+}
 constexpr int64_t kLongBlocks = 64;   // blocks of rows of norm_columns_long
 
 // rows and vectors on 16-byte boundaries
@@ -395,7 +447,7 @@ vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, co
 
 size_t vqc_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || cols > 0x7fffffff) return (size_t)-1;
-    const int64_t blocks = cols > kMostBackward ? kLongBlocks : backward_ctas(cols <= 256 ? 1 : 2, rows);
+    const int64_t blocks = cols > kMostBackward ? kLongBlocks : backward_ctas(cols, rows);
     return align256((size_t)2 * blocks * cols * 4);
 }
 
@@ -438,7 +490,7 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             }
         } else if (rows > 0) {
             const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
-            blocks = columns ? backward_ctas(p.warps, rows) : row_ctas(p.warps, rows, 0x7fffffff);
+            blocks = columns ? backward_ctas(cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
             void* args[] = {&a};
             const cudaError_t err = cudaLaunchKernel(p.fn, dim3((unsigned)blocks), dim3(p.threads), args, 0, s);
             if (err != cudaSuccess) return launched(err);

@@ -186,12 +186,14 @@ vqc_status join_run(const Product& p, const float* part, int splits, cudaStream_
 
 size_t product_workspace(const Product& p, bool aligned) {
     if (p.m == 0 || p.k == 0) return 0;
+    if (rows_takes(p)) return 0;
     if (tc_takes(p)) return tc_workspace(p, aligned);
     return part_bytes(p, pick_splits(p, pick_tile(p)));
 }
 
 vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
     if (p.m == 0 || p.n == 0) return VQC_OK;
+    if (rows_takes(p)) return rows_run(p, s);
     if (tc_takes(p)) return tc_run(p, ws, ws_bytes, s);
     const Tile t = pick_tile(p);
     ProductArgs a{};
@@ -222,27 +224,38 @@ namespace {
 // and over the CTAs by sum_kernel, both in a fixed order.
 constexpr int kGradCols = 256;
 
-template <bool VEC> __device__ __forceinline__ void load8(const void* p, int dtype, int64_t row, int64_t c, int64_t n, float (&v)[8]) {
+// 8 elements as they lie in memory, and as floats
+struct Raw8 {
+    uint32_t w[8];
+};
+template <bool VEC> __device__ __forceinline__ void load8(const void* p, int dtype, int64_t row, int64_t c, int64_t n, Raw8& v) {
     if constexpr (VEC) {
         if (dtype == VQC_F32) {
-            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
-            const float4 a = q[0], b = q[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + row + c);
+            const uint4 a = __ldcs(q), b = __ldcs(q + 1);
+            v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
+            v.w[4] = b.x; v.w[5] = b.y; v.w[6] = b.z; v.w[7] = b.w;
         } else {
-            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = dtype == VQC_BF16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]))
-                                                   : __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                v[2 * i] = f.x;
-                v[2 * i + 1] = f.y;
-            }
+            const uint4 a = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c));
+            v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + 32 * i < n ? load_as(p, dtype, row + c + 32 * i) : 0.f;
+        for (int i = 0; i < 8; ++i) v.w[i] = c + 32 * i < n ? __float_as_uint(load_as(p, dtype, row + c + 32 * i)) : 0u;
+    }
+}
+template <bool VEC> __device__ __forceinline__ void floats8(const Raw8& r, int dtype, float (&v)[8]) {
+    if (VEC && dtype != VQC_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = dtype == VQC_BF16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r.w[i]))
+                                               : __half22float2(*reinterpret_cast<const __half2*>(&r.w[i]));
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
     }
 }
 template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, int64_t row, int64_t c, int64_t n, const float (&v)[8]) {
@@ -260,28 +273,43 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, 
     }
 }
 
+// The loads of UR rows are issued before the first of them is used.
 template <typename T, bool VEC, int ACT, bool GATE>
 __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
-#pragma unroll 2
-    for (int64_t r = r0; r < r1; r += 8) {
-        float gy[8], z[8], u[8], d[8];
-        load8<VEC>(A.gy, A.gy_dtype, r * A.ld_gy, c, A.n, gy);
-        if (ACT != VQC_ACT_NONE || GATE) load8<VEC>(A.z[0], VQC_F32, r * A.n, c, A.n, z);
-        if (GATE) load8<VEC>(A.z[1], VQC_F32, r * A.n, c, A.n, u);
+    constexpr int UR = GATE ? 1 : 2;
+    for (int64_t r = r0; r < r1; r += 8 * UR) {
+        Raw8 rg[UR], rz[UR], ru[UR];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (GATE) {
-                const float2 v = act_both(ACT, z[i]);
-                d[i] = gy[i] * u[i] * v.y;
-                u[i] = gy[i] * v.x;
-                s1[i] += u[i];
-            } else {
-                d[i] = ACT == VQC_ACT_NONE ? gy[i] : gy[i] * act_both(ACT, z[i]).y;
-            }
-            s0[i] += d[i];
+        for (int k = 0; k < UR; ++k) {
+            const int64_t q = r + 8 * k;
+            if (q >= r1) break;
+            load8<VEC>(A.gy, A.gy_dtype, q * A.ld_gy, c, A.n, rg[k]);
+            if (ACT != VQC_ACT_NONE || GATE) load8<VEC>(A.z[0], VQC_F32, q * A.n, c, A.n, rz[k]);
+            if (GATE) load8<VEC>(A.z[1], VQC_F32, q * A.n, c, A.n, ru[k]);
         }
-        if (A.dz[0]) store8<T, VEC>(A.dz[0], r * A.ld_dz, c, A.n, d);
-        if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], r * A.ld_dz, c, A.n, u);
+#pragma unroll
+        for (int k = 0; k < UR; ++k) {
+            const int64_t q = r + 8 * k;
+            if (q >= r1) break;
+            float gy[8], z[8], u[8], d[8];
+            floats8<VEC>(rg[k], A.gy_dtype, gy);
+            if (ACT != VQC_ACT_NONE || GATE) floats8<VEC>(rz[k], VQC_F32, z);
+            if (GATE) floats8<VEC>(ru[k], VQC_F32, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (GATE) {
+                    const float2 v = act_both(ACT, z[i]);
+                    d[i] = gy[i] * u[i] * v.y;
+                    u[i] = gy[i] * v.x;
+                    s1[i] += u[i];
+                } else {
+                    d[i] = ACT == VQC_ACT_NONE ? gy[i] : gy[i] * act_both(ACT, z[i]).y;
+                }
+                s0[i] += d[i];
+            }
+            if (A.dz[0]) store8<T, VEC>(A.dz[0], q * A.ld_dz, c, A.n, d);
+            if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], q * A.ld_dz, c, A.n, u);
+        }
     }
 }
 template <typename T, bool VEC, bool GATE>
@@ -297,7 +325,7 @@ __device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
+__global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
     __shared__ float sums[8][kGradCols];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across, blocks = gridDim.x / across;
