@@ -358,8 +358,8 @@ template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
 template <typename T, int VEC> Plan forward_choice(int64_t cols) {
     constexpr int N8 = 8 / VEC, N16 = 16 / VEC, N32 = 32 / VEC;
     if (cols <= 256) return forward_plan<T, VEC, 1, N8>();
-    if (cols <= 512) return forward_plan<T, VEC, 1, N16>();
-    if (cols <= 1024) return forward_plan<T, VEC, 1, N32>();
+    if (cols <= 512) return forward_plan<T, VEC, 2, N8>();
+    if (cols <= 1024) return forward_plan<T, VEC, 4, N8>();
     if (cols <= 2048) return forward_plan<T, VEC, 4, N16>();
     if (cols <= 4096) return forward_plan<T, VEC, 8, N16>();
     if (cols <= 8192) return forward_plan<T, VEC, 16, N16>();
@@ -495,7 +495,7 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             const cudaError_t err = cudaLaunchKernel(p.fn, dim3((unsigned)blocks), dim3(p.threads), args, 0, s);
             if (err != cudaSuccess) return launched(err);
         }
-        return columns ? sum_run(a.part, blocks, cols, grad_weight, grad_bias, dtype, s) : VQC_OK;
+        return columns ? sum_run(a.part, blocks, cols, cols, blocks * cols, grad_weight, grad_bias, dtype, s) : VQC_OK;
     } catch (...) {
         return VQC_ERR_OUT_OF_MEMORY;
     }

@@ -29,7 +29,7 @@ bool on(const void* p, size_t a) { return aligned_to(p, a); }
 // Space of a backward call: dz (and du), then the column sums, then the products.
 struct BackSpace {
     int64_t ld_dz;
-    size_t dz, sums, product, total;
+    size_t dz, sums, gx, gw, total;
     bool own_dz;
 };
 
@@ -84,9 +84,9 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     b.sums = act_grad_workspace(rows, out, gated);
     const void* none[2] = {nullptr, nullptr};
     void* nothing[2] = {nullptr, nullptr};
-    b.product = std::max(product_workspace(product_gx(dtype, rows, in, out, none, b.ld_dz, none, ld_w, gated, nullptr), aligned),
-                         product_workspace(product_gw(dtype, rows, in, out, none, b.ld_dz, nullptr, ld_x, gated, nothing), aligned));
-    b.total = b.dz * (gated ? 2 : 1) + b.sums + b.product;
+    b.gx = product_workspace(product_gx(dtype, rows, in, out, none, b.ld_dz, none, ld_w, gated, nullptr), aligned);
+    b.gw = product_workspace(product_gw(dtype, rows, in, out, none, b.ld_dz, nullptr, ld_x, gated, nothing), aligned);
+    b.total = b.dz * (gated ? 2 : 1) + b.sums + b.gx + b.gw;
     return b;
 }
 
@@ -110,7 +110,9 @@ vqc_status forward(const char* call, int dtype, int out_dtype, int64_t rows, int
     p.f.y[0] = y;
     p.f.z[0] = saved;
     p.f.z[1] = saved && gated ? saved + rows * out : nullptr;
-    return product_run(p, ws, ws_bytes, static_cast<cudaStream_t>(stream));
+    Joins joins{};
+    const vqc_status st = products_run(&p, 1, &ws, &ws_bytes, joins, static_cast<cudaStream_t>(stream));
+    return st == VQC_OK ? join_run(joins, static_cast<cudaStream_t>(stream)) : st;
 }
 
 vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, int64_t in, int64_t out, const void* gy,
@@ -133,6 +135,7 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     if (ws_bytes < b.total || !ws) return set_error(VQC_ERR_WORKSPACE, std::string(call) + ": workspace too small");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char* at = static_cast<char*>(ws);
+    Joins joins{};
     const bool need_dz = (gx || gw[0]) && b.own_dz;
     const void* dz[2] = {gy, nullptr};
     ActGrad g{};
@@ -147,16 +150,26 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
         g.sum[0] = gb[0]; g.sum[1] = gated ? gb[1] : nullptr;
         g.rows = rows; g.n = out;
         g.act = act; g.dtype = dtype; g.gy_dtype = out_dtype; g.gated = gated;
-        const vqc_status st = act_grad_run(g, at, b.sums, s);
+        const vqc_status st = act_grad_run(g, at, b.sums, joins, s);
         if (st != VQC_OK) return st;
     }
     at += b.sums;
+    Product p[2];
+    void* spaces[2];
+    size_t bytes[2];
+    int count = 0;
     if (gx) {
-        const vqc_status st = product_run(product_gx(dtype, rows, in, out, dz, b.ld_dz, w, ld_w, gated, gx), at, b.product, s);
-        if (st != VQC_OK) return st;
+        p[count] = product_gx(dtype, rows, in, out, dz, b.ld_dz, w, ld_w, gated, gx);
+        spaces[count] = at;
+        bytes[count++] = b.gx;
     }
-    if (gw[0]) return product_run(product_gw(dtype, rows, in, out, dz, b.ld_dz, x, ld_x, gated, gw), at, b.product, s);
-    return VQC_OK;
+    if (gw[0]) {
+        p[count] = product_gw(dtype, rows, in, out, dz, b.ld_dz, x, ld_x, gated, gw);
+        spaces[count] = at + b.gx;
+        bytes[count++] = b.gw;
+    }
+    const vqc_status st = products_run(p, count, spaces, bytes, joins, s);
+    return st == VQC_OK ? join_run(joins, s) : st;
 }
 
 size_t workspace(int mode, int dtype, int out_dtype, int64_t rows, int64_t in, int64_t out, int64_t ld_x, int64_t ld_w,

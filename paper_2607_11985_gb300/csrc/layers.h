@@ -58,10 +58,36 @@ struct Product {
     Finish f;
 };
 
+// The float operands of a product that the tensor cores ran in parts: an output
+// that is not finite is worked out again from them (see layers_tc.cu).
+struct Exact {
+    Operand a[2], b[2];
+    int64_t k;       // 0: not asked for
+    int32_t form;
+};
+
+// Sums of a contraction that was cut, [splits][1 or 2][m][n] (two for GATED and PAIR),
+// still to be joined in the order of the cuts and finished.
+struct Join {
+    Finish f;
+    Exact exact;
+    const float* part;
+    int32_t splits, form;
+};
+constexpr int kMostJoins = 4;
+struct Joins {
+    Join j[kMostJoins];
+    int count;
+};
+vqc_status join_run(const Joins& joins, cudaStream_t s);
+
 // Bytes of workspace of a product.  `aligned`: the operands' addresses are
 // multiples of 16 bytes (their strides are looked at).
 size_t product_workspace(const Product& p, bool aligned);
-vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s);
+// Runs products that do not depend on one another, in as few launches as they
+// allow; what is left to be joined is added to `joins`.  ws[i], bytes[i]: the workspace
+// of product i, in use until the joins have run.
+vqc_status products_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s);
 
 // dz = grad_y * act'(z) (gated: dg and du from grad_h, g and u) and the column sums.
 struct ActGrad {
@@ -75,11 +101,13 @@ struct ActGrad {
     int32_t act, dtype, gy_dtype, gated;
 };
 size_t act_grad_workspace(int64_t rows, int64_t n, bool gated);
-vqc_status act_grad_run(const ActGrad& a, void* ws, size_t ws_bytes, cudaStream_t s);
+// Column sums of few blocks of rows are left to `joins`.
+vqc_status act_grad_run(const ActGrad& a, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s);
 
-// out[i][c] = sum over j of part[i][j][c] for i = 0, 1 ([count][n] each), in a fixed
+// out_i[c] = sum over j < count of part[i * second + j * ld + c] for i = 0, 1, in a fixed
 // order; either output may be NULL.
-vqc_status sum_run(const float* part, int64_t count, int64_t n, void* out0, void* out1, int dtype, cudaStream_t s);
+vqc_status sum_run(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second, void* out0, void* out1, int dtype,
+                   cudaStream_t s);
 
 }  // namespace layers
 }  // namespace vqc

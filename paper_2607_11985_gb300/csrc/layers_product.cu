@@ -1,8 +1,9 @@
-// layers_product.cu -- matrix products on the FP32 units, for every type,
-// layout, stride and size, and the join of products that were cut along the
-// contraction.
+// layers_product.cu -- matrix products on the FP32 units, the join of products that
+// were cut along the contraction, and the pass over dz of a backward.
 //
-// Operands become float in shared memory, sums are float FMAs in a fixed order.
+// 16-bit operands go to the tensor cores, products with few rows to
+// layers_rows.cu; what is left here are float products of moderate size, for
+// every layout, stride and size, with sums in a fixed order.
 #include <algorithm>
 
 #include "layers_elem.cuh"
@@ -31,26 +32,87 @@ struct ProductArgs {
     Operand a[2], b[2];
     Finish f;
     int64_t k;
-    float* part;     // [splits][2 or 1][m][n] sums of a cut contraction, or NULL
-    int32_t form, splits;
-    int64_t tiles_m, tiles_n;
+    float* part;     // sums of a cut contraction, or NULL
+    int32_t form, splits, vec_a, vec_b;
+    int64_t tiles_m, tiles_n, ctas;
+};
+// Up to two products of one launch, the CTAs of the first before those of the second.
+struct ProductPair {
+    ProductArgs p[2];
 };
 
-// A BM x BN tile of outputs per CTA of 256 threads, BK contracted elements at a
-// time.  Each thread holds TM x TN sums: columns tx * TN/2 + [0, TN/2) of both
-// halves of the tile.  In GATED form the first half of the tile's columns
-// belongs to b0 and the second half to b1 (the same outputs), so that both
-// factors of an output meet in one thread.
-template <typename T, int BM, int BN, int TM, int TN>
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ ProductArgs A) {
-    constexpr int BK = 16, NT = 256, TX = BN / TN;
+constexpr int BK = 16, NT = 256;
+
+// The elements of a tile of W outer rows x BK contracted that one thread moves:
+// groups of 4 neighbours in memory, one 16-byte load each where `vec` allows.
+template <int W> struct Slice {
+    static constexpr int kGroups = (W * BK / 4 + NT - 1) / NT;
+    float v[kGroups][4];
+
+    __device__ __forceinline__ void load(const Operand& o, const float* second, int64_t ld, bool vec, int64_t i0, int64_t outer, int64_t k0, int64_t k,
+                                         int split_at) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int e = threadIdx.x + g * NT;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[g][j] = 0.f;
+            if (W * BK / 4 < NT && e >= W * BK / 4) continue;
+            int i = o.k_outer ? e % (W / 4) * 4 : e / (BK / 4);
+            const int kk = o.k_outer ? e / (W / 4) : e % (BK / 4) * 4;
+            const float* p = static_cast<const float*>(o.p);
+            if (second && i >= split_at) {
+                p = second;
+                i -= split_at;
+            }
+            const int64_t r = i0 + i, c = k0 + kk;
+            const int64_t at = o.k_outer ? c * ld + r : r * ld + c;
+            const int64_t inner = o.k_outer ? outer - r : k - c;     // elements left in this direction
+            if (o.k_outer ? c >= k : r >= outer) continue;
+            if (vec && inner >= 4) {
+                const float4 q = *reinterpret_cast<const float4*>(p + at);
+                v[g][0] = q.x; v[g][1] = q.y; v[g][2] = q.z; v[g][3] = q.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < inner) v[g][j] = p[at + j];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float (*s)[W + 4], bool k_outer) const {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int e = threadIdx.x + g * NT;
+            if (W * BK / 4 < NT && e >= W * BK / 4) continue;
+            if (k_outer) {
+                *reinterpret_cast<float4*>(&s[e / (W / 4)][e % (W / 4) * 4]) = make_float4(v[g][0], v[g][1], v[g][2], v[g][3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[e % (BK / 4) * 4 + j][e / (BK / 4)] = v[g][j];
+            }
+        }
+    }
+};
+
+// A BM x BN tile of outputs per CTA of 256 threads, 16 contracted elements at a time,
+// the next ones in flight meanwhile.  Each thread holds TM x TN sums (packed pairs along n): columns
+// tx * TN/2 + [0, TN/2) of both halves of the tile.  In GATED form the first
+// half of the tile's columns belongs to b0 and the second half to b1 (the same
+// outputs), so that both factors of an output meet in one thread.
+template <int BM, int BN, int TM, int TN>
+__global__ void __launch_bounds__(NT) product_kernel(const __grid_constant__ ProductPair P) {
+    constexpr int TX = BN / TN, TH = TN / 2;
     static_assert((BM / TM) * TX == NT && TN % 2 == 0, "tile");
-    __shared__ float sa[BK][BM + 4], sb[BK][BN + 4];
+    __shared__ __align__(16) float sa[2][BK][BM + 4], sb[2][BK][BN + 4];
     const int tid = threadIdx.x, tx = tid % TX, ty = tid / TX;
+    int64_t block = blockIdx.x;
+    const int which_product = block >= P.p[0].ctas ? 1 : 0;
+    const ProductArgs& A = P.p[which_product];
+    if (which_product) block -= P.p[0].ctas;
     const bool gated = A.form == GATED;
-    const int64_t tile = blockIdx.x / A.tiles_n;
-    const int64_t n0 = (blockIdx.x % A.tiles_n) * (gated ? BN / 2 : BN), m0 = tile % A.tiles_m * BM;
-    const int split = (int)(tile / A.tiles_m), which = blockIdx.y;
+    int64_t tile = block / A.tiles_n;
+    const int64_t n0 = block % A.tiles_n * (gated ? BN / 2 : BN), m0 = tile % A.tiles_m * BM;
+    tile /= A.tiles_m;
+    const int split = (int)(tile % A.splits), which = (int)(tile / A.splits);
     const int64_t m = A.f.m, n = A.f.n;
     const int64_t blocks = (A.k + BK - 1) / BK, terms = A.form == SUM ? 2 : 1;
     const int64_t kb0 = blocks * terms * split / A.splits, kb1 = blocks * terms * (split + 1) / A.splits;
@@ -61,40 +123,40 @@ __global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ Pr
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = 0.f;
 
-    for (int64_t kb = kb0; kb < kb1; ++kb) {
+    Slice<BM> na;
+    Slice<BN> nb;
+    auto load = [&](int64_t kb) {
         const int term = kb >= blocks ? 1 : 0;
         const int64_t k0 = (kb - term * blocks) * BK;
-        const Operand oa = A.a[which + term], ob = A.b[which + term];
-        const T* pa = static_cast<const T*>(oa.p);
-        for (int e = tid; e < BM * BK; e += NT) {
-            const int i = oa.k_outer ? e % BM : e / BK, kk = oa.k_outer ? e / BM : e % BK;
-            const int64_t r = m0 + i, c = k0 + kk;
-            sa[kk][i] = r < m && c < A.k ? to_f(pa[oa.k_outer ? c * oa.ld + r : r * oa.ld + c]) : 0.f;
-        }
-        for (int e = tid; e < BN * BK; e += NT) {
-            const int i = ob.k_outer ? e % BN : e / BK, kk = ob.k_outer ? e / BN : e % BK;
-            const bool up = gated && i >= BN / 2;
-            const T* pb = static_cast<const T*>(up ? A.b[1].p : ob.p);
-            const int64_t ld = up ? A.b[1].ld : ob.ld, r = n0 + (up ? i - BN / 2 : i), c = k0 + kk;
-            sb[kk][i] = r < n && c < A.k ? to_f(pb[ob.k_outer ? c * ld + r : r * ld + c]) : 0.f;
-        }
-        __syncthreads();
+        na.load(A.a[which + term], nullptr, A.a[which + term].ld, A.vec_a, m0, m, k0, A.k, BM);
+        nb.load(A.b[which + term], gated ? static_cast<const float*>(A.b[1].p) : nullptr, A.b[which + term].ld, A.vec_b, n0, n, k0, A.k, BN / 2);
+    };
+    if (kb0 < kb1) load(kb0);
+    int buf = 0;
+    for (int64_t kb = kb0; kb < kb1; ++kb, buf ^= 1) {
+        na.store(sa[buf], A.a[0].k_outer);
+        nb.store(sb[buf], A.b[0].k_outer);
+        __syncthreads();       // the other buffer was read before the barrier of the step before
+        if (kb + 1 < kb1) load(kb + 1);
 #pragma unroll
         for (int kk = 0; kk < BK; ++kk) {
             float a[TM], b[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = sa[kk][ty * TM + i];
+            for (int i = 0; i < TM; ++i) a[i] = sa[buf][kk][ty * TM + i];
 #pragma unroll
-            for (int j = 0; j < TN / 2; ++j) {
-                b[j] = sb[kk][tx * (TN / 2) + j];
-                b[TN / 2 + j] = sb[kk][BN / 2 + tx * (TN / 2) + j];
+            for (int j = 0; j < TH; ++j) {
+                b[j] = sb[buf][kk][tx * TH + j];
+                b[TH + j] = sb[buf][kk][BN / 2 + tx * TH + j];
             }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+                for (int j = 0; j < TN; j += 2) {
+                    const float2 r = fma2(make_float2(a[i], a[i]), make_float2(b[j], b[j + 1]), make_float2(acc[i][j], acc[i][j + 1]));
+                    acc[i][j] = r.x;
+                    acc[i][j + 1] = r.y;
+                }
         }
-        __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -102,8 +164,8 @@ __global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ Pr
         if (row >= m) continue;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const bool second = j >= TN / 2;
-            const int64_t c = tx * (TN / 2) + (second ? j - TN / 2 : j);
+            const bool second = j >= TH;
+            const int64_t c = tx * TH + (second ? j - TH : j);
             const int64_t col = n0 + c + (second && !gated ? BN / 2 : 0);
             if (col >= n) continue;
             if (A.part) {
@@ -112,25 +174,34 @@ __global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ Pr
             } else if (!gated) {
                 finish_one(A.f, which, row, col, acc[i][j], 0.f);
             } else if (!second) {
-                finish_one(A.f, 0, row, col, acc[i][j], acc[i][TN / 2 + j]);
+                finish_one(A.f, 0, row, col, acc[i][j], acc[i][TH + j]);
             }
         }
     }
 }
 
-// Sums of a cut contraction joined in the order of the cuts, then finished.
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Finish f, const float* part, int splits,
-                                                   int form) {
-    const int64_t size = f.m * f.n, step = (int64_t)gridDim.x * blockDim.x;
-    const int which = blockIdx.y;
-    const int64_t slots = form == GATED || form == PAIR ? 2 : 1;
+// Sums of cut contractions joined in the order of the cuts, then finished: job
+// blockIdx.y / 2, its product blockIdx.y % 2 (PAIR).
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Joins J) {
+    const Join& j = J.j[blockIdx.y >> 1];
+    const int which = blockIdx.y & 1;
+    if (which && j.form != PAIR) return;
+    const int64_t size = j.f.m * j.f.n, step = (int64_t)gridDim.x * blockDim.x;
+    const int64_t stride = size * (j.form == GATED || j.form == PAIR ? 2 : 1);
     for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < size; e += step) {
+        const float* p = j.part + which * size + e;
         float v0 = 0.f, v1 = 0.f;
-        for (int s = 0; s < splits; ++s) {
-            v0 += part[(s * slots + which) * size + e];
-            if (form == GATED) v1 += part[(s * slots + 1) * size + e];
+#pragma unroll 8
+        for (int s = 0; s < j.splits; ++s) {
+            v0 += p[s * stride];
+            if (j.form == GATED) v1 += p[s * stride + size];
         }
-        finish_one(f, which, e / f.n, e % f.n, v0, v1);
+        const int64_t row = e / j.f.n, col = e % j.f.n;
+        if (j.exact.k) {
+            v0 = exact_if_not_finite(j.exact, which, row, col, v0);
+            if (j.form == GATED) v1 = exact_if_not_finite(j.exact, 1, row, col, v1);
+        }
+        finish_one(j.f, which, row, col, v0, v1);
     }
 }
 
@@ -138,8 +209,8 @@ struct Tile {
     int bm, bn;
 };
 
-// Tiles by the number of outputs; few outputs over a long contraction are cut
-// along it until the SMs have two CTAs each (cuts of at least 128 elements).
+// Tiles by the number of outputs' columns; few outputs over a long contraction are cut
+// along it until the SMs have two CTAs each (cuts of at least 64 elements).
 Tile pick_tile(const Product& p) {
     const int64_t cols = p.form == GATED ? 2 * p.n : p.n;
     if (cols <= 16) return {128, 16};
@@ -147,70 +218,89 @@ Tile pick_tile(const Product& p) {
 }
 
 int pick_splits(const Product& p, Tile t) {
+    if (p.k == 0) return 1;
     const int64_t tiles = ceil_div(p.m, t.bm) * ceil_div(p.n, p.form == GATED ? t.bn / 2 : t.bn) * (p.form == PAIR ? 2 : 1);
-    const int64_t most = ceil_div(p.k * (p.form == SUM ? 2 : 1), 128);
+    const int64_t most = ceil_div(p.k * (p.form == SUM ? 2 : 1), 64);
     return (int)std::max<int64_t>(1, std::min<int64_t>({most, 2LL * sm_count() / std::max<int64_t>(tiles, 1), 64}));
-}
-
-template <typename T, int BM, int BN, int TM, int TN>
-cudaError_t launch_product(ProductArgs a, cudaStream_t s) {
-    a.tiles_m = ceil_div(a.f.m, BM);
-    a.tiles_n = ceil_div(a.f.n, a.form == GATED ? BN / 2 : BN);
-    const int64_t grid = a.tiles_m * a.tiles_n * a.splits;
-    if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    void* args[] = {&a};
-    return cudaLaunchKernel((const void*)product_kernel<T, BM, BN, TM, TN>, dim3((unsigned)grid, a.form == PAIR ? 2 : 1),
-                            dim3(256), args, 0, s);
-}
-
-template <typename T> cudaError_t launch_tile(const ProductArgs& a, Tile t, cudaStream_t s) {
-    if (t.bn == 16) return launch_product<T, 128, 16, 4, 2>(a, s);
-    return launch_product<T, 64, 64, 4, 4>(a, s);
 }
 
 size_t part_bytes(const Product& p, int splits) {
     return splits > 1 ? align256((size_t)splits * (p.form == GATED || p.form == PAIR ? 2 : 1) * p.m * p.n * 4) : 0;
 }
 
+// rows of float operands on 16-byte boundaries
+bool packed(const Operand& o) { return o.ld % 4 == 0 && aligned_to(o.p, 16); }
+
+vqc_status product_args(const Product& p, Tile t, void* ws, size_t ws_bytes, ProductArgs& a, Joins& joins) {
+    for (int i = 0; i < 2; ++i) { a.a[i] = p.a[i]; a.b[i] = p.b[i]; }
+    const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == PLAIN ? 1 : 2;
+    a.vec_a = packed(p.a[0]) && (na == 1 || packed(p.a[1]));
+    a.vec_b = packed(p.b[0]) && (nb == 1 || packed(p.b[1]));
+    a.f = p.f;
+    a.k = p.k;
+    a.form = p.form;
+    a.splits = pick_splits(p, t);
+    a.tiles_m = ceil_div(p.m, t.bm);
+    a.tiles_n = ceil_div(p.n, p.form == GATED ? t.bn / 2 : t.bn);
+    a.ctas = a.tiles_m * a.tiles_n * a.splits * (p.form == PAIR ? 2 : 1);
+    const size_t need = part_bytes(p, a.splits);
+    if (need > ws_bytes || (need && !ws)) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
+    a.part = need ? static_cast<float*>(ws) : nullptr;
+    if (need) {
+        Join& j = joins.j[joins.count++];
+        j.f = p.f;
+        j.part = a.part;
+        j.splits = a.splits;
+        j.form = p.form;
+    }
+    return VQC_OK;
+}
+
 }  // namespace
 
-vqc_status join_run(const Product& p, const float* part, int splits, cudaStream_t s) {
-    Finish f = p.f;
-    int form = p.form;
-    const int64_t blocks = std::min<int64_t>(ceil_div(p.m * p.n, 256), 8LL * sm_count());
-    void* args[] = {&f, &part, &splits, &form};
-    const cudaError_t e = cudaLaunchKernel((const void*)join_kernel, dim3((unsigned)blocks, form == PAIR ? 2 : 1),
+vqc_status join_run(const Joins& joins, cudaStream_t s) {
+    if (!joins.count) return VQC_OK;
+    int64_t most = 1;
+    for (int i = 0; i < joins.count; ++i) most = std::max(most, joins.j[i].f.m * joins.j[i].f.n);
+    void* args[] = {const_cast<Joins*>(&joins)};
+    const cudaError_t e = cudaLaunchKernel((const void*)join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), 2 * joins.count),
                                            dim3(256), args, 0, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "join launch");
 }
 
 size_t product_workspace(const Product& p, bool aligned) {
-    if (p.m == 0 || p.k == 0) return 0;
-    if (rows_takes(p)) return 0;
+    if (p.m == 0 || rows_takes(p)) return 0;
     if (tc_takes(p)) return tc_workspace(p, aligned);
     return part_bytes(p, pick_splits(p, pick_tile(p)));
 }
 
-vqc_status product_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
-    if (p.m == 0 || p.n == 0) return VQC_OK;
-    if (rows_takes(p)) return rows_run(p, s);
-    if (tc_takes(p)) return tc_run(p, ws, ws_bytes, s);
-    const Tile t = pick_tile(p);
-    ProductArgs a{};
-    for (int i = 0; i < 2; ++i) { a.a[i] = p.a[i]; a.b[i] = p.b[i]; }
-    if (p.form == GATED) a.a[1] = p.a[0];
-    a.f = p.f;
-    a.k = p.k;
-    a.form = p.form;
-    a.splits = p.k == 0 ? 1 : pick_splits(p, t);
-    const size_t need = part_bytes(p, a.splits);
-    if (need > ws_bytes || (need && !ws)) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
-    a.part = need ? static_cast<float*>(ws) : nullptr;
-    const cudaError_t e = p.f.dtype == VQC_F32    ? launch_tile<float>(a, t, s)
-                          : p.f.dtype == VQC_BF16 ? launch_tile<__nv_bfloat16>(a, t, s)
-                                                  : launch_tile<__half>(a, t, s);
-    if (e != cudaSuccess) return cuda_error(e, "product launch");
-    return need ? join_run(p, a.part, a.splits, s) : VQC_OK;
+vqc_status products_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s) {
+    ProductPair pair[2]{};       // those of tiles 64 x 64, those of tiles 128 x 16
+    int have[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+        if (p[i].m == 0 || p[i].n == 0) continue;
+        vqc_status st;
+        if (rows_takes(p[i])) {
+            st = rows_run(p[i], s);
+        } else if (tc_takes(p[i])) {
+            st = tc_run(p[i], ws[i], bytes[i], joins, s);
+        } else {
+            const Tile t = pick_tile(p[i]);
+            const int kind = t.bn == 16;
+            st = product_args(p[i], t, ws[i], bytes[i], pair[kind].p[have[kind]++], joins);
+        }
+        if (st != VQC_OK) return st;
+    }
+    for (int kind = 0; kind < 2; ++kind) {
+        if (!have[kind]) continue;
+        const int64_t grid = pair[kind].p[0].ctas + pair[kind].p[1].ctas;
+        if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "product: too many tiles");
+        void* args[] = {&pair[kind]};
+        const void* fn = kind ? (const void*)product_kernel<128, 16, 4, 2> : (const void*)product_kernel<64, 64, 4, 4>;
+        const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(NT), args, 0, s);
+        if (e != cudaSuccess) return cuda_error(e, "product launch");
+    }
+    return VQC_OK;
 }
 
 // ---------------------------------------------------------------- dz and column sums
@@ -328,7 +418,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
     __shared__ float sums[8][kGradCols];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across, blocks = gridDim.x / across;
+    const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across;
     const int64_t c0 = blockIdx.x % across * kGradCols, c = c0 + (VEC ? 8 * lane : lane);
     float s0[8] = {}, s1[8] = {};
     if (c < A.n) {
@@ -346,24 +436,24 @@ __global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant_
             float v = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v += sums[i][threadIdx.x];
-            part[(w * blocks + block) * A.n + c0 + threadIdx.x] = v;
+            part[(block * (A.gated ? 2 : 1) + w) * A.n + c0 + threadIdx.x] = v;
         }
     }
 }
 
 // 32 columns per CTA: warp w adds the rows w, w + 32, ..., then the 32 sums are added.
-__global__ void __launch_bounds__(1024) sum_kernel(const float* part, int64_t count, int64_t n, void* out0, void* out1,
-                                                   int dtype) {
+__global__ void __launch_bounds__(1024) sum_kernel(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second,
+                                                   void* out0, void* out1, int dtype) {
     __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     void* out = blockIdx.y ? out1 : out0;
     if (!out) return;
-    part += (int64_t)blockIdx.y * count * n;
+    part += blockIdx.y * second;
     float v = 0.f;
     if (c < n)
-#pragma unroll 4
-        for (int64_t i = warp; i < count; i += 32) v += part[i * n + c];
+#pragma unroll 8
+        for (int64_t i = warp; i < count; i += 32) v += part[i * ld + c];
     sums[warp][lane] = v;
     __syncthreads();
     // transposed, so that a warp joins the sums of one column
@@ -381,8 +471,9 @@ int64_t grad_rows(int64_t rows, int64_t n) {
 
 }  // namespace
 
-vqc_status sum_run(const float* part, int64_t count, int64_t n, void* out0, void* out1, int dtype, cudaStream_t s) {
-    void* args[] = {&part, &count, &n, &out0, &out1, &dtype};
+vqc_status sum_run(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second, void* out0, void* out1, int dtype,
+                   cudaStream_t s) {
+    void* args[] = {&part, &count, &n, &ld, &second, &out0, &out1, &dtype};
     const cudaError_t e = cudaLaunchKernel((const void*)sum_kernel, dim3((unsigned)ceil_div(n, 32), out1 ? 2 : 1),
                                            dim3(1024), args, 0, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "sum launch");
@@ -392,7 +483,7 @@ size_t act_grad_workspace(int64_t rows, int64_t n, bool gated) {
     return align256((size_t)std::max<int64_t>(1, ceil_div(rows, grad_rows(rows, n))) * n * (gated ? 2 : 1) * 4);
 }
 
-vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, cudaStream_t s) {
+vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
     ActGrad a = a0;
     const bool sums = a.sum[0] != nullptr;
     float* part = sums ? static_cast<float*>(ws) : nullptr;
@@ -411,7 +502,22 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, cudaStream
         const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(256), args, 0, s);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
-    return sums ? sum_run(part, blocks, a.n, a.sum[0], a.gated ? a.sum[1] : nullptr, a.dtype, s) : VQC_OK;
+    if (!sums) return VQC_OK;
+    // A thread of the join adds up to 64 blocks one by one; more take a kernel of their own.
+    if (blocks > 64) {
+        const int64_t ld = a.n * (a.gated ? 2 : 1);
+        return sum_run(part, blocks, a.n, ld, a.n, a.sum[0], a.gated ? a.sum[1] : nullptr, a.dtype, s);
+    }
+    Join& j = joins.j[joins.count++];
+    j.f.m = 1;
+    j.f.n = a.n;
+    j.f.dtype = j.f.out_dtype = a.dtype;
+    j.f.y[0] = a.sum[0];
+    j.f.y[1] = a.gated ? a.sum[1] : nullptr;
+    j.part = part;
+    j.splits = (int)blocks;
+    j.form = a.gated ? PAIR : PLAIN;
+    return VQC_OK;
 }
 
 }  // namespace layers

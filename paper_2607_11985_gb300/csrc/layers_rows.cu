@@ -2,7 +2,7 @@
 // weights are all there is to read, so they stream through registers once.
 //
 // A group of KW warps takes four rows of weights (two of each in GATED form) and
-// up to 8 rows of x; a lane holds 16 bytes of each weight row per step, the
+// up to 4 rows of x; a lane holds 16 bytes of each weight row per step, the
 // group's warps take turns along k.  Sums are packed pairs of floats (even and
 // odd k), joined over the lanes, then over the warps, in a fixed order.
 #include <algorithm>
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
 #pragma unroll
         for (int i = 0; i < kWeights; ++i) acc[r][i] = make_float2(0.f, 0.f);
     if (c0 < n) {
-#pragma unroll(R <= 2 ? 4 : 2)
+#pragma unroll(VEC == 1 ? 8 : 4)
         for (int64_t k = ((int64_t)(warp % kw) * 32 + lane) * VEC; k - lane * VEC < A.k; k += (int64_t)kw * 32 * VEC) {
             const bool in = k < A.k;
             Pairs<T, VEC> pw[kWeights];
@@ -115,8 +115,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
 template <typename T, int VEC, bool GATE> const void* kernel_of(int64_t m) {
     return m == 1   ? (const void*)rows_kernel<T, VEC, 1, GATE>
            : m == 2 ? (const void*)rows_kernel<T, VEC, 2, GATE>
-           : m <= 4 ? (const void*)rows_kernel<T, VEC, 4, GATE>
-                    : (const void*)rows_kernel<T, VEC, 8, GATE>;
+                    : (const void*)rows_kernel<T, VEC, 4, GATE>;
 }
 template <typename T> const void* kernel_as(int64_t m, bool vec, bool gate) {
     constexpr int V = 16 / sizeof(T);
@@ -127,7 +126,7 @@ template <typename T> const void* kernel_as(int64_t m, bool vec, bool gate) {
 }  // namespace
 
 bool rows_takes(const Product& p) {
-    return p.m >= 1 && p.m <= 8 && p.k > 0 && (p.form == PLAIN || p.form == GATED) && !p.a[0].k_outer && !p.b[0].k_outer;
+    return p.m >= 1 && p.m <= 4 && p.k > 0 && (p.form == PLAIN || p.form == GATED) && !p.a[0].k_outer && !p.b[0].k_outer;
 }
 
 vqc_status rows_run(const Product& p, cudaStream_t s) {

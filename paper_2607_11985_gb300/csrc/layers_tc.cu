@@ -1,4 +1,9 @@
-// layers_tc.cu -- products of 16-bit operands on the tensor cores (tcgen05).
+// layers_tc.cu -- products on the tensor cores (tcgen05).
+//
+// Float operands are multiplied as well: each is the sum of three bf16 parts, and
+// the six products of parts down to 2^-16 of the whole are one contraction of
+// six times the depth (what is dropped is about 2^-24 of the magnitudes, as a float's
+// own rounding).
 //
 // One persistent kernel for every form: y = finish(A B^T) with A [m, k] and B
 // [n, k] stored along k or along their outer index (the backward's products
@@ -48,14 +53,20 @@ template <int CG, int BN> struct Shape {
     static constexpr int kTmem = 2 * BN;             // two accumulators, a power of two >= 32
 };
 
+// Maps of the operands: [operand][part].
 struct TcArgs {
-    CUtensorMap ma[2], mb[2];
+    CUtensorMap ma[2][3], mb[2][3];
     Finish f;
+    Exact exact;                // of float operands
     float* part;                // sums of a cut contraction, or NULL
     unsigned* err;
-    int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec;
+    int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec, bf16;
     long long tiles;
 };
+
+// Products of parts of float operands, small ones first: parts of a and b, 2 bits each.
+constexpr unsigned kPartsA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
+constexpr unsigned kPartsB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -262,12 +273,35 @@ __device__ __forceinline__ TileAt tile_at(const TcArgs& A, long long t) {
 // rows, finished and written.  Aligned outputs go straight from the lanes, 32
 // bytes of a row each; others are turned in shared memory so that lanes write
 // neighbouring columns.
-template <bool kGated>
+template <bool kGated, int kParts>
 __device__ __forceinline__ void write16(const TcArgs& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
                                         float (&v)[16], float (&u)[16], float* stage) {
     const Finish& f = A.f;
     const int64_t n = f.n;
     if (col0 >= n) return;
+    if (kParts > 1 && !A.part && row0 + lane < f.m) {
+        float t = 0.f;       // NaN if one of the sums is not finite
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t = fmaf(v[i], 0.f, kGated ? fmaf(u[i], 0.f, t) : t);
+        if (t != 0.f) {
+            for (int i = 0; i < 16; ++i) {
+                float a = 0.f, b = 0.f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (j == i) { a = v[j]; b = kGated ? u[j] : 0.f; }
+                if (col0 + i >= n) break;
+                a = exact_if_not_finite(A.exact, T.which, row0 + lane, col0 + i, a);
+                if (kGated) b = exact_if_not_finite(A.exact, 1, row0 + lane, col0 + i, b);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (j == i) {
+                        v[j] = a;
+                        if (kGated) u[j] = b;
+                    }
+            }
+        }
+    }
+    if (kParts > 1) __syncwarp();
     if (A.vec && col0 + 16 <= n) {
         const int64_t row = row0 + lane;
         if (A.part) {
@@ -326,7 +360,7 @@ __device__ __forceinline__ void write16(const TcArgs& A, const TileAt& T, int64_
     __syncwarp();
 }
 
-template <int CG, int BN, bool kGated>
+template <int CG, int BN, bool kGated, int kParts>
 __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs A) {
     using S = Shape<CG, BN>;
     constexpr int NS = S::kStages;
@@ -354,8 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         for (int i = 0; i < 2; ++i) {
-            tma_prefetch(&A.ma[i]);
-            tma_prefetch(&A.mb[i]);
+            tma_prefetch(&A.ma[i][0]);
+            tma_prefetch(&A.mb[i][0]);
         }
     }
     if (warp == 2) {
@@ -380,7 +414,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     tc_fence_after();
     const uint32_t tmem = *tslot;
 
-    const int kblocks = A.kblocks * (A.form == SUM ? 2 : 1);
+    constexpr int kPairs = kParts == 3 ? 6 : 1;      // products of parts per product
+    const int kblocks = A.kblocks * kPairs * (A.form == SUM ? 2 : 1);
     const long long first = blockIdx.x / CG, step = gridDim.x / CG;
     // a role that gives up tells the others, in both CTAs
     auto give_up = [&]() {
@@ -401,14 +436,20 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
                 const int m0 = T.m * BM * CG + (int)rank * BM;
                 const int n0 = T.n * (kGated ? BN / 2 : BN) + (kGated ? 0 : (int)rank * (BN / CG));
-                for (int kb = kb0; kb < kb1; ++kb) {
+                int term = kb0 / A.kblocks, k0 = (kb0 - term * A.kblocks) * BK;
+                for (int kb = kb0; kb < kb1; ++kb, k0 += BK) {
+                    if (k0 >= A.kblocks * BK) {
+                        ++term;
+                        k0 = 0;
+                    }
                     if (!mbar_wait(empty + 8 * s, ph ^ 1, gave_up)) {
                         ok = false;
                         break;
                     }
-                    const int term = kb >= A.kblocks ? 1 : 0, k0 = (kb - term * A.kblocks) * BK;
-                    const CUtensorMap* ma = &A.ma[T.which + term];
-                    const CUtensorMap* mb = &A.mb[T.which + term];
+                    const int sum = term >= kPairs ? 1 : 0, pair = term - sum * kPairs;
+                    const int pa = kPairs == 6 ? kPartsA >> (2 * pair) & 3 : 0, pb = kPairs == 6 ? kPartsB >> (2 * pair) & 3 : 0;
+                    const CUtensorMap* ma = &A.ma[T.which + sum][pa];
+                    const CUtensorMap* mb = &A.mb[T.which + sum][pb];
                     const uint32_t sa = base + s * S::kStage, sb = sa + kStageA;
                     const uint32_t bar = CG == 2 ? at_cta(full + 8 * s, 0) : full + 8 * s;
                     if (rank == 0)
@@ -423,10 +464,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                     }
                     if (kGated) {
                         if (CG == 2) {
-                            tma_load<CG>(sb, &A.mb[rank], k0, n0, bar);
+                            tma_load<CG>(sb, &A.mb[rank][pb], k0, n0, bar);
                         } else {
-                            tma_load<CG>(sb, &A.mb[0], k0, n0, bar);
-                            tma_load<CG>(sb + S::kStageB / 2, &A.mb[1], k0, n0, bar);
+                            tma_load<CG>(sb, &A.mb[0][pb], k0, n0, bar);
+                            tma_load<CG>(sb + S::kStageB / 2, &A.mb[1][pb], k0, n0, bar);
                         }
                     } else if (A.b_mn) {
 #pragma unroll
@@ -454,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = (1u << 4) | ((A.f.dtype == VQC_BF16 ? 1u : 0u) << 7) | ((A.f.dtype == VQC_BF16 ? 1u : 0u) << 10) |
+            const uint32_t idesc = (1u << 4) | ((uint32_t)A.bf16 << 7) | ((uint32_t)A.bf16 << 10) |
                                    ((uint32_t)A.a_mn << 15) | ((uint32_t)A.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
                                    ((uint32_t)(BM * CG >> 4) << 24);
             const uint32_t step_a = A.a_mn ? 2048 >> 4 : 32 >> 4, step_b = A.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -524,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 tmem_ld(tmem + lanes + acc * BN + c, v);
                 if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
                 tmem_wait();
-                write16<kGated>(A, T, row0, n0 + c, lane, v, u, stage);
+                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, stage);
             }
             tc_fence_before();
             __syncwarp();
@@ -559,6 +600,54 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
 
 __device__ unsigned g_layers_err;
 
+// A float as the sum of three bf16, 8 bits of it each, rounded to nearest: exact for
+// normal results.  A value that is not finite is its own first part (and the sums
+// that it enters are worked out again, see Exact); one that would round to
+// infinity is cut instead.
+__device__ __forceinline__ void bf16_parts(float x, uint16_t (&o)[3]) {
+    float rest = x;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        __nv_bfloat16 h = __float2bfloat16(rest);
+        uint16_t bits = __bfloat16_as_ushort(h);
+        if ((bits & 0x7fff) == 0x7f80 && fabsf(rest) <= 3.4028234e38f) bits -= 1;
+        o[i] = bits;
+        rest = (bits & 0x7f80) == 0x7f80 ? 0.f : rest - __uint_as_float((uint32_t)bits << 16);
+    }
+}
+
+// [rows, cols] of floats as three matrices of parts, rows of `ld_to` elements (a multiple
+// of 8): 8 elements per thread.
+__global__ void __launch_bounds__(256) parts_kernel(const float* from, int64_t ld, int64_t rows, int64_t cols, uint16_t* to,
+                                                    int64_t ld_to, int vec) {
+    const int64_t across = ld_to / 8, plane = rows * ld_to, count = rows * across, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < count; e += step) {
+        const int64_t r = e / across, c = e % across * 8;
+        const float* p = from + r * ld + c;
+        float v[8];
+        if (vec && c + 8 <= cols) {
+            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? p[i] : 0.f;
+        }
+        uint32_t w[3][4];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            uint16_t a[3], b[3];
+            bf16_parts(v[i], a);
+            bf16_parts(v[i + 1], b);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) w[q][i / 2] = (uint32_t)a[q] | (uint32_t)b[q] << 16;
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            *reinterpret_cast<uint4*>(to + q * plane + r * ld_to + c) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    }
+}
+
 // 16-bit copy of [rows, cols] with rows of `ld_to` elements (a multiple of 8)
 __global__ void __launch_bounds__(256) align_kernel(const uint16_t* from, int64_t ld, int64_t rows, int64_t cols, uint16_t* to,
                                                     int64_t ld_to) {
@@ -592,16 +681,18 @@ bool make_map(CUtensorMap* m, const Operand& o, int dtype, int64_t outer, int64_
     const cuuint64_t dims[2] = {(cuuint64_t)(o.k_outer ? outer : k), (cuuint64_t)(o.k_outer ? k : outer)};
     const cuuint64_t strides[1] = {(cuuint64_t)o.ld * 2};
     const cuuint32_t boxes[2] = {64, (cuuint32_t)(o.k_outer ? BK : box)}, one[2] = {1, 1};
-    return enc(m, dtype == VQC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+    return enc(m, dtype != VQC_F16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
                const_cast<void*>(o.p), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// TMA reads rows at multiples of 16 bytes; other operands are copied first.
-bool ready(const Operand& o, bool aligned) { return aligned && o.ld % 8 == 0; }
+// TMA reads rows at multiples of 16 bytes; other operands are copied first, and
+// float operands are written as three bf16 parts.
+bool ready(const Operand& o, int dtype, bool aligned) { return dtype != VQC_F32 && aligned && o.ld % 8 == 0; }
 int64_t copy_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
-size_t copy_bytes(const Operand& o, int64_t outer, int64_t k) {
-    return align256((size_t)(o.k_outer ? k : outer) * copy_ld(o.k_outer ? outer : k) * 2);
+int parts_of(int dtype) { return dtype == VQC_F32 ? 3 : 1; }
+size_t copy_bytes(const Operand& o, int dtype, int64_t outer, int64_t k) {
+    return align256((size_t)(o.k_outer ? k : outer) * copy_ld(o.k_outer ? outer : k) * 2 * parts_of(dtype));
 }
 
 struct Choice {
@@ -615,7 +706,7 @@ struct Choice {
 Choice choose(const Product& p) {
     static const struct { int cg, bn, stage; } kTiles[] = {{2, 256, 560}, {2, 128, 400}, {1, 128, 512}, {1, 64, 384}};
     const int sms = sm_count();
-    const int64_t kblocks = ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1);
+    const int64_t kblocks = ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * (p.f.dtype == VQC_F32 ? 6 : 1);
     Choice best{1, 64, 1};
     double least = 1e300;
     for (const auto& t : kTiles) {
@@ -637,13 +728,13 @@ Choice choose(const Product& p) {
     return best;
 }
 
-template <int CG, int BN, bool kGated> cudaError_t launch_tc(const TcArgs& a, cudaStream_t s) {
+template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const TcArgs& a, cudaStream_t s) {
     using S = Shape<CG, BN>;
     static std::atomic<unsigned long long> prepared{0};    // devices whose limit is raised
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(prepared.load() >> (dev & 63) & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute((const void*)tc_kernel<CG, BN, kGated>,
+        const cudaError_t e = cudaFuncSetAttribute((const void*)tc_kernel<CG, BN, kGated, kParts>,
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         if (e != cudaSuccess) return e;
         prepared.fetch_or(1ull << (dev & 63));
@@ -660,34 +751,39 @@ template <int CG, int BN, bool kGated> cudaError_t launch_tc(const TcArgs& a, cu
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tc_kernel<CG, BN, kGated>, a);
+    return cudaLaunchKernelEx(&cfg, tc_kernel<CG, BN, kGated, kParts>, a);
 }
 
-template <bool kGated> cudaError_t launch_choice(const Choice& c, const TcArgs& a, cudaStream_t s) {
-    if (c.cg == 2) return c.bn == 256 ? launch_tc<2, 256, kGated>(a, s) : launch_tc<2, 128, kGated>(a, s);
-    return c.bn == 128 ? launch_tc<1, 128, kGated>(a, s) : launch_tc<1, 64, kGated>(a, s);
+template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, const TcArgs& a, cudaStream_t s) {
+    if (c.cg == 2) return c.bn == 256 ? launch_tc<2, 256, kGated, kParts>(a, s) : launch_tc<2, 128, kGated, kParts>(a, s);
+    return c.bn == 128 ? launch_tc<1, 128, kGated, kParts>(a, s) : launch_tc<1, 64, kGated, kParts>(a, s);
 }
 
 }  // namespace
 
+// Float products come here where six products of parts (and writing the parts)
+// take less time than float FMAs.
 bool tc_takes(const Product& p) {
     constexpr int64_t kMost = 1 << 30;
-    return p.f.dtype != VQC_F32 && p.m > 0 && p.k > 0 && p.m < kMost && p.n < kMost && p.k < kMost;
+    if (p.m <= 0 || p.k <= 0 || p.m >= kMost || p.n >= kMost || p.k >= kMost) return false;
+    if (p.f.dtype != VQC_F32) return true;
+    const double flops = 2.0 * p.m * p.n * p.k * (p.form == PLAIN ? 1 : 2);
+    return flops >= 5e8 && p.k >= 64 && std::min(p.m, p.n) >= 64;
 }
 
 size_t tc_workspace(const Product& p, bool aligned) {
     size_t bytes = 0;
     const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == SUM || p.form == GATED ? 2 : 1;
     for (int i = 0; i < na; ++i)
-        if (!ready(p.a[i], aligned)) bytes += copy_bytes(p.a[i], p.m, p.k);
+        if (!ready(p.a[i], p.f.dtype, aligned)) bytes += copy_bytes(p.a[i], p.f.dtype, p.m, p.k);
     for (int i = 0; i < nb; ++i)
-        if (!ready(p.b[i], aligned)) bytes += copy_bytes(p.b[i], p.n, p.k);
+        if (!ready(p.b[i], p.f.dtype, aligned)) bytes += copy_bytes(p.b[i], p.f.dtype, p.n, p.k);
     const Choice c = choose(p);
     if (c.splits > 1) bytes += align256((size_t)c.splits * (p.form == GATED || p.form == PAIR ? 2 : 1) * p.m * p.n * 4);
     return bytes;
 }
 
-vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
+vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
     TcArgs a{};
     char* at = static_cast<char*>(ws);
     size_t left = ws ? ws_bytes : 0;
@@ -699,32 +795,45 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
         return r;
     };
     const Choice c = choose(p);
-    const bool gated = p.form == GATED;
+    const bool gated = p.form == GATED, split = p.f.dtype == VQC_F32;
     const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == SUM || gated ? 2 : 1;
+    const int parts = parts_of(p.f.dtype);
     for (int side = 0; side < 2; ++side)
         for (int i = 0; i < (side ? nb : na); ++i) {
             Operand o = side ? p.b[i] : p.a[i];
             const int64_t outer = side ? p.n : p.m;
-            if (!ready(o, aligned_to(o.p, 16))) {
-                void* to = take(copy_bytes(o, outer, p.k));
+            int64_t rows = o.k_outer ? p.k : outer, cols = o.k_outer ? outer : p.k, ld = o.ld, ld_to = copy_ld(cols);
+            if (!ready(o, p.f.dtype, aligned_to(o.p, 16))) {
+                void* to = take(copy_bytes(o, p.f.dtype, outer, p.k));
                 if (!to) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
-                int64_t rows = o.k_outer ? p.k : outer, cols = o.k_outer ? outer : p.k, ld = o.ld, ld_to = copy_ld(cols);
                 const void* from = o.p;
-                void* args[] = {&from, &ld, &rows, &cols, &to, &ld_to};
-                const cudaError_t e = cudaLaunchKernel((const void*)align_kernel, dim3((unsigned)std::min<int64_t>(rows, 16LL * sm_count())),
+                int vec = ld % 4 == 0 && aligned_to(from, 16);
+                void* args[] = {&from, &ld, &rows, &cols, &to, &ld_to, &vec};
+                const int64_t grid = split ? std::min<int64_t>(ceil_div(rows * ld_to / 8, 256), 8LL * sm_count()) : std::min<int64_t>(rows, 16LL * sm_count());
+                const cudaError_t e = cudaLaunchKernel(split ? (const void*)parts_kernel : (const void*)align_kernel, dim3((unsigned)grid),
                                                        dim3(256), args, 0, s);
                 if (e != cudaSuccess) return cuda_error(e, "operand copy launch");
                 o.p = to;
                 o.ld = ld_to;
             }
             const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
-            if (!make_map(side ? &a.mb[i] : &a.ma[i], o, p.f.dtype, outer, p.k, box))
-                return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
+            for (int q = 0; q < parts; ++q) {
+                Operand part = o;
+                part.p = static_cast<const uint16_t*>(o.p) + q * rows * ld_to;
+                if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
+                    return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
+            }
         }
-    if (na == 1) a.ma[1] = a.ma[0];
-    if (nb == 1) a.mb[1] = a.mb[0];
+    for (int q = 0; q < 3; ++q) {      // the maps that no operand has of its own
+        if (q >= parts) { a.ma[0][q] = a.ma[0][0]; a.mb[0][q] = a.mb[0][0]; }
+        if (na == 1) a.ma[1][q] = a.ma[0][q];
+        else if (q >= parts) a.ma[1][q] = a.ma[1][0];
+        if (nb == 1) a.mb[1][q] = a.mb[0][q];
+        else if (q >= parts) a.mb[1][q] = a.mb[1][0];
+    }
     a.f = p.f;
     a.form = p.form;
+    a.bf16 = p.f.dtype != VQC_F16;
     a.splits = c.splits;
     a.tiles_m = (int)ceil_div(p.m, BM * c.cg);
     a.tiles_n = (int)ceil_div(p.n, gated ? c.bn / 2 : c.bn);
@@ -732,9 +841,20 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
     a.a_mn = p.a[0].k_outer;
     a.b_mn = p.b[0].k_outer;
     a.tiles = (long long)a.tiles_m * a.tiles_n * a.splits * (p.form == PAIR ? 2 : 1);
+    if (split) {
+        for (int i = 0; i < 2; ++i) { a.exact.a[i] = p.a[i]; a.exact.b[i] = p.b[i]; }
+        a.exact.k = p.k;
+        a.exact.form = p.form;
+    }
     if (c.splits > 1) {
         a.part = static_cast<float*>(take(align256((size_t)c.splits * (gated || p.form == PAIR ? 2 : 1) * p.m * p.n * 4)));
         if (!a.part) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
+        Join& j = joins.j[joins.count++];
+        j.f = p.f;
+        j.exact = a.exact;
+        j.part = a.part;
+        j.splits = c.splits;
+        j.form = p.form;
     }
     // every row of every output on a 32-byte boundary
     const int64_t eo = (int64_t)elem_size(p.f.out_dtype);
@@ -747,9 +867,9 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s) {
     cudaError_t e = cudaGetSymbolAddress(&ep, g_layers_err);
     if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
     a.err = static_cast<unsigned*>(ep);
-    e = gated ? launch_choice<true>(c, a, s) : launch_choice<false>(c, a, s);
-    if (e != cudaSuccess) return cuda_error(e, "tensor-core product launch");
-    return a.part ? join_run(p, a.part, a.splits, s) : VQC_OK;
+    if (split) e = gated ? launch_choice<true, 3>(c, a, s) : launch_choice<false, 3>(c, a, s);
+    else e = gated ? launch_choice<true, 1>(c, a, s) : launch_choice<false, 1>(c, a, s);
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "tensor-core product launch");
 }
 
 }  // namespace layers

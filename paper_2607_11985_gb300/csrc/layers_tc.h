@@ -8,15 +8,11 @@ namespace layers {
 
 bool tc_takes(const Product& p);
 size_t tc_workspace(const Product& p, bool aligned);
-vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, cudaStream_t s);
+vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s);
 
-// Products with up to 8 rows.
+// Products with up to 4 rows.
 bool rows_takes(const Product& p);
 vqc_status rows_run(const Product& p, cudaStream_t s);
-
-// Sums of a contraction that was cut, [splits][one or two products][m][n], joined
-// in the order of the cuts and finished.
-vqc_status join_run(const Product& p, const float* part, int splits, cudaStream_t s);
 
 }  // namespace layers
 
