@@ -127,17 +127,47 @@ __device__ __forceinline__ float exact_if_not_finite(const Exact& x, int which, 
     return fabsf(v) <= 3.4028234e38f ? v : exact_sum(x, which, row, col);
 }
 
-// The end of a product for one element: v0 (and v1, gated) are its sums.
-__device__ __forceinline__ void finish_one(const Finish& f, int which, int64_t row, int64_t col, float v0, float v1) {
-    if (f.bias[which]) v0 += load_as(f.bias[which], f.dtype, col);
-    if (f.gated && f.bias[1]) v1 += load_as(f.bias[1], f.dtype, col);
+// The end of a product for W neighbouring elements of a row (1, or 4 where a row holds a
+// multiple of 4: outputs are then written at once): v (and u, gated) are the sums.
+template <int W>
+__device__ __forceinline__ void finish_some(const Finish& f, int which, int64_t row, int64_t col, float (&v)[W], float (&u)[W]) {
     const int64_t at = row * f.n + col;
-    if (f.z[which]) f.z[which][at] = v0;
-    if (f.gated && f.z[1]) f.z[1][at] = v1;
-    float r = act_value(f.act, v0);
-    if (f.gated) r *= v1;
-    if (f.res) r += load_as(f.res, f.out_dtype, row * f.ld_res + col);
-    store_as(f.y[which], f.out_dtype, at, r);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if (f.bias[which]) v[i] += load_as(f.bias[which], f.dtype, col + i);
+        if (f.gated && f.bias[1]) u[i] += load_as(f.bias[1], f.dtype, col + i);
+    }
+    if (f.z[which]) {
+        if constexpr (W == 4) {
+            *reinterpret_cast<float4*>(f.z[which] + at) = make_float4(v[0], v[1], v[2], v[3]);
+            if (f.gated && f.z[1]) *reinterpret_cast<float4*>(f.z[1] + at) = make_float4(u[0], u[1], u[2], u[3]);
+        } else {
+            f.z[which][at] = v[0];
+            if (f.gated && f.z[1]) f.z[1][at] = u[0];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        v[i] = act_value(f.act, v[i]);
+        if (f.gated) v[i] *= u[i];
+        if (f.res) v[i] += load_as(f.res, f.out_dtype, row * f.ld_res + col + i);
+    }
+    if constexpr (W == 4) {
+        if (f.out_dtype == VQC_F32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(f.y[which]) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            const bool b = f.out_dtype == VQC_BF16;
+            const uint2 r = make_uint2(b ? pack2<__nv_bfloat16>(v[0], v[1]) : pack2<__half>(v[0], v[1]),
+                                       b ? pack2<__nv_bfloat16>(v[2], v[3]) : pack2<__half>(v[2], v[3]));
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(f.y[which]) + at) = r;
+        }
+    } else {
+        store_as(f.y[which], f.out_dtype, at, v[0]);
+    }
+}
+__device__ __forceinline__ void finish_one(const Finish& f, int which, int64_t row, int64_t col, float v0, float v1) {
+    float v[1] = {v0}, u[1] = {v1};
+    finish_some<1>(f, which, row, col, v, u);
 }
 
 }  // namespace layers

@@ -181,27 +181,51 @@ __global__ void __launch_bounds__(NT) product_kernel(const __grid_constant__ Pro
 }
 
 // Sums of cut contractions joined in the order of the cuts, then finished: job
-// blockIdx.y / 2, its product blockIdx.y % 2 (PAIR).
+// blockIdx.y / 2, its product blockIdx.y % 2 (PAIR).  Four neighbouring outputs per
+// thread where a row holds a multiple of four.
+template <int W> __device__ __forceinline__ void join_at(const Join& j, int which, int64_t size, int64_t stride, int64_t e) {
+    const float* p = j.part + which * size + e;
+    float v0[W], v1[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) v0[i] = v1[i] = 0.f;
+    auto add = [&](const float* q, float (&v)[W]) {
+        if constexpr (W == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(q);
+            v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
+        } else {
+            v[0] += *q;
+        }
+    };
+    if (j.form == GATED) {
+#pragma unroll 4
+        for (int s = 0; s < j.splits; ++s) {
+            add(p + s * stride, v0);
+            add(p + s * stride + size, v1);
+        }
+    } else {
+#pragma unroll 8
+        for (int s = 0; s < j.splits; ++s) add(p + s * stride, v0);
+    }
+    // most outputs count less than 2^32 elements: a short division
+    const int64_t row = size >> 32 ? e / j.f.n : (int64_t)((uint32_t)e / (uint32_t)j.f.n), col = e - row * j.f.n;
+    if (j.exact.k) {
+        for (int i = 0; i < W; ++i) {
+            v0[i] = exact_if_not_finite(j.exact, which, row, col + i, v0[i]);
+            if (j.form == GATED) v1[i] = exact_if_not_finite(j.exact, 1, row, col + i, v1[i]);
+        }
+    }
+    finish_some<W>(j.f, which, row, col, v0, v1);
+}
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Joins J) {
     const Join& j = J.j[blockIdx.y >> 1];
     const int which = blockIdx.y & 1;
     if (which && j.form != PAIR) return;
-    const int64_t size = j.f.m * j.f.n, step = (int64_t)gridDim.x * blockDim.x;
+    const int64_t size = j.f.m * j.f.n, step = (int64_t)gridDim.x * blockDim.x, at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t stride = size * (j.form == GATED || j.form == PAIR ? 2 : 1);
-    for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < size; e += step) {
-        const float* p = j.part + which * size + e;
-        float v0 = 0.f, v1 = 0.f;
-#pragma unroll 8
-        for (int s = 0; s < j.splits; ++s) {
-            v0 += p[s * stride];
-            if (j.form == GATED) v1 += p[s * stride + size];
-        }
-        const int64_t row = e / j.f.n, col = e % j.f.n;
-        if (j.exact.k) {
-            v0 = exact_if_not_finite(j.exact, which, row, col, v0);
-            if (j.form == GATED) v1 = exact_if_not_finite(j.exact, 1, row, col, v1);
-        }
-        finish_one(j.f, which, row, col, v0, v1);
+    if (j.f.n % 4 == 0) {
+        for (int64_t e = 4 * at; e < size; e += 4 * step) join_at<4>(j, which, size, stride, e);
+    } else {
+        for (int64_t e = at; e < size; e += step) join_at<1>(j, which, size, stride, e);
     }
 }
 
