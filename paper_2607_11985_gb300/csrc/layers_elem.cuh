@@ -46,6 +46,12 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return pair_of(r);
 }
 
+__device__ __forceinline__ float exp2f_fast(float x) {
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // two neighbouring 16-bit elements in a word
 template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
 template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w) {
@@ -74,14 +80,34 @@ __device__ __forceinline__ void store_as(void* p, int dtype, int64_t i, float v)
     else static_cast<__half*>(p)[i] = __float2half(v);
 }
 
+// 1 / (1 + exp(-z)), exp by the hardware's power of two: relative error about
+// |z| 2^-23, 1 and 0 beyond the range of exp.
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + exp2f_fast(-1.4426950408889634f * z)); }
+
+// The normal distribution function of -|z| and exp(-z^2 / 2): erfc(x) = exp(-x^2) P(t),
+// t = 1 / (1 + 0.3275911 x), by Abramowitz and Stegun 7.1.26 (absolute error of the
+// error function at most 1.5e-7), x = |z| / sqrt(2).
+__device__ __forceinline__ float2 normal_tail(float z) {
+    const float t = __fdividef(1.f, fmaf(0.23164189f, fabsf(z), 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float e = exp2f_fast(-0.72134752044448170f * z * z);
+    return make_float2(0.5f * p * t * e, e);
+}
+
 // act(z) in float.  A NaN stays one.
 __device__ __forceinline__ float act_value(int act, float z) {
     switch (act) {
         case VQC_ACT_RELU: return z < 0.f ? 0.f : z;
-        case VQC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case VQC_ACT_SILU: return z / (1.f + expf(-z));
+        case VQC_ACT_GELU: {
+            const float q = normal_tail(z).x;
+            return z * (z < 0.f ? q : 1.f - q);
+        }
+        case VQC_ACT_SILU: return z * logistic(z);
         case VQC_ACT_TANH: return tanhf(z);
-        case VQC_ACT_SIGMOID: return 1.f / (1.f + expf(-z));
+        case VQC_ACT_SIGMOID: return logistic(z);
         default: return z;
     }
 }
@@ -91,19 +117,20 @@ __device__ __forceinline__ float2 act_both(int act, float z) {
     switch (act) {
         case VQC_ACT_RELU: return z < 0.f ? make_float2(0.f, 0.f) : make_float2(z, z == 0.f ? 0.f : 1.f);
         case VQC_ACT_GELU: {
-            const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-            return make_float2(z * p, p + z * (0.39894228040143268f * expf(-0.5f * z * z)));
+            const float2 t = normal_tail(z);
+            const float p = z < 0.f ? t.x : 1.f - t.x;
+            return make_float2(z * p, fmaf(z, 0.39894228040143268f * t.y, p));
         }
         case VQC_ACT_SILU: {
-            const float p = 1.f / (1.f + expf(-z));
-            return make_float2(z * p, p * (1.f + z * (1.f - p)));
+            const float p = logistic(z);
+            return make_float2(z * p, p * fmaf(z, 1.f - p, 1.f));
         }
         case VQC_ACT_TANH: {
             const float a = tanhf(z);
             return make_float2(a, 1.f - a * a);
         }
         case VQC_ACT_SIGMOID: {
-            const float p = 1.f / (1.f + expf(-z));
+            const float p = logistic(z);
             return make_float2(p, p * (1.f - p));
         }
         default: return make_float2(z, 1.f);

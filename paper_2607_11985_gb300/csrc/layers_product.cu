@@ -5,6 +5,7 @@
 // layers_rows.cu; what is left here are float products of moderate size, for
 // every layout, stride and size, with sums in a fixed order.
 #include <algorithm>
+#include <atomic>
 
 #include "layers_elem.cuh"
 #include "layers_tc.h"
@@ -17,13 +18,17 @@ vqc_status cuda_error(cudaError_t e, const char* what) {
 }
 
 int sm_count() {
+    static std::atomic<int> known[64];
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
-        cudaGetLastError();
-        return 152;
+    if (cudaGetDevice(&dev) == cudaSuccess) {
+        if (dev < 64 && (sms = known[dev].load())) return sms;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0) {
+            if (dev < 64) known[dev].store(sms);
+            return sms;
+        }
     }
-    return sms;
+    cudaGetLastError();
+    return 152;
 }
 
 namespace {

@@ -54,8 +54,8 @@ template <int CG, int BN> struct Shape {
 };
 
 // Maps of the operands: [operand][part].
-struct TcArgs {
-    CUtensorMap ma[2][3], mb[2][3];
+template <int kParts> struct TcArgs {
+    CUtensorMap ma[2][kParts], mb[2][kParts];
     Finish f;
     Exact exact;                // of float operands
     float* part;                // sums of a cut contraction, or NULL
@@ -212,24 +212,27 @@ __device__ __forceinline__ void store16(void* base, int dtype, int64_t at, const
     }
     store32(static_cast<char*>(base) + 2 * at, r);
 }
-__device__ __forceinline__ void add16(const void* base, int dtype, int64_t at, float (&v)[16]) {
+// 16 elements of the residual as they lie in memory
+struct Res16 {
+    uint32_t w[2][8];
+};
+__device__ __forceinline__ void load_res(const void* base, int dtype, int64_t at, Res16& r) {
+    if (dtype == VQC_F32) {
+        load32(static_cast<const float*>(base) + at, r.w[0]);
+        load32(static_cast<const float*>(base) + at + 8, r.w[1]);
+    } else {
+        load32(static_cast<const char*>(base) + 2 * at, r.w[0]);
+    }
+}
+__device__ __forceinline__ void add_res(const Res16& r, int dtype, float (&v)[16]) {
     if (dtype == VQC_F32) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t r[8];
-            load32(static_cast<const float*>(base) + at + 8 * h, r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * h + i] += __uint_as_float(r[i]);
-        }
+        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(r.w[i / 8][i % 8]);
         return;
     }
-    uint32_t r[8];
-    load32(static_cast<const char*>(base) + 2 * at, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float2 p;
-        if (dtype == VQC_BF16) p = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r[i]));
-        else p = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+        const float2 p = dtype == VQC_BF16 ? unpack2<__nv_bfloat16>(r.w[0][i]) : unpack2<__half>(r.w[0][i]);
         v[2 * i] += p.x;
         v[2 * i + 1] += p.y;
     }
@@ -255,7 +258,7 @@ struct TileAt {
 };
 // Tiles in groups of 16 tiles of rows, so that the CTAs at work at one time share
 // rows of both operands in the L2.
-__device__ __forceinline__ TileAt tile_at(const TcArgs& A, long long t) {
+template <int P> __device__ __forceinline__ TileAt tile_at(const TcArgs<P>& A, long long t) {
     TileAt r;
     const long long plane = (long long)A.tiles_m * A.tiles_n;
     const int p = (int)(t / plane);
@@ -274,8 +277,8 @@ __device__ __forceinline__ TileAt tile_at(const TcArgs& A, long long t) {
 // bytes of a row each; others are turned in shared memory so that lanes write
 // neighbouring columns.
 template <bool kGated, int kParts>
-__device__ __forceinline__ void write16(const TcArgs& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
-                                        float (&v)[16], float (&u)[16], float* stage) {
+__device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
+                                        float (&v)[16], float (&u)[16], const Res16& res, float* stage) {
     const Finish& f = A.f;
     const int64_t n = f.n;
     if (col0 >= n) return;
@@ -332,7 +335,7 @@ __device__ __forceinline__ void write16(const TcArgs& A, const TileAt& T, int64_
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] *= u[i];
         }
-        if (f.res) add16(f.res, f.out_dtype, row * f.ld_res + col0, v);
+        if (!kGated && f.res) add_res(res, f.out_dtype, v);
         store16(f.y[T.which], f.out_dtype, at, v);
         return;
     }
@@ -361,7 +364,7 @@ __device__ __forceinline__ void write16(const TcArgs& A, const TileAt& T, int64_
 }
 
 template <int CG, int BN, bool kGated, int kParts>
-__global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs A) {
+__global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs<kParts> A) {
     using S = Shape<CG, BN>;
     constexpr int NS = S::kStages;
     extern __shared__ __align__(1024) unsigned char sm[];
@@ -558,14 +561,23 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             tc_fence_after();
             const int64_t row0 = ((int64_t)T.m * CG + rank) * BM + quad * 32;
             const int64_t n0 = (int64_t)T.n * kCols;
+            // the residual is read one step ahead
+            const bool ahead = !kGated && A.f.res && A.vec && !A.part && row0 + lane < A.f.m;
+            auto fetch = [&](int c, Res16& r) {
+                if (ahead && n0 + c + 16 <= A.f.n) load_res(A.f.res, A.f.out_dtype, (row0 + lane) * A.f.ld_res + n0 + c, r);
+            };
+            Res16 res, next;
+            fetch(half * (kCols / 2), next);
 #pragma unroll 1
             for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 16) {
                 float v[16], u[16];
+                res = next;
+                if (c + 16 < (half + 1) * (kCols / 2)) fetch(c + 16, next);
                 __syncwarp();
                 tmem_ld(tmem + lanes + acc * BN + c, v);
                 if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
                 tmem_wait();
-                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, stage);
+                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage);
             }
             tc_fence_before();
             __syncwarp();
@@ -599,6 +611,22 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
 }
 
 __device__ unsigned g_layers_err;
+
+// Its address on the current device, looked up once per device.
+cudaError_t error_word(unsigned** p) {
+    static std::atomic<void*> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    void* q = dev < 64 ? known[dev].load() : nullptr;
+    if (!q) {
+        e = cudaGetSymbolAddress(&q, g_layers_err);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) known[dev].store(q);
+    }
+    *p = static_cast<unsigned*>(q);
+    return cudaSuccess;
+}
 
 // A float as the sum of three bf16, 8 bits of it each, rounded to nearest: exact for
 // normal results.  A value that is not finite is its own first part (and the sums
@@ -703,7 +731,7 @@ struct Choice {
 // stage of 64 costs its products (8192 per cycle and SM) or its bytes (about 64
 // per cycle and SM from the L2), whichever is longer, a tile its start and end, a
 // cut the traffic of its sums.
-Choice choose(const Product& p) {
+Choice choose_new(const Product& p) {
     static const struct { int cg, bn, stage; } kTiles[] = {{2, 256, 560}, {2, 128, 400}, {1, 128, 512}, {1, 64, 384}};
     const int sms = sm_count();
     const int64_t kblocks = ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * (p.f.dtype == VQC_F32 ? 6 : 1);
@@ -728,7 +756,25 @@ Choice choose(const Product& p) {
     return best;
 }
 
-template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const TcArgs& a, cudaStream_t s) {
+// The choices of the sizes that a thread asked for last.
+Choice choose(const Product& p) {
+    struct Known {
+        int64_t m = 0, n = 0, k = 0;
+        int form = -1, dtype = -1, sms = 0;
+        Choice c;
+    };
+    static thread_local Known known[64];
+    const bool parts = p.f.dtype == VQC_F32;
+    Known& q = known[(uint64_t)(p.m * 0x9E3779B1 + p.n * 0x85EBCA77 + p.k * 0xC2B2AE3D + p.form + 4 * parts) >> 7 & 63];
+    const int sms = sm_count();
+    if (q.m != p.m || q.n != p.n || q.k != p.k || q.form != p.form || q.dtype != parts || q.sms != sms) {
+        q.c = choose_new(p);
+        q.m = p.m; q.n = p.n; q.k = p.k; q.form = p.form; q.dtype = parts; q.sms = sms;
+    }
+    return q.c;
+}
+
+template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const TcArgs<kParts>& a, cudaStream_t s) {
     using S = Shape<CG, BN>;
     static std::atomic<unsigned long long> prepared{0};    // devices whose limit is raised
     int dev = 0;
@@ -754,7 +800,7 @@ template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const T
     return cudaLaunchKernelEx(&cfg, tc_kernel<CG, BN, kGated, kParts>, a);
 }
 
-template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, const TcArgs& a, cudaStream_t s) {
+template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, const TcArgs<kParts>& a, cudaStream_t s) {
     if (c.cg == 2) return c.bn == 256 ? launch_tc<2, 256, kGated, kParts>(a, s) : launch_tc<2, 128, kGated, kParts>(a, s);
     return c.bn == 128 ? launch_tc<1, 128, kGated, kParts>(a, s) : launch_tc<1, 64, kGated, kParts>(a, s);
 }
@@ -783,8 +829,9 @@ size_t tc_workspace(const Product& p, bool aligned) {
     return bytes;
 }
 
-vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
-    TcArgs a{};
+namespace {
+template <int kParts> vqc_status run_parts(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
+    TcArgs<kParts> a;
     char* at = static_cast<char*>(ws);
     size_t left = ws ? ws_bytes : 0;
     auto take = [&](size_t bytes) -> void* {
@@ -795,9 +842,9 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cud
         return r;
     };
     const Choice c = choose(p);
-    const bool gated = p.form == GATED, split = p.f.dtype == VQC_F32;
+    const bool gated = p.form == GATED;
+    constexpr bool split = kParts == 3;
     const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == SUM || gated ? 2 : 1;
-    const int parts = parts_of(p.f.dtype);
     for (int side = 0; side < 2; ++side)
         for (int i = 0; i < (side ? nb : na); ++i) {
             Operand o = side ? p.b[i] : p.a[i];
@@ -817,19 +864,16 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cud
                 o.ld = ld_to;
             }
             const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
-            for (int q = 0; q < parts; ++q) {
+            for (int q = 0; q < kParts; ++q) {
                 Operand part = o;
                 part.p = static_cast<const uint16_t*>(o.p) + q * rows * ld_to;
                 if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
                     return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
             }
         }
-    for (int q = 0; q < 3; ++q) {      // the maps that no operand has of its own
-        if (q >= parts) { a.ma[0][q] = a.ma[0][0]; a.mb[0][q] = a.mb[0][0]; }
+    for (int q = 0; q < kParts; ++q) {      // an operand of both products
         if (na == 1) a.ma[1][q] = a.ma[0][q];
-        else if (q >= parts) a.ma[1][q] = a.ma[1][0];
         if (nb == 1) a.mb[1][q] = a.mb[0][q];
-        else if (q >= parts) a.mb[1][q] = a.mb[1][0];
     }
     a.f = p.f;
     a.form = p.form;
@@ -841,6 +885,8 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cud
     a.a_mn = p.a[0].k_outer;
     a.b_mn = p.b[0].k_outer;
     a.tiles = (long long)a.tiles_m * a.tiles_n * a.splits * (p.form == PAIR ? 2 : 1);
+    a.exact = Exact{};
+    a.part = nullptr;
     if (split) {
         for (int i = 0; i < 2; ++i) { a.exact.a[i] = p.a[i]; a.exact.b[i] = p.b[i]; }
         a.exact.k = p.k;
@@ -863,13 +909,15 @@ vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cud
                    : p.n * eo % 32 == 0 && on32(p.f.y[0]) && on32(p.f.y[1]) &&
                          (!p.f.z[0] || (p.n % 8 == 0 && on32(p.f.z[0]) && on32(p.f.z[1]))) &&
                          (!p.f.res || (p.f.ld_res * eo % 32 == 0 && on32(p.f.res)));
-    void* ep = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(&ep, g_layers_err);
+    cudaError_t e = error_word(&a.err);
     if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
-    a.err = static_cast<unsigned*>(ep);
-    if (split) e = gated ? launch_choice<true, 3>(c, a, s) : launch_choice<false, 3>(c, a, s);
-    else e = gated ? launch_choice<true, 1>(c, a, s) : launch_choice<false, 1>(c, a, s);
+    e = gated ? launch_choice<true, kParts>(c, a, s) : launch_choice<false, kParts>(c, a, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "tensor-core product launch");
+}
+}  // namespace
+
+vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
+    return p.f.dtype == VQC_F32 ? run_parts<3>(p, ws, ws_bytes, joins, s) : run_parts<1>(p, ws, ws_bytes, joins, s);
 }
 
 }  // namespace layers

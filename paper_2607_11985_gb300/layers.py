@@ -16,6 +16,8 @@ supplies device memory and the current stream only.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -77,12 +79,24 @@ def _weight(t, cols, dtype, name):
     return _rows(t, cols, name, dtype)
 
 
-def _workspace(nbytes, name):
-    if nbytes == 0:
-        return None
-    if nbytes == 2 ** 64 - 1:
-        raise ValueError("%s: sizes out of range" % name)
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+def _sized(query):
+    """A workspace query whose answers (functions of sizes, types and alignment) are kept."""
+    @functools.lru_cache(maxsize=4096)
+    def size(*args):
+        nbytes = query(*args)
+        if nbytes == 2 ** 64 - 1:
+            raise ValueError("sizes out of range: %s" % (args,))
+        return nbytes
+    return size
+
+
+_norm_bytes = _sized(B.vqc_layer_norm_workspace_bytes)
+_linear_bytes = _sized(B.vqc_linear_workspace_bytes)
+_gated_bytes = _sized(B.vqc_gated_workspace_bytes)
+
+
+def _workspace(nbytes):
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
 
 
 def _aligned(*tensors):
@@ -120,8 +134,8 @@ def layer_norm_backward(grad_y, x, weight, saved, need_x=True, need_weight=True,
     gb = torch.empty(cols, dtype=x.dtype, device=x.device) if need_bias else None
     ws, nbytes = None, 0
     if need_weight or need_bias:
-        nbytes = B.vqc_layer_norm_workspace_bytes(rows, cols)
-        ws = _workspace(nbytes, "layer_norm_backward")
+        nbytes = _norm_bytes(rows, cols)
+        ws = _workspace(nbytes)
     B.vqc_layer_norm_backward(code, rows, cols, gy.data_ptr(), ld_gy, x2.data_ptr(), ld, _ptr(weight),
                               saved.data_ptr(), _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws), nbytes,
                               _here()[1])
@@ -162,8 +176,8 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, out_d
     y_type = x.dtype if out_dtype is None else out_dtype
     res, ld_res = (None, 0) if residual is None else _rows(residual, out, "residual", y_type, rows)
     y_code = _out_code(x.dtype, y_type)
-    nbytes = B.vqc_linear_workspace_bytes(0, code, y_code, rows, cols, out, ld, ld_w, 0, act, _aligned(x2, w))
-    ws = _workspace(nbytes, "linear_forward")
+    nbytes = _linear_bytes(0, code, y_code, rows, cols, out, ld, ld_w, 0, act, _aligned(x2, w))
+    ws = _workspace(nbytes)
     y = torch.empty(x.shape[:-1] + (out,), dtype=y_type, device=x.device)
     z = torch.empty(rows, out, dtype=torch.float32, device=x.device) if save and act else None
     B.vqc_linear_forward(code, y_code, rows, cols, out, x2.data_ptr(), ld, w.data_ptr(), ld_w, _ptr(bias), act,
@@ -186,9 +200,8 @@ def linear_backward(grad_y, x, weight, saved, activation="none", need_x=True, ne
     gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
     gw = torch.empty(out, cols, dtype=x.dtype, device=x.device) if need_weight else None
     gb = torch.empty(out, dtype=x.dtype, device=x.device) if need_bias else None
-    nbytes = B.vqc_linear_workspace_bytes(1, code, y_code, rows, cols, out, ld, ld_w, ld_gy, act,
-                                          _aligned(x2, w, gy))
-    ws = _workspace(nbytes, "linear_backward")
+    nbytes = _linear_bytes(1, code, y_code, rows, cols, out, ld, ld_w, ld_gy, act, _aligned(x2, w, gy))
+    ws = _workspace(nbytes)
     B.vqc_linear_backward(code, y_code, rows, cols, out, gy.data_ptr(), ld_gy, x2.data_ptr(), ld, w.data_ptr(),
                           ld_w, _ptr(saved), act, _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws), nbytes, _here()[1])
     return gx, gw, gb
@@ -241,8 +254,8 @@ def gated_forward(x, weight_gate, weight_up, bias_gate=None, bias_up=None, activ
     wg, wu, ld_w = _pair(weight_gate, weight_up, cols, x.dtype)
     rows, out = x2.shape[0], wg.shape[0]
     bg, bu = _vector(bias_gate, out, x.dtype, "bias_gate"), _vector(bias_up, out, x.dtype, "bias_up")
-    nbytes = B.vqc_gated_workspace_bytes(0, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
-    ws = _workspace(nbytes, "gated_forward")
+    nbytes = _gated_bytes(0, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
+    ws = _workspace(nbytes)
     h = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=x.device)
     z = torch.empty(2, rows, out, dtype=torch.float32, device=x.device) if save else None
     B.vqc_gated_forward(code, rows, cols, out, x2.data_ptr(), ld, wg.data_ptr(), wu.data_ptr(), ld_w, _ptr(bg),
@@ -264,8 +277,8 @@ def gated_backward(grad_h, x, weight_gate, weight_up, saved, activation="silu", 
     gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
     gw = [torch.empty(out, cols, dtype=x.dtype, device=x.device) if need_weight else None for _ in range(2)]
     gb = [torch.empty(out, dtype=x.dtype, device=x.device) if need_bias else None for _ in range(2)]
-    nbytes = B.vqc_gated_workspace_bytes(1, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
-    ws = _workspace(nbytes, "gated_backward")
+    nbytes = _gated_bytes(1, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
+    ws = _workspace(nbytes)
     B.vqc_gated_backward(code, rows, cols, out, gh.data_ptr(), ld_gh, x2.data_ptr(), ld, wg.data_ptr(),
                          wu.data_ptr(), ld_w, saved.data_ptr(), act, _ptr(gx), _ptr(gw[0]), _ptr(gw[1]),
                          _ptr(gb[0]), _ptr(gb[1]), _ptr(ws), nbytes, _here()[1])
