@@ -238,6 +238,17 @@ __device__ __forceinline__ void add_res(const Res16& r, int dtype, float (&v)[16
     }
 }
 
+// The epilogue keeps the biases of a warp's columns in its staging space (which only
+// outputs that are not aligned use): those of the gate, then those of the other factor.
+constexpr int kBiasUp = 128;
+__device__ __forceinline__ void add_bias(const float* b, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(b + i);
+        v[i] += q.x; v[i + 1] += q.y; v[i + 2] += q.z; v[i + 3] += q.w;
+    }
+}
+
 template <int ACT> __device__ __forceinline__ void act16_as(float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = act_value(ACT, v[i]);
@@ -278,7 +289,7 @@ template <int P> __device__ __forceinline__ TileAt tile_at(const TcArgs<P>& A, l
 // neighbouring columns.
 template <bool kGated, int kParts>
 __device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
-                                        float (&v)[16], float (&u)[16], const Res16& res, float* stage) {
+                                        float (&v)[16], float (&u)[16], const Res16& res, const float* bias, float* stage) {
     const Finish& f = A.f;
     const int64_t n = f.n;
     if (col0 >= n) return;
@@ -316,17 +327,9 @@ __device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T
             }
             return;
         }
-        if (f.bias[T.which]) {
-            const float b = load_as(f.bias[T.which], f.dtype, col0 + (lane & 15));
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += __shfl_sync(~0u, b, i);
-        }
-        if (kGated && f.bias[1]) {
-            const float b = load_as(f.bias[1], f.dtype, col0 + (lane & 15));
-#pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] += __shfl_sync(~0u, b, i);
-        }
         if (row >= f.m) return;
+        if (f.bias[T.which]) add_bias(bias, v);
+        if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
         const int64_t at = row * n + col0;
         if (f.z[T.which]) store16f(f.z[T.which] + at, v);
         if (kGated && f.z[1]) store16f(f.z[1] + at, u);
@@ -554,6 +557,17 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         uint32_t aph = 0;
         for (long long t = first; t < A.tiles; t += step) {
             const TileAt T = tile_at(A, t);
+            if (A.vec && !A.part) {      // biases of this warp's columns
+                __syncwarp();
+                for (int w = 0; w < (kGated ? 2 : 1); ++w) {
+                    const void* from = A.f.bias[kGated ? w : T.which];
+                    if (from)
+                        for (int c = lane; c < kCols / 2; c += 32) {
+                            const int64_t col = (int64_t)T.n * kCols + half * (kCols / 2) + c;
+                            stage[w * kBiasUp + c] = col < A.f.n ? load_as(from, A.f.dtype, col) : 0.f;
+                        }
+                }
+            }
             if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
                 if (lane == 0) give_up();
                 break;
@@ -577,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 tmem_ld(tmem + lanes + acc * BN + c, v);
                 if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
                 tmem_wait();
-                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage);
+                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + c - half * (kCols / 2), stage);
             }
             tc_fence_before();
             __syncwarp();
