@@ -84,8 +84,12 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     b.sums = act_grad_workspace(rows, out, gated);
     const void* none[2] = {nullptr, nullptr};
     void* nothing[2] = {nullptr, nullptr};
-    b.gx = product_workspace(product_gx(dtype, rows, in, out, none, b.ld_dz, none, ld_w, gated, nullptr), aligned);
-    b.gw = product_workspace(product_gw(dtype, rows, in, out, none, b.ld_dz, nullptr, ld_x, gated, nothing), aligned);
+    const Product p[2] = {product_gx(dtype, rows, in, out, none, b.ld_dz, none, ld_w, gated, nullptr),
+                          product_gw(dtype, rows, in, out, none, b.ld_dz, nullptr, ld_x, gated, nothing)};
+    size_t bytes[2];
+    products_workspace(p, 2, aligned, bytes);
+    b.gx = bytes[0];
+    b.gw = bytes[1];
     b.total = b.dz * (gated ? 2 : 1) + b.sums + b.gx + b.gw;
     return b;
 }
@@ -179,8 +183,10 @@ size_t workspace(int mode, int dtype, int out_dtype, int64_t rows, int64_t in, i
         return (size_t)-1;
     if (mode == 1) return back_space(dtype, out_dtype, rows, in, out, ld_x, ld_w, ld_gy, act, gated, aligned != 0).total;
     const void* none[2] = {nullptr, nullptr};
-    return product_workspace(product_forward(dtype, out_dtype, rows, in, out, nullptr, ld_x, none, ld_w, act, gated),
-                             aligned != 0);
+    const Product p = product_forward(dtype, out_dtype, rows, in, out, nullptr, ld_x, none, ld_w, act, gated);
+    size_t bytes = 0;
+    products_workspace(&p, 1, aligned != 0, &bytes);
+    return bytes;
 }
 
 }  // namespace

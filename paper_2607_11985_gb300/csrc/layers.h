@@ -81,9 +81,10 @@ struct Joins {
 };
 vqc_status join_run(const Joins& joins, cudaStream_t s);
 
-// Bytes of workspace of a product.  `aligned`: the operands' addresses are
-// multiples of 16 bytes (their strides are looked at).
-size_t product_workspace(const Product& p, bool aligned);
+// Bytes of workspace of each of up to two products that run together (or one of them
+// alone).  `aligned`: the operands' addresses are multiples of 16 bytes (their
+// strides are looked at).
+void products_workspace(const Product* p, int count, bool aligned, size_t* bytes);
 // Runs products that do not depend on one another, in as few launches as they
 // allow; what is left to be joined is added to `joins`.  ws[i], bytes[i]: the workspace
 // of product i, in use until the joins have run.

@@ -297,27 +297,49 @@ vqc_status join_run(const Joins& joins, cudaStream_t s) {
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "join launch");
 }
 
-size_t product_workspace(const Product& p, bool aligned) {
-    if (p.m == 0 || rows_takes(p)) return 0;
-    if (tc_takes(p)) return tc_workspace(p, aligned);
-    return part_bytes(p, pick_splits(p, pick_tile(p)));
+void products_workspace(const Product* p, int count, bool aligned, size_t* bytes) {
+    Product tc[2];
+    int index[2], have = 0;
+    for (int i = 0; i < count; ++i) {
+        bytes[i] = 0;
+        if (p[i].m == 0 || rows_takes(p[i])) continue;
+        if (tc_takes(p[i])) {
+            tc[have] = p[i];
+            index[have++] = i;
+        } else {
+            bytes[i] = part_bytes(p[i], pick_splits(p[i], pick_tile(p[i])));
+        }
+    }
+    if (!have) return;
+    size_t need[2];
+    tc_workspace(tc, have, aligned, need);
+    for (int i = 0; i < have; ++i) bytes[index[i]] = need[i];
 }
 
 vqc_status products_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s) {
     ProductPair pair[2]{};       // those of tiles 64 x 64, those of tiles 128 x 16
-    int have[2] = {0, 0};
+    int have[2] = {0, 0}, tcs = 0;
+    Product tc[2];
+    void* tc_ws[2];
+    size_t tc_bytes[2];
     for (int i = 0; i < count; ++i) {
         if (p[i].m == 0 || p[i].n == 0) continue;
-        vqc_status st;
+        vqc_status st = VQC_OK;
         if (rows_takes(p[i])) {
             st = rows_run(p[i], s);
         } else if (tc_takes(p[i])) {
-            st = tc_run(p[i], ws[i], bytes[i], joins, s);
+            tc[tcs] = p[i];
+            tc_ws[tcs] = ws[i];
+            tc_bytes[tcs++] = bytes[i];
         } else {
             const Tile t = pick_tile(p[i]);
             const int kind = t.bn == 16;
             st = product_args(p[i], t, ws[i], bytes[i], pair[kind].p[have[kind]++], joins);
         }
+        if (st != VQC_OK) return st;
+    }
+    if (tcs) {
+        const vqc_status st = tc_run(tc, tcs, tc_ws, tc_bytes, joins, s);
         if (st != VQC_OK) return st;
     }
     for (int kind = 0; kind < 2; ++kind) {

@@ -9,6 +9,9 @@
 // [n, k] stored along k or along their outer index (the backward's products
 // contract over rows: no operand is ever transposed in memory).
 //
+// Two products that do not depend on one another (the two of a backward) share a launch:
+// one's tiles fill the SMs that the other's last tiles leave idle.
+//
 // A CTA, or a pair of CTAs on two SMs (cta_group::2), computes a tile of
 // 128 x BN (256 x BN) outputs.  Warp 0 moves 64-deep slices of both operands
 // into a ring of stages with TMA (128-byte swizzle; rows and columns beyond the
@@ -53,15 +56,42 @@ template <int CG, int BN> struct Shape {
     static constexpr int kTmem = 2 * BN;             // two accumulators, a power of two >= 32
 };
 
-// Maps of the operands: [operand][part].
-template <int kParts> struct TcArgs {
+// One product; maps of its operands: [operand][part].
+template <int kParts> struct Problem {
     CUtensorMap ma[2][kParts], mb[2][kParts];
     Finish f;
     Exact exact;                // of float operands
     float* part;                // sums of a cut contraction, or NULL
+    int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec;   // vec: bytes of a store
+};
+
+// The tiles of one or two products among the units (CTAs or pairs): those of the first
+// product in turn, then those of the second, of which units that had one tile less
+// of the first get more (first tiles are the longer ones).
+struct Schedule {
+    long long first, second;     // tiles
+    int units, rounds, extra;    // first = rounds * units + extra
+    int second_rounds;           // tiles of the second product that every unit has
+};
+__device__ __forceinline__ bool tile_of(const Schedule& S, int unit, int i, int& q, long long& t) {
+    const int mine = S.rounds + (unit < S.extra ? 1 : 0);
+    q = i >= mine ? 1 : 0;
+    if (!q) {
+        t = (long long)i * S.units + unit;
+        return true;
+    }
+    const int j = i - mine;
+    if (j < S.second_rounds) t = (long long)j * S.units + unit;
+    else if (unit >= S.extra) t = (long long)S.second_rounds * S.units + (long long)(j - S.second_rounds) * (S.units - S.extra) + (unit - S.extra);
+    else return false;
+    return t < S.second;
+}
+
+template <int kParts> struct TcArgs {
+    Problem<kParts> q[2];
+    Schedule plan;
     unsigned* err;
-    int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec, bf16;
-    long long tiles;
+    int bf16;
 };
 
 // Products of parts of float operands, small ones first: parts of a and b, 2 bits each.
@@ -84,6 +114,15 @@ __device__ __forceinline__ unsigned long long now_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;\n" : "=l"(t));
     return t;
 }
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
+}
+template <bool B> struct Flag {
+    static constexpr bool value = B;
+};
 __device__ __forceinline__ void mbar_init(uint32_t mbar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(mbar), "r"(count) : "memory");
 }
@@ -182,46 +221,51 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
                  "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-__device__ __forceinline__ void load32(const void* p, uint32_t (&r)[8]) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "l"(p)
-                 : "memory");
+__device__ __forceinline__ void load_bytes(const void* p, int wide, uint32_t (&r)[8]) {
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "l"(p)
+                     : "memory");
+    } else {
+        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+        r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
+        r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+    }
 }
-__device__ __forceinline__ void store16f(float* p, const float (&v)[16]) {
+// 32 bytes, at once where `wide`, else as two
+__device__ __forceinline__ void store_bytes(void* p, int wide, const uint32_t (&r)[8]) {
+    if (wide) return store32(p, r);
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+}
+__device__ __forceinline__ void store16f(float* p, int wide, const float (&v)[16]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         uint32_t r[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[8 * h + i]);
-        store32(p + 8 * h, r);
+        store_bytes(p + 8 * h, wide, r);
     }
 }
-__device__ __forceinline__ void store16(void* base, int dtype, int64_t at, const float (&v)[16]) {
-    if (dtype == VQC_F32) return store16f(static_cast<float*>(base) + at, v);
+__device__ __forceinline__ void store16(void* base, int dtype, int64_t at, int wide, const float (&v)[16]) {
+    if (dtype == VQC_F32) return store16f(static_cast<float*>(base) + at, wide, v);
     uint32_t r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (dtype == VQC_BF16) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            r[i] = *reinterpret_cast<const uint32_t*>(&p);
-        } else {
-            const __half2 p = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-            r[i] = *reinterpret_cast<const uint32_t*>(&p);
-        }
-    }
-    store32(static_cast<char*>(base) + 2 * at, r);
+    for (int i = 0; i < 8; ++i)
+        r[i] = dtype == VQC_BF16 ? pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]) : pack2<__half>(v[2 * i], v[2 * i + 1]);
+    store_bytes(static_cast<char*>(base) + 2 * at, wide, r);
 }
 // 16 elements of the residual as they lie in memory
 struct Res16 {
     uint32_t w[2][8];
 };
-__device__ __forceinline__ void load_res(const void* base, int dtype, int64_t at, Res16& r) {
+__device__ __forceinline__ void load_res(const void* base, int dtype, int64_t at, int wide, Res16& r) {
     if (dtype == VQC_F32) {
-        load32(static_cast<const float*>(base) + at, r.w[0]);
-        load32(static_cast<const float*>(base) + at + 8, r.w[1]);
+        load_bytes(static_cast<const float*>(base) + at, wide, r.w[0]);
+        load_bytes(static_cast<const float*>(base) + at + 8, wide, r.w[1]);
     } else {
-        load32(static_cast<const char*>(base) + 2 * at, r.w[0]);
+        load_bytes(static_cast<const char*>(base) + 2 * at, wide, r.w[0]);
     }
 }
 __device__ __forceinline__ void add_res(const Res16& r, int dtype, float (&v)[16]) {
@@ -238,9 +282,9 @@ __device__ __forceinline__ void add_res(const Res16& r, int dtype, float (&v)[16
     }
 }
 
-// The epilogue keeps the biases of a warp's columns in its staging space (which only
-// outputs that are not aligned use): those of the gate, then those of the other factor.
-constexpr int kBiasUp = 128;
+// A warp's staging space: 32 x 17 floats to turn outputs, then the biases of its columns
+// (16-byte aligned): those of the gate, then those of the other factor.
+constexpr int kBias = 32 * 17 + 16, kBiasUp = 128;
 __device__ __forceinline__ void add_bias(const float* b, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
@@ -269,7 +313,7 @@ struct TileAt {
 };
 // Tiles in groups of 16 tiles of rows, so that the CTAs at work at one time share
 // rows of both operands in the L2.
-template <int P> __device__ __forceinline__ TileAt tile_at(const TcArgs<P>& A, long long t) {
+template <int P> __device__ __forceinline__ TileAt tile_at(const Problem<P>& A, long long t) {
     TileAt r;
     const long long plane = (long long)A.tiles_m * A.tiles_n;
     const int p = (int)(t / plane);
@@ -283,17 +327,50 @@ template <int P> __device__ __forceinline__ TileAt tile_at(const TcArgs<P>& A, l
     return r;
 }
 
+// A warp's 32 x 16 values to memory, turned in shared memory so that lanes write
+// neighbouring columns: put(row, column, value) for those inside the matrix.
+template <typename F>
+__device__ __forceinline__ void turned(const float (&v)[16], int64_t row0, int64_t col0, int64_t m, int64_t n, int lane, float* stage, F put) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) stage[lane * 17 + i] = v[i];
+    __syncwarp();
+    const int64_t col = col0 + (lane & 15);
+    if (col < n) {
+#pragma unroll 8
+        for (int r = lane >> 4; r < 32; r += 2)
+            if (row0 + r < m) put(row0 + r, col, stage[r * 17 + (lane & 15)]);
+    }
+}
+
 // Accumulator columns c0..c0+15 (and their partners of the gate) of a warp's 32
-// rows, finished and written.  Aligned outputs go straight from the lanes, 32
-// bytes of a row each; others are turned in shared memory so that lanes write
-// neighbouring columns.
+// rows, finished and written.  Outputs whose rows lie on 16-byte boundaries go
+// straight from the lanes, 16 or 32 bytes of a row at once; others are turned.
 template <bool kGated, int kParts>
-__device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
+__device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
                                         float (&v)[16], float (&u)[16], const Res16& res, const float* bias, float* stage) {
     const Finish& f = A.f;
-    const int64_t n = f.n;
+    const int64_t n = f.n, row = row0 + lane;
+    const bool in = row < f.m, vec = A.vec && col0 + 16 <= n;
+    const int wide = A.vec == 32;
     if (col0 >= n) return;
-    if (kParts > 1 && !A.part && row0 + lane < f.m) {
+    if (A.part) {
+        const int64_t slots = A.form == GATED || A.form == PAIR ? 2 : 1;
+        float* to = A.part + (T.split * slots + T.which) * f.m * n;
+        if (vec) {
+            if (in) {
+                store16f(to + row * n + col0, wide, v);
+                if (kGated) store16f(to + (f.m + row) * n + col0, wide, u);
+            }
+        } else {
+            auto put = [&](int64_t r, int64_t c, float x) { to[r * n + c] = x; };
+            turned(v, row0, col0, f.m, n, lane, stage, put);
+            to += f.m * n;
+            if (kGated) turned(u, row0, col0, f.m, n, lane, stage, put);
+        }
+        return;
+    }
+    if (kParts > 1 && in) {
         float t = 0.f;       // NaN if one of the sums is not finite
 #pragma unroll
         for (int i = 0; i < 16; ++i) t = fmaf(v[i], 0.f, kGated ? fmaf(u[i], 0.f, t) : t);
@@ -304,8 +381,8 @@ __device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T
                 for (int j = 0; j < 16; ++j)
                     if (j == i) { a = v[j]; b = kGated ? u[j] : 0.f; }
                 if (col0 + i >= n) break;
-                a = exact_if_not_finite(A.exact, T.which, row0 + lane, col0 + i, a);
-                if (kGated) b = exact_if_not_finite(A.exact, 1, row0 + lane, col0 + i, b);
+                a = exact_if_not_finite(A.exact, T.which, row, col0 + i, a);
+                if (kGated) b = exact_if_not_finite(A.exact, 1, row, col0 + i, b);
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     if (j == i) {
@@ -315,59 +392,36 @@ __device__ __forceinline__ void write16(const TcArgs<kParts>& A, const TileAt& T
             }
         }
     }
-    if (kParts > 1) __syncwarp();
-    if (A.vec && col0 + 16 <= n) {
-        const int64_t row = row0 + lane;
-        if (A.part) {
-            if (row < f.m) {
-                const int64_t slots = A.form == GATED || A.form == PAIR ? 2 : 1;
-                float* at = A.part + ((T.split * slots + T.which) * f.m + row) * n + col0;
-                store16f(at, v);
-                if (kGated) store16f(at + f.m * n, u);
-            }
-            return;
-        }
-        if (row >= f.m) return;
-        if (f.bias[T.which]) add_bias(bias, v);
-        if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
-        const int64_t at = row * n + col0;
-        if (f.z[T.which]) store16f(f.z[T.which] + at, v);
-        if (kGated && f.z[1]) store16f(f.z[1] + at, u);
-        act16(f.act, v);
-        if (kGated) {
+    if (f.bias[T.which]) add_bias(bias, v);
+    if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
+    const int64_t at = row * n + col0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] *= u[i];
-        }
+    for (int w = 0; w < (kGated ? 2 : 1); ++w) {
+        float* z = f.z[kGated ? w : T.which];
+        if (!z) continue;
+        if (!vec) turned(w ? u : v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { z[r * n + c] = x; });
+        else if (in) store16f(z + at, wide, w ? u : v);
+    }
+    act16(f.act, v);
+    if (kGated) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= u[i];
+    }
+    if (vec) {
+        if (!in) return;
         if (!kGated && f.res) add_res(res, f.out_dtype, v);
-        store16(f.y[T.which], f.out_dtype, at, v);
-        return;
+        store16(f.y[T.which], f.out_dtype, at, wide, v);
+    } else if (!kGated && f.res) {
+        turned(v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) {
+            store_as(f.y[T.which], f.out_dtype, r * n + c, x + load_as(f.res, f.out_dtype, r * f.ld_res + c));
+        });
+    } else {
+        turned(v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { store_as(f.y[T.which], f.out_dtype, r * n + c, x); });
     }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        stage[lane * 17 + i] = v[i];
-        if (kGated) stage[32 * 17 + lane * 17 + i] = u[i];
-    }
-    __syncwarp();
-    const int64_t col = col0 + (lane & 15);
-    if (col < n) {
-        for (int r = lane >> 4; r < 32 && row0 + r < f.m; r += 2) {
-            const float a = stage[r * 17 + (lane & 15)], b = kGated ? stage[32 * 17 + r * 17 + (lane & 15)] : 0.f;
-            if (A.part) {
-                const int64_t slots = A.form == GATED || A.form == PAIR ? 2 : 1;
-                float* at = A.part + ((T.split * slots + T.which) * f.m + row0 + r) * n + col;
-                *at = a;
-                if (kGated) at[f.m * n] = b;
-            } else {
-                finish_one(f, T.which, row0 + r, col, a, b);
-            }
-        }
-    }
-    __syncwarp();
 }
 
 template <int CG, int BN, bool kGated, int kParts>
-__global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs<kParts> A) {
+__global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs<kParts> P) {
     using S = Shape<CG, BN>;
     constexpr int NS = S::kStages;
     extern __shared__ __align__(1024) unsigned char sm[];
@@ -394,8 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         for (int i = 0; i < 2; ++i) {
-            tma_prefetch(&A.ma[i][0]);
-            tma_prefetch(&A.mb[i][0]);
+            tma_prefetch(&P.q[i].ma[0][0]);
+            tma_prefetch(&P.q[i].mb[0][0]);
         }
     }
     if (warp == 2) {
@@ -421,65 +475,75 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     const uint32_t tmem = *tslot;
 
     constexpr int kPairs = kParts == 3 ? 6 : 1;      // products of parts per product
-    const int kblocks = A.kblocks * kPairs * (A.form == SUM ? 2 : 1);
-    const long long first = blockIdx.x / CG, step = gridDim.x / CG;
+    const int unit = blockIdx.x / CG;
+    int which;
+    long long t;
     // a role that gives up tells the others, in both CTAs
     auto give_up = [&]() {
         *gave_up = 1;
         if (CG == 2)
             asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"(at_cta(smem_u32((const void*)gave_up), rank ^ 1)), "r"(1)
                          : "memory");
-        atomicOr(A.err, 1u);
+        atomicOr(P.err, 1u);
     };
 
+    // Whole warps walk the loops of the two issuing roles (uniform control flow is cheaper
+    // than one lane's); one elected lane issues.
     if (warp == 0) {
-        if (lane == 0) {
-            int s = 0, used = 0;
-            uint32_t ph = 0;
-            bool ok = true;
-            for (long long t = first; t < A.tiles && ok; t += step) {
-                const TileAt T = tile_at(A, t);
-                const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
-                const int m0 = T.m * BM * CG + (int)rank * BM;
-                const int n0 = T.n * (kGated ? BN / 2 : BN) + (kGated ? 0 : (int)rank * (BN / CG));
+        const bool issuer = elect_one();
+        const uint32_t full0 = CG == 2 ? at_cta(full, 0) : full;
+        int s = 0, used = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int i = 0; ok && tile_of(P.plan, unit, i, which, t); ++i) {
+            const Problem<kParts>& A = P.q[which];
+            const TileAt T = tile_at(A, t);
+            const int kblocks = A.kblocks * kPairs * (A.form == SUM ? 2 : 1);
+            const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
+            const int m0 = T.m * BM * CG + (int)rank * BM;
+            const int n0 = T.n * (kGated ? BN / 2 : BN) + (kGated ? 0 : (int)rank * (BN / CG));
+            const int depth = A.kblocks * BK;
+            // slices of stages, the operands' layouts known
+            auto slices = [&](auto a_mn, auto b_mn) {
                 int term = kb0 / A.kblocks, k0 = (kb0 - term * A.kblocks) * BK;
+                const CUtensorMap *ma, *mb, *mb1;
+                auto maps = [&]() {
+                    const int sum = term >= kPairs ? 1 : 0, pair = term - sum * kPairs;
+                    const int pa = kPairs == 6 ? kPartsA >> (2 * pair) & 3 : 0, pb = kPairs == 6 ? kPartsB >> (2 * pair) & 3 : 0;
+                    ma = &A.ma[T.which + sum][pa];
+                    mb = &A.mb[kGated ? (int)rank : T.which + sum][pb];
+                    mb1 = &A.mb[1][pb];
+                };
+                maps();
                 for (int kb = kb0; kb < kb1; ++kb, k0 += BK) {
-                    if (k0 >= A.kblocks * BK) {
+                    if (k0 >= depth) {
                         ++term;
                         k0 = 0;
+                        maps();
                     }
-                    if (!mbar_wait(empty + 8 * s, ph ^ 1, gave_up)) {
+                    if (!__all_sync(~0u, mbar_wait(empty + 8 * s, ph ^ 1, gave_up))) {
                         ok = false;
                         break;
                     }
-                    const int sum = term >= kPairs ? 1 : 0, pair = term - sum * kPairs;
-                    const int pa = kPairs == 6 ? kPartsA >> (2 * pair) & 3 : 0, pb = kPairs == 6 ? kPartsB >> (2 * pair) & 3 : 0;
-                    const CUtensorMap* ma = &A.ma[T.which + sum][pa];
-                    const CUtensorMap* mb = &A.mb[T.which + sum][pb];
-                    const uint32_t sa = base + s * S::kStage, sb = sa + kStageA;
-                    const uint32_t bar = CG == 2 ? at_cta(full + 8 * s, 0) : full + 8 * s;
-                    if (rank == 0)
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(full + 8 * s),
-                                     "r"(CG * S::kStage)
-                                     : "memory");
-                    if (A.a_mn) {
+                    const uint32_t sa = base + s * S::kStage, sb = sa + kStageA, bar = full0 + 8 * s;
+                    if (issuer) {
+                        if (rank == 0)
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(full + 8 * s),
+                                         "r"(CG * S::kStage)
+                                         : "memory");
+                        if constexpr (decltype(a_mn)::value) {
 #pragma unroll
-                        for (int j = 0; j < BM / 64; ++j) tma_load<CG>(sa + j * 8192, ma, m0 + 64 * j, k0, bar);
-                    } else {
-                        tma_load<CG>(sa, ma, k0, m0, bar);
-                    }
-                    if (kGated) {
-                        if (CG == 2) {
-                            tma_load<CG>(sb, &A.mb[rank][pb], k0, n0, bar);
+                            for (int j = 0; j < BM / 64; ++j) tma_load<CG>(sa + j * 8192, ma, m0 + 64 * j, k0, bar);
                         } else {
-                            tma_load<CG>(sb, &A.mb[0][pb], k0, n0, bar);
-                            tma_load<CG>(sb + S::kStageB / 2, &A.mb[1][pb], k0, n0, bar);
+                            tma_load<CG>(sa, ma, k0, m0, bar);
                         }
-                    } else if (A.b_mn) {
+                        if constexpr (decltype(b_mn)::value) {
 #pragma unroll
-                        for (int j = 0; j < BN / CG / 64; ++j) tma_load<CG>(sb + j * 8192, mb, n0 + 64 * j, k0, bar);
-                    } else {
-                        tma_load<CG>(sb, mb, k0, n0, bar);
+                            for (int j = 0; j < BN / CG / 64; ++j) tma_load<CG>(sb + j * 8192, mb, n0 + 64 * j, k0, bar);
+                        } else {
+                            tma_load<CG>(sb, mb, k0, n0, bar);
+                            if (kGated && CG == 1) tma_load<CG>(sb + S::kStageB / 2, mb1, k0, n0, bar);
+                        }
                     }
                     used = used < NS ? used + 1 : NS;
                     if (++s == NS) {
@@ -487,65 +551,73 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                         ph ^= 1;
                     }
                 }
-            }
-            if (!ok) {
-                give_up();
-                // copies still in flight land before this CTA's memory is given back: the
-                // last `used` stages, in the order of their issue
-                if (rank == 0)
-                    for (int i = used; i > 0; --i) {
-                        const int q = (s - i + NS) % NS;
-                        mbar_wait(full + 8 * q, q < s ? ph : ph ^ 1, nullptr);
-                    }
+            };
+            if constexpr (kGated) {
+                slices(Flag<false>{}, Flag<false>{});
+            } else {       // forward, gradient of x, gradient of the weight
+                if (!A.b_mn) slices(Flag<false>{}, Flag<false>{});
+                else if (!A.a_mn) slices(Flag<false>{}, Flag<true>{});
+                else slices(Flag<true>{}, Flag<true>{});
             }
         }
-    } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            const uint32_t idesc = (1u << 4) | ((uint32_t)A.bf16 << 7) | ((uint32_t)A.bf16 << 10) |
-                                   ((uint32_t)A.a_mn << 15) | ((uint32_t)A.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
-                                   ((uint32_t)(BM * CG >> 4) << 24);
+        if (!ok) {
+            if (issuer) give_up();
+            // copies still in flight land before this CTA's memory is given back: the
+            // last `used` stages, in the order of their issue
+            if (rank == 0)
+                for (int i = used; i > 0; --i) {
+                    const int q = (s - i + NS) % NS;
+                    mbar_wait(full + 8 * q, q < s ? ph : ph ^ 1, nullptr);
+                }
+        }
+    } else if (warp == 1 && rank == 0) {
+        const bool issuer = elect_one();
+        int s = 0, acc = 0;
+        uint32_t ph = 0, aph = 0;
+        bool ok = true, issued = false;
+        for (int i = 0; ok && tile_of(P.plan, unit, i, which, t); ++i) {
+            const Problem<kParts>& A = P.q[which];
+            const TileAt T = tile_at(A, t);
+            const int kblocks = A.kblocks * kPairs * (A.form == SUM ? 2 : 1);
+            const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
+            const uint32_t idesc = (1u << 4) | ((uint32_t)P.bf16 << 7) | ((uint32_t)P.bf16 << 10) | ((uint32_t)A.a_mn << 15) |
+                                   ((uint32_t)A.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM * CG >> 4) << 24);
             const uint32_t step_a = A.a_mn ? 2048 >> 4 : 32 >> 4, step_b = A.b_mn ? 2048 >> 4 : 32 >> 4;
-            int s = 0, acc = 0;
-            uint32_t ph = 0, aph = 0;
-            bool ok = true, issued = false;
-            for (long long t = first; t < A.tiles && ok; t += step) {
-                const TileAt T = tile_at(A, t);
-                const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
-                if (!mbar_wait(tempty + 8 * acc, aph ^ 1, gave_up)) {
+            if (!__all_sync(~0u, mbar_wait(tempty + 8 * acc, aph ^ 1, gave_up))) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!__all_sync(~0u, mbar_wait(full + 8 * s, ph, gave_up))) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(full + 8 * s, ph, gave_up)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint64_t da = smem_desc(base + s * S::kStage, 8192), db = smem_desc(base + s * S::kStage + kStageA, 8192);
+                const uint64_t da = smem_desc(base + s * S::kStage, 8192), db = smem_desc(base + s * S::kStage + kStageA, 8192);
+                if (issuer) {
 #pragma unroll
                     for (int j = 0; j < BK / 16; ++j)
                         mma<CG>(tmem + acc * BN, da + j * step_a, db + j * step_b, idesc, kb > kb0 || j > 0);
-                    issued = true;
                     mma_commit<CG>(empty + 8 * s);
-                    if (++s == NS) {
-                        s = 0;
-                        ph ^= 1;
-                    }
+                    if (kb + 1 == kb1) mma_commit<CG>(tfull + 8 * acc);
                 }
-                if (!ok) break;
-                mma_commit<CG>(tfull + 8 * acc);
-                if (++acc == 2) {
-                    acc = 0;
-                    aph ^= 1;
+                issued = true;
+                if (++s == NS) {
+                    s = 0;
+                    ph ^= 1;
                 }
             }
-            if (!ok) {
-                give_up();
-                if (issued) {   // products in flight finish before the tensor memory is freed
-                    mma_commit<CG>(drain);
-                    mbar_wait(drain, 0, nullptr);
-                }
+            if (++acc == 2) {
+                acc = 0;
+                aph ^= 1;
+            }
+        }
+        if (!ok) {
+            if (issuer) give_up();
+            if (issued) {   // products in flight finish before the tensor memory is freed
+                if (issuer) mma_commit<CG>(drain);
+                mbar_wait(drain, 0, nullptr);
             }
         }
     } else if (warp >= 4) {
@@ -555,16 +627,17 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         constexpr int kCols = kGated ? BN / 2 : BN;   // output columns of a tile
         int acc = 0;
         uint32_t aph = 0;
-        for (long long t = first; t < A.tiles; t += step) {
+        for (int i = 0; tile_of(P.plan, unit, i, which, t); ++i) {
+            const Problem<kParts>& A = P.q[which];
             const TileAt T = tile_at(A, t);
-            if (A.vec && !A.part) {      // biases of this warp's columns
+            if (!A.part) {      // biases of this warp's columns
                 __syncwarp();
                 for (int w = 0; w < (kGated ? 2 : 1); ++w) {
                     const void* from = A.f.bias[kGated ? w : T.which];
                     if (from)
                         for (int c = lane; c < kCols / 2; c += 32) {
                             const int64_t col = (int64_t)T.n * kCols + half * (kCols / 2) + c;
-                            stage[w * kBiasUp + c] = col < A.f.n ? load_as(from, A.f.dtype, col) : 0.f;
+                            stage[kBias + w * kBiasUp + c] = col < A.f.n ? load_as(from, A.f.dtype, col) : 0.f;
                         }
                 }
             }
@@ -578,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             // the residual is read one step ahead
             const bool ahead = !kGated && A.f.res && A.vec && !A.part && row0 + lane < A.f.m;
             auto fetch = [&](int c, Res16& r) {
-                if (ahead && n0 + c + 16 <= A.f.n) load_res(A.f.res, A.f.out_dtype, (row0 + lane) * A.f.ld_res + n0 + c, r);
+                if (ahead && n0 + c + 16 <= A.f.n) load_res(A.f.res, A.f.out_dtype, (row0 + lane) * A.f.ld_res + n0 + c, A.vec == 32, r);
             };
             Res16 res, next;
             fetch(half * (kCols / 2), next);
@@ -591,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 tmem_ld(tmem + lanes + acc * BN + c, v);
                 if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
                 tmem_wait();
-                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + c - half * (kCols / 2), stage);
+                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + kBias + c - half * (kCols / 2), stage);
             }
             tc_fence_before();
             __syncwarp();
@@ -658,43 +731,59 @@ __device__ __forceinline__ void bf16_parts(float x, uint16_t (&o)[3]) {
     }
 }
 
-// [rows, cols] of floats as three matrices of parts, rows of `ld_to` elements (a multiple
-// of 8): 8 elements per thread.
-__global__ void __launch_bounds__(256) parts_kernel(const float* from, int64_t ld, int64_t rows, int64_t cols, uint16_t* to,
-                                                    int64_t ld_to, int vec) {
-    const int64_t across = ld_to / 8, plane = rows * ld_to, count = rows * across, step = (int64_t)gridDim.x * blockDim.x;
+// Copies of operands that TMA cannot read in place, up to four in one launch (job
+// blockIdx.y): [rows, cols] with rows of `ld_to` elements (a multiple of 8).  Floats
+// become three matrices of parts, 16-bit elements keep their bits.  8 elements
+// per thread.
+struct CopyJob {
+    const void* from;
+    uint16_t* to;
+    int64_t ld, rows, cols, ld_to;
+    int vec;            // rows of `from` on 16-byte boundaries
+};
+constexpr int kMostCopies = 8;
+struct CopyJobs {
+    CopyJob j[kMostCopies];
+    int count;
+};
+template <int kParts> __global__ void __launch_bounds__(256) copy_kernel(const __grid_constant__ CopyJobs J) {
+    const CopyJob& A = J.j[blockIdx.y];
+    const int64_t across = A.ld_to / 8, plane = A.rows * A.ld_to, count = A.rows * across, step = (int64_t)gridDim.x * blockDim.x;
     for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < count; e += step) {
-        const int64_t r = e / across, c = e % across * 8;
-        const float* p = from + r * ld + c;
-        float v[8];
-        if (vec && c + 8 <= cols) {
-            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        const int64_t r = count >> 32 ? e / across : (int64_t)((uint32_t)e / (uint32_t)across), c = (e - r * across) * 8;
+        uint16_t* to = A.to + r * A.ld_to + c;
+        if constexpr (kParts == 1) {
+            const uint16_t* p = static_cast<const uint16_t*>(A.from) + r * A.ld + c;
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = (c + 2 * i < A.cols ? (uint32_t)p[2 * i] : 0u) | (c + 2 * i + 1 < A.cols ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+            *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
+            const float* p = static_cast<const float*>(A.from) + r * A.ld + c;
+            float v[8];
+            if (A.vec && c + 8 <= A.cols) {
+                const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+                v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? p[i] : 0.f;
+                for (int i = 0; i < 8; ++i) v[i] = c + i < A.cols ? p[i] : 0.f;
+            }
+            uint32_t w[3][4];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                uint16_t a[3], b[3];
+                bf16_parts(v[i], a);
+                bf16_parts(v[i + 1], b);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) w[q][i / 2] = (uint32_t)a[q] | (uint32_t)b[q] << 16;
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+                *reinterpret_cast<uint4*>(to + q * plane) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
         }
-        uint32_t w[3][4];
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            uint16_t a[3], b[3];
-            bf16_parts(v[i], a);
-            bf16_parts(v[i + 1], b);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) w[q][i / 2] = (uint32_t)a[q] | (uint32_t)b[q] << 16;
-        }
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-            *reinterpret_cast<uint4*>(to + q * plane + r * ld_to + c) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
     }
-}
-
-// 16-bit copy of [rows, cols] with rows of `ld_to` elements (a multiple of 8)
-__global__ void __launch_bounds__(256) align_kernel(const uint16_t* from, int64_t ld, int64_t rows, int64_t cols, uint16_t* to,
-                                                    int64_t ld_to) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) to[r * ld_to + c] = from[r * ld + c];
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -737,53 +826,116 @@ size_t copy_bytes(const Operand& o, int dtype, int64_t outer, int64_t k) {
     return align256((size_t)(o.k_outer ? k : outer) * copy_ld(o.k_outer ? outer : k) * 2 * parts_of(dtype));
 }
 
+// The tile, and the cuts of each of up to two products.
 struct Choice {
-    int cg, bn, splits;
+    int cg, bn, splits[2];
 };
+struct TileKind {
+    int cg, bn;
+    double stage;      // cycles of one stage of 64
+};
+constexpr TileKind kTiles[] = {{2, 256, 560}, {2, 128, 400}, {1, 128, 512}, {1, 64, 384}};
 
-// The tile and the cuts that finish first, by a count of cycles on one SM: a
-// stage of 64 costs its products (8192 per cycle and SM) or its bytes (about 64
-// per cycle and SM from the L2), whichever is longer, a tile its start and end, a
-// cut the traffic of its sums.
-Choice choose_new(const Product& p) {
-    static const struct { int cg, bn, stage; } kTiles[] = {{2, 256, 560}, {2, 128, 400}, {1, 128, 512}, {1, 64, 384}};
-    const int sms = sm_count();
-    const int64_t kblocks = ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * (p.f.dtype == VQC_F32 ? 6 : 1);
-    Choice best{1, 64, 1};
-    double least = 1e300;
-    for (const auto& t : kTiles) {
-        const int64_t cols = p.form == GATED ? t.bn / 2 : t.bn;
-        const int64_t tiles = ceil_div(p.m, BM * t.cg) * ceil_div(p.n, cols) * (p.form == PAIR ? 2 : 1);
-        for (int64_t s = 1; s <= std::min<int64_t>(kblocks, 64); s = s < 4 ? s + 1 : s + s / 4) {
-            const int64_t units = sms / t.cg, waves = ceil_div(tiles * s, units);
-            const double end = 3.0 * t.bn;      // taking an accumulator out
-            const double tile = (double)ceil_div(kblocks, s) * t.stage;
-            double c = waves * std::max(tile, end) + end + 2500;
-            // sums written and read once by all SMs together, and a second launch
-            if (s > 1) c += 4000 + (double)(s + 1) * p.m * p.n * (p.form == GATED || p.form == PAIR ? 2 : 1) * 4 / (sms * 24.0);
-            if (c < least) {
-                least = c;
-                best = {t.cg, t.bn, (int)s};
-            }
+int64_t tiles_of(const Product& p, const TileKind& t) {
+    return ceil_div(p.m, BM * t.cg) * ceil_div(p.n, p.form == GATED ? t.bn / 2 : t.bn) * (p.form == PAIR ? 2 : 1);
+}
+int64_t depth_of(const Product& p) { return ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * (p.f.dtype == VQC_F32 ? 6 : 1); }
+
+// The schedule of `first` tiles of c0 cycles and `second` of c1 <= c0, and its length.
+double make_schedule(int64_t first, double c0, int64_t second, double c1, int units, Schedule& s) {
+    s.first = first;
+    s.second = second;
+    s.units = (int)std::min<int64_t>(units, first + second);
+    s.rounds = (int)(first / s.units);
+    s.extra = (int)(first % s.units);
+    s.second_rounds = 0;
+    const double most = (s.rounds + (s.extra ? 1 : 0)) * c0;
+    if (!second) return most;
+    if (!s.extra) {
+        s.second_rounds = (int)ceil_div(second, s.units);
+        return most + s.second_rounds * c1;
+    }
+    const int rest = s.units - s.extra;
+    const int64_t guess = (int64_t)(((first * c0 + second * c1) / s.units - most) / c1);
+    double best = 1e300;
+    for (int64_t r = std::max<int64_t>(0, guess - 1); r <= std::max<int64_t>(0, guess) + 1; ++r) {
+        const int64_t left = std::max<int64_t>(0, second - r * s.units);
+        const double span = std::max(most + std::min<int64_t>(r, ceil_div(second, s.units)) * c1, s.rounds * c0 + (r + ceil_div(left, rest)) * c1);
+        if (span < best) {
+            best = span;
+            s.second_rounds = (int)r;
         }
     }
     return best;
 }
 
+// Cycles of a tile: its stages (the products, 8192 per cycle and SM, or the bytes from the
+// L2, whichever takes longer), or taking out its accumulator.
+double tile_cycles(const Product& p, const TileKind& t, int64_t splits) {
+    return std::max((double)ceil_div(depth_of(p), splits) * t.stage, 3.0 * t.bn);
+}
+// of a cut: sums written and read once by all SMs together, and the launch of the join
+double cut_cycles(const Product& p, int64_t splits, int sms) {
+    return splits > 1 ? (double)(splits + 1) * p.m * p.n * (p.form == GATED || p.form == PAIR ? 2 : 1) * 4 / (sms * 24.0) : 0.0;
+}
+
+// The first of two products is the one with the longer tiles.
+bool swapped(const Product* p, int count, const TileKind& t, const int* splits) {
+    return count == 2 && tile_cycles(p[0], t, splits[0]) < tile_cycles(p[1], t, splits[1]);
+}
+double schedule_of(const Product* p, int count, const TileKind& t, const int* splits, int sms, Schedule& s) {
+    const int a = swapped(p, count, t, splits), b = 1 - a;
+    return make_schedule(tiles_of(p[a], t) * splits[a], tile_cycles(p[a], t, splits[a]), count == 2 ? tiles_of(p[b], t) * splits[b] : 0,
+                         count == 2 ? tile_cycles(p[b], t, splits[b]) : 1.0, sms / t.cg, s);
+}
+
+Choice choose_new(const Product* p, int count, int sms) {
+    static constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    Choice best{1, 64, {1, 1}};
+    double least = 1e300;
+    for (const TileKind& t : kTiles)
+        for (int s0 : kCuts) {
+            if (s0 > depth_of(p[0])) break;
+            for (int s1 : kCuts) {
+                if (s1 > (count == 2 ? depth_of(p[1]) : 1)) break;
+                const int splits[2] = {s0, s1};
+                Schedule plan;
+                double c = schedule_of(p, count, t, splits, sms, plan) + 3.0 * t.bn + cut_cycles(p[0], s0, sms);
+                if (count == 2) c += cut_cycles(p[1], s1, sms);
+                if (s0 > 1 || s1 > 1) c += 4000;
+                if (c < least) {
+                    least = c;
+                    best = {t.cg, t.bn, {s0, s1}};
+                }
+            }
+        }
+    return best;
+}
+
 // The choices of the sizes that a thread asked for last.
-Choice choose(const Product& p) {
+Choice choose(const Product* p, int count) {
+    struct Key {
+        int64_t v[9];
+        bool operator==(const Key& o) const { return std::equal(v, v + 9, o.v); }
+    };
     struct Known {
-        int64_t m = 0, n = 0, k = 0;
-        int form = -1, dtype = -1, sms = 0;
-        Choice c;
+        Key key{};
+        Choice c{};
     };
     static thread_local Known known[64];
-    const bool parts = p.f.dtype == VQC_F32;
-    Known& q = known[(uint64_t)(p.m * 0x9E3779B1 + p.n * 0x85EBCA77 + p.k * 0xC2B2AE3D + p.form + 4 * parts) >> 7 & 63];
     const int sms = sm_count();
-    if (q.m != p.m || q.n != p.n || q.k != p.k || q.form != p.form || q.dtype != parts || q.sms != sms) {
-        q.c = choose_new(p);
-        q.m = p.m; q.n = p.n; q.k = p.k; q.form = p.form; q.dtype = parts; q.sms = sms;
+    Key key{};
+    uint64_t hash = 0;
+    key.v[0] = sms;
+    for (int i = 0; i < count; ++i) {
+        key.v[4 * i + 1] = p[i].m; key.v[4 * i + 2] = p[i].n; key.v[4 * i + 3] = p[i].k;
+        key.v[4 * i + 4] = 1 + p[i].form + 8 * (p[i].f.dtype == VQC_F32);
+    }
+    for (int64_t v : key.v) hash = (hash ^ (uint64_t)v) * 0x9E3779B97F4A7C15ull;
+    Known& q = known[hash >> 58];
+    if (!(q.key == key)) {
+        q.c = choose_new(p, count, sms);
+        q.key = key;
     }
     return q.c;
 }
@@ -799,9 +951,8 @@ template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const T
         if (e != cudaSuccess) return e;
         prepared.fetch_or(1ull << (dev & 63));
     }
-    const long long units = sm_count() / CG;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(std::min<long long>(a.tiles, units) * CG));
+    cfg.gridDim = dim3((unsigned)(a.plan.units * CG));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = s;
@@ -819,6 +970,148 @@ template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, co
     return c.bn == 128 ? launch_tc<1, 128, kGated, kParts>(a, s) : launch_tc<1, 64, kGated, kParts>(a, s);
 }
 
+int left_operands(const Product& p) { return p.form == SUM || p.form == PAIR ? 2 : 1; }
+int right_operands(const Product& p) { return p.form == SUM || p.form == GATED ? 2 : 1; }
+
+size_t space(const Product& p, bool aligned, int splits) {
+    size_t bytes = 0;
+    for (int i = 0; i < left_operands(p); ++i)
+        if (!ready(p.a[i], p.f.dtype, aligned)) bytes += copy_bytes(p.a[i], p.f.dtype, p.m, p.k);
+    for (int i = 0; i < right_operands(p); ++i)
+        if (!ready(p.b[i], p.f.dtype, aligned)) bytes += copy_bytes(p.b[i], p.f.dtype, p.n, p.k);
+    if (splits > 1) bytes += align256((size_t)splits * (p.form == GATED || p.form == PAIR ? 2 : 1) * p.m * p.n * 4);
+    return bytes;
+}
+
+// The copies that a product's operands need (one copy of a matrix that two products
+// read), and the operands as the kernel reads them.
+struct Placed {
+    Operand a[2], b[2];
+    char* at;         // what is left of the workspace
+    size_t left;
+};
+vqc_status place(const Product& p, void* ws, size_t ws_bytes, CopyJobs& jobs, Placed& r) {
+    r.at = static_cast<char*>(ws);
+    r.left = ws ? ws_bytes : 0;
+    for (int side = 0; side < 2; ++side)
+        for (int i = 0; i < (side ? right_operands(p) : left_operands(p)); ++i) {
+            Operand o = side ? p.b[i] : p.a[i];
+            const int64_t outer = side ? p.n : p.m;
+            if (!ready(o, p.f.dtype, aligned_to(o.p, 16))) {
+                CopyJob j{o.p, nullptr, o.ld, o.k_outer ? p.k : outer, o.k_outer ? outer : p.k, 0, o.ld % 4 == 0 && aligned_to(o.p, 16)};
+                j.ld_to = copy_ld(j.cols);
+                const CopyJob* same = nullptr;
+                for (int q = 0; q < jobs.count; ++q)
+                    if (jobs.j[q].from == j.from && jobs.j[q].ld == j.ld && jobs.j[q].rows == j.rows && jobs.j[q].cols == j.cols) same = &jobs.j[q];
+                if (!same) {
+                    const size_t bytes = copy_bytes(o, p.f.dtype, outer, p.k);
+                    if (bytes > r.left || jobs.count == kMostCopies) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
+                    j.to = reinterpret_cast<uint16_t*>(r.at);
+                    r.at += bytes;
+                    r.left -= bytes;
+                    same = &(jobs.j[jobs.count++] = j);
+                }
+                o.p = same->to;
+                o.ld = same->ld_to;
+            }
+            (side ? r.b : r.a)[i] = o;
+        }
+    return VQC_OK;
+}
+
+template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c, int splits, Placed& r, Problem<kParts>& a, Joins& joins) {
+    const bool gated = p.form == GATED;
+    const int na = left_operands(p), nb = right_operands(p);
+    for (int side = 0; side < 2; ++side)
+        for (int i = 0; i < (side ? nb : na); ++i) {
+            const Operand& o = (side ? r.b : r.a)[i];
+            const int64_t outer = side ? p.n : p.m, rows = o.k_outer ? p.k : outer;
+            const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
+            for (int q = 0; q < kParts; ++q) {
+                Operand part = o;
+                part.p = static_cast<const uint16_t*>(o.p) + q * rows * o.ld;
+                if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
+                    return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
+            }
+        }
+    for (int q = 0; q < kParts; ++q) {      // an operand of both products
+        if (na == 1) a.ma[1][q] = a.ma[0][q];
+        if (nb == 1) a.mb[1][q] = a.mb[0][q];
+    }
+    a.f = p.f;
+    a.form = p.form;
+    a.splits = splits;
+    a.tiles_m = (int)ceil_div(p.m, BM * c.cg);
+    a.tiles_n = (int)ceil_div(p.n, gated ? c.bn / 2 : c.bn);
+    a.kblocks = (int)ceil_div(p.k, BK);
+    a.a_mn = p.a[0].k_outer;
+    a.b_mn = p.b[0].k_outer;
+    a.exact = Exact{};
+    a.part = nullptr;
+    if (kParts == 3) {
+        for (int i = 0; i < 2; ++i) { a.exact.a[i] = p.a[i]; a.exact.b[i] = p.b[i]; }
+        a.exact.k = p.k;
+        a.exact.form = p.form;
+    }
+    if (splits > 1) {
+        if (align256((size_t)splits * (gated || p.form == PAIR ? 2 : 1) * p.m * p.n * 4) > r.left)
+            return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
+        a.part = reinterpret_cast<float*>(r.at);
+        Join& j = joins.j[joins.count++];
+        j.f = p.f;
+        j.exact = a.exact;
+        j.part = a.part;
+        j.splits = splits;
+        j.form = p.form;
+    }
+    // the widest store that every row of every output allows
+    const int64_t eo = (int64_t)elem_size(p.f.out_dtype);
+    auto on = [&](int w) {
+        if (a.part) return p.n * 4 % w == 0;
+        return p.n * eo % w == 0 && aligned_to(p.f.y[0], w) && aligned_to(p.f.y[1], w) &&
+               (!p.f.z[0] || (p.n * 4 % w == 0 && aligned_to(p.f.z[0], w) && aligned_to(p.f.z[1], w))) &&
+               (!p.f.res || (p.f.ld_res * eo % w == 0 && aligned_to(p.f.res, w)));
+    };
+    a.vec = on(32) ? 32 : on(16) ? 16 : 0;
+    return VQC_OK;
+}
+
+template <int kParts> vqc_status run_parts(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s) {
+    const Choice c = choose(p, count);
+    const bool gated = p[0].form == GATED;
+    CopyJobs jobs;
+    jobs.count = 0;
+    Placed placed[2];
+    for (int i = 0; i < count; ++i) {
+        const vqc_status st = place(p[i], ws[i], bytes[i], jobs, placed[i]);
+        if (st != VQC_OK) return st;
+    }
+    if (jobs.count) {
+        int64_t most = 1;
+        for (int i = 0; i < jobs.count; ++i) most = std::max(most, jobs.j[i].rows * jobs.j[i].ld_to / 8);
+        void* args[] = {&jobs};
+        const cudaError_t e = cudaLaunchKernel((const void*)copy_kernel<kParts>, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), jobs.count),
+                                               dim3(256), args, 0, s);
+        if (e != cudaSuccess) return cuda_error(e, "operand copy launch");
+    }
+    const TileKind* tile = kTiles;
+    while (tile->cg != c.cg || tile->bn != c.bn) ++tile;
+    TcArgs<kParts> a;
+    schedule_of(p, count, *tile, c.splits, sm_count(), a.plan);
+    const int order = swapped(p, count, *tile, c.splits);
+    for (int i = 0; i < count; ++i) {
+        const int from = order ? 1 - i : i;
+        const vqc_status st = fill_problem<kParts>(p[from], c, c.splits[from], placed[from], a.q[i], joins);
+        if (st != VQC_OK) return st;
+    }
+    if (count == 1) a.q[1] = a.q[0];
+    a.bf16 = p[0].f.dtype != VQC_F16;
+    cudaError_t e = error_word(&a.err);
+    if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
+    e = gated ? launch_choice<true, kParts>(c, a, s) : launch_choice<false, kParts>(c, a, s);
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "tensor-core product launch");
+}
+
 }  // namespace
 
 // Float products come here where six products of parts (and writing the parts)
@@ -831,107 +1124,16 @@ bool tc_takes(const Product& p) {
     return flops >= 5e8 && p.k >= 64 && std::min(p.m, p.n) >= 64;
 }
 
-size_t tc_workspace(const Product& p, bool aligned) {
-    size_t bytes = 0;
-    const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == SUM || p.form == GATED ? 2 : 1;
-    for (int i = 0; i < na; ++i)
-        if (!ready(p.a[i], p.f.dtype, aligned)) bytes += copy_bytes(p.a[i], p.f.dtype, p.m, p.k);
-    for (int i = 0; i < nb; ++i)
-        if (!ready(p.b[i], p.f.dtype, aligned)) bytes += copy_bytes(p.b[i], p.f.dtype, p.n, p.k);
-    const Choice c = choose(p);
-    if (c.splits > 1) bytes += align256((size_t)c.splits * (p.form == GATED || p.form == PAIR ? 2 : 1) * p.m * p.n * 4);
-    return bytes;
+void tc_workspace(const Product* p, int count, bool aligned, size_t* bytes) {
+    const Choice both = choose(p, count);
+    for (int i = 0; i < count; ++i) {
+        bytes[i] = space(p[i], aligned, both.splits[i]);
+        if (count == 2) bytes[i] = std::max(bytes[i], space(p[i], aligned, choose(p + i, 1).splits[0]));   // either may run alone
+    }
 }
 
-namespace {
-template <int kParts> vqc_status run_parts(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
-    TcArgs<kParts> a;
-    char* at = static_cast<char*>(ws);
-    size_t left = ws ? ws_bytes : 0;
-    auto take = [&](size_t bytes) -> void* {
-        if (bytes > left) return nullptr;
-        void* r = at;
-        at += bytes;
-        left -= bytes;
-        return r;
-    };
-    const Choice c = choose(p);
-    const bool gated = p.form == GATED;
-    constexpr bool split = kParts == 3;
-    const int na = p.form == SUM || p.form == PAIR ? 2 : 1, nb = p.form == SUM || gated ? 2 : 1;
-    for (int side = 0; side < 2; ++side)
-        for (int i = 0; i < (side ? nb : na); ++i) {
-            Operand o = side ? p.b[i] : p.a[i];
-            const int64_t outer = side ? p.n : p.m;
-            int64_t rows = o.k_outer ? p.k : outer, cols = o.k_outer ? outer : p.k, ld = o.ld, ld_to = copy_ld(cols);
-            if (!ready(o, p.f.dtype, aligned_to(o.p, 16))) {
-                void* to = take(copy_bytes(o, p.f.dtype, outer, p.k));
-                if (!to) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
-                const void* from = o.p;
-                int vec = ld % 4 == 0 && aligned_to(from, 16);
-                void* args[] = {&from, &ld, &rows, &cols, &to, &ld_to, &vec};
-                const int64_t grid = split ? std::min<int64_t>(ceil_div(rows * ld_to / 8, 256), 8LL * sm_count()) : std::min<int64_t>(rows, 16LL * sm_count());
-                const cudaError_t e = cudaLaunchKernel(split ? (const void*)parts_kernel : (const void*)align_kernel, dim3((unsigned)grid),
-                                                       dim3(256), args, 0, s);
-                if (e != cudaSuccess) return cuda_error(e, "operand copy launch");
-                o.p = to;
-                o.ld = ld_to;
-            }
-            const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
-            for (int q = 0; q < kParts; ++q) {
-                Operand part = o;
-                part.p = static_cast<const uint16_t*>(o.p) + q * rows * ld_to;
-                if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
-                    return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
-            }
-        }
-    for (int q = 0; q < kParts; ++q) {      // an operand of both products
-        if (na == 1) a.ma[1][q] = a.ma[0][q];
-        if (nb == 1) a.mb[1][q] = a.mb[0][q];
-    }
-    a.f = p.f;
-    a.form = p.form;
-    a.bf16 = p.f.dtype != VQC_F16;
-    a.splits = c.splits;
-    a.tiles_m = (int)ceil_div(p.m, BM * c.cg);
-    a.tiles_n = (int)ceil_div(p.n, gated ? c.bn / 2 : c.bn);
-    a.kblocks = (int)ceil_div(p.k, BK);
-    a.a_mn = p.a[0].k_outer;
-    a.b_mn = p.b[0].k_outer;
-    a.tiles = (long long)a.tiles_m * a.tiles_n * a.splits * (p.form == PAIR ? 2 : 1);
-    a.exact = Exact{};
-    a.part = nullptr;
-    if (split) {
-        for (int i = 0; i < 2; ++i) { a.exact.a[i] = p.a[i]; a.exact.b[i] = p.b[i]; }
-        a.exact.k = p.k;
-        a.exact.form = p.form;
-    }
-    if (c.splits > 1) {
-        a.part = static_cast<float*>(take(align256((size_t)c.splits * (gated || p.form == PAIR ? 2 : 1) * p.m * p.n * 4)));
-        if (!a.part) return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
-        Join& j = joins.j[joins.count++];
-        j.f = p.f;
-        j.exact = a.exact;
-        j.part = a.part;
-        j.splits = c.splits;
-        j.form = p.form;
-    }
-    // every row of every output on a 32-byte boundary
-    const int64_t eo = (int64_t)elem_size(p.f.out_dtype);
-    auto on32 = [](const void* q) { return aligned_to(q, 32); };
-    a.vec = a.part ? p.n % 8 == 0
-                   : p.n * eo % 32 == 0 && on32(p.f.y[0]) && on32(p.f.y[1]) &&
-                         (!p.f.z[0] || (p.n % 8 == 0 && on32(p.f.z[0]) && on32(p.f.z[1]))) &&
-                         (!p.f.res || (p.f.ld_res * eo % 32 == 0 && on32(p.f.res)));
-    cudaError_t e = error_word(&a.err);
-    if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
-    e = gated ? launch_choice<true, kParts>(c, a, s) : launch_choice<false, kParts>(c, a, s);
-    return e == cudaSuccess ? VQC_OK : cuda_error(e, "tensor-core product launch");
-}
-}  // namespace
-
-vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
-    return p.f.dtype == VQC_F32 ? run_parts<3>(p, ws, ws_bytes, joins, s) : run_parts<1>(p, ws, ws_bytes, joins, s);
+vqc_status tc_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s) {
+    return p[0].f.dtype == VQC_F32 ? run_parts<3>(p, count, ws, bytes, joins, s) : run_parts<1>(p, count, ws, bytes, joins, s);
 }
 
 }  // namespace layers

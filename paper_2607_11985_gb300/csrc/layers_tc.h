@@ -7,8 +7,10 @@ namespace vqc {
 namespace layers {
 
 bool tc_takes(const Product& p);
-size_t tc_workspace(const Product& p, bool aligned);
-vqc_status tc_run(const Product& p, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s);
+// One or two products of one type (a GATED one alone); bytes[i]: the workspace of
+// product i, enough for it alone as well.
+void tc_workspace(const Product* p, int count, bool aligned, size_t* bytes);
+vqc_status tc_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s);
 
 // Products with up to 4 rows.
 bool rows_takes(const Product& p);
