@@ -8,11 +8,15 @@ What stands around a ``Circuit`` inside a network, in the library's kernels:
   gated        h = act(x weight_gate^T + bias_gate) * (x weight_up^T + bias_up)
 
 Each has three forms: ``linear_forward`` and ``linear_backward`` are the two
-launches of a training step (or inference with ``save=False``), ``linear`` the
+calls of a training step (or inference with ``save=False``), ``linear`` the
 same under autograd.  x may have any leading axes; rows may be strided (other
 layouts are copied).  Types: float32, bfloat16 and float16, sums and
-statistics in float; see include/vqc.h for the formulas and roundings.  Torch
-supplies device memory and the current stream only.
+statistics in float; see include/vqc.h for the formulas and roundings.  Tensors
+are on the current device, work goes to its current stream.  Torch supplies
+device memory and the stream only.
+
+A call on a few rows costs its host path, so that is kept short: checks are one
+test each where they pass, and the C entry points are called directly.
 """
 from __future__ import annotations
 
@@ -22,61 +26,78 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
-from .circuit import _here, _ptr
+from .circuit import _raw_stream
 
 _REAL = {torch.float32: B.VQC_F32, torch.bfloat16: B.VQC_BF16, torch.float16: B.VQC_F16}
+_ACT = B.ACTIVATIONS
+_F32 = torch.float32
+_empty = torch.empty
+_device = torch.cuda.current_device
 
 
-def _code(t, name):
+def _matrix(t, name):
+    """(type code, t as [rows, cols] with adjacent row elements, rows, cols, row stride)."""
     code = _REAL.get(t.dtype)
-    if code is None or not t.is_cuda:
-        raise ValueError("%s must be a CUDA float32, bfloat16 or float16 tensor (got %s %s)"
-                         % (name, t.device, t.dtype))
-    return code
-
-
-def _out_code(dtype, out_dtype):
-    if out_dtype not in _REAL or (out_dtype is not dtype and torch.float32 not in (dtype, out_dtype)):
-        raise ValueError("the output of %s operands must be %s, float32 or, from float32, a 16-bit type (got %s)"
-                         % (dtype, dtype, out_dtype))
-    return _REAL[out_dtype]
-
-
-def _act(activation):
-    code = B.ACTIVATIONS.get(activation)
-    if code is None:
-        raise ValueError("activation must be one of %s (got %r)" % (sorted(B.ACTIVATIONS), activation))
-    return code
-
-
-def _rows(t, cols, name, dtype=None, rows=None):
-    """(t as [rows, cols] with adjacent row elements, its row stride)."""
-    if t.dim() == 0 or t.shape[-1] != cols or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
-        raise ValueError("%s must be a CUDA %s tensor of shape [..., %d] (got %s %s %s)"
-                         % (name, dtype or "", cols, t.device, t.dtype, tuple(t.shape)))
+    if code is None or t.get_device() != _device() or t.dim() == 0:
+        raise ValueError("%s must be a CUDA float32, bfloat16 or float16 tensor on the current device (got %s %s %s)"
+                         % (name, t.device, t.dtype, tuple(t.shape)))
     if t.dim() != 2:
-        t = t.reshape(-1, cols)
-    if rows is not None and t.shape[0] != rows:
-        raise ValueError("%s must have %d rows (got %d)" % (name, rows, t.shape[0]))
+        t = t.reshape(-1, t.shape[-1])
+    rows, cols = t.shape
+    if t.is_contiguous():
+        return code, t, rows, cols, cols
     ld, one = t.stride()
-    if (one != 1 and cols > 1) or (ld < cols and t.shape[0] > 1):
-        t, ld = t.contiguous(), cols
-    return t, (ld if ld > cols else cols)
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        return code, t.contiguous(), rows, cols, cols
+    return code, t, rows, cols, max(ld, cols)
+
+
+def _like(t, rows, cols, code, name):
+    """(t as a matrix, its row stride), t of the given sizes and type (None: any type)."""
+    got, t, r, c, ld = _matrix(t, name)
+    if (r != rows and rows is not None) or c != cols or (got != code and code is not None):
+        raise ValueError("%s must have %s rows of %d elements and the operands' type (got %s %s)"
+                         % (name, rows, cols, tuple(t.shape), t.dtype))
+    return t, ld
+
+
+def _weight(t, cols, code, name):
+    if t.dim() != 2 or t.shape[0] < 1:
+        raise ValueError("%s must have two axes (got %s)" % (name, tuple(t.shape)))
+    return _like(t, None, cols, code, name)
 
 
 def _vector(t, n, dtype, name):
+    """(t, its address), or Nones."""
     if t is None:
-        return None
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_cuda:
+        return None, None
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_cuda:
         raise ValueError("%s must be a CUDA %s tensor of shape (%d,) (got %s %s %s)"
                          % (name, dtype, n, t.device, t.dtype, tuple(t.shape)))
-    return t if t.is_contiguous() else t.contiguous()
+    if not t.is_contiguous():
+        t = t.contiguous()
+    return t, t.data_ptr()
 
 
-def _weight(t, cols, dtype, name):
-    if t.dim() != 2 or t.shape[0] < 1:
-        raise ValueError("%s must have two axes (got %s)" % (name, tuple(t.shape)))
-    return _rows(t, cols, name, dtype)
+def _saved(t, shape):
+    if t is None or t.shape != shape or t.dtype is not _F32 or not t.is_contiguous():
+        raise ValueError("saved must be what the forward returned for these rows")
+    return t.data_ptr()
+
+
+def _out_code(dtype, out_dtype):
+    code = _REAL.get(out_dtype)
+    if code is None or (out_dtype is not dtype and _F32 not in (dtype, out_dtype)):
+        raise ValueError("the output of %s operands must be %s, float32 or, from float32, a 16-bit type (got %s)"
+                         % (dtype, dtype, out_dtype))
+    return code
+
+
+def _act(activation):
+    code = _ACT.get(activation)
+    if code is None:
+        raise ValueError("activation must be one of %s (got %r)" % (sorted(_ACT), activation))
+    return code
 
 
 def _sized(query):
@@ -96,50 +117,65 @@ _gated_bytes = _sized(B.vqc_gated_workspace_bytes)
 
 
 def _workspace(nbytes):
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+    """(a workspace, its address): fresh for every call, so that calls of several
+    threads and streams never share one."""
+    if nbytes == 0:
+        return None, None
+    ws = _empty(nbytes, dtype=torch.uint8, device="cuda")
+    return ws, ws.data_ptr()
 
 
-def _aligned(*tensors):
-    for t in tensors:
-        if t.data_ptr() & 15:
-            return 0
-    return 1
+def _new(need, shape, like):
+    """(an output tensor of like's type, its address), or Nones."""
+    if not need:
+        return None, None
+    t = like.new_empty(shape)
+    return t, t.data_ptr()
+
+
+def _stream():
+    return _raw_stream(_device())
 
 
 # ------------------------------------------------------------------ layer norm
 
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, save=True):
     """y, or (y, saved) where ``save``: saved holds the rows' mean and 1 / sqrt(var + eps)."""
-    code, cols = _code(x, "x"), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    weight, bias = _vector(weight, cols, x.dtype, "weight"), _vector(bias, cols, x.dtype, "bias")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty(x2.shape[0], 2, dtype=torch.float32, device=x.device) if save else None
-    B.vqc_layer_norm_forward(code, x2.shape[0], cols, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), eps,
-                             y.data_ptr(), _ptr(stats), _here()[1])
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    weight, pw = _vector(weight, cols, x.dtype, "weight")
+    bias, pb = _vector(bias, cols, x.dtype, "bias")
+    y, py = _new(True, x.shape, x)
+    stats = _empty(rows, 2, dtype=_F32, device=x.device) if save else None
+    st = B.lib().vqc_layer_norm_forward(code, rows, cols, x2.data_ptr(), ld, pw, pb, eps, py,
+                                        stats.data_ptr() if save else None, _stream())
+    if st:
+        B._check(st)
     return (y, stats) if save else y
 
 
 def layer_norm_backward(grad_y, x, weight, saved, need_x=True, need_weight=True, need_bias=True):
     """(grad_x, grad_weight, grad_bias), None for those not needed."""
-    code, cols = _code(x, "x"), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    rows = x2.shape[0]
-    gy, ld_gy = _rows(grad_y, cols, "grad_y", x.dtype, rows)
-    weight = _vector(weight, cols, x.dtype, "weight")
-    if saved.shape != (rows, 2) or saved.dtype is not torch.float32 or not saved.is_contiguous():
-        raise ValueError("saved must be what layer_norm_forward returned for these rows")
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
-    gw = torch.empty(cols, dtype=x.dtype, device=x.device) if need_weight else None
-    gb = torch.empty(cols, dtype=x.dtype, device=x.device) if need_bias else None
-    ws, nbytes = None, 0
-    if need_weight or need_bias:
-        nbytes = _norm_bytes(rows, cols)
-        ws = _workspace(nbytes)
-    B.vqc_layer_norm_backward(code, rows, cols, gy.data_ptr(), ld_gy, x2.data_ptr(), ld, _ptr(weight),
-                              saved.data_ptr(), _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws), nbytes,
-                              _here()[1])
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    gy, ld_gy = _like(grad_y, rows, cols, code, "grad_y")
+    weight, pw = _vector(weight, cols, x.dtype, "weight")
+    stats = _saved(saved, (rows, 2))
+    gx, px = _new(need_x, x.shape, x)
+    gw, pgw = _new(need_weight, cols, x)
+    gb, pgb = _new(need_bias, cols, x)
+    nbytes = _norm_bytes(rows, cols) if need_weight or need_bias else 0
+    ws, pws = _workspace(nbytes)
+    st = B.lib().vqc_layer_norm_backward(code, rows, cols, gy.data_ptr(), ld_gy, x2.data_ptr(), ld, pw, stats, px, pgw,
+                                         pgb, pws, nbytes, _stream())
+    if st:
+        B._check(st)
     return gx, gw, gb
+
+
+def _norm_gradients(ctx, gy):
+    x, weight, stats = ctx.saved_tensors
+    need = ctx.needs_input_grad
+    gx, gw, gb = layer_norm_backward(gy, x, weight, stats, need[0], need[1], need[2])
+    return gx, gw, gb, None
 
 
 class LayerNormFunction(torch.autograd.Function):
@@ -149,13 +185,7 @@ class LayerNormFunction(torch.autograd.Function):
         ctx.save_for_backward(x, weight, stats)
         return y
 
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, gy):
-        x, weight, stats = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        gx, gw, gb = layer_norm_backward(gy, x, weight, stats, need[0], need[1], need[2])
-        return gx, gw, gb, None
+    backward = staticmethod(once_differentiable(_norm_gradients))
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
@@ -168,43 +198,59 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 def linear_forward(x, weight, bias=None, activation="none", residual=None, out_dtype=None, save=True):
     """y = act(x weight^T + bias) + residual, or (y, saved) where ``save``:
     saved holds the float32 pre-activations (None where there is no activation)."""
-    code, act, cols = _code(x, "x"), _act(activation), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    w, ld_w = _weight(weight, cols, x.dtype, "weight")
-    rows, out = x2.shape[0], w.shape[0]
-    bias = _vector(bias, out, x.dtype, "bias")
-    y_type = x.dtype if out_dtype is None else out_dtype
-    res, ld_res = (None, 0) if residual is None else _rows(residual, out, "residual", y_type, rows)
-    y_code = _out_code(x.dtype, y_type)
-    nbytes = _linear_bytes(0, code, y_code, rows, cols, out, ld, ld_w, 0, act, _aligned(x2, w))
-    ws = _workspace(nbytes)
-    y = torch.empty(x.shape[:-1] + (out,), dtype=y_type, device=x.device)
-    z = torch.empty(rows, out, dtype=torch.float32, device=x.device) if save and act else None
-    B.vqc_linear_forward(code, y_code, rows, cols, out, x2.data_ptr(), ld, w.data_ptr(), ld_w, _ptr(bias), act,
-                         _ptr(res), ld_res, y.data_ptr(), _ptr(z), _ptr(ws), nbytes, _here()[1])
+    act = _act(activation)
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    w, ld_w = _weight(weight, cols, code, "weight")
+    out = w.shape[0]
+    bias, pb = _vector(bias, out, x.dtype, "bias")
+    y_type, y_code = (x.dtype, code) if out_dtype is None else (out_dtype, _out_code(x.dtype, out_dtype))
+    res = pr = None
+    ld_res = 0
+    if residual is not None:
+        res, ld_res = _like(residual, rows, out, y_code, "residual")
+        pr = res.data_ptr()
+    px, pw = x2.data_ptr(), w.data_ptr()
+    nbytes = _linear_bytes(0, code, y_code, rows, cols, out, ld, ld_w, 0, act, 0 if (px | pw) & 15 else 1)
+    ws, pws = _workspace(nbytes)
+    y = _empty(x.shape[:-1] + (out,), dtype=y_type, device=x.device)
+    z = _empty(rows, out, dtype=_F32, device=x.device) if save and act else None
+    st = B.lib().vqc_linear_forward(code, y_code, rows, cols, out, px, ld, pw, ld_w, pb, act, pr, ld_res, y.data_ptr(),
+                                    None if z is None else z.data_ptr(), pws, nbytes, _stream())
+    if st:
+        B._check(st)
     return (y, z) if save else y
 
 
 def linear_backward(grad_y, x, weight, saved, activation="none", need_x=True, need_weight=True, need_bias=True):
     """(grad_x, grad_weight, grad_bias), None for those not needed.  The
     residual's gradient is grad_y."""
-    code, act, cols = _code(x, "x"), _act(activation), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    w, ld_w = _weight(weight, cols, x.dtype, "weight")
-    rows, out = x2.shape[0], w.shape[0]
+    act = _act(activation)
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    w, ld_w = _weight(weight, cols, code, "weight")
+    out = w.shape[0]
     y_code = _out_code(x.dtype, grad_y.dtype)
-    gy, ld_gy = _rows(grad_y, out, "grad_y", None, rows)
-    if act and (saved is None or saved.shape != (rows, out) or saved.dtype is not torch.float32
-                or not saved.is_contiguous()):
-        raise ValueError("saved must be what linear_forward returned for these rows")
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
-    gw = torch.empty(out, cols, dtype=x.dtype, device=x.device) if need_weight else None
-    gb = torch.empty(out, dtype=x.dtype, device=x.device) if need_bias else None
-    nbytes = _linear_bytes(1, code, y_code, rows, cols, out, ld, ld_w, ld_gy, act, _aligned(x2, w, gy))
-    ws = _workspace(nbytes)
-    B.vqc_linear_backward(code, y_code, rows, cols, out, gy.data_ptr(), ld_gy, x2.data_ptr(), ld, w.data_ptr(),
-                          ld_w, _ptr(saved), act, _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws), nbytes, _here()[1])
+    gy, ld_gy = _like(grad_y, rows, out, y_code, "grad_y")
+    pz = _saved(saved, (rows, out)) if act else None
+    gx, pgx = _new(need_x, x.shape, x)
+    gw, pgw = _new(need_weight, (out, cols), x)
+    gb, pgb = _new(need_bias, out, x)
+    px, pw, pg = x2.data_ptr(), w.data_ptr(), gy.data_ptr()
+    nbytes = _linear_bytes(1, code, y_code, rows, cols, out, ld, ld_w, ld_gy, act, 0 if (px | pw | pg) & 15 else 1)
+    ws, pws = _workspace(nbytes)
+    st = B.lib().vqc_linear_backward(code, y_code, rows, cols, out, pg, ld_gy, px, ld, pw, ld_w, pz, act, pgx, pgw, pgb,
+                                     pws, nbytes, _stream())
+    if st:
+        B._check(st)
     return gx, gw, gb
+
+
+def _linear_gradients(ctx, gy):
+    x, weight, z = ctx.saved_tensors
+    need = ctx.needs_input_grad
+    gx = gw = gb = None
+    if need[0] or need[1] or need[2]:
+        gx, gw, gb = linear_backward(gy, x, weight, z, ctx.activation, need[0], need[1], need[2])
+    return gx, gw, gb, None, (gy if need[4] else None), None
 
 
 class LinearFunction(torch.autograd.Function):
@@ -215,15 +261,7 @@ class LinearFunction(torch.autograd.Function):
         ctx.save_for_backward(x, weight, z)
         return y
 
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, gy):
-        x, weight, z = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        gx = gw = gb = None
-        if need[0] or need[1] or need[2]:
-            gx, gw, gb = linear_backward(gy, x, weight, z, ctx.activation, need[0], need[1], need[2])
-        return gx, gw, gb, None, (gy if need[4] else None), None
+    backward = staticmethod(once_differentiable(_linear_gradients))
 
 
 def linear(x, weight, bias=None, activation="none", residual=None, out_dtype=None):
@@ -236,12 +274,12 @@ def linear(x, weight, bias=None, activation="none", residual=None, out_dtype=Non
 
 # ------------------------------------------------------------------ gated
 
-def _pair(weight_gate, weight_up, cols, dtype):
+def _pair(weight_gate, weight_up, cols, code):
     if weight_gate.shape != weight_up.shape:
         raise ValueError("weight_gate and weight_up must have one shape (got %s and %s)"
                          % (tuple(weight_gate.shape), tuple(weight_up.shape)))
-    wg, ld_g = _weight(weight_gate, cols, dtype, "weight_gate")
-    wu, ld_u = _weight(weight_up, cols, dtype, "weight_up")
+    wg, ld_g = _weight(weight_gate, cols, code, "weight_gate")
+    wu, ld_u = _weight(weight_up, cols, code, "weight_up")
     if ld_g != ld_u:
         wg, wu, ld_g = wg.contiguous(), wu.contiguous(), cols
     return wg, wu, ld_g
@@ -249,17 +287,21 @@ def _pair(weight_gate, weight_up, cols, dtype):
 
 def gated_forward(x, weight_gate, weight_up, bias_gate=None, bias_up=None, activation="silu", save=True):
     """h = act(g) * u, or (h, saved) where ``save``: saved holds g and u in float32."""
-    code, act, cols = _code(x, "x"), _act(activation), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    wg, wu, ld_w = _pair(weight_gate, weight_up, cols, x.dtype)
-    rows, out = x2.shape[0], wg.shape[0]
-    bg, bu = _vector(bias_gate, out, x.dtype, "bias_gate"), _vector(bias_up, out, x.dtype, "bias_up")
-    nbytes = _gated_bytes(0, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
-    ws = _workspace(nbytes)
-    h = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=x.device)
-    z = torch.empty(2, rows, out, dtype=torch.float32, device=x.device) if save else None
-    B.vqc_gated_forward(code, rows, cols, out, x2.data_ptr(), ld, wg.data_ptr(), wu.data_ptr(), ld_w, _ptr(bg),
-                        _ptr(bu), act, h.data_ptr(), _ptr(z), _ptr(ws), nbytes, _here()[1])
+    act = _act(activation)
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    wg, wu, ld_w = _pair(weight_gate, weight_up, cols, code)
+    out = wg.shape[0]
+    bias_gate, pbg = _vector(bias_gate, out, x.dtype, "bias_gate")
+    bias_up, pbu = _vector(bias_up, out, x.dtype, "bias_up")
+    px, pwg, pwu = x2.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    nbytes = _gated_bytes(0, code, rows, cols, out, ld, ld_w, 0 if (px | pwg | pwu) & 15 else 1)
+    ws, pws = _workspace(nbytes)
+    h, ph = _new(True, x.shape[:-1] + (out,), x)
+    z = _empty(2, rows, out, dtype=_F32, device=x.device) if save else None
+    st = B.lib().vqc_gated_forward(code, rows, cols, out, px, ld, pwg, pwu, ld_w, pbg, pbu, act, ph,
+                                   None if z is None else z.data_ptr(), pws, nbytes, _stream())
+    if st:
+        B._check(st)
     return (h, z) if save else h
 
 
@@ -267,22 +309,32 @@ def gated_backward(grad_h, x, weight_gate, weight_up, saved, activation="silu", 
                    need_bias=True):
     """(grad_x, grad_weight_gate, grad_weight_up, grad_bias_gate, grad_bias_up),
     None for those not needed."""
-    code, act, cols = _code(x, "x"), _act(activation), x.shape[-1] if x.dim() else 0
-    x2, ld = _rows(x, cols, "x")
-    wg, wu, ld_w = _pair(weight_gate, weight_up, cols, x.dtype)
-    rows, out = x2.shape[0], wg.shape[0]
-    gh, ld_gh = _rows(grad_h, out, "grad_h", x.dtype, rows)
-    if saved.shape != (2, rows, out) or saved.dtype is not torch.float32 or not saved.is_contiguous():
-        raise ValueError("saved must be what gated_forward returned for these rows")
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
-    gw = [torch.empty(out, cols, dtype=x.dtype, device=x.device) if need_weight else None for _ in range(2)]
-    gb = [torch.empty(out, dtype=x.dtype, device=x.device) if need_bias else None for _ in range(2)]
-    nbytes = _gated_bytes(1, code, rows, cols, out, ld, ld_w, _aligned(x2, wg, wu))
-    ws = _workspace(nbytes)
-    B.vqc_gated_backward(code, rows, cols, out, gh.data_ptr(), ld_gh, x2.data_ptr(), ld, wg.data_ptr(),
-                         wu.data_ptr(), ld_w, saved.data_ptr(), act, _ptr(gx), _ptr(gw[0]), _ptr(gw[1]),
-                         _ptr(gb[0]), _ptr(gb[1]), _ptr(ws), nbytes, _here()[1])
-    return gx, gw[0], gw[1], gb[0], gb[1]
+    act = _act(activation)
+    code, x2, rows, cols, ld = _matrix(x, "x")
+    wg, wu, ld_w = _pair(weight_gate, weight_up, cols, code)
+    out = wg.shape[0]
+    gh, ld_gh = _like(grad_h, rows, out, code, "grad_h")
+    pz = _saved(saved, (2, rows, out))
+    gx, pgx = _new(need_x, x.shape, x)
+    gwg, pgwg = _new(need_weight, (out, cols), x)
+    gwu, pgwu = _new(need_weight, (out, cols), x)
+    gbg, pgbg = _new(need_bias, out, x)
+    gbu, pgbu = _new(need_bias, out, x)
+    px, pwg, pwu, pg = x2.data_ptr(), wg.data_ptr(), wu.data_ptr(), gh.data_ptr()
+    nbytes = _gated_bytes(1, code, rows, cols, out, ld, ld_w, 0 if (px | pwg | pwu | pg) & 15 else 1)
+    ws, pws = _workspace(nbytes)
+    st = B.lib().vqc_gated_backward(code, rows, cols, out, pg, ld_gh, px, ld, pwg, pwu, ld_w, pz, act, pgx, pgwg, pgwu,
+                                    pgbg, pgbu, pws, nbytes, _stream())
+    if st:
+        B._check(st)
+    return gx, gwg, gwu, gbg, gbu
+
+
+def _gated_gradients(ctx, gh):
+    x, wg, wu, z = ctx.saved_tensors
+    need = ctx.needs_input_grad
+    got = gated_backward(gh, x, wg, wu, z, ctx.activation, need[0], need[1] or need[2], need[3] or need[4])
+    return tuple(g if n else None for g, n in zip(got, need)) + (None,)
 
 
 class GatedFunction(torch.autograd.Function):
@@ -293,13 +345,7 @@ class GatedFunction(torch.autograd.Function):
         ctx.save_for_backward(x, weight_gate, weight_up, z)
         return h
 
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, gh):
-        x, wg, wu, z = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        got = gated_backward(gh, x, wg, wu, z, ctx.activation, need[0], need[1] or need[2], need[3] or need[4])
-        return tuple(g if n else None for g, n in zip(got, need)) + (None,)
+    backward = staticmethod(once_differentiable(_gated_gradients))
 
 
 def gated(x, weight_gate, weight_up, bias_gate=None, bias_up=None, activation="silu"):
