@@ -1,21 +1,26 @@
-"""Build ``libvqc.so`` in-tree with nvcc for sm_103a (GB300).
+"""Build ``libvqc.so`` in-tree with nvcc for sm_103a (GB300), and ``_layers.so``.
 
 The translation units (host compiler, C ABI, one kernel unit per real type and
 mode) compile in parallel; the result is linked into one shared library next
-to this file.  Nothing is installed outside the source tree.
+to this file.  The torch binding of the layer operators (host code) compiles beside
+them with the host compiler.  Nothing is installed outside the source tree.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import hashlib
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 OUT = os.path.join(HERE, "libvqc.so")
+OUT_LAYERS = os.path.join(HERE, "_layers.so")
 BUILD = os.path.join(HERE, "_build")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -46,6 +51,7 @@ def _sources_digest() -> str:
             h.update(name.encode() + f.read())
     with open(os.path.join(ROOT, "include", "vqc.h"), "rb") as f:
         h.update(f.read())
+    h.update(importlib.metadata.version("torch").encode())     # _layers.so is built against it
     # flags without the include path, so that a checkout anywhere hashes alike
     h.update(" ".join(ARCH + [f for f in NVCC_FLAGS if not f.startswith("-I")]).encode())
     return h.hexdigest()
@@ -55,7 +61,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     """Compile and link libvqc.so if the sources changed; return its path."""
     digest = _sources_digest()
     stamp = OUT + ".sha256"
-    if not force and os.path.exists(OUT) and os.path.exists(stamp):
+    if not force and os.path.exists(OUT) and os.path.exists(OUT_LAYERS) and os.path.exists(stamp):
         with open(stamp) as f:
             if f.read().strip() == digest:
                 return OUT
@@ -73,8 +79,26 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             raise RuntimeError("nvcc failed for %s:\n%s%s" % (unit, r.stdout, r.stderr))
         return obj, r.stdout + r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=len(UNITS)) as ex:
+    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
+    layers_obj = os.path.join(BUILD, "layers_torch.cpp.o")
+
+    def host(*args):
+        r = subprocess.run(["g++", *args], capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("g++ failed for _layers.so:\n%s%s" % (r.stdout, r.stderr))
+
+    def compile_layers():
+        inc = os.path.join(torch_dir, "include")
+        host("-O2", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"),
+             "-I" + sysconfig.get_paths()["include"], "-isystem", inc, "-isystem",
+             os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem",
+             os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(cc))), "include"),
+             "-c", os.path.join(CSRC, "layers_torch.cpp"), "-o", layers_obj)
+
+    with cf.ThreadPoolExecutor(max_workers=len(UNITS) + 1) as ex:
+        layers = ex.submit(compile_layers)
         results = list(ex.map(compile_one, UNITS))
+        layers.result()
     if verbose or ptxas_info:
         for _, log in results:
             if log.strip():
@@ -85,6 +109,11 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s%s" % (r.stdout, r.stderr))
     os.replace(tmp, OUT)
+    tmp = OUT_LAYERS + ".tmp.%d" % os.getpid()
+    lib = os.path.join(torch_dir, "lib")
+    host("-shared", "-o", tmp, layers_obj, "-L" + HERE, "-l:libvqc.so", "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch",
+         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN")
+    os.replace(tmp, OUT_LAYERS)
     with open(stamp, "w") as f:
         f.write(digest)
     return OUT

@@ -396,3 +396,33 @@ def test_refusals_on_the_gpu(layers):
         with pytest.raises(ValueError):
             call()
     sync()
+
+
+@pytest.mark.parametrize("which", ["layer_norm", "linear", "gated"])
+def test_operands_left_out_and_second_derivatives(layers, which):
+    """Every combination of optional operands and of inputs that need a gradient;
+    create_graph gives the gradients and refuses theirs."""
+    x, w, u = normal(1, 30, 16).cuda(), normal(2, 12, 16).cuda(), normal(3, 12, 16).cuda()
+    b, c, r, nw, nb = (normal(i, *s).cuda() for i, s in ((4, (12,)), (5, (12,)), (6, (30, 12)), (7, (16,)), (8, (16,))))
+    for given in range(4):
+        first, second = given & 1, given >> 1
+        if which == "layer_norm":
+            ops, f = [x, nw if first else None, nb if second else None], layers.layer_norm
+        elif which == "linear":
+            ops, f = [x, w, b if first else None, r if second else None], \
+                lambda x, w, b, r: layers.linear(x, w, b, "none" if given == 3 else "tanh", r)
+        else:
+            ops, f = [x, w, u, b if first else None, c if second else None], layers.gated
+        present = [i for i, t in enumerate(ops) if t is not None]
+        full = [t.clone().requires_grad_() if t is not None else None for t in ops]
+        y = f(*full)
+        gy = normal(9, *y.shape).cuda()
+        want = dict(zip(present, torch.autograd.grad(y, [full[i] for i in present], gy, create_graph=True)))
+        with pytest.raises(RuntimeError, match="once"):
+            torch.autograd.grad(want[0].sum(), full[0])
+        with torch.no_grad():
+            assert torch.equal(f(*full), y) and not f(*full).requires_grad
+        for i in present:                      # this input alone needs a gradient
+            some = [t.clone().requires_grad_(k == i) if t is not None else None for k, t in enumerate(ops)]
+            got, = torch.autograd.grad(f(*some), [some[i]], gy)
+            assert torch.equal(got, want[i]), (given, i)
