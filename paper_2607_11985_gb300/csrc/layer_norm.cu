@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, 1024 / Row<VEC, WARPS>:
 norm_forward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
     __shared__ float buf[2][WARPS];
+    stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
     for (int64_t r = R::first(); r < A.rows; r += R::step()) {
@@ -183,6 +184,7 @@ template <typename T, int VEC, int WARPS, int NV>
 __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
     __shared__ float2 buf[2][WARPS];
+    stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
     float gw[NV][VEC], gb[NV][VEC];
@@ -271,6 +273,7 @@ constexpr int kLong = 512;
 
 template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long(const __grid_constant__ NormArgs A) {
     __shared__ float buf[2][kLong / 32];
+    stream_order();
     for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
         float s = 0.f;
@@ -294,6 +297,7 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long
 
 template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_long(const __grid_constant__ NormArgs A) {
     __shared__ float2 buf[2][kLong / 32];
+    stream_order();
     int turn = 0;
     for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x, turn ^= 1) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
@@ -318,6 +322,7 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_lon
 
 // Column sums over `per` rows: thread = column.
 template <typename T> __global__ void __launch_bounds__(256) norm_columns_long(const __grid_constant__ NormArgs A, int64_t per) {
+    stream_order();
     const int64_t across = (A.cols + 255) / 256, block = blockIdx.x / across, blocks = gridDim.x / across;
     const int64_t c = blockIdx.x % across * 256 + threadIdx.x;
     if (c >= A.cols) return;
@@ -436,10 +441,9 @@ vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, co
         void* args[] = {&a};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         if (cols > kMostForward)
-            return launched(cudaLaunchKernel(long_kernel(dtype, 0), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())),
-                                             dim3(kLong), args, 0, s));
+            return launched(launch(long_kernel(dtype, 0), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())), kLong, args, s));
         const Plan p = choose_plan(dtype, true, cols, packs(e, cols, {x, weight, bias, y}, {x_stride}));
-        return launched(cudaLaunchKernel(p.fn, dim3((unsigned)row_ctas(p.warps, rows, 0x7fffffff)), dim3(p.threads), args, 0, s));
+        return launched(launch(p.fn, dim3((unsigned)row_ctas(p.warps, rows, 0x7fffffff)), p.threads, args, s));
     } catch (...) {
         return VQC_ERR_OUT_OF_MEMORY;
     }
@@ -477,22 +481,21 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             int64_t per = ceil_div(rows, kLongBlocks);
             void* args[] = {&a, &per};
             if (grad_x) {
-                const cudaError_t err = cudaLaunchKernel(long_kernel(dtype, 1), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())),
-                                                         dim3(kLong), args, 0, s);
+                const cudaError_t err = launch(long_kernel(dtype, 1), dim3((unsigned)std::min<int64_t>(rows, 4LL * sm_count())), kLong, args, s);
                 if (err != cudaSuccess) return launched(err);
             }
             if (columns) {
                 blocks = ceil_div(rows, per);
                 const int64_t grid = blocks * ceil_div(cols, 256);
                 if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "vqc_layer_norm_backward: too many columns");
-                const cudaError_t err = cudaLaunchKernel(long_kernel(dtype, 2), dim3((unsigned)grid), dim3(256), args, 0, s);
+                const cudaError_t err = launch(long_kernel(dtype, 2), dim3((unsigned)grid), 256, args, s);
                 if (err != cudaSuccess) return launched(err);
             }
         } else if (rows > 0) {
             const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
             blocks = columns ? backward_ctas(cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
             void* args[] = {&a};
-            const cudaError_t err = cudaLaunchKernel(p.fn, dim3((unsigned)blocks), dim3(p.threads), args, 0, s);
+            const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s);
             if (err != cudaSuccess) return launched(err);
         }
         return columns ? sum_run(a.part, blocks, cols, cols, blocks * cols, grad_weight, grad_bias, dtype, s) : VQC_OK;

@@ -22,6 +22,12 @@ inline size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 vqc_status cuda_error(cudaError_t e, const char* what);
+
+// A launch that may begin while the kernel before it in the stream ends: its CTAs are
+// placed and set up, then wait in stream_order() (layers_elem.cuh), which every kernel
+// here calls before it touches memory.  Between two dependent kernels this takes
+// away about 2 us.
+cudaError_t launch(const void* fn, dim3 grid, int threads, void** args, cudaStream_t s, size_t shared = 0, int cluster = 1);
 int sm_count();   // of the current device (the GB300's 152 where there is none)
 
 // A matrix operand of a product: element (i, k) of the outer index i and the

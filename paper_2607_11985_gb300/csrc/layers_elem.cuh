@@ -10,6 +10,14 @@
 namespace vqc {
 namespace layers {
 
+// Lets the next kernel of the stream be placed, and waits until those before have
+// ended and their writes are seen.  In every thread, before any access to memory
+// that another kernel may write.
+__device__ __forceinline__ void stream_order() {
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+}
+
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }

@@ -17,6 +17,23 @@ vqc_status cuda_error(cudaError_t e, const char* what) {
     return set_error(VQC_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
 
+cudaError_t launch(const void* fn, dim3 grid, int threads, void** args, cudaStream_t s, size_t shared, int cluster) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
 int sm_count() {
     static std::atomic<int> known[64];
     int dev = 0, sms = 0;
@@ -105,6 +122,7 @@ template <int W> struct Slice {
 // outputs), so that both factors of an output meet in one thread.
 template <int BM, int BN, int TM, int TN>
 __global__ void __launch_bounds__(NT) product_kernel(const __grid_constant__ ProductPair P) {
+    stream_order();
     constexpr int TX = BN / TN, TH = TN / 2;
     static_assert((BM / TM) * TX == NT && TN % 2 == 0, "tile");
     __shared__ __align__(16) float sa[2][BK][BM + 4], sb[2][BK][BN + 4];
@@ -221,13 +239,40 @@ template <int W> __device__ __forceinline__ void join_at(const Join& j, int whic
     }
     finish_some<W>(j.f, which, row, col, v0, v1);
 }
+// One row of many cuts (column sums): a warp's lanes take 32 columns, warp w the cuts w,
+// w + 8, ..., then the eight sums are added.
+__device__ __forceinline__ void join_row(const Join& j, int which, int64_t stride) {
+    __shared__ float sums[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t n = j.f.n;
+    for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < n; c0 += (int64_t)gridDim.x * 32) {
+        float v = 0.f;
+        if (c0 + lane < n) {
+            const float* p = j.part + which * n + c0 + lane;
+#pragma unroll 8
+            for (int s = warp; s < j.splits; s += 8) v += p[s * stride];
+        }
+        sums[warp][lane] = v;
+        __syncthreads();
+        if (warp == 0 && c0 + lane < n) {
+            v = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += sums[i][lane];
+            finish_one(j.f, which, 0, c0 + lane, v, 0.f);
+        }
+        __syncthreads();
+    }
+}
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Joins J) {
+    stream_order();
     const Join& j = J.j[blockIdx.y >> 1];
     const int which = blockIdx.y & 1;
     if (which && j.form != PAIR) return;
     const int64_t size = j.f.m * j.f.n, step = (int64_t)gridDim.x * blockDim.x, at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t stride = size * (j.form == GATED || j.form == PAIR ? 2 : 1);
-    if (j.f.n % 4 == 0) {
+    if (j.f.m == 1 && j.form != GATED && !j.exact.k && j.splits >= 8) {
+        join_row(j, which, stride);
+    } else if (j.f.n % 4 == 0) {
         for (int64_t e = 4 * at; e < size; e += 4 * step) join_at<4>(j, which, size, stride, e);
     } else {
         for (int64_t e = at; e < size; e += step) join_at<1>(j, which, size, stride, e);
@@ -290,10 +335,10 @@ vqc_status product_args(const Product& p, Tile t, void* ws, size_t ws_bytes, Pro
 vqc_status join_run(const Joins& joins, cudaStream_t s) {
     if (!joins.count) return VQC_OK;
     int64_t most = 1;
-    for (int i = 0; i < joins.count; ++i) most = std::max(most, joins.j[i].f.m * joins.j[i].f.n);
+    for (int i = 0; i < joins.count; ++i) most = std::max(most, joins.j[i].f.m * joins.j[i].f.n * (joins.j[i].f.m == 1 ? 8 : 1));
     void* args[] = {const_cast<Joins*>(&joins)};
-    const cudaError_t e = cudaLaunchKernel((const void*)join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), 2 * joins.count),
-                                           dim3(256), args, 0, s);
+    const cudaError_t e = launch((const void*)join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), 2 * joins.count),
+                                 256, args, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "join launch");
 }
 
@@ -302,7 +347,7 @@ void products_workspace(const Product* p, int count, bool aligned, size_t* bytes
     int index[2], have = 0;
     for (int i = 0; i < count; ++i) {
         bytes[i] = 0;
-        if (p[i].m == 0 || rows_takes(p[i])) continue;
+        if (p[i].m == 0 || rows_takes(p[i], aligned)) continue;
         if (tc_takes(p[i])) {
             tc[have] = p[i];
             index[have++] = i;
@@ -325,8 +370,9 @@ vqc_status products_run(const Product* p, int count, void* const* ws, const size
     for (int i = 0; i < count; ++i) {
         if (p[i].m == 0 || p[i].n == 0) continue;
         vqc_status st = VQC_OK;
-        if (rows_takes(p[i])) {
-            st = rows_run(p[i], s);
+        const bool aligned = aligned_to(p[i].a[0].p, 16) && aligned_to(p[i].b[0].p, 16) && aligned_to(p[i].b[1].p, 16);
+        if (rows_takes(p[i], aligned)) {
+            st = rows_run(p[i], aligned, s);
         } else if (tc_takes(p[i])) {
             tc[tcs] = p[i];
             tc_ws[tcs] = ws[i];
@@ -348,7 +394,7 @@ vqc_status products_run(const Product* p, int count, void* const* ws, const size
         if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "product: too many tiles");
         void* args[] = {&pair[kind]};
         const void* fn = kind ? (const void*)product_kernel<128, 16, 4, 2> : (const void*)product_kernel<64, 64, 4, 4>;
-        const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(NT), args, 0, s);
+        const cudaError_t e = launch(fn, dim3((unsigned)grid), NT, args, s);
         if (e != cudaSuccess) return cuda_error(e, "product launch");
     }
     return VQC_OK;
@@ -469,6 +515,7 @@ __device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
     __shared__ float sums[8][kGradCols];
+    stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across;
     const int64_t c0 = blockIdx.x % across * kGradCols, c = c0 + (VEC ? 8 * lane : lane);
@@ -497,6 +544,7 @@ __global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant_
 __global__ void __launch_bounds__(1024) sum_kernel(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second,
                                                    void* out0, void* out1, int dtype) {
     __shared__ float sums[32][33];
+    stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     void* out = blockIdx.y ? out1 : out0;
@@ -526,8 +574,7 @@ int64_t grad_rows(int64_t rows, int64_t n) {
 vqc_status sum_run(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second, void* out0, void* out1, int dtype,
                    cudaStream_t s) {
     void* args[] = {&part, &count, &n, &ld, &second, &out0, &out1, &dtype};
-    const cudaError_t e = cudaLaunchKernel((const void*)sum_kernel, dim3((unsigned)ceil_div(n, 32), out1 ? 2 : 1),
-                                           dim3(1024), args, 0, s);
+    const cudaError_t e = launch((const void*)sum_kernel, dim3((unsigned)ceil_div(n, 32), out1 ? 2 : 1), 1024, args, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "sum launch");
 }
 
@@ -551,15 +598,10 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
         const void* fn = a.dtype == VQC_F32 ? (vec ? (const void*)act_grad_kernel<float, true> : (const void*)act_grad_kernel<float, false>)
                          : a.dtype == VQC_BF16 ? (vec ? (const void*)act_grad_kernel<__nv_bfloat16, true> : (const void*)act_grad_kernel<__nv_bfloat16, false>)
                                                : (vec ? (const void*)act_grad_kernel<__half, true> : (const void*)act_grad_kernel<__half, false>);
-        const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(256), args, 0, s);
+        const cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
     if (!sums) return VQC_OK;
-    // A thread of the join adds up to 64 blocks one by one; more take a kernel of their own.
-    if (blocks > 64) {
-        const int64_t ld = a.n * (a.gated ? 2 : 1);
-        return sum_run(part, blocks, a.n, ld, a.n, a.sum[0], a.gated ? a.sum[1] : nullptr, a.dtype, s);
-    }
     Join& j = joins.j[joins.count++];
     j.f.m = 1;
     j.f.n = a.n;

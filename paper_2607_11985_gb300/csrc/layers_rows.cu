@@ -1,7 +1,7 @@
 // layers_rows.cu -- products with few rows (single tokens, small batches): the
 // weights are all there is to read, so they stream through registers once.
 //
-// A group of KW warps takes four rows of weights (two of each in GATED form) and
+// Two kernels.  Up to 4 rows of any type and layout, FP32 units: a group of KW warps takes four rows of weights (two of each in GATED form) and
 // up to 4 rows of x; a lane holds 16 bytes of each weight row per step, the
 // group's warps take turns along k.  Sums are packed pairs of floats (even and
 // odd k), joined over the lanes, then over the warps, in a fixed order.
@@ -52,6 +52,7 @@ template <typename T, int VEC, int R, bool GATE>
 __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant__ RowsArgs A) {
     constexpr int C = GATE ? kWeights / 2 : kWeights;   // output columns of a group
     __shared__ float sums[kWarps][R * kWeights];
+    stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = A.kw;
     const int64_t group = (int64_t)blockIdx.x * (kWarps / kw) + warp / kw, c0 = group * C;
     const int64_t n = A.f.n;
@@ -112,6 +113,88 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
     }
 }
 
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2], __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2], __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+// A group of KW warps takes 16 rows of weights (8 of each in GATED form: then both
+// factors of an output are in one lane) and NB * 8 rows of x.  Lane 4 g + q loads 16
+// bytes, k = 8 q + [0, 8) of the step's 32, of weight rows g and g + 8 and of rows g
+// (and g + 8) of x; a contraction may take its elements in any order, so these are the
+// operands of two products of depth 16 as they are: no shared memory, no shuffles.
+template <typename T, int NB, bool GATE>
+__global__ void __launch_bounds__(kWarps * 32) mma_rows_kernel(const __grid_constant__ RowsArgs A) {
+    constexpr int C = GATE ? 8 : 16, U = 4;      // columns of a group, steps in flight
+    __shared__ float sums[kWarps][NB * 4][33];
+    stream_order();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = A.kw, g = lane >> 2;
+    const int64_t group = (int64_t)blockIdx.x * (kWarps / kw) + warp / kw, c0 = group * C, n = A.f.n;
+    const int m = (int)A.f.m;
+    const int64_t second = GATE ? c0 + g : c0 + g + 8;
+    const T* w0 = static_cast<const T*>(A.w0) + min(c0 + g, n - 1) * A.ld_w;
+    const T* w1 = static_cast<const T*>(GATE ? A.w1 : A.w0) + min(second, n - 1) * A.ld_w;
+    const T* x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) x[b] = static_cast<const T*>(A.x) + min(8 * b + g, m - 1) * A.ld_x;
+    float acc[NB][4] = {};
+    if (c0 < n) {
+        const int64_t step = 32 * kw;
+        for (int64_t k0 = 32 * (warp % kw); k0 < A.k; k0 += U * step) {
+            uint4 a[U], b[U], y[U][NB];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t k = k0 + u * step + 8 * (lane & 3);
+                const bool in = k < A.k;
+                const uint4 zero = make_uint4(0, 0, 0, 0);
+                a[u] = in ? __ldcs(reinterpret_cast<const uint4*>(w0 + k)) : zero;
+                b[u] = in ? __ldcs(reinterpret_cast<const uint4*>(w1 + k)) : zero;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) y[u][i] = in ? *reinterpret_cast<const uint4*>(x[i] + k) : zero;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const uint32_t a0[4] = {a[u].x, b[u].x, a[u].y, b[u].y}, a1[4] = {a[u].z, b[u].z, a[u].w, b[u].w};
+                    const uint32_t y0[2] = {y[u][i].x, y[u][i].y}, y1[2] = {y[u][i].z, y[u][i].w};
+                    mma_16816(acc[i], a0, y0, T());
+                    mma_16816(acc[i], a1, y1, T());
+                }
+        }
+    }
+    // sums of weight rows g (0, 1) and g + 8 (2, 3) with rows 2 q and 2 q + 1 of x
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[warp][4 * i + e][lane] = acc[i][e];
+    __syncthreads();
+    const int groups = kWarps / kw;
+    for (int e = threadIdx.x; e < groups * 8 * NB * C; e += kWarps * 32) {
+        const int q = e / (8 * NB * C), r = e / C % (8 * NB), i = e % C;       // group, row of x, column
+        const int64_t c = ((int64_t)blockIdx.x * groups + q) * C + i;
+        if (r >= m || c >= n) continue;
+        const int at = 4 * (r / 8) + (r & 1), from = 4 * (i & 7) + (r % 8) / 2;
+        float v0 = 0.f, v1 = 0.f;
+        for (int k = 0; k < kw; ++k) {
+            v0 += sums[q * kw + k][at + (!GATE && i >= 8 ? 2 : 0)][from];
+            if (GATE) v1 += sums[q * kw + k][at + 2][from];
+        }
+        finish_one(A.f, 0, r, c, v0, v1);
+    }
+}
+
+template <typename T> const void* mma_kernel_of(int64_t m, bool gate) {
+    if (m <= 8) return gate ? (const void*)mma_rows_kernel<T, 1, true> : (const void*)mma_rows_kernel<T, 1, false>;
+    return gate ? (const void*)mma_rows_kernel<T, 2, true> : (const void*)mma_rows_kernel<T, 2, false>;
+}
+
 template <typename T, int VEC, bool GATE> const void* kernel_of(int64_t m) {
     return m == 1   ? (const void*)rows_kernel<T, VEC, 1, GATE>
            : m == 2 ? (const void*)rows_kernel<T, VEC, 2, GATE>
@@ -123,15 +206,22 @@ template <typename T> const void* kernel_as(int64_t m, bool vec, bool gate) {
     return gate ? kernel_of<T, 1, true>(m) : kernel_of<T, 1, false>(m);
 }
 
-}  // namespace
-
-bool rows_takes(const Product& p) {
-    return p.m >= 1 && p.m <= 4 && p.k > 0 && (p.form == PLAIN || p.form == GATED) && !p.a[0].k_outer && !p.b[0].k_outer;
+// operands whose rows hold whole packs of 16 bytes on 16-byte boundaries
+bool packed(const Product& p) {
+    const int64_t per16 = 16 / (int64_t)elem_size(p.f.dtype);
+    return p.k % per16 == 0 && p.a[0].ld % per16 == 0 && p.b[0].ld % per16 == 0;
 }
 
-vqc_status rows_run(const Product& p, cudaStream_t s) {
+}  // namespace
+
+bool rows_takes(const Product& p, bool aligned) {
+    if (p.m < 1 || p.k <= 0 || (p.form != PLAIN && p.form != GATED) || p.a[0].k_outer || p.b[0].k_outer) return false;
+    return p.m <= 4 || (p.m <= 16 && p.f.dtype != VQC_F32 && aligned && packed(p));
+}
+
+vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s) {
     RowsArgs a{};
-    const bool gate = p.form == GATED;
+    const bool gate = p.form == GATED, vec = aligned && packed(p), mma = vec && p.m > 1 && p.f.dtype != VQC_F32;
     a.x = p.a[0].p;
     a.w0 = p.b[0].p;
     a.w1 = gate ? p.b[1].p : nullptr;
@@ -139,20 +229,20 @@ vqc_status rows_run(const Product& p, cudaStream_t s) {
     a.ld_x = p.a[0].ld;
     a.ld_w = p.b[0].ld;
     a.k = p.k;
-    const int64_t per16 = 16 / (int64_t)elem_size(p.f.dtype);
-    const bool vec = p.k % per16 == 0 && a.ld_x % per16 == 0 && a.ld_w % per16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w0, 16) && aligned_to(a.w1, 16);
-    // Warps per group: until there are 24 warps per SM, with two steps each at least
-    const int64_t groups = ceil_div(p.n, gate ? kWeights / 2 : kWeights), step = 32 * (vec ? per16 : 1);
+    // Warps per group: until there are enough per SM, with two steps (four) each at least
+    const int64_t weights = mma ? 16 : kWeights, groups = ceil_div(p.n, gate ? weights / 2 : weights);
+    const int64_t step = mma ? 32 * 4 : 32 * (vec ? 16 / (int64_t)elem_size(p.f.dtype) : 1);
     int kw = 1;
-    while (kw < kWarps && groups * kw < 24LL * sm_count() && p.k >= 4 * step * kw) kw *= 2;
+    while (kw < kWarps && groups * kw < (mma ? 16LL : 24LL) * sm_count() && p.k >= (mma ? 2 : 4) * step * kw) kw *= 2;
     a.kw = kw;
     const int64_t grid = ceil_div(groups, kWarps / kw);
     if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "too many columns");
     void* args[] = {&a};
-    const void* fn = p.f.dtype == VQC_F32    ? kernel_as<float>(p.m, vec, gate)
-                     : p.f.dtype == VQC_BF16 ? kernel_as<__nv_bfloat16>(p.m, vec, gate)
-                                             : kernel_as<__half>(p.m, vec, gate);
-    const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3(kWarps * 32), args, 0, s);
+    const void* fn = mma                        ? (p.f.dtype == VQC_BF16 ? mma_kernel_of<__nv_bfloat16>(p.m, gate) : mma_kernel_of<__half>(p.m, gate))
+                     : p.f.dtype == VQC_F32     ? kernel_as<float>(p.m, vec, gate)
+                     : p.f.dtype == VQC_BF16    ? kernel_as<__nv_bfloat16>(p.m, vec, gate)
+                                                : kernel_as<__half>(p.m, vec, gate);
+    const cudaError_t e = launch(fn, dim3((unsigned)grid), kWarps * 32, args, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "product of few rows launch");
 }
 

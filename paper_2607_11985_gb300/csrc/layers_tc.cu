@@ -473,6 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     }
     tc_fence_after();
     const uint32_t tmem = *tslot;
+    stream_order();
 
     constexpr int kPairs = kParts == 3 ? 6 : 1;      // products of parts per product
     const int unit = blockIdx.x / CG;
@@ -747,6 +748,7 @@ struct CopyJobs {
     int count;
 };
 template <int kParts> __global__ void __launch_bounds__(256) copy_kernel(const __grid_constant__ CopyJobs J) {
+    stream_order();
     const CopyJob& A = J.j[blockIdx.y];
     const int64_t across = A.ld_to / 8, plane = A.rows * A.ld_to, count = A.rows * across, step = (int64_t)gridDim.x * blockDim.x;
     for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < count; e += step) {
@@ -951,18 +953,8 @@ template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const T
         if (e != cudaSuccess) return e;
         prepared.fetch_or(1ull << (dev & 63));
     }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(a.plan.units * CG));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = S::kSmem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tc_kernel<CG, BN, kGated, kParts>, a);
+    void* args[] = {const_cast<TcArgs<kParts>*>(&a)};
+    return launch((const void*)tc_kernel<CG, BN, kGated, kParts>, dim3((unsigned)(a.plan.units * CG)), kThreads, args, s, S::kSmem, CG);
 }
 
 template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, const TcArgs<kParts>& a, cudaStream_t s) {
@@ -1090,8 +1082,7 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
         int64_t most = 1;
         for (int i = 0; i < jobs.count; ++i) most = std::max(most, jobs.j[i].rows * jobs.j[i].ld_to / 8);
         void* args[] = {&jobs};
-        const cudaError_t e = cudaLaunchKernel((const void*)copy_kernel<kParts>, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), jobs.count),
-                                               dim3(256), args, 0, s);
+        const cudaError_t e = launch((const void*)copy_kernel<kParts>, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), jobs.count), 256, args, s);
         if (e != cudaSuccess) return cuda_error(e, "operand copy launch");
     }
     const TileKind* tile = kTiles;

@@ -12,9 +12,9 @@ bool tc_takes(const Product& p);
 void tc_workspace(const Product* p, int count, bool aligned, size_t* bytes);
 vqc_status tc_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s);
 
-// Products with up to 4 rows.
-bool rows_takes(const Product& p);
-vqc_status rows_run(const Product& p, cudaStream_t s);
+// Products with few rows (no workspace); `aligned`: operands on 16-byte boundaries.
+bool rows_takes(const Product& p, bool aligned);
+vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s);
 
 }  // namespace layers
 

@@ -426,3 +426,11 @@ def test_operands_left_out_and_second_derivatives(layers, which):
             some = [t.clone().requires_grad_(k == i) if t is not None else None for k, t in enumerate(ops)]
             got, = torch.autograd.grad(f(*some), [some[i]], gy)
             assert torch.equal(got, want[i]), (given, i)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [2, 5, 8, 9, 13, 16, 17])
+@pytest.mark.parametrize("inp,out", [(8, 3), (40, 30), (1000, 129), (4096, 64)])
+def test_few_rows(layers, dtype, rows, inp, out):
+    run_linear(layers, rows, inp, out, dtype, "gelu", residual=True, seed=1000 + rows)
+    run_gated(layers, rows, inp, out, dtype, "silu", how="wide", seed=1100 + rows)
