@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
             store_pack<T, VEC>(gx + R::column(i), k[i]);
         }
     }
+    let_next();
     if (!A.part) return;
     if constexpr (WARPS == 1) {   // the CTA's 8 rows' sums in the order of the warps
         __shared__ float sums[8][NV * VEC * 32];

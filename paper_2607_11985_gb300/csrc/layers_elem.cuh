@@ -10,13 +10,13 @@
 namespace vqc {
 namespace layers {
 
-// Lets the next kernel of the stream be placed, and waits until those before have
-// ended and their writes are seen.  In every thread, before any access to memory
-// that another kernel may write.
-__device__ __forceinline__ void stream_order() {
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-}
+// Waits until the kernels before in the stream have ended and their writes are seen: in
+// every thread, before any access to memory that another kernel may write.
+__device__ __forceinline__ void stream_order() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+// Lets the next kernel of the stream be placed once every CTA has come here: before the
+// last stores, not at the start, where its waiting CTAs would take the SMs' room from
+// this kernel's later ones.
+__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }

@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(NT) product_kernel(const __grid_constant__ Pro
                 }
         }
     }
+    let_next();
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t row = m0 + ty * TM + i;
@@ -525,6 +526,7 @@ __global__ void __launch_bounds__(256, 3) act_grad_kernel(const __grid_constant_
         if (A.gated) act_grad_as<T, VEC, true>(A, r0, r1, c, s0, s1);
         else act_grad_as<T, VEC, false>(A, r0, r1, c, s0, s1);
     }
+    let_next();
     if (!part) return;
     for (int w = 0; w < (A.gated ? 2 : 1); ++w) {
         __syncthreads();

@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
             }
         }
     }
+    let_next();
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -169,6 +170,7 @@ __global__ void __launch_bounds__(kWarps * 32) mma_rows_kernel(const __grid_cons
                 }
         }
     }
+    let_next();
     // sums of weight rows g (0, 1) and g + 8 (2, 3) with rows 2 q and 2 q + 1 of x
 #pragma unroll
     for (int i = 0; i < NB; ++i)

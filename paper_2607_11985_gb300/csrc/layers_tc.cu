@@ -561,6 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 else slices(Flag<true>{}, Flag<true>{});
             }
         }
+        let_next();
         if (!ok) {
             if (issuer) give_up();
             // copies still in flight land before this CTA's memory is given back: the
