@@ -9,6 +9,11 @@
 // [n, k] stored along k or along their outer index (the backward's products
 // contract over rows: no operand is ever transposed in memory).
 //
+// The tensor cores cut the low bits of a running sum at every product of depth 16 where
+// float32 would round (measured: a bias of 1.7e-8 of the result per product, 4e-6
+// at a depth of 4096).  Where the output is float32 a tile's contraction is therefore taken out in chunks
+// of 256, which the epilogue adds up in registers (kSums: tiles up to 128 columns).
+//
 // Two products that do not depend on one another (the two of a backward) share a launch:
 // one's tiles fill the SMs that the other's last tiles leave idle.
 //
@@ -420,7 +425,15 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
     }
 }
 
-template <int CG, int BN, bool kGated, int kParts>
+// The end of the chunk that begins at block kb: 4 blocks of the product of the first
+// parts (of the only ones), all of the products of small parts together.
+template <int kPairs> __device__ __forceinline__ int chunk_end(int kb, int kb1, int kblocks) {
+    const int term = kb / kblocks, pair = term % kPairs;
+    const int end = pair == kPairs - 1 ? term * kblocks + min(kblocks, ((kb - term * kblocks) / 4 + 1) * 4) : (term - pair + kPairs - 1) * kblocks;
+    return min(end, kb1);
+}
+
+template <int CG, int BN, bool kGated, int kParts, bool kSums>
 __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__ TcArgs<kParts> P) {
     using S = Shape<CG, BN>;
     constexpr int NS = S::kStages;
@@ -585,34 +598,39 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             const uint32_t idesc = (1u << 4) | ((uint32_t)P.bf16 << 7) | ((uint32_t)P.bf16 << 10) | ((uint32_t)A.a_mn << 15) |
                                    ((uint32_t)A.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM * CG >> 4) << 24);
             const uint32_t step_a = A.a_mn ? 2048 >> 4 : 32 >> 4, step_b = A.b_mn ? 2048 >> 4 : 32 >> 4;
-            if (!__all_sync(~0u, mbar_wait(tempty + 8 * acc, aph ^ 1, gave_up))) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!__all_sync(~0u, mbar_wait(full + 8 * s, ph, gave_up))) {
+            const int nb = A.kblocks;
+            for (int from = kb0; ok && from < kb1;) {      // an accumulator's share: all, or a chunk
+                const int end = kSums ? chunk_end<kPairs>(from, kb1, nb) : kb1;
+                if (!__all_sync(~0u, mbar_wait(tempty + 8 * acc, aph ^ 1, gave_up))) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint64_t da = smem_desc(base + s * S::kStage, 8192), db = smem_desc(base + s * S::kStage + kStageA, 8192);
-                if (issuer) {
+                for (int kb = from; kb < end; ++kb) {
+                    if (!__all_sync(~0u, mbar_wait(full + 8 * s, ph, gave_up))) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t da = smem_desc(base + s * S::kStage, 8192), db = smem_desc(base + s * S::kStage + kStageA, 8192);
+                    if (issuer) {
 #pragma unroll
-                    for (int j = 0; j < BK / 16; ++j)
-                        mma<CG>(tmem + acc * BN, da + j * step_a, db + j * step_b, idesc, kb > kb0 || j > 0);
-                    mma_commit<CG>(empty + 8 * s);
-                    if (kb + 1 == kb1) mma_commit<CG>(tfull + 8 * acc);
+                        for (int j = 0; j < BK / 16; ++j)
+                            mma<CG>(tmem + acc * BN, da + j * step_a, db + j * step_b, idesc, kb > from || j > 0);
+                        mma_commit<CG>(empty + 8 * s);
+                        if (kb + 1 == end) mma_commit<CG>(tfull + 8 * acc);
+                    }
+                    issued = true;
+                    if (++s == NS) {
+                        s = 0;
+                        ph ^= 1;
+                    }
                 }
-                issued = true;
-                if (++s == NS) {
-                    s = 0;
-                    ph ^= 1;
+                from = end;
+                if (++acc == 2) {
+                    acc = 0;
+                    aph ^= 1;
                 }
-            }
-            if (++acc == 2) {
-                acc = 0;
-                aph ^= 1;
             }
         }
         if (!ok) {
@@ -643,43 +661,90 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                         }
                 }
             }
-            if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
-                if (lane == 0) give_up();
-                break;
-            }
-            tc_fence_after();
             const int64_t row0 = ((int64_t)T.m * CG + rank) * BM + quad * 32;
             const int64_t n0 = (int64_t)T.n * kCols;
+            auto release = [&]() {       // the accumulator may be written again
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    const uint32_t bar = tempty + 8 * acc;
+                    if (CG == 2)
+                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at_cta(bar, 0)) : "memory");
+                    else
+                        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
+                }
+                if (++acc == 2) {
+                    acc = 0;
+                    aph ^= 1;
+                }
+            };
             // the residual is read one step ahead
             const bool ahead = !kGated && A.f.res && A.vec && !A.part && row0 + lane < A.f.m;
             auto fetch = [&](int c, Res16& r) {
                 if (ahead && n0 + c + 16 <= A.f.n) load_res(A.f.res, A.f.out_dtype, (row0 + lane) * A.f.ld_res + n0 + c, A.vec == 32, r);
             };
-            Res16 res, next;
-            fetch(half * (kCols / 2), next);
+            if constexpr (!kSums) {
+                if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
+                    if (lane == 0) give_up();
+                    break;
+                }
+                tc_fence_after();
+                Res16 res, next;
+                fetch(half * (kCols / 2), next);
 #pragma unroll 1
-            for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 16) {
-                float v[16], u[16];
-                res = next;
-                if (c + 16 < (half + 1) * (kCols / 2)) fetch(c + 16, next);
-                __syncwarp();
-                tmem_ld(tmem + lanes + acc * BN + c, v);
-                if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
-                tmem_wait();
-                write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + kBias + c - half * (kCols / 2), stage);
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t bar = tempty + 8 * acc;
-                if (CG == 2)
-                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at_cta(bar, 0)) : "memory");
-                else
-                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
-            }
-            if (++acc == 2) {
-                acc = 0;
-                aph ^= 1;
+                for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 16) {
+                    float v[16], u[16];
+                    res = next;
+                    if (c + 16 < (half + 1) * (kCols / 2)) fetch(c + 16, next);
+                    __syncwarp();
+                    tmem_ld(tmem + lanes + acc * BN + c, v);
+                    if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
+                    tmem_wait();
+                    write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + kBias + c - half * (kCols / 2), stage);
+                }
+                release();
+            } else {
+                constexpr int kSteps = kCols / 32;       // steps of 16 columns
+                float v[kSteps][16], u[kSteps][16];
+#pragma unroll
+                for (int q = 0; q < kSteps; ++q)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[q][e] = u[q][e] = 0.f;
+                const int kblocks = A.kblocks * kPairs * (A.form == SUM ? 2 : 1), nb = A.kblocks;
+                const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
+                bool ok = true;
+                for (int from = kb0; from < kb1; from = chunk_end<kPairs>(from, kb1, nb)) {
+                    if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
+                        if (lane == 0) give_up();
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    __syncwarp();
+#pragma unroll
+                    for (int q = 0; q < kSteps; ++q) {
+                        float x[16];
+                        tmem_ld(tmem + lanes + acc * BN + half * (kCols / 2) + 16 * q, x);
+                        tmem_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[q][e] += x[e];
+                        if constexpr (kGated) {
+                            tmem_ld(tmem + lanes + acc * BN + BN / 2 + half * (kCols / 2) + 16 * q, x);
+                            tmem_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) u[q][e] += x[e];
+                        }
+                    }
+                    release();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int q = 0; q < kSteps; ++q) {
+                    const int c = half * (kCols / 2) + 16 * q;
+                    Res16 res;
+                    fetch(c, res);
+                    write16<kGated, kParts>(A, T, row0, n0 + c, lane, v[q], u[q], res, stage + kBias + 16 * q, stage);
+                }
             }
         }
     }
@@ -892,11 +957,16 @@ double schedule_of(const Product* p, int count, const TileKind& t, const int* sp
                          count == 2 ? tile_cycles(p[b], t, splits[b]) : 1.0, sms / t.cg, s);
 }
 
+// float32 outputs (and operands): sums of chunks in the epilogue's registers, tiles up to 128 columns.
+// (The two products of a backward have one type of output.)
+bool in_chunks(const Product& p) { return p.f.out_dtype == VQC_F32 || p.f.dtype == VQC_F32; }
+
 Choice choose_new(const Product* p, int count, int sms) {
     static constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     Choice best{1, 64, {1, 1}};
     double least = 1e300;
-    for (const TileKind& t : kTiles)
+    for (const TileKind& t : kTiles) {
+        if (in_chunks(p[0]) && t.bn == 256) continue;
         for (int s0 : kCuts) {
             if (s0 > depth_of(p[0])) break;
             for (int s1 : kCuts) {
@@ -912,6 +982,7 @@ Choice choose_new(const Product* p, int count, int sms) {
                 }
             }
         }
+    }
     return best;
 }
 
@@ -932,7 +1003,7 @@ Choice choose(const Product* p, int count) {
     key.v[0] = sms;
     for (int i = 0; i < count; ++i) {
         key.v[4 * i + 1] = p[i].m; key.v[4 * i + 2] = p[i].n; key.v[4 * i + 3] = p[i].k;
-        key.v[4 * i + 4] = 1 + p[i].form + 8 * (p[i].f.dtype == VQC_F32);
+        key.v[4 * i + 4] = 1 + p[i].form + 8 * (p[i].f.dtype == VQC_F32) + 16 * in_chunks(p[i]);
     }
     for (int64_t v : key.v) hash = (hash ^ (uint64_t)v) * 0x9E3779B97F4A7C15ull;
     Known& q = known[hash >> 58];
@@ -943,24 +1014,26 @@ Choice choose(const Product* p, int count) {
     return q.c;
 }
 
-template <int CG, int BN, bool kGated, int kParts> cudaError_t launch_tc(const TcArgs<kParts>& a, cudaStream_t s) {
+template <int CG, int BN, bool kGated, int kParts, bool kSums> cudaError_t launch_tc(const TcArgs<kParts>& a, cudaStream_t s) {
     using S = Shape<CG, BN>;
     static std::atomic<unsigned long long> prepared{0};    // devices whose limit is raised
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(prepared.load() >> (dev & 63) & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute((const void*)tc_kernel<CG, BN, kGated, kParts>,
+        const cudaError_t e = cudaFuncSetAttribute((const void*)tc_kernel<CG, BN, kGated, kParts, kSums>,
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         if (e != cudaSuccess) return e;
         prepared.fetch_or(1ull << (dev & 63));
     }
     void* args[] = {const_cast<TcArgs<kParts>*>(&a)};
-    return launch((const void*)tc_kernel<CG, BN, kGated, kParts>, dim3((unsigned)(a.plan.units * CG)), kThreads, args, s, S::kSmem, CG);
+    return launch((const void*)tc_kernel<CG, BN, kGated, kParts, kSums>, dim3((unsigned)(a.plan.units * CG)), kThreads, args, s, S::kSmem, CG);
 }
 
-template <bool kGated, int kParts> cudaError_t launch_choice(const Choice& c, const TcArgs<kParts>& a, cudaStream_t s) {
-    if (c.cg == 2) return c.bn == 256 ? launch_tc<2, 256, kGated, kParts>(a, s) : launch_tc<2, 128, kGated, kParts>(a, s);
-    return c.bn == 128 ? launch_tc<1, 128, kGated, kParts>(a, s) : launch_tc<1, 64, kGated, kParts>(a, s);
+template <bool kGated, int kParts, bool kSums> cudaError_t launch_choice(const Choice& c, const TcArgs<kParts>& a, cudaStream_t s) {
+    if constexpr (!kSums)
+        if (c.cg == 2 && c.bn == 256) return launch_tc<2, 256, kGated, kParts, false>(a, s);
+    if (c.cg == 2) return launch_tc<2, 128, kGated, kParts, kSums>(a, s);
+    return c.bn == 128 ? launch_tc<1, 128, kGated, kParts, kSums>(a, s) : launch_tc<1, 64, kGated, kParts, kSums>(a, s);
 }
 
 int left_operands(const Product& p) { return p.form == SUM || p.form == PAIR ? 2 : 1; }
@@ -1100,7 +1173,13 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
     a.bf16 = p[0].f.dtype != VQC_F16;
     cudaError_t e = error_word(&a.err);
     if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
-    e = gated ? launch_choice<true, kParts>(c, a, s) : launch_choice<false, kParts>(c, a, s);
+    if constexpr (kParts == 3) {
+        e = gated ? launch_choice<true, 3, true>(c, a, s) : launch_choice<false, 3, true>(c, a, s);
+    } else {
+        e = gated             ? launch_choice<true, 1, false>(c, a, s)
+            : in_chunks(p[0]) ? launch_choice<false, 1, true>(c, a, s)
+                              : launch_choice<false, 1, false>(c, a, s);
+    }
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "tensor-core product launch");
 }
 
