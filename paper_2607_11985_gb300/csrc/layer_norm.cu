@@ -64,6 +64,14 @@ struct NormArgs {
     float eps;
 };
 
+// (the type of unpack2 where T is a 16-bit type)
+template <typename T> struct Half {
+    using type = T;
+};
+template <> struct Half<float> {
+    using type = __half;
+};
+
 // VEC neighbouring elements as they lie in memory: one element, or 16 bytes
 template <typename T, int VEC> struct Pack {
     uint32_t w[VEC == 1 ? 1 : 4];
@@ -80,32 +88,35 @@ template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_pack
     }
     return r;
 }
-template <typename T, int VEC> __device__ __forceinline__ void unpack(const Pack<T, VEC>& p, float (&v)[VEC]) {
-    if constexpr (sizeof(T) == 4) {
+// the same as floats, in pairs (one element: the first of a pair)
+template <int VEC> struct Lanes {
+    static constexpr int N = VEC == 1 ? 1 : VEC / 2;
+    float2 p[N];
+};
+template <typename T, int VEC> __device__ __forceinline__ void unpack(const Pack<T, VEC>& p, Lanes<VEC>& v) {
+    if constexpr (VEC == 1) {
+        v.p[0] = make_float2(sizeof(T) == 4 ? __uint_as_float(p.w[0]) : unpack2<typename Half<T>::type>(p.w[0]).x, 0.f);
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = __uint_as_float(p.w[e]);
-    } else if constexpr (VEC == 1) {
-        v[0] = unpack2<T>(p.w[0]).x;
+        for (int e = 0; e < VEC / 2; ++e) v.p[e] = make_float2(__uint_as_float(p.w[2 * e]), __uint_as_float(p.w[2 * e + 1]));
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) {
-            const float2 f = unpack2<T>(p.w[e / 2]);
-            v[e] = f.x;
-            v[e + 1] = f.y;
-        }
+        for (int e = 0; e < VEC / 2; ++e) v.p[e] = unpack2<T>(p.w[e]);
     }
 }
-template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* p, const float (&v)[VEC]) {
-    if constexpr (VEC == 1) *p = from_f<T>(v[0]);
-    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* p, const Lanes<VEC>& v) {
+    if constexpr (VEC == 1) *p = from_f<T>(v.p[0].x);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y);
+    else
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(v.p[0].x, v.p[0].y), pack2<T>(v.p[1].x, v.p[1].y), pack2<T>(v.p[2].x, v.p[2].y),
+                                                  pack2<T>(v.p[3].x, v.p[3].y));
 }
-template <typename T, int VEC> __device__ __forceinline__ void load_param(const void* p, int c, float other, float (&v)[VEC]) {
+template <typename T, int VEC> __device__ __forceinline__ void load_param(const void* p, int c, float other, Lanes<VEC>& v) {
     if (p) {
         unpack<T, VEC>(load_pack<T, VEC>(static_cast<const T*>(p) + c), v);
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = other;
+        for (int e = 0; e < Lanes<VEC>::N; ++e) v.p[e] = make_float2(other, other);
     }
 }
 
@@ -136,7 +147,7 @@ __device__ __forceinline__ void load_row(const NormArgs& A, const void* p, int64
 // 8192 x 4096 bfloat16: see the table of the operators' cases; instructions count here as
 // much as bytes, so elements are converted once and kept as floats.
 template <typename T, int VEC, int WARPS, int NV>
-__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, 1024 / Row<VEC, WARPS>::kCta)
+__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, (VEC * NV <= 16 ? 1024 : 768) / Row<VEC, WARPS>::kCta)
 norm_forward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
     __shared__ float buf[2][WARPS];
@@ -146,34 +157,36 @@ norm_forward_kernel(const __grid_constant__ NormArgs A) {
     for (int64_t r = R::first(); r < A.rows; r += R::step()) {
         Pack<T, VEC> raw[NV];
         load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r, raw);
-        float v[NV][VEC], s = 0.f, q = 0.f;
+        Lanes<VEC> v[NV];
+        float2 s = make_float2(0.f, 0.f), q = s;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             unpack<T, VEC>(raw[i], v[i]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s += v[i][e];
+            for (int e = 0; e < Lanes<VEC>::N; ++e) s = add2(s, v[i].p[e]);
         }
-        const float mean = row_sum<WARPS>(s, buf[0]) * inv;
+        const float mean = row_sum<WARPS>(s.x + s.y, buf[0]) * inv;
+        const float2 minus = make_float2(-mean, VEC == 1 ? 0.f : -mean);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (R::column(i) < cols)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[i][e] -= mean;
-                    q = fmaf(v[i][e], v[i][e], q);
+                for (int e = 0; e < Lanes<VEC>::N; ++e) {
+                    v[i].p[e] = add2(v[i].p[e], minus);
+                    q = fma2(v[i].p[e], v[i].p[e], q);
                 }
-        const float rstd = rsqrtf(row_sum<WARPS>(q, buf[1]) * inv + A.eps);
+        const float rstd = rsqrtf(row_sum<WARPS>(q.x + q.y, buf[1]) * inv + A.eps);
         if (A.stats && R::column(0) == 0) *reinterpret_cast<float2*>(A.stats + 2 * r) = make_float2(mean, rstd);
         T* y = static_cast<T*>(A.y) + r * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = R::column(i);
             if (c >= cols) continue;
-            float w[VEC], b[VEC];
+            Lanes<VEC> w, b;
             load_param<T, VEC>(A.weight, c, 1.f, w);
             load_param<T, VEC>(A.bias, c, 0.f, b);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[e], b[e]);
+            for (int e = 0; e < Lanes<VEC>::N; ++e) v[i].p[e] = fma2(mul2(v[i].p[e], make_float2(rstd, rstd)), w.p[e], b.p[e]);
             store_pack<T, VEC>(y + c, v[i]);
         }
     }
@@ -187,18 +200,19 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
     stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
-    float gw[NV][VEC], gb[NV][VEC];
+    constexpr int N = Lanes<VEC>::N;
+    float2 gw[NV][N], gb[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) gw[i][e] = gb[i][e] = 0.f;
+        for (int e = 0; e < N; ++e) gw[i][e] = gb[i][e] = make_float2(0.f, 0.f);
     int turn = 0;
     Pack<T, VEC> nx[NV], ng[NV];
     load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
     load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
     for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
         const float2 st = *reinterpret_cast<const float2*>(A.stats_in + 2 * r);
-        float h[NV][VEC], k[NV][VEC];
+        Lanes<VEC> h[NV], k[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             unpack<T, VEC>(nx[i], h[i]);
@@ -206,31 +220,32 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
         }
         load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
         load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
-        float s = 0.f, t = 0.f;
+        const float2 minus = make_float2(-st.x, VEC == 1 ? 0.f : -st.x), scale = make_float2(st.y, st.y);
+        float2 s = make_float2(0.f, 0.f), t = s;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (R::column(i) >= cols) continue;
-            float w[VEC];
+            Lanes<VEC> w;
             load_param<T, VEC>(A.weight, R::column(i), 1.f, w);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                h[i][e] = (h[i][e] - st.x) * st.y;
-                gw[i][e] = fmaf(k[i][e], h[i][e], gw[i][e]);
-                gb[i][e] += k[i][e];
-                k[i][e] *= w[e];
-                s += k[i][e];
-                t = fmaf(k[i][e], h[i][e], t);
+            for (int e = 0; e < N; ++e) {
+                h[i].p[e] = mul2(add2(h[i].p[e], minus), scale);
+                gw[i][e] = fma2(k[i].p[e], h[i].p[e], gw[i][e]);
+                gb[i][e] = add2(gb[i][e], k[i].p[e]);
+                k[i].p[e] = mul2(k[i].p[e], w.p[e]);
+                s = add2(s, k[i].p[e]);
+                t = fma2(k[i].p[e], h[i].p[e], t);
             }
         }
         if (!A.gx) continue;
-        const float2 sum = row_sum<WARPS>(s, t, buf[turn]);
-        const float ms = sum.x * inv, mt = sum.y * inv;
+        const float2 sum = row_sum<WARPS>(s.x + s.y, t.x + t.y, buf[turn]);
+        const float2 ms = make_float2(-sum.x * inv, -sum.x * inv), mt = make_float2(-sum.y * inv, -sum.y * inv);
         T* gx = static_cast<T*>(A.gx) + r * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (R::column(i) >= cols) continue;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) k[i][e] = st.y * fmaf(-h[i][e], mt, k[i][e] - ms);
+            for (int e = 0; e < N; ++e) k[i].p[e] = mul2(scale, fma2(h[i].p[e], mt, add2(k[i].p[e], ms)));
             store_pack<T, VEC>(gx + R::column(i), k[i]);
         }
     }
@@ -244,7 +259,10 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sums[threadIdx.x >> 5][R::column(i) + e] = which ? gb[i][e] : gw[i][e];
+                for (int e = 0; e < VEC; ++e) {
+                    const float2 p = which ? gb[i][e / 2] : gw[i][e / 2];
+                    sums[threadIdx.x >> 5][R::column(i) + e] = e & 1 ? p.y : p.x;
+                }
             __syncthreads();
             for (int c = threadIdx.x; c < cols; c += 256) {
                 float a = 0.f;
@@ -261,8 +279,8 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
             if (R::column(i) < cols) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    pw[R::column(i) + e] = gw[i][e];
-                    pb[R::column(i) + e] = gb[i][e];
+                    pw[R::column(i) + e] = e & 1 ? gw[i][e / 2].y : gw[i][e / 2].x;
+                    pb[R::column(i) + e] = e & 1 ? gb[i][e / 2].y : gb[i][e / 2].x;
                 }
             }
     }
@@ -363,13 +381,23 @@ template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
 // E: elements per thread and step of the ladder
 template <typename T, int VEC> Plan forward_choice(int64_t cols) {
     constexpr int N8 = 8 / VEC, N16 = 16 / VEC, N32 = 32 / VEC;
-    if (cols <= 256) return forward_plan<T, VEC, 1, N8>();
-    if (cols <= 512) return forward_plan<T, VEC, 2, N8>();
-    if (cols <= 1024) return forward_plan<T, VEC, 4, N8>();
-    if (cols <= 2048) return forward_plan<T, VEC, 4, N16>();
-    if (cols <= 4096) return forward_plan<T, VEC, 8, N16>();
-    if (cols <= 8192) return forward_plan<T, VEC, 16, N16>();
-    return forward_plan<T, VEC, 16, N32>();
+    if constexpr (VEC == 1) {      // single elements: more threads, fewer loads each
+        if (cols <= 256) return forward_plan<T, VEC, 1, N8>();
+        if (cols <= 512) return forward_plan<T, VEC, 2, N8>();
+        if (cols <= 1024) return forward_plan<T, VEC, 4, N8>();
+        if (cols <= 2048) return forward_plan<T, VEC, 8, N8>();
+        if (cols <= 4096) return forward_plan<T, VEC, 16, N8>();
+        if (cols <= 8192) return forward_plan<T, VEC, 16, N16>();
+        return forward_plan<T, VEC, 16, N32>();
+    } else {
+        if (cols <= 256) return forward_plan<T, VEC, 1, N8>();
+        if (cols <= 512) return forward_plan<T, VEC, 1, N16>();
+        if (cols <= 1024) return forward_plan<T, VEC, 1, N32>();
+        if (cols <= 2048) return forward_plan<T, VEC, 2, N32>();
+        if (cols <= 4096) return forward_plan<T, VEC, 4, N32>();
+        if (cols <= 8192) return forward_plan<T, VEC, 8, N32>();
+        return forward_plan<T, VEC, 16, N32>();
+    }
 }
 template <typename T, int VEC> Plan backward_choice(int64_t cols) {
     constexpr int N8 = 8 / VEC, N16 = 16 / VEC;

@@ -126,13 +126,14 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
 }
 
 // A group of KW warps takes 16 rows of weights (8 of each in GATED form: then both
-// factors of an output are in one lane) and NB * 8 rows of x.  Lane 4 g + q loads 16
-// bytes, k = 8 q + [0, 8) of the step's 32, of weight rows g and g + 8 and of rows g
-// (and g + 8) of x; a contraction may take its elements in any order, so these are the
-// operands of two products of depth 16 as they are: no shared memory, no shuffles.
+// factors of an output are in one lane) and NB * 8 rows of x.  Lane 4 g + q loads 32
+// bytes, k = 16 q + [0, 16) of the step's 64, of weight rows g and g + 8 (a whole line
+// of each row by four lanes) and of rows g (and g + 8) of x; a contraction may take its
+// elements in any order, so these are the operands of four products of depth 16 as they
+// are: no shared memory, no shuffles.
 template <typename T, int NB, bool GATE>
 __global__ void __launch_bounds__(kWarps * 32) mma_rows_kernel(const __grid_constant__ RowsArgs A) {
-    constexpr int C = GATE ? 8 : 16, U = 4;      // columns of a group, steps in flight
+    constexpr int C = GATE ? 8 : 16, U = 2;      // columns of a group, steps in flight
     __shared__ float sums[kWarps][NB * 4][33];
     stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = A.kw, g = lane >> 2;
@@ -146,28 +147,33 @@ __global__ void __launch_bounds__(kWarps * 32) mma_rows_kernel(const __grid_cons
     for (int b = 0; b < NB; ++b) x[b] = static_cast<const T*>(A.x) + min(8 * b + g, m - 1) * A.ld_x;
     float acc[NB][4] = {};
     if (c0 < n) {
-        const int64_t step = 32 * kw;
-        for (int64_t k0 = 32 * (warp % kw); k0 < A.k; k0 += U * step) {
-            uint4 a[U], b[U], y[U][NB];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t k = k0 + u * step + 8 * (lane & 3);
-                const bool in = k < A.k;
-                const uint4 zero = make_uint4(0, 0, 0, 0);
-                a[u] = in ? __ldcs(reinterpret_cast<const uint4*>(w0 + k)) : zero;
-                b[u] = in ? __ldcs(reinterpret_cast<const uint4*>(w1 + k)) : zero;
-#pragma unroll
-                for (int i = 0; i < NB; ++i) y[u][i] = in ? *reinterpret_cast<const uint4*>(x[i] + k) : zero;
-            }
+        const int64_t step = 64 * kw;
+        for (int64_t k0 = 64 * (warp % kw); k0 < A.k; k0 += U * step) {
+            uint4 a[U][2], b[U][2], y[U][NB][2];
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    const uint32_t a0[4] = {a[u].x, b[u].x, a[u].y, b[u].y}, a1[4] = {a[u].z, b[u].z, a[u].w, b[u].w};
-                    const uint32_t y0[2] = {y[u][i].x, y[u][i].y}, y1[2] = {y[u][i].z, y[u][i].w};
-                    mma_16816(acc[i], a0, y0, T());
-                    mma_16816(acc[i], a1, y1, T());
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t k = k0 + u * step + 16 * (lane & 3) + 8 * h;
+                    const bool in = k < A.k;
+                    const uint4 zero = make_uint4(0, 0, 0, 0);
+                    a[u][h] = in ? *reinterpret_cast<const uint4*>(w0 + k) : zero;
+                    b[u][h] = in ? *reinterpret_cast<const uint4*>(w1 + k) : zero;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) y[u][i][h] = in ? *reinterpret_cast<const uint4*>(x[i] + k) : zero;
                 }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) {
+                        const uint4 &p = a[u][h], &q = b[u][h], &z = y[u][i][h];
+                        const uint32_t a0[4] = {p.x, q.x, p.y, q.y}, a1[4] = {p.z, q.z, p.w, q.w};
+                        const uint32_t y0[2] = {z.x, z.y}, y1[2] = {z.z, z.w};
+                        mma_16816(acc[i], a0, y0, T());
+                        mma_16816(acc[i], a1, y1, T());
+                    }
         }
     }
     let_next();
@@ -233,7 +239,7 @@ vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s) {
     a.k = p.k;
     // Warps per group: until there are enough per SM, with two steps (four) each at least
     const int64_t weights = mma ? 16 : kWeights, groups = ceil_div(p.n, gate ? weights / 2 : weights);
-    const int64_t step = mma ? 32 * 4 : 32 * (vec ? 16 / (int64_t)elem_size(p.f.dtype) : 1);
+    const int64_t step = mma ? 64 * 2 : 32 * (vec ? 16 / (int64_t)elem_size(p.f.dtype) : 1);
     int kw = 1;
     while (kw < kWarps && groups * kw < (mma ? 16LL : 24LL) * sm_count() && p.k >= (mma ? 2 : 4) * step * kw) kw *= 2;
     a.kw = kw;
