@@ -73,7 +73,7 @@ template <> struct Half<float> {
 };
 
 // VEC neighbouring elements as they lie in memory: one element, or 16 bytes
-template <typename T, int VEC> struct Pack {
+template <typename T, int VEC> struct alignas(VEC == 1 ? 4 : 16) Pack {
     uint32_t w[VEC == 1 ? 1 : 4];
 };
 template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_pack(const T* p) {
@@ -147,7 +147,7 @@ __device__ __forceinline__ void load_row(const NormArgs& A, const void* p, int64
 // 8192 x 4096 bfloat16: see the table of the operators' cases; instructions count here as
 // much as bytes, so elements are converted once and kept as floats.
 template <typename T, int VEC, int WARPS, int NV>
-__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, (VEC * NV <= 16 ? 1024 : 768) / Row<VEC, WARPS>::kCta)
+__global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, (VEC * NV <= 16 || WARPS == 16 ? 1024 : 768) / Row<VEC, WARPS>::kCta)
 norm_forward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
     __shared__ float buf[2][WARPS];
@@ -192,7 +192,13 @@ norm_forward_kernel(const __grid_constant__ NormArgs A) {
     }
 }
 
-// Loads run a row ahead, so that they are in flight during the sums of the row before.
+// Loads run 2 or 4 rows ahead (as shared memory allows), by copies into the thread's own places in shared memory (packs) or a
+// row ahead in registers (single elements), so that they are in flight during the
+// sums of the rows before: bytes in flight are what a stream of rows with a sum in
+// each needs most.
+template <int NV> constexpr int rows_ahead(int threads) { return 4 * 2 * NV * 16 * threads <= 128 * 1024 ? 4 : 2; }
+template <int VEC, int NV> constexpr size_t ahead_bytes(int threads) { return VEC > 1 ? (size_t)rows_ahead<NV>(threads) * 2 * NV * 16 * threads : 0; }
+
 template <typename T, int VEC, int WARPS, int NV>
 __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
@@ -200,26 +206,56 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
     stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
-    constexpr int N = Lanes<VEC>::N;
+    constexpr int N = Lanes<VEC>::N, kAhead = rows_ahead<NV>(R::kCta);
     float2 gw[NV][N], gb[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < N; ++e) gw[i][e] = gb[i][e] = make_float2(0.f, 0.f);
     int turn = 0;
+    extern __shared__ uint4 ring[];
+    auto place = [&](int slot, int which, int i) { return ring + ((slot * 2 + which) * NV + i) * R::kCta + threadIdx.x; };
+    auto ask = [&](int64_t r, int slot) {
+        if (r < A.rows)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (R::column(i) < cols) {
+                    copy16_async(place(slot, 0, i), static_cast<const T*>(A.x) + r * A.ld_x + R::column(i));
+                    copy16_async(place(slot, 1, i), static_cast<const T*>(A.gy) + r * A.ld_gy + R::column(i));
+                }
+        copies_commit();
+    };
     Pack<T, VEC> nx[NV], ng[NV];
-    load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
-    load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
+    if constexpr (VEC > 1) {
+        for (int d = 0; d < kAhead; ++d) ask(R::first() + d * R::step(), d);
+    } else {
+        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
+        load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
+    }
+    int slot = 0;
     for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
         const float2 st = *reinterpret_cast<const float2*>(A.stats_in + 2 * r);
         Lanes<VEC> h[NV], k[NV];
+        if constexpr (VEC > 1) {
+            copies_wait<kAhead - 1>();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                *reinterpret_cast<uint4*>(nx[i].w) = *place(slot, 0, i);
+                *reinterpret_cast<uint4*>(ng[i].w) = *place(slot, 1, i);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             unpack<T, VEC>(nx[i], h[i]);
             unpack<T, VEC>(ng[i], k[i]);
         }
-        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
-        load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
+        if constexpr (VEC > 1) {
+            ask(r + kAhead * R::step(), slot);
+            slot = slot + 1 == kAhead ? 0 : slot + 1;
+        } else {
+            load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
+            load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
+        }
         const float2 minus = make_float2(-st.x, VEC == 1 ? 0.f : -st.x), scale = make_float2(st.y, st.y);
         float2 s = make_float2(0.f, 0.f), t = s;
 #pragma unroll
@@ -371,12 +407,13 @@ int64_t row_ctas(int warps, int64_t rows, int64_t most) {
 struct Plan {
     const void* fn;
     int warps, threads;
+    size_t shared;
 };
 template <typename T, int VEC, int WARPS, int NV> Plan forward_plan() {
-    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
+    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta, 0};
 }
 template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
-    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
+    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta, ahead_bytes<VEC, NV>(Row<VEC, WARPS>::kCta)};
 }
 // E: elements per thread and step of the ladder
 template <typename T, int VEC> Plan forward_choice(int64_t cols) {
@@ -524,7 +561,7 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
             blocks = columns ? backward_ctas(cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
             void* args[] = {&a};
-            const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s);
+            const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s, p.shared);
             if (err != cudaSuccess) return launched(err);
         }
         return columns ? sum_run(a.part, blocks, cols, cols, blocks * cols, grad_weight, grad_bias, dtype, s) : VQC_OK;

@@ -6,6 +6,9 @@
 // every layout, stride and size, with sums in a fixed order.
 #include <algorithm>
 #include <atomic>
+#include <mutex>
+#include <set>
+#include <utility>
 
 #include "layers_elem.cuh"
 #include "layers_tc.h"
@@ -18,6 +21,19 @@ vqc_status cuda_error(cudaError_t e, const char* what) {
 }
 
 cudaError_t launch(const void* fn, dim3 grid, int threads, void** args, cudaStream_t s, size_t shared, int cluster) {
+    if (shared > 32 * 1024) {     // with a kernel's static shared memory, possibly above the default limit
+        static std::mutex mu;
+        static std::set<std::pair<const void*, int>> raised;
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        std::lock_guard<std::mutex> lk(mu);
+        if (!raised.count({fn, dev})) {      // one size per kernel: the launches of a kernel ask for no other
+            e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+            if (e != cudaSuccess) return e;
+            raised.insert({fn, dev});
+        }
+    }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
@@ -416,21 +432,9 @@ constexpr int kGradCols = 256;
 struct Raw8 {
     uint32_t w[8];
 };
-template <bool VEC> __device__ __forceinline__ void load8(const void* p, int dtype, int64_t row, int64_t c, int64_t n, Raw8& v) {
-    if constexpr (VEC) {
-        if (dtype == VQC_F32) {
-            const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + row + c);
-            const uint4 a = __ldcs(q), b = __ldcs(q + 1);
-            v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
-            v.w[4] = b.x; v.w[5] = b.y; v.w[6] = b.z; v.w[7] = b.w;
-        } else {
-            const uint4 a = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c));
-            v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
-        }
-    } else {
+__device__ __forceinline__ void load8(const void* p, int dtype, int64_t row, int64_t c, int64_t n, Raw8& v) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v.w[i] = c + 32 * i < n ? __float_as_uint(load_as(p, dtype, row + c + 32 * i)) : 0u;
-    }
+    for (int i = 0; i < 8; ++i) v.w[i] = c + 32 * i < n ? __float_as_uint(load_as(p, dtype, row + c + 32 * i)) : 0u;
 }
 template <bool VEC> __device__ __forceinline__ void floats8(const Raw8& r, int dtype, float (&v)[8]) {
     if (VEC && dtype != VQC_F32) {
@@ -461,44 +465,73 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, 
     }
 }
 
-// The loads of UR rows are issued before the first of them is used.
+// Packs come by copies into the thread's own places in shared memory, kGradAhead rows ahead
+// of their use; single elements by plain loads.
+constexpr int kGradAhead = 2, kGradPlaces = 6;     // 16-byte places of a row: 2 of grad_y, z and u each
 template <typename T, bool VEC, int ACT, bool GATE>
 __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
-    constexpr int UR = GATE ? 1 : 2;
-    for (int64_t r = r0; r < r1; r += 8 * UR) {
-        Raw8 rg[UR], rz[UR], ru[UR];
+    extern __shared__ uint4 ring[];
+    auto place = [&](int slot, int i) { return ring + (slot * kGradPlaces + i) * 256 + threadIdx.x; };
+    const bool wide = A.gy_dtype == VQC_F32;
+    auto ask = [&](int64_t q, int slot) {
+        if (q < r1) {
+            const char* g = static_cast<const char*>(A.gy) + (q * A.ld_gy + c) * (wide ? 4 : 2);
+            copy16_async(place(slot, 0), g);
+            if (wide) copy16_async(place(slot, 1), g + 16);
 #pragma unroll
-        for (int k = 0; k < UR; ++k) {
-            const int64_t q = r + 8 * k;
-            if (q >= r1) break;
-            load8<VEC>(A.gy, A.gy_dtype, q * A.ld_gy, c, A.n, rg[k]);
-            if (ACT != VQC_ACT_NONE || GATE) load8<VEC>(A.z[0], VQC_F32, q * A.n, c, A.n, rz[k]);
-            if (GATE) load8<VEC>(A.z[1], VQC_F32, q * A.n, c, A.n, ru[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < UR; ++k) {
-            const int64_t q = r + 8 * k;
-            if (q >= r1) break;
-            float gy[8], z[8], u[8], d[8];
-            floats8<VEC>(rg[k], A.gy_dtype, gy);
-            if (ACT != VQC_ACT_NONE || GATE) floats8<VEC>(rz[k], VQC_F32, z);
-            if (GATE) floats8<VEC>(ru[k], VQC_F32, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (GATE) {
-                    const float2 v = act_both(ACT, z[i]);
-                    // rounded products (not fused into the sums), whether or not dz is stored
-                    d[i] = __fmul_rn(__fmul_rn(gy[i], u[i]), v.y);
-                    u[i] = __fmul_rn(gy[i], v.x);
-                    s1[i] += u[i];
-                } else {
-                    d[i] = ACT == VQC_ACT_NONE ? gy[i] : __fmul_rn(gy[i], act_both(ACT, z[i]).y);
-                }
-                s0[i] += d[i];
+            for (int i = 0; i < 2; ++i) {
+                if (ACT != VQC_ACT_NONE || GATE) copy16_async(place(slot, 2 + i), A.z[0] + q * A.n + c + 4 * i);
+                if (GATE) copy16_async(place(slot, 4 + i), A.z[1] + q * A.n + c + 4 * i);
             }
-            if (A.dz[0]) store8<T, VEC>(A.dz[0], q * A.ld_dz, c, A.n, d);
-            if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], q * A.ld_dz, c, A.n, u);
         }
+        copies_commit();
+    };
+    auto take = [&](int slot, int first, Raw8& r, bool both) {
+        const uint4 a = *place(slot, first);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+        if (both) {
+            const uint4 b = *place(slot, first + 1);
+            r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+        }
+    };
+    int slot = 0;
+    if (VEC)
+        for (int d = 0; d < kGradAhead; ++d) ask(r0 + 8 * d, d);
+    for (int64_t q = r0; q < r1; q += 8) {
+        Raw8 rg, rz, ru;
+        if constexpr (VEC) {
+            copies_wait<kGradAhead - 1>();
+            take(slot, 0, rg, wide);
+            if (ACT != VQC_ACT_NONE || GATE) take(slot, 2, rz, true);
+            if (GATE) take(slot, 4, ru, true);
+        } else {
+            load8(A.gy, A.gy_dtype, q * A.ld_gy, c, A.n, rg);
+            if (ACT != VQC_ACT_NONE || GATE) load8(A.z[0], VQC_F32, q * A.n, c, A.n, rz);
+            if (GATE) load8(A.z[1], VQC_F32, q * A.n, c, A.n, ru);
+        }
+        float gy[8], z[8], u[8], d[8];
+        floats8<VEC>(rg, A.gy_dtype, gy);
+        if (ACT != VQC_ACT_NONE || GATE) floats8<VEC>(rz, VQC_F32, z);
+        if (GATE) floats8<VEC>(ru, VQC_F32, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (GATE) {
+                const float2 v = act_both(ACT, z[i]);
+                // rounded products (not fused into the sums), whether or not dz is stored
+                d[i] = __fmul_rn(__fmul_rn(gy[i], u[i]), v.y);
+                u[i] = __fmul_rn(gy[i], v.x);
+                s1[i] += u[i];
+            } else {
+                d[i] = ACT == VQC_ACT_NONE ? gy[i] : __fmul_rn(gy[i], act_both(ACT, z[i]).y);
+            }
+            s0[i] += d[i];
+        }
+        if (VEC) {       // the place is read: its values were used above
+            ask(q + 8 * kGradAhead, slot);
+            slot = slot + 1 == kGradAhead ? 0 : slot + 1;
+        }
+        if (A.dz[0]) store8<T, VEC>(A.dz[0], q * A.ld_dz, c, A.n, d);
+        if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], q * A.ld_dz, c, A.n, u);
     }
 }
 template <typename T, bool VEC, bool GATE>
@@ -600,7 +633,8 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
         const void* fn = a.dtype == VQC_F32 ? (vec ? (const void*)act_grad_kernel<float, true> : (const void*)act_grad_kernel<float, false>)
                          : a.dtype == VQC_BF16 ? (vec ? (const void*)act_grad_kernel<__nv_bfloat16, true> : (const void*)act_grad_kernel<__nv_bfloat16, false>)
                                                : (vec ? (const void*)act_grad_kernel<__half, true> : (const void*)act_grad_kernel<__half, false>);
-        const cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
+        const size_t shared = vec ? (size_t)kGradAhead * kGradPlaces * 256 * 16 : 0;      // 48 KB
+        const cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s, shared);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
     if (!sums) return VQC_OK;

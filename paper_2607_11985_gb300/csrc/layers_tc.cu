@@ -1016,15 +1016,6 @@ Choice choose(const Product* p, int count) {
 
 template <int CG, int BN, bool kGated, int kParts, bool kSums> cudaError_t launch_tc(const TcArgs<kParts>& a, cudaStream_t s) {
     using S = Shape<CG, BN>;
-    static std::atomic<unsigned long long> prepared{0};    // devices whose limit is raised
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (!(prepared.load() >> (dev & 63) & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute((const void*)tc_kernel<CG, BN, kGated, kParts, kSums>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-        if (e != cudaSuccess) return e;
-        prepared.fetch_or(1ull << (dev & 63));
-    }
     void* args[] = {const_cast<TcArgs<kParts>*>(&a)};
     return launch((const void*)tc_kernel<CG, BN, kGated, kParts, kSums>, dim3((unsigned)(a.plan.units * CG)), kThreads, args, s, S::kSmem, CG);
 }
