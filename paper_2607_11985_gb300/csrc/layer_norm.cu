@@ -196,8 +196,8 @@ norm_forward_kernel(const __grid_constant__ NormArgs A) {
 // row ahead in registers (single elements), so that they are in flight during the
 // sums of the rows before: bytes in flight are what a stream of rows with a sum in
 // each needs most.
-template <int NV> constexpr int rows_ahead(int threads) { return 4 * 2 * NV * 16 * threads <= 128 * 1024 ? 4 : 2; }
-template <int VEC, int NV> constexpr size_t ahead_bytes(int threads) { return VEC > 1 ? (size_t)rows_ahead<NV>(threads) * 2 * NV * 16 * threads : 0; }
+template <int NV> constexpr int rows_ahead() { return NV <= 2 ? 4 : 2; }
+template <int VEC, int NV> constexpr size_t ahead_bytes(int threads) { return VEC > 1 ? (size_t)rows_ahead<NV>() * 2 * NV * 16 * threads : 0; }
 
 template <typename T, int VEC, int WARPS, int NV>
 __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
     stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
-    constexpr int N = Lanes<VEC>::N, kAhead = rows_ahead<NV>(R::kCta);
+    constexpr int N = Lanes<VEC>::N, kAhead = rows_ahead<NV>();
     float2 gw[NV][N], gb[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -232,9 +232,13 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
         load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
         load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
     }
+    auto stats_of = [&](int64_t r) { return r < A.rows ? *reinterpret_cast<const float2*>(A.stats_in + 2 * r) : make_float2(0.f, 0.f); };
     int slot = 0;
+    float2 s1 = stats_of(R::first()), s2 = stats_of(R::first() + R::step());     // two rows ahead as well
     for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
-        const float2 st = *reinterpret_cast<const float2*>(A.stats_in + 2 * r);
+        const float2 st = s1;
+        s1 = s2;
+        s2 = stats_of(r + 2 * R::step());
         Lanes<VEC> h[NV], k[NV];
         if constexpr (VEC > 1) {
             copies_wait<kAhead - 1>();
@@ -313,10 +317,16 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (R::column(i) < cols) {
+                float *qw = pw + R::column(i), *qb = pb + R::column(i);
+                if constexpr (VEC == 1) {
+                    *qw = gw[i][0].x;
+                    *qb = gb[i][0].x;
+                } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    pw[R::column(i) + e] = e & 1 ? gw[i][e / 2].y : gw[i][e / 2].x;
-                    pb[R::column(i) + e] = e & 1 ? gb[i][e / 2].y : gb[i][e / 2].x;
+                    for (int e = 0; e < VEC; e += 4) {
+                        *reinterpret_cast<float4*>(qw + e) = make_float4(gw[i][e / 2].x, gw[i][e / 2].y, gw[i][e / 2 + 1].x, gw[i][e / 2 + 1].y);
+                        *reinterpret_cast<float4*>(qb + e) = make_float4(gb[i][e / 2].x, gb[i][e / 2].y, gb[i][e / 2 + 1].x, gb[i][e / 2 + 1].y);
+                    }
                 }
             }
     }
@@ -439,10 +449,17 @@ template <typename T, int VEC> Plan forward_choice(int64_t cols) {
 template <typename T, int VEC> Plan backward_choice(int64_t cols) {
     constexpr int N8 = 8 / VEC, N16 = 16 / VEC;
     if (cols <= 256) return backward_plan<T, VEC, 1, N8>();
-    if (cols <= 512) return backward_plan<T, VEC, 2, N8>();
-    if (cols <= 1024) return backward_plan<T, VEC, 4, N8>();
-    if (cols <= 2048) return backward_plan<T, VEC, 8, N8>();
-    if (cols <= 4096) return backward_plan<T, VEC, 16, N8>();
+    if constexpr (VEC == 1) {
+        if (cols <= 512) return backward_plan<T, VEC, 2, N8>();
+        if (cols <= 1024) return backward_plan<T, VEC, 4, N8>();
+        if (cols <= 2048) return backward_plan<T, VEC, 8, N8>();
+        if (cols <= 4096) return backward_plan<T, VEC, 16, N8>();
+    } else {
+        if (cols <= 512) return backward_plan<T, VEC, 1, N16>();
+        if (cols <= 1024) return backward_plan<T, VEC, 2, N16>();
+        if (cols <= 2048) return backward_plan<T, VEC, 4, N16>();
+        if (cols <= 4096) return backward_plan<T, VEC, 8, N16>();
+    }
     return backward_plan<T, VEC, 16, N16>();
 }
 template <typename T> Plan choose_plan(bool forward, int64_t cols, bool vec) {
@@ -463,10 +480,12 @@ const void* long_kernel(int dtype, int which) {
     return dtype == VQC_F32 ? long_kernel<float>(which) : dtype == VQC_BF16 ? long_kernel<__nv_bfloat16>(which) : long_kernel<__half>(which);
 }
 
-// CTAs of the backward (each with its column sums): 1024 threads per SM
-int64_t backward_ctas(int64_t cols, int64_t rows) {
-    const int warps = cols <= 256 ? 1 : cols <= 512 ? 2 : cols <= 1024 ? 4 : cols <= 2048 ? 8 : 16;
-    return row_ctas(warps, rows, (int64_t)sm_count() * (warps == 1 ? 4 : 32 / warps));
+// CTAs of the backward, each with its column sums: few, since the sums are written and read
+// again; the copies ahead keep enough bytes in flight.  4096 x 2048 bfloat16 with 2 CTAs
+// of 8 warps per SM in place of 4: see the table of the operators' cases.
+int64_t backward_ctas(int warps, int64_t cols, int64_t rows) {
+    const int per_sm = cols <= 256 ? 4 : cols <= 512 ? 2 : cols <= 1024 ? 4 : cols <= 2048 ? 3 : cols <= 4096 ? 2 : 1;
+    return row_ctas(warps, rows, (int64_t)sm_count() * per_sm);
 }
 constexpr int64_t kLongBlocks = 64;   // blocks of rows of norm_columns_long
 
@@ -517,7 +536,7 @@ vqc_status vqc_layer_norm_forward(vqc_real dtype, int64_t rows, int64_t cols, co
 
 size_t vqc_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || cols > 0x7fffffff) return (size_t)-1;
-    const int64_t blocks = cols > kMostBackward ? kLongBlocks : backward_ctas(cols, rows);
+    const int64_t blocks = cols > kMostBackward ? kLongBlocks : backward_ctas(2, cols, rows);     // a CTA with 8 rows has fewer
     return align256((size_t)2 * blocks * cols * 4);
 }
 
@@ -559,7 +578,7 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             }
         } else if (rows > 0) {
             const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
-            blocks = columns ? backward_ctas(cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
+            blocks = columns ? backward_ctas(p.warps, cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
             void* args[] = {&a};
             const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s, p.shared);
             if (err != cudaSuccess) return launched(err);
