@@ -1,7 +1,7 @@
 // layers_rows.cu -- products with few rows (single tokens, small batches): the
 // weights are all there is to read, so they stream through registers once.
 //
-// Two kernels.  Up to 4 rows of any type and layout, FP32 units: a group of KW warps takes four rows of weights (two of each in GATED form) and
+// Two kernels.  Up to 4 rows of any type and layout (up to 16 of float, four at a time), FP32 units: a group of KW warps takes four rows of weights (two of each in GATED form) and
 // up to 4 rows of x; a lane holds 16 bytes of each weight row per step, the
 // group's warps take turns along k.  Sums are packed pairs of floats (even and
 // odd k), joined over the lanes, then over the warps, in a fixed order.
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = A.kw;
     const int64_t group = (int64_t)blockIdx.x * (kWarps / kw) + warp / kw, c0 = group * C;
     const int64_t n = A.f.n;
-    const int m = (int)A.f.m;
+    const int first = (int)blockIdx.y * R, m = (int)A.f.m - first;      // rows first, ..., first + R - 1
     const T* w[kWeights];
 #pragma unroll
     for (int i = 0; i < kWeights; ++i) {
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
     }
     const T* x[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = static_cast<const T*>(A.x) + min(r, m - 1) * A.ld_x;
+    for (int r = 0; r < R; ++r) x[r] = static_cast<const T*>(A.x) + (first + min(r, m - 1)) * A.ld_x;
     float2 acc[R][kWeights];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
             v0 += sums[g * kw + q][r * kWeights + i];
             if (GATE) v1 += sums[g * kw + q][r * kWeights + C + i];
         }
-        finish_one(A.f, 0, r, c, v0, v1);
+        finish_one(A.f, 0, first + r, c, v0, v1);
     }
 }
 
@@ -224,7 +224,7 @@ bool packed(const Product& p) {
 
 bool rows_takes(const Product& p, bool aligned) {
     if (p.m < 1 || p.k <= 0 || (p.form != PLAIN && p.form != GATED) || p.a[0].k_outer || p.b[0].k_outer) return false;
-    return p.m <= 4 || (p.m <= 16 && p.f.dtype != VQC_F32 && aligned && packed(p));
+    return p.m <= 4 || (p.m <= 16 && (p.f.dtype == VQC_F32 || (aligned && packed(p))));
 }
 
 vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s) {
@@ -250,7 +250,7 @@ vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s) {
                      : p.f.dtype == VQC_F32     ? kernel_as<float>(p.m, vec, gate)
                      : p.f.dtype == VQC_BF16    ? kernel_as<__nv_bfloat16>(p.m, vec, gate)
                                                 : kernel_as<__half>(p.m, vec, gate);
-    const cudaError_t e = launch(fn, dim3((unsigned)grid), kWarps * 32, args, s);
+    const cudaError_t e = launch(fn, dim3((unsigned)grid, mma ? 1 : (unsigned)ceil_div(p.m, 4)), kWarps * 32, args, s);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "product of few rows launch");
 }
 

@@ -428,7 +428,7 @@ def test_operands_left_out_and_second_derivatives(layers, which):
             assert torch.equal(got, want[i]), (given, i)
 
 
-@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows", [2, 5, 8, 9, 13, 16, 17])
 @pytest.mark.parametrize("inp,out", [(8, 3), (40, 30), (1000, 129), (4096, 64)])
 def test_few_rows(layers, dtype, rows, inp, out):
