@@ -456,7 +456,8 @@ vqc_status vqc_linear_forward(vqc_real dtype, vqc_real out_dtype, int64_t rows, 
                               size_t workspace_bytes, void* stream);
 
 /* Gradients of vqc_linear_forward.  dz = grad_y * act'(z), rounded to dtype
- * where that is a 16-bit type (the operand of the two products below);
+ * where that is a 16-bit type (the operand of the two products below; where these
+ * are small, up to 6e9 operations, dz is held as the sum of two values of dtype);
  * grad_x = dz weight, grad_weight = dz^T x, grad_bias = sum over rows of dz (summed
  * before the rounding).  The residual's gradient is grad_y.
  *   grad_y    [rows, out] of out_dtype.
@@ -484,7 +485,7 @@ vqc_status vqc_gated_forward(vqc_real dtype, int64_t rows, int64_t in, int64_t o
                              size_t workspace_bytes, void* stream);
 
 /* Gradients of vqc_gated_forward: dg = grad_h u act'(g), du = grad_h act(g), rounded
- * to dtype as operands; grad_x = dg weight_gate + du weight_up, grad_weight_gate = dg^T x,
+ * to dtype as operands (as in vqc_linear_backward); grad_x = dg weight_gate + du weight_up, grad_weight_gate = dg^T x,
  * grad_weight_up = du^T x, grad_bias_gate and grad_bias_up the sums of dg and du over
  * the rows.  Each gradient or NULL; the two weight gradients both or neither, and
  * the two bias gradients both or neither.  workspace:
@@ -510,7 +511,7 @@ size_t vqc_gated_workspace_bytes(int32_t mode, vqc_real dtype, int64_t rows, int
  * checks its launch geometry against the plan before touching memory and, on
  * a mismatch (an engine bug, never the caller's data), records it there and
  * skips its work; such a record returns VQC_ERR_DEVICE_CHECK naming the
- * kernel kind. */
+ * kernel kind.  So does a wait of the tensor-core products that ran out. */
 vqc_status vqc_sync_check(void* stream);
 
 /* Thread-local message of the last failing call ("" if none). */

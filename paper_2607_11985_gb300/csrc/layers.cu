@@ -27,20 +27,25 @@ bool sizes_ok(int64_t rows, int64_t in, int64_t out) {
 bool on(const void* p, size_t a) { return aligned_to(p, a); }
 
 // Space of a backward call: dz (and du), then the column sums, then the products.
+// Rounding dz to 16 bits adds its own error to the gradients' (1.4 of one rounding
+// together).  Where the products are short of work, in time a launch or two, dz
+// is therefore the sum of two 16-bit matrices and the gradients have the error of their one rounding;
+// above that the second matrix would cost its products: 8192 x 2048 x 2048, both
+// gradients, 74 us for one matrix.
 struct BackSpace {
-    int64_t ld_dz;
+    int64_t ld_dz, second;
     size_t dz, sums, gx, gw, total;
     bool own_dz;
 };
 
-Product product_gx(int dtype, int64_t rows, int64_t in, int64_t out, const void* const* dz, int64_t ld_dz,
+Product product_gx(int dtype, int64_t rows, int64_t in, int64_t out, const void* const* dz, int64_t ld_dz, int64_t second,
                    const void* const* w, int64_t ld_w, bool gated, void* gx) {
     Product p{};
     p.form = gated ? SUM : PLAIN;
     p.m = rows; p.n = in; p.k = out;
     for (int i = 0; i < (gated ? 2 : 1); ++i) {
-        p.a[i] = {dz[i], ld_dz, false};
-        p.b[i] = {w[i], ld_w, true};
+        p.a[i] = {dz[i], ld_dz, false, second};
+        p.b[i] = {w[i], ld_w, true, 0};
     }
     p.f.y[0] = gx;
     p.f.m = rows; p.f.n = in;
@@ -48,14 +53,14 @@ Product product_gx(int dtype, int64_t rows, int64_t in, int64_t out, const void*
     return p;
 }
 
-Product product_gw(int dtype, int64_t rows, int64_t in, int64_t out, const void* const* dz, int64_t ld_dz,
+Product product_gw(int dtype, int64_t rows, int64_t in, int64_t out, const void* const* dz, int64_t ld_dz, int64_t second,
                    const void* x, int64_t ld_x, bool gated, void* const* gw) {
     Product p{};
     p.form = gated ? PAIR : PLAIN;
     p.m = out; p.n = in; p.k = rows;
     for (int i = 0; i < (gated ? 2 : 1); ++i) {
-        p.a[i] = {dz[i], ld_dz, true};
-        p.b[i] = {x, ld_x, true};
+        p.a[i] = {dz[i], ld_dz, true, second};
+        p.b[i] = {x, ld_x, true, 0};
         p.f.y[i] = gw[i];
     }
     p.f.m = out; p.f.n = in;
@@ -68,8 +73,8 @@ Product product_forward(int dtype, int out_dtype, int64_t rows, int64_t in, int6
     Product p{};
     p.form = gated ? GATED : PLAIN;
     p.m = rows; p.n = out; p.k = in;
-    p.a[0] = {x, ld_x, false};
-    for (int i = 0; i < (gated ? 2 : 1); ++i) p.b[i] = {w[i], ld_w, false};
+    p.a[0] = {x, ld_x, false, 0};
+    for (int i = 0; i < (gated ? 2 : 1); ++i) p.b[i] = {w[i], ld_w, false, 0};
     p.f.m = rows; p.f.n = out;
     p.f.act = act; p.f.dtype = dtype; p.f.out_dtype = out_dtype; p.f.gated = gated;
     return p;
@@ -80,12 +85,14 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     BackSpace b{};
     b.own_dz = gated || act != VQC_ACT_NONE || dtype != out_dtype;
     b.ld_dz = b.own_dz ? (out + 7) / 8 * 8 : ld_gy;
-    b.dz = b.own_dz ? align256((size_t)rows * b.ld_dz * elem_size(dtype)) : 0;
+    const bool two = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
+    b.second = two ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
+    b.dz = b.own_dz ? align256((size_t)(two ? 2 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
     b.sums = act_grad_workspace(rows, out, gated);
     const void* none[2] = {nullptr, nullptr};
     void* nothing[2] = {nullptr, nullptr};
-    const Product p[2] = {product_gx(dtype, rows, in, out, none, b.ld_dz, none, ld_w, gated, nullptr),
-                          product_gw(dtype, rows, in, out, none, b.ld_dz, nullptr, ld_x, gated, nothing)};
+    const Product p[2] = {product_gx(dtype, rows, in, out, none, b.ld_dz, b.second, none, ld_w, gated, nullptr),
+                          product_gw(dtype, rows, in, out, none, b.ld_dz, b.second, nullptr, ld_x, gated, nothing)};
     size_t bytes[2];
     products_workspace(p, 2, aligned, bytes);
     b.gx = bytes[0];
@@ -151,6 +158,7 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
         g.gy = gy; g.ld_gy = ld_gy;
         g.z[0] = saved; g.z[1] = gated ? saved + rows * out : nullptr;
         g.ld_dz = b.ld_dz;
+        g.second = b.second;
         g.sum[0] = gb[0]; g.sum[1] = gated ? gb[1] : nullptr;
         g.rows = rows; g.n = out;
         g.act = act; g.dtype = dtype; g.gy_dtype = out_dtype; g.gated = gated;
@@ -163,12 +171,12 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     size_t bytes[2];
     int count = 0;
     if (gx) {
-        p[count] = product_gx(dtype, rows, in, out, dz, b.ld_dz, w, ld_w, gated, gx);
+        p[count] = product_gx(dtype, rows, in, out, dz, b.ld_dz, b.second, w, ld_w, gated, gx);
         spaces[count] = at;
         bytes[count++] = b.gx;
     }
     if (gw[0]) {
-        p[count] = product_gw(dtype, rows, in, out, dz, b.ld_dz, x, ld_x, gated, gw);
+        p[count] = product_gw(dtype, rows, in, out, dz, b.ld_dz, b.second, x, ld_x, gated, gw);
         spaces[count] = at + b.gx;
         bytes[count++] = b.gw;
     }

@@ -465,6 +465,15 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, 
     }
 }
 
+template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
+    store8<T, VEC>(A.dz[i], row, c, A.n, v);
+    if (A.second) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] -= to_f(from_f<T>(v[e]));
+        store8<T, VEC>(A.dz[i], row + A.second, c, A.n, v);
+    }
+}
+
 // Packs come by copies into the thread's own places in shared memory, kGradAhead rows ahead
 // of their use; single elements by plain loads.
 constexpr int kGradAhead = 2, kGradPlaces = 6;     // 16-byte places of a row: 2 of grad_y, z and u each
@@ -530,8 +539,8 @@ __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int6
             ask(q + 8 * kGradAhead, slot);
             slot = slot + 1 == kGradAhead ? 0 : slot + 1;
         }
-        if (A.dz[0]) store8<T, VEC>(A.dz[0], q * A.ld_dz, c, A.n, d);
-        if (GATE && A.dz[0]) store8<T, VEC>(A.dz[1], q * A.ld_dz, c, A.n, u);
+        if (A.dz[0]) store_dz<T, VEC>(A, 0, q * A.ld_dz, c, d);
+        if (GATE && A.dz[0]) store_dz<T, VEC>(A, 1, q * A.ld_dz, c, u);
     }
 }
 template <typename T, bool VEC, bool GATE>

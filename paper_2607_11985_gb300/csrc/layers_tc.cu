@@ -61,9 +61,11 @@ template <int CG, int BN> struct Shape {
     static constexpr int kTmem = 2 * BN;             // two accumulators, a power of two >= 32
 };
 
-// One product; maps of its operands: [operand][part].
+// One product; maps of its operands: [operand][part].  kParts: 1, or 3 of float
+// operands, or 2: two of a (one 16-bit matrix and what its rounding left), one of b.
 template <int kParts> struct Problem {
-    CUtensorMap ma[2][kParts], mb[2][kParts];
+    static constexpr int kPartsB = kParts == 2 ? 1 : kParts;
+    CUtensorMap ma[2][kParts], mb[2][kPartsB];
     Finish f;
     Exact exact;                // of float operands
     float* part;                // sums of a cut contraction, or NULL
@@ -99,9 +101,10 @@ template <int kParts> struct TcArgs {
     int bf16;
 };
 
+constexpr int pairs_of(int parts) { return parts == 3 ? 6 : parts; }
 // Products of parts of float operands, small ones first: parts of a and b, 2 bits each.
-constexpr unsigned kPartsA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
-constexpr unsigned kPartsB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+constexpr unsigned kOrderA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
+constexpr unsigned kOrderB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -375,7 +378,7 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
         }
         return;
     }
-    if (kParts > 1 && in) {
+    if (kParts == 3 && in) {
         float t = 0.f;       // NaN if one of the sums is not finite
 #pragma unroll
         for (int i = 0; i < 16; ++i) t = fmaf(v[i], 0.f, kGated ? fmaf(u[i], 0.f, t) : t);
@@ -488,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     const uint32_t tmem = *tslot;
     stream_order();
 
-    constexpr int kPairs = kParts == 3 ? 6 : 1;      // products of parts per product
+    constexpr int kPairs = pairs_of(kParts);      // products of parts per product
     const int unit = blockIdx.x / CG;
     int which;
     long long t;
@@ -523,7 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 const CUtensorMap *ma, *mb, *mb1;
                 auto maps = [&]() {
                     const int sum = term >= kPairs ? 1 : 0, pair = term - sum * kPairs;
-                    const int pa = kPairs == 6 ? kPartsA >> (2 * pair) & 3 : 0, pb = kPairs == 6 ? kPartsB >> (2 * pair) & 3 : 0;
+                    const int pa = kParts == 3 ? kOrderA >> (2 * pair) & 3 : kParts == 2 ? 1 - pair : 0;
+                    const int pb = kParts == 3 ? kOrderB >> (2 * pair) & 3 : 0;
                     ma = &A.ma[T.which + sum][pa];
                     mb = &A.mb[kGated ? (int)rank : T.which + sum][pb];
                     mb1 = &A.mb[1][pb];
@@ -907,7 +911,8 @@ constexpr TileKind kTiles[] = {{2, 256, 560}, {2, 128, 400}, {1, 128, 512}, {1, 
 int64_t tiles_of(const Product& p, const TileKind& t) {
     return ceil_div(p.m, BM * t.cg) * ceil_div(p.n, p.form == GATED ? t.bn / 2 : t.bn) * (p.form == PAIR ? 2 : 1);
 }
-int64_t depth_of(const Product& p) { return ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * (p.f.dtype == VQC_F32 ? 6 : 1); }
+int parts_in(const Product& p) { return p.f.dtype == VQC_F32 ? 3 : p.a[0].second ? 2 : 1; }
+int64_t depth_of(const Product& p) { return ceil_div(p.k, BK) * (p.form == SUM ? 2 : 1) * pairs_of(parts_in(p)); }
 
 // The schedule of `first` tiles of c0 cycles and `second` of c1 <= c0, and its length.
 double make_schedule(int64_t first, double c0, int64_t second, double c1, int units, Schedule& s) {
@@ -1003,7 +1008,7 @@ Choice choose(const Product* p, int count) {
     key.v[0] = sms;
     for (int i = 0; i < count; ++i) {
         key.v[4 * i + 1] = p[i].m; key.v[4 * i + 2] = p[i].n; key.v[4 * i + 3] = p[i].k;
-        key.v[4 * i + 4] = 1 + p[i].form + 8 * (p[i].f.dtype == VQC_F32) + 16 * in_chunks(p[i]);
+        key.v[4 * i + 4] = 1 + p[i].form + 8 * parts_in(p[i]) + 64 * in_chunks(p[i]);
     }
     for (int64_t v : key.v) hash = (hash ^ (uint64_t)v) * 0x9E3779B97F4A7C15ull;
     Known& q = known[hash >> 58];
@@ -1084,17 +1089,16 @@ template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c,
             const Operand& o = (side ? r.b : r.a)[i];
             const int64_t outer = side ? p.n : p.m, rows = o.k_outer ? p.k : outer;
             const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
-            for (int q = 0; q < kParts; ++q) {
+            for (int q = 0; q < (side ? Problem<kParts>::kPartsB : kParts); ++q) {
                 Operand part = o;
-                part.p = static_cast<const uint16_t*>(o.p) + q * rows * o.ld;
+                part.p = static_cast<const uint16_t*>(o.p) + q * (kParts == 2 ? o.second : rows * o.ld);
                 if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
                     return set_error(VQC_ERR_CUDA, "product: cuTensorMapEncodeTiled failed");
             }
         }
-    for (int q = 0; q < kParts; ++q) {      // an operand of both products
-        if (na == 1) a.ma[1][q] = a.ma[0][q];
-        if (nb == 1) a.mb[1][q] = a.mb[0][q];
-    }
+    // an operand of both products
+    for (int q = 0; q < kParts && na == 1; ++q) a.ma[1][q] = a.ma[0][q];
+    for (int q = 0; q < Problem<kParts>::kPartsB && nb == 1; ++q) a.mb[1][q] = a.mb[0][q];
     a.f = p.f;
     a.form = p.form;
     a.splits = splits;
@@ -1147,7 +1151,7 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
         int64_t most = 1;
         for (int i = 0; i < jobs.count; ++i) most = std::max(most, jobs.j[i].rows * jobs.j[i].ld_to / 8);
         void* args[] = {&jobs};
-        const cudaError_t e = launch((const void*)copy_kernel<kParts>, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), jobs.count), 256, args, s);
+        const cudaError_t e = launch((const void*)copy_kernel<kParts == 3 ? 3 : 1>, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), 8LL * sm_count()), jobs.count), 256, args, s);
         if (e != cudaSuccess) return cuda_error(e, "operand copy launch");
     }
     const TileKind* tile = kTiles;
@@ -1166,6 +1170,8 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
     if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
     if constexpr (kParts == 3) {
         e = gated ? launch_choice<true, 3, true>(c, a, s) : launch_choice<false, 3, true>(c, a, s);
+    } else if constexpr (kParts == 2) {
+        e = launch_choice<false, 2, false>(c, a, s);
     } else {
         e = gated             ? launch_choice<true, 1, false>(c, a, s)
             : in_chunks(p[0]) ? launch_choice<false, 1, true>(c, a, s)
@@ -1195,7 +1201,11 @@ void tc_workspace(const Product* p, int count, bool aligned, size_t* bytes) {
 }
 
 vqc_status tc_run(const Product* p, int count, void* const* ws, const size_t* bytes, Joins& joins, cudaStream_t s) {
-    return p[0].f.dtype == VQC_F32 ? run_parts<3>(p, count, ws, bytes, joins, s) : run_parts<1>(p, count, ws, bytes, joins, s);
+    switch (parts_in(p[0])) {
+        case 3: return run_parts<3>(p, count, ws, bytes, joins, s);
+        case 2: return run_parts<2>(p, count, ws, bytes, joins, s);
+        default: return run_parts<1>(p, count, ws, bytes, joins, s);
+    }
 }
 
 }  // namespace layers

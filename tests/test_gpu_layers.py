@@ -454,3 +454,32 @@ def test_float_outputs_of_deep_contractions(layers, dtype, rows, inp, out):
     assert float((y.double() - want).norm() / want.norm()) <= limit
     if h is not None:
         assert float((h.double() - want * want).norm() / (want * want).norm()) <= 2 * limit
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_large_products_of_a_backward(layers, dtype):
+    """Above 6e9 operations dz is one 16-bit matrix."""
+    run_linear(layers, 2048, 1024, 1024, dtype, "gelu", residual=True, seed=1200)
+    run_gated(layers, 1100, 1024, 1024, dtype, "silu", seed=1210)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,inp,out", [(300, 200, 150), (77, 96, 640)])
+def test_small_products_of_a_backward_round_once(layers, dtype, rows, inp, out):
+    """Below, dz keeps twice the bits: what is left of its rounding (2^-16 or less of it)
+    and of the float sums is far below the one rounding of a gradient, so that the
+    gradients are as near as the rounded float64 ones (5 percent for what float sums move)."""
+    x, w, u = normal(1, rows, inp, dtype=dtype), *(normal(i, out, inp, scale=inp ** -0.5, dtype=dtype) for i in (2, 3))
+    gy = normal(4, rows, out, dtype=dtype)
+    X, W, V, G = (t.cuda() for t in (x, w, u, gy))
+    _, z = layers.linear_forward(X, W, None, "tanh")
+    _, zz = layers.gated_forward(X, W, V)
+    lin = layers.linear_backward(G, X, W, z, "tanh", need_bias=False)[:2]
+    gat = layers.gated_backward(G, X, W, V, zz, need_bias=False)[:3]
+    sync()
+    a = ref.linear(d64(x), d64(w), None, "tanh", None, d64(gy), dtype, dtype)
+    b = ref.gated(d64(x), d64(w), d64(u), None, None, "silu", d64(gy), dtype)
+    for got, want in list(zip(lin, (a["gx"], a["gw"]))) + list(zip(gat, (b["gx"], b["gw"], b["gup"]))):
+        exact = want[0]
+        once = float((exact.to(dtype).double() - exact).norm())
+        assert float((got.double().cpu() - exact).norm()) <= 1.05 * once
