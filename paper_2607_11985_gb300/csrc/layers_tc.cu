@@ -247,17 +247,49 @@ __device__ __forceinline__ void store_bytes(void* p, int wide, const uint32_t (&
     reinterpret_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
     reinterpret_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
 }
-__device__ __forceinline__ void store16f(float* p, int wide, const float (&v)[16]) {
+
+// A warp's 32 rows x 64 bytes (a row per lane) to or from memory by way of shared memory,
+// so that four lanes move a row's 64 bytes and an instruction touches 8 lines, not 32: the
+// L1 takes a line per cycle, and the end of a tile is bound by that.  Pieces of 16
+// bytes, piece c of row r at place c ^ (r / 2 % 4): no bank twice.  `rows`: rows that exist.
+__device__ __forceinline__ uint4* piece(uint4* stage, int row, int c) { return stage + 4 * row + (c ^ (row >> 1 & 3)); }
+__device__ __forceinline__ void rows_out(uint4* stage, const uint32_t (&w)[16], char* to, int64_t pitch, int rows, int lane) {
+    __syncwarp();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t r[8];
+    for (int c = 0; c < 4; ++c) *piece(stage, lane, c) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[8 * h + i]);
-        store_bytes(p + 8 * h, wide, r);
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        if (r < rows) *reinterpret_cast<uint4*>(to + r * pitch + 16 * (lane & 3)) = *piece(stage, r, lane & 3);
     }
 }
+__device__ __forceinline__ void rows_ask(uint4 (&w)[4], const char* from, int64_t pitch, int rows, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        if (r < rows) w[i] = *reinterpret_cast<const uint4*>(from + r * pitch + 16 * (lane & 3));
+    }
+}
+__device__ __forceinline__ void rows_in(uint4* stage, const uint4 (&w)[4], uint32_t (&v)[16], int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *piece(stage, 8 * i + (lane >> 2), lane & 3) = w[i];
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint4 q = *piece(stage, lane, c);
+        v[4 * c] = q.x; v[4 * c + 1] = q.y; v[4 * c + 2] = q.z; v[4 * c + 3] = q.w;
+    }
+}
+// 16 floats per lane to `to`, the address of the warp's first row
+__device__ __forceinline__ void floats_out(float* stage, const float* v, float* to, int64_t n, int rows, int lane) {
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
+    rows_out(reinterpret_cast<uint4*>(stage), w, reinterpret_cast<char*>(to), 4 * n, rows, lane);
+}
 __device__ __forceinline__ void store16(void* base, int dtype, int64_t at, int wide, const float (&v)[16]) {
-    if (dtype == VQC_F32) return store16f(static_cast<float*>(base) + at, wide, v);
     uint32_t r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -352,24 +384,22 @@ __device__ __forceinline__ void turned(const float (&v)[16], int64_t row0, int64
 }
 
 // Accumulator columns c0..c0+15 (and their partners of the gate) of a warp's 32
-// rows, finished and written.  Outputs whose rows lie on 16-byte boundaries go
-// straight from the lanes, 16 or 32 bytes of a row at once; others are turned.
+// rows, finished and written: outputs whose rows lie on 16-byte boundaries by rows_out
+// (floats) or straight from the lanes, others turned.
 template <bool kGated, int kParts>
 __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
-                                        float (&v)[16], float (&u)[16], const Res16& res, const float* bias, float* stage) {
+                                        float (&v)[16], float (&u)[16], const float* bias, float* stage) {
     const Finish& f = A.f;
     const int64_t n = f.n, row = row0 + lane;
-    const bool in = row < f.m, vec = A.vec && col0 + 16 <= n;
-    const int wide = A.vec == 32;
+    const int rows = (int)max((int64_t)0, min((int64_t)32, f.m - row0));
+    const bool in = lane < rows, vec = A.vec && col0 + 16 <= n;
     if (col0 >= n) return;
     if (A.part) {
         const int64_t slots = A.form == GATED || A.form == PAIR ? 2 : 1;
         float* to = A.part + (T.split * slots + T.which) * f.m * n;
         if (vec) {
-            if (in) {
-                store16f(to + row * n + col0, wide, v);
-                if (kGated) store16f(to + (f.m + row) * n + col0, wide, u);
-            }
+            floats_out(stage, v, to + row0 * n + col0, n, rows, lane);
+            if (kGated) floats_out(stage, u, to + (f.m + row0) * n + col0, n, rows, lane);
         } else {
             auto put = [&](int64_t r, int64_t c, float x) { to[r * n + c] = x; };
             turned(v, row0, col0, f.m, n, lane, stage, put);
@@ -402,13 +432,12 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
     }
     if (f.bias[T.which]) add_bias(bias, v);
     if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
-    const int64_t at = row * n + col0;
 #pragma unroll
     for (int w = 0; w < (kGated ? 2 : 1); ++w) {
         float* z = f.z[kGated ? w : T.which];
         if (!z) continue;
-        if (!vec) turned(w ? u : v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { z[r * n + c] = x; });
-        else if (in) store16f(z + at, wide, w ? u : v);
+        if (vec) floats_out(stage, w ? u : v, z + row0 * n + col0, n, rows, lane);
+        else turned(w ? u : v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { z[r * n + c] = x; });
     }
     act16(f.act, v);
     if (kGated) {
@@ -416,9 +445,13 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
         for (int i = 0; i < 16; ++i) v[i] *= u[i];
     }
     if (vec) {
-        if (!in) return;
-        if (!kGated && f.res) add_res(res, f.out_dtype, v);
-        store16(f.y[T.which], f.out_dtype, at, wide, v);
+        if (!kGated && f.res && in) {
+            Res16 res;
+            load_res(f.res, f.out_dtype, row * f.ld_res + col0, A.vec == 32, res);
+            add_res(res, f.out_dtype, v);
+        }
+        if (f.out_dtype == VQC_F32) floats_out(stage, v, static_cast<float*>(f.y[T.which]) + row0 * n + col0, n, rows, lane);
+        else if (in) store16(f.y[T.which], f.out_dtype, row * n + col0, A.vec == 32, v);
     } else if (!kGated && f.res) {
         turned(v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) {
             store_as(f.y[T.which], f.out_dtype, r * n + c, x + load_as(f.res, f.out_dtype, r * f.ld_res + c));
@@ -426,6 +459,45 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
     } else {
         turned(v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { store_as(f.y[T.which], f.out_dtype, r * n + c, x); });
     }
+}
+
+// 32 columns at once of a 16-bit output with whole rows of 64 bytes; `res`: the
+// residual's, asked for a step ahead.
+template <bool kGated, int kParts>
+__device__ __forceinline__ void write32(const Problem<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
+                                        float (&v)[2][16], float (&u)[2][16], const uint4 (&res)[4], const float* bias, float* stage) {
+    const Finish& f = A.f;
+    const int64_t n = f.n, at = row0 * n + col0;
+    const int rows = (int)max((int64_t)0, min((int64_t)32, f.m - row0));
+    uint4* pieces = reinterpret_cast<uint4*>(stage);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (f.bias[T.which]) add_bias(bias + 16 * h, v[h]);
+        if (kGated && f.bias[1]) add_bias(bias + kBiasUp + 16 * h, u[h]);
+        if (f.z[T.which]) floats_out(stage, v[h], f.z[T.which] + at + 16 * h, n, rows, lane);
+        if (kGated && f.z[1]) floats_out(stage, u[h], f.z[1] + at + 16 * h, n, rows, lane);
+        act16(f.act, v[h]);
+        if (kGated) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[h][i] *= u[h][i];
+        }
+    }
+    uint32_t w[16];
+    if (!kGated && f.res) {
+        rows_in(pieces, res, w, lane);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 p = f.out_dtype == VQC_BF16 ? unpack2<__nv_bfloat16>(w[i]) : unpack2<__half>(w[i]);
+            v[i / 8][2 * (i % 8)] += p.x;
+            v[i / 8][2 * (i % 8) + 1] += p.y;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float a = v[i / 8][2 * (i % 8)], b = v[i / 8][2 * (i % 8) + 1];
+        w[i] = f.out_dtype == VQC_BF16 ? pack2<__nv_bfloat16>(a, b) : pack2<__half>(a, b);
+    }
+    rows_out(pieces, w, static_cast<char*>(f.y[T.which]) + 2 * at, 2 * n, rows, lane);
 }
 
 // The end of the chunk that begins at block kb: 4 blocks of the product of the first
@@ -682,29 +754,42 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                     aph ^= 1;
                 }
             };
-            // the residual is read one step ahead
-            const bool ahead = !kGated && A.f.res && A.vec && !A.part && row0 + lane < A.f.m;
-            auto fetch = [&](int c, Res16& r) {
-                if (ahead && n0 + c + 16 <= A.f.n) load_res(A.f.res, A.f.out_dtype, (row0 + lane) * A.f.ld_res + n0 + c, A.vec == 32, r);
-            };
             if constexpr (!kSums) {
+                constexpr int kStep = kCols / 2 < 32 ? 16 : 32;
+                const int first = half * (kCols / 2), rows = (int)max((int64_t)0, min((int64_t)32, A.f.m - row0));
+                auto whole = [&](int c) { return kStep == 32 && A.vec && !A.part && n0 + c + 32 <= A.f.n; };
+                // the residual is asked for one step ahead
+                auto ask = [&](int c, uint4 (&r)[4]) {
+                    if (!kGated && A.f.res && c < first + kCols / 2 && whole(c))
+                        rows_ask(r, static_cast<const char*>(A.f.res) + 2 * (row0 * A.f.ld_res + n0 + c), 2 * A.f.ld_res, rows, lane);
+                };
+                uint4 res[4] = {}, next[4] = {};
+                ask(first, next);
                 if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
                     if (lane == 0) give_up();
                     break;
                 }
                 tc_fence_after();
-                Res16 res, next;
-                fetch(half * (kCols / 2), next);
 #pragma unroll 1
-                for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 16) {
-                    float v[16], u[16];
-                    res = next;
-                    if (c + 16 < (half + 1) * (kCols / 2)) fetch(c + 16, next);
+                for (int c = first; c < first + kCols / 2; c += kStep) {
+                    const float* bias = stage + kBias + c - first;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) res[i] = next[i];
+                    ask(c + kStep, next);
+                    float v[2][16], u[2][16];
                     __syncwarp();
-                    tmem_ld(tmem + lanes + acc * BN + c, v);
-                    if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c, u);
+#pragma unroll
+                    for (int h = 0; h < kStep / 16; ++h) {
+                        tmem_ld(tmem + lanes + acc * BN + c + 16 * h, v[h]);
+                        if (kGated) tmem_ld(tmem + lanes + acc * BN + BN / 2 + c + 16 * h, u[h]);
+                    }
                     tmem_wait();
-                    write16<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, stage + kBias + c - half * (kCols / 2), stage);
+                    if (whole(c)) {
+                        write32<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, bias, stage);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < kStep / 16; ++h) write16<kGated, kParts>(A, T, row0, n0 + c + 16 * h, lane, v[h], u[h], bias + 16 * h, stage);
+                    }
                 }
                 release();
             } else {
@@ -744,10 +829,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 if (!ok) break;
 #pragma unroll
                 for (int q = 0; q < kSteps; ++q) {
-                    const int c = half * (kCols / 2) + 16 * q;
-                    Res16 res;
-                    fetch(c, res);
-                    write16<kGated, kParts>(A, T, row0, n0 + c, lane, v[q], u[q], res, stage + kBias + 16 * q, stage);
+                    write16<kGated, kParts>(A, T, row0, n0 + half * (kCols / 2) + 16 * q, lane, v[q], u[q], stage + kBias + 16 * q, stage);
                 }
             }
         }
@@ -942,10 +1024,13 @@ double make_schedule(int64_t first, double c0, int64_t second, double c1, int un
     return best;
 }
 
+// Taking out an accumulator: measured about 2500 cycles for 256 columns in whole pieces of
+// 16 bytes, five times that where rows are turned element by element.
+double end_cycles(const Product& p, const TileKind& t) { return (p.n % 8 == 0 ? 10.0 : 50.0) * t.bn; }
 // Cycles of a tile: its stages (the products, 8192 per cycle and SM, or the bytes from the
 // L2, whichever takes longer), or taking out its accumulator.
 double tile_cycles(const Product& p, const TileKind& t, int64_t splits) {
-    return std::max((double)ceil_div(depth_of(p), splits) * t.stage, 3.0 * t.bn);
+    return std::max((double)ceil_div(depth_of(p), splits) * t.stage, end_cycles(p, t));
 }
 // of a cut: sums written and read once by all SMs together, and the launch of the join
 double cut_cycles(const Product& p, int64_t splits, int sms) {
@@ -978,7 +1063,7 @@ Choice choose_new(const Product* p, int count, int sms) {
                 if (s1 > (count == 2 ? depth_of(p[1]) : 1)) break;
                 const int splits[2] = {s0, s1};
                 Schedule plan;
-                double c = schedule_of(p, count, t, splits, sms, plan) + 3.0 * t.bn + cut_cycles(p[0], s0, sms);
+                double c = schedule_of(p, count, t, splits, sms, plan) + end_cycles(p[0], t) + cut_cycles(p[0], s0, sms);
                 if (count == 2) c += cut_cycles(p[1], s1, sms);
                 if (s0 > 1 || s1 > 1) c += 4000;
                 if (c < least) {
