@@ -395,7 +395,8 @@ vqc_status vqc_frames_export(const vqc_plan* plan, void* buf, size_t* inout_byte
  * adjacent).  Outputs are dense and 16-byte aligned; inputs may have any alignment.  `dtype`
  * is the type of x, the weights, the biases and their gradients; sums, row
  * statistics and saved pre-activations are float.  rows >= 0 (0 rows: outputs
- * per row are empty, sums over rows zero), columns 1..2^31-1.  Calls are
+ * per row are empty, sums over rows zero); a norm's columns 1..2^31-1, the sizes
+ * of linear and gated below 2^30.  Calls are
  * stream-ordered and use no memory but their arguments; results do not depend
  * on timing (sums have a fixed order).  A call whose workspace size is 0 may
  * be given NULL.  Buffers must not overlap. */

@@ -9,7 +9,7 @@ namespace vqc {
 namespace layers {
 namespace {
 
-constexpr int64_t kMostColumns = 0x7fffffff;
+constexpr int64_t kMost = (1 << 30) - 1;   // TMA coordinates are 32 bits, tiles and all
 
 vqc_status bad(const char* call, const char* what) {
     return set_error(VQC_ERR_INVALID_ARG, std::string(call) + ": " + what);
@@ -21,7 +21,7 @@ bool types_ok(int dtype, int out_dtype) {
 }
 bool act_ok(int a) { return a >= VQC_ACT_NONE && a <= VQC_ACT_SIGMOID; }
 bool sizes_ok(int64_t rows, int64_t in, int64_t out) {
-    return rows >= 0 && rows <= kMostColumns && in >= 1 && in <= kMostColumns && out >= 1 && out <= kMostColumns;
+    return rows >= 0 && rows <= kMost && in >= 1 && in <= kMost && out >= 1 && out <= kMost;
 }
 // operands lie on boundaries of their elements, outputs on 16 bytes
 bool on(const void* p, size_t a) { return aligned_to(p, a); }

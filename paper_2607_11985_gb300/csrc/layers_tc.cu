@@ -1267,11 +1267,11 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
 
 }  // namespace
 
-// Float products come here where six products of parts (and writing the parts)
-// take less time than float FMAs.
+// 16-bit products with anything to add up, and float products where six products of parts
+// (and writing the parts) take less time than float FMAs: 1000^3 35 us against 195 on the FP32
+// units, 512 x 512 x 512 about 19 either way.
 bool tc_takes(const Product& p) {
-    constexpr int64_t kMost = 1 << 30;
-    if (p.m <= 0 || p.k <= 0 || p.m >= kMost || p.n >= kMost || p.k >= kMost) return false;
+    if (p.m <= 0 || p.k <= 0) return false;
     if (p.f.dtype != VQC_F32) return true;
     const double flops = 2.0 * p.m * p.n * p.k * (p.form == PLAIN ? 1 : 2);
     return flops >= 5e8 && p.k >= 64 && std::min(p.m, p.n) >= 64;

@@ -483,3 +483,42 @@ def test_small_products_of_a_backward_round_once(layers, dtype, rows, inp, out):
         exact = want[0]
         once = float((exact.to(dtype).double() - exact).norm())
         assert float((got.double().cpu() - exact).norm()) <= 1.05 * once
+
+
+def test_float_parts_with_infinities_nan_and_large_values(layers):
+    """Float products that run in bf16 parts keep float arithmetic's infinities, NaN and
+    range: 3.4e38 would round to an infinite part."""
+    rows, inp, out = 600, 1024, 520
+    x, w, u = normal(1, rows, inp), normal(2, out, inp, scale=inp ** -0.5), normal(3, out, inp, scale=inp ** -0.5)
+    x[5, 3], x[6, 4], x[7, 9], x[7, 10] = math.inf, math.nan, math.inf, -math.inf
+    x[8, 11], w[:, 11] = 3.4e38, w[:, 11].clamp(-0.2, 0.2)
+    X, W, V = x.cuda(), w.cuda(), u.cuda()
+    y = layers.linear_forward(X, W, None, "none", save=False).cpu().double()
+    h = layers.gated_forward(X, W, V, None, None, "sigmoid", save=False).cpu().double()
+    sync()
+    clean = torch.ones(rows, dtype=torch.bool)
+    clean[5:9] = False
+    want = x.double() @ w.double().t()
+    ref.check(y[clean].float(), ref.linear(d64(x[clean]), d64(w), None, "none", None, None, F32, F32)["y"], F32, 8, "y")
+    for row in (5, 6, 7):
+        assert torch.equal(torch.isnan(y[row]), torch.isnan(want[row])), row
+        fine = ~torch.isnan(want[row])
+        assert torch.equal(y[row][fine], want[row][fine]), row
+    assert bool(torch.isfinite(y[8]).all()) and float((y[8] - want[8]).norm() / want[8].norm()) <= 1e-6
+    gate, up = torch.sigmoid(want), x.double() @ u.double().t()
+    assert bool(torch.isfinite(h[clean]).all()) and bool(torch.isnan(h[6]).all())
+    assert torch.equal(torch.isnan(h[5]), torch.isnan((gate * up)[5]))
+    # gradients: an infinite incoming gradient reaches its row of gx and its column's row of gw, no more
+    gy = normal(4, rows, out)
+    gy[17, 33] = math.inf
+    xc = normal(5, rows, inp)
+    gx, gw, gb = layers.linear_backward(gy.cuda(), xc.cuda(), W, None, "none")
+    sync()
+    want_x, want_w = gy.double() @ w.double(), gy.double().t() @ xc.double()
+    for got, exact in ((gx, want_x), (gw, want_w)):
+        got = got.cpu().double()
+        assert torch.equal(torch.isfinite(got), torch.isfinite(exact)) and torch.equal(torch.isnan(got), torch.isnan(exact))
+        bad = ~torch.isfinite(exact)
+        assert torch.equal(got[bad], exact[bad])
+        assert float((got[~bad] - exact[~bad]).norm() / exact[~bad].norm()) <= 1e-6
+    assert math.isinf(float(gb[33])) and bool(torch.isfinite(torch.cat([gb[:33], gb[34:]])).all())
