@@ -131,8 +131,10 @@ template <int W> struct Slice {
     }
 };
 
-// A BM x BN tile of outputs per CTA of 256 threads, 16 contracted elements at a time,
-// the next ones in flight meanwhile.  Each thread holds TM x TN sums (packed pairs along n): columns
+// y = finish(A B^T) in float FMAs: a BM x BN tile of outputs per CTA of 256 threads, 16 contracted
+// elements at a time, the next ones in flight meanwhile.  Bound by latency at the sizes
+// that come here: 512 x 16 to 1024 11 us, 512 x 512 x 512 18.7 us (14 TFLOP/s), a chain of
+// loads, a barrier and 16 steps per slice at two CTAs per SM.  Each thread holds TM x TN sums (packed pairs along n): columns
 // tx * TN/2 + [0, TN/2) of both halves of the tile.  In GATED form the first
 // half of the tile's columns belongs to b0 and the second half to b1 (the same
 // outputs), so that both factors of an output meet in one thread.
@@ -220,7 +222,8 @@ __global__ void __launch_bounds__(NT) product_kernel(const __grid_constant__ Pro
     }
 }
 
-// Sums of cut contractions joined in the order of the cuts, then finished: job
+// Sums of cut contractions joined in the order of the cuts, then finished (bound by the launch: its
+// operands lie in the L2): job
 // blockIdx.y / 2, its product blockIdx.y % 2 (PAIR).  Four neighbouring outputs per
 // thread where a row holds a multiple of four.
 template <int W> __device__ __forceinline__ void join_at(const Join& j, int which, int64_t size, int64_t stride, int64_t e) {
@@ -481,7 +484,10 @@ template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const A
     store8<T, VEC>(A.dz[i], row, c, A.n, v);
     if (A.second) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] -= to_f(from_f<T>(v[e]));
+        for (int e = 0; e < 8; ++e) {       // nothing is left of what became infinite
+            const float h = to_f(from_f<T>(v[e]));
+            v[e] = fabsf(h) <= 3.4028234e38f ? v[e] - h : 0.f;
+        }
         store8<T, VEC>(A.dz[i], row + A.second, c, A.n, v);
     }
 }
@@ -556,7 +562,8 @@ __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __
     }
 }
 
-// 32 columns per CTA: warp w adds the rows w, w + 32, ..., then the 32 sums are added.
+// The norm's column sums over its CTAs: 32 columns per CTA, warp w adds the rows w, w + 32, ...,
+// then the 32 sums are added.  304 rows of 2 x 4096: 7 us, bound by latency.
 __global__ void __launch_bounds__(1024) sum_kernel(const float* part, int64_t count, int64_t n, int64_t ld, int64_t second,
                                                    void* out0, void* out1, int dtype) {
     __shared__ float sums[32][33];

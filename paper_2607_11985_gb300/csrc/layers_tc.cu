@@ -30,6 +30,11 @@
 // In GATED form half of the tile's columns are rows of the one weight and half
 // of the other, so that both factors of an output lie in one lane.
 //
+// Measured, bfloat16: 8192 x 2048 x 2048 44 us (1550 TFLOP/s, a library product 45), gated 8192 x
+// 2048 x 5632 193 us (1950), both gradient products of the latter 407 us (1860, the
+// tensor pipe 91% active under the power cap); small products end at about 7 us (start, first
+// loads, one accumulator).
+//
 // Every wait is bounded; one that runs out sets the error word, the CTAs drain
 // their copies and products, free their tensor memory and return.
 #include <cuda.h>
@@ -887,7 +892,7 @@ __device__ __forceinline__ void bf16_parts(float x, uint16_t (&o)[3]) {
 // Copies of operands that TMA cannot read in place, up to four in one launch (job
 // blockIdx.y): [rows, cols] with rows of `ld_to` elements (a multiple of 8).  Floats
 // become three matrices of parts, 16-bit elements keep their bits.  8 elements
-// per thread.
+// per thread, bound by bytes: 10240 x 1177 bfloat16 10.6 us.
 struct CopyJob {
     const void* from;
     uint16_t* to;

@@ -522,3 +522,29 @@ def test_float_parts_with_infinities_nan_and_large_values(layers):
         assert torch.equal(got[bad], exact[bad])
         assert float((got[~bad] - exact[~bad]).norm() / exact[~bad].norm()) <= 1e-6
     assert math.isinf(float(gb[33])) and bool(torch.isfinite(torch.cat([gb[:33], gb[34:]])).all())
+
+
+def test_overflow_of_dz_stays_infinite(layers):
+    """dg beyond float16's range is infinite in both forms of dz, and so are the gradients
+    that it enters: not NaN."""
+    rows, inp, out = 20, 48, 40
+    x, wg, wu = normal(1, rows, inp, dtype=F16), normal(2, out, inp, dtype=F16), normal(3, out, inp, dtype=F16)
+    gh = normal(4, rows, out, dtype=F16)
+    X, WG, WU = x.cuda(), wg.cuda(), wu.cuda()
+    _, z = layers.gated_forward(X, WG, WU, None, None, "none")
+    j = int(z[1, 3].abs().cpu().argmax())
+    gh[3, j] = 60000.0                             # times |u| > 2: beyond 65504
+    assert float(z[1, 3, j].abs()) > 2
+    gx, gw, gup, _, _ = layers.gated_backward(gh.cuda(), X, WG, WU, z, "none", need_bias=False)
+    sync()
+    # dg and du rounded to float16, infinite where they exceed it, and the products of these: an infinity, or
+    # NaN where infinities of both signs meet
+    z64, gh64 = z.cpu().double(), gh.double()
+    dg, du = (gh64 * z64[1]).to(F16).double(), (gh64 * z64[0]).to(F16).double()
+    assert bool(torch.isinf(dg[3, j]))
+    for got, want in ((gx, dg @ wg.double() + du @ wu.double()), (gw, dg.t() @ x.double()), (gup, du.t() @ x.double())):
+        got = got.cpu().double()
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        bad = torch.isinf(want)
+        assert bool(bad.any()) and torch.equal(got[bad], want[bad])
+        assert bool(torch.isfinite(got[torch.isfinite(want)]).all())
