@@ -12,8 +12,8 @@
 // weights would go by way of shared memory; see mma_rows_kernel.
 //
 // Measured on 4096 x 4096 bfloat16 in the L2, us: 1 row 5.1 (6.6 TB/s) on the FP32
-// units; 4 rows 10.1 on them and 6.1 by mma.sync, 8 rows 6.4, 16 rows 9.0; the
-// tcgen05 kernel and its join 12.0 at 17 rows.
+// units; 4 rows 10.1 on them and 5.4 by mma.sync, 8 rows 5.7, 16 rows 7.1; the
+// tcgen05 kernel and its join 12.8 at 17 rows.
 #include <algorithm>
 
 #include "layers_elem.cuh"
@@ -34,25 +34,39 @@ struct RowsArgs {
     int kw;
 };
 
-// VEC elements as pairs of floats
-template <typename T, int VEC> struct Pairs {
-    float2 p[VEC < 2 ? 1 : VEC / 2];
+// VEC elements as they lie in memory, and as pairs of floats
+template <int VEC> struct Raw {
+    uint32_t w[VEC == 1 ? 1 : 4];
 };
-template <typename T, int VEC> __device__ __forceinline__ Pairs<T, VEC> load_pairs(const T* q, bool in) {
-    Pairs<T, VEC> r;
-    if constexpr (VEC == 1) {
-        r.p[0] = make_float2(in ? to_f(*q) : 0.f, 0.f);
+template <typename T, int VEC> __device__ __forceinline__ Raw<VEC> load_raw(const T* q, bool in) {
+    Raw<VEC> r{};
+    if (!in) return r;
+    if constexpr (VEC > 1) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    } else if constexpr (sizeof(T) == 4) {
+        r.w[0] = __float_as_uint(*q);
     } else {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (in) v = *reinterpret_cast<const uint4*>(q);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        if constexpr (sizeof(T) == 4) {
-            r.p[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
-            r.p[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+        r.w[0] = *reinterpret_cast<const uint16_t*>(q);
+    }
+    return r;
+}
+template <int VEC> struct Pairs {
+    static constexpr int N = VEC < 2 ? 1 : VEC / 2;
+    float2 p[N];
+};
+template <typename T, int VEC> __device__ __forceinline__ Pairs<VEC> pairs(const Raw<VEC>& v) {
+    Pairs<VEC> r;
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (VEC == 1) {
+            r.p[0] = make_float2(__uint_as_float(v.w[0]), 0.f);
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r.p[i] = unpack2<T>(w[i]);
+            r.p[0] = make_float2(__uint_as_float(v.w[0]), __uint_as_float(v.w[1]));
+            r.p[1] = make_float2(__uint_as_float(v.w[2]), __uint_as_float(v.w[3]));
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < Pairs<VEC>::N; ++i) r.p[i] = unpack2<T>(v.w[i]);      // one element: its pair's other is 0
     }
     return r;
 }
@@ -81,19 +95,31 @@ __global__ void __launch_bounds__(kWarps * 32) rows_kernel(const __grid_constant
 #pragma unroll
         for (int i = 0; i < kWeights; ++i) acc[r][i] = make_float2(0.f, 0.f);
     if (c0 < n) {
-#pragma unroll(VEC == 1 ? 8 : 4)
-        for (int64_t k = ((int64_t)(warp % kw) * 32 + lane) * VEC; k - lane * VEC < A.k; k += (int64_t)kw * 32 * VEC) {
-            const bool in = k < A.k;
-            Pairs<T, VEC> pw[kWeights];
+        // the weights of U steps are asked for before the first is used
+        constexpr int U = VEC == 1 ? 8 : R == 1 && sizeof(T) == 2 ? 4 : 2;
+        const int64_t step = (int64_t)kw * 32 * VEC;
+        for (int64_t k0 = (int64_t)(warp % kw) * 32 * VEC; k0 < A.k; k0 += U * step) {
+            Raw<VEC> rw[U][kWeights];
 #pragma unroll
-            for (int i = 0; i < kWeights; ++i) pw[i] = load_pairs<T, VEC>(w[i] + k, in);
+            for (int u = 0; u < U; ++u) {
+                const int64_t k = k0 + u * step + lane * VEC;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const Pairs<T, VEC> px = load_pairs<T, VEC>(x[r] + k, in);
+                for (int i = 0; i < kWeights; ++i) rw[u][i] = load_raw<T, VEC>(w[i] + k, k < A.k);
+            }
 #pragma unroll
-                for (int i = 0; i < kWeights; ++i)
+            for (int u = 0; u < U; ++u) {
+                const int64_t k = k0 + u * step + lane * VEC;
+                Pairs<VEC> pw[kWeights];
 #pragma unroll
-                    for (int e = 0; e < (VEC < 2 ? 1 : VEC / 2); ++e) acc[r][i] = fma2(pw[i].p[e], px.p[e], acc[r][i]);
+                for (int i = 0; i < kWeights; ++i) pw[i] = pairs<T, VEC>(rw[u][i]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const Pairs<VEC> px = pairs<T, VEC>(load_raw<T, VEC>(x[r] + k, k < A.k));
+#pragma unroll
+                    for (int i = 0; i < kWeights; ++i)
+#pragma unroll
+                        for (int e = 0; e < Pairs<VEC>::N; ++e) acc[r][i] = fma2(pw[i].p[e], px.p[e], acc[r][i]);
+                }
             }
         }
     }
@@ -134,6 +160,12 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
+// Steps whose loads a warp has in flight: many warps with one each of a gate's weights, fewer warps
+// with four of a plain product's.  From HBM, us: 4 x 2048 to 2 x 5632 9.7 so and 10.9 the
+// other way, 4 x 4096 to 2 x 11008 31 and 32; 4 x 4096 to 4096 7.7 and 10.0, 4 x 8192 to 8192 21.7
+// (6.2 TB/s) and 24.0.
+constexpr int steps_ahead(bool gate) { return gate ? 1 : 4; }
+
 // A group of KW warps takes 16 rows of weights (8 of each in GATED form: then both
 // factors of an output are in one lane) and NB * 8 rows of x.  Lane 4 g + q loads 32
 // bytes, k = 16 q + [0, 16) of the step's 64, of weight rows g and g + 8 (a whole line
@@ -141,8 +173,8 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
 // elements in any order, so these are the operands of four products of depth 16 as they
 // are: no shared memory, no shuffles.
 template <typename T, int NB, bool GATE>
-__global__ void __launch_bounds__(kWarps * 32) mma_rows_kernel(const __grid_constant__ RowsArgs A) {
-    constexpr int C = GATE ? 8 : 16, U = 2;      // columns of a group, steps in flight
+__global__ void __launch_bounds__(kWarps * 32, GATE ? 6 - NB : 2) mma_rows_kernel(const __grid_constant__ RowsArgs A) {
+    constexpr int C = GATE ? 8 : 16, U = steps_ahead(GATE);      // columns of a group, steps in flight
     __shared__ float sums[kWarps][NB * 4][33];
     stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = A.kw, g = lane >> 2;
@@ -246,11 +278,12 @@ vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s) {
     a.ld_x = p.a[0].ld;
     a.ld_w = p.b[0].ld;
     a.k = p.k;
-    // Warps per group: until there are enough per SM, with two steps (four) each at least
+    // Warps per group: until there are enough per SM, with a few steps each at least
     const int64_t weights = mma ? 16 : kWeights, groups = ceil_div(p.n, gate ? weights / 2 : weights);
-    const int64_t step = mma ? 64 * 2 : 32 * (vec ? 16 / (int64_t)elem_size(p.f.dtype) : 1);
+    const int64_t step = mma ? 64 * steps_ahead(gate) : 32 * (vec ? 16 / (int64_t)elem_size(p.f.dtype) : 1);
     int kw = 1;
-    while (kw < kWarps && groups * kw < (mma ? 16LL : 24LL) * sm_count() && p.k >= (mma ? 2 : 4) * step * kw) kw *= 2;
+    const int64_t enough = (mma ? (gate ? 32LL : 8LL) : 24LL) * sm_count(), rounds = mma ? (gate ? 2 : 1) : 4;
+    while (kw < kWarps && groups * kw < enough && p.k >= rounds * step * kw) kw *= 2;
     a.kw = kw;
     const int64_t grid = ceil_div(groups, kWarps / kw);
     if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "too many columns");

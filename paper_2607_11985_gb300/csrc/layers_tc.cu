@@ -1189,6 +1189,7 @@ template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c,
     // an operand of both products
     for (int q = 0; q < kParts && na == 1; ++q) a.ma[1][q] = a.ma[0][q];
     for (int q = 0; q < Problem<kParts>::kPartsB && nb == 1; ++q) a.mb[1][q] = a.mb[0][q];
+    if (splits < 1 || splits > depth_of(p)) return set_error(VQC_ERR_DEVICE_CHECK, "product: more cuts than blocks");   // a tile with nothing to add
     a.f = p.f;
     a.form = p.form;
     a.splits = splits;
