@@ -29,9 +29,10 @@ bool on(const void* p, size_t a) { return aligned_to(p, a); }
 // Space of a backward call: dz (and du), then the column sums, then the products.
 // Rounding dz to 16 bits adds its own error to the gradients' (1.4 of one rounding
 // together).  Where the products are short of work, in time a launch or two, dz
-// is therefore the sum of two 16-bit matrices and the gradients have the error of their one rounding;
-// above that the second matrix would cost its products: 8192 x 2048 x 2048, both
-// gradients, 74 us for one matrix.
+// is therefore the sum of three 16-bit matrices, which hold all bits of a float, and the gradients
+// have the error of their one rounding (two bfloat16 matrices hold 16 to 18 bits: one gradient in
+// 4000 rounded the other way); above that the further matrices would cost their products: 8192 x
+// 2048 x 2048, both gradients, 74 us for one matrix.
 struct BackSpace {
     int64_t ld_dz, second;
     size_t dz, sums, gx, gw, total;
@@ -85,9 +86,9 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     BackSpace b{};
     b.own_dz = gated || act != VQC_ACT_NONE || dtype != out_dtype;
     b.ld_dz = b.own_dz ? (out + 7) / 8 * 8 : ld_gy;
-    const bool two = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
-    b.second = two ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
-    b.dz = b.own_dz ? align256((size_t)(two ? 2 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
+    const bool three = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
+    b.second = three ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
+    b.dz = b.own_dz ? align256((size_t)(three ? 3 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
     b.sums = act_grad_workspace(rows, out, gated);
     const void* none[2] = {nullptr, nullptr};
     void* nothing[2] = {nullptr, nullptr};

@@ -33,8 +33,8 @@ int sm_count();   // of the current device (the GB300's 152 where there is none)
 
 // A matrix operand of a product: element (i, k) of the outer index i and the
 // contracted index k is p[i * ld + k], or p[k * ld + i] where k_outer is set.
-// A 16-bit operand may be the sum of two matrices, the second `second` elements behind
-// the first (0: there is none).
+// A 16-bit operand may be the sum of three matrices, each `second` elements behind the
+// one before (0: there is one).
 struct Operand {
     const void* p;
     int64_t ld;
@@ -107,7 +107,7 @@ struct ActGrad {
     const float* z[2];       // dense [rows, n]; z[0] may be NULL without an activation
     void* dz[2];             // of dtype, rows ld_dz apart, or NULL
     int64_t ld_dz;
-    int64_t second;          // what the rounding to dtype leaves goes this many elements behind dz (0: nowhere)
+    int64_t second;          // what the rounding to dtype leaves goes this many elements behind dz, what is left then as far again (0: nowhere)
     void* sum[2];            // [n] of dtype: column sums, or NULL
     int64_t rows, n;
     int32_t act, dtype, gy_dtype, gated;

@@ -482,13 +482,15 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, 
 
 template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
     store8<T, VEC>(A.dz[i], row, c, A.n, v);
-    if (A.second) {
+    if (!A.second) return;
+#pragma unroll
+    for (int part = 1; part < 3; ++part) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {       // nothing is left of what became infinite
             const float h = to_f(from_f<T>(v[e]));
             v[e] = fabsf(h) <= 3.4028234e38f ? v[e] - h : 0.f;
         }
-        store8<T, VEC>(A.dz[i], row + A.second, c, A.n, v);
+        store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, v);
     }
 }
 
