@@ -33,9 +33,10 @@ bool on(const void* p, size_t a) { return aligned_to(p, a); }
 // have the error of their one rounding (two bfloat16 matrices hold 16 to 18 bits: one gradient in
 // 4000 rounded the other way); above that the further matrices would cost their products: 8192 x
 // 2048 x 2048, both gradients, 74 us for one matrix.
+// A float16 dz is stored times a power of two, so that its range does not matter (see act_grad_run).
 struct BackSpace {
     int64_t ld_dz, second;
-    size_t dz, sums, gx, gw, total;
+    size_t dz, scale, sums, gx, gw, total;
     bool own_dz;
 };
 
@@ -89,7 +90,8 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     const bool three = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
     b.second = three ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
     b.dz = b.own_dz ? align256((size_t)(three ? 3 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
-    b.sums = act_grad_workspace(rows, out, gated);
+    b.scale = b.own_dz && dtype == VQC_F16 ? 256 : 0;
+    b.sums = act_grad_workspace(rows, out, gated, b.scale > 0);
     const void* none[2] = {nullptr, nullptr};
     void* nothing[2] = {nullptr, nullptr};
     const Product p[2] = {product_gx(dtype, rows, in, out, none, b.ld_dz, b.second, none, ld_w, gated, nullptr),
@@ -98,7 +100,7 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     products_workspace(p, 2, aligned, bytes);
     b.gx = bytes[0];
     b.gw = bytes[1];
-    b.total = b.dz * (gated ? 2 : 1) + b.sums + b.gx + b.gw;
+    b.total = b.dz * (gated ? 2 : 1) + b.scale + b.sums + b.gx + b.gw;
     return b;
 }
 
@@ -155,6 +157,8 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
         for (int i = 0; i < (gated ? 2 : 1); ++i) { g.dz[i] = at + i * b.dz; dz[i] = g.dz[i]; }
     }
     at += b.dz * (gated ? 2 : 1);
+    if (need_dz && b.scale && rows > 0) g.scale = reinterpret_cast<float*>(at);
+    at += b.scale;
     if (need_dz || gb[0]) {
         g.gy = gy; g.ld_gy = ld_gy;
         g.z[0] = saved; g.z[1] = gated ? saved + rows * out : nullptr;
@@ -173,11 +177,13 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     int count = 0;
     if (gx) {
         p[count] = product_gx(dtype, rows, in, out, dz, b.ld_dz, b.second, w, ld_w, gated, gx);
+        p[count].f.scale = g.scale ? g.scale + 1 : nullptr;
         spaces[count] = at;
         bytes[count++] = b.gx;
     }
     if (gw[0]) {
         p[count] = product_gw(dtype, rows, in, out, dz, b.ld_dz, b.second, x, ld_x, gated, gw);
+        p[count].f.scale = g.scale ? g.scale + 1 : nullptr;
         spaces[count] = at + b.gx;
         bytes[count++] = b.gw;
     }

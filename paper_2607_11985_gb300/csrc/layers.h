@@ -51,6 +51,7 @@ enum Form {
 
 // What is done with the sums of a product before they are written.
 struct Finish {
+    const float* scale;    // what they are multiplied by first, or NULL
     const void* bias[2];   // per column, of the operands' type, or NULL
     const void* res;       // added last, of y's type, or NULL
     int64_t ld_res;
@@ -109,10 +110,11 @@ struct ActGrad {
     int64_t ld_dz;
     int64_t second;          // what the rounding to dtype leaves goes this many elements behind dz, what is left then as far again (0: nowhere)
     void* sum[2];            // [n] of dtype: column sums, or NULL
+    float* scale;            // [2] of float16: dz is stored times scale[0], a power of two, and scale[1] = 1 / scale[0]; or NULL
     int64_t rows, n;
     int32_t act, dtype, gy_dtype, gated;
 };
-size_t act_grad_workspace(int64_t rows, int64_t n, bool gated);
+size_t act_grad_workspace(int64_t rows, int64_t n, bool gated, bool scaled);
 // Column sums of few blocks of rows are left to `joins`.
 vqc_status act_grad_run(const ActGrad& a, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s);
 

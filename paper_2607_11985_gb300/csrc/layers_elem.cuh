@@ -167,8 +167,10 @@ __device__ __forceinline__ float exact_if_not_finite(const Exact& x, int which, 
 template <int W>
 __device__ __forceinline__ void finish_some(const Finish& f, int which, int64_t row, int64_t col, float (&v)[W], float (&u)[W]) {
     const int64_t at = row * f.n + col;
+    const float scale = f.scale ? *f.scale : 1.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
+        v[i] *= scale;
         if (f.bias[which]) v[i] += load_as(f.bias[which], f.dtype, col + i);
         if (f.gated && f.bias[1]) u[i] += load_as(f.bias[1], f.dtype, col + i);
     }

@@ -8,6 +8,7 @@
 #include <atomic>
 #include <mutex>
 #include <set>
+#include <type_traits>
 #include <utility>
 
 #include "layers_elem.cuh"
@@ -494,8 +495,18 @@ template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const A
     }
 }
 
+// the largest of |v| that is finite, and `top`
+__device__ __forceinline__ float top_of(float top, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (fabsf(v[i]) <= 3.4028234e38f) top = fmaxf(top, fabsf(v[i]));
+    return top;
+}
+
 template <typename T, bool VEC, int ACT, bool GATE>
-__device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
+__device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
+    constexpr bool kScaled = std::is_same<T, __half>::value;
+    const float scale = kScaled && A.scale && A.dz[0] ? A.scale[0] : 1.f;
     for (int64_t q = r0; q < r1; q += 8) {
         Raw8 rg, rz, ru;
         load8<VEC>(A.gy, A.gy_dtype, q * A.ld_gy, c, A.n, rg);
@@ -518,37 +529,59 @@ __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int6
             }
             s0[i] += d[i];
         }
+        if constexpr (kScaled) {
+            if (A.dz[0]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    d[i] *= scale;
+                    if (GATE) u[i] *= scale;
+                }
+            } else if (A.scale) {
+                top = top_of(top, d);
+                if (GATE) top = top_of(top, u);
+            }
+        }
         if (A.dz[0]) store_dz<T, VEC>(A, 0, q * A.ld_dz, c, d);
         if (GATE && A.dz[0]) store_dz<T, VEC>(A, 1, q * A.ld_dz, c, u);
     }
 }
 template <typename T, bool VEC, bool GATE>
-__device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8]) {
+__device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
     switch (A.act) {
-        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE>(A, r0, r1, c, s0, s1);
-        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE>(A, r0, r1, c, s0, s1);
-        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE>(A, r0, r1, c, s0, s1);
-        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE>(A, r0, r1, c, s0, s1);
-        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE>(A, r0, r1, c, s0, s1);
-        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE>(A, r0, r1, c, s0, s1);
+        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE>(A, r0, r1, c, s0, s1, top);
+        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE>(A, r0, r1, c, s0, s1, top);
     }
 }
 
 // CTAs per SM: by the registers
 constexpr int grad_ctas(bool gate) { return gate ? 3 : 4; }
 template <typename T, bool VEC, bool GATE>
-__global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, int64_t per) {
+__global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, float* tops, int64_t per) {
     __shared__ float sums[8][kGradCols];
     stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t across = (A.n + kGradCols - 1) / kGradCols, block = blockIdx.x / across;
     const int64_t c0 = blockIdx.x % across * kGradCols, c = c0 + (VEC ? 8 * lane : lane);
-    float s0[8] = {}, s1[8] = {};
+    float s0[8] = {}, s1[8] = {}, top = 0.f;
     if (c < A.n) {
         const int64_t r0 = block * per + warp, r1 = min(A.rows, (block + 1) * per);
-        act_grad_as<T, VEC, GATE>(A, r0, r1, c, s0, s1);
+        act_grad_as<T, VEC, GATE>(A, r0, r1, c, s0, s1, top);
     }
     let_next();
+    if (tops) {       // the CTA's largest magnitude
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+        if (lane == 0) sums[0][warp] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, sums[0][i]);
+            tops[blockIdx.x] = top;
+        }
+    }
     if (!part) return;
     for (int w = 0; w < (GATE ? 2 : 1); ++w) {
         __syncthreads();
@@ -561,6 +594,26 @@ __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __
             for (int i = 0; i < 8; ++i) v += sums[i][threadIdx.x];
             part[(block * (GATE ? 2 : 1) + w) * A.n + c0 + threadIdx.x] = v;
         }
+    }
+}
+
+// The power of two that brings the largest of `count` magnitudes to [2^14, 2^15), and its inverse;
+// at least 1 where `up`.
+__global__ void __launch_bounds__(1024) scale_kernel(const float* tops, int64_t count, int up, float* scale) {
+    __shared__ float warps[32];
+    stream_order();
+    float top = 0.f;
+    for (int64_t i = threadIdx.x; i < count; i += 1024) top = fmaxf(top, tops[i]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, warps[i]);
+        int e = top > 0.f ? min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126) : 0;      // -113 at least
+        if (up) e = max(e, 0);
+        scale[0] = __uint_as_float((uint32_t)(127 + e) << 23);
+        scale[1] = __uint_as_float((uint32_t)(127 - e) << 23);
     }
 }
 
@@ -608,25 +661,54 @@ vqc_status sum_run(const float* part, int64_t count, int64_t n, int64_t ld, int6
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "sum launch");
 }
 
-size_t act_grad_workspace(int64_t rows, int64_t n, bool gated) {
+namespace {
+size_t grad_sums_bytes(int64_t rows, int64_t n, bool gated) {
     return align256((size_t)std::max<int64_t>(1, ceil_div(rows, grad_rows(rows, n, gated))) * n * (gated ? 2 : 1) * 4);
+}
+int64_t grad_grid(int64_t rows, int64_t n, bool gated) { return ceil_div(rows, grad_rows(rows, n, gated)) * ceil_div(n, kGradCols); }
+}  // namespace
+
+size_t act_grad_workspace(int64_t rows, int64_t n, bool gated, bool scaled) {
+    return grad_sums_bytes(rows, n, gated) + (scaled ? align256((size_t)grad_grid(rows, n, gated) * 4) : 0);
 }
 
 vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joins, cudaStream_t s) {
     ActGrad a = a0;
     const bool sums = a.sum[0] != nullptr;
     float* part = sums ? static_cast<float*>(ws) : nullptr;
-    if (sums && (!ws || ws_bytes < act_grad_workspace(a.rows, a.n, a.gated)))
+    if ((sums || a.scale) && (!ws || ws_bytes < act_grad_workspace(a.rows, a.n, a.gated, a.scale)))
         return set_error(VQC_ERR_WORKSPACE, "column sums: workspace too small");
     int64_t per = grad_rows(a.rows, a.n, a.gated);
-    const int64_t blocks = ceil_div(a.rows, per), grid = blocks * ceil_div(a.n, kGradCols);
+    const int64_t blocks = ceil_div(a.rows, per);
+    int64_t grid = grad_grid(a.rows, a.n, a.gated);
     if (grid > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, "too many rows times columns");
     if (grid > 0) {
         // whole packs of 8 elements on 16-byte boundaries (z is dense, dz the library's own)
         const bool vec = a.n % 8 == 0 && a.ld_gy % 8 == 0 && aligned_to(a.gy, 16) && aligned_to(a.z[0], 16) && aligned_to(a.z[1], 16);
-        void* args[] = {&a, &part, &per};
+        float* tops = nullptr;
+        void* args[] = {&a, &part, &tops, &per};
         const void* fn = vec ? (a.gated ? grad_kernel<true, true>(a.dtype) : grad_kernel<true, false>(a.dtype))
                              : (a.gated ? grad_kernel<false, true>(a.dtype) : grad_kernel<false, false>(a.dtype));
+        if (a.scale) {
+            // float16 holds 2^-24 to 65504 only, and dz is an operand, not a result: what is small in
+            // it counts in sums over many rows, and what is large (from a float32 grad_y) may meet small weights.
+            // A first pass finds its largest magnitude (and the column sums), a second writes it times a
+            // power of two, which the products' ends undo exactly: 2^-38 of the largest is kept.
+            // A float16 grad_y is scaled up only: there a dz beyond 65504 stays infinite, the overflow that
+            // training in float16 looks for.
+            tops = reinterpret_cast<float*>(static_cast<char*>(ws) + grad_sums_bytes(a.rows, a.n, a.gated));
+            a.dz[0] = a.dz[1] = nullptr;
+            cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
+            if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
+            int up = a.gy_dtype == VQC_F16;
+            void* of[] = {&tops, &grid, &up, &a.scale};
+            e = launch((const void*)scale_kernel, dim3(1), 1024, of, s);
+            if (e != cudaSuccess) return cuda_error(e, "scale launch");
+            a.dz[0] = a0.dz[0];
+            a.dz[1] = a0.dz[1];
+            part = nullptr;
+            tops = nullptr;
+        }
         const cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
@@ -637,7 +719,7 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
     j.f.dtype = j.f.out_dtype = a.dtype;
     j.f.y[0] = a.sum[0];
     j.f.y[1] = a.gated ? a.sum[1] : nullptr;
-    j.part = part;
+    j.part = static_cast<float*>(ws);
     j.splits = (int)blocks;
     j.form = a.gated ? PAIR : PLAIN;
     return VQC_OK;

@@ -338,6 +338,10 @@ __device__ __forceinline__ void add_bias(const float* b, float (&v)[16]) {
     }
 }
 
+__device__ __forceinline__ void scale16(float scale, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= scale;
+}
 template <int ACT> __device__ __forceinline__ void act16_as(float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = act_value(ACT, v[i]);
@@ -435,6 +439,7 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
             }
         }
     }
+    if (!kGated && f.scale) scale16(*f.scale, v);
     if (f.bias[T.which]) add_bias(bias, v);
     if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
 #pragma unroll
@@ -477,6 +482,7 @@ __device__ __forceinline__ void write32(const Problem<kParts>& A, const TileAt& 
     uint4* pieces = reinterpret_cast<uint4*>(stage);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+        if (!kGated && f.scale) scale16(*f.scale, v[h]);
         if (f.bias[T.which]) add_bias(bias + 16 * h, v[h]);
         if (kGated && f.bias[1]) add_bias(bias + kBiasUp + 16 * h, u[h]);
         if (f.z[T.which]) floats_out(stage, v[h], f.z[T.which] + at + 16 * h, n, rows, lane);

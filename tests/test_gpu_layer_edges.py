@@ -70,3 +70,44 @@ def test_gradients_of_float_outputs_round_once(layers, dtype, rows, inp, out):
     sync()
     once(gx, gy.double(), w.double(), dtype, "gx")
     once(gw, gy.double().t(), x.double(), dtype, "gw")
+
+
+@pytest.mark.parametrize("scale", [1e-7, 1e5])
+@pytest.mark.parametrize("rows,inp,out", [(4096, 64, 12), (2048, 1024, 1024)])
+def test_float16_gradients_of_small_and_large_dz(layers, scale, rows, inp, out):
+    """dz outside of float16's range, its gradients inside: the sums of many small terms,
+    the products of large ones with small weights.  Above 6e9 operations dz is rounded to
+    11 bits, 2^-11 of each term; what is below 2^-38 of the largest may be lost."""
+    toward = 1.0 if scale < 1 else 1e-5
+    x, w = normal(1, rows, inp, scale=toward, dtype=F16), normal(2, out, inp, scale=toward, dtype=F16)
+    gy = normal(3, rows, out, scale=scale)
+    gx, gw, _ = layers.linear_backward(gy.cuda(), x.cuda(), w.cuda(), None, "none")
+    sync()
+    rounding = 2.0 ** -11 if 4.0 * rows * inp * out > 6e9 else 0.0
+    for got, a, b in ((gx, gy.double(), w.double()), (gw, gy.double().t(), x.double())):
+        lost = 2.0 ** -38 * gy.abs().max().double() * b.abs().sum(0, keepdim=True)
+        once(got, a, b, F16, "scale %g" % scale, lost + rounding * (a.abs() @ b.abs()))
+
+
+def test_float16_gate_of_small_gradients(layers):
+    """dg = grad_h u act'(g) and du = grad_h act(g) of a grad_h near float16's smallest
+    numbers: bits of dg and du below those numbers count in sums over many rows.
+    Bound: the forward's g and u are known to 2^-20 of their terms (depth 32), silu and
+    its slope to 2^-20; three roundings of dg, float sums, one rounding."""
+    rows, inp, out = 4096, 32, 16
+    x, wg, wu = normal(1, rows, inp, dtype=F16), normal(2, out, inp, scale=0.1, dtype=F16), normal(3, out, inp, scale=0.1, dtype=F16)
+    gh = normal(4, rows, out, scale=1e-6).to(F16)
+    X, WG, WU = x.cuda(), wg.cuda(), wu.cuda()
+    _, saved = layers.gated_forward(X, WG, WU)
+    gx, gwg, gwu, _, _ = layers.gated_backward(gh.cuda(), X, WG, WU, saved, need_bias=False)
+    sync()
+    g, u = saved.cpu().double()
+    p = torch.sigmoid(g)
+    dg, du = gh.double() * u * p * (1 + g * (1 - p)), gh.double() * g * p
+    for got, d in ((gwg, dg), (gwu, du)):
+        once(got, d.t(), x.double(), F16, "gw", 2.0 ** -18 * (d.t().abs() @ x.double().abs()) +
+             2.0 ** -38 * float(d.abs().max()) * x.double().abs().sum(0, keepdim=True) +
+             2.0 ** -20 * (gh.double().abs().t() @ x.double().abs()))
+    both, wide = torch.cat([dg, du], 1), torch.cat([wg, wu], 0).double()
+    once(gx, both, wide, F16, "gx", 2.0 ** -18 * (both.abs() @ wide.abs()) + 2.0 ** -38 * float(both.abs().max()) * wide.abs().sum(0, keepdim=True)
+         + 2.0 ** -20 * (torch.cat([gh, gh], 1).double().abs() @ wide.abs()))
