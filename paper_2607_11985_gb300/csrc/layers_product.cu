@@ -481,18 +481,49 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(void* p, 
     }
 }
 
+// v cut towards zero to a value of T, one step further towards zero, the smallest value of T
+template <typename T> struct Cut;
+template <> struct Cut<__nv_bfloat16> {
+    static __device__ __forceinline__ float cut(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+    static __device__ __forceinline__ float before(float h) { return __uint_as_float(__float_as_uint(h) - 0x10000u); }
+    static __device__ __forceinline__ float least() { return __uint_as_float(0x10000u); }
+};
+template <> struct Cut<__half> {
+    static __device__ __forceinline__ float cut(float v) { return __half2float(__float2half_rz(v)); }
+    static __device__ __forceinline__ float before(float h) { return __half2float(__ushort_as_half(__half_as_ushort(__float2half(h)) - 1)); }
+    static __device__ __forceinline__ float least() { return 5.9604644775390625e-8f; }
+};
+
+// The next of the three parts that add up to a value; `rest` becomes what is left.  Every part of a
+// value other than zero has its sign and is not zero itself, so that a factor that is
+// infinite makes the one infinity of all their products (zero or the other sign would make
+// it NaN).  Where the value ends early a part gives one unit to the next; what the smallest
+// values of T add is a few of these.  All parts of an infinity or NaN are that.
+template <typename T> __device__ __forceinline__ float next_part(float& rest, bool last) {
+    const float near = to_f(from_f<T>(rest));
+    if (rest == 0.f || !(fabsf(near) <= 3.4028234e38f)) return rest;
+    float h = last ? near : Cut<T>::cut(rest);
+    if (!last && h == rest) h = Cut<T>::before(h);
+    if (h == 0.f) h = copysignf(Cut<T>::least(), rest);
+    const float left = fabsf(rest) - fabsf(h);
+    rest = copysignf(left > 0.f ? left : 1.4e-45f, rest);
+    return h;
+}
+
 template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
-    store8<T, VEC>(A.dz[i], row, c, A.n, v);
-    if (!A.second) return;
+    if constexpr (sizeof(T) == 2) {
+        if (A.second) {
+#pragma unroll 1
+            for (int part = 0; part < 3; ++part) {
+                float h[8];
 #pragma unroll
-    for (int part = 1; part < 3; ++part) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {       // nothing is left of what became infinite
-            const float h = to_f(from_f<T>(v[e]));
-            v[e] = fabsf(h) <= 3.4028234e38f ? v[e] - h : 0.f;
+                for (int e = 0; e < 8; ++e) h[e] = next_part<T>(v[e], part == 2);
+                store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, h);
+            }
+            return;
         }
-        store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, v);
     }
+    store8<T, VEC>(A.dz[i], row, c, A.n, v);
 }
 
 // the largest of |v| that is finite, and `top`

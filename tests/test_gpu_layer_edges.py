@@ -2,6 +2,7 @@
 and devices, and of the time that they may take.
 """
 
+import math
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -60,6 +61,14 @@ def once(got, a, b, dtype, what, more=0.0):
         what, int((d > bound).sum()), d.numel(), float((d / bound).max()))
 
 
+def same_infinities(got, want, what):
+    got = got.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    there = torch.isinf(want)
+    assert bool(there.any()) and torch.equal(got[there], want[there]), what
+    assert bool(torch.isfinite(got[torch.isfinite(want)]).all()), what
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("rows,inp,out", [(512, 1024, 4), (8, 1000, 600)])
 def test_gradients_of_float_outputs_round_once(layers, dtype, rows, inp, out):
@@ -70,6 +79,21 @@ def test_gradients_of_float_outputs_round_once(layers, dtype, rows, inp, out):
     sync()
     once(gx, gy.double(), w.double(), dtype, "gx")
     once(gw, gy.double().t(), x.double(), dtype, "gw")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,inp,out", [(40, 24, 16), (2048, 1024, 1024)])
+def test_infinite_weights_and_features_in_gradients(layers, dtype, rows, inp, out):
+    """An infinite weight makes the gradients that it enters infinite, of the sign of dz
+    times its own, or NaN where dz is zero, in both sizes of a backward; so does an
+    infinite feature."""
+    x, w, gy = normal(1, rows, inp, dtype=dtype), normal(2, out, inp, dtype=dtype), normal(3, rows, out)
+    gy[0, 3], gy[1, 3], gy[2, 3], gy[3, 3], gy[4, 3] = 0.5, 0.0, 1.0, -2.0, 0.3
+    w[3, 5], w[3, 6], x[2, 7], x[4, 8] = math.inf, -math.inf, math.inf, -math.inf
+    gx, gw, _ = layers.linear_backward(gy.cuda(), x.cuda(), w.cuda(), None, "none")
+    sync()
+    same_infinities(gx, gy.double() @ w.double(), "gx")
+    same_infinities(gw, gy.double().t() @ x.double(), "gw")
 
 
 @pytest.mark.parametrize("scale", [1e-7, 1e5])
