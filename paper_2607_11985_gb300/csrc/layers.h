@@ -69,19 +69,10 @@ struct Product {
     Finish f;
 };
 
-// The float operands of a product that the tensor cores ran in parts: an output
-// that is not finite is worked out again from them (see layers_tc.cu).
-struct Exact {
-    Operand a[2], b[2];
-    int64_t k;       // 0: not asked for
-    int32_t form;
-};
-
 // Sums of a contraction that was cut, [splits][1 or 2][m][n] (two for GATED and PAIR),
 // still to be joined in the order of the cuts and finished.
 struct Join {
     Finish f;
-    Exact exact;
     const float* part;
     int32_t splits, form;
 };

@@ -145,23 +145,6 @@ __device__ __forceinline__ float2 act_both(int act, float z) {
     }
 }
 
-// v, or where it is not finite the sum itself, one product after the other (rare:
-// infinities, NaN, overflow).
-__device__ __noinline__ inline float exact_sum(const Exact& x, int which, int64_t row, int64_t col) {
-    float v = 0.f;
-    for (int t = 0; t < (x.form == SUM ? 2 : 1); ++t) {
-        const int ia = x.form == GATED ? 0 : which + t, ib = x.form == GATED ? which : which + t;
-        const Operand &a = x.a[ia], &b = x.b[ib];
-        const float* pa = static_cast<const float*>(a.p) + (a.k_outer ? row : row * a.ld);
-        const float* pb = static_cast<const float*>(b.p) + (b.k_outer ? col : col * b.ld);
-        for (int64_t k = 0; k < x.k; ++k) v = fmaf(pa[a.k_outer ? k * a.ld : k], pb[b.k_outer ? k * b.ld : k], v);
-    }
-    return v;
-}
-__device__ __forceinline__ float exact_if_not_finite(const Exact& x, int which, int64_t row, int64_t col, float v) {
-    return fabsf(v) <= 3.4028234e38f ? v : exact_sum(x, which, row, col);
-}
-
 // The end of a product for W neighbouring elements of a row (1, or 4 where a row holds a
 // multiple of 4: outputs are then written at once): v (and u, gated) are the sums.
 template <int W>

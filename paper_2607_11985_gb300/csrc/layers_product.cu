@@ -252,12 +252,6 @@ template <int W> __device__ __forceinline__ void join_at(const Join& j, int whic
     }
     // most outputs count less than 2^32 elements: a short division
     const int64_t row = size >> 32 ? e / j.f.n : (int64_t)((uint32_t)e / (uint32_t)j.f.n), col = e - row * j.f.n;
-    if (j.exact.k) {
-        for (int i = 0; i < W; ++i) {
-            v0[i] = exact_if_not_finite(j.exact, which, row, col + i, v0[i]);
-            if (j.form == GATED) v1[i] = exact_if_not_finite(j.exact, 1, row, col + i, v1[i]);
-        }
-    }
     finish_some<W>(j.f, which, row, col, v0, v1);
 }
 // One row of many cuts (column sums): a warp's lanes take 32 columns, warp w the cuts w,
@@ -291,7 +285,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Joins
     if (which && j.form != PAIR) return;
     const int64_t size = j.f.m * j.f.n, step = (int64_t)gridDim.x * blockDim.x, at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t stride = size * (j.form == GATED || j.form == PAIR ? 2 : 1);
-    if (j.f.m == 1 && j.form != GATED && !j.exact.k && j.splits >= 8) {
+    if (j.f.m == 1 && j.form != GATED && j.splits >= 8) {
         join_row(j, which, stride);
     } else if (j.f.n % 4 == 0) {
         for (int64_t e = 4 * at; e < size; e += 4 * step) join_at<4>(j, which, size, stride, e);

@@ -72,7 +72,6 @@ template <int kParts> struct Problem {
     static constexpr int kPartsA = kParts == 1 ? 1 : 3, kPartsB = kParts == 3 ? 3 : 1;
     CUtensorMap ma[2][kPartsA], mb[2][kPartsB];
     Finish f;
-    Exact exact;                // of float operands
     float* part;                // sums of a cut contraction, or NULL
     int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec;   // vec: bytes of a store
 };
@@ -416,28 +415,6 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
             if (kGated) turned(u, row0, col0, f.m, n, lane, stage, put);
         }
         return;
-    }
-    if (kParts == 3 && in) {
-        float t = 0.f;       // NaN if one of the sums is not finite
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t = fmaf(v[i], 0.f, kGated ? fmaf(u[i], 0.f, t) : t);
-        if (t != 0.f) {
-            for (int i = 0; i < 16; ++i) {
-                float a = 0.f, b = 0.f;
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (j == i) { a = v[j]; b = kGated ? u[j] : 0.f; }
-                if (col0 + i >= n) break;
-                a = exact_if_not_finite(A.exact, T.which, row, col0 + i, a);
-                if (kGated) b = exact_if_not_finite(A.exact, 1, row, col0 + i, b);
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (j == i) {
-                        v[j] = a;
-                        if (kGated) u[j] = b;
-                    }
-            }
-        }
     }
     if (!kGated && f.scale) scale16(*f.scale, v);
     if (f.bias[T.which]) add_bias(bias, v);
@@ -879,19 +856,30 @@ cudaError_t error_word(unsigned** p) {
     return cudaSuccess;
 }
 
-// A float as the sum of three bf16, 8 bits of it each, rounded to nearest: exact for
-// normal results.  A value that is not finite is its own first part (and the sums
-// that it enters are worked out again, see Exact); one that would round to
-// infinity is cut instead.
+// A float as the sum of three bf16, 8 bits of it each: exact for normal results.  The six products
+// of parts (kOrderA, kOrderB) have to make float's infinities and NaN of two operands' parts:
+//   - a value below 2^8 is rounded to nearest at each part, so that what the six products drop has either sign;
+//   - above, where a product of two such parts could leave the range with the other sign, it is cut, all
+//     parts with its sign (an infinity of the whole product is then that of its parts);
+//   - an infinity is 1, 0 and the infinity: that third part meets the other operand's first
+//     part only, which is zero, positive or negative as the operand is (1 where that is an infinity too).  A
+//     NaN, so placed, is in every sum.
+// (A finite product within 2^-8 of the largest float may come out infinite, and a finite operand
+// below 2^-134 counts as zero beside an infinite one.)
 __device__ __forceinline__ void bf16_parts(float x, uint16_t (&o)[3]) {
+    const float size = fabsf(x);
+    if (!(size <= 3.4028234e38f)) {
+        o[0] = 0x3f80 | (uint16_t)(__float_as_uint(x) >> 16 & 0x8000);
+        o[1] = 0;
+        o[2] = __bfloat16_as_ushort(__float2bfloat16(x));
+        return;
+    }
     float rest = x;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-        __nv_bfloat16 h = __float2bfloat16(rest);
-        uint16_t bits = __bfloat16_as_ushort(h);
-        if ((bits & 0x7fff) == 0x7f80 && fabsf(rest) <= 3.4028234e38f) bits -= 1;
-        o[i] = bits;
-        rest = (bits & 0x7f80) == 0x7f80 ? 0.f : rest - __uint_as_float((uint32_t)bits << 16);
+        const uint16_t near = __bfloat16_as_ushort(__float2bfloat16(rest));
+        o[i] = size < 256.f ? near : (uint16_t)(__float_as_uint(rest) >> 16);
+        rest -= __uint_as_float((uint32_t)o[i] << 16);
     }
 }
 
@@ -1205,20 +1193,13 @@ template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c,
     a.kblocks = (int)ceil_div(p.k, BK);
     a.a_mn = p.a[0].k_outer;
     a.b_mn = p.b[0].k_outer;
-    a.exact = Exact{};
     a.part = nullptr;
-    if (kParts == 3) {
-        for (int i = 0; i < 2; ++i) { a.exact.a[i] = p.a[i]; a.exact.b[i] = p.b[i]; }
-        a.exact.k = p.k;
-        a.exact.form = p.form;
-    }
     if (splits > 1) {
         if (align256((size_t)splits * (gated || p.form == PAIR ? 2 : 1) * p.m * p.n * 4) > r.left)
             return set_error(VQC_ERR_WORKSPACE, "product: workspace too small");
         a.part = reinterpret_cast<float*>(r.at);
         Join& j = joins.j[joins.count++];
         j.f = p.f;
-        j.exact = a.exact;
         j.part = a.part;
         j.splits = splits;
         j.form = p.form;

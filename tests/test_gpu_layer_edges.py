@@ -135,3 +135,50 @@ def test_float16_gate_of_small_gradients(layers):
     both, wide = torch.cat([dg, du], 1), torch.cat([wg, wu], 0).double()
     once(gx, both, wide, F16, "gx", 2.0 ** -18 * (both.abs() @ wide.abs()) + 2.0 ** -38 * float(both.abs().max()) * wide.abs().sum(0, keepdim=True)
          + 2.0 ** -20 * (torch.cat([gh, gh], 1).double().abs() @ wide.abs()))
+
+
+def milliseconds(f):
+    for _ in range(3):
+        f()
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    torch.cuda.synchronize()
+    start.record()
+    for _ in range(5):
+        f()
+    end.record()
+    torch.cuda.synchronize()
+    return start.elapsed_time(end) / 5
+
+
+def test_float_products_of_values_that_are_not_finite_take_no_longer(layers):
+    """A NaN in one weight row, and a model that is NaN throughout: the work of a product does
+    not depend on its values (tenfold for what a clock may move)."""
+    x, w = normal(1, 1024, 1024).cuda(), normal(2, 1024, 1024).cuda()
+    clean = milliseconds(lambda: layers.linear_forward(x, w, save=False))
+    w[17] = math.nan
+    row = milliseconds(lambda: layers.linear_forward(x, w, save=False))
+    y = layers.linear_forward(x, w, save=False)
+    assert bool(torch.isnan(y[:, 17]).all()) and int(torch.isnan(y).sum()) == 1024
+    w[:] = math.inf
+    x[:] = -1.0
+    full = milliseconds(lambda: layers.linear_forward(x, w, save=False))
+    assert bool((layers.linear_forward(x, w, save=False) == -math.inf).all())
+    sync()
+    assert max(row, full) <= 10 * clean, (clean, row, full)
+
+
+def test_float_parts_of_infinite_and_zero_operands(layers):
+    """Infinite against infinite, zero, positive and negative operands on both sides of a
+    float product in parts, and sums that leave the range."""
+    rows, inp, out = 800, 640, 800
+    x, w, gy = normal(1, rows, inp), normal(2, out, inp), normal(3, rows, out)
+    x[0, 0], x[1, 0], x[2, 1], x[3, 2] = math.inf, -math.inf, math.nan, math.inf
+    w[0, 0], w[1, 0], w[2, 0], w[3, 5], w[4, 2], w[5, 2] = math.inf, -math.inf, 0.0, math.nan, 0.0, -1e-30
+    gy[6, 0], gy[6, 1], gy[7, 0], gy[8, 9], gy[10, 11] = 0.0, 2.0, math.inf, -math.inf, 1e-30
+    x[9], w[9] = 1e30, 1e30
+    y = layers.linear_forward(x.cuda(), w.cuda(), save=False)
+    gx, gw, _ = layers.linear_backward(gy.cuda(), x.cuda(), w.cuda(), None, "none")
+    sync()
+    for got, a, b in ((y, x, w.t()), (gx, gy, w), (gw, gy.t(), x)):
+        want = a.double() @ b.double()
+        same_infinities(got, torch.where(want.abs() > 3.4028235677973366e38, torch.sign(want) * math.inf, want), got.shape)
