@@ -142,7 +142,7 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     if (gated && (!gw[0] != !gw[1] || !gb[0] != !gb[1])) return bad(call, "one of two gradients is NULL");
     const size_t e = elem_size(dtype), eo = elem_size(out_dtype);
     if (!on(gy, eo) || !on(x, e) || !on(w[0], e) || (gated && !on(w[1], e)) || !on(saved, 4) || !on(gx, 16) ||
-        !on(gw[0], 16) || (gated && !on(gw[1], 16)) || !on(gb[0], e) || (gated && !on(gb[1], e)) || !on(ws, 256))
+        !on(gw[0], 16) || (gated && !on(gw[1], 16)) || !on(gb[0], 16) || (gated && !on(gb[1], 16)) || !on(ws, 256))
         return bad(call, "misaligned operand, output or workspace");
     const bool aligned = on(x, 16) && on(w[0], 16) && (!gated || on(w[1], 16)) && on(gy, 16);
     const BackSpace b = back_space(dtype, out_dtype, rows, in, out, ld_x, ld_w, ld_gy, act, gated, aligned);
