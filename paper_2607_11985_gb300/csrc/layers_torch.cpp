@@ -54,6 +54,8 @@ std::string told(const Tensor& t) {
     return s + "]";
 }
 
+bool here(const Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+
 // [rows, cols] with adjacent row elements, `ld` elements from row to row
 struct Matrix {
     Tensor t;
@@ -63,7 +65,7 @@ struct Matrix {
 };
 Matrix matrix(const Tensor& given, const char* name) {
     const int code = given.defined() ? code_of(given.scalar_type()) : -1;
-    if (code < 0 || !given.is_cuda() || given.dim() == 0 || given.get_device() != c10::cuda::current_device())
+    if (code < 0 || given.dim() == 0 || !here(given))
         throw Refused(std::string(name) + " must be a CUDA float32, bfloat16 or float16 tensor on the current device (got " + told(given) + ")");
     const int64_t cols = given.size(given.dim() - 1);
     if (cols < 1) throw Refused(std::string(name) + " must have at least one column (got " + told(given) + ")");
@@ -90,14 +92,14 @@ Matrix weight(const Tensor& given, int64_t cols, int code, const char* name) {
 }
 Tensor vector(const Tensor& given, int64_t n, int code, const char* name) {
     if (!given.defined()) return given;
-    if (given.scalar_type() != type_of(code) || given.dim() != 1 || given.size(0) != n || !given.is_cuda())
+    if (given.scalar_type() != type_of(code) || given.dim() != 1 || given.size(0) != n || !here(given))
         throw Refused(std::string(name) + " must be a CUDA " + c10::toString(type_of(code)) + " tensor of " + std::to_string(n) +
-                      " elements (got " + told(given) + ")");
+                      " elements on the current device (got " + told(given) + ")");
     return given.is_contiguous() ? given : given.contiguous();
 }
 const float* saved_of(const Tensor& t, at::IntArrayRef shape) {
-    if (!t.defined() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !t.is_cuda())
-        throw Refused("saved must be what the forward returned for these rows");
+    if (!t.defined() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !here(t))
+        throw Refused("saved must be what the forward returned for these rows, on the current device (got " + told(t) + ")");
     return static_cast<const float*>(t.data_ptr());
 }
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }

@@ -182,3 +182,39 @@ def test_float_parts_of_infinite_and_zero_operands(layers):
     for got, a, b in ((y, x, w.t()), (gx, gy, w), (gw, gy.t(), x)):
         want = a.double() @ b.double()
         same_infinities(got, torch.where(want.abs() > 3.4028235677973366e38, torch.sign(want) * math.inf, want), got.shape)
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that says it is on another device, without memory there."""
+
+    @staticmethod
+    def __new__(cls, size, dtype=F32):
+        return torch.Tensor._make_wrapper_subclass(cls, size, dtype=dtype, device="cuda:1")
+
+    @classmethod
+    def __torch_dispatch__(cls, f, types, args=(), kwargs=None):
+        raise RuntimeError("no operation here")
+
+
+def test_tensors_of_another_device_are_refused(layers):
+    x, w, b, n = (torch.ones(s, device="cuda") for s in ((4, 8), (6, 8), (6,), (8,)))
+    gy, z = torch.ones(4, 6, device="cuda"), torch.ones(4, 6, device="cuda")
+    stats = torch.ones(4, 2, device="cuda")
+    E = Elsewhere
+    for call in (lambda: layers.linear_forward(E((4, 8)), w, b),
+                 lambda: layers.linear_forward(x, E((6, 8)), b),
+                 lambda: layers.linear_forward(x, w, E((6,))),
+                 lambda: layers.linear(x, w, E((6,))),
+                 lambda: layers.linear_forward(x, w, b, residual=E((4, 6))),
+                 lambda: layers.linear_backward(E((4, 6)), x, w, z, "tanh"),
+                 lambda: layers.linear_backward(gy, x, w, E((4, 6)), "tanh"),
+                 lambda: layers.gated_forward(x, w, w, E((6,)), b),
+                 lambda: layers.gated_forward(x, w, w, b, E((6,))),
+                 lambda: layers.gated_backward(gy, x, w, w, E((2, 4, 6))),
+                 lambda: layers.layer_norm_forward(x, E((8,)), n),
+                 lambda: layers.layer_norm_forward(x, n, E((8,))),
+                 lambda: layers.layer_norm_backward(x, x, E((8,)), stats),
+                 lambda: layers.layer_norm_backward(x, x, n, E((4, 2)))):
+        with pytest.raises(ValueError):
+            call()
+    sync()
