@@ -56,6 +56,12 @@ std::string told(const Tensor& t) {
 
 bool here(const Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
 
+// Every operand comes by here: a tangent, which no operator carries on, is refused, not dropped.
+void no_tangent(const Tensor& t, const char* name) {
+    if (t._fw_grad(0).defined())
+        throw std::runtime_error(std::string("forward-mode derivatives of the layer operators are not implemented (") + name + " has a tangent)");
+}
+
 // [rows, cols] with adjacent row elements, `ld` elements from row to row
 struct Matrix {
     Tensor t;
@@ -69,6 +75,7 @@ Matrix matrix(const Tensor& given, const char* name) {
         throw Refused(std::string(name) + " must be a CUDA float32, bfloat16 or float16 tensor on the current device (got " + told(given) + ")");
     const int64_t cols = given.size(given.dim() - 1);
     if (cols < 1) throw Refused(std::string(name) + " must have at least one column (got " + told(given) + ")");
+    no_tangent(given, name);
     Matrix m{given, 0, cols, cols, code};
     if (given.dim() != 2) m.t = given.reshape({-1, cols});
     m.rows = m.t.size(0);
@@ -95,11 +102,13 @@ Tensor vector(const Tensor& given, int64_t n, int code, const char* name) {
     if (given.scalar_type() != type_of(code) || given.dim() != 1 || given.size(0) != n || !here(given))
         throw Refused(std::string(name) + " must be a CUDA " + c10::toString(type_of(code)) + " tensor of " + std::to_string(n) +
                       " elements on the current device (got " + told(given) + ")");
+    no_tangent(given, name);
     return given.is_contiguous() ? given : given.contiguous();
 }
 const float* saved_of(const Tensor& t, at::IntArrayRef shape) {
     if (!t.defined() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !here(t))
         throw Refused("saved must be what the forward returned for these rows, on the current device (got " + told(t) + ")");
+    no_tangent(t, "saved");
     return static_cast<const float*>(t.data_ptr());
 }
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }

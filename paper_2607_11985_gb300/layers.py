@@ -9,12 +9,13 @@ What stands around a ``Circuit`` inside a network, in the library's kernels:
 
 Each has three forms: ``linear_forward`` and ``linear_backward`` are the two
 calls of a training step (or inference with ``save=False``), ``linear`` the
-same under autograd.  x may have any leading axes; rows may be strided (other
-layouts are copied).  Types: float32, bfloat16 and float16, sums and
-statistics in float; see include/vqc.h for the formulas and roundings.  Tensors
-are on the current device, work goes to its current stream.  Torch supplies
-device memory and the stream only.  Arguments that do not fit raise ValueError,
-statuses of the library ``binding.VQCError``.
+same under autograd (once; forward-mode derivatives are refused).  x may have
+any leading axes; rows may be strided (other layouts are copied).  Types:
+float32, bfloat16 and float16, sums and statistics in float; see include/vqc.h
+for the formulas and roundings.  Tensors are on the current device, work goes to
+its current stream.  Torch supplies device memory and the stream only.
+Arguments that do not fit raise ValueError, statuses of the library
+``binding.VQCError``.
 
 A call on a few rows costs its host path, so the checks, the allocations and the
 calls of the C entry points are native (csrc/layers_torch.cpp, ``_layers.so``).

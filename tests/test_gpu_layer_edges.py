@@ -184,6 +184,36 @@ def test_float_parts_of_infinite_and_zero_operands(layers):
         same_infinities(got, torch.where(want.abs() > 3.4028235677973366e38, torch.sign(want) * math.inf, want), got.shape)
 
 
+@pytest.mark.parametrize("which", ["layer_norm", "linear", "gated"])
+def test_tangents_are_refused(layers, which):
+    """Forward-mode derivatives are not there: refused, not dropped, for every input, for
+    inputs that need a gradient as well, and for an incoming gradient."""
+    import torch.autograd.forward_ad as fwd
+    x, w, u, b, c, r, nw, nb = (normal(i, *s).cuda() for i, s in
+                                enumerate([(6, 8), (5, 8), (5, 8), (5,), (5,), (6, 5), (8,), (8,)]))
+    f, ops = {"layer_norm": (layers.layer_norm, [x, nw, nb]),
+              "linear": (lambda x, w, b, r: layers.linear(x, w, b, "tanh", r), [x, w, b, r]),
+              "gated": (layers.gated, [x, w, u, b, c])}[which]
+    for i in range(len(ops)):
+        for needs in (False, True):
+            with fwd.dual_level():
+                some = [t.clone().requires_grad_(needs) for t in ops]
+                some[i] = fwd.make_dual(some[i], torch.ones_like(some[i]))
+                with pytest.raises(RuntimeError, match="[Ff]orward"):
+                    f(*some)
+                with torch.no_grad(), pytest.raises(RuntimeError, match="[Ff]orward"):
+                    f(*some)
+    leaves = [t.clone().requires_grad_() for t in ops]
+    y = f(*leaves)
+    with fwd.dual_level():
+        gy = fwd.make_dual(torch.ones_like(y), torch.ones_like(y))
+        for graph in (False, True):
+            with pytest.raises(RuntimeError, match="[Ff]orward"):
+                torch.autograd.grad(y, leaves, gy, retain_graph=True, create_graph=graph)
+    torch.autograd.grad(y, leaves, torch.ones_like(y))
+    sync()
+
+
 class Elsewhere(torch.Tensor):
     """A tensor that says it is on another device, without memory there."""
 
