@@ -327,6 +327,7 @@ struct LinearFunction : Function<LinearFunction> {
         else ctx->save_for_backward({x, w});
         ctx->saved_data["present"] = (int64_t)(3 | (b ? 4 : 0) | (res ? 8 : 0));
         ctx->saved_data["act"] = act;
+        if (res && res->sizes() != y.sizes()) ctx->saved_data["residual"] = res->sizes().vec();      // as many rows, other leading axes
         return y;
     }
     static variable_list backward(AutogradContext* ctx, variable_list g) {
@@ -340,7 +341,8 @@ struct LinearFunction : Function<LinearFunction> {
         if (nx || nw || nb)
             r = at::GradMode::is_enabled() ? spread(LinearGradients::apply(g[0], s[0], s[1], optional(z), act, nx, nw, nb), {nx, nw, nb})
                                            : linear_backward(g[0], s[0], s[1], z, act, nx, nw, nb);
-        r.push_back(nr ? g[0] : Tensor());
+        const auto shape = ctx->saved_data.find("residual");
+        r.push_back(!nr ? Tensor() : shape == ctx->saved_data.end() ? g[0] : g[0].reshape(shape->second.toIntVector()));
         r.resize(6);
         return r;
     }

@@ -77,6 +77,7 @@ def linear_backward(grad_y, x, weight, saved, activation="none", need_x=True, ne
 
 def linear(x, weight, bias=None, activation="none", residual=None, out_dtype=None):
     """act(x weight^T + bias) + residual, differentiable in all four tensors.
+    The residual has as many rows as x, in any leading axes.
     ``activation``: "none", "relu", "gelu", "silu", "tanh" or "sigmoid";
     ``out_dtype`` (and the residual's type) may be float32 for 16-bit x, or a
     16-bit type for float32 x."""

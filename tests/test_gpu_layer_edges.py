@@ -214,6 +214,20 @@ def test_tangents_are_refused(layers, which):
     sync()
 
 
+def test_residual_of_other_leading_axes(layers):
+    """A residual with as many rows as x in other leading axes: its gradient has its shape."""
+    x, w = normal(1, 3, 5, 8).cuda().requires_grad_(), normal(2, 6, 8).cuda().requires_grad_()
+    for shape in ((15, 6), (5, 3, 6), (1, 15, 6), (3, 5, 6)):
+        r = normal(3, *shape).cuda().requires_grad_()
+        y = layers.linear(x, w, None, "tanh", r)
+        gy = normal(4, *y.shape).cuda()
+        for graph in (False, True):
+            gx, gw, gr = torch.autograd.grad(y, (x, w, r), gy, retain_graph=True, create_graph=graph)
+            assert y.shape == (3, 5, 6) and gr.shape == r.shape and torch.equal(gr.reshape(15, 6), gy.reshape(15, 6))
+            assert gx.shape == x.shape and gw.shape == w.shape
+    sync()
+
+
 class Elsewhere(torch.Tensor):
     """A tensor that says it is on another device, without memory there."""
 
