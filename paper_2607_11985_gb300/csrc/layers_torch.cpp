@@ -76,8 +76,8 @@ Matrix matrix(const Tensor& given, const char* name) {
     const int64_t cols = given.size(given.dim() - 1);
     if (cols < 1) throw Refused(std::string(name) + " must have at least one column (got " + told(given) + ")");
     no_tangent(given, name);
-    Matrix m{given, 0, cols, cols, code};
-    if (given.dim() != 2) m.t = given.reshape({-1, cols});
+    Matrix m{given.resolve_neg(), 0, cols, cols, code};      // (a view that torch negates when it reads it)
+    if (given.dim() != 2) m.t = m.t.reshape({-1, cols});
     m.rows = m.t.size(0);
     if (m.t.is_contiguous()) return m;
     const int64_t ld = m.t.stride(0);
@@ -103,10 +103,10 @@ Tensor vector(const Tensor& given, int64_t n, int code, const char* name) {
         throw Refused(std::string(name) + " must be a CUDA " + c10::toString(type_of(code)) + " tensor of " + std::to_string(n) +
                       " elements on the current device (got " + told(given) + ")");
     no_tangent(given, name);
-    return given.is_contiguous() ? given : given.contiguous();
+    return given.resolve_neg().contiguous();
 }
 const float* saved_of(const Tensor& t, at::IntArrayRef shape) {
-    if (!t.defined() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !here(t))
+    if (!t.defined() || t.is_neg() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !here(t))
         throw Refused("saved must be what the forward returned for these rows, on the current device (got " + told(t) + ")");
     no_tangent(t, "saved");
     return static_cast<const float*>(t.data_ptr());

@@ -228,6 +228,19 @@ def test_residual_of_other_leading_axes(layers):
     sync()
 
 
+def test_negated_views(layers):
+    """The imaginary part of a conjugate is a view that torch negates when it is read."""
+    c = torch.complex(normal(1, 40, 1), normal(2, 40, 1)).cuda()
+    x, w = torch.conj(c).imag, torch.ones(4, 1, device="cuda")
+    assert x.is_neg()
+    want = layers.linear_forward(x.clone(), w, save=False)
+    assert torch.equal(layers.linear_forward(x, w, save=False), want) and float(want.norm()) > 0
+    b = torch.conj(torch.complex(normal(3, 1), normal(4, 1)).cuda()).imag
+    got = layers.linear_forward(x.clone(), w[:1], b, save=False)
+    assert b.is_neg() and torch.equal(got, layers.linear_forward(x.clone(), w[:1], b.clone(), save=False))
+    sync()
+
+
 class Elsewhere(torch.Tensor):
     """A tensor that says it is on another device, without memory there."""
 
