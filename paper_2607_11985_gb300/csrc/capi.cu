@@ -1509,6 +1509,9 @@ vqc_status check_ptrs(const HostPlan& p, const void* x, const void* w, const voi
 
 vqc_status set_error(vqc_status s, const std::string& msg) { return fail(s, msg); }
 
+// The same switch for the launches of the layer operators (layers_product.cu).
+bool programmatic_launches() { return use_pdl(); }
+
 // tc_stage.cu: the error word of vqc_stage_apply's kernels (read and cleared).
 vqc_status stage_error_check();
 

@@ -13,6 +13,7 @@
 namespace vqc {
 
 vqc_status set_error(vqc_status s, const std::string& msg);
+bool programmatic_launches();   // false where the environment sets VQC_PDL=0
 
 namespace layers {
 
@@ -26,7 +27,7 @@ vqc_status cuda_error(cudaError_t e, const char* what);
 // A launch that may begin while the kernel before it in the stream ends: its CTAs are
 // placed and set up, then wait in stream_order() (layers_elem.cuh), which every kernel
 // here calls before it touches memory.  Between two dependent kernels this takes
-// away about 2 us.
+// away about 2 us.  (In plain stream order where programmatic launches are switched off.)
 // The limit of a kernel's dynamic shared memory is raised at its first launch on a device.
 cudaError_t launch(const void* fn, dim3 grid, int threads, void** args, cudaStream_t s, size_t shared = 0, int cluster = 1);
 int sm_count();   // of the current device (the GB300's 152 where there is none)

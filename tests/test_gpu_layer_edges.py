@@ -2,13 +2,18 @@
 and devices, and of the time that they may take.
 """
 
+import json
 import math
+import os
+import subprocess
+import sys
 import pytest
 
 torch = pytest.importorskip("torch")
 
 pytestmark = pytest.mark.gpu
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 DIGITS = {F32: 24, BF16: 8, F16: 11}                 # significant bits of a type
 LEAST = {F32: -149, BF16: -133, F16: -24}            # exponent of its smallest number
@@ -275,3 +280,46 @@ def test_tensors_of_another_device_are_refused(layers):
         with pytest.raises(ValueError):
             call()
     sync()
+
+
+def child(code, **env):
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env={**os.environ, **env}, capture_output=True,
+                       text=True, timeout=600)
+    assert r.returncode == 0, r.stdout + r.stderr
+    return json.loads(r.stdout.strip().splitlines()[-1])
+
+
+EDGES = """
+import ctypes, json, torch
+from paper_2607_11985_gb300 import layers
+x, w = torch.ones(64, 256, device="cuda", dtype=torch.bfloat16), torch.ones(128, 256, device="cuda", dtype=torch.bfloat16)
+def step():
+    n, s = layers.layer_norm_forward(x)
+    y, z = layers.linear_forward(n, w, None, "tanh")
+    return layers.linear_backward(y, n, w, z, "tanh")
+step()
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph(keep_graph=True)
+with torch.cuda.graph(graph):
+    out = step()
+rt = None
+for line in open("/proc/self/maps"):
+    if "libcudart" in line:
+        rt = ctypes.CDLL(line.split()[-1].strip())
+        break
+n = ctypes.c_size_t()
+handle = ctypes.c_void_p(graph.raw_cuda_graph())
+assert rt.cudaGraphGetEdges(handle, None, None, None, ctypes.byref(n)) == 0
+a, b, data = (ctypes.c_void_p * n.value)(), (ctypes.c_void_p * n.value)(), ((ctypes.c_ubyte * 8) * n.value)()
+assert rt.cudaGraphGetEdges(handle, a, b, data, ctypes.byref(n)) == 0
+print(json.dumps([n.value, sum(e[2] == 1 for e in data)]))
+"""
+
+
+def test_plain_stream_order_on_request():
+    """VQC_PDL=0: no kernel of the layer operators is let in before the one ahead of it ends.
+    Counted in a captured graph: edges, and those of them that are programmatic."""
+    edges, programmatic = child(EDGES, VQC_PDL="1")
+    assert edges >= 3 and programmatic >= 1
+    edges, programmatic = child(EDGES, VQC_PDL="0")
+    assert edges >= 3 and programmatic == 0
