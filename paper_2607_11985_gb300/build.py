@@ -3,13 +3,13 @@
 The translation units (host compiler, C ABI, one kernel unit per real type and
 mode) compile in parallel; the result is linked into one shared library next
 to this file.  The torch binding of the layer operators (host code) compiles beside
-them with the host compiler.  Nothing is installed outside the source tree.
+them with the host compiler, where a torch with CUDA is installed; the library
+needs none.  Nothing is installed outside the source tree.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import hashlib
-import importlib.metadata
 import importlib.util
 import os
 import shutil
@@ -44,6 +44,13 @@ def nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libvqc.so")
 
 
+def torch_dir():
+    """The folder of an installed torch with CUDA, or None."""
+    spec = importlib.util.find_spec("torch")
+    where = os.path.dirname(spec.origin) if spec and spec.origin else None
+    return where if where and os.path.exists(os.path.join(where, "lib", "libc10_cuda.so")) else None
+
+
 def _sources_digest() -> str:
     h = hashlib.sha256()
     for name in sorted(os.listdir(CSRC)):
@@ -51,7 +58,9 @@ def _sources_digest() -> str:
             h.update(name.encode() + f.read())
     with open(os.path.join(ROOT, "include", "vqc.h"), "rb") as f:
         h.update(f.read())
-    h.update(importlib.metadata.version("torch").encode())     # _layers.so is built against it
+    if torch_dir():
+        with open(os.path.join(torch_dir(), "version.py"), "rb") as f:     # _layers.so is built against it
+            h.update(f.read())
     # flags without the include path, so that a checkout anywhere hashes alike
     h.update(" ".join(ARCH + [f for f in NVCC_FLAGS if not f.startswith("-I")]).encode())
     return h.hexdigest()
@@ -61,7 +70,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     """Compile and link libvqc.so if the sources changed; return its path."""
     digest = _sources_digest()
     stamp = OUT + ".sha256"
-    if not force and os.path.exists(OUT) and os.path.exists(OUT_LAYERS) and os.path.exists(stamp):
+    torch = torch_dir()
+    if not force and os.path.exists(OUT) and (not torch or os.path.exists(OUT_LAYERS)) and os.path.exists(stamp):
         with open(stamp) as f:
             if f.read().strip() == digest:
                 return OUT
@@ -79,7 +89,6 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             raise RuntimeError("nvcc failed for %s:\n%s%s" % (unit, r.stdout, r.stderr))
         return obj, r.stdout + r.stderr
 
-    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     layers_obj = os.path.join(BUILD, "layers_torch.cpp.o")
 
     def host(*args):
@@ -88,7 +97,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             raise RuntimeError("g++ failed for _layers.so:\n%s%s" % (r.stdout, r.stderr))
 
     def compile_layers():
-        inc = os.path.join(torch_dir, "include")
+        inc = os.path.join(torch, "include")
         host("-O2", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"),
              "-I" + sysconfig.get_paths()["include"], "-isystem", inc, "-isystem",
              os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem",
@@ -96,9 +105,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
              "-c", os.path.join(CSRC, "layers_torch.cpp"), "-o", layers_obj)
 
     with cf.ThreadPoolExecutor(max_workers=len(UNITS) + 1) as ex:
-        layers = ex.submit(compile_layers)
+        layers = ex.submit(compile_layers) if torch else None
         results = list(ex.map(compile_one, UNITS))
-        layers.result()
     if verbose or ptxas_info:
         for _, log in results:
             if log.strip():
@@ -109,11 +117,12 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s%s" % (r.stdout, r.stderr))
     os.replace(tmp, OUT)
-    tmp = OUT_LAYERS + ".tmp.%d" % os.getpid()
-    lib = os.path.join(torch_dir, "lib")
-    host("-shared", "-o", tmp, layers_obj, "-L" + HERE, "-l:libvqc.so", "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch",
-         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN")
-    os.replace(tmp, OUT_LAYERS)
+    if torch:
+        layers.result()
+        tmp = OUT_LAYERS + ".tmp.%d" % os.getpid()
+        host("-shared", "-o", tmp, layers_obj, "-L" + os.path.dirname(OUT), "-l:libvqc.so", "-L" + os.path.join(torch, "lib"),
+             "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN")
+        os.replace(tmp, OUT_LAYERS)
     with open(stamp, "w") as f:
         f.write(digest)
     return OUT

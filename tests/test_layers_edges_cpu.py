@@ -26,3 +26,32 @@ def test_misaligned_bias_gradients_are_refused(dtype, e):
         assert linear(A + off) == 1 and "vqc_linear_backward: misaligned" in B.vqc_last_error()
         assert gated(A + off, A) == 1 and gated(A, A + off) == 1
         assert "vqc_gated_backward: misaligned" in B.vqc_last_error()
+
+
+def test_library_builds_without_torch(monkeypatch, tmp_path):
+    """libvqc.so is a C library: with no torch, or one without CUDA, it is compiled and linked as
+    before, and only the torch binding is left out."""
+    from paper_2607_11985_gb300 import build
+    real, ran = build.importlib.util.find_spec, []
+
+    class Done:
+        returncode, stdout, stderr = 0, "", ""
+
+    def run(cmd, **_):
+        ran.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+        return Done
+
+    class Spec:
+        origin = str(tmp_path / "torch" / "__init__.py")       # nothing of CUDA beside it
+    monkeypatch.setattr(build.subprocess, "run", run)
+    monkeypatch.setattr(build, "BUILD", str(tmp_path))
+    for k, found in enumerate((None, Spec)):
+        monkeypatch.setattr(build.importlib.util, "find_spec", lambda name, *a: found if name == "torch" else real(name, *a))
+        monkeypatch.setattr(build, "OUT", str(tmp_path / ("libvqc%d.so" % k)))
+        monkeypatch.setattr(build, "OUT_LAYERS", str(tmp_path / "_layers.so"))
+        ran.clear()
+        assert build.build() == build.OUT
+        assert len(ran) == len(build.UNITS) + 1 and not any("layers_torch" in a for cmd in ran for a in cmd)
+        ran.clear()
+        assert build.build() == build.OUT and not ran       # nothing has changed
