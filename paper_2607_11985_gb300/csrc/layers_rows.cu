@@ -171,7 +171,9 @@ constexpr int steps_ahead(bool gate) { return gate ? 1 : 4; }
 // bytes, k = 16 q + [0, 16) of the step's 64, of weight rows g and g + 8 (a whole line
 // of each row by four lanes) and of rows g (and g + 8) of x; a contraction may take its
 // elements in any order, so these are the operands of four products of depth 16 as they
-// are: no shared memory, no shuffles.
+// are: no shared memory, no shuffles.  The tensor cores cut the low bits of a running sum at
+// every product (all terms positive, depth 8192 in one sum: 4.7e-5 of it), so a step's
+// four products are a sum of their own and the steps are added as floats.
 template <typename T, int NB, bool GATE>
 __global__ void __launch_bounds__(kWarps * 32, GATE ? 6 - NB : 2) mma_rows_kernel(const __grid_constant__ RowsArgs A) {
     constexpr int C = GATE ? 8 : 16, U = steps_ahead(GATE);      // columns of a group, steps in flight
@@ -204,7 +206,8 @@ __global__ void __launch_bounds__(kWarps * 32, GATE ? 6 - NB : 2) mma_rows_kerne
                     for (int i = 0; i < NB; ++i) y[u][i][h] = in ? *reinterpret_cast<const uint4*>(x[i] + k) : zero;
                 }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                float part[NB][4] = {};      // a step's sum
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -212,9 +215,14 @@ __global__ void __launch_bounds__(kWarps * 32, GATE ? 6 - NB : 2) mma_rows_kerne
                         const uint4 &p = a[u][h], &q = b[u][h], &z = y[u][i][h];
                         const uint32_t a0[4] = {p.x, q.x, p.y, q.y}, a1[4] = {p.z, q.z, p.w, q.w};
                         const uint32_t y0[2] = {z.x, z.y}, y1[2] = {z.z, z.w};
-                        mma_16816(acc[i], a0, y0, T());
-                        mma_16816(acc[i], a1, y1, T());
+                        mma_16816(part[i], a0, y0, T());
+                        mma_16816(part[i], a1, y1, T());
                     }
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][e] += part[i][e];
+            }
         }
     }
     let_next();

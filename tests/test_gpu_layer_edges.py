@@ -189,6 +189,23 @@ def test_float_parts_of_infinite_and_zero_operands(layers):
         same_infinities(got, torch.where(want.abs() > 3.4028235677973366e38, torch.sign(want) * math.inf, want), got.shape)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [2, 8, 16])
+def test_float_outputs_of_few_rows_and_deep_contractions(layers, dtype, rows):
+    """A float32 output keeps a float32 sum's accuracy with few rows as well.  All terms
+    positive, so that cuts add up: at most 2^-23 of a chunk's sum at each of its 16 products,
+    half of that on average (16 * 2^-24), and 32 roundings of the sum of chunks
+    (32 * 2^-25)."""
+    inp, out = 8192, 20000
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (0.5 + torch.rand(rows, inp, generator=g, device="cuda")).to(dtype)
+    w = (0.5 + torch.rand(out, inp, generator=g, device="cuda")).to(dtype)
+    y = layers.linear_forward(x, w, None, "none", out_dtype=F32, save=False)
+    sync()
+    want = torch.cat([x.double() @ w[i:i + 4000].double().t() for i in range(0, out, 4000)], 1)
+    assert float((y.double() - want).norm() / want.norm()) <= 16 * 2.0 ** -24 + 32 * 2.0 ** -25
+
+
 @pytest.mark.parametrize("which", ["layer_norm", "linear", "gated"])
 def test_tangents_are_refused(layers, which):
     """Forward-mode derivatives are not there: refused, not dropped, for every input, for
