@@ -548,13 +548,13 @@ __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int6
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (GATE) {
-                const float2 v = act_both(ACT, z[i]);
+                const float2 v = act_both<sizeof(T) == 4>(ACT, z[i]);
                 // rounded products (not fused into the sums), whether or not dz is stored
                 d[i] = __fmul_rn(__fmul_rn(gy[i], u[i]), v.y);
                 u[i] = __fmul_rn(gy[i], v.x);
                 s1[i] += u[i];
             } else {
-                d[i] = ACT == VQC_ACT_NONE ? gy[i] : __fmul_rn(gy[i], act_both(ACT, z[i]).y);
+                d[i] = ACT == VQC_ACT_NONE ? gy[i] : __fmul_rn(gy[i], act_both<sizeof(T) == 4>(ACT, z[i]).y);
             }
             s0[i] += d[i];
         }

@@ -341,17 +341,17 @@ __device__ __forceinline__ void scale16(float scale, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] *= scale;
 }
-template <int ACT> __device__ __forceinline__ void act16_as(float (&v)[16]) {
+template <int ACT, bool kFull> __device__ __forceinline__ void act16_as(float (&v)[16]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = act_value(ACT, v[i]);
+    for (int i = 0; i < 16; ++i) v[i] = act_value<kFull>(ACT, v[i]);
 }
-__device__ __forceinline__ void act16(int act, float (&v)[16]) {
+template <bool kFull> __device__ __forceinline__ void act16(int act, float (&v)[16]) {
     switch (act) {
-        case VQC_ACT_RELU: return act16_as<VQC_ACT_RELU>(v);
-        case VQC_ACT_GELU: return act16_as<VQC_ACT_GELU>(v);
-        case VQC_ACT_SILU: return act16_as<VQC_ACT_SILU>(v);
-        case VQC_ACT_TANH: return act16_as<VQC_ACT_TANH>(v);
-        case VQC_ACT_SIGMOID: return act16_as<VQC_ACT_SIGMOID>(v);
+        case VQC_ACT_RELU: return act16_as<VQC_ACT_RELU, kFull>(v);
+        case VQC_ACT_GELU: return act16_as<VQC_ACT_GELU, kFull>(v);
+        case VQC_ACT_SILU: return act16_as<VQC_ACT_SILU, kFull>(v);
+        case VQC_ACT_TANH: return act16_as<VQC_ACT_TANH, kFull>(v);
+        case VQC_ACT_SIGMOID: return act16_as<VQC_ACT_SIGMOID, kFull>(v);
         default: return;
     }
 }
@@ -394,7 +394,7 @@ __device__ __forceinline__ void turned(const float (&v)[16], int64_t row0, int64
 // Accumulator columns c0..c0+15 (and their partners of the gate) of a warp's 32
 // rows, finished and written: outputs whose rows lie on 16-byte boundaries by rows_out
 // (floats) or straight from the lanes, others turned.
-template <bool kGated, int kParts>
+template <bool kGated, int kParts, bool kSums>
 __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& T, int64_t row0, int64_t col0, int lane,
                                         float (&v)[16], float (&u)[16], const float* bias, float* stage) {
     const Finish& f = A.f;
@@ -426,7 +426,7 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
         if (vec) floats_out(stage, w ? u : v, z + row0 * n + col0, n, rows, lane);
         else turned(w ? u : v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { z[r * n + c] = x; });
     }
-    act16(f.act, v);
+    act16<kSums>(f.act, v);
     if (kGated) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] *= u[i];
@@ -464,7 +464,7 @@ __device__ __forceinline__ void write32(const Problem<kParts>& A, const TileAt& 
         if (kGated && f.bias[1]) add_bias(bias + kBiasUp + 16 * h, u[h]);
         if (f.z[T.which]) floats_out(stage, v[h], f.z[T.which] + at + 16 * h, n, rows, lane);
         if (kGated && f.z[1]) floats_out(stage, u[h], f.z[1] + at + 16 * h, n, rows, lane);
-        act16(f.act, v[h]);
+        act16<false>(f.act, v[h]);      // (16-bit outputs)
         if (kGated) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[h][i] *= u[h][i];
@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                         write32<kGated, kParts>(A, T, row0, n0 + c, lane, v, u, res, bias, stage);
                     } else {
 #pragma unroll
-                        for (int h = 0; h < kStep / 16; ++h) write16<kGated, kParts>(A, T, row0, n0 + c + 16 * h, lane, v[h], u[h], bias + 16 * h, stage);
+                        for (int h = 0; h < kStep / 16; ++h) write16<kGated, kParts, kSums>(A, T, row0, n0 + c + 16 * h, lane, v[h], u[h], bias + 16 * h, stage);
                     }
                 }
                 release();
@@ -817,7 +817,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 if (!ok) break;
 #pragma unroll
                 for (int q = 0; q < kSteps; ++q) {
-                    write16<kGated, kParts>(A, T, row0, n0 + half * (kCols / 2) + 16 * q, lane, v[q], u[q], stage + kBias + 16 * q, stage);
+                    write16<kGated, kParts, kSums>(A, T, row0, n0 + half * (kCols / 2) + 16 * q, lane, v[q], u[q], stage + kBias + 16 * q, stage);
                 }
             }
         }

@@ -206,6 +206,24 @@ def test_float_outputs_of_few_rows_and_deep_contractions(layers, dtype, rows):
     assert float((y.double() - want).norm() / want.norm()) <= 16 * 2.0 ** -24 + 32 * 2.0 ** -25
 
 
+def test_gelu_in_float_over_its_range(layers):
+    """z Phi(z) and its derivative to 2^-20 of their terms, as functions of the math library
+    are: the tail as well, where Phi itself is small."""
+    z = torch.cat([torch.linspace(-12.5, 12.5, 40001), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 30.0, -30.0, 1e19, -1e19])])
+    x, one = z[:, None].cuda(), torch.ones(1, 1, device="cuda")
+    y, saved = layers.linear_forward(x, one, None, "gelu")
+    gx, _, _ = layers.linear_backward(torch.ones_like(y), x, one, saved, "gelu", need_weight=False, need_bias=False)
+    sync()
+    assert torch.equal(saved.cpu()[:, 0], z)
+    v = z.double()
+    phi, pdf = 0.5 * torch.erfc(-v / math.sqrt(2.0)), torch.exp(-0.5 * v * v) / math.sqrt(2.0 * math.pi)
+    tiny = 2.0 ** -126
+    d = (y[:, 0].double().cpu() - v * phi).abs() / (2.0 ** -20 * (v * phi).abs() + tiny)
+    assert float(d.max()) <= 1, (float(d.max()), float(v[d.argmax()]))
+    d = (gx[:, 0].double().cpu() - phi - v * pdf).abs() / (2.0 ** -20 * (phi + (v * pdf).abs()) + tiny)
+    assert float(d.max()) <= 1, (float(d.max()), float(v[d.argmax()]))
+
+
 @pytest.mark.parametrize("which", ["layer_norm", "linear", "gated"])
 def test_tangents_are_refused(layers, which):
     """Forward-mode derivatives are not there: refused, not dropped, for every input, for
