@@ -398,7 +398,9 @@ vqc_status vqc_frames_export(const vqc_plan* plan, void* buf, size_t* inout_byte
  * per row are empty, sums over rows zero); a norm's columns 1..2^31-1, the sizes
  * of linear and gated below 2^30.  Calls are
  * stream-ordered and use no memory but their arguments; results do not depend
- * on timing (sums have a fixed order).  A call whose workspace size is 0 may
+ * on timing (sums have a fixed order).  The tensor-core products wait for their own copies
+ * inside the GPU; a wait that takes longer than 4 s, or the environment's VQC_WAIT_NS
+ * nanoseconds, ends the kernel with its output incomplete (see vqc_sync_check).  A call whose workspace size is 0 may
  * be given NULL.  Buffers must not overlap. */
 typedef enum { VQC_F32 = 0, VQC_BF16 = 1, VQC_F16 = 2 } vqc_real;
 

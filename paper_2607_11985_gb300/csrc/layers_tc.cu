@@ -35,12 +35,15 @@
 // tensor pipe 91% active under the power cap); small products end at about 7 us (start, first
 // loads, one accumulator).
 //
-// Every wait is bounded; one that runs out sets the error word, the CTAs drain
-// their copies and products, free their tensor memory and return.
+// Every wait is bounded (4 s, or the environment's VQC_WAIT_NS).  A warp whose wait runs out sets the
+// error word and tells the other warps of both CTAs, whose own waits then end; all meet at the
+// kernel's last barrier, copies and products still in flight are waited for, tensor memory is
+// freed and the CTAs return.
 #include <cuda.h>
 
 #include <algorithm>
 #include <atomic>
+#include <cstdlib>
 
 #include "layers_elem.cuh"
 #include "layers_tc.h"
@@ -56,7 +59,7 @@ constexpr int kStageA = BM * BK * 2;                 // 16 KB
 constexpr int kStaging = kEpiWarps * 2 * 32 * 17 * 4;   // transposition of unaligned outputs
 constexpr int kBarriers = 1024;
 constexpr int kSmemLimit = 232448;
-constexpr unsigned long long kWaitNs = 4000000000ull;   // bound of every wait
+constexpr unsigned long long kWaitNs = 4000000000ull;   // bound of a wait
 
 template <int CG, int BN> struct Shape {
     static constexpr int kStageB = BN / CG * BK * 2;
@@ -102,6 +105,7 @@ template <int kParts> struct TcArgs {
     Problem<kParts> q[2];
     Schedule plan;
     unsigned* err;
+    unsigned long long wait_ns;
     int bf16;
 };
 
@@ -148,17 +152,23 @@ __device__ __forceinline__ bool mbar_try(uint32_t mbar, uint32_t parity) {
     return done != 0;
 }
 
-// Bounded wait for a phase; false when it ran out or another role gave up.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t mbar, uint32_t parity, const volatile int* gave_up) {
-    const unsigned long long end = now_ns() + kWaitNs;
-    for (unsigned i = 0;; ++i) {
-        if (mbar_try(mbar, parity)) return true;
-        if ((i & 63) == 63 && ((gave_up && *gave_up) || now_ns() > end)) return false;
-    }
+// Bounded wait for a phase; false when it ran out or another role gave up.  Lanes may see the end
+// at different times: the warp goes by what all of them saw.
+__device__ __noinline__ bool mbar_wait_slow(uint32_t mbar, uint32_t parity, unsigned long long ns, const volatile int* gave_up) {
+    const unsigned long long end = now_ns() + ns;
+    while (!mbar_try(mbar, parity))      // (which itself waits for some time)
+        if ((gave_up && *gave_up) || now_ns() > end) return false;
+    return true;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t mbar, uint32_t parity, const volatile int* gave_up) {
-    if (mbar_try(mbar, parity)) return true;
-    return mbar_wait_slow(mbar, parity, gave_up);
+__device__ __forceinline__ bool mbar_wait(uint32_t mbar, uint32_t parity, unsigned long long ns, const volatile int* gave_up) {
+    return __all_sync(~0u, mbar_try(mbar, parity) || mbar_wait_slow(mbar, parity, ns, gave_up));
+}
+
+// a word of the shared memory of another CTA of the cluster
+__device__ __forceinline__ uint32_t peer_word(uint32_t addr, uint32_t rank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(at_cta(addr, rank)) : "memory");
+    return v;
 }
 
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* m) {
@@ -507,6 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                    drain = tempty + 16;
     volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 5);
     uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 6);
+    uint32_t* count = reinterpret_cast<uint32_t*>(bars + 2 * NS + 7);      // stages that this CTA asked for
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const uint32_t base = smem_u32(sm);
@@ -522,6 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         }
         mbar_init(drain, 1);
         *gave_up = 0;
+        *count = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         for (int i = 0; i < 2; ++i) {
             tma_prefetch(&P.q[i].ma[0][0]);
@@ -566,11 +578,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
 
     // Whole warps walk the loops of the two issuing roles (uniform control flow is cheaper
     // than one lane's); one elected lane issues.
+    const bool issuer = elect_one();
+    int s = 0;                   // the issuing roles' next stage, its phase
+    uint32_t ph = 0;
+    bool issued = false;         // products
     if (warp == 0) {
-        const bool issuer = elect_one();
         const uint32_t full0 = CG == 2 ? at_cta(full, 0) : full;
-        int s = 0, used = 0;
-        uint32_t ph = 0;
+        uint32_t asked = 0;
         bool ok = true;
         for (int i = 0; ok && tile_of(P.plan, unit, i, which, t); ++i) {
             const Problem<kParts>& A = P.q[which];
@@ -599,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                         k0 = 0;
                         maps();
                     }
-                    if (!__all_sync(~0u, mbar_wait(empty + 8 * s, ph ^ 1, gave_up))) {
+                    if (!mbar_wait(empty + 8 * s, ph ^ 1, P.wait_ns, gave_up)) {
                         ok = false;
                         break;
                     }
@@ -623,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                             if (kGated && CG == 1) tma_load<CG>(sb + S::kStageB / 2, mb1, k0, n0, bar);
                         }
                     }
-                    used = used < NS ? used + 1 : NS;
+                    ++asked;
                     if (++s == NS) {
                         s = 0;
                         ph ^= 1;
@@ -639,21 +653,14 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             }
         }
         let_next();
-        if (!ok) {
-            if (issuer) give_up();
-            // copies still in flight land before this CTA's memory is given back: the
-            // last `used` stages, in the order of their issue
-            if (rank == 0)
-                for (int i = used; i > 0; --i) {
-                    const int q = (s - i + NS) % NS;
-                    mbar_wait(full + 8 * q, q < s ? ph : ph ^ 1, nullptr);
-                }
+        if (issuer) {
+            *count = asked;
+            if (!ok) give_up();
         }
     } else if (warp == 1 && rank == 0) {
-        const bool issuer = elect_one();
-        int s = 0, acc = 0;
-        uint32_t ph = 0, aph = 0;
-        bool ok = true, issued = false;
+        int acc = 0;
+        uint32_t aph = 0;
+        bool ok = true;
         for (int i = 0; ok && tile_of(P.plan, unit, i, which, t); ++i) {
             const Problem<kParts>& A = P.q[which];
             const TileAt T = tile_at(A, t);
@@ -665,13 +672,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             const int nb = A.kblocks;
             for (int from = kb0; ok && from < kb1;) {      // an accumulator's share: all, or a chunk
                 const int end = kSums ? chunk_end<kPairs>(from, kb1, nb) : kb1;
-                if (!__all_sync(~0u, mbar_wait(tempty + 8 * acc, aph ^ 1, gave_up))) {
+                if (!mbar_wait(tempty + 8 * acc, aph ^ 1, P.wait_ns, gave_up)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
                 for (int kb = from; kb < end; ++kb) {
-                    if (!__all_sync(~0u, mbar_wait(full + 8 * s, ph, gave_up))) {
+                    if (!mbar_wait(full + 8 * s, ph, P.wait_ns, gave_up)) {
                         ok = false;
                         break;
                     }
@@ -697,13 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 }
             }
         }
-        if (!ok) {
-            if (issuer) give_up();
-            if (issued) {   // products in flight finish before the tensor memory is freed
-                if (issuer) mma_commit<CG>(drain);
-                mbar_wait(drain, 0, nullptr);
-            }
-        }
+        if (!ok && issuer) give_up();
     } else if (warp >= 4) {
         const int quad = warp & 3, half = (warp - 4) >> 2;
         float* stage = staging + (warp - 4) * 2 * 32 * 17;
@@ -753,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 };
                 uint4 res[4] = {}, next[4] = {};
                 ask(first, next);
-                if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
+                if (!mbar_wait(tfull + 8 * acc, aph, P.wait_ns, gave_up)) {
                     if (lane == 0) give_up();
                     break;
                 }
@@ -791,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 const int kb0 = (int)((long long)kblocks * T.split / A.splits), kb1 = (int)((long long)kblocks * (T.split + 1) / A.splits);
                 bool ok = true;
                 for (int from = kb0; from < kb1; from = chunk_end<kPairs>(from, kb1, nb)) {
-                    if (!mbar_wait(tfull + 8 * acc, aph, gave_up)) {
+                    if (!mbar_wait(tfull + 8 * acc, aph, P.wait_ns, gave_up)) {
                         if (lane == 0) give_up();
                         ok = false;
                         break;
@@ -822,14 +823,45 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
             }
         }
     }
-    __syncwarp();
-    tc_fence_before();
-    __syncthreads();
-    if (CG == 2) {   // no CTA leaves while its partner may still signal it or read its memory
-        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    auto meet = [&]() {
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+        if (CG == 2) {   // no CTA leaves while its partner may still signal it or read its memory
+            asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        }
+        tc_fence_after();
+    };
+    meet();
+    if (*gave_up) {      // the same in both CTAs
+        if (warp == 1 && issued) {      // products in flight, of any role's giving up
+            if (issuer) mma_commit<CG>(drain);
+            mbar_wait(drain, 0, kWaitNs, nullptr);
+        }
+        // Copies in flight, of both CTAs, at the first one's barriers.  A pair's CTAs may have asked for
+        // a different number of stages (by NS at most: further ones wait for the products of both
+        // halves).  Stage j, counted from the first CTA's next one, is the last use of its place in
+        // the ring for each of the NS values of j.
+        if (warp == 0 && rank == 0) {
+            const uint32_t mine = *count;
+            const int ahead = CG == 2 ? (int)(peer_word(smem_u32(count), 1) - mine) : 0, last = max(ahead, 0);
+            for (int j = last - NS; j < last; ++j) {
+                if (j < 0 && mine < (uint32_t)-j) continue;       // never asked for
+                const int at = s + j, q = at < 0 ? at + NS : at >= NS ? at - NS : at;
+                const uint32_t bar = full + 8 * q;
+                if (CG == 2 && lane == 0) {
+                    if (j >= 0)              // the second CTA's half alone: its bytes are announced here
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(S::kStage) : "memory");
+                    else if (j >= ahead)     // the first CTA's half alone: the other's bytes never come
+                        asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(S::kStage) : "memory");
+                }
+                __syncwarp();
+                if (!mbar_wait(bar, at == q ? ph : ph ^ 1, kWaitNs, nullptr)) break;
+            }
+        }
+        meet();
     }
-    tc_fence_after();
     if (warp == 2) {
         if (CG == 2)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(S::kTmem) : "memory");
@@ -839,6 +871,16 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
 }
 
 __device__ unsigned g_layers_err;
+
+// Nanoseconds after which a wait gives up: VQC_WAIT_NS of the environment, or 4 s.
+unsigned long long wait_limit() {
+    static const unsigned long long ns = [] {
+        const char* v = std::getenv("VQC_WAIT_NS");
+        const unsigned long long given = v ? std::strtoull(v, nullptr, 10) : 0;
+        return given ? given : kWaitNs;
+    }();
+    return ns;
+}
 
 // Its address on the current device, looked up once per device.
 cudaError_t error_word(unsigned** p) {
@@ -1245,6 +1287,7 @@ template <int kParts> vqc_status run_parts(const Product* p, int count, void* co
     }
     if (count == 1) a.q[1] = a.q[0];
     a.bf16 = p[0].f.dtype != VQC_F16;
+    a.wait_ns = wait_limit();
     cudaError_t e = error_word(&a.err);
     if (e != cudaSuccess) return cuda_error(e, "cudaGetSymbolAddress");
     if constexpr (kParts == 3) {

@@ -358,3 +358,40 @@ def test_plain_stream_order_on_request():
     assert edges >= 3 and programmatic >= 1
     edges, programmatic = child(EDGES, VQC_PDL="0")
     assert edges >= 3 and programmatic == 0
+
+
+LIMIT = """
+import json, torch
+from paper_2607_11985_gb300 import binding as B, layers
+def ran_out():
+    try:
+        B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
+        return False
+    except B.VQCError as e:
+        assert B.STATUS[e.status] == "VQC_ERR_DEVICE_CHECK" and "timed out" in str(e), e
+        return True
+def matrix(rows, cols, dtype):
+    return torch.ones(rows, cols, dtype=dtype, device="cuda")
+seen = []
+for dtype, rows, out, inp in ((torch.bfloat16, 4096, 4096, 65536), (torch.float16, 2048, 1024, 65536),
+                              (torch.float32, 1024, 1024, 16384), (torch.bfloat16, 128, 64, 1 << 20)):
+    x, w = matrix(rows, inp, dtype), matrix(out, inp, dtype)
+    for call in (lambda: layers.linear_forward(x, w, save=False), lambda: layers.gated_forward(x, w, w, save=False),
+                 lambda: layers.linear_backward(matrix(rows, out, dtype), x, w, None, "none")):
+        call()
+        seen.append(ran_out())
+        # the device and the library go on: torch's kernels, and a product without such waits
+        assert float(x[:, 0].float().sum()) == rows
+        y = layers.linear_forward(x[:1, :64].contiguous(), w[:8, :64].contiguous(), save=False)
+        assert float(y.float().sum()) == 8 * 64 and not ran_out()
+print(json.dumps(seen))
+"""
+
+
+def test_waits_that_run_out_end_the_kernel_and_are_reported():
+    """With a limit of one microsecond the roles of the tensor-core products give up in the
+    middle of their work, with copies and products in flight: the kernel ends, the status
+    says so, and the device can be used as before."""
+    seen = child(LIMIT, VQC_WAIT_NS="1000")
+    assert len(seen) == 12 and sum(seen[:3]) == 3, seen
+    assert sum(child(LIMIT, VQC_WAIT_NS="4000000000")) == 0
