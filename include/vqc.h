@@ -400,7 +400,9 @@ vqc_status vqc_frames_export(const vqc_plan* plan, void* buf, size_t* inout_byte
  * stream-ordered and use no memory but their arguments; results do not depend
  * on timing (sums have a fixed order).  The tensor-core products wait for their own copies
  * inside the GPU; a wait that takes longer than 4 s, or the environment's VQC_WAIT_NS
- * nanoseconds, ends the kernel with its output incomplete (see vqc_sync_check).  A call whose workspace size is 0 may
+ * nanoseconds, ends the kernel with its output incomplete.  Every linear and gated call of the
+ * process on that device then returns VQC_ERR_DEVICE_CHECK and does nothing, until
+ * vqc_sync_check has reported it.  A call whose workspace size is 0 may
  * be given NULL.  Buffers must not overlap. */
 typedef enum { VQC_F32 = 0, VQC_BF16 = 1, VQC_F16 = 2 } vqc_real;
 

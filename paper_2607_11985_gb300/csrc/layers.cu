@@ -4,6 +4,7 @@
 #include <initializer_list>
 
 #include "layers.h"
+#include "layers_tc.h"
 
 namespace vqc {
 namespace layers {
@@ -116,6 +117,8 @@ vqc_status forward(const char* call, int dtype, int out_dtype, int64_t rows, int
     if (!on(x, e) || !on(w[0], e) || (gated && !on(w[1], e)) || !on(bias[0], e) || (gated && !on(bias[1], e)) ||
         !on(res, eo) || !on(y, 16) || !on(saved, 16) || !on(ws, 256))
         return bad(call, "misaligned operand, output or workspace");
+    const vqc_status before = layers_pending();
+    if (before != VQC_OK) return before;
     Product p = product_forward(dtype, out_dtype, rows, in, out, x, ld_x, w, ld_w, act, gated);
     p.f.bias[0] = bias[0];
     p.f.bias[1] = gated ? bias[1] : nullptr;
@@ -144,6 +147,8 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     if (!on(gy, eo) || !on(x, e) || !on(w[0], e) || (gated && !on(w[1], e)) || !on(saved, 4) || !on(gx, 16) ||
         !on(gw[0], 16) || (gated && !on(gw[1], 16)) || !on(gb[0], 16) || (gated && !on(gb[1], 16)) || !on(ws, 256))
         return bad(call, "misaligned operand, output or workspace");
+    const vqc_status before = layers_pending();
+    if (before != VQC_OK) return before;
     const bool aligned = on(x, 16) && on(w[0], 16) && (!gated || on(w[1], 16)) && on(gy, 16);
     const BackSpace b = back_space(dtype, out_dtype, rows, in, out, ld_x, ld_w, ld_gy, act, gated, aligned);
     if (ws_bytes < b.total || !ws) return set_error(VQC_ERR_WORKSPACE, std::string(call) + ": workspace too small");

@@ -44,6 +44,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdlib>
+#include <mutex>
 
 #include "layers_elem.cuh"
 #include "layers_tc.h"
@@ -573,7 +574,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
         if (CG == 2)
             asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"(at_cta(smem_u32((const void*)gave_up), rank ^ 1)), "r"(1)
                          : "memory");
-        atomicOr(P.err, 1u);
+        *static_cast<volatile unsigned*>(P.err) = 1u;       // (of the host)
+        __threadfence_system();
     };
 
     // Whole warps walk the loops of the two issuing roles (uniform control flow is cheaper
@@ -870,8 +872,6 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     }
 }
 
-__device__ unsigned g_layers_err;
-
 // Nanoseconds after which a wait gives up: VQC_WAIT_NS of the environment, or 4 s.
 unsigned long long wait_limit() {
     static const unsigned long long ns = [] {
@@ -882,20 +882,41 @@ unsigned long long wait_limit() {
     return ns;
 }
 
-// Its address on the current device, looked up once per device.
+// A word per device that a kernel sets when it gave up, in memory of the host, where every later call
+// looks at it for nothing.
+constexpr int kDevices = 64;
+std::atomic<unsigned*> g_words{nullptr};
+
 cudaError_t error_word(unsigned** p) {
-    static std::atomic<void*> known[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    void* q = dev < 64 ? known[dev].load() : nullptr;
-    if (!q) {
-        e = cudaGetSymbolAddress(&q, g_layers_err);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) known[dev].store(q);
+    if (dev >= kDevices) return cudaErrorInvalidDevice;
+    unsigned* words = g_words.load();
+    if (!words) {
+        static std::mutex mu;
+        std::lock_guard<std::mutex> lk(mu);
+        words = g_words.load();
+        if (!words) {
+            // (allowed while a stream is captured: nothing of it enters the graph)
+            cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+            cudaThreadExchangeStreamCaptureMode(&mode);
+            void* q = nullptr;
+            e = cudaHostAlloc(&q, kDevices * sizeof(unsigned), cudaHostAllocPortable | cudaHostAllocMapped);
+            cudaThreadExchangeStreamCaptureMode(&mode);
+            if (e != cudaSuccess) return e;
+            words = static_cast<unsigned*>(q);
+            std::fill(words, words + kDevices, 0u);
+            g_words.store(words);
+        }
     }
-    *p = static_cast<unsigned*>(q);
-    return cudaSuccess;
+    return cudaHostGetDevicePointer(reinterpret_cast<void**>(p), words + dev, 0);
+}
+// the current device's word as the host reads it, or NULL where no product has run
+volatile unsigned* host_word() {
+    unsigned* words = g_words.load();
+    int dev = 0;
+    return words && cudaGetDevice(&dev) == cudaSuccess && dev < kDevices ? words + dev : nullptr;
 }
 
 // A float as the sum of three bf16, 8 bits of it each: exact for normal results.  The six products
@@ -1332,14 +1353,19 @@ vqc_status tc_run(const Product* p, int count, void* const* ws, const size_t* by
 
 }  // namespace layers
 
-// vqc_sync_check's view of the tensor-core products' error word (read and cleared).
+// What an earlier product's wait left behind: reported to every call until vqc_sync_check has been told.
+vqc_status layers_pending() {
+    const volatile unsigned* w = layers::host_word();
+    if (!w || !*w) return VQC_OK;
+    return set_error(VQC_ERR_DEVICE_CHECK, "an earlier tensor-core product's wait timed out and its output is incomplete (vqc_sync_check "
+                                           "reports this and clears it)");
+}
+
+// vqc_sync_check's view of the error word (read and cleared).
 vqc_status layers_error_check() {
-    unsigned e = 0;
-    cudaError_t c = cudaMemcpyFromSymbol(&e, layers::g_layers_err, sizeof(e));
-    if (c != cudaSuccess) return set_error(VQC_ERR_CUDA, std::string("layers error word: ") + cudaGetErrorString(c));
-    if (!e) return VQC_OK;
-    const unsigned zero = 0;
-    cudaMemcpyToSymbol(layers::g_layers_err, &zero, sizeof(zero));
+    volatile unsigned* w = layers::host_word();
+    if (!w || !*w) return VQC_OK;
+    *w = 0;
     return set_error(VQC_ERR_DEVICE_CHECK, "a tensor-core product's wait timed out");
 }
 

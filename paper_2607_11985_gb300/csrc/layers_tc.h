@@ -19,5 +19,6 @@ vqc_status rows_run(const Product& p, bool aligned, cudaStream_t s);
 }  // namespace layers
 
 vqc_status layers_error_check();
+vqc_status layers_pending();
 
 }  // namespace vqc

@@ -20,7 +20,7 @@ import argparse
 
 import torch
 
-from . import layers, workloads as wl
+from . import binding as B, layers, workloads as wl
 from .circuit import Circuit
 
 
@@ -88,6 +88,7 @@ def train(width=256, qubits=6, batch=512, steps=40, rate=0.02, dtype=torch.bfloa
         opt.step()
         losses.append(loss.detach())
     losses = [float(v) for v in losses]
+    B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
     for step in range(0, steps, max(1, steps // 8)):
         say("step %3d  loss %.4f" % (step, losses[step]))
     say("step %3d  loss %.4f" % (steps - 1, losses[-1]))

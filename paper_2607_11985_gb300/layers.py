@@ -15,7 +15,8 @@ float32, bfloat16 and float16, sums and statistics in float; see include/vqc.h
 for the formulas and roundings.  Tensors are on the current device, work goes to
 its current stream.  Torch supplies device memory and the stream only.
 Arguments that do not fit raise ValueError, statuses of the library
-``binding.VQCError``.
+``binding.VQCError``.  A product whose waits ran out (VQC_WAIT_NS, 4 s) leaves its
+output incomplete: later calls raise until ``binding.vqc_sync_check`` has been told.
 
 A call on a few rows costs its host path, so the checks, the allocations and the
 calls of the C entry points are native (csrc/layers_torch.cpp, ``_layers.so``).

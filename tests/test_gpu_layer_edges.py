@@ -395,3 +395,41 @@ def test_waits_that_run_out_end_the_kernel_and_are_reported():
     seen = child(LIMIT, VQC_WAIT_NS="1000")
     assert len(seen) == 12 and sum(seen[:3]) == 3, seen
     assert sum(child(LIMIT, VQC_WAIT_NS="4000000000")) == 0
+
+
+REPORTED = """
+import json, torch
+from paper_2607_11985_gb300 import binding as B, layers
+x, w = torch.ones(4096, 65536, dtype=torch.bfloat16, device="cuda"), torch.ones(4096, 65536, dtype=torch.bfloat16, device="cuda")
+few = torch.ones(2, 64, dtype=torch.bfloat16, device="cuda").requires_grad_()
+small = torch.ones(8, 64, dtype=torch.bfloat16, device="cuda")
+y = layers.linear(few, small)
+layers.linear_forward(x, w, save=False)
+torch.cuda.synchronize()
+def status(call):
+    try:
+        call()
+        return "VQC_OK"
+    except B.VQCError as e:
+        return B.STATUS[e.status]
+def backward():
+    try:
+        torch.autograd.grad(y, few, torch.ones_like(y), retain_graph=True)
+        return "VQC_OK"
+    except RuntimeError as e:
+        return "timed out" if "timed out" in str(e) else str(e)
+calls = [lambda: layers.linear_forward(few.detach(), small), lambda: layers.gated_forward(few.detach(), small, small),
+         lambda: layers.linear(few, small), lambda: layers.linear_backward(y.detach(), few.detach(), small, None),
+         lambda: B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)]
+before, during = [status(c) for c in calls[:4]], backward()
+told = [status(calls[4]) for _ in range(2)]
+print(json.dumps([before, during, told, status(calls[0]), status(calls[2])]))
+"""
+
+
+def test_a_wait_that_ran_out_is_reported_by_later_calls():
+    """Nobody needs to ask: calls after the one whose wait ran out raise, under autograd too,
+    until vqc_sync_check has reported it, once."""
+    before, during, told, one, two = child(REPORTED, VQC_WAIT_NS="1000")
+    assert before == ["VQC_ERR_DEVICE_CHECK"] * 4 and during == "timed out"
+    assert told == ["VQC_ERR_DEVICE_CHECK", "VQC_OK"] and one == two == "VQC_OK"
