@@ -165,10 +165,13 @@ template <bool kFull> __device__ __forceinline__ float2 act_both(int act, float 
 template <int W>
 __device__ __forceinline__ void finish_some(const Finish& f, int which, int64_t row, int64_t col, float (&v)[W], float (&u)[W]) {
     const int64_t at = row * f.n + col;
-    const float scale = f.scale ? *f.scale : 1.f;
+    if (f.scale) {
+        const float scale = *f.scale;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] *= scale;
+    }
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        v[i] *= scale;
         if (f.bias[which]) v[i] += load_as(f.bias[which], f.dtype, col + i);
         if (f.gated && f.bias[1]) u[i] += load_as(f.bias[1], f.dtype, col + i);
     }

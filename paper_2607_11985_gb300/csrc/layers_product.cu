@@ -282,7 +282,7 @@ __device__ __forceinline__ void join_row(const Join& j, int which, int64_t strid
         __syncthreads();
     }
 }
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Joins J) {
+__global__ void __launch_bounds__(256, 2) join_kernel(const __grid_constant__ Joins J) {
     stream_order();
     const Join& j = J.j[blockIdx.y >> 1];
     const int which = blockIdx.y & 1;
@@ -508,20 +508,20 @@ template <typename T> __device__ __forceinline__ float next_part(float& rest, bo
     return h;
 }
 
-template <typename T, bool VEC> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        if (A.second) {
+// THREE: as three parts, A.second elements apart.  (A kernel of its own: with that code beside it the loop of
+// the one-matrix form keeps fewer loads in flight, 14.5 against 13.1 us for 8192 x 2048.)
+template <typename T, bool VEC, bool THREE> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
+    if constexpr (THREE) {
 #pragma unroll 1
-            for (int part = 0; part < 3; ++part) {
-                float h[8];
+        for (int part = 0; part < 3; ++part) {
+            float h[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = next_part<T>(v[e], part == 2);
-                store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, h);
-            }
-            return;
+            for (int e = 0; e < 8; ++e) h[e] = next_part<T>(v[e], part == 2);
+            store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, h);
         }
+    } else {
+        store8<T, VEC>(A.dz[i], row, c, A.n, v);
     }
-    store8<T, VEC>(A.dz[i], row, c, A.n, v);
 }
 
 // the largest of |v| that is finite, and `top`
@@ -532,7 +532,7 @@ __device__ __forceinline__ float top_of(float top, const float (&v)[8]) {
     return top;
 }
 
-template <typename T, bool VEC, int ACT, bool GATE>
+template <typename T, bool VEC, int ACT, bool GATE, bool THREE>
 __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
     constexpr bool kScaled = std::is_same<T, __half>::value;
     const float scale = kScaled && A.scale && A.dz[0] ? A.scale[0] : 1.f;
@@ -570,25 +570,25 @@ __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int6
                 if (GATE) top = top_of(top, u);
             }
         }
-        if (A.dz[0]) store_dz<T, VEC>(A, 0, q * A.ld_dz, c, d);
-        if (GATE && A.dz[0]) store_dz<T, VEC>(A, 1, q * A.ld_dz, c, u);
+        if (A.dz[0]) store_dz<T, VEC, THREE>(A, 0, q * A.ld_dz, c, d);
+        if (GATE && A.dz[0]) store_dz<T, VEC, THREE>(A, 1, q * A.ld_dz, c, u);
     }
 }
-template <typename T, bool VEC, bool GATE>
+template <typename T, bool VEC, bool GATE, bool THREE>
 __device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
     switch (A.act) {
-        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE>(A, r0, r1, c, s0, s1, top);
-        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE, THREE>(A, r0, r1, c, s0, s1, top);
     }
 }
 
 // CTAs per SM: by the registers
 constexpr int grad_ctas(bool gate) { return gate ? 3 : 4; }
-template <typename T, bool VEC, bool GATE>
+template <typename T, bool VEC, bool GATE, bool THREE>
 __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, float* tops, int64_t per) {
     __shared__ float sums[8][kGradCols];
     stream_order();
@@ -598,10 +598,10 @@ __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __
     float s0[8] = {}, s1[8] = {}, top = 0.f;
     if (c < A.n) {
         const int64_t r0 = block * per + warp, r1 = min(A.rows, (block + 1) * per);
-        act_grad_as<T, VEC, GATE>(A, r0, r1, c, s0, s1, top);
+        act_grad_as<T, VEC, GATE, THREE>(A, r0, r1, c, s0, s1, top);
     }
     let_next();
-    if (tops) {       // the CTA's largest magnitude
+    if (std::is_same<T, __half>::value && tops) {       // the CTA's largest magnitude
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
         if (lane == 0) sums[0][warp] = top;
@@ -675,10 +675,11 @@ int64_t grad_rows(int64_t rows, int64_t n, bool gate) {
     const int64_t want = ceil_div(rows * ceil_div(n, kGradCols), (int64_t)grad_ctas(gate) * sm_count());
     return std::min<int64_t>(256, std::max<int64_t>(16, (want + 7) / 8 * 8));
 }
-template <bool VEC, bool GATE> const void* grad_kernel(int dtype) {
-    return dtype == VQC_F32    ? (const void*)act_grad_kernel<float, VEC, GATE>
-           : dtype == VQC_BF16 ? (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE>
-                               : (const void*)act_grad_kernel<__half, VEC, GATE>;
+template <bool VEC, bool GATE> const void* grad_kernel(int dtype, bool three) {
+    if (dtype == VQC_F32) return (const void*)act_grad_kernel<float, VEC, GATE, false>;
+    if (dtype == VQC_BF16)
+        return three ? (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, true> : (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, false>;
+    return three ? (const void*)act_grad_kernel<__half, VEC, GATE, true> : (const void*)act_grad_kernel<__half, VEC, GATE, false>;
 }
 
 }  // namespace
@@ -716,8 +717,10 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
         const bool vec = a.n % 8 == 0 && a.ld_gy % 8 == 0 && aligned_to(a.gy, 16) && aligned_to(a.z[0], 16) && aligned_to(a.z[1], 16);
         float* tops = nullptr;
         void* args[] = {&a, &part, &tops, &per};
-        const void* fn = vec ? (a.gated ? grad_kernel<true, true>(a.dtype) : grad_kernel<true, false>(a.dtype))
-                             : (a.gated ? grad_kernel<false, true>(a.dtype) : grad_kernel<false, false>(a.dtype));
+        auto kernel = [&](bool three) {
+            return vec ? (a.gated ? grad_kernel<true, true>(a.dtype, three) : grad_kernel<true, false>(a.dtype, three))
+                       : (a.gated ? grad_kernel<false, true>(a.dtype, three) : grad_kernel<false, false>(a.dtype, three));
+        };
         if (a.scale) {
             // float16 holds 2^-24 to 65504 only, and dz is an operand, not a result: what is small in
             // it counts in sums over many rows, and what is large (from a float32 grad_y) may meet small weights.
@@ -727,7 +730,7 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
             // training in float16 looks for.
             tops = reinterpret_cast<float*>(static_cast<char*>(ws) + grad_sums_bytes(a.rows, a.n, a.gated));
             a.dz[0] = a.dz[1] = nullptr;
-            cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
+            cudaError_t e = launch(kernel(false), dim3((unsigned)grid), 256, args, s);
             if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
             int up = a.gy_dtype == VQC_F16;
             void* of[] = {&tops, &grid, &up, &a.scale};
@@ -738,7 +741,7 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
             part = nullptr;
             tops = nullptr;
         }
-        const cudaError_t e = launch(fn, dim3((unsigned)grid), 256, args, s);
+        const cudaError_t e = launch(kernel(a.dz[0] && a.second), dim3((unsigned)grid), 256, args, s);
         if (e != cudaSuccess) return cuda_error(e, "activation gradient launch");
     }
     if (!sums) return VQC_OK;

@@ -56,6 +56,10 @@ std::string told(const Tensor& t) {
 
 bool here(const Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
 
+// A view that torch negates when it reads it, so read.  (Asking torch to resolve it is a call through the
+// dispatcher, 0.7 us a tensor: only where it is one.)
+Tensor as_read(const Tensor& t) { return t.is_neg() ? t.resolve_neg() : t; }
+
 // Every operand comes by here: a tangent, which no operator carries on, is refused, not dropped.
 void no_tangent(const Tensor& t, const char* name) {
     if (t._fw_grad(0).defined())
@@ -76,7 +80,7 @@ Matrix matrix(const Tensor& given, const char* name) {
     const int64_t cols = given.size(given.dim() - 1);
     if (cols < 1) throw Refused(std::string(name) + " must have at least one column (got " + told(given) + ")");
     no_tangent(given, name);
-    Matrix m{given.resolve_neg(), 0, cols, cols, code};      // (a view that torch negates when it reads it)
+    Matrix m{as_read(given), 0, cols, cols, code};
     if (given.dim() != 2) m.t = m.t.reshape({-1, cols});
     m.rows = m.t.size(0);
     if (m.t.is_contiguous()) return m;
@@ -103,7 +107,7 @@ Tensor vector(const Tensor& given, int64_t n, int code, const char* name) {
         throw Refused(std::string(name) + " must be a CUDA " + c10::toString(type_of(code)) + " tensor of " + std::to_string(n) +
                       " elements on the current device (got " + told(given) + ")");
     no_tangent(given, name);
-    return given.resolve_neg().contiguous();
+    return as_read(given).contiguous();
 }
 const float* saved_of(const Tensor& t, at::IntArrayRef shape) {
     if (!t.defined() || t.is_neg() || t.sizes() != shape || t.scalar_type() != at::kFloat || !t.is_contiguous() || !here(t))
