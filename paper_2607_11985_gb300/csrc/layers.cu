@@ -182,13 +182,19 @@ vqc_status backward(const char* call, int dtype, int out_dtype, int64_t rows, in
     int count = 0;
     if (gx) {
         p[count] = product_gx(dtype, rows, in, out, dz, b.ld_dz, b.second, w, ld_w, gated, gx);
-        p[count].f.scale = g.scale ? g.scale + 1 : nullptr;
+        if (g.scale) {
+            p[count].f.scale = g.scale + 1;
+            p[count].f.act = kActScale;
+        }
         spaces[count] = at;
         bytes[count++] = b.gx;
     }
     if (gw[0]) {
         p[count] = product_gw(dtype, rows, in, out, dz, b.ld_dz, b.second, x, ld_x, gated, gw);
-        p[count].f.scale = g.scale ? g.scale + 1 : nullptr;
+        if (g.scale) {
+            p[count].f.scale = g.scale + 1;
+            p[count].f.act = kActScale;
+        }
         spaces[count] = at + b.gx;
         bytes[count++] = b.gw;
     }

@@ -50,9 +50,12 @@ enum Form {
     GATED = 3    // y0 = act(a0 b0^T + bias0) * (a0 b1^T + bias1)
 };
 
+// In the place of an activation: times *scale.
+constexpr int kActScale = VQC_ACT_SIGMOID + 1;
+
 // What is done with the sums of a product before they are written.
 struct Finish {
-    const float* scale;    // what they are multiplied by first, or NULL
+    const float* scale;    // of kActScale
     const void* bias[2];   // per column, of the operands' type, or NULL
     const void* res;       // added last, of y's type, or NULL
     int64_t ld_res;

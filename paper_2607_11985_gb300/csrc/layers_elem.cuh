@@ -165,11 +165,6 @@ template <bool kFull> __device__ __forceinline__ float2 act_both(int act, float 
 template <int W>
 __device__ __forceinline__ void finish_some(const Finish& f, int which, int64_t row, int64_t col, float (&v)[W], float (&u)[W]) {
     const int64_t at = row * f.n + col;
-    if (f.scale) {
-        const float scale = *f.scale;
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] *= scale;
-    }
 #pragma unroll
     for (int i = 0; i < W; ++i) {
         if (f.bias[which]) v[i] += load_as(f.bias[which], f.dtype, col + i);
@@ -186,7 +181,7 @@ __device__ __forceinline__ void finish_some(const Finish& f, int which, int64_t 
     }
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        v[i] = act_value<true>(f.act, v[i]);
+        v[i] = f.act == kActScale ? v[i] * *f.scale : act_value<true>(f.act, v[i]);
         if (f.gated) v[i] *= u[i];
         if (f.res) v[i] += load_as(f.res, f.out_dtype, row * f.ld_res + col + i);
     }

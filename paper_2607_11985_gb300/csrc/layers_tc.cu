@@ -356,8 +356,9 @@ template <int ACT, bool kFull> __device__ __forceinline__ void act16_as(float (&
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = act_value<kFull>(ACT, v[i]);
 }
-template <bool kFull> __device__ __forceinline__ void act16(int act, float (&v)[16]) {
-    switch (act) {
+template <bool kFull> __device__ __forceinline__ void act16(const Finish& f, float (&v)[16]) {
+    switch (f.act) {
+        case kActScale: return scale16(*f.scale, v);
         case VQC_ACT_RELU: return act16_as<VQC_ACT_RELU, kFull>(v);
         case VQC_ACT_GELU: return act16_as<VQC_ACT_GELU, kFull>(v);
         case VQC_ACT_SILU: return act16_as<VQC_ACT_SILU, kFull>(v);
@@ -427,7 +428,6 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
         }
         return;
     }
-    if (!kGated && f.scale) scale16(*f.scale, v);
     if (f.bias[T.which]) add_bias(bias, v);
     if (kGated && f.bias[1]) add_bias(bias + kBiasUp, u);
 #pragma unroll
@@ -437,7 +437,7 @@ __device__ __forceinline__ void write16(const Problem<kParts>& A, const TileAt& 
         if (vec) floats_out(stage, w ? u : v, z + row0 * n + col0, n, rows, lane);
         else turned(w ? u : v, row0, col0, f.m, n, lane, stage, [&](int64_t r, int64_t c, float x) { z[r * n + c] = x; });
     }
-    act16<kSums>(f.act, v);
+    act16<kSums>(f, v);
     if (kGated) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] *= u[i];
@@ -470,12 +470,11 @@ __device__ __forceinline__ void write32(const Problem<kParts>& A, const TileAt& 
     uint4* pieces = reinterpret_cast<uint4*>(stage);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        if (!kGated && f.scale) scale16(*f.scale, v[h]);
         if (f.bias[T.which]) add_bias(bias + 16 * h, v[h]);
         if (kGated && f.bias[1]) add_bias(bias + kBiasUp + 16 * h, u[h]);
         if (f.z[T.which]) floats_out(stage, v[h], f.z[T.which] + at + 16 * h, n, rows, lane);
         if (kGated && f.z[1]) floats_out(stage, u[h], f.z[1] + at + 16 * h, n, rows, lane);
-        act16<false>(f.act, v[h]);      // (16-bit outputs)
+        act16<false>(f, v[h]);      // (16-bit outputs)
         if (kGated) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[h][i] *= u[h][i];
