@@ -462,7 +462,7 @@ vqc_status vqc_linear_forward(vqc_real dtype, vqc_real out_dtype, int64_t rows, 
 
 /* Gradients of vqc_linear_forward.  dz = grad_y * act'(z), rounded to dtype
  * where that is a 16-bit type (the operand of the two products below; where these
- * are small, up to 6e9 operations, dz is held as the sum of three values of dtype; a
+ * are small, up to 6e9 operations, dz is held as the sum of two values of dtype; a
  * VQC_F16 dz is held times a power of two that brings its largest value near 2^15, which
  * the gradients are divided by again, but not less than 1 where grad_y is VQC_F16: there a
  * dz beyond 65504 is infinite);

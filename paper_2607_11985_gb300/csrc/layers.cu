@@ -29,11 +29,14 @@ bool on(const void* p, size_t a) { return aligned_to(p, a); }
 
 // Space of a backward call: dz (and du), then the column sums, then the products.
 // Rounding dz to 16 bits adds its own error to the gradients' (1.4 of one rounding
-// together).  Where the products are short of work, in time a launch or two, dz
-// is therefore the sum of three 16-bit matrices, which hold all bits of a float, and the gradients
-// have the error of their one rounding (two bfloat16 matrices hold 16 to 18 bits: one gradient in
-// 4000 rounded the other way); above that the further matrices would cost their products: 8192 x
-// 2048 x 2048, both gradients, 74 us for one matrix.
+// together).  Where the products are short of work dz is therefore the sum of two 16-bit
+// matrices (16 bits of dz in bfloat16, 22 in float16) and the gradients have the error of their one
+// rounding, for 10 us at most.  Both gradients, bfloat16, us with one matrix and with two, by
+// operations: 0.4e9 (8192 x 1024 to 12) 26.6 and 29.0; 4.3e9 (1024^3) 14.2 and 18.8, gated (777 x 504
+// to 1365) 25.6 and 35.0; 5.7e9 (1024 x 1024 to 1365) 18.4 and 28.5; 8.6e9 (2048 x 1024 to 1024) 18.6 and 26.0;
+// 17e9 (4096 x 1024 to 1024) 26.8 and 45.4; 24e9 (gated, 1024 x 1024 to 2816) 32.7 and 53.2; from
+// there on the second costs its products, near half of the call.  A third matrix would hold all bits of
+// a bfloat16 dz and round one gradient in 1000 the other way, for 7 to 13 us more.
 // A float16 dz is stored times a power of two, so that its range does not matter (see act_grad_run).
 struct BackSpace {
     int64_t ld_dz, second;
@@ -88,9 +91,9 @@ BackSpace back_space(int dtype, int out_dtype, int64_t rows, int64_t in, int64_t
     BackSpace b{};
     b.own_dz = gated || act != VQC_ACT_NONE || dtype != out_dtype;
     b.ld_dz = b.own_dz ? (out + 7) / 8 * 8 : ld_gy;
-    const bool three = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
-    b.second = three ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
-    b.dz = b.own_dz ? align256((size_t)(three ? 3 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
+    const bool two = b.own_dz && dtype != VQC_F32 && 4.0 * rows * in * out * (gated ? 2 : 1) <= 6e9;
+    b.second = two ? (rows * b.ld_dz + 127) / 128 * 128 : 0;
+    b.dz = b.own_dz ? align256((size_t)(two ? 2 * b.second : rows * b.ld_dz) * elem_size(dtype)) : 0;
     b.scale = b.own_dz && dtype == VQC_F16 ? 256 : 0;
     b.sums = act_grad_workspace(rows, out, gated, b.scale > 0);
     const void* none[2] = {nullptr, nullptr};

@@ -34,8 +34,8 @@ int sm_count();   // of the current device (the GB300's 152 where there is none)
 
 // A matrix operand of a product: element (i, k) of the outer index i and the
 // contracted index k is p[i * ld + k], or p[k * ld + i] where k_outer is set.
-// A 16-bit operand may be the sum of three matrices, each `second` elements behind the
-// one before (0: there is one).
+// A 16-bit operand may be the sum of two matrices, the second `second` elements behind
+// the first (0: there is none).
 struct Operand {
     const void* p;
     int64_t ld;
@@ -103,7 +103,7 @@ struct ActGrad {
     const float* z[2];       // dense [rows, n]; z[0] may be NULL without an activation
     void* dz[2];             // of dtype, rows ld_dz apart, or NULL
     int64_t ld_dz;
-    int64_t second;          // what the rounding to dtype leaves goes this many elements behind dz, what is left then as far again (0: nowhere)
+    int64_t second;          // a second part, what the first leaves of dz, goes this many elements behind it (0: there is none)
     void* sum[2];            // [n] of dtype: column sums, or NULL
     float* scale;            // [2] of float16: dz is stored times scale[0], a power of two, and scale[1] = 1 / scale[0]; or NULL
     int64_t rows, n;

@@ -492,33 +492,28 @@ template <> struct Cut<__half> {
     static __device__ __forceinline__ float least() { return 5.9604644775390625e-8f; }
 };
 
-// The next of the three parts that add up to a value; `rest` becomes what is left.  Every part of a
-// value other than zero has its sign and is not zero itself, so that a factor that is
-// infinite makes the one infinity of all their products (zero or the other sign would make
-// it NaN).  Where the value ends early a part gives one unit to the next; what the smallest
-// values of T add is a few of these.  All parts of an infinity or NaN are that.
-template <typename T> __device__ __forceinline__ float next_part(float& rest, bool last) {
-    const float near = to_f(from_f<T>(rest));
-    if (rest == 0.f || !(fabsf(near) <= 3.4028234e38f)) return rest;
-    float h = last ? near : Cut<T>::cut(rest);
-    if (!last && h == rest) h = Cut<T>::before(h);
-    if (h == 0.f) h = copysignf(Cut<T>::least(), rest);
-    const float left = fabsf(rest) - fabsf(h);
-    rest = copysignf(left > 0.f ? left : 1.4e-45f, rest);
+// The first of the two parts that add up to a value; v becomes the second.  Both parts of a
+// value other than zero have its sign and are not zero themselves, so that a factor that is
+// infinite makes the one infinity of their products (zero or the other sign would make it
+// NaN): the first is cut, and gives one unit to the second where nothing would be left.  What the
+// smallest values of T add is a few of these.  Both parts of an infinity or NaN are that.
+template <typename T> __device__ __forceinline__ float first_part(float& v) {
+    if (v == 0.f || !(fabsf(to_f(from_f<T>(v))) <= 3.4028234e38f)) return v;
+    float h = Cut<T>::cut(v);
+    if (h == v) h = Cut<T>::before(h);
+    if (h == 0.f) h = copysignf(Cut<T>::least(), v);
+    v = copysignf(fmaxf(fabsf(v) - fabsf(h), Cut<T>::least()), v);
     return h;
 }
 
-// THREE: as three parts, A.second elements apart.  (A kernel of its own: with that code beside it the loop of
-// the one-matrix form keeps fewer loads in flight, 14.5 against 13.1 us for 8192 x 2048.)
-template <typename T, bool VEC, bool THREE> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
-    if constexpr (THREE) {
-#pragma unroll 1
-        for (int part = 0; part < 3; ++part) {
-            float h[8];
+// TWO: as two parts, the second A.second elements behind the first
+template <typename T, bool VEC, bool TWO> __device__ __forceinline__ void store_dz(const ActGrad& A, int i, int64_t row, int64_t c, float (&v)[8]) {
+    if constexpr (TWO) {
+        float h[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = next_part<T>(v[e], part == 2);
-            store8<T, VEC>(A.dz[i], row + part * A.second, c, A.n, h);
-        }
+        for (int e = 0; e < 8; ++e) h[e] = first_part<T>(v[e]);
+        store8<T, VEC>(A.dz[i], row, c, A.n, h);
+        store8<T, VEC>(A.dz[i], row + A.second, c, A.n, v);
     } else {
         store8<T, VEC>(A.dz[i], row, c, A.n, v);
     }
@@ -532,7 +527,7 @@ __device__ __forceinline__ float top_of(float top, const float (&v)[8]) {
     return top;
 }
 
-template <typename T, bool VEC, int ACT, bool GATE, bool THREE>
+template <typename T, bool VEC, int ACT, bool GATE, bool TWO>
 __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
     constexpr bool kScaled = std::is_same<T, __half>::value;
     const float scale = kScaled && A.scale && A.dz[0] ? A.scale[0] : 1.f;
@@ -570,25 +565,25 @@ __device__ __forceinline__ void act_grad_rows(const ActGrad& A, int64_t r0, int6
                 if (GATE) top = top_of(top, u);
             }
         }
-        if (A.dz[0]) store_dz<T, VEC, THREE>(A, 0, q * A.ld_dz, c, d);
-        if (GATE && A.dz[0]) store_dz<T, VEC, THREE>(A, 1, q * A.ld_dz, c, u);
+        if (A.dz[0]) store_dz<T, VEC, TWO>(A, 0, q * A.ld_dz, c, d);
+        if (GATE && A.dz[0]) store_dz<T, VEC, TWO>(A, 1, q * A.ld_dz, c, u);
     }
 }
-template <typename T, bool VEC, bool GATE, bool THREE>
+template <typename T, bool VEC, bool GATE, bool TWO>
 __device__ __forceinline__ void act_grad_as(const ActGrad& A, int64_t r0, int64_t r1, int64_t c, float (&s0)[8], float (&s1)[8], float& top) {
     switch (A.act) {
-        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE, THREE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE, THREE>(A, r0, r1, c, s0, s1, top);
-        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE, THREE>(A, r0, r1, c, s0, s1, top);
-        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_RELU: return act_grad_rows<T, VEC, VQC_ACT_RELU, GATE, TWO>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_GELU: return act_grad_rows<T, VEC, VQC_ACT_GELU, GATE, TWO>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SILU: return act_grad_rows<T, VEC, VQC_ACT_SILU, GATE, TWO>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_TANH: return act_grad_rows<T, VEC, VQC_ACT_TANH, GATE, TWO>(A, r0, r1, c, s0, s1, top);
+        case VQC_ACT_SIGMOID: return act_grad_rows<T, VEC, VQC_ACT_SIGMOID, GATE, TWO>(A, r0, r1, c, s0, s1, top);
+        default: return act_grad_rows<T, VEC, VQC_ACT_NONE, GATE, TWO>(A, r0, r1, c, s0, s1, top);
     }
 }
 
 // CTAs per SM: by the registers
 constexpr int grad_ctas(bool gate) { return gate ? 3 : 4; }
-template <typename T, bool VEC, bool GATE, bool THREE>
+template <typename T, bool VEC, bool GATE, bool TWO>
 __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __grid_constant__ ActGrad A, float* part, float* tops, int64_t per) {
     __shared__ float sums[8][kGradCols];
     stream_order();
@@ -598,7 +593,7 @@ __global__ void __launch_bounds__(256, grad_ctas(GATE)) act_grad_kernel(const __
     float s0[8] = {}, s1[8] = {}, top = 0.f;
     if (c < A.n) {
         const int64_t r0 = block * per + warp, r1 = min(A.rows, (block + 1) * per);
-        act_grad_as<T, VEC, GATE, THREE>(A, r0, r1, c, s0, s1, top);
+        act_grad_as<T, VEC, GATE, TWO>(A, r0, r1, c, s0, s1, top);
     }
     let_next();
     if (std::is_same<T, __half>::value && tops) {       // the CTA's largest magnitude
@@ -675,11 +670,11 @@ int64_t grad_rows(int64_t rows, int64_t n, bool gate) {
     const int64_t want = ceil_div(rows * ceil_div(n, kGradCols), (int64_t)grad_ctas(gate) * sm_count());
     return std::min<int64_t>(256, std::max<int64_t>(16, (want + 7) / 8 * 8));
 }
-template <bool VEC, bool GATE> const void* grad_kernel(int dtype, bool three) {
+template <bool VEC, bool GATE> const void* grad_kernel(int dtype, bool two) {
     if (dtype == VQC_F32) return (const void*)act_grad_kernel<float, VEC, GATE, false>;
     if (dtype == VQC_BF16)
-        return three ? (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, true> : (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, false>;
-    return three ? (const void*)act_grad_kernel<__half, VEC, GATE, true> : (const void*)act_grad_kernel<__half, VEC, GATE, false>;
+        return two ? (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, true> : (const void*)act_grad_kernel<__nv_bfloat16, VEC, GATE, false>;
+    return two ? (const void*)act_grad_kernel<__half, VEC, GATE, true> : (const void*)act_grad_kernel<__half, VEC, GATE, false>;
 }
 
 }  // namespace
@@ -717,9 +712,9 @@ vqc_status act_grad_run(const ActGrad& a0, void* ws, size_t ws_bytes, Joins& joi
         const bool vec = a.n % 8 == 0 && a.ld_gy % 8 == 0 && aligned_to(a.gy, 16) && aligned_to(a.z[0], 16) && aligned_to(a.z[1], 16);
         float* tops = nullptr;
         void* args[] = {&a, &part, &tops, &per};
-        auto kernel = [&](bool three) {
-            return vec ? (a.gated ? grad_kernel<true, true>(a.dtype, three) : grad_kernel<true, false>(a.dtype, three))
-                       : (a.gated ? grad_kernel<false, true>(a.dtype, three) : grad_kernel<false, false>(a.dtype, three));
+        auto kernel = [&](bool two) {
+            return vec ? (a.gated ? grad_kernel<true, true>(a.dtype, two) : grad_kernel<true, false>(a.dtype, two))
+                       : (a.gated ? grad_kernel<false, true>(a.dtype, two) : grad_kernel<false, false>(a.dtype, two));
         };
         if (a.scale) {
             // float16 holds 2^-24 to 65504 only, and dz is an operand, not a result: what is small in

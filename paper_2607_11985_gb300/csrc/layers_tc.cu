@@ -70,11 +70,11 @@ template <int CG, int BN> struct Shape {
     static constexpr int kTmem = 2 * BN;             // two accumulators, a power of two >= 32
 };
 
-// One product; maps of its operands: [operand][part].  kParts: 1, or 3: three of each of
-// float operands, or 2: three of a (float values as 16-bit matrices), one of b.
+// One product; maps of its operands: [operand][part].  kParts: 1, or 3 of float
+// operands, or 2: two of a (one 16-bit matrix and what it leaves), one of b.
 template <int kParts> struct Problem {
-    static constexpr int kPartsA = kParts == 1 ? 1 : 3, kPartsB = kParts == 3 ? 3 : 1;
-    CUtensorMap ma[2][kPartsA], mb[2][kPartsB];
+    static constexpr int kPartsB = kParts == 2 ? 1 : kParts;
+    CUtensorMap ma[2][kParts], mb[2][kPartsB];
     Finish f;
     float* part;                // sums of a cut contraction, or NULL
     int form, splits, tiles_m, tiles_n, kblocks, a_mn, b_mn, vec;   // vec: bytes of a store
@@ -110,7 +110,7 @@ template <int kParts> struct TcArgs {
     int bf16;
 };
 
-constexpr int pairs_of(int parts) { return parts == 3 ? 6 : parts == 2 ? 3 : 1; }
+constexpr int pairs_of(int parts) { return parts == 3 ? 6 : parts; }
 // Products of parts of float operands, small ones first: parts of a and b, 2 bits each.
 constexpr unsigned kOrderA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 constexpr unsigned kOrderB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
                 const CUtensorMap *ma, *mb, *mb1;
                 auto maps = [&]() {
                     const int sum = term >= kPairs ? 1 : 0, pair = term - sum * kPairs;
-                    const int pa = kParts == 3 ? kOrderA >> (2 * pair) & 3 : kParts == 2 ? 2 - pair : 0;
+                    const int pa = kParts == 3 ? kOrderA >> (2 * pair) & 3 : kParts == 2 ? 1 - pair : 0;
                     const int pb = kParts == 3 ? kOrderB >> (2 * pair) & 3 : 0;
                     ma = &A.ma[T.which + sum][pa];
                     mb = &A.mb[kGated ? (int)rank : T.which + sum][pb];
@@ -1236,7 +1236,7 @@ template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c,
             const Operand& o = (side ? r.b : r.a)[i];
             const int64_t outer = side ? p.n : p.m, rows = o.k_outer ? p.k : outer;
             const int box = side ? (gated ? c.bn / 2 : c.bn / c.cg) : BM;
-            for (int q = 0; q < (side ? Problem<kParts>::kPartsB : Problem<kParts>::kPartsA); ++q) {
+            for (int q = 0; q < (side ? Problem<kParts>::kPartsB : kParts); ++q) {
                 Operand part = o;
                 part.p = static_cast<const uint16_t*>(o.p) + q * (kParts == 2 ? o.second : rows * o.ld);
                 if (!make_map(side ? &a.mb[i][q] : &a.ma[i][q], part, p.f.dtype, outer, p.k, box))
@@ -1244,7 +1244,7 @@ template <int kParts> vqc_status fill_problem(const Product& p, const Choice& c,
             }
         }
     // an operand of both products
-    for (int q = 0; q < Problem<kParts>::kPartsA && na == 1; ++q) a.ma[1][q] = a.ma[0][q];
+    for (int q = 0; q < kParts && na == 1; ++q) a.ma[1][q] = a.ma[0][q];
     for (int q = 0; q < Problem<kParts>::kPartsB && nb == 1; ++q) a.mb[1][q] = a.mb[0][q];
     if (splits < 1 || splits > depth_of(p)) return set_error(VQC_ERR_DEVICE_CHECK, "product: more cuts than blocks");   // a tile with nothing to add
     a.f = p.f;

@@ -78,12 +78,14 @@ def same_infinities(got, want, what):
 @pytest.mark.parametrize("rows,inp,out", [(512, 1024, 4), (8, 1000, 600)])
 def test_gradients_of_float_outputs_round_once(layers, dtype, rows, inp, out):
     """dz is grad_y itself here, a float32 matrix: the gradients are its products in float
-    sums, rounded once, so that no bit of dz is missing."""
+    sums, rounded once.  dz is held in two parts, to 2^-16 in bfloat16 (the first is cut to 8 bits, the
+    second rounded to 8) and to 2^-22 in float16."""
     x, w, gy = normal(1, rows, inp, dtype=dtype), normal(2, out, inp, dtype=dtype), normal(3, rows, out)
     gx, gw, _ = layers.linear_backward(gy.cuda(), x.cuda(), w.cuda(), None, "none")
     sync()
-    once(gx, gy.double(), w.double(), dtype, "gx")
-    once(gw, gy.double().t(), x.double(), dtype, "gw")
+    held = 2.0 ** (-16 if dtype == BF16 else -22)
+    for got, a, b in ((gx, gy.double(), w.double()), (gw, gy.double().t(), x.double())):
+        once(got, a, b, dtype, "gradient", held * (a.abs() @ b.abs()))
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
