@@ -1,5 +1,6 @@
 // layers_rows.cu -- products with few rows (single tokens, small batches): the
-// weights are all there is to read, so they stream through registers once.
+// weights are all there is to read; they stream through registers once (5 to 16 rows of float:
+// once for every four rows).
 //
 // Up to 4 rows of any type and layout (up to 16 of float, four at a time), FP32
 // units: a group of KW warps takes four rows of weights (two of each in GATED

@@ -55,3 +55,21 @@ def test_library_builds_without_torch(monkeypatch, tmp_path):
         assert len(ran) == len(build.UNITS) + 1 and not any("layers_torch" in a for cmd in ran for a in cmd)
         ran.clear()
         assert build.build() == build.OUT and not ran       # nothing has changed
+
+
+def test_binding_raises_statuses():
+    """The ctypes calls of the same names: sizes come back, refusals are VQCError."""
+    n = B.vqc_linear_workspace_bytes(1, B.VQC_BF16, B.VQC_BF16, 64, 32, 16, 32, 32, 16, B.ACTIVATIONS["gelu"], 1)
+    assert 0 < n < 1 << 20 and n % 256 == 0
+    assert 0 < B.vqc_gated_workspace_bytes(1, B.VQC_F16, 64, 32, 16, 32, 32, 1) < 1 << 20
+    assert 0 < B.vqc_layer_norm_workspace_bytes(64, 32) < 1 << 20
+    calls = [(B.vqc_layer_norm_forward, (B.VQC_F32, 4, 8, A, 7, None, None, 1e-5, A, None, None)),
+             (B.vqc_layer_norm_backward, (B.VQC_F32, 4, 8, A, 7, A, 8, None, A, A, None, None, None, 0, None)),
+             (B.vqc_linear_forward, (B.VQC_F32, B.VQC_F32, 4, 8, 6, A, 7, A, 8, None, 0, None, 0, A, None, None, 0, None)),
+             (B.vqc_linear_backward, (B.VQC_F32, B.VQC_F32, 4, 8, 6, A, 6, A, 7, A, 8, A, 2, A, A, A, A, 1 << 30, None)),
+             (B.vqc_gated_forward, (B.VQC_F32, 4, 8, 6, A, 7, A, A, 8, None, None, 3, A, None, None, 0, None)),
+             (B.vqc_gated_backward, (B.VQC_F32, 4, 8, 6, A, 6, A, 7, A, A, 8, A, 3, A, A, A, A, A, A, 1 << 30, None))]
+    for call, args in calls:
+        with pytest.raises(B.VQCError, match=call.__name__) as e:
+            call(*args)
+        assert B.STATUS[e.value.status] == "VQC_ERR_INVALID_ARG"
