@@ -435,3 +435,42 @@ def test_a_wait_that_ran_out_is_reported_by_later_calls():
     before, during, told, one, two = child(REPORTED, VQC_WAIT_NS="1000")
     assert before == ["VQC_ERR_DEVICE_CHECK"] * 4 and during == "timed out"
     assert told == ["VQC_ERR_DEVICE_CHECK", "VQC_OK"] and one == two == "VQC_OK"
+
+
+def test_float_parts_of_large_operands(layers):
+    """Operands of 2^8 and more are cut, not rounded, into their parts: the products that are left
+    out are then 2^-22 of a term each, two of them, of its sign.  With random signs the 2-norm
+    of the error is that of float sums (2^-24 sqrt(n / 3)) and of the cuts in a chunk (16 * 2^-25)
+    besides."""
+    rows, inp, out = 1024, 2048, 1024
+    for a, b in ((1e3, 1e3), (1e3, 1.0), (1e18, 1e18)):
+        x, w = normal(1, rows, inp, scale=a).cuda(), normal(2, out, inp, scale=b).cuda()
+        y = layers.linear_forward(x, w, save=False)
+        sync()
+        want = x.double() @ w.double().t()
+        limit = 2 * 2.0 ** -22 + 2.0 ** -24 * math.sqrt(inp / 3) + 16 * 2.0 ** -25
+        assert float((y.double() - want).norm() / want.norm()) <= limit
+
+
+CAPTURED = """
+import json, torch
+from paper_2607_11985_gb300 import binding as B, layers
+x, w = torch.randn(256, 512, device="cuda").bfloat16(), torch.randn(128, 512, device="cuda").bfloat16()
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    y, z = layers.linear_forward(x, w, None, "gelu")
+    g = layers.linear_backward(y, x, w, z, "gelu")
+for t in (y, z) + tuple(g):
+    t.zero_()
+graph.replay()
+torch.cuda.synchronize()
+u, v = layers.linear_forward(x, w, None, "gelu")
+h = layers.linear_backward(u, x, w, v, "gelu")
+B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
+print(json.dumps([torch.equal(a, b) for a, b in zip((y, z) + tuple(g), (u, v) + tuple(h))]))
+"""
+
+
+def test_first_products_of_a_process_inside_a_capture():
+    assert child(CAPTURED) == [True] * 5
