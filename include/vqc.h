@@ -451,9 +451,10 @@ vqc_status vqc_layer_norm_backward(vqc_real dtype, int64_t rows, int64_t cols, c
  *   saved     [rows, out] float: z, for the backward; or NULL.
  *   workspace vqc_linear_workspace_bytes(0, ...) bytes, 256-byte aligned (not
  *             read before it is written).
- * 16-bit operands are multiplied on the tensor cores, sums in float; VQC_F32
- * operands in float.  Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE,
- * VQC_ERR_CUDA. */
+ * 16-bit operands are multiplied on the tensor cores, sums in float; these cut a running
+ * sum where float32 would round, 4e-6 of it at 4096 terms for a 16-bit output and its
+ * saved values (a VQC_F32 output is summed in short pieces).  VQC_F32 operands in float.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA, VQC_ERR_DEVICE_CHECK. */
 vqc_status vqc_linear_forward(vqc_real dtype, vqc_real out_dtype, int64_t rows, int64_t in, int64_t out,
                               const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
                               const void* bias, vqc_activation act, const void* residual,

@@ -12,7 +12,10 @@
 // The tensor cores cut the low bits of a running sum at every product of depth 16 where
 // float32 would round (measured: a bias of 1.7e-8 of the result per product, 4e-6
 // at a depth of 4096).  Where the output is float32 a tile's contraction is therefore taken out in chunks
-// of 256, which the epilogue adds up in registers (kSums: tiles up to 128 columns).
+// of 256, which the epilogue adds up in registers (kSums: tiles up to 128 columns).  Where it has 16 bits the
+// running sum stays in tensor memory, and with it what is saved in float beside it (z; g and u) and
+// the sums of cuts: at that depth the bias is 1/400 of an output's own rounding in bfloat16, 1/50 in float16,
+// and the registers of chunks would not fit tiles of 256 columns.
 //
 // Two products that do not depend on one another (the two of a backward) share a launch:
 // one's tiles fill the SMs that the other's last tiles leave idle.
