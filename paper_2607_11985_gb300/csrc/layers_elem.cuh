@@ -92,12 +92,14 @@ __device__ __forceinline__ void store_as(void* p, int dtype, int64_t i, float v)
 // |z| 2^-23, 1 and 0 beyond the range of exp.
 __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + exp2f_fast(-1.4426950408889634f * z)); }
 
-// The normal distribution function of -a, a = |z|, and exp(-a^2 / 2).  Phi(-a) = exp(-a^2 / 2) R(a), R(a) = erfcx(a / sqrt 2) / 2 = t P(t), t = 1 / (1 + 0.3 a): P by
-// least squares of the relative error, weighted towards its largest (Lawson), 1.7e-7 at most on 0 <= a <= 14.5.
-// kFull: for float results the exponent's roundings (of a^2, of log2(e) / 2 and of their product) are taken
-// along as a factor: both values are good to a relative 2^-20 down to the smallest floats.  A result of
-// 16 bits does not show them (8e-6 at a = 12), and they would take 4 of the 65 us of 8192 x 2048 x 2048 with
-// residual and z.
+// The normal distribution function of -a, a = |z|, and exp(-a^2 / 2).
+// Phi(-a) = exp(-a^2 / 2) R(a), R(a) = erfcx(a / sqrt 2) / 2 = t P(t), t = 1 / (1 + 0.3 a): P by least
+// squares of the relative error, weighted towards its largest (Lawson), 1.7e-7 at most on
+// 0 <= a <= 14.5.
+// kFull: for float results the exponent's roundings (of a^2, of log2(e) / 2 and of their
+// product) are taken along as a factor: both values are good to a relative 2^-20 down to the smallest
+// floats.  A result of 16 bits does not show them (8e-6 at a = 12), and they would take 4 of the
+// 65 us of 8192 x 2048 x 2048 with residual and z.
 template <bool kFull> __device__ __forceinline__ float2 normal_tail(float z) {
     const float a = fminf(fabsf(z), 15.f);      // both are 0 beyond
     const float t = __fdividef(1.f, fmaf(0.3f, a, 1.f));
