@@ -515,6 +515,129 @@ size_t vqc_linear_workspace_bytes(int32_t mode, vqc_real dtype, vqc_real out_dty
 size_t vqc_gated_workspace_bytes(int32_t mode, vqc_real dtype, int64_t rows, int64_t in, int64_t out,
                                  int64_t x_stride, int64_t weight_stride, int32_t aligned);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a sequence: tokens of the same sequence attend to one another, around the blocks
+ * above.  Conventions as there; tokens, sequences and their product, and a cache's capacity below 2^30,
+ * heads and groups up to 65536. */
+
+/* Dropout and a residual: y = residual + x / (1 - p) where an element is kept, residual where it is not.
+ * Element e, counted over [rows, cols] in rows, is kept where word e % 4 of Philox 4x32-10 (Salmon et
+ * al. 2011; counter: the 64 bits of e / 4, then those of the offset; key: the seed) is at least
+ * p 2^32 (rounded, 2^32 - 1 at most).  No mask is stored: the backward draws it again.
+ *   p         0 <= p < 1.
+ *   state     device, two words (8-byte aligned), or NULL: seed and offset, read when the kernel runs, so
+ *             that a captured call draws anew in every replay; `seed` is then ignored and `offset` added.
+ *   residual  [rows, cols] or NULL (0).   y  [rows, cols].
+ * An element that is dropped counts as zero whatever it holds.  cols 1..2^31-1.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_CUDA. */
+vqc_status vqc_dropout_forward(vqc_real dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                               const void* residual, int64_t residual_stride, double p, uint64_t seed,
+                               uint64_t offset, const uint64_t* state, void* y, void* stream);
+/* grad_x = grad_y / (1 - p) where the element was kept, else 0; the residual's gradient is grad_y. */
+vqc_status vqc_dropout_backward(vqc_real dtype, int64_t rows, int64_t cols, const void* grad_y,
+                                int64_t grad_y_stride, double p, uint64_t seed, uint64_t offset,
+                                const uint64_t* state, void* grad_x, void* stream);
+
+/* [batch, tokens, heads, dim]: the elements of a head are adjacent, the strides (in elements, >= 0) any;
+ * `data` lies on a boundary of its elements. */
+typedef struct {
+    const void* data;
+    int64_t batch_stride, token_stride, head_stride;
+} vqc_heads;
+
+/* Norms of queries and keys for each head, and the rotation of positions, in one pass:
+ *   h = x / sqrt(mean(x^2) + eps) * weight,
+ *   y_i = h_i cos a - h_{n+i} sin a, y_{n+i} = h_{n+i} cos a + h_i sin a, a = position * frequency_i, i < n = pairs.
+ *   q [batch, tokens, heads, dim], k [batch, tokens, groups, dim], dim 1..256.
+ *   weight_q, weight_k  [dim] of dtype, or NULL (1).
+ *   frequencies  device [pairs] double, finite: radians per position; 2 pairs <= dim; elements from 2 pairs on are
+ *             not turned.  Angles are exact to a float's rounding at any position.
+ *   positions device int32 [batch or 1][tokens], rows positions_stride apart (0: one row for all
+ *             sequences), or NULL: the token's index.
+ *   q_out, k_out  dense, of dtype.
+ * Sums in float, results rounded once.  Errors: VQC_ERR_INVALID_ARG, VQC_ERR_CUDA. */
+vqc_status vqc_norm_rotary_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                   int64_t dim, const vqc_heads* q, const vqc_heads* k, const void* weight_q,
+                                   const void* weight_k, const double* frequencies, int64_t pairs,
+                                   const int32_t* positions, int64_t positions_stride, double eps, void* q_out,
+                                   void* k_out, void* stream);
+
+/* Gradients, from q and k themselves (nothing is saved).  With g the incoming gradient turned back, r = 1 /
+ * sqrt(mean(x^2) + eps), m = x r, u = g weight: grad_x = r (u - m mean(u m)), grad_weight = sum over
+ * tokens and heads of g m.
+ *   grad_q, grad_k  dense of dtype, both or NULL; grad_weight_q, grad_weight_k [dim] of dtype, each or NULL.
+ *   workspace vqc_norm_rotary_workspace_bytes(...) bytes, 256-byte aligned; NULL without gradients of weights.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA. */
+size_t vqc_norm_rotary_workspace_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim);
+vqc_status vqc_norm_rotary_backward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                    int64_t dim, const vqc_heads* grad_q_out, const vqc_heads* grad_k_out,
+                                    const vqc_heads* q, const vqc_heads* k, const void* weight_q,
+                                    const void* weight_k, const double* frequencies, int64_t pairs,
+                                    const int32_t* positions, int64_t positions_stride, double eps, void* grad_q,
+                                    void* grad_k, void* grad_weight_q, void* grad_weight_k, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* The same for serving, into a cache: token t of a sequence stands at position lengths[b] - tokens + t
+ * (lengths: device int32 [batch], tokens in the cache with the new ones); its normalised, turned key and
+ * its value as it is are written at that place of cache_k and cache_v [batch, capacity, groups, dim], its query
+ * to q_out (dense).  Places outside of the cache are not written.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_CUDA. */
+vqc_status vqc_norm_rotary_step(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                int64_t dim, int64_t capacity, const vqc_heads* q, const vqc_heads* k,
+                                const vqc_heads* v, const void* weight_q, const void* weight_k,
+                                const double* frequencies, int64_t pairs, double eps, const int32_t* lengths,
+                                void* q_out, const vqc_heads* cache_k, const vqc_heads* cache_v, void* stream);
+
+/* Causal attention through a window and over the first tokens.  Query i of a sequence sees key j where
+ * j <= i < lengths[b] and (i - j < window or j < sinks); with z_j = scale q . k_j over the keys in sight,
+ * o = sum_j softmax(z)_j v_j.
+ *   q [batch, tokens, heads, dim]; k, v [batch, tokens, groups, dim], dim 1..256; heads a multiple of
+ *             groups: head h reads the keys of group h / (heads / groups).
+ *   window    0: every earlier position.   scale > 0.
+ *   lengths   device int32 [batch] (values outside of 0..tokens count as the nearest), or NULL: all tokens.
+ *   o         [batch, tokens, heads, dim] dense, of dtype; rows from a sequence's length on are zero.
+ *   saved     [batch, heads, tokens] float: log of the sum of exp(z) (-infinity for rows that see nothing), for
+ *             the backward; or NULL.
+ *   workspace vqc_attention_workspace_bytes(0, ...) bytes, 256-byte aligned.
+ * Tokens from a sequence's length on are not read into any result.  Keys and values that are not finite
+ * may make NaN of outputs of their sequence that do not see them.  16-bit operands: the
+ * probabilities are rounded to dtype before their product with v, sums in float.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA, VQC_ERR_DEVICE_CHECK. */
+vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                 int64_t dim, const vqc_heads* q, const vqc_heads* k, const vqc_heads* v,
+                                 int64_t window, int64_t sinks, double scale, const int32_t* lengths, void* o,
+                                 float* saved, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of vqc_attention_forward, from its o and saved: p = exp(z - saved), ds = p (grad_o . v -
+ * grad_o . o), grad_v = sum p grad_o, grad_k = scale sum ds q, grad_q = scale sum ds k; grad_k and grad_v
+ * summed over the queries of all heads that read the key, in a fixed order; p and ds rounded to
+ * dtype before their products.  Rows from a sequence's length on are zero.
+ *   grad_q, grad_k, grad_v  dense of dtype; grad_q or NULL, grad_k and grad_v both or neither.
+ *   workspace vqc_attention_workspace_bytes(1, ...) bytes, 256-byte aligned.
+ * Errors as vqc_attention_forward. */
+vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                  int64_t dim, const vqc_heads* grad_o, const vqc_heads* q, const vqc_heads* k,
+                                  const vqc_heads* v, const void* o, const float* saved, int64_t window,
+                                  int64_t sinks, double scale, const int32_t* lengths, void* grad_q, void* grad_k,
+                                  void* grad_v, void* workspace, size_t workspace_bytes, void* stream);
+/* mode 0 forward, 1 backward; `aligned` 1 where all operands and their strides are multiples of 16 bytes. */
+size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads,
+                                     int64_t groups, int64_t dim, int32_t aligned);
+
+/* Attention of the last `tokens` tokens of sequences over a cache: token t stands at position
+ * lengths[b] - tokens + t and sees the keys of vqc_attention_forward at that position (lengths beyond
+ * 0..capacity count as the nearest; a token at a negative position sees nothing: zeros).
+ *   q [batch, tokens, heads, dim]; cache_k, cache_v [batch, capacity, groups, dim]; o dense.
+ * Places of a cache from the length on are not read.  No backward.
+ * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA. */
+vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                              int64_t dim, int64_t capacity, const vqc_heads* q, const vqc_heads* cache_k,
+                              const vqc_heads* cache_v, int64_t window, int64_t sinks, double scale,
+                              const int32_t* lengths, void* o, void* workspace, size_t workspace_bytes,
+                              void* stream);
+size_t vqc_attention_step_workspace_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
+                                          int64_t dim, int64_t capacity, int64_t window, int64_t sinks);
+
 /* Synchronise `stream` and report any CUDA error, then read (and clear) the
  * error word of every plan of this process on the current device: each kernel
  * checks its launch geometry against the plan before touching memory and, on

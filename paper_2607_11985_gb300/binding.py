@@ -53,6 +53,12 @@ class vqc_plan_stats(ctypes.Structure):
 assert ctypes.sizeof(vqc_gate) == 48
 
 
+class vqc_heads(ctypes.Structure):
+    """[batch, tokens, heads, dim] with adjacent elements of a head; strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
 class VQCError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("%s: %s" % (STATUS.get(status, status), msg))
@@ -63,6 +69,7 @@ _lib = None
 
 # C entry points and their signatures: (name, restype, argtypes)
 _P, _I, _S, _L, _D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64, ctypes.c_double
+_U, _H = ctypes.c_uint64, ctypes.POINTER(vqc_heads)
 SIGNATURES = [
     ("vqc_compile", _I, [ctypes.POINTER(vqc_gate), _I, _I, _I, _I, _I, ctypes.POINTER(_P)]),
     ("vqc_free", None, [_P]),
@@ -96,6 +103,19 @@ SIGNATURES = [
     ("vqc_gated_backward", _I, [_I, _L, _L, _L, _P, _L, _P, _L, _P, _P, _L, _P, _I, _P, _P, _P, _P, _P, _P,
                                 _S, _P]),
     ("vqc_gated_workspace_bytes", _S, [_I, _I, _L, _L, _L, _L, _L, _I]),
+    ("vqc_dropout_forward", _I, [_I, _L, _L, _P, _L, _P, _L, _D, _U, _U, _P, _P, _P]),
+    ("vqc_dropout_backward", _I, [_I, _L, _L, _P, _L, _D, _U, _U, _P, _P, _P]),
+    ("vqc_norm_rotary_forward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _P, _P, _P, _L, _P, _L, _D, _P, _P, _P]),
+    ("vqc_norm_rotary_workspace_bytes", _S, [_L, _L, _L, _L, _L]),
+    ("vqc_norm_rotary_backward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _H, _H, _P, _P, _P, _L, _P, _L, _D, _P, _P, _P, _P,
+                                      _P, _S, _P]),
+    ("vqc_norm_rotary_step", _I, [_I, _L, _L, _L, _L, _L, _L, _H, _H, _H, _P, _P, _P, _L, _D, _P, _P, _H, _H, _P]),
+    ("vqc_attention_forward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _H, _L, _L, _D, _P, _P, _P, _P, _S, _P]),
+    ("vqc_attention_backward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _H, _H, _P, _P, _L, _L, _D, _P, _P, _P, _P, _P, _S,
+                                    _P]),
+    ("vqc_attention_workspace_bytes", _S, [_I, _I, _L, _L, _L, _L, _L, _I]),
+    ("vqc_attention_step", _I, [_I, _L, _L, _L, _L, _L, _L, _H, _H, _H, _L, _L, _D, _P, _P, _P, _S, _P]),
+    ("vqc_attention_step_workspace_bytes", _S, [_L, _L, _L, _L, _L, _L, _L, _L]),
 ]
 
 
@@ -278,6 +298,68 @@ def vqc_gated_backward(dtype, rows, in_, out, grad_h, grad_h_stride, x, x_stride
 
 def vqc_gated_workspace_bytes(mode, dtype, rows, in_, out, x_stride, weight_stride, aligned):
     return lib().vqc_gated_workspace_bytes(mode, dtype, rows, in_, out, x_stride, weight_stride, aligned)
+
+
+def vqc_dropout_forward(dtype, rows, cols, x, x_stride, residual, residual_stride, p, seed, offset, state, y, stream):
+    _check(lib().vqc_dropout_forward(dtype, rows, cols, x, x_stride, residual, residual_stride, p, seed, offset,
+                                     state, y, stream))
+
+
+def vqc_dropout_backward(dtype, rows, cols, grad_y, grad_y_stride, p, seed, offset, state, grad_x, stream):
+    _check(lib().vqc_dropout_backward(dtype, rows, cols, grad_y, grad_y_stride, p, seed, offset, state, grad_x,
+                                      stream))
+
+
+def vqc_norm_rotary_forward(dtype, batch, tokens, heads, groups, dim, q, k, weight_q, weight_k, frequencies, pairs,
+                            positions, positions_stride, eps, q_out, k_out, stream):
+    _check(lib().vqc_norm_rotary_forward(dtype, batch, tokens, heads, groups, dim, q, k, weight_q, weight_k,
+                                         frequencies, pairs, positions, positions_stride, eps, q_out, k_out, stream))
+
+
+def vqc_norm_rotary_workspace_bytes(batch, tokens, heads, groups, dim):
+    return lib().vqc_norm_rotary_workspace_bytes(batch, tokens, heads, groups, dim)
+
+
+def vqc_norm_rotary_backward(dtype, batch, tokens, heads, groups, dim, grad_q_out, grad_k_out, q, k, weight_q,
+                             weight_k, frequencies, pairs, positions, positions_stride, eps, grad_q, grad_k,
+                             grad_weight_q, grad_weight_k, workspace, workspace_bytes, stream):
+    _check(lib().vqc_norm_rotary_backward(dtype, batch, tokens, heads, groups, dim, grad_q_out, grad_k_out, q, k,
+                                          weight_q, weight_k, frequencies, pairs, positions, positions_stride, eps,
+                                          grad_q, grad_k, grad_weight_q, grad_weight_k, workspace, workspace_bytes,
+                                          stream))
+
+
+def vqc_norm_rotary_step(dtype, batch, tokens, heads, groups, dim, capacity, q, k, v, weight_q, weight_k, frequencies,
+                         pairs, eps, lengths, q_out, cache_k, cache_v, stream):
+    _check(lib().vqc_norm_rotary_step(dtype, batch, tokens, heads, groups, dim, capacity, q, k, v, weight_q, weight_k,
+                                      frequencies, pairs, eps, lengths, q_out, cache_k, cache_v, stream))
+
+
+def vqc_attention_forward(dtype, batch, tokens, heads, groups, dim, q, k, v, window, sinks, scale, lengths, o, saved,
+                          workspace, workspace_bytes, stream):
+    _check(lib().vqc_attention_forward(dtype, batch, tokens, heads, groups, dim, q, k, v, window, sinks, scale,
+                                       lengths, o, saved, workspace, workspace_bytes, stream))
+
+
+def vqc_attention_backward(dtype, batch, tokens, heads, groups, dim, grad_o, q, k, v, o, saved, window, sinks, scale,
+                           lengths, grad_q, grad_k, grad_v, workspace, workspace_bytes, stream):
+    _check(lib().vqc_attention_backward(dtype, batch, tokens, heads, groups, dim, grad_o, q, k, v, o, saved, window,
+                                        sinks, scale, lengths, grad_q, grad_k, grad_v, workspace, workspace_bytes,
+                                        stream))
+
+
+def vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, aligned):
+    return lib().vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, aligned)
+
+
+def vqc_attention_step(dtype, batch, tokens, heads, groups, dim, capacity, q, cache_k, cache_v, window, sinks, scale,
+                       lengths, o, workspace, workspace_bytes, stream):
+    _check(lib().vqc_attention_step(dtype, batch, tokens, heads, groups, dim, capacity, q, cache_k, cache_v, window,
+                                    sinks, scale, lengths, o, workspace, workspace_bytes, stream))
+
+
+def vqc_attention_step_workspace_bytes(batch, tokens, heads, groups, dim, capacity, window, sinks):
+    return lib().vqc_attention_step_workspace_bytes(batch, tokens, heads, groups, dim, capacity, window, sinks)
 
 
 def vqc_plan_info(plan, batch):

@@ -1,0 +1,31 @@
+// attention.h -- what the translation units of attention share.
+#pragma once
+
+#include "sequence.h"
+
+namespace vqc {
+namespace layers {
+
+// Which keys a query sees: j <= i < length and (i - j < window or j < sinks).
+struct Sight {
+    const int32_t* lengths;      // [batch], or NULL: all tokens
+    int64_t tokens, window, sinks;
+};
+
+struct AttentionArgs {
+    Heads q, k, v, g;            // g: the incoming gradient
+    Sight sight;
+    void* o;                     // dense [batch, tokens, heads, dim]
+    float* saved;                // forward: lse [batch, heads, tokens], or NULL
+    const float* lse;            // backward
+    float* d;                    // g . o of the rows, [batch, heads, tokens]
+    void *gq, *gk, *gv;          // dense
+    int64_t batch;
+    float scale, scale2;         // scale2: times log2(e)
+    int heads, groups, dim, dtype;
+};
+
+constexpr int64_t kMostDim = 256;
+
+}  // namespace layers
+}  // namespace vqc

@@ -10,11 +10,13 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
 #include <optional>
 #include <stdexcept>
@@ -250,6 +252,202 @@ variable_list gated_backward(const Tensor& gh, const Tensor& x, const Tensor& wg
     return {gx, gwg, gwu, gbg, gbu};
 }
 
+// [batch, tokens, heads, dim] with adjacent elements of a head
+struct HeadRows {
+    Tensor t;
+    int code;
+    vqc_heads h;
+    int64_t size(int i) const { return t.size(i); }
+};
+HeadRows head_rows(const Tensor& given, const char* name) {
+    const int code = given.defined() ? code_of(given.scalar_type()) : -1;
+    if (code < 0 || given.dim() != 4 || !here(given))
+        throw Refused(std::string(name) + " must be a CUDA float32, bfloat16 or float16 tensor [batch, tokens, heads, dim] on the current device (got " + told(given) + ")");
+    if (given.size(2) < 1 || given.size(3) < 1) throw Refused(std::string(name) + " must have a head of at least one element (got " + told(given) + ")");
+    no_tangent(given, name);
+    HeadRows r{as_read(given), code, {}};
+    if (r.t.stride(3) != 1 && r.t.size(3) > 1) r.t = r.t.contiguous();
+    r.h = {r.t.data_ptr(), r.t.stride(0), r.t.stride(1), r.t.stride(2)};
+    return r;
+}
+HeadRows head_rows(const Tensor& given, const HeadRows& like, int64_t heads, const char* name) {
+    HeadRows r = head_rows(given, name);
+    if (r.code != like.code || r.size(0) != like.size(0) || r.size(1) != like.size(1) || (heads > 0 && r.size(2) != heads) || r.size(3) != like.size(3))
+        throw Refused(std::string(name) + " does not fit: " + told(given) + " beside " + told(like.t));
+    return r;
+}
+// A cache [batch, capacity, groups, dim], read or written in place.
+HeadRows cache_rows(const Tensor& given, const HeadRows& q, int64_t groups, int64_t capacity, bool written, const char* name) {
+    if (written && given.defined() && (given.is_neg() || (at::GradMode::is_enabled() && given.requires_grad())))
+        throw Refused(std::string(name) + " is written: it must be no view that torch negates, and need no gradient");
+    HeadRows r = head_rows(given, name);
+    if (r.code != q.code || r.size(0) != q.size(0) || (groups > 0 && r.size(2) != groups) || (capacity >= 0 && r.size(1) != capacity) || r.size(3) != q.size(3))
+        throw Refused(std::string(name) + " does not fit: " + told(given) + " beside " + told(q.t));
+    if (written) {
+        bool apart = r.t.is_same(given);
+        for (int i = 0; i < 3; ++i) apart = apart && (r.t.stride(i) != 0 || r.t.size(i) == 1);
+        if (!apart) throw Refused(std::string(name) + " is written: the elements of a head must be adjacent and no two places one (got " + told(given) + ")");
+    }
+    return r;
+}
+Tensor int_rows(const Tensor& given, int64_t batch, int64_t tokens, const char* name) {      // tokens < 0: [batch]
+    if (!given.defined()) return given;
+    const bool one = tokens < 0;
+    const bool fits = one ? given.dim() == 1 && given.size(0) == batch
+                          : (given.dim() == 1 && given.size(0) == tokens) ||
+                                (given.dim() == 2 && given.size(1) == tokens && (given.size(0) == batch || given.size(0) == 1));
+    if (given.scalar_type() != at::kInt || !here(given) || !fits)
+        throw Refused(std::string(name) + " must be a CUDA int32 tensor " + (one ? "[batch]" : "[batch, tokens] or [tokens]") + " on the current device (got " + told(given) + ")");
+    return given.contiguous();
+}
+
+struct Draw {
+    double p;
+    uint64_t seed, offset;
+    Tensor state;      // in the place of the seed, or undefined
+    const uint64_t* words() const { return static_cast<const uint64_t*>(address(state)); }
+};
+Tensor dropout_run(const Tensor& x, const Draw& d, const Tensor& res, bool back) {
+    const Matrix m = matrix(x, back ? "grad_y" : "x");
+    if (!(d.p >= 0) || !(d.p < 1)) throw Refused("p must be at least 0 and less than 1 (got " + std::to_string(d.p) + ")");
+    if (d.state.defined() && (d.state.scalar_type() != at::kLong || d.state.dim() != 1 || d.state.size(0) != 2 || !d.state.is_contiguous() || !here(d.state)))
+        throw Refused("seed must be an integer, or a dense CUDA int64 tensor of two elements (seed, offset) on the current device (got " + told(d.state) + ")");
+    Tensor y = output(x, m.cols, x.scalar_type());
+    if (back) {
+        check(vqc_dropout_backward((vqc_real)m.code, m.rows, m.cols, m.data(), m.ld, d.p, d.seed, d.offset, d.words(), y.data_ptr(), stream()));
+        return y;
+    }
+    Matrix r{};
+    if (res.defined()) r = like(res, m.rows, m.cols, m.code, "residual");
+    check(vqc_dropout_forward((vqc_real)m.code, m.rows, m.cols, m.data(), m.ld, address(r.t), r.ld, d.p, d.seed, d.offset, d.words(), y.data_ptr(),
+                              stream()));
+    return y;
+}
+
+// What turns and scales queries and keys.
+struct Turn {
+    Tensor wq, wk, frequencies, positions;
+    double eps;
+    int64_t pairs() const { return frequencies.defined() ? frequencies.size(0) : 0; }
+};
+Turn turn_of(const HeadRows& q, const Turn& t) {
+    const int64_t dim = q.size(3);
+    Turn r{vector(t.wq, dim, q.code, "weight_q"), vector(t.wk, dim, q.code, "weight_k"), t.frequencies, int_rows(t.positions, q.size(0), q.size(1), "positions"), t.eps};
+    if (r.frequencies.defined()) {
+        if (r.frequencies.scalar_type() != at::kDouble || r.frequencies.dim() != 1 || 2 * r.frequencies.size(0) > dim || !here(r.frequencies))
+            throw Refused("frequencies must be a CUDA float64 tensor of at most half as many elements as a head on the current device (got " + told(r.frequencies) + ")");
+        r.frequencies = as_read(r.frequencies).contiguous();
+    }
+    if (!(t.eps >= 0)) throw Refused("eps must not be negative (got " + std::to_string(t.eps) + ")");
+    if (dim > 256) throw Refused("heads of at most 256 elements (got " + told(q.t) + ")");
+    return r;
+}
+int64_t rows_apart(const Tensor& positions, const HeadRows& q) {
+    return positions.defined() && positions.dim() == 2 && positions.size(0) == q.size(0) ? q.size(1) : 0;
+}
+Tensor dense(const HeadRows& like, int64_t heads) { return at::empty({like.size(0), like.size(1), heads, like.size(3)}, like.t.options()); }
+
+variable_list rotary_forward(const Tensor& q, const Tensor& k, const Turn& given) {
+    const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k");
+    const Turn t = turn_of(a, given);
+    Tensor yq = dense(a, a.size(2)), yk = dense(a, b.size(2));
+    check(vqc_norm_rotary_forward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &a.h, &b.h, address(t.wq), address(t.wk),
+                                  static_cast<const double*>(address(t.frequencies)), t.pairs(), static_cast<const int32_t*>(address(t.positions)),
+                                  rows_apart(t.positions, a), t.eps, yq.data_ptr(), yk.data_ptr(), stream()));
+    return {yq, yk};
+}
+variable_list rotary_backward(const Tensor& gq, const Tensor& gk, const Tensor& q, const Tensor& k, const Turn& given, bool need_x, bool need_wq, bool need_wk) {
+    const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k");
+    const HeadRows ga = head_rows(gq, a, a.size(2), "grad_q"), gb = head_rows(gk, a, b.size(2), "grad_k");
+    const Turn t = turn_of(a, given);
+    need_wq = need_wq && t.wq.defined();
+    need_wk = need_wk && t.wk.defined();
+    Tensor xq = need_x ? dense(a, a.size(2)) : Tensor(), xk = need_x ? dense(a, b.size(2)) : Tensor();
+    Tensor wq = fresh(need_wq, {a.size(3)}, a.t), wk = fresh(need_wk, {a.size(3)}, a.t);
+    const size_t bytes = need_wq || need_wk ? vqc_norm_rotary_workspace_bytes(a.size(0), a.size(1), a.size(2), b.size(2), a.size(3)) : 0;
+    const Tensor ws = space(bytes, a.t);
+    check(vqc_norm_rotary_backward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &ga.h, &gb.h, &a.h, &b.h, address(t.wq),
+                                   address(t.wk), static_cast<const double*>(address(t.frequencies)), t.pairs(),
+                                   static_cast<const int32_t*>(address(t.positions)), rows_apart(t.positions, a), t.eps, address(xq), address(xk),
+                                   address(wq), address(wk), address(ws), bytes, stream()));
+    return {xq, xk, wq, wk};
+}
+void written(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+Tensor rotary_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& ck, const Tensor& cv, const Tensor& lengths, const Turn& given) {
+    const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v");
+    const HeadRows kc = cache_rows(ck, a, b.size(2), -1, true, "cache_k"), vc = cache_rows(cv, a, b.size(2), kc.size(1), true, "cache_v");
+    const Turn t = turn_of(a, given);
+    if (!lengths.defined()) throw Refused("lengths must be given");
+    const Tensor n = int_rows(lengths, a.size(0), -1, "lengths");
+    Tensor yq = dense(a, a.size(2));
+    check(vqc_norm_rotary_step((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), kc.size(1), &a.h, &b.h, &c.h, address(t.wq),
+                               address(t.wk), static_cast<const double*>(address(t.frequencies)), t.pairs(), t.eps,
+                               static_cast<const int32_t*>(address(n)), yq.data_ptr(), &kc.h, &vc.h, stream()));
+    written(ck);
+    written(cv);
+    return yq;
+}
+
+// What a query sees.
+struct Sight {
+    int64_t window, sinks;
+    double scale;       // 0: 1 / sqrt(dim)
+    Tensor lengths;
+};
+Sight sight_of(const HeadRows& q, int64_t groups, const Sight& s) {
+    if (s.window < 0 || s.sinks < 0) throw Refused("window must be None or at least 1, sinks at least 0");
+    if (q.size(2) % groups) throw Refused("the heads of q must be a multiple of those of k (got " + std::to_string(q.size(2)) + " and " + std::to_string(groups) + ")");
+    if (q.size(3) > 256) throw Refused("heads of at most 256 elements (got " + told(q.t) + ")");
+    Sight r{s.window, s.sinks, s.scale == 0 ? 1.0 / std::sqrt((double)q.size(3)) : s.scale, int_rows(s.lengths, q.size(0), -1, "lengths")};
+    if (!(r.scale > 1e-30) || !(r.scale < 1e30)) throw Refused("scale must be positive and within float's range (got " + std::to_string(s.scale) + ")");
+    return r;
+}
+bool on16(const HeadRows& r) {
+    const int64_t n = r.code == VQC_F32 ? 4 : 8;
+    return aligned({r.h.data}) && r.h.batch_stride % n == 0 && r.h.token_stride % n == 0 && r.h.head_stride % n == 0;
+}
+std::pair<Tensor, Tensor> attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Sight& given, bool save) {
+    const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v");
+    const Sight s = sight_of(a, b.size(2), given);
+    Tensor o = dense(a, a.size(2)), saved;
+    if (save) saved = at::empty({a.size(0), a.size(2), a.size(1)}, a.t.options().dtype(at::kFloat));
+    const size_t bytes = vqc_attention_workspace_bytes(0, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), on16(a) && on16(b) && on16(c));
+    const Tensor ws = space(bytes, a.t);
+    check(vqc_attention_forward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &a.h, &b.h, &c.h, s.window, s.sinks, s.scale,
+                                static_cast<const int32_t*>(address(s.lengths)), o.data_ptr(), static_cast<float*>(address(saved)), address(ws), bytes,
+                                stream()));
+    return {o, saved};
+}
+variable_list attention_backward(const Tensor& go, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& o, const Tensor& saved,
+                                 const Sight& given, bool need_q, bool need_kv) {
+    const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v"), g = head_rows(go, a, a.size(2), "grad_o");
+    const HeadRows y = head_rows(o, a, a.size(2), "o");
+    const Sight s = sight_of(a, b.size(2), given);
+    const float* lse = saved_of(saved, {a.size(0), a.size(2), a.size(1)});
+    const Tensor out = y.t.contiguous();
+    Tensor gq = need_q ? dense(a, a.size(2)) : Tensor(), gk = need_kv ? dense(a, b.size(2)) : Tensor(), gv = need_kv ? dense(a, b.size(2)) : Tensor();
+    const size_t bytes = vqc_attention_workspace_bytes(1, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3),
+                                                       on16(a) && on16(b) && on16(c) && on16(g));
+    const Tensor ws = space(bytes, a.t);
+    check(vqc_attention_backward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &g.h, &a.h, &b.h, &c.h, out.data_ptr(), lse,
+                                 s.window, s.sinks, s.scale, static_cast<const int32_t*>(address(s.lengths)), address(gq), address(gk), address(gv),
+                                 address(ws), bytes, stream()));
+    return {gq, gk, gv};
+}
+Tensor attention_step(const Tensor& q, const Tensor& ck, const Tensor& cv, const Sight& given) {
+    const HeadRows a = head_rows(q, "q"), kc = cache_rows(ck, a, -1, -1, false, "cache_k"), vc = cache_rows(cv, a, kc.size(2), kc.size(1), false, "cache_v");
+    if (!given.lengths.defined()) throw Refused("lengths must be given");
+    const Sight s = sight_of(a, kc.size(2), given);
+    Tensor o = dense(a, a.size(2));
+    const size_t bytes = vqc_attention_step_workspace_bytes(a.size(0), a.size(1), a.size(2), kc.size(2), a.size(3), kc.size(1), s.window, s.sinks);
+    const Tensor ws = space(bytes, a.t);
+    check(vqc_attention_step((vqc_real)a.code, a.size(0), a.size(1), a.size(2), kc.size(2), a.size(3), kc.size(1), &a.h, &kc.h, &vc.h, s.window, s.sinks,
+                             s.scale, static_cast<const int32_t*>(address(s.lengths)), o.data_ptr(), address(ws), bytes, stream()));
+    return o;
+}
+
 // ---------------------------------------------------------------- autograd
 
 [[noreturn]] variable_list only_once() { throw std::runtime_error("these layer operators can be differentiated once only"); }
@@ -378,6 +576,124 @@ struct GatedFunction : Function<GatedFunction> {
     }
 };
 
+struct DropoutGradient : Function<DropoutGradient> {
+    static Tensor forward(AutogradContext*, const Tensor& gy, const Optional& state, double p, int64_t seed, int64_t offset) {
+        return dropout_run(gy, {p, (uint64_t)seed, (uint64_t)offset, tensor(state)}, Tensor(), true);
+    }
+    static variable_list backward(AutogradContext*, variable_list) { only_once(); }
+};
+struct RotaryGradients : Function<RotaryGradients> {
+    static variable_list forward(AutogradContext*, const Tensor& gq, const Tensor& gk, const Tensor& q, const Tensor& k, const Optional& wq, const Optional& wk,
+                                 const Optional& f, const Optional& pos, double eps, bool nx, bool nwq, bool nwk) {
+        return only(rotary_backward(gq, gk, q, k, {tensor(wq), tensor(wk), tensor(f), tensor(pos), eps}, nx, nwq, nwk));
+    }
+    static variable_list backward(AutogradContext*, variable_list) { only_once(); }
+};
+struct AttentionGradients : Function<AttentionGradients> {
+    static variable_list forward(AutogradContext*, const Tensor& go, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& o, const Tensor& saved,
+                                 const Optional& lengths, int64_t window, int64_t sinks, double scale, bool nq, bool nkv) {
+        return only(attention_backward(go, q, k, v, o, saved, {window, sinks, scale, tensor(lengths)}, nq, nkv));
+    }
+    static variable_list backward(AutogradContext*, variable_list) { only_once(); }
+};
+
+struct DropoutFunction : Function<DropoutFunction> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Optional& res, const Optional& state, double p, int64_t seed, int64_t offset) {
+        Tensor y = dropout_run(x, {p, (uint64_t)seed, (uint64_t)offset, tensor(state)}, tensor(res), false);
+        if (state) ctx->save_for_backward({*state});      // (a state that has changed since is refused)
+        ctx->saved_data["present"] = (int64_t)(1 | (res ? 2 : 0));
+        ctx->saved_data["p"] = p;
+        ctx->saved_data["seed"] = seed;
+        ctx->saved_data["offset"] = offset;
+        if (res && res->sizes() != y.sizes()) ctx->saved_data["residual"] = res->sizes().vec();
+        return y;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        if (!g[0].defined()) return variable_list(6);
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor state = s.empty() ? Tensor() : s[0];
+        Inputs in{ctx, ctx->saved_data["present"].toInt()};
+        const bool nx = in.needed(0), nr = in.needed(1);
+        const double p = ctx->saved_data["p"].toDouble();
+        const int64_t seed = ctx->saved_data["seed"].toInt(), offset = ctx->saved_data["offset"].toInt();
+        variable_list r(6);
+        if (nx)
+            r[0] = at::GradMode::is_enabled() ? DropoutGradient::apply(g[0], optional(state), p, seed, offset)
+                                              : dropout_run(g[0], {p, (uint64_t)seed, (uint64_t)offset, state}, Tensor(), true);
+        const auto shape = ctx->saved_data.find("residual");
+        if (nr) r[1] = shape == ctx->saved_data.end() ? g[0] : g[0].reshape(shape->second.toIntVector());
+        return r;
+    }
+};
+
+struct RotaryFunction : Function<RotaryFunction> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Optional& wq, const Optional& wk, const Optional& f,
+                                 const Optional& pos, double eps) {
+        variable_list y = rotary_forward(q, k, {tensor(wq), tensor(wk), tensor(f), tensor(pos), eps});
+        variable_list keep = {q, k};
+        for (const Optional* t : {&wq, &wk, &f, &pos})
+            if (*t) keep.push_back(**t);
+        ctx->save_for_backward(keep);
+        ctx->saved_data["present"] = (int64_t)(3 | (wq ? 4 : 0) | (wk ? 8 : 0) | (f ? 16 : 0) | (pos ? 32 : 0));
+        ctx->saved_data["eps"] = eps;
+        return y;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        if (!g[0].defined() && !g[1].defined()) return variable_list(7);
+        const variable_list s = ctx->get_saved_variables();
+        const int64_t present = ctx->saved_data["present"].toInt();
+        size_t next = 2;
+        auto take = [&](int bit) { return present >> bit & 1 ? s[next++] : Tensor(); };
+        Turn t;
+        t.wq = take(2);
+        t.wk = take(3);
+        t.frequencies = take(4);
+        t.positions = take(5);
+        t.eps = ctx->saved_data["eps"].toDouble();
+        Inputs in{ctx, present};
+        const bool nq = in.needed(0), nk = in.needed(1), nwq = in.needed(2), nwk = in.needed(3), nx = nq || nk;
+        for (int i = 0; i < 2; ++i)      // an output that was not used
+            if (!g[i].defined()) g[i] = at::zeros(s[i].sizes(), s[i].options());
+        variable_list r(4);
+        if (nx || nwq || nwk)
+            r = at::GradMode::is_enabled() ? spread(RotaryGradients::apply(g[0], g[1], s[0], s[1], optional(t.wq), optional(t.wk), optional(t.frequencies),
+                                                                           optional(t.positions), t.eps, nx, nwq, nwk), {nx, nx, nwq, nwk})
+                                           : rotary_backward(g[0], g[1], s[0], s[1], t, nx, nwq, nwk);
+        if (!nq) r[0] = Tensor();
+        if (!nk) r[1] = Tensor();
+        r.resize(7);
+        return r;
+    }
+};
+
+struct AttentionFunction : Function<AttentionFunction> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Optional& lengths, int64_t window, int64_t sinks,
+                          double scale) {
+        auto [o, saved] = attention_forward(q, k, v, {window, sinks, scale, tensor(lengths)}, true);
+        if (lengths) ctx->save_for_backward({q, k, v, o, saved, *lengths});
+        else ctx->save_for_backward({q, k, v, o, saved});
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["sinks"] = sinks;
+        ctx->saved_data["scale"] = scale;
+        return o;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        if (!g[0].defined()) return variable_list(7);
+        const variable_list s = ctx->get_saved_variables();
+        const Sight sight{ctx->saved_data["window"].toInt(), ctx->saved_data["sinks"].toInt(), ctx->saved_data["scale"].toDouble(), s.size() > 5 ? s[5] : Tensor()};
+        const bool nq = ctx->needs_input_grad(0), nk = ctx->needs_input_grad(1), nv = ctx->needs_input_grad(2), nkv = nk || nv;
+        variable_list r(3);
+        if (nq || nkv)
+            r = at::GradMode::is_enabled() ? spread(AttentionGradients::apply(g[0], s[0], s[1], s[2], s[3], s[4], optional(sight.lengths), sight.window,
+                                                                              sight.sinks, sight.scale, nq, nkv), {nq, nkv, nkv})
+                                           : attention_backward(g[0], s[0], s[1], s[2], s[3], s[4], sight, nq, nkv);
+        if (!nk) r[1] = Tensor();
+        if (!nv) r[2] = Tensor();
+        r.resize(7);
+        return r;
+    }
+};
+
 bool recorded(std::initializer_list<const Tensor*> inputs) {
     if (!at::GradMode::is_enabled()) return false;
     for (const Tensor* t : inputs)
@@ -394,6 +710,18 @@ Tensor linear(const Tensor& x, const Tensor& w, const Tensor& b, int64_t act, co
 Tensor gated(const Tensor& x, const Tensor& wg, const Tensor& wu, const Tensor& bg, const Tensor& bu, int64_t act) {
     return recorded({&x, &wg, &wu, &bg, &bu}) ? GatedFunction::apply(x, wg, wu, optional(bg), optional(bu), act)
                                               : gated_forward(x, wg, wu, bg, bu, act, false).first;
+}
+
+Tensor dropout(const Tensor& x, const Draw& d, const Tensor& res) {
+    return recorded({&x, &res}) ? DropoutFunction::apply(x, optional(res), optional(d.state), d.p, (int64_t)d.seed, (int64_t)d.offset)
+                                : dropout_run(x, d, res, false);
+}
+variable_list rotary(const Tensor& q, const Tensor& k, const Turn& t) {
+    return recorded({&q, &k, &t.wq, &t.wk}) ? RotaryFunction::apply(q, k, optional(t.wq), optional(t.wk), optional(t.frequencies), optional(t.positions), t.eps)
+                                            : rotary_forward(q, k, t);
+}
+Tensor attention(const Tensor& q, const Tensor& k, const Tensor& v, const Sight& s) {
+    return recorded({&q, &k, &v}) ? AttentionFunction::apply(q, k, v, optional(s.lengths), s.window, s.sinks, s.scale) : attention_forward(q, k, v, s, false).first;
 }
 
 // ---------------------------------------------------------------- Python
@@ -538,9 +866,115 @@ PyObject* py_gated(ARGS) {
     });
 }
 
+// p, seed (an integer or a tensor), offset
+Draw draw_arg(PyObject* const* a) {
+    Draw d{float_arg(a[0]), 0, 0, Tensor()};
+    if (THPVariable_Check(a[1])) {
+        d.state = THPVariable_Unpack(a[1]);
+    } else {
+        d.seed = PyLong_AsUnsignedLongLongMask(a[1]);
+        if (PyErr_Occurred()) throw python_error();
+    }
+    d.offset = PyLong_AsUnsignedLongLongMask(a[2]);
+    if (PyErr_Occurred()) throw python_error();
+    return d;
+}
+PyObject* py_dropout_forward(ARGS) {
+    return guarded(n, 5, [&] {
+        const Tensor x = tensor_arg(a[0]), r = tensor_arg(a[4]);
+        const Draw d = draw_arg(a + 1);
+        return wrapped(released([&] { return dropout_run(x, d, r, false); }));
+    });
+}
+PyObject* py_dropout_backward(ARGS) {
+    return guarded(n, 4, [&] {
+        const Tensor g = tensor_arg(a[0]);
+        const Draw d = draw_arg(a + 1);
+        return wrapped(released([&] { return dropout_run(g, d, Tensor(), true); }));
+    });
+}
+PyObject* py_dropout(ARGS) {
+    return guarded(n, 5, [&] {
+        const Tensor x = tensor_arg(a[0]), r = tensor_arg(a[4]);
+        const Draw d = draw_arg(a + 1);
+        return wrapped(released([&] { return dropout(x, d, r); }));
+    });
+}
+// weight_q, weight_k, frequencies, positions, eps
+Turn turn_arg(PyObject* const* a) { return {tensor_arg(a[0]), tensor_arg(a[1]), tensor_arg(a[2]), tensor_arg(a[3]), float_arg(a[4])}; }
+PyObject* py_rotary_forward(ARGS) {
+    return guarded(n, 7, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]);
+        const Turn t = turn_arg(a + 2);
+        return wrapped(released([&] { return rotary_forward(q, k, t); }));
+    });
+}
+PyObject* py_rotary_backward(ARGS) {
+    return guarded(n, 11, [&] {
+        const Tensor gq = tensor_arg(a[0]), gk = tensor_arg(a[1]), q = tensor_arg(a[2]), k = tensor_arg(a[3]);
+        const Turn t = turn_arg(a + 4);
+        const bool nx = bool_arg(a[9]), nw = bool_arg(a[10]);
+        return wrapped(released([&] { return rotary_backward(gq, gk, q, k, t, nx, nw, nw); }));
+    });
+}
+PyObject* py_rotary(ARGS) {
+    return guarded(n, 7, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]);
+        const Turn t = turn_arg(a + 2);
+        return wrapped(released([&] { return rotary(q, k, t); }));
+    });
+}
+PyObject* py_rotary_step(ARGS) {
+    return guarded(n, 10, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]), v = tensor_arg(a[2]), ck = tensor_arg(a[3]), cv = tensor_arg(a[4]), l = tensor_arg(a[5]);
+        const Turn t{tensor_arg(a[6]), tensor_arg(a[7]), tensor_arg(a[8]), Tensor(), float_arg(a[9])};
+        return wrapped(released([&] { return rotary_step(q, k, v, ck, cv, l, t); }));
+    });
+}
+// window, sinks, scale, lengths
+Sight sight_arg(PyObject* const* a) {
+    Sight s{0, int_arg(a[1]), 0, tensor_arg(a[3])};
+    if (a[0] != Py_None && (s.window = int_arg(a[0])) < 1) throw Refused("window must be None or at least 1 (got " + std::to_string(s.window) + ")");
+    if (a[2] != Py_None && !((s.scale = float_arg(a[2])) > 0)) throw Refused("scale must be positive (got " + std::to_string(s.scale) + ")");
+    return s;
+}
+PyObject* py_attention_forward(ARGS) {
+    return guarded(n, 8, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]), v = tensor_arg(a[2]);
+        const Sight s = sight_arg(a + 3);
+        const bool save = bool_arg(a[7]);
+        return wrapped(released([&] { return attention_forward(q, k, v, s, save); }), save);
+    });
+}
+PyObject* py_attention_backward(ARGS) {
+    return guarded(n, 12, [&] {
+        const Tensor g = tensor_arg(a[0]), q = tensor_arg(a[1]), k = tensor_arg(a[2]), v = tensor_arg(a[3]), o = tensor_arg(a[4]), l = tensor_arg(a[5]);
+        const Sight s = sight_arg(a + 6);
+        const bool nq = bool_arg(a[10]), nkv = bool_arg(a[11]);
+        return wrapped(released([&] { return attention_backward(g, q, k, v, o, l, s, nq, nkv); }));
+    });
+}
+PyObject* py_attention(ARGS) {
+    return guarded(n, 7, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]), v = tensor_arg(a[2]);
+        const Sight s = sight_arg(a + 3);
+        return wrapped(released([&] { return attention(q, k, v, s); }));
+    });
+}
+PyObject* py_attention_step(ARGS) {
+    return guarded(n, 7, [&] {
+        const Tensor q = tensor_arg(a[0]), k = tensor_arg(a[1]), v = tensor_arg(a[2]);
+        const Sight s = sight_arg(a + 3);
+        return wrapped(released([&] { return attention_step(q, k, v, s); }));
+    });
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {METHOD(norm_forward),    METHOD(norm_backward),  METHOD(norm),  METHOD(linear_forward), METHOD(linear_backward),
-                          METHOD(linear),          METHOD(gated_forward),  METHOD(gated_backward), METHOD(gated), {nullptr, nullptr, 0, nullptr}};
+                          METHOD(linear),          METHOD(gated_forward),  METHOD(gated_backward), METHOD(gated),
+                          METHOD(dropout_forward), METHOD(dropout_backward), METHOD(dropout), METHOD(rotary_forward), METHOD(rotary_backward),
+                          METHOD(rotary),          METHOD(rotary_step),    METHOD(attention_forward), METHOD(attention_backward), METHOD(attention),
+                          METHOD(attention_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_layers", "Native calls of paper_2607_11985_gb300.layers.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
