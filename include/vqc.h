@@ -620,7 +620,8 @@ vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens,
                                   const vqc_heads* v, const void* o, const float* saved, int64_t window,
                                   int64_t sinks, double scale, const int32_t* lengths, void* grad_q, void* grad_k,
                                   void* grad_v, void* workspace, size_t workspace_bytes, void* stream);
-/* mode 0 forward, 1 backward; `aligned` 1 where all operands and their strides are multiples of 16 bytes. */
+/* mode 0 forward, 1 backward; `aligned` 1 where all operands lie on 16-byte boundaries and the strides of axes
+ * longer than one are positive multiples of 16 bytes, else 0. */
 size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads,
                                      int64_t groups, int64_t dim, int32_t aligned);
 

@@ -35,7 +35,7 @@ UNITS = ["compiler.cpp", "frames.cpp", "qasm.cpp", "capi.cu", "noalloc.cu", "hos
          "tc_stage.cu", "kernels_f32_fwd_nph.cu", "kernels_f32_bwd_nph.cu", "kernels_hbm_nph.cu",
          "kernels_f32_fused_nph.cu", "kernels_cluster_bwd.cu",
          "layers.cu", "layers_tc.cu", "layers_rows.cu", "layers_product.cu", "layer_norm.cu",
-         "dropout.cu", "norm_rotary.cu", "attention.cu", "attention_cached.cu"]
+         "dropout.cu", "norm_rotary.cu", "attention.cu", "attention_tc.cu", "attention_cached.cu"]
 
 
 def nvcc() -> str:

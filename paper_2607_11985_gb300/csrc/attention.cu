@@ -429,8 +429,8 @@ size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch
                                      int32_t aligned) {
     if ((mode != 0 && mode != 1) || checked("", dtype, batch, tokens, heads, groups, dim, 0, 0, 1.0) != VQC_OK || !grid_ok(batch, tokens, heads, dim))
         return (size_t)-1;
-    (void)aligned;
-    return mode ? saved_bytes(batch, tokens, heads) : 0;
+    const size_t copies = attention_tc_takes(dtype, dim) && mode == 0 ? attention_tc_workspace(mode, batch, tokens, heads, groups, dim, aligned != 0) : 0;
+    return copies + (mode ? saved_bytes(batch, tokens, heads) : 0);
 }
 
 vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, const vqc_heads* q,
@@ -451,6 +451,10 @@ vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, 
         a.q = heads_of(*q); a.k = heads_of(*k); a.v = heads_of(*v);
         a.o = o;
         a.saved = saved;
+        if (attention_tc_takes(dtype, dim)) {
+            const vqc_status before = layers_pending();
+            return before != VQC_OK ? before : attention_tc_forward(a, workspace, workspace ? workspace_bytes : 0, static_cast<cudaStream_t>(stream));
+        }
         const cudaError_t err = run_plain(a, 0, static_cast<cudaStream_t>(stream));
         return err == cudaSuccess ? VQC_OK : cuda_error(err, "attention launch");
     } catch (...) {

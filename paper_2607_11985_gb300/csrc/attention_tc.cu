@@ -1,0 +1,604 @@
+// attention_tc.cu -- attention on the tensor cores (tcgen05) for 16-bit types and heads of up to 128
+// elements; the formulas are those of attention.cu.
+//
+// Forward.  A CTA owns 256 queries of a head, two halves of 128 rows, and goes through the tiles of 128 keys that
+// one of them sees.  Warp 0 moves tiles of keys and values into a ring with TMA, warp 1 issues the products:
+// scores S = Q K^T into tensor memory, and O += P V with P read from tensor memory (it lies where S lay).
+// Warps 4..7 and 8..11 take the scores of one half out, a row per lane, and put the probabilities back: while one half's are
+// worked on, the tensor cores multiply the other's.  A row's running maximum is followed only when it has grown by
+// more than 2^8: P and the row's sum are relative to the followed one, and O is rescaled in tensor memory
+// then (the product that last wrote it has ended: its scores' successor was committed after it).
+//
+// P is rounded to the operands' type (one rounding of a probability, whose error averages out over the keys
+// of a row), its sum is taken before.  float16 probabilities are held times 2^6: 2^-30 of the largest.
+//
+// Every wait is bounded, as in layers_tc.cu: a warp that gives up tells the others, copies and products
+// in flight are waited for, tensor memory is freed and the error word set.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention.h"
+#include "layers_elem.cuh"
+#include "layers_tc.h"
+#include "tensor_core.cuh"
+
+namespace vqc {
+namespace layers {
+
+namespace {
+
+constexpr int N = 128;                               // queries of a half, keys of a tile
+constexpr int kThreads = 384;
+constexpr int kChunk = N * 128;                      // 128 rows of 64 elements, 128-byte swizzle
+constexpr int kBarriers = 1024;
+constexpr unsigned long long kWaitNs = 4000000000ull;   // bound of the waits for what is in flight
+constexpr float kLn2 = 0.693147180559945309f;
+
+// Which keys a query sees, in 32 bits (tokens are below 2^30; so are a window and sinks that matter).
+struct View {
+    const int32_t* lengths;
+    int tokens, window, sinks;
+    __device__ __forceinline__ int length(int b) const { return lengths ? min(max(lengths[b], 0), tokens) : tokens; }
+};
+
+struct TcAttention {
+    CUtensorMap q, k, v, g;
+    View sight;
+    void* o;
+    float* saved;
+    unsigned* err;
+    unsigned long long wait_ns;
+    int tiles, items;            // tiles of a head, of all heads of all sequences
+    float scale, scale2;
+    int heads, groups, dim, bf16;
+};
+
+// The tiles of keys that rows first..last - 1 see: [0, sinks) and [from, to); none where there are no rows.
+struct Span {
+    int sinks, from, to;
+    __device__ __forceinline__ bool has(int t) const { return t < sinks || (t >= from && t < to); }
+};
+__device__ __forceinline__ Span span_of(const View& S, int first, int last) {
+    Span r{0, 0, 0};
+    if (first >= last) return r;
+    r.to = (last + N - 1) / N;
+    r.from = max(0, first - S.window + 1) / N;
+    r.sinks = min((min(S.sinks, S.tokens) + N - 1) / N, r.from);
+    return r;
+}
+// All keys of a tile are seen by all rows first..first + N - 1 (of those that there are)?
+__device__ __forceinline__ bool all_seen(const View& S, int first, int tile) {
+    const int k0 = tile * N, k1 = k0 + N - 1;
+    return k1 <= first && (first + N - 1 - k0 < S.window || k1 < S.sinks);
+}
+
+// 2^x, zero below the smallest normal number (without that, three more instructions)
+__device__ __forceinline__ float power(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// the n lowest bits (none below 0, all from 32 on)
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
+// The pieces that every kernel here has: barriers, tensor memory, a bounded end.
+struct Roles {
+    const volatile int* gave_up;
+    unsigned long long ns;
+    // (The bound is looked at after some tries, each of which waits by itself: reading the clock takes longer than
+    // most waits here.)
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)
+            if (__all_sync(~0u, mbar_try(bar, parity))) return true;
+        return mbar_wait(bar, parity, ns, gave_up);
+    }
+};
+__device__ __forceinline__ void give_up(volatile int* flag, unsigned* err) {
+    *flag = 1;
+    *static_cast<volatile unsigned*>(err) = 1u;       // (of the host)
+    __threadfence_system();
+}
+// A ring of stages, counted.
+template <int NS> struct Ring {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == NS) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// zeros in the rows of a tile from `row` on (its chunks lie one after the other), by one warp
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int chunks, int row, int lane) {
+    for (int c = 0; c < chunks; ++c)
+        for (int i = row * 8 + lane; i < N * 8; i += 32) *reinterpret_cast<uint4*>(tile + c * kChunk + i * 16) = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    __syncwarp();
+}
+
+// A warp's 32 rows x 64 elements (a row per lane, packed) to memory by way of shared memory, so that eight lanes
+// write 128 bytes of a row: straight from the lanes a store touches 32 lines, 4100 cycles for a CTA's output.
+// Piece c (16 bytes) of row r lies at place c ^ (r % 8).  `rows`: rows that exist; `cols`: elements that exist.
+__device__ __forceinline__ void rows_out(unsigned char* stage, const uint32_t (&w)[32], char* to, int64_t pitch, int rows, int cols, int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<uint4*>(stage + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    __syncwarp();
+    const int c = lane & 7;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        if (r < rows && 8 * c < cols)
+            *reinterpret_cast<uint4*>(to + r * pitch + 16 * c) = *reinterpret_cast<const uint4*>(stage + r * 128 + ((c ^ (r & 7)) << 4));
+    }
+}
+
+// C chunks of 64 elements in a head.  Stage i of the ring holds the values of tile i - 1 and the keys of
+// tile i, which are used one after the other.
+template <int C> struct ForwardShape {
+    static constexpr int kTile = C * kChunk;
+    static constexpr int kStages = C == 1 ? 4 : 2;
+    static constexpr int kOut = (2 + 2 * kStages) * kTile;      // where the warps' outputs are turned
+    static constexpr int kSmem = kOut + 8 * 4096 + kBarriers;
+};
+
+// 256 queries of a head of a sequence.
+struct Place {
+    int b, head, q0, length;
+};
+// The n-th of a CTA: long ones first, and every second round of CTAs in the other order.
+__device__ __forceinline__ bool place_of(const TcAttention& A, int n, int rows, Place& w) {
+    const int64_t i = (int64_t)n * gridDim.x + (n & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (i >= A.items) return false;
+    const int plane = A.items / A.tiles, tile = A.tiles - 1 - (int)i / plane, which = (int)i % plane;
+    w.b = which / A.heads;
+    w.head = which - w.b * A.heads;
+    w.length = A.sight.length(w.b);
+    w.q0 = tile * rows;
+    return true;
+}
+// The tiles that one of its halves sees: [0, sinks) and [from, to).
+struct Item : Place {
+    int group, sinks, from, count;
+    Span half[2];
+    __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : from + i - sinks; }
+};
+__device__ __forceinline__ bool item_of(const TcAttention& A, int n, Item& w) {
+    if (!place_of(A, n, 2 * N, w)) return false;
+    w.group = w.head / (A.heads / A.groups);
+    for (int h = 0; h < 2; ++h) w.half[h] = span_of(A.sight, w.q0 + h * N, min(w.q0 + (h + 1) * N, w.length));
+    const int to = max(w.half[0].to, w.half[1].to);
+    w.from = w.half[0].from;
+    w.sinks = min(max(w.half[0].sinks, w.half[1].sinks), w.from);
+    w.count = to ? w.sinks + to - w.from : 0;
+    return true;
+}
+
+template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forward_tc(const __grid_constant__ TcAttention A) {
+    using L = ForwardShape<C>;
+    constexpr int NS = L::kStages;
+    constexpr float kShift = std::is_same<T, __nv_bfloat16>::value ? 0.f : 6.f, kGrowth = 8.f;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::kOut + 8 * 4096);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, qfull = empty + 8 * NS, qempty = qfull + 16, sfull = qempty + 16, ready = sfull + 16,
+                   ofull = ready + 32, drain = ofull + 16;
+    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 14);
+    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 15);
+    volatile int* turn = reinterpret_cast<volatile int*>(bars + 2 * NS + 16);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t base = smem_u32(sm), ring = base + 2 * L::kTile;
+
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 2);
+        }
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(qfull + 8 * h, 1);
+            mbar_init(qempty + 8 * h, 1);
+            mbar_init(sfull + 8 * h, 1);
+            mbar_init(ready + 16 * h, 4);
+            mbar_init(ready + 16 * h + 8, 4);
+            mbar_init(ofull + 8 * h, 1);
+            mbar_init(drain + 8 * h, 1);
+        }
+        *gave_up = 0;
+        *turn = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        tma_prefetch(&A.q);
+        tma_prefetch(&A.k);
+        tma_prefetch(&A.v);
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tslot)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tslot;
+    stream_order();
+
+    const Roles R{gave_up, A.wait_ns};
+    const bool issuer = elect_one();
+    uint32_t asked = 0, queries[2] = {0, 0};      // stages and halves asked for
+    bool issued = false;
+    if (warp == 0) {
+        Ring<NS> r;
+        Item w;
+        bool ok = true;
+        for (int n = 0; ok && item_of(A, n, w); ++n) {
+            if (!w.count) continue;
+            for (int h = 0; ok && h < 2; ++h) {
+                if (!w.half[h].to) continue;
+                ok = R.wait(qempty + 8 * h, (queries[h] & 1) ^ 1);
+                if (!ok) break;
+                if (issuer) {
+                    mbar_expect(qfull + 8 * h, L::kTile);
+                    for (int c = 0; c < C; ++c)
+                        tma_load4(base + h * L::kTile + c * kChunk, &A.q, 64 * c, w.q0 + h * N, w.head, w.b, qfull + 8 * h);
+                }
+                ++queries[h];
+            }
+            for (int i = 0; ok && i <= w.count; ++i) {
+                ok = R.wait(empty + 8 * r.slot, r.phase ^ 1);
+                if (!ok) break;
+                if (issuer) {
+                    const uint32_t values = ring + r.slot * 2 * L::kTile, bar = full + 8 * r.slot;
+                    mbar_expect(bar, (i > 0 && i < w.count ? 2 : 1) * L::kTile);
+                    if (i < w.count)
+                        for (int c = 0; c < C; ++c) tma_load4(values + L::kTile + c * kChunk, &A.k, 64 * c, w.tile(i) * N, w.group, w.b, bar);
+                    if (i > 0)
+                        for (int c = 0; c < C; ++c) tma_load4(values + c * kChunk, &A.v, 64 * c, w.tile(i - 1) * N, w.group, w.b, bar);
+                }
+                ++asked;
+                r.next();
+            }
+        }
+        let_next();
+        if (!ok && issuer) give_up(gave_up, A.err);
+    } else if (warp == 1 || warp == 3) {
+        // A warp per half: issuing a product and waiting takes its time, which the other's products fill.
+        constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u << 7 | 1u << 10 : 0u;
+        const uint32_t scores = 1u << 4 | kType | (uint32_t)(N >> 3) << 17 | (uint32_t)(N >> 4) << 24;
+        const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
+        const int h = warp >> 1;
+        const uint32_t ts = tmem + h * N, to_o = tmem + 2 * N + h * 64 * C;
+        const uint64_t dq = smem_desc(base + h * L::kTile, 0);
+        // The products of the halves take turns: mixed, both halves' scores would come at one time, and the tensor
+        // cores would stand still while both are worked on (4100 cycles a tile and half in the place of 3200).
+        // Nothing but the time depends on it: who has not got its turn after some tries goes on.
+        auto take_turn = [&]() {
+            if (issuer)
+                for (int tries = 0; tries < 2000 && atomicCAS_block(const_cast<int*>(turn), 0, 1); ++tries) {}
+            __syncwarp();
+        };
+        Ring<NS> r;
+        uint32_t taken = 0;
+        Item w;
+        bool ok = true;
+        for (int n = 0; ok && item_of(A, n, w); ++n) {
+            if (!w.count) continue;
+            const Span mine = w.half[h];
+            if (mine.to) {
+                ok = R.wait(qfull + 8 * h, queries[h] & 1);
+                ++queries[h];
+            }
+            const int tail = w.length < A.sight.tokens ? w.length % N : 0;      // rows behind the sequence: values there are not read
+            bool before = false, any = false;      // the last tile was of this half, a tile was
+            for (int i = 0; ok && i <= w.count; ++i) {
+                const bool now = i < w.count && mine.has(w.tile(i));
+                ok = R.wait(full + 8 * r.slot, r.phase);
+                if (!ok) break;
+                const uint32_t values = ring + r.slot * 2 * L::kTile;
+                if (before) {
+                    if (tail && w.tile(i - 1) == w.length / N) clear_rows(sm + (2 + 2 * r.slot) * L::kTile, C, tail, lane);   // (one half sees it)
+                    const uint64_t dv = smem_desc(values, kChunk);
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        ok = R.wait(ready + 16 * h + 8 * part, taken & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (part == 0) take_turn();
+                        if (issuer) {
+#pragma unroll
+                            for (int j = part * N / 32; j < (part + 1) * N / 32; ++j) mma_rows(to_o, ts + 8 * j, dv + j * (2048 >> 4), outputs, any || j > 0);
+                        }
+                    }
+                    if (!ok) break;
+                    ++taken;
+                    any = true;
+                } else {
+                    tc_fence_after();
+                    if (now) take_turn();
+                }
+                if (issuer) {
+                    if (now) {
+                        const uint64_t dk = smem_desc(values + L::kTile, 0);
+#pragma unroll
+                        for (int j = 0; j < 4 * C; ++j) {
+                            const uint32_t step = (j / 4 * kChunk + j % 4 * 32) >> 4;
+                            mma<1>(ts, dq + step, dk + step, scores, j > 0);
+                        }
+                        mma_commit<1>(sfull + 8 * h);
+                        if (w.tile(i) == mine.to - 1) mma_commit<1>(qempty + 8 * h);
+                    } else if (before && w.tile(i - 1) == mine.to - 1) {
+                        mma_commit<1>(ofull + 8 * h);
+                    }
+                    if (now || before) mma_commit<1>(empty + 8 * r.slot);
+                    else mbar_arrive(empty + 8 * r.slot);
+                    *turn = 0;
+                }
+                issued = issued || now;
+                before = now;
+                r.next();
+            }
+        }
+        if (!ok && issuer) give_up(gave_up, A.err);
+    } else if (warp >= 4) {
+        const int h = (warp - 4) >> 2, quad = warp & 3;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16, scores = tmem + lanes + h * N, outputs = tmem + lanes + 2 * N + h * 64 * C;
+        unsigned char* stage = sm + L::kOut + (warp - 4) * 4096;
+        uint32_t tiles = 0, outs = 0;      // so far
+        bool ok = true;
+        Place w;
+        for (int n = 0; ok && place_of(A, n, 2 * N, w); ++n) {
+            const int first = w.q0 + h * N, row0 = first + quad * 32, row = row0 + lane;
+            const Span mine = span_of(A.sight, first, min(first + N, w.length));
+            float followed = -INFINITY;        // the maximum that P is relative to, in powers of two
+            float2 total = make_float2(0.f, 0.f);
+            bool any = false;
+            for (int t = mine.sinks ? 0 : mine.from; t < mine.to; t = t + 1 == mine.sinks ? mine.from : t + 1) {
+                ok = R.wait(sfull + 8 * h, tiles & 1);
+                if (!ok) break;
+                ++tiles;
+                tc_fence_after();
+                uint32_t s[N];
+#pragma unroll
+                for (int c = 0; c < N; c += 32) tmem_ld32(scores + c, s + c);
+                tmem_wait();
+                if (!all_seen(A.sight, first, t)) {
+                    // seen: columns up to `near`, and of these the ones after `far` or before `open`, as bits
+                    const int near = row - t * N, far = near - A.sight.window, open = A.sight.sinks - t * N;
+#pragma unroll
+                    for (int c = 0; c < N; c += 32) {
+                        const uint32_t bits = low_bits(near + 1 - c) & (~low_bits(far + 1 - c) | low_bits(open - c));
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[c + e] = bits & 1u << e ? s[c + e] : 0xff800000u;
+                    }
+                }
+                float most[4] = {__uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2]), __uint_as_float(s[3])};
+#pragma unroll
+                for (int c = 4; c < N; c += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most[e] = c + 4 + e < N ? fmaxf(fmaxf(most[e], __uint_as_float(s[c + e])), __uint_as_float(s[c + 4 + e]))
+                                                                        : fmaxf(most[e], __uint_as_float(s[c + e]));
+                const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * A.scale2;
+                if (__any_sync(~0u, top > followed + kGrowth)) {
+                    const float now = fmaxf(top, followed), shrink = power(followed - (now == -INFINITY ? 0.f : now));
+                    followed = now;
+                    total.x *= shrink;
+                    total.y *= shrink;
+                    if (any) {
+#pragma unroll 1
+                        for (int c = 0; c < 64 * C; c += 16) {
+                            float o[16];
+                            tmem_ld(outputs + c, o);
+                            tmem_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] *= shrink;
+                            tmem_st(outputs + c, o);
+                        }
+                    }
+                }
+                any = true;
+                const float less = followed == -INFINITY ? 0.f : kShift - followed;
+                const float2 scale = make_float2(A.scale2, A.scale2), minus = make_float2(less, less);
+                // in two parts, the first of which is multiplied while the second is computed
+#pragma unroll
+                for (int c = 0; c < N; c += 64) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        float2 x = fma2(make_float2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, minus);
+                        x.x = power(x.x);
+                        x.y = power(x.y);
+                        total = add2(total, x);
+                        p[e / 2] = pack2<T>(x.x, x.y);
+                    }
+                    tmem_st32(scores + c / 2, p);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(ready + 16 * h + c / 8);
+                }
+            }
+            if (!ok) break;
+            if (any) {
+                ok = R.wait(ofull + 8 * h, outs & 1);
+                if (!ok) break;
+                ++outs;
+                tc_fence_after();
+            }
+            const float sum = total.x + total.y;
+            const bool in = row < w.length;
+            const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+            const int rows = min(32, A.sight.tokens - row0);
+            T* to_row = static_cast<T*>(A.o) + (((int64_t)w.b * A.sight.tokens + row0) * A.heads + w.head) * (int64_t)A.dim;
+            const int64_t pitch = (int64_t)A.heads * A.dim;
+#pragma unroll 1
+            for (int c = 0; c < 64 * C; c += 64) {
+                uint32_t o[64], packed[32];
+                tmem_ld32(outputs + c, o);      // (whatever it holds, where the half has no rows)
+                tmem_ld32(outputs + c + 32, o + 32);
+                tmem_wait();
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    const bool real = any && in;
+                    packed[e / 2] = pack2<T>(real ? __uint_as_float(o[e]) * inverse : 0.f, real ? __uint_as_float(o[e + 1]) * inverse : 0.f);
+                }
+                if (A.dim % 8 == 0) {
+                    rows_out(stage, packed, reinterpret_cast<char*>(to_row + c), pitch * 2, rows, A.dim - c, lane);
+                } else if (lane < rows) {
+                    T* to = to_row + lane * pitch + c;
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (c + e < A.dim) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(packed[e / 2] >> 16 * (e & 1));
+                }
+            }
+            if (A.saved && lane < rows)
+                A.saved[((int64_t)w.b * A.heads + w.head) * A.sight.tokens + row] = in ? (followed - kShift + log2f(sum)) * kLn2 : -INFINITY;
+        }
+        if (!ok && lane == 0) give_up(gave_up, A.err);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (*gave_up) {
+        if ((warp == 1 || warp == 3) && issued) {
+            if (issuer) mma_commit<1>(drain + 8 * (warp >> 1));
+            mbar_wait(drain + 8 * (warp >> 1), 0, kWaitNs, nullptr);
+        }
+        if (warp == 0) {
+            for (int h = 0; h < 2; ++h)
+                if (queries[h]) mbar_wait(qfull + 8 * h, (queries[h] - 1) & 1, kWaitNs, nullptr);
+            for (uint32_t a = asked > NS ? asked - NS : 0; a < asked; ++a)
+                if (!mbar_wait(full + 8 * (a % NS), a / NS & 1, kWaitNs, nullptr)) break;
+        }
+        __syncthreads();
+    }
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// Map of heads [batch, tokens, heads, dim]: boxes of 64 elements x 128 tokens of one head.
+bool make_map(CUtensorMap* m, const Heads& h, int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+    EncodeTiled enc = encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)batch};
+    // (the stride of an axis of one is not used: any that the driver takes)
+    const cuuint64_t strides[3] = {(cuuint64_t)(tokens > 1 ? h.token * 2 : 16), (cuuint64_t)(heads > 1 ? h.head * 2 : 16), (cuuint64_t)(batch > 1 ? h.batch * 2 : 16)};
+    const cuuint32_t boxes[4] = {64, N, 1, 1}, one[4] = {1, 1, 1, 1};
+    return enc(m, dtype == VQC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(h.p), dims, strides, boxes, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Heads that TMA cannot read in place (rows off 16-byte boundaries, or one place of memory for several tokens,
+// heads or sequences) are copied: dense, rows of a multiple of 8 elements.
+struct CopyJob {
+    Heads from;
+    uint16_t* to;
+    int64_t rows;      // batch * tokens * heads
+    int heads;
+};
+struct CopyJobs {
+    CopyJob j[4];
+    int64_t tokens;
+    int dim, padded;
+};
+__global__ void __launch_bounds__(256) copy_heads_kernel(const __grid_constant__ CopyJobs J) {
+    stream_order();
+    const CopyJob& A = J.j[blockIdx.y];
+    const int across = J.padded / 8;
+    const int64_t count = A.rows * across, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < count; e += step) {
+        const int64_t row = e / across, bt = row / A.heads, b = bt / J.tokens;
+        const int c = (int)(e - row * across) * 8;
+        const uint16_t* p = static_cast<const uint16_t*>(A.from.p) + b * A.from.batch + (bt - b * J.tokens) * A.from.token + (row - bt * A.heads) * A.from.head + c;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (c + 2 * i < J.dim ? (uint32_t)p[2 * i] : 0u) | (c + 2 * i + 1 < J.dim ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+        *reinterpret_cast<uint4*>(A.to + row * J.padded + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+int64_t padded(int64_t dim) { return (dim + 7) / 8 * 8; }
+bool in_place(const Heads& h, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+    constexpr int64_t kMost = int64_t(1) << 38;      // elements: strides of maps have 40 bits of bytes
+    return dim % 8 == 0 && heads_on(h, 2, 16) && (tokens == 1 || h.token > 0) && (heads == 1 || h.head > 0) && (batch == 1 || h.batch > 0) && h.token < kMost &&
+           h.head < kMost && h.batch < kMost;
+}
+size_t copy_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t dim) { return align256((size_t)(batch * tokens * heads) * padded(dim) * 2); }
+
+// Maps of the operands, after copies of those that need one into `ws`.
+vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* heads, CUtensorMap* const* map, int count, char* ws, size_t bytes, cudaStream_t s) {
+    CopyJobs jobs{};
+    jobs.tokens = a.sight.tokens;
+    jobs.dim = a.dim;
+    jobs.padded = (int)padded(a.dim);
+    int copies = 0;
+    int64_t rows = 0;
+    for (int i = 0; i < count; ++i) {
+        Heads h = *from[i];
+        int64_t dim = a.dim;
+        if (!in_place(h, a.batch, a.sight.tokens, heads[i], a.dim)) {
+            const size_t need = copy_bytes(a.batch, a.sight.tokens, heads[i], a.dim);
+            if (need > bytes) return set_error(VQC_ERR_WORKSPACE, "attention: workspace too small");
+            CopyJob& j = jobs.j[copies++];
+            j = {h, reinterpret_cast<uint16_t*>(ws), a.batch * a.sight.tokens * heads[i], heads[i]};
+            dim = jobs.padded;
+            h = {ws, a.sight.tokens * heads[i] * dim, heads[i] * dim, dim};
+            rows = std::max(rows, j.rows);
+            ws += need;
+            bytes -= need;
+        }
+        if (!make_map(map[i], h, a.dtype, a.batch, a.sight.tokens, heads[i], dim)) return set_error(VQC_ERR_CUDA, "attention: a tensor map was refused");
+    }
+    if (!copies) return VQC_OK;
+    void* args[] = {&jobs};
+    const int64_t blocks = std::min<int64_t>(ceil_div(rows * (jobs.padded / 8), 256), 8LL * sm_count());
+    const cudaError_t e = launch((const void*)copy_heads_kernel, dim3((unsigned)blocks, copies), 256, args, s);
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "copy launch");
+}
+
+vqc_status start(const AttentionArgs& a, TcAttention& t) {
+    t.sight = {a.sight.lengths, (int)a.sight.tokens, (int)a.sight.window, (int)a.sight.sinks};
+    t.scale = a.scale;
+    t.scale2 = a.scale2;
+    t.heads = a.heads; t.groups = a.groups; t.dim = a.dim;
+    t.bf16 = a.dtype == VQC_BF16;
+    t.wait_ns = wait_limit();
+    const cudaError_t e = error_word(&t.err);
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "error word");
+}
+
+template <typename T, int C> cudaError_t launch_forward(const TcAttention& t, unsigned grid, cudaStream_t s) {
+    void* args[] = {const_cast<TcAttention*>(&t)};
+    return launch((const void*)forward_tc<T, C>, dim3(grid), kThreads, args, s, ForwardShape<C>::kSmem);
+}
+
+}  // namespace
+
+bool attention_tc_takes(int dtype, int64_t dim) { return dtype != VQC_F32 && dim <= 128; }
+
+size_t attention_tc_workspace(int mode, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, bool aligned) {
+    if (aligned && dim % 8 == 0) return 0;
+    const size_t q = copy_bytes(batch, tokens, heads, dim), k = copy_bytes(batch, tokens, groups, dim);
+    return mode ? 2 * q + 2 * k : q + 2 * k;
+}
+
+vqc_status attention_tc_forward(const AttentionArgs& a, void* ws, size_t bytes, cudaStream_t s) {
+    TcAttention t{};
+    vqc_status st = start(a, t);
+    if (st != VQC_OK) return st;
+    const Heads* from[3] = {&a.q, &a.k, &a.v};
+    const int heads[3] = {a.heads, a.groups, a.groups};
+    CUtensorMap* map[3] = {&t.q, &t.k, &t.v};
+    st = maps_of(a, from, heads, map, 3, static_cast<char*>(ws), bytes, s);
+    if (st != VQC_OK) return st;
+    t.o = a.o;
+    t.saved = a.saved;
+    t.tiles = (int)ceil_div(a.sight.tokens, 2 * N);
+    t.items = (int)(t.tiles * a.batch * a.heads);
+    const unsigned grid = (unsigned)std::min<int64_t>(t.items, sm_count());
+    const cudaError_t e = t.bf16 ? (a.dim <= 64 ? launch_forward<__nv_bfloat16, 1>(t, grid, s) : launch_forward<__nv_bfloat16, 2>(t, grid, s))
+                                 : (a.dim <= 64 ? launch_forward<__half, 1>(t, grid, s) : launch_forward<__half, 2>(t, grid, s));
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "attention launch");
+}
+
+}  // namespace layers
+}  // namespace vqc

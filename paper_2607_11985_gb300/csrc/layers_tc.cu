@@ -51,6 +51,7 @@
 
 #include "layers_elem.cuh"
 #include "layers_tc.h"
+#include "tensor_core.cuh"
 
 namespace vqc {
 namespace layers {
@@ -117,129 +118,6 @@ constexpr int pairs_of(int parts) { return parts == 3 ? 6 : parts; }
 // Products of parts of float operands, small ones first: parts of a and b, 2 bits each.
 constexpr unsigned kOrderA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 constexpr unsigned kOrderB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t at_cta(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;\n" : "=l"(t));
-    return t;
-}
-// true in one lane of a converged warp
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(r));
-    return r != 0;
-}
-template <bool B> struct Flag {
-    static constexpr bool value = B;
-};
-__device__ __forceinline__ void mbar_init(uint32_t mbar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(mbar), "r"(count) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t mbar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n"
-        : "=r"(done)
-        : "r"(mbar), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-
-// Bounded wait for a phase; false when it ran out or another role gave up.  Lanes may see the end
-// at different times: the warp goes by what all of them saw.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t mbar, uint32_t parity, unsigned long long ns, const volatile int* gave_up) {
-    const unsigned long long end = now_ns() + ns;
-    while (!mbar_try(mbar, parity))      // (which itself waits for some time)
-        if ((gave_up && *gave_up) || now_ns() > end) return false;
-    return true;
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t mbar, uint32_t parity, unsigned long long ns, const volatile int* gave_up) {
-    return __all_sync(~0u, mbar_try(mbar, parity) || mbar_wait_slow(mbar, parity, ns, gave_up));
-}
-
-// a word of the shared memory of another CTA of the cluster
-__device__ __forceinline__ uint32_t peer_word(uint32_t addr, uint32_t rank) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(at_cta(addr, rank)) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ void tma_prefetch(const CUtensorMap* m) {
-    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
-}
-// One box at (x, y) into this CTA's shared memory; `mbar` may be the pair's first CTA's.
-template <int CG> __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t mbar) {
-    if (CG == 2)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
-            "%3}], [%4];\n" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(mbar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(
-                dst),
-            "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(mbar)
-            : "memory");
-}
-
-// Shared-memory matrix descriptor, 128-byte swizzle: start, leading byte offset
-// (between chunks of 64 outer elements; unused along k), stride byte offset
-// (between groups of 8 rows of 128 bytes), version 1.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo) {
-    return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
-template <int CG> __device__ __forceinline__ void mma(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, int accumulate) {
-    if (CG == 2)
-        asm volatile(
-            "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem),
-            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-            : "memory");
-}
-// One arrival at the barrier (of both CTAs of a pair) once all products issued so far are done.
-template <int CG> __device__ __forceinline__ void mma_commit(uint32_t mbar) {
-    if (CG == 2)
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(mbar),
-            "h"((uint16_t)3)
-            : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(mbar) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
-
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
-        "%12, %13, %14, %15}, [%16];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 
 // 32 bytes at a 32-byte boundary
 __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
@@ -874,6 +752,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_kernel(const __grid_constant__
     }
 }
 
+}  // namespace
+
 // Nanoseconds after which a wait gives up: VQC_WAIT_NS of the environment, or 4 s.
 unsigned long long wait_limit() {
     static const unsigned long long ns = [] {
@@ -886,8 +766,10 @@ unsigned long long wait_limit() {
 
 // A word per device that a kernel sets when it gave up, in memory of the host, where every later call
 // looks at it for nothing.
+namespace {
 constexpr int kDevices = 64;
 std::atomic<unsigned*> g_words{nullptr};
+}  // namespace
 
 cudaError_t error_word(unsigned** p) {
     int dev = 0;
@@ -914,6 +796,8 @@ cudaError_t error_word(unsigned** p) {
     }
     return cudaHostGetDevicePointer(reinterpret_cast<void**>(p), words + dev, 0);
 }
+
+namespace {
 // the current device's word as the host reads it, or NULL where no product has run
 volatile unsigned* host_word() {
     unsigned* words = g_words.load();
@@ -1004,9 +888,7 @@ template <int kParts> __global__ void __launch_bounds__(256) copy_kernel(const _
     }
 }
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+}  // namespace
 
 EncodeTiled encode_tiled() {
     static std::atomic<void*> fn{nullptr};
@@ -1020,6 +902,8 @@ EncodeTiled encode_tiled() {
     }
     return reinterpret_cast<EncodeTiled>(p);
 }
+
+namespace {
 
 // Map of an operand with `outer` rows of the outer index: boxes of 64 contracted
 // elements x `box` rows, or of 64 outer elements x 64 contracted where the outer

@@ -406,7 +406,9 @@ Sight sight_of(const HeadRows& q, int64_t groups, const Sight& s) {
 }
 bool on16(const HeadRows& r) {
     const int64_t n = r.code == VQC_F32 ? 4 : 8;
-    return aligned({r.h.data}) && r.h.batch_stride % n == 0 && r.h.token_stride % n == 0 && r.h.head_stride % n == 0;
+    bool on = aligned({r.h.data});
+    for (int i = 0; i < 3; ++i) on = on && r.t.stride(i) % n == 0 && (r.t.stride(i) > 0 || r.t.size(i) == 1);
+    return on;
 }
 std::pair<Tensor, Tensor> attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Sight& given, bool save) {
     const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v");
