@@ -188,14 +188,13 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
                    ofull = ready + 32, drain = ofull + 16;
     volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 14);
     uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 15);
-    volatile int* turn = reinterpret_cast<volatile int*>(bars + 2 * NS + 16);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = smem_u32(sm), ring = base + 2 * L::kTile;
 
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) {
             mbar_init(full + 8 * i, 1);
-            mbar_init(empty + 8 * i, 2);
+            mbar_init(empty + 8 * i, 1);
         }
         for (int h = 0; h < 2; ++h) {
             mbar_init(qfull + 8 * h, 1);
@@ -204,10 +203,9 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
             mbar_init(ready + 16 * h, 4);
             mbar_init(ready + 16 * h + 8, 4);
             mbar_init(ofull + 8 * h, 1);
-            mbar_init(drain + 8 * h, 1);
         }
+        mbar_init(drain, 1);
         *gave_up = 0;
-        *turn = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         tma_prefetch(&A.q);
         tma_prefetch(&A.k);
@@ -261,80 +259,68 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
         }
         let_next();
         if (!ok && issuer) give_up(gave_up, A.err);
-    } else if (warp == 1 || warp == 3) {
-        // A warp per half: issuing a product and waiting takes its time, which the other's products fill.
+    } else if (warp == 1) {
+        // Strictly one half after the other: while one's scores are worked on, the other's are multiplied.  One thread
+        // issues all products: with a warp per half, committed products were seen unfinished.
         constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u << 7 | 1u << 10 : 0u;
         const uint32_t scores = 1u << 4 | kType | (uint32_t)(N >> 3) << 17 | (uint32_t)(N >> 4) << 24;
         const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
-        const int h = warp >> 1;
-        const uint32_t ts = tmem + h * N, to_o = tmem + 2 * N + h * 64 * C;
-        const uint64_t dq = smem_desc(base + h * L::kTile, 0);
-        // The products of the halves take turns: mixed, both halves' scores would come at one time, and the tensor
-        // cores would stand still while both are worked on (4100 cycles a tile and half in the place of 3200).
-        // Nothing but the time depends on it: who has not got its turn after some tries goes on.
-        auto take_turn = [&]() {
-            if (issuer)
-                for (int tries = 0; tries < 2000 && atomicCAS_block(const_cast<int*>(turn), 0, 1); ++tries) {}
-            __syncwarp();
-        };
         Ring<NS> r;
-        uint32_t taken = 0;
+        uint32_t taken[2] = {0, 0};
         Item w;
         bool ok = true;
         for (int n = 0; ok && item_of(A, n, w); ++n) {
             if (!w.count) continue;
-            const Span mine = w.half[h];
-            if (mine.to) {
-                ok = R.wait(qfull + 8 * h, queries[h] & 1);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!w.half[h].to) continue;
+                ok = ok && R.wait(qfull + 8 * h, queries[h] & 1);
                 ++queries[h];
             }
             const int tail = w.length < A.sight.tokens ? w.length % N : 0;      // rows behind the sequence: values there are not read
-            bool before = false, any = false;      // the last tile was of this half, a tile was
+            bool before[2] = {false, false}, any[2] = {false, false};      // the last tile was of this half, a tile was
             for (int i = 0; ok && i <= w.count; ++i) {
-                const bool now = i < w.count && mine.has(w.tile(i));
                 ok = R.wait(full + 8 * r.slot, r.phase);
                 if (!ok) break;
+                tc_fence_after();
                 const uint32_t values = ring + r.slot * 2 * L::kTile;
-                if (before) {
-                    if (tail && w.tile(i - 1) == w.length / N) clear_rows(sm + (2 + 2 * r.slot) * L::kTile, C, tail, lane);   // (one half sees it)
-                    const uint64_t dv = smem_desc(values, kChunk);
+                const uint64_t dv = smem_desc(values, kChunk), dk = smem_desc(values + L::kTile, 0);
+                if (i > 0 && tail && w.tile(i - 1) == w.length / N) clear_rows(sm + (2 + 2 * r.slot) * L::kTile, C, tail, lane);
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        ok = R.wait(ready + 16 * h + 8 * part, taken & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (part == 0) take_turn();
-                        if (issuer) {
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t ts = tmem + h * N, to_o = tmem + 2 * N + h * 64 * C;
+                    const bool now = i < w.count && w.half[h].has(w.tile(i));
+                    if (before[h]) {
 #pragma unroll
-                            for (int j = part * N / 32; j < (part + 1) * N / 32; ++j) mma_rows(to_o, ts + 8 * j, dv + j * (2048 >> 4), outputs, any || j > 0);
+                        for (int part = 0; part < 2; ++part) {
+                            ok = ok && R.wait(ready + 16 * h + 8 * part, taken[h] & 1);
+                            tc_fence_after();
+                            if (issuer && ok) {
+#pragma unroll
+                                for (int j = part * N / 32; j < (part + 1) * N / 32; ++j) mma_rows(to_o, ts + 8 * j, dv + j * (2048 >> 4), outputs, any[h] || j > 0);
+                            }
+                        }
+                        ++taken[h];
+                        any[h] = true;
+                    }
+                    if (issuer && ok) {
+                        if (now) {
+                            const uint64_t dq = smem_desc(base + h * L::kTile, 0);
+#pragma unroll
+                            for (int j = 0; j < 4 * C; ++j) {
+                                const uint32_t step = (j / 4 * kChunk + j % 4 * 32) >> 4;
+                                mma<1>(ts, dq + step, dk + step, scores, j > 0);
+                            }
+                            mma_commit<1>(sfull + 8 * h);
+                            if (w.tile(i) == w.half[h].to - 1) mma_commit<1>(qempty + 8 * h);
+                        } else if (before[h] && w.tile(i - 1) == w.half[h].to - 1) {
+                            mma_commit<1>(ofull + 8 * h);
                         }
                     }
-                    if (!ok) break;
-                    ++taken;
-                    any = true;
-                } else {
-                    tc_fence_after();
-                    if (now) take_turn();
+                    before[h] = now;
                 }
-                if (issuer) {
-                    if (now) {
-                        const uint64_t dk = smem_desc(values + L::kTile, 0);
-#pragma unroll
-                        for (int j = 0; j < 4 * C; ++j) {
-                            const uint32_t step = (j / 4 * kChunk + j % 4 * 32) >> 4;
-                            mma<1>(ts, dq + step, dk + step, scores, j > 0);
-                        }
-                        mma_commit<1>(sfull + 8 * h);
-                        if (w.tile(i) == mine.to - 1) mma_commit<1>(qempty + 8 * h);
-                    } else if (before && w.tile(i - 1) == mine.to - 1) {
-                        mma_commit<1>(ofull + 8 * h);
-                    }
-                    if (now || before) mma_commit<1>(empty + 8 * r.slot);
-                    else mbar_arrive(empty + 8 * r.slot);
-                    *turn = 0;
-                }
-                issued = issued || now;
-                before = now;
+                if (issuer && ok) mma_commit<1>(empty + 8 * r.slot);
+                issued = true;
                 r.next();
             }
         }
@@ -455,15 +441,15 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
         }
         if (!ok && lane == 0) give_up(gave_up, A.err);
     }
+    if (warp == 1 && issued) {      // nothing is in flight when tensor memory goes back
+        if (issuer) mma_commit<1>(drain);
+        mbar_wait(drain, 0, kWaitNs, nullptr);
+    }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (*gave_up) {
-        if ((warp == 1 || warp == 3) && issued) {
-            if (issuer) mma_commit<1>(drain + 8 * (warp >> 1));
-            mbar_wait(drain + 8 * (warp >> 1), 0, kWaitNs, nullptr);
-        }
         if (warp == 0) {
             for (int h = 0; h < 2; ++h)
                 if (queries[h]) mbar_wait(qfull + 8 * h, (queries[h] - 1) & 1, kWaitNs, nullptr);
