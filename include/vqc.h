@@ -601,7 +601,8 @@ vqc_status vqc_norm_rotary_step(vqc_real dtype, int64_t batch, int64_t tokens, i
  *   workspace vqc_attention_workspace_bytes(0, ...) bytes, 256-byte aligned.
  * Tokens from a sequence's length on are not read into any result.  Keys and values that are not finite
  * may make NaN of outputs of their sequence that do not see them.  16-bit operands: the
- * probabilities are rounded to dtype before their product with v, sums in float.
+ * probabilities are rounded to dtype before their product with v, sums in float.  Probabilities
+ * below 2^-126 count as zero.
  * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA, VQC_ERR_DEVICE_CHECK. */
 vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
                                  int64_t dim, const vqc_heads* q, const vqc_heads* k, const vqc_heads* v,
@@ -623,7 +624,7 @@ vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens,
 /* mode 0 forward, 1 backward; `aligned` 1 where all operands lie on 16-byte boundaries and the strides of axes
  * longer than one are positive multiples of 16 bytes, else 0. */
 size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads,
-                                     int64_t groups, int64_t dim, int32_t aligned);
+                                     int64_t groups, int64_t dim, int64_t window, int64_t sinks, int32_t aligned);
 
 /* Attention of the last `tokens` tokens of sequences over a cache: token t stands at position
  * lengths[b] - tokens + t and sees the keys of vqc_attention_forward at that position (lengths beyond

@@ -113,7 +113,7 @@ SIGNATURES = [
     ("vqc_attention_forward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _H, _L, _L, _D, _P, _P, _P, _P, _S, _P]),
     ("vqc_attention_backward", _I, [_I, _L, _L, _L, _L, _L, _H, _H, _H, _H, _P, _P, _L, _L, _D, _P, _P, _P, _P, _P, _S,
                                     _P]),
-    ("vqc_attention_workspace_bytes", _S, [_I, _I, _L, _L, _L, _L, _L, _I]),
+    ("vqc_attention_workspace_bytes", _S, [_I, _I, _L, _L, _L, _L, _L, _L, _L, _I]),
     ("vqc_attention_step", _I, [_I, _L, _L, _L, _L, _L, _L, _H, _H, _H, _L, _L, _D, _P, _P, _P, _S, _P]),
     ("vqc_attention_step_workspace_bytes", _S, [_L, _L, _L, _L, _L, _L, _L, _L]),
 ]
@@ -348,8 +348,8 @@ def vqc_attention_backward(dtype, batch, tokens, heads, groups, dim, grad_o, q, 
                                         stream))
 
 
-def vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, aligned):
-    return lib().vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, aligned)
+def vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, window, sinks, aligned):
+    return lib().vqc_attention_workspace_bytes(mode, dtype, batch, tokens, heads, groups, dim, window, sinks, aligned)
 
 
 def vqc_attention_step(dtype, batch, tokens, heads, groups, dim, capacity, q, cache_k, cache_v, window, sinks, scale,

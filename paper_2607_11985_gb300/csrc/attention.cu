@@ -426,11 +426,13 @@ using namespace vqc::layers;
 extern "C" {
 
 size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim,
-                                     int32_t aligned) {
-    if ((mode != 0 && mode != 1) || checked("", dtype, batch, tokens, heads, groups, dim, 0, 0, 1.0) != VQC_OK || !grid_ok(batch, tokens, heads, dim))
+                                     int64_t window, int64_t sinks, int32_t aligned) {
+    if ((mode != 0 && mode != 1) || checked("", dtype, batch, tokens, heads, groups, dim, window, sinks, 1.0) != VQC_OK || !grid_ok(batch, tokens, heads, dim))
         return (size_t)-1;
-    const size_t copies = attention_tc_takes(dtype, dim) && mode == 0 ? attention_tc_workspace(mode, batch, tokens, heads, groups, dim, aligned != 0) : 0;
-    return copies + (mode ? saved_bytes(batch, tokens, heads) : 0);
+    const Sight s = arguments(dtype, batch, tokens, heads, groups, dim, window, sinks, 1.0, nullptr).sight;
+    if (attention_tc_takes(dtype, dim))
+        return batch * tokens ? attention_tc_workspace(mode, dtype, batch, tokens, heads, groups, dim, s.window, s.sinks, aligned != 0) : 0;
+    return mode ? saved_bytes(batch, tokens, heads) : 0;
 }
 
 vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, const vqc_heads* q,
@@ -479,7 +481,9 @@ vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens,
             return set_error(VQC_ERR_INVALID_ARG, std::string(call) + ": misaligned output, lengths or workspace");
         if (!grid_ok(batch, tokens, heads, dim)) return set_error(VQC_ERR_INVALID_ARG, std::string(call) + ": sizes out of range");
         if (batch * tokens == 0 || (!grad_q && !grad_k)) return VQC_OK;
-        if (!workspace || workspace_bytes < saved_bytes(batch, tokens, heads)) return set_error(VQC_ERR_WORKSPACE, std::string(call) + ": workspace too small");
+        const bool tc = attention_tc_takes(dtype, dim);
+        if (!workspace || (!tc && workspace_bytes < saved_bytes(batch, tokens, heads)))
+            return set_error(VQC_ERR_WORKSPACE, std::string(call) + ": workspace too small");
         AttentionArgs a = arguments(dtype, batch, tokens, heads, groups, dim, window, sinks, scale, lengths);
         a.q = heads_of(*q); a.k = heads_of(*k); a.v = heads_of(*v); a.g = heads_of(*grad_o);
         a.o = const_cast<void*>(o);
@@ -487,6 +491,10 @@ vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens,
         a.d = static_cast<float*>(workspace);
         a.gq = grad_q; a.gk = grad_k; a.gv = grad_v;
         cudaStream_t s = static_cast<cudaStream_t>(stream);
+        if (tc) {
+            const vqc_status before = layers_pending();
+            return before != VQC_OK ? before : attention_tc_backward(a, workspace, workspace_bytes, s);
+        }
         cudaError_t err = rows_run_plain(a, s);
         if (err == cudaSuccess && grad_k) err = run_plain(a, 2, s);
         if (err == cudaSuccess && grad_q) err = run_plain(a, 1, s);

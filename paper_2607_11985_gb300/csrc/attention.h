@@ -29,7 +29,9 @@ constexpr int64_t kMostDim = 256;
 
 // On the tensor cores (attention_tc.cu).  `aligned`: q, k, v and the gradient, and their strides, lie on 16 bytes.
 bool attention_tc_takes(int dtype, int64_t dim);
-size_t attention_tc_workspace(int mode, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, bool aligned);
+size_t attention_tc_workspace(int mode, int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t window, int64_t sinks,
+                              bool aligned);
+vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes, cudaStream_t s);
 vqc_status attention_tc_forward(const AttentionArgs& a, void* ws, size_t bytes, cudaStream_t s);
 
 }  // namespace layers

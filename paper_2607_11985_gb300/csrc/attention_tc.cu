@@ -50,7 +50,7 @@ struct TcAttention {
     unsigned long long wait_ns;
     int tiles, items;            // tiles of a head, of all heads of all sequences
     float scale, scale2;
-    int heads, groups, dim, bf16;
+    int heads, groups, dim;
 };
 
 // The tiles of keys that rows first..last - 1 see: [0, sinks) and [from, to); none where there are no rows.
@@ -111,10 +111,10 @@ template <int NS> struct Ring {
     }
 };
 
-// zeros in the rows of a tile from `row` on (its chunks lie one after the other), by one warp
-__device__ __forceinline__ void clear_rows(unsigned char* tile, int chunks, int row, int lane) {
+// zeros in the rows of a tile from `row` on (its chunks of `rows` rows lie one after the other), by one warp
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int chunks, int rows, int row, int lane) {
     for (int c = 0; c < chunks; ++c)
-        for (int i = row * 8 + lane; i < N * 8; i += 32) *reinterpret_cast<uint4*>(tile + c * kChunk + i * 16) = make_uint4(0, 0, 0, 0);
+        for (int i = row * 8 + lane; i < rows * 8; i += 32) *reinterpret_cast<uint4*>(tile + c * rows * 128 + i * 16) = make_uint4(0, 0, 0, 0);
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     __syncwarp();
 }
@@ -285,7 +285,7 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
                 tc_fence_after();
                 const uint32_t values = ring + r.slot * 2 * L::kTile;
                 const uint64_t dv = smem_desc(values, kChunk), dk = smem_desc(values + L::kTile, 0);
-                if (i > 0 && tail && w.tile(i - 1) == w.length / N) clear_rows(sm + (2 + 2 * r.slot) * L::kTile, C, tail, lane);
+                if (i > 0 && tail && w.tile(i - 1) == w.length / N) clear_rows(sm + (2 + 2 * r.slot) * L::kTile, C, N, tail, lane);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t ts = tmem + h * N, to_o = tmem + 2 * N + h * 64 * C;
@@ -461,14 +461,485 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// Map of heads [batch, tokens, heads, dim]: boxes of 64 elements x 128 tokens of one head.
-bool make_map(CUtensorMap* m, const Heads& h, int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+// Backward.  Both kernels have one shape: 128 resident rows (queries: Q and dO; keys: K and V) and units of 64 rows of
+// the other side that stream by (X and Y: K and V, or Q and dO):
+//   S = R1 X^T, dP = R2 Y^T   (128 x 64, two buffers in tensor memory, one unit after the other)
+//   P = exp(scale S - lse), dS = P (dP - d), each put back as 16-bit elements where S and dP lay
+//   queries: dQ += dS X      keys: dK += dS X, dV += P Y
+// With keys resident S is the transposed one, so that P and dS are the left operands of their products as they
+// lie in tensor memory; lse and d of the columns come with the unit.  Warps 4..7 work on the even units,
+// 8..11 on the odd ones.  P and dS are rounded to the operands' type.  float16 holds P times 2^14 and
+// dS times the power of two that keeps its largest possible value, 2 max|dO| max|V| (row norms), below 2^15: gradients
+// of any size keep their bits.
+//
+// Keys that stay visible through a window are seen by all later queries: their tiles' far queries are cut into
+// pieces, a CTA each, whose sums are joined in their order.
+constexpr int kUnit = 64;
+constexpr int kHalf = kUnit * 128;        // 64 rows of 64 elements
+
+template <int C> struct BackShape {
+    static constexpr int kResident = 2 * C * kChunk, kStageX = C * kHalf, kStage = 2 * kStageX;
+    static constexpr int kStages = C == 2 ? 5 : 6;
+    static constexpr int kStats = kResident + kStages * kStage;      // lse and -d of 64 columns for each stage
+    static constexpr int kBars = kStats + kStages * 512;
+    static constexpr int kSmem = kBars + 256;
+};
+
+struct TcBack {
+    CUtensorMap q, k, v, g;
+    View sight;
+    const float *lse, *d;        // [batch, heads, pitch]: log2 of the sum (infinity behind a sequence), and -d
+    const float* most;           // float16: largest row norms of dO and V
+    void *gq, *gk, *gv;          // dense; for keys' tiles that are cut:
+    float* part;                 // [tile][piece][batch * groups][2][128][64 C]
+    unsigned* err;
+    unsigned long long wait_ns;
+    int64_t pitch;
+    int tiles, planes;           // of 128 resident rows; heads (groups) of all sequences
+    int cut, pieces, piece;      // keys: tiles that are cut, pieces behind the first, queries of one
+    float scale, scale2;
+    int heads, groups, dim;
+};
+
+// 2^k of float16's dS
+__device__ __forceinline__ float float16_factor(const float* most) {
+    const float bound = 2.f * sqrtf(most[0]) * sqrtf(most[1]);
+    if (!(bound > 0.f) || !(bound < 3e38f)) return 1.f;
+    int e;
+    frexpf(bound, &e);      // bound < 2^e
+    return ldexpf(1.f, 15 - e);
+}
+
+template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThreads, 1) back_tc(const __grid_constant__ TcBack A) {
+    using L = BackShape<C>;
+    constexpr int NS = L::kStages;
+    constexpr bool kF16 = !std::is_same<T, __nv_bfloat16>::value;
+    constexpr float kShift = kF16 ? 14.f : 0.f;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::kBars);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, rfull = empty + 8 * NS, sfull = rfull + 8, ready = sfull + 16, done = ready + 16, drain = done + 8;
+    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 7);
+    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 8);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t base = smem_u32(sm), ring = base + L::kResident;
+
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        mbar_init(rfull, 1);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(sfull + 8 * h, 1);
+            mbar_init(ready + 8 * h, 4);
+        }
+        mbar_init(done, 1);
+        mbar_init(drain, 1);
+        *gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        tma_prefetch(&A.q);
+        tma_prefetch(&A.k);
+        tma_prefetch(&A.v);
+        tma_prefetch(&A.g);
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tslot)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tslot;
+    stream_order();
+
+    // The CTA's tile, long ones first: queries from the end; keys: pieces of cut tiles, then the tiles from the start.
+    const int per = A.heads / A.groups, which = blockIdx.x % A.planes, row_heads = kKeys ? A.groups : A.heads;
+    int tile = blockIdx.x / A.planes, piece = 0;
+    if (kKeys) {
+        if (tile < A.cut * A.pieces) {
+            piece = 1 + tile % A.pieces;
+            tile /= A.pieces;
+        } else {
+            tile -= A.cut * A.pieces;
+        }
+    } else {
+        tile = A.tiles - 1 - tile;
+    }
+    const int b = which / row_heads, own = which - b * row_heads, length = A.sight.length(b), r0 = tile * N;
+    const bool cut = kKeys && tile < A.cut;
+    // The units: queries: keys [0, sinks) and [from, to); keys: queries [from, to), of each head of the group.
+    int sinks = 0, from = 0, to = 0;
+    if (r0 < length) {
+        if constexpr (kKeys) {
+            // past the window of all, in whole units
+            const int near = (int)min(((int64_t)r0 + N + min(A.sight.window, A.sight.tokens) + kUnit - 1) / kUnit * kUnit, (int64_t)1 << 30);
+            const bool all = (r0 < A.sight.sinks || A.sight.window > A.sight.tokens) && !cut;
+            int first = r0, last = all ? length : min(length, cut ? near : min(r0 + N, length) - 1 + A.sight.window);
+            if (piece) {
+                first = near + (piece - 1) * A.piece;
+                last = min(length, first + A.piece);
+            }
+            from = first / kUnit;
+            to = last > first ? (last + kUnit - 1) / kUnit : from;
+        } else {
+            to = (min(r0 + N, length) + kUnit - 1) / kUnit;
+            from = max(0, r0 - A.sight.window + 1) / kUnit;
+            sinks = min((min(A.sight.sinks, A.sight.tokens) + kUnit - 1) / kUnit, from);
+        }
+    }
+    const int span = sinks + to - from, units = kKeys ? span * per : span;
+    // first row of a unit, and its head
+    auto row_of = [&](int u) {
+        const int i = kKeys ? u % span : u;
+        return (i < sinks ? i : from + i - sinks) * kUnit;
+    };
+    auto head_of = [&](int u) { return kKeys ? own * per + u / span : own / per; };
+    const int tail = length < A.sight.tokens ? length % kUnit : 0;
+
+    const Roles R{gave_up, A.wait_ns};
+    const bool issuer = elect_one();
+    uint32_t asked = 0;
+    bool issued = false;
+    if (warp == 0) {
+        bool ok = true;
+        if (units && issuer) {
+            mbar_expect(rfull, L::kResident);
+            for (int o = 0; o < 2; ++o)
+                for (int c = 0; c < C; ++c)
+                    for (int j = 0; j < 2; ++j)
+                        tma_load4(base + (o * C + c) * kChunk + j * kHalf, kKeys ? (o ? &A.v : &A.k) : (o ? &A.g : &A.q), 64 * c, r0 + kUnit * j, own, b, rfull);
+        }
+        Ring<NS> r;
+        for (int u = 0; u < units; ++u) {
+            ok = R.wait(empty + 8 * r.slot, r.phase ^ 1);
+            if (!ok) break;
+            if (issuer) {
+                const uint32_t x = ring + r.slot * L::kStage, bar = full + 8 * r.slot;
+                const int row = row_of(u), head = head_of(u);
+                mbar_expect(bar, L::kStage + (kKeys ? 512 : 0));
+                for (int c = 0; c < C; ++c) tma_load4(x + c * kHalf, kKeys ? &A.q : &A.k, 64 * c, row, head, b, bar);
+                for (int c = 0; c < C; ++c) tma_load4(x + L::kStageX + c * kHalf, kKeys ? &A.g : &A.v, 64 * c, row, head, b, bar);
+                if (kKeys) {
+                    const int64_t at = ((int64_t)b * A.heads + head) * A.pitch + row;
+                    const uint32_t stats = base + L::kStats + r.slot * 512;
+                    bulk_load(stats, A.lse + at, 256, bar);
+                    bulk_load(stats + 256, A.d + at, 256, bar);
+                }
+            }
+            ++asked;
+            r.next();
+        }
+        let_next();
+        if (!ok && issuer) give_up(gave_up, A.err);
+    } else if (warp == 1) {
+        constexpr uint32_t kType = kF16 ? 0u : 1u << 7 | 1u << 10;
+        const uint32_t scores = 1u << 4 | kType | (uint32_t)(kUnit >> 3) << 17 | (uint32_t)(N >> 4) << 24;
+        const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
+        const uint64_t d1 = smem_desc(base, 0), d2 = smem_desc(base + C * kChunk, 0);
+        const uint32_t acc1 = tmem + 256, acc2 = tmem + 256 + 64 * C;
+        Ring<NS> now, then;      // the stages of units u and u - 2
+        bool ok = units == 0 || R.wait(rfull, 0);
+        for (int u = 0; ok && units && u < units + 2; ++u) {
+            const uint32_t buffer = tmem + (u & 1) * 128;
+            if (u >= 2) {
+                ok = R.wait(ready + 8 * (u & 1), (u - 2) >> 1 & 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (issuer) {
+                    const uint64_t dx = smem_desc(ring + then.slot * L::kStage, kHalf), dy = smem_desc(ring + then.slot * L::kStage + L::kStageX, kHalf);
+#pragma unroll
+                    for (int j = 0; j < kUnit / 16; ++j) mma_rows(acc1, buffer + 64 + 8 * j, dx + j * (2048 >> 4), outputs, u > 2 || j > 0);
+                    if (kKeys) {
+#pragma unroll
+                        for (int j = 0; j < kUnit / 16; ++j) mma_rows(acc2, buffer + 8 * j, dy + j * (2048 >> 4), outputs, u > 2 || j > 0);
+                    }
+                    mma_commit<1>(empty + 8 * then.slot);
+                }
+                then.next();
+            }
+            if (u < units) {
+                ok = R.wait(full + 8 * now.slot, now.phase);
+                if (!ok) break;
+                tc_fence_after();
+                // rows behind the sequence: what they hold meets zeros in the products
+                if (tail && row_of(u) == length - tail) clear_rows(sm + L::kResident + now.slot * L::kStage, 2 * C, kUnit, tail, lane);
+                if (issuer) {
+                    const uint64_t dx = smem_desc(ring + now.slot * L::kStage, 0), dy = smem_desc(ring + now.slot * L::kStage + L::kStageX, 0);
+#pragma unroll
+                    for (int j = 0; j < 4 * C; ++j)
+                        mma<1>(buffer, d1 + ((j / 4 * kChunk + j % 4 * 32) >> 4), dx + ((j / 4 * kHalf + j % 4 * 32) >> 4), scores, j > 0);
+#pragma unroll
+                    for (int j = 0; j < 4 * C; ++j)
+                        mma<1>(buffer + 64, d2 + ((j / 4 * kChunk + j % 4 * 32) >> 4), dy + ((j / 4 * kHalf + j % 4 * 32) >> 4), scores, j > 0);
+                    mma_commit<1>(sfull + 8 * (u & 1));
+                }
+                issued = true;
+                now.next();
+            }
+        }
+        if (issuer) {
+            if (!ok) give_up(gave_up, A.err);
+            else if (units) mma_commit<1>(done);
+        }
+    } else if (warp >= 4) {
+        const int h = (warp - 4) >> 2, quad = warp & 3, row0 = r0 + quad * 32, row = row0 + lane;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16, buffer = tmem + lanes + h * 128;
+        const float factor = kF16 ? float16_factor(A.most) : 1.f;      // of dS
+        const float2 scale = make_float2(A.scale2, A.scale2), times = make_float2(factor * 6.103515625e-05f, factor * 6.103515625e-05f);   // 2^-14
+        float2 less, minus;       // of a resident query
+        if (!kKeys) {
+            const int64_t at = ((int64_t)b * A.heads + own) * A.pitch + row;
+            less.x = less.y = kShift - A.lse[at];
+            minus.x = minus.y = A.d[at];
+        }
+        bool ok = true;
+        Ring<NS> r;
+        if (h) r.next();
+        for (int u = h; u < units; u += 2) {
+            if (kKeys) {
+                ok = R.wait(full + 8 * r.slot, r.phase);      // lse and d
+                if (!ok) break;
+            }
+            ok = R.wait(sfull + 8 * h, u >> 1 & 1);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[kUnit], p[kUnit];
+            tmem_ld32(buffer, s);
+            tmem_ld32(buffer + 32, s + 32);
+            tmem_ld32(buffer + 64, p);
+            tmem_ld32(buffer + 96, p + 32);
+            tmem_wait();
+            const int c0 = row_of(u);
+            uint32_t bits[2] = {~0u, ~0u};
+            bool some;        // of the unit is not seen by some row
+            if (kKeys) {
+                some = r0 + N - 1 > c0 || !(c0 + kUnit - 1 - r0 < A.sight.window || r0 + N - 1 < A.sight.sinks) || c0 + kUnit > length;
+                if (some) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        bits[c] = ~low_bits(row - c0 - 32 * c) & low_bits(length - c0 - 32 * c) & (row < A.sight.sinks ? ~0u : low_bits(row - c0 - 32 * c + A.sight.window));
+                }
+            } else {
+                some = c0 + kUnit - 1 > r0 || !(r0 + N - 1 - c0 < A.sight.window || c0 + kUnit - 1 < A.sight.sinks);
+                if (some) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        bits[c] = low_bits(row + 1 - c0 - 32 * c) & (~low_bits(row - A.sight.window + 1 - c0 - 32 * c) | low_bits(A.sight.sinks - c0 - 32 * c));
+                }
+            }
+            const float4* lse = reinterpret_cast<const float4*>(sm + L::kStats + r.slot * 512);
+#pragma unroll
+            for (int c = 0; c < kUnit; c += 4) {
+                float4 l, d;
+                if (kKeys) {
+                    l = lse[c / 4];
+                    d = lse[16 + c / 4];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    if (kKeys) {
+                        less = e ? make_float2(kShift - l.z, kShift - l.w) : make_float2(kShift - l.x, kShift - l.y);
+                        minus = e ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
+                    }
+                    float2 x = fma2(make_float2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, less);
+                    x.x = power(x.x);
+                    x.y = power(x.y);
+                    float2 y = mul2(kF16 ? mul2(x, times) : x, add2(make_float2(__uint_as_float(p[c + e]), __uint_as_float(p[c + e + 1])), minus));
+                    s[c + e] = __float_as_uint(x.x);
+                    s[c + e + 1] = __float_as_uint(x.y);
+                    p[c + e] = __float_as_uint(y.x);
+                    p[c + e + 1] = __float_as_uint(y.y);
+                }
+            }
+            if (some) {
+#pragma unroll
+                for (int c = 0; c < kUnit; ++c) {
+                    const bool seen = bits[c / 32] & 1u << c % 32;
+                    s[c] = seen ? s[c] : 0u;
+                    p[c] = seen ? p[c] : 0u;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kUnit / 2; ++c) {
+                s[c] = pack2<T>(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+                p[c] = pack2<T>(__uint_as_float(p[2 * c]), __uint_as_float(p[2 * c + 1]));
+            }
+            if (kKeys) tmem_st32(buffer, s);
+            tmem_st32(buffer + 64, p);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready + 8 * h);
+            r.next();
+            r.next();
+        }
+        if (ok && units) ok = R.wait(done, 0);
+        if (ok) {
+            tc_fence_after();
+            // keys: dK by the first four warps, dV by the others; queries: 64 columns each
+            const bool values = kKeys && h, real = units && row < length;
+            const float times_out = values ? (kF16 ? 6.103515625e-05f : 1.f) : A.scale / factor;
+            const int rows = min(32, A.sight.tokens - row0);
+            unsigned char* stage = sm + L::kResident + (warp - 4) * 4096;      // all products are done: the ring is free
+            T* to_rows = static_cast<T*>(kKeys ? (h ? A.gv : A.gk) : A.gq) + (((int64_t)b * A.sight.tokens + row0) * row_heads + own) * (int64_t)A.dim;
+            const int64_t pitch = (int64_t)row_heads * A.dim;
+            float* part = nullptr;
+            if (cut) part = A.part + ((((int64_t)tile * (A.pieces + 1) + piece) * A.planes + which) * 2 + h) * N * 64 * C + quad * 32 * 64 * C;
+#pragma unroll 1
+            for (int c = kKeys ? 0 : 64 * h; c < (kKeys ? 64 * C : 64 * min(C, h + 1)); c += 64) {
+                uint32_t o[64];
+                tmem_ld32(tmem + lanes + 256 + (values ? 64 * C : 0) + c, o);
+                tmem_ld32(tmem + lanes + 256 + (values ? 64 * C : 0) + c + 32, o + 32);
+                tmem_wait();
+#pragma unroll
+                for (int e = 0; e < 64; ++e) o[e] = real ? __float_as_uint(__uint_as_float(o[e]) * times_out) : 0u;
+                if (cut) {
+                    uint32_t v[32];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = o[32 * j + e];
+                        rows_out(stage, v, reinterpret_cast<char*>(part + c + 32 * j), 64 * C * 4, 32, 64, lane);
+                    }
+                } else {
+                    uint32_t v[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = pack2<T>(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+                    if (A.dim % 8 == 0) {
+                        rows_out(stage, v, reinterpret_cast<char*>(to_rows + c), pitch * 2, rows, A.dim - c, lane);
+                    } else if (lane < rows) {
+                        uint16_t* to_row = reinterpret_cast<uint16_t*>(to_rows + lane * pitch + c);
+#pragma unroll
+                        for (int e = 0; e < 64; ++e)
+                            if (c + e < A.dim) to_row[e] = (uint16_t)(v[e / 2] >> 16 * (e & 1));
+                    }
+                }
+            }
+        } else if (lane == 0) {
+            give_up(gave_up, A.err);
+        }
+    }
+    if (warp == 1 && issued) {      // nothing is in flight when tensor memory goes back
+        if (issuer) mma_commit<1>(drain);
+        mbar_wait(drain, 0, kWaitNs, nullptr);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (*gave_up) {
+        if (warp == 0 && units) {
+            mbar_wait(rfull, 0, kWaitNs, nullptr);
+            for (uint32_t a = asked > NS ? asked - NS : 0; a < asked; ++a)
+                if (!mbar_wait(full + 8 * (a % NS), a / NS & 1, kWaitNs, nullptr)) break;
+        }
+        __syncthreads();
+    }
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// What the backward needs of each row: -g . o and lse in powers of two (infinity behind a sequence: no probability), 16
+// lanes a row, and for float16 the largest squared norms of g's and v's rows.  Bound by HBM.
+struct RowArgs {
+    Heads g, v;
+    const void* o;
+    const float* saved;
+    float *lse, *d, *most;       // most: [2], or NULL
+    const int32_t* lengths;
+    int64_t batch, tokens, pitch;
+    int heads, groups, dim, packs;
+};
+__device__ __forceinline__ float sum16(float v) {
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+template <typename T> __device__ __forceinline__ void load8(const T* p, int c, int dim, int packs, float2 (&v)[4]) {
+    if (packs) {
+        const uint4 q = c < dim ? *reinterpret_cast<const uint4*>(p + c) : make_uint4(0, 0, 0, 0);
+        v[0] = unpack2<T>(q.x); v[1] = unpack2<T>(q.y); v[2] = unpack2<T>(q.z); v[3] = unpack2<T>(q.w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = make_float2(c + 2 * i < dim ? to_f(p[c + 2 * i]) : 0.f, c + 2 * i + 1 < dim ? to_f(p[c + 2 * i + 1]) : 0.f);
+    }
+}
+__device__ __forceinline__ float dot8(const float2 (&a)[4], const float2 (&b)[4]) {
+    float2 s = mul2(a[0], b[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = fma2(a[i], b[i], s);
+    return s.x + s.y;
+}
+template <typename T> __global__ void __launch_bounds__(256) rows_tc_kernel(const __grid_constant__ RowArgs A) {
+    stream_order();
+    const int c = 8 * (threadIdx.x & 15);
+    const int64_t step = (int64_t)gridDim.x * 16, rows = A.batch * A.heads * A.pitch, values = A.most ? A.batch * A.tokens * A.groups : 0;
+    float most[2] = {0.f, 0.f};
+    // (a warp's two rows stay together: rows is a multiple of 128)
+    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < rows; i += step) {
+        // heads inside of tokens, so that neighbouring rows of a sequence lie together
+        const int64_t b = i / (A.pitch * A.heads), j = i - b * A.pitch * A.heads, t = j / A.heads;
+        const int h = (int)(j - t * A.heads);
+        const int64_t at = (b * A.heads + h) * A.pitch + t;
+        const bool in = t < (A.lengths ? min(max((int64_t)A.lengths[b], (int64_t)0), A.tokens) : A.tokens);
+        float s = 0.f, n = 0.f;
+        if (in) {
+            float2 g[4], o[4];
+            load8(static_cast<const T*>(A.g.p) + b * A.g.batch + t * A.g.token + h * A.g.head, c, A.dim, A.packs, g);
+            load8(static_cast<const T*>(A.o) + ((b * A.tokens + t) * A.heads + h) * A.dim, c, A.dim, A.packs, o);
+            s = dot8(g, o);
+            n = dot8(g, g);
+        }
+        s = sum16(s);
+        if (A.most) most[0] = fmaxf(most[0], sum16(n));
+        if (c == 0) {
+            A.d[at] = in ? -s : 0.f;
+            A.lse[at] = in ? A.saved[(b * A.heads + h) * A.tokens + t] * 1.44269504088896341f : INFINITY;
+        }
+    }
+    if (!A.most) return;
+    for (int64_t i0 = (int64_t)blockIdx.x * 16; i0 < values; i0 += step) {
+        const int64_t i = i0 + (threadIdx.x >> 4), b = i / (A.tokens * A.groups), j = i - b * A.tokens * A.groups, t = j / A.groups;
+        const bool in = i < values && t < (A.lengths ? min(max((int64_t)A.lengths[b], (int64_t)0), A.tokens) : A.tokens);
+        float n = 0.f;
+        if (in) {
+            float2 v[4];
+            load8(static_cast<const T*>(A.v.p) + b * A.v.batch + t * A.v.token + (j - t * A.groups) * A.v.head, c, A.dim, A.packs, v);
+            n = dot8(v, v);
+        }
+        most[1] = fmaxf(most[1], sum16(n));
+    }
+    // the largest of non-negative floats as integers: in any order the same (NaN counts as none, an infinity switches the factor off)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float v = fmaxf(most[k], __shfl_xor_sync(~0u, most[k], 16));
+        if ((threadIdx.x & 31) == 0) atomicMax(reinterpret_cast<int*>(A.most + k), __float_as_int(v));
+    }
+}
+
+// Sums of the pieces of cut tiles, in their order: keys and values [tiles * 128 rows] of every group.
+template <typename T> __global__ void __launch_bounds__(256) join_tc_kernel(const __grid_constant__ TcBack A, int width) {
+    stream_order();
+    const int64_t rows = min((int64_t)A.cut * N, (int64_t)A.sight.tokens), count = (int64_t)A.planes * 2 * rows * width, step = (int64_t)gridDim.x * 256;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < count; e += step) {
+        const int c = (int)(e % width);
+        const int64_t row = e / width % rows, side = e / width / rows % 2, which = e / width / rows / 2, tile = row / N;
+        if (c >= A.dim) continue;
+        float s = 0.f;
+        for (int p = 0; p <= A.pieces; ++p)
+            s += A.part[((((tile * (A.pieces + 1) + p) * A.planes + which) * 2 + side) * N + row % N) * width + c];
+        const int64_t b = which / A.groups;
+        static_cast<T*>(side ? A.gv : A.gk)[((b * A.sight.tokens + row) * A.groups + which % A.groups) * A.dim + c] = from_f<T>(s);
+    }
+}
+
+// Map of heads [batch, tokens, heads, dim]: boxes of 64 elements x `rows` tokens of one head.
+bool make_map(CUtensorMap* m, const Heads& h, int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t dim, int rows) {
     EncodeTiled enc = encode_tiled();
     if (!enc) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)batch};
     // (the stride of an axis of one is not used: any that the driver takes)
     const cuuint64_t strides[3] = {(cuuint64_t)(tokens > 1 ? h.token * 2 : 16), (cuuint64_t)(heads > 1 ? h.head * 2 : 16), (cuuint64_t)(batch > 1 ? h.batch * 2 : 16)};
-    const cuuint32_t boxes[4] = {64, N, 1, 1}, one[4] = {1, 1, 1, 1};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
     return enc(m, dtype == VQC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(h.p), dims, strides, boxes, one,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -511,7 +982,8 @@ bool in_place(const Heads& h, int64_t batch, int64_t tokens, int64_t heads, int6
 size_t copy_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t dim) { return align256((size_t)(batch * tokens * heads) * padded(dim) * 2); }
 
 // Maps of the operands, after copies of those that need one into `ws`.
-vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* heads, CUtensorMap* const* map, int count, char* ws, size_t bytes, cudaStream_t s) {
+vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* heads, CUtensorMap* const* map, int count, int box, char*& ws, size_t& bytes,
+                   cudaStream_t s) {
     CopyJobs jobs{};
     jobs.tokens = a.sight.tokens;
     jobs.dim = a.dim;
@@ -532,7 +1004,7 @@ vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* 
             ws += need;
             bytes -= need;
         }
-        if (!make_map(map[i], h, a.dtype, a.batch, a.sight.tokens, heads[i], dim)) return set_error(VQC_ERR_CUDA, "attention: a tensor map was refused");
+        if (!make_map(map[i], h, a.dtype, a.batch, a.sight.tokens, heads[i], dim, box)) return set_error(VQC_ERR_CUDA, "attention: a tensor map was refused");
     }
     if (!copies) return VQC_OK;
     void* args[] = {&jobs};
@@ -541,12 +1013,11 @@ vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* 
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "copy launch");
 }
 
-vqc_status start(const AttentionArgs& a, TcAttention& t) {
+template <typename A> vqc_status start(const AttentionArgs& a, A& t) {
     t.sight = {a.sight.lengths, (int)a.sight.tokens, (int)a.sight.window, (int)a.sight.sinks};
     t.scale = a.scale;
     t.scale2 = a.scale2;
     t.heads = a.heads; t.groups = a.groups; t.dim = a.dim;
-    t.bf16 = a.dtype == VQC_BF16;
     t.wait_ns = wait_limit();
     const cudaError_t e = error_word(&t.err);
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "error word");
@@ -557,14 +1028,64 @@ template <typename T, int C> cudaError_t launch_forward(const TcAttention& t, un
     return launch((const void*)forward_tc<T, C>, dim3(grid), kThreads, args, s, ForwardShape<C>::kSmem);
 }
 
+template <typename T, int C, bool kKeys> cudaError_t launch_back(const TcBack& t, cudaStream_t s) {
+    void* args[] = {const_cast<TcBack*>(&t)};
+    const int64_t tiles = t.tiles + (kKeys ? (int64_t)t.cut * t.pieces : 0);
+    return launch((const void*)back_tc<T, C, kKeys>, dim3((unsigned)(tiles * t.planes)), kThreads, args, s, BackShape<C>::kSmem);
+}
+template <typename T, int C> cudaError_t run_back(TcBack& t, const AttentionArgs& a, cudaStream_t s) {
+    cudaError_t e = cudaSuccess;
+    if (a.gk) {
+        t.planes = (int)(a.batch * a.groups);
+        e = launch_back<T, C, true>(t, s);
+        if (e == cudaSuccess && t.cut) {
+            int width = 64 * C;
+            void* args[] = {&t, &width};
+            const int64_t count = (int64_t)t.planes * 2 * t.cut * N * width;
+            e = launch((const void*)join_tc_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(count, 256), 8LL * sm_count())), 256, args, s);
+        }
+    }
+    if (e == cudaSuccess && a.gq) {
+        t.planes = (int)(a.batch * a.heads);
+        e = launch_back<T, C, false>(t, s);
+    }
+    return e;
+}
+
+// The space of a backward behind the copies: stats of rows, float16's norms, sums of pieces.
+struct BackSpace {
+    int64_t pitch;
+    int cut, pieces, piece;
+    size_t stats, most, part;
+};
+BackSpace back_space(int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t window, int64_t sinks) {
+    BackSpace b{};
+    b.pitch = ceil_div(tokens, N) * N;
+    b.stats = align256((size_t)(batch * heads * b.pitch) * 4);
+    b.most = dtype == VQC_F16 ? 256 : 0;
+    // Keys seen from behind the window: pieces as long as a window, 2048 queries at least (a piece writes its sums as floats).
+    if (sinks > 0 && window < tokens) {
+        b.piece = (int)std::max<int64_t>(2048, ceil_div(window + N, kUnit) * kUnit);
+        b.pieces = (int)ceil_div(tokens - window, b.piece);
+        b.cut = (int)std::min(ceil_div(sinks, N), ceil_div(tokens, N));
+        // (where most keys are such there is nothing to even out)
+        if (2 * b.cut > ceil_div(tokens, N)) b.cut = b.pieces = 0;
+        b.part = align256((size_t)b.cut * (b.pieces + 1) * batch * groups * 2 * N * (dim <= 64 ? 64 : 128) * 4);
+    }
+    return b;
+}
+
 }  // namespace
 
 bool attention_tc_takes(int dtype, int64_t dim) { return dtype != VQC_F32 && dim <= 128; }
 
-size_t attention_tc_workspace(int mode, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, bool aligned) {
-    if (aligned && dim % 8 == 0) return 0;
-    const size_t q = copy_bytes(batch, tokens, heads, dim), k = copy_bytes(batch, tokens, groups, dim);
-    return mode ? 2 * q + 2 * k : q + 2 * k;
+size_t attention_tc_workspace(int mode, int dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t window, int64_t sinks,
+                              bool aligned) {
+    size_t bytes = 0;
+    if (!aligned || dim % 8) bytes = (mode ? 2 : 1) * copy_bytes(batch, tokens, heads, dim) + 2 * copy_bytes(batch, tokens, groups, dim);
+    if (!mode) return bytes;
+    const BackSpace b = back_space(dtype, batch, tokens, heads, groups, dim, window, sinks);
+    return bytes + 2 * b.stats + b.most + b.part;
 }
 
 vqc_status attention_tc_forward(const AttentionArgs& a, void* ws, size_t bytes, cudaStream_t s) {
@@ -574,15 +1095,63 @@ vqc_status attention_tc_forward(const AttentionArgs& a, void* ws, size_t bytes, 
     const Heads* from[3] = {&a.q, &a.k, &a.v};
     const int heads[3] = {a.heads, a.groups, a.groups};
     CUtensorMap* map[3] = {&t.q, &t.k, &t.v};
-    st = maps_of(a, from, heads, map, 3, static_cast<char*>(ws), bytes, s);
+    char* at = static_cast<char*>(ws);
+    st = maps_of(a, from, heads, map, 3, N, at, bytes, s);
     if (st != VQC_OK) return st;
     t.o = a.o;
     t.saved = a.saved;
     t.tiles = (int)ceil_div(a.sight.tokens, 2 * N);
     t.items = (int)(t.tiles * a.batch * a.heads);
     const unsigned grid = (unsigned)std::min<int64_t>(t.items, sm_count());
-    const cudaError_t e = t.bf16 ? (a.dim <= 64 ? launch_forward<__nv_bfloat16, 1>(t, grid, s) : launch_forward<__nv_bfloat16, 2>(t, grid, s))
+    const cudaError_t e = a.dtype == VQC_BF16 ? (a.dim <= 64 ? launch_forward<__nv_bfloat16, 1>(t, grid, s) : launch_forward<__nv_bfloat16, 2>(t, grid, s))
                                  : (a.dim <= 64 ? launch_forward<__half, 1>(t, grid, s) : launch_forward<__half, 2>(t, grid, s));
+    return e == cudaSuccess ? VQC_OK : cuda_error(e, "attention launch");
+}
+
+vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes, cudaStream_t s) {
+    TcBack t{};
+    vqc_status st = start(a, t);
+    if (st != VQC_OK) return st;
+    const Heads* from[4] = {&a.q, &a.k, &a.v, &a.g};
+    const int heads[4] = {a.heads, a.groups, a.groups, a.heads};
+    CUtensorMap* map[4] = {&t.q, &t.k, &t.v, &t.g};
+    char* at = static_cast<char*>(ws);
+    st = maps_of(a, from, heads, map, 4, kUnit, at, bytes, s);
+    if (st != VQC_OK) return st;
+    const BackSpace b = back_space(a.dtype, a.batch, a.sight.tokens, a.heads, a.groups, a.dim, a.sight.window, a.sight.sinks);
+    if (2 * b.stats + b.most + b.part > bytes) return set_error(VQC_ERR_WORKSPACE, "attention: workspace too small");
+    RowArgs r{};
+    r.g = a.g; r.v = a.v;
+    r.o = a.o;
+    r.saved = a.lse;
+    r.lse = reinterpret_cast<float*>(at);
+    r.d = reinterpret_cast<float*>(at + b.stats);
+    at += 2 * b.stats;
+    r.most = b.most ? reinterpret_cast<float*>(at) : nullptr;
+    at += b.most;
+    r.lengths = a.sight.lengths;
+    r.batch = a.batch; r.tokens = a.sight.tokens; r.pitch = b.pitch;
+    r.heads = a.heads; r.groups = a.groups; r.dim = a.dim;
+    r.packs = a.dim % 8 == 0 && heads_on(a.g, 2, 16) && heads_on(a.v, 2, 16);
+    cudaError_t e = cudaSuccess;
+    if (r.most) e = cudaMemsetAsync(r.most, 0, 8, s);
+    if (e == cudaSuccess) {
+        void* args[] = {&r};
+        const int64_t rows = a.batch * a.heads * b.pitch;
+        e = launch(a.dtype == VQC_BF16 ? (const void*)rows_tc_kernel<__nv_bfloat16> : (const void*)rows_tc_kernel<__half>,
+                   dim3((unsigned)std::min<int64_t>(ceil_div(rows, 16), 16LL * sm_count())), 256, args, s);
+    }
+    if (e != cudaSuccess) return cuda_error(e, "attention launch");
+    t.lse = r.lse;
+    t.d = r.d;
+    t.most = r.most;
+    t.gq = a.gq; t.gk = a.gk; t.gv = a.gv;
+    t.part = reinterpret_cast<float*>(at);
+    t.pitch = b.pitch;
+    t.tiles = (int)ceil_div(a.sight.tokens, N);
+    t.cut = b.cut; t.pieces = b.pieces; t.piece = b.piece;
+    e = a.dtype == VQC_BF16 ? (a.dim <= 64 ? run_back<__nv_bfloat16, 1>(t, a, s) : run_back<__nv_bfloat16, 2>(t, a, s))
+                            : (a.dim <= 64 ? run_back<__half, 1>(t, a, s) : run_back<__half, 2>(t, a, s));
     return e == cudaSuccess ? VQC_OK : cuda_error(e, "attention launch");
 }
 

@@ -415,7 +415,8 @@ std::pair<Tensor, Tensor> attention_forward(const Tensor& q, const Tensor& k, co
     const Sight s = sight_of(a, b.size(2), given);
     Tensor o = dense(a, a.size(2)), saved;
     if (save) saved = at::empty({a.size(0), a.size(2), a.size(1)}, a.t.options().dtype(at::kFloat));
-    const size_t bytes = vqc_attention_workspace_bytes(0, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), on16(a) && on16(b) && on16(c));
+    const size_t bytes = vqc_attention_workspace_bytes(0, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), s.window, s.sinks,
+                                                       on16(a) && on16(b) && on16(c));
     const Tensor ws = space(bytes, a.t);
     check(vqc_attention_forward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &a.h, &b.h, &c.h, s.window, s.sinks, s.scale,
                                 static_cast<const int32_t*>(address(s.lengths)), o.data_ptr(), static_cast<float*>(address(saved)), address(ws), bytes,
@@ -430,7 +431,7 @@ variable_list attention_backward(const Tensor& go, const Tensor& q, const Tensor
     const float* lse = saved_of(saved, {a.size(0), a.size(2), a.size(1)});
     const Tensor out = y.t.contiguous();
     Tensor gq = need_q ? dense(a, a.size(2)) : Tensor(), gk = need_kv ? dense(a, b.size(2)) : Tensor(), gv = need_kv ? dense(a, b.size(2)) : Tensor();
-    const size_t bytes = vqc_attention_workspace_bytes(1, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3),
+    const size_t bytes = vqc_attention_workspace_bytes(1, (vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), s.window, s.sinks,
                                                        on16(a) && on16(b) && on16(c) && on16(g));
     const Tensor ws = space(bytes, a.t);
     check(vqc_attention_backward((vqc_real)a.code, a.size(0), a.size(1), a.size(2), b.size(2), a.size(3), &g.h, &a.h, &b.h, &c.h, out.data_ptr(), lse,

@@ -148,6 +148,9 @@ def attention(q, k, v, g, window, sinks, scale, lengths, dtype):
             if dtype == torch.float16:
                 eds = eds + r["seen"].double() * 2.0 ** -34 * gb.norm(dim=1).max() * vb.norm(dim=1).max()
             epr = p * (r["ep"] + u) + (2.0 ** -39 if dtype == torch.float16 else 0.0) * r["seen"].double()
+            # a probability below 2^-126, the smallest normal number, may count as zero: p is off by less than that, ds by
+            # that times |dp - d|
+            epr, eds = epr + 2.0 ** -126 * r["seen"], eds + 2.0 ** -126 * r["seen"] * (dp.abs() + d.abs())
             for name, a, ea, x, at in (("gq", ds, eds, kb, (b, slice(0, n), h)), ("gk", ds.t(), eds.t(), qb, (b, slice(0, n), j)),
                                        ("gv", p.t(), epr.t(), gb, (b, slice(0, n), j))):
                 f = 1.0 if name == "gv" else scale

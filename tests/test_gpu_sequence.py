@@ -188,6 +188,8 @@ CASES = [
     (1, 70, 2, 1, 160, None, 0, None, 0),
     (2, 100, 2, 2, 256, 33, 2, [100, 50], 8),
     (1, 1100, 1, 1, 128, 256, 130, None, 0),
+    (1, 5000, 2, 1, 64, 64, 130, [4900], 0),      # keys that stay visible: several pieces of far queries
+    (1, 4500, 2, 2, 128, 300, 2, None, 0),
 ]
 
 

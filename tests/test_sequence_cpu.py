@@ -71,8 +71,8 @@ def test_attention_refusals():
     refused(B.vqc_attention_step, args, [(0, 7), (3, 3), (5, 257), (6, -1), (6, 1 << 30), (7, heads(None)), (8, heads(A + 2)), (9, None), (10, -1), (11, -1),
                                          (12, float("nan")), (13, None), (13, A + 1), (14, None), (15, A + 2)])
     refused(B.vqc_attention_step, args, [(15, None), (16, 16)], "VQC_ERR_WORKSPACE")
-    assert B.vqc_attention_workspace_bytes(2, B.VQC_F32, 2, 3, 4, 2, 8, 1) == 2 ** 64 - 1
-    assert B.vqc_attention_workspace_bytes(0, B.VQC_F32, 2, 3, 4, 3, 8, 1) == 2 ** 64 - 1
+    assert B.vqc_attention_workspace_bytes(2, B.VQC_F32, 2, 3, 4, 2, 8, 0, 0, 1) == 2 ** 64 - 1
+    assert B.vqc_attention_workspace_bytes(0, B.VQC_F32, 2, 3, 4, 3, 8, 0, 0, 1) == 2 ** 64 - 1
     assert B.vqc_attention_step_workspace_bytes(1, 1, 4, 2, 8, -1, 0, 0) == 2 ** 64 - 1
     # no more than a window's keys are cut, whatever the capacity
     assert B.vqc_attention_step_workspace_bytes(1, 1, 4, 2, 64, 1 << 29, 64, 0) < 1 << 20
