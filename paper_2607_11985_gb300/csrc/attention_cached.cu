@@ -11,6 +11,7 @@
 // lengths keep all SMs busy without the host knowing the lengths.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attention.h"
 #include "layers_elem.cuh"
@@ -20,7 +21,7 @@ namespace layers {
 
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct CachedArgs {
@@ -47,40 +48,43 @@ __device__ __forceinline__ Keys keys_of(const CachedArgs& A, int64_t b) {
 }
 __device__ __forceinline__ int64_t key_at(const Keys& K, int64_t i) { return i < K.first ? i : K.from + (i - K.first); }
 
-// V elements of a row, as floats
-template <typename T, int V> __device__ __forceinline__ void load_some(const T* p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = to_f(*p);
-    } else {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// 16 bytes to shared memory, or zeros; the end of a group of copies; at most M groups still on the way
+__device__ __forceinline__ void copy16(void* to, const void* from, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;\n" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int M> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(M) : "memory"); }
+template <typename T> __device__ __forceinline__ void as_floats(const uint4& q, float* v) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                v[i] = __uint_as_float(w[i]);
-            } else {
-                const float2 a = unpack2<T>(w[i]);
-                v[2 * i] = a.x;
-                v[2 * i + 1] = a.y;
-            }
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(w[i]);
+        } else {
+            const float2 a = unpack2<T>(w[i]);
+            v[2 * i] = a.x;
+            v[2 * i + 1] = a.y;
         }
     }
 }
+constexpr int kDepth = 4;      // groups of keys of a warp, on the way or being worked on
 
 // Any type and head size: 8 lanes hold a key (V elements at a time), 4 keys per warp, RB queries; each of
 // the 16 places of a CTA has a maximum, a sum and an output of its own until the chunk ends.
 template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(kThreads) cached_kernel(const __grid_constant__ CachedArgs A) {
     stream_order();
     constexpr int NE = DM / 8, NL = NE / V;      // elements of a lane, loads
-    __shared__ float joined[16 * RB * (DM + 2)];
+    extern __shared__ __align__(16) float joined[];     // the ring, and after it the places' sums
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = warp * 4 + lane / 8, part = lane & 7;
-    int64_t w = blockIdx.x;
-    const int64_t chunk = w % A.chunks;
-    w /= A.chunks;
+    int64_t w = blockIdx.x;      // all groups of a chunk together: they read neighbouring memory
+    const int group = (int)(w % A.groups);
+    w /= A.groups;
     const int block = (int)(w % A.blocks);
     w /= A.blocks;
-    const int group = (int)(w % A.groups);
-    const int64_t b = w / A.groups;
+    const int64_t chunk = w % A.chunks, b = w / A.chunks;
     const Keys K = keys_of(A, b);
     const int64_t i0 = chunk * A.chunk, i1 = min(i0 + A.chunk, K.count);
     if (i0 >= i1 && chunk > 0) return;
@@ -103,23 +107,46 @@ template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(k
         }
     }
     const T *kp = static_cast<const T*>(A.k.p) + b * A.k.batch + group * A.k.head, *vp = static_cast<const T*>(A.v.p) + b * A.v.batch + group * A.v.head;
+    // Keys and values on the way: a lane copies the 16 bytes that it will read itself, so that nobody waits for another's
+    // (elements that are not there arrive as zeros).  Single elements (V = 1) are loaded when they are needed.
+    unsigned char* ring = reinterpret_cast<unsigned char*>(joined) + warp * kDepth * 2 * NL * 512 + lane * 16;
+    auto ask = [&](int64_t i, int stage) {
+        if constexpr (V > 1) {
+            const bool there = i + slot < i1;
+            const int64_t j = there ? key_at(K, i + slot) : 0;
+#pragma unroll
+            for (int l = 0; l < NL; ++l) {
+                const bool in = there && col(l, 0) < A.dim;
+                copy16(ring + (stage * 2 * NL + l) * 512, in ? kp + j * A.k.token + col(l, 0) : kp, in);
+                copy16(ring + (stage * 2 * NL + NL + l) * 512, in ? vp + j * A.v.token + col(l, 0) : vp, in);
+            }
+            copies_end();
+        }
+    };
+    if (i1 > i0) {
+#pragma unroll
+        for (int d = 0; d < kDepth - 1; ++d) ask(i0 + 16 * d, d);
+    }
+    int stage = 0;
     for (int64_t i = i0; i < i1; i += 16) {
         const bool in = i + slot < i1;
         const int64_t j = in ? key_at(K, i + slot) : 0;
         float k[NE], v[NE];
+        if constexpr (V > 1) {
+            copies_wait<kDepth - 2>();
+            const int last = stage ? stage - 1 : kDepth - 1;
 #pragma unroll
-        for (int l = 0; l < NL; ++l) {
-            float x[V], y[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = y[e] = 0.f;
-            if (in && col(l, 0) < A.dim) {
-                load_some<T, V>(kp + j * A.k.token + col(l, 0), x);
-                load_some<T, V>(vp + j * A.v.token + col(l, 0), y);
+            for (int l = 0; l < NL; ++l) {
+                as_floats<T>(*reinterpret_cast<const uint4*>(ring + (stage * 2 * NL + l) * 512), k + l * V);
+                as_floats<T>(*reinterpret_cast<const uint4*>(ring + (stage * 2 * NL + NL + l) * 512), v + l * V);
             }
+            ask(i + 16 * (kDepth - 1), last);
+            stage = stage + 1 == kDepth ? 0 : stage + 1;
+        } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                k[l * V + e] = x[e];
-                v[l * V + e] = y[e];
+            for (int e = 0; e < NE; ++e) {
+                k[e] = in && col(e, 0) < A.dim ? to_f(kp[j * A.k.token + col(e, 0)]) : 0.f;
+                v[e] = in && col(e, 0) < A.dim ? to_f(vp[j * A.v.token + col(e, 0)]) : 0.f;
             }
         }
 #pragma unroll
@@ -146,6 +173,8 @@ template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(k
         __syncwarp();
     }
     constexpr int P = DM + 2;
+    if (V > 1) copies_wait<0>();
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
 #pragma unroll
@@ -177,6 +206,263 @@ template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(k
             }
         } else {
             static_cast<T*>(A.o)[((b * A.tokens + t) * A.heads + h) * A.dim + c] = from_f<T>(sum == 0.f ? 0.f : out / sum);
+        }
+    }
+}
+
+// 16-bit types with heads of up to 128 elements, on the tensor cores' mma.sync (a few rows leave tcgen05's tiles of 128
+// empty, and what bounds this is the loads): a warp takes 16 keys at a time for 16 rows (queries of a group, all tokens).
+// Both operands go from memory to registers as they lie there.  The scores contract over a head's elements, in
+// any order that both operands share: a lane's 16 bytes of a key, elements 32 i + 8 t + [0, 8), are its
+// parts of two steps.  The output's columns are free as well: column n of block j is element 64 (j / 8) + 8 n + j % 8, so that
+// a lane's 16 bytes of a value are its column in eight blocks; two keys' halves are paired by a byte permutation.
+// A lane copies the 16 bytes that it will read itself to shared memory, three stages deep: nobody waits for another's
+// copies, and what is on the way takes no registers (in registers 5.2 TB/s).
+constexpr int kRows = 16;
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float power(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// A stage: the pieces of 16 keys and values of a warp, each where the lane that copied it reads it.
+template <int DM> struct MmaShape {
+    static constexpr int NK = DM / 32, NV = DM / 64, kPieces = 2 * NK + 4 * NV, kStage = kPieces * 512, kDeep = DM == 64 ? 4 : 3;
+    static constexpr int kRing = kWarps * kDeep * kStage, kSums = kWarps * kRows * (DM + 4) * 4;
+    static constexpr int kSmem = (kRing > kSums ? kRing : kSums) + kWarps * kRows * 8;
+};
+
+template <typename T, int DM> __global__ void __launch_bounds__(kThreads, DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
+    using L = MmaShape<DM>;
+    constexpr int NK = L::NK, NV = L::NV, kDeep = L::kDeep;      // pieces of 16 bytes of a lane: of a key, of a value
+    constexpr float kShift = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value ? 6.f : 0.f;
+    constexpr int P = DM + 4;
+    extern __shared__ __align__(16) unsigned char shared[];
+    float(*joined)[kRows][P] = reinterpret_cast<float(*)[kRows][P]>(shared);      // in the place of the ring, after it
+    float(*stats)[kRows][2] = reinterpret_cast<float(*)[kRows][2]>(shared + L::kSmem - kWarps * kRows * 8);
+    stream_order();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    int64_t w = blockIdx.x;      // all groups of a chunk together: they read neighbouring memory
+    const int group = (int)(w % A.groups);
+    w /= A.groups;
+    const int block = (int)(w % A.blocks);
+    w /= A.blocks;
+    const int64_t chunk = w % A.chunks, b = w / A.chunks;
+    const Keys K = keys_of(A, b);
+    const int64_t i0 = chunk * A.chunk;
+    if (i0 >= K.count && chunk > 0) return;
+    const int count = (int)max((int64_t)0, min((int64_t)A.chunk, K.count - i0));
+    const int per = A.heads / A.groups, tokens = (int)A.tokens, rows = min(kRows, per * tokens - block * kRows);
+    // this lane's rows: g and g + 8; their queries, and positions less the first key's
+    uint32_t q[2 * NK][4];
+    int at[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = block * kRows + g + 8 * r, h = group * per + row / tokens, tok = row % tokens;
+        const bool in = g + 8 * r < rows;
+        at[r] = (int)(K.length - tokens) + tok;
+        const T* p = static_cast<const T*>(A.q.p) + b * A.q.batch + tok * A.q.token + h * A.q.head;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int c = 32 * i + 8 * t;
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {      // (queries may have any alignment)
+                const uint32_t lo = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e] : 0u, hi = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e + 1] : 0u;
+                x[e] = lo | hi << 16;
+            }
+            q[2 * i][r] = x[0];
+            q[2 * i][2 + r] = x[1];
+            q[2 * i + 1][r] = x[2];
+            q[2 * i + 1][2 + r] = x[3];
+        }
+    }
+    const T *kp = static_cast<const T*>(A.k.p) + b * A.k.batch + group * A.k.head, *vp = static_cast<const T*>(A.v.p) + b * A.v.batch + group * A.v.head;
+    unsigned char* ring = shared + warp * kDeep * L::kStage + lane * 16;
+    // keys and values of index i0 + i behind the first ones
+    const T *kq = kp + (K.from - K.first + i0 + g) * A.k.token + 8 * t, *vq = vp + (K.from - K.first + i0 + 2 * t) * A.v.token + 8 * g;
+    const uint32_t ring32 = (uint32_t)__cvta_generic_to_shared(ring);
+    auto ask = [&](int i, int stage) {
+        unsigned char* to = ring + stage * L::kStage;
+        if (i + 16 <= count && i0 + i >= K.first && A.dim == DM) {      // nearly always
+            const uint32_t to32 = ring32 + stage * L::kStage;
+            const T *pk = kq + i * A.k.token, *pv = vq + i * A.v.token;
+#pragma unroll
+            for (int n = 0; n < 2; ++n, pk += 8 * A.k.token)
+#pragma unroll
+                for (int c = 0; c < NK; ++c) copy16(to32 + (n * NK + c) * 512, pk + 32 * c);
+#pragma unroll
+            for (int n = 0; n < 4; ++n, pv += n == 2 ? 7 * A.v.token : A.v.token)
+#pragma unroll
+                for (int c = 0; c < NV; ++c) copy16(to32 + (2 * NK + n * NV + c) * 512, pv + 64 * c);
+            copies_end();
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int at_i = i + g + 8 * n;
+            const T* p = kp + key_at(K, i0 + at_i) * A.k.token + 8 * t;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) {
+                const bool in = at_i < count && 32 * c + 8 * t < A.dim;
+                copy16(to + (n * NK + c) * 512, in ? p + 32 * c : kp, in);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int at_i = i + 2 * t + (n & 1) + 8 * (n >> 1);
+            const T* p = vp + key_at(K, i0 + at_i) * A.v.token + 8 * g;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const bool in = at_i < count && 64 * c + 8 * g < A.dim;
+                copy16(to + (2 * NK + n * NV + c) * 512, in ? p + 64 * c : vp, in);
+            }
+        }
+        copies_end();
+    };
+    constexpr int kStep = 16 * kWarps;
+    float o[8 * NV][4], followed[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 8 * NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    if (count) {
+#pragma unroll
+        for (int d = 0; d < kDeep - 1; ++d) ask(16 * warp + d * kStep, d);
+    }
+    int stage = 0;
+    for (int i = 16 * warp; i < count; i += kStep) {
+        copies_wait<kDeep - 2>();
+        const unsigned char* from = ring + stage * L::kStage;
+        ask(i + (kDeep - 1) * kStep, stage ? stage - 1 : kDeep - 1);
+        stage = stage + 1 == kDeep ? 0 : stage + 1;
+        float s[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) {
+                const uint4 k = *reinterpret_cast<const uint4*>(from + (n * NK + c) * 512);
+                mma_16816(s[n], q[2 * c], k.x, k.y, T());
+                mma_16816(s[n], q[2 * c + 1], k.z, k.w, T());
+            }
+        }
+        // element e of s[n]: row g + 8 (e / 2), key i + 8 n + 2 t + e % 2
+        if (tokens > 1 || i + 16 > count)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at_i = i + 8 * n + 2 * t + (e & 1);
+                bool seen = at_i < count;
+                if (tokens > 1) {      // (one token sees every key that is counted)
+                    const int64_t j = key_at(K, i0 + at_i), p = at[e >> 1];
+                    seen = seen && j <= p && (p - j < A.window || j < A.sinks);
+                }
+                if (!seen) s[n][e] = -INFINITY;
+            }
+        float top[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * A.scale2;
+            top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
+        }
+        // the followed maximum moves when it has grown by more than 2^8
+        if (__any_sync(~0u, top[0] > followed[0] + 8.f || top[1] > followed[1] + 8.f)) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float now = fmaxf(followed[r], top[r]), shrink = power(followed[r] - (now == -INFINITY ? 0.f : now));
+                followed[r] = now;
+                total[r] *= shrink;
+#pragma unroll
+                for (int j = 0; j < 8 * NV; ++j) {
+                    o[j][2 * r] *= shrink;
+                    o[j][2 * r + 1] *= shrink;
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = followed[e >> 1];
+                s[n][e] = power(fmaf(s[n][e], A.scale2, f == -INFINITY ? 0.f : kShift - f));
+                total[e >> 1] += s[n][e];
+            }
+        const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]), pack2<T>(s[1][2], s[1][3])};
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            uint32_t v[4][4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const uint4 x = *reinterpret_cast<const uint4*>(from + (2 * NK + n * NV + c) * 512);
+                v[n][0] = x.x; v[n][1] = x.y; v[n][2] = x.z; v[n][3] = x.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t order = j & 1 ? 0x7632 : 0x5410;
+                mma_16816(o[8 * c + j], p, __byte_perm(v[0][j / 2], v[1][j / 2], order), __byte_perm(v[2][j / 2], v[3][j / 2], order), T());
+            }
+        }
+    }
+    copies_wait<0>();
+    __syncthreads();
+    // a warp's sums to shared memory: row g + 8 r, element 64 c + 8 n + j of o[8 c + j][2 r + n % 2], n = 2 t, 2 t + 1
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        total[r] += __shfl_xor_sync(~0u, total[r], 1);
+        total[r] += __shfl_xor_sync(~0u, total[r], 2);
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; j += 4)
+                    *reinterpret_cast<float4*>(&joined[warp][g + 8 * r][64 * c + 16 * t + 8 * n + j]) =
+                        make_float4(o[8 * c + j][2 * r + n], o[8 * c + j + 1][2 * r + n], o[8 * c + j + 2][2 * r + n], o[8 * c + j + 3][2 * r + n]);
+        if (t == 0) {
+            stats[warp][g + 8 * r][0] = followed[r];
+            stats[warp][g + 8 * r][1] = total[r];
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * (DM / 4); e += kThreads) {
+        const int r = e / (DM / 4), c = e % (DM / 4) * 4;
+        if (c >= A.dim) continue;      // (dim is a multiple of 8)
+        float most = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) most = fmaxf(most, stats[k][r][0]);
+        float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+            const float f = stats[k][r][0] == -INFINITY ? (stats[k][r][1] == 0.f ? 0.f : 1.f) : power(stats[k][r][0] - most);
+            const float4 x = *reinterpret_cast<const float4*>(&joined[k][r][c]);
+            sum += f * stats[k][r][1];
+            out.x += f * x.x; out.y += f * x.y; out.z += f * x.z; out.w += f * x.w;
+        }
+        const int row = block * kRows + r;
+        const int64_t h = group * per + row / tokens, tok = row % tokens;
+        if (A.part) {
+            const int64_t to = ((b * A.heads + h) * tokens + tok) * A.chunks + chunk;
+            *reinterpret_cast<float4*>(A.part + to * A.dim + c) = out;
+            if (c == 0) {
+                A.stats[2 * to] = most;
+                A.stats[2 * to + 1] = sum;
+            }
+        } else {
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
+            *reinterpret_cast<uint2*>(static_cast<T*>(A.o) + ((b * tokens + tok) * A.heads + h) * A.dim + c) = make_uint2(pack2<T>(out.x * f, out.y * f), pack2<T>(out.z * f, out.w * f));
         }
     }
 }
@@ -223,12 +509,23 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const _
     }
 }
 
-template <typename T, int DM, int RB> const void* cached_fn(bool packs) {
-    constexpr int V = 16 / sizeof(T);
-    return packs && DM / 8 >= V ? (const void*)cached_kernel<T, DM, (DM / 8 >= V ? V : 1), RB> : (const void*)cached_kernel<T, DM, 1, RB>;
+// A kernel and its shared memory.
+struct Chosen {
+    const void* fn;
+    size_t shared;
+};
+template <typename T, int DM, int RB> Chosen cached_fn(bool packs) {
+    constexpr int V = 16 / sizeof(T), W = DM / 8 >= V ? V : 1;
+    constexpr size_t sums = 16 * RB * (DM + 2) * 4, ring = (size_t)kWarps * kDepth * 2 * (DM / 8 / W) * 512;
+    if (packs && W > 1) return {(const void*)cached_kernel<T, DM, W, RB>, std::max(sums, ring)};
+    return {(const void*)cached_kernel<T, DM, 1, RB>, sums};
 }
-template <typename T> const void* cached_fn(int dim, bool packs) {
+template <typename T> Chosen cached_fn(int dim, bool packs) {
     return dim <= 32 ? cached_fn<T, 32, 4>(packs) : dim <= 64 ? cached_fn<T, 64, 4>(packs) : dim <= 128 ? cached_fn<T, 128, 4>(packs) : cached_fn<T, 256, 2>(packs);
+}
+template <typename T> Chosen cached_mma_fn(int dim) {
+    if (dim <= 64) return {(const void*)cached_mma_kernel<T, 64>, MmaShape<64>::kSmem};
+    return {(const void*)cached_mma_kernel<T, 128>, MmaShape<128>::kSmem};
 }
 
 // How the keys are cut.  `most`: keys that can be in sight at once.  Chunks of 64 to 512 keys: short ones where
@@ -237,12 +534,12 @@ struct Cut {
     int chunk, chunks, blocks;
     size_t part, stats;      // bytes
 };
-Cut cut_of(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity, int64_t window, int64_t sinks) {
+Cut cut_of(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity, int64_t window, int64_t sinks, bool mma) {
     Cut c{};
     const int64_t most = window ? std::min(capacity, std::min(window, kMostTokens) + tokens - 1 + std::min(sinks, kMostTokens)) : capacity;
-    c.blocks = (int)ceil_div(heads / groups * tokens, dim > 128 ? 2 : 4);
+    c.blocks = (int)ceil_div(heads / groups * tokens, mma ? kRows : dim > 128 ? 2 : 4);
     const int64_t units = batch * groups * c.blocks, even = ceil_div(most * units, 6LL * sm_count());
-    c.chunk = (int)std::min<int64_t>(512, std::max<int64_t>(64, ceil_div(even, 64) * 64));
+    c.chunk = (int)std::min<int64_t>(2048, std::max<int64_t>(64, ceil_div(even, 64) * 64));
     c.chunks = (int)std::max<int64_t>(1, ceil_div(most, c.chunk));
     if (c.chunks > 1) {
         const size_t rows = (size_t)batch * heads * tokens * c.chunks;
@@ -267,8 +564,9 @@ extern "C" {
 size_t vqc_attention_step_workspace_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity, int64_t window,
                                           int64_t sinks) {
     if (!sizes_ok(batch, tokens, heads, groups, dim, capacity) || window < 0 || sinks < 0) return (size_t)-1;
-    const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks);
-    return c.part + c.stats;
+    // (the most of the two kernels, one of which the cache's alignment decides on)
+    const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, false), m = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, true);
+    return std::max(c.part + c.stats, m.part + m.stats);
 }
 
 vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity,
@@ -288,7 +586,9 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
         if (!aligned_to(o, 16) || !aligned_to(lengths, 4) || !aligned_to(workspace, 256))
             return set_error(VQC_ERR_INVALID_ARG, call + ": misaligned output, lengths or workspace");
         if (batch * tokens == 0) return VQC_OK;
-        const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks);
+        const bool packs = dim % (16 / (int64_t)e) == 0 && heads_on(heads_of(*cache_k), e, 16) && heads_on(heads_of(*cache_v), e, 16);
+        const bool mma = packs && dtype != VQC_F32 && dim <= 128;
+        const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, mma);
         if (c.chunks > 1 && (!workspace || workspace_bytes < c.part + c.stats)) return set_error(VQC_ERR_WORKSPACE, call + ": workspace too small");
         const int64_t grid = batch * groups * c.blocks * c.chunks, rows = batch * heads * tokens;
         if (grid > 0x7fffffff || rows > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, call + ": sizes out of range");
@@ -307,10 +607,9 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
             a.stats = reinterpret_cast<float*>(static_cast<char*>(workspace) + c.part);
         }
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        const bool packs = dim % (16 / (int64_t)e) == 0 && heads_on(a.k, e, 16) && heads_on(a.v, e, 16);
         void* args[] = {&a};
-        const void* fn = dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
-        cudaError_t err = launch(fn, dim3((unsigned)grid), kThreads, args, s);
+        const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim) : cached_mma_fn<__half>(a.dim)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
+        cudaError_t err = launch(fn.fn, dim3((unsigned)grid), kThreads, args, s, fn.shared);
         if (err == cudaSuccess && c.chunks > 1) {
             const void* join = dtype == VQC_F32 ? (const void*)join_kernel<float> : dtype == VQC_BF16 ? (const void*)join_kernel<__nv_bfloat16> : (const void*)join_kernel<__half>;
             err = launch(join, dim3((unsigned)rows), 256, args, s);

@@ -30,7 +30,7 @@ struct DropArgs {
 
 __device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t seed) {
     uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
-    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);       // (the rounds' keys are the same in all threads)
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
@@ -47,23 +47,36 @@ __device__ __forceinline__ uint32_t word(const uint4& w, int i) { return i == 0 
 
 // What was dropped is zero whatever it held; one rounding of the sum.
 __device__ __forceinline__ float dropped(float x, float res, uint32_t w, const DropArgs& A) {
-    return w < A.limit ? res : fmaf(x, A.scale, res);
+    float y = res;
+    if (w >= A.limit) y = fmaf(x, A.scale, res);
+    return y;
 }
 
 // V elements (16 bytes) of a row at a time; a row holds whole packs, but for the last one of a single row.
-template <typename T, bool kRes> __global__ void __launch_bounds__(256) drop_kernel(const __grid_constant__ DropArgs A) {
+// kState: seed and offset from memory (as arguments they stay out of the vector registers, with all the rounds' keys).
+template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(256, 5) drop_kernel(const __grid_constant__ DropArgs A) {
     constexpr int V = 16 / sizeof(T);
     stream_order();
-    const uint64_t seed = A.state ? A.state[0] : A.seed, offset = A.offset + (A.state ? A.state[1] : 0);
+    const uint64_t seed = kState ? A.state[0] : A.seed, offset = A.offset + (kState ? A.state[1] : 0);
     const int64_t across = A.cols / V, packs = A.rows * across, step = (int64_t)gridDim.x * blockDim.x;
     const T *x = static_cast<const T*>(A.x), *res = static_cast<const T*>(A.res);
     T* y = static_cast<T*>(A.y);
     const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    auto at = [&](int64_t i, int64_t ld) {
+        const int64_t r = A.rows == 1 ? 0 : packs >> 32 ? i / across : (int64_t)((uint32_t)i / (uint32_t)across);
+        return r * ld + (i - r * across) * V;
+    };
+    // the next pack is on the way while this one's words are drawn
+    uint4 xn = make_uint4(0, 0, 0, 0), rn = xn;
+    auto ask = [&](int64_t i) {
+        if (i >= packs) return;
+        xn = *reinterpret_cast<const uint4*>(x + at(i, A.ld_x));
+        if (kRes) rn = *reinterpret_cast<const uint4*>(res + at(i, A.ld_res));
+    };
+    ask(first);
     for (int64_t i = first; i < packs; i += step) {
-        const int64_t r = A.rows == 1 ? 0 : packs >> 32 ? i / across : (int64_t)((uint32_t)i / (uint32_t)across), c = (i - r * across) * V;
-        const uint4 xv = *reinterpret_cast<const uint4*>(x + r * A.ld_x + c);
-        const uint4 rv = kRes ? *reinterpret_cast<const uint4*>(res + r * A.ld_res + c) : make_uint4(0, 0, 0, 0);
-        const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, rw[4] = {rv.x, rv.y, rv.z, rv.w};
+        const uint32_t xw[4] = {xn.x, xn.y, xn.z, xn.w}, rw[4] = {rn.x, rn.y, rn.z, rn.w};
+        ask(i + step);
         uint32_t out[4];
 #pragma unroll
         for (int b = 0; b < V / 4; ++b) {
@@ -109,9 +122,10 @@ template <typename T> __global__ void __launch_bounds__(256) drop_any_kernel(con
     }
 }
 
-template <typename T> const void* drop_fn(bool packs, bool res) {
+template <typename T> const void* drop_fn(bool packs, bool res, bool state) {
     if (!packs) return (const void*)drop_any_kernel<T>;
-    return res ? (const void*)drop_kernel<T, true> : (const void*)drop_kernel<T, false>;
+    if (state) return res ? (const void*)drop_kernel<T, true, true> : (const void*)drop_kernel<T, false, true>;
+    return res ? (const void*)drop_kernel<T, true, false> : (const void*)drop_kernel<T, false, false>;
 }
 
 vqc_status dropout(const char* call, int dtype, int64_t rows, int64_t cols, const void* x, int64_t ld_x, const void* res, int64_t ld_res,
@@ -132,10 +146,10 @@ vqc_status dropout(const char* call, int dtype, int64_t rows, int64_t cols, cons
     a.limit = (uint32_t)std::fmin(std::nearbyint(p * 4294967296.0), 4294967295.0);
     const int64_t v = 16 / (int64_t)e;
     const bool packs = aligned_to(x, 16) && aligned_to(res, 16) && (rows == 1 || (cols % v == 0 && ld_x % v == 0 && (!res || ld_res % v == 0)));
-    const void* fn = dtype == VQC_F32 ? drop_fn<float>(packs, res) : dtype == VQC_BF16 ? drop_fn<__nv_bfloat16>(packs, res) : drop_fn<__half>(packs, res);
+    const void* fn = dtype == VQC_F32 ? drop_fn<float>(packs, res, state) : dtype == VQC_BF16 ? drop_fn<__nv_bfloat16>(packs, res, state) : drop_fn<__half>(packs, res, state);
     const int64_t threads = ceil_div(rows * cols, packs ? v : 4);
     void* args[] = {&a};
-    const cudaError_t err = launch(fn, dim3((unsigned)std::min<int64_t>(std::max<int64_t>(1, ceil_div(threads, 256)), 16LL * sm_count())), 256, args,
+    const cudaError_t err = launch(fn, dim3((unsigned)std::min<int64_t>(std::max<int64_t>(1, ceil_div(threads, 256)), 5LL * sm_count())), 256, args,
                                    static_cast<cudaStream_t>(stream));
     return err == cudaSuccess ? VQC_OK : cuda_error(err, "dropout launch");
 }

@@ -47,30 +47,46 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
     for (int o = lanes / 2; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
     return v;
 }
+// A frequency as a fraction of a turn per position, in 2^-64: a double's mantissa moved to its place (one double product;
+// doubles are slow here).
+__device__ __forceinline__ uint64_t turn_of(double frequency) {
+    const uint64_t u = (uint64_t)__double_as_longlong(frequency * 0.15915494309189533577);      // 1 / 2 pi
+    const int biased = (int)(u >> 52 & 0x7ff), up = biased - 1075 + 64;
+    const uint64_t m = (u & 0xfffffffffffffull) | (biased ? 1ull << 52 : 0);
+    const uint64_t r = up >= 64 || up <= -64 ? 0 : up >= 0 ? m << up : m >> -up;
+    return (int64_t)u < 0 ? 0 - r : r;
+}
 // sin and cos of position * frequency
-__device__ __forceinline__ float2 turned(double frequency, int64_t position) {
-    const double turns = frequency * 0.15915494309189533577;      // 1 / 2 pi
-    const uint64_t f = (uint64_t)((turns - floor(turns)) * 18446744073709551616.0);
-    const int32_t part = (int32_t)((f * (uint64_t)position + 0x80000000ull) >> 32);      // 2^-32 of a turn, to nearest
+__device__ __forceinline__ float2 turned(uint64_t turn, int64_t position) {
+    const int32_t part = (int32_t)((turn * (uint64_t)position + 0x80000000ull) >> 32);      // 2^-32 of a turn, to nearest
     float2 r;
     sincospif((float)part * 4.65661287307739e-10f, &r.x, &r.y);      // 2^-31
     return r;
 }
 
-template <typename T> __device__ __forceinline__ void load4(const T* p, float (&v)[4]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 q = *reinterpret_cast<const float4*>(p);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-    } else {
-        const uint2 q = *reinterpret_cast<const uint2*>(p);
-        const float2 a = unpack2<T>(q.x), b = unpack2<T>(q.y);
-        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+// 4 elements as they lie in memory, and as two pairs of floats
+template <typename T> struct Four {
+    uint2 w;
+    __device__ __forceinline__ void ask(const T* p) { w = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void get(float2 (&v)[2]) const {
+        v[0] = unpack2<T>(w.x);
+        v[1] = unpack2<T>(w.y);
     }
+};
+template <> struct Four<float> {
+    float4 w;
+    __device__ __forceinline__ void ask(const float* p) { w = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void get(float2 (&v)[2]) const {
+        v[0] = make_float2(w.x, w.y);
+        v[1] = make_float2(w.z, w.w);
+    }
+};
+template <typename T> __device__ __forceinline__ void store4(T* p, float2 a, float2 b) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(a.x, a.y), pack2<T>(b.x, b.y));
 }
-template <typename T> __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
-}
+__device__ __forceinline__ float2 neg2(float2 a) { return make_float2(-a.x, -a.y); }
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
 // A unit of work: up to `chunk` heads of one token, by one group of LANES lanes.
 struct Unit {
@@ -80,8 +96,9 @@ struct Unit {
 };
 __device__ __forceinline__ Unit unit_at(const RotaryArgs& A, int64_t u, int total) {
     Unit r;
-    const int64_t token = u / A.chunks;
-    r.first = (int)(u - token * A.chunks) * A.chunk;
+    // (neighbouring groups of lanes have the same heads of neighbouring tokens: a warp's groups walk the same loops)
+    const int64_t tokens = A.batch * A.tokens, token = u % tokens;
+    r.first = (int)(u / tokens) * A.chunk;
     r.last = min(total, r.first + A.chunk);
     r.b = token / A.tokens;
     r.t = token - r.b * A.tokens;
@@ -104,108 +121,162 @@ template <typename T> __device__ __forceinline__ T* out_at(const RotaryArgs& A, 
 // Lane j of a group holds the 4 pairs (4j, n + 4j) for 4j < n, or 8 elements that are not turned.
 template <typename T, int LANES, bool kBack> __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs A) {
     stream_order();
-    constexpr int kGroups = kThreads / LANES;
+    constexpr int kGroups = kThreads / LANES, HB = sizeof(T) == 4 || kBack ? 2 : 4;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, total = A.side[0].heads + A.side[1].heads + A.side[2].heads;
+    const uint32_t peers = LANES == 32 ? ~0u : ((1u << (LANES & 31)) - 1) << (threadIdx.x & 31 & ~(LANES - 1));
     const int turning = A.pairs / 4;
     const bool on = lane < A.dim / 8, turns = lane < turning;
     const int ca = turns ? 4 * lane : 2 * A.pairs + 8 * (lane - turning), cb = turns ? A.pairs + 4 * lane : ca + 4;
     const int64_t units = A.batch * A.tokens * A.chunks, step = (int64_t)gridDim.x * kGroups;
-    double freq[4] = {0, 0, 0, 0};
+    const float per = 1.f / (float)A.dim;
+    auto group_sum = [&](float v) {
+#pragma unroll
+        for (int o = LANES / 2; o; o >>= 1) v += __shfl_xor_sync(peers, v, o);
+        return v;
+    };
+    uint64_t freq[4] = {0, 0, 0, 0};
     if (turns) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) freq[i] = A.frequency[4 * lane + i];
+        for (int i = 0; i < 4; ++i) freq[i] = turn_of(A.frequency[4 * lane + i]);
     }
-    float sum[2][8];
+    float2 sum[2][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[0][i] = sum[1][i] = 0.f;
-    // (every lane of a warp takes part in the sums over lanes: groups without a unit go along with the first)
-    for (int64_t u0 = (int64_t)blockIdx.x * kGroups; u0 < units; u0 += step) {
-        const bool real = u0 + group < units;
-        const Unit U = unit_at(A, real ? u0 + group : u0, total);
-        float cosine[4], sine[4];
+    for (int i = 0; i < 4; ++i) sum[0][i] = sum[1][i] = both(0.f);
+    for (int64_t u = (int64_t)blockIdx.x * kGroups + group; u < units; u += step) {
+        const Unit U = unit_at(A, u, total);
+        float2 cosine[2], sine[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 q = turns ? turned(freq[i], U.pos) : make_float2(0.f, 1.f);
-            sine[i] = q.x;
-            cosine[i] = q.y;
+        for (int i = 0; i < 2; ++i) {
+            const float2 p = turns ? turned(freq[2 * i], U.pos) : make_float2(0.f, 1.f), q = turns ? turned(freq[2 * i + 1], U.pos) : make_float2(0.f, 1.f);
+            sine[i] = make_float2(p.x, q.x);
+            cosine[i] = make_float2(p.y, q.y);
         }
-        float w[8];
-        int last_side = -1;
-        const int most = A.chunk;
-        for (int k = 0; k < most; ++k) {
-            const int hh = U.first + k;
-            const bool have = real && on && hh < U.last;
-            const int s = hh < A.side[0].heads ? 0 : hh < A.side[0].heads + A.side[1].heads ? 1 : 2;
-            const int h = hh - (s > 0 ? A.side[0].heads : 0) - (s > 1 ? A.side[1].heads : 0);
+        int before = 0;
+#pragma unroll
+        for (int s = 0; s < (kBack ? 2 : 3); ++s) {
             const Side& S = A.side[s];
-            if (s != last_side && have && s < 2) {
-                last_side = s;
-                if (S.weight) {
-                    float p[4], q[4];
-                    load4(static_cast<const T*>(S.weight) + ca, p);
-                    load4(static_cast<const T*>(S.weight) + cb, q);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { w[i] = p[i]; w[4 + i] = q[i]; }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = 1.f;
-                }
+            const int lo = max(U.first - before, 0), hi = min(U.last - before, S.heads);
+            before += S.heads;
+            if (lo >= hi) continue;
+            float2 w[4] = {both(1.f), both(1.f), both(1.f), both(1.f)};
+            if (S.weight && on) {
+                Four<T> p[2];
+                float2 v[2];
+                p[0].ask(static_cast<const T*>(S.weight) + ca);
+                p[1].ask(static_cast<const T*>(S.weight) + cb);
+                p[0].get(v);
+                w[0] = v[0]; w[1] = v[1];
+                p[1].get(v);
+                w[2] = v[0]; w[3] = v[1];
             }
-            float x[2][4] = {}, g[2][4] = {};
-            if (have) {
-                const T* p = static_cast<const T*>(S.x.p) + U.b * S.x.batch + U.t * S.x.token + (int64_t)h * S.x.head;
-                load4(p + ca, x[0]);
-                load4(p + cb, x[1]);
-                if constexpr (kBack) {
-                    const T* q = static_cast<const T*>(S.g.p) + U.b * S.g.batch + U.t * S.g.token + (int64_t)h * S.g.head;
-                    load4(q + ca, g[0]);
-                    load4(q + cb, g[1]);
-                }
-            }
-            float ss = 0.f;
+            const T *px = static_cast<const T*>(S.x.p) + U.b * S.x.batch + U.t * S.x.token + lo * S.x.head + ca, *pg = nullptr;
+            if (kBack) pg = static_cast<const T*>(S.g.p) + U.b * S.g.batch + U.t * S.g.token + lo * S.g.head + ca;
+            T* py = out_at<T>(A, U, s, lo);
+            const bool writes = py && on && (!kBack || S.y.p);
+            py += ca;
+            const int other = cb - ca;
+            // The next HB heads' elements are asked for before these are worked on: 8 bytes a load alone would leave HBM waiting.
+            Four<T> next[HB][kBack ? 4 : 2], these[HB][kBack ? 4 : 2];
+            auto ask = [&](int h) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ss += x[0][i] * x[0][i] + x[1][i] * x[1][i];
-            const float r = rsqrtf(group_sum(ss, LANES) / (float)A.dim + A.eps);
-            float out[2][4];
-            if constexpr (!kBack) {
-                if (!have) continue;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float a = x[0][i] * r * w[i], b = x[1][i] * r * w[4 + i];
-                    out[0][i] = a * cosine[i] - b * sine[i];
-                    out[1][i] = b * cosine[i] + a * sine[i];
-                }
-                if (s == 2) {      // values go into the cache as they are
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { out[0][i] = x[0][i]; out[1][i] = x[1][i]; }
-                }
-            } else {
-                float um[2][4], dot = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float ga = g[0][i] * cosine[i] + g[1][i] * sine[i], gb = g[1][i] * cosine[i] - g[0][i] * sine[i];
-                    x[0][i] *= r;
-                    x[1][i] *= r;
-                    if (have && A.part) {
-                        if (s == 0) { sum[0][i] += ga * x[0][i]; sum[0][4 + i] += gb * x[1][i]; }
-                        else { sum[1][i] += ga * x[0][i]; sum[1][4 + i] += gb * x[1][i]; }
+                for (int j = 0; j < HB; ++j) {
+                    if (on && h + j < hi) {
+                        next[j][0].ask(px);
+                        next[j][1].ask(px + other);
+                        if constexpr (kBack) {
+                            next[j][2].ask(pg);
+                            next[j][3].ask(pg + other);
+                        }
                     }
-                    um[0][i] = have ? ga * w[i] : 0.f;
-                    um[1][i] = have ? gb * w[4 + i] : 0.f;
-                    dot += um[0][i] * x[0][i] + um[1][i] * x[1][i];
+                    px += S.x.head;
+                    if (kBack) pg += S.g.head;
                 }
-                dot = group_sum(dot, LANES) / (float)A.dim;
-                if (!have || !S.y.p) continue;
+            };
+            ask(lo);
+#pragma unroll 1
+            for (int h = lo; h < hi; h += HB) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    out[0][i] = r * (um[0][i] - x[0][i] * dot);
-                    out[1][i] = r * (um[1][i] - x[1][i] * dot);
+                for (int j = 0; j < HB; ++j)
+#pragma unroll
+                    for (int i = 0; i < (kBack ? 4 : 2); ++i) these[j][i] = next[j][i];
+                ask(h + HB);
+                float r[HB];
+                float2 x[HB][4];
+#pragma unroll
+                for (int j = 0; j < HB; ++j) {
+                    float2 v[2];
+                    these[j][0].get(v);
+                    x[j][0] = v[0]; x[j][1] = v[1];
+                    these[j][1].get(v);
+                    x[j][2] = v[0]; x[j][3] = v[1];
+                    if (!on || h + j >= hi) x[j][0] = x[j][1] = x[j][2] = x[j][3] = both(0.f);
+                    float2 ss = mul2(x[j][0], x[j][0]);
+#pragma unroll
+                    for (int i = 1; i < 4; ++i) ss = fma2(x[j][i], x[j][i], ss);
+                    r[j] = ss.x + ss.y;
+                }
+#pragma unroll
+                for (int j = 0; j < HB; ++j) r[j] = rsqrtf(fmaf(group_sum(r[j]), per, A.eps));
+                if constexpr (!kBack) {
+#pragma unroll
+                    for (int j = 0; j < HB; ++j) {
+                        if (s < 2) {      // (values go into the cache as they are)
+                            float2 h0[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h0[i] = mul2(mul2(x[j][i], both(r[j])), w[i]);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                x[j][i] = fma2(h0[i], cosine[i], neg2(mul2(h0[2 + i], sine[i])));
+                                x[j][2 + i] = fma2(h0[2 + i], cosine[i], mul2(h0[i], sine[i]));
+                            }
+                        }
+                        if (writes && h + j < hi) {
+                            store4(py, x[j][0], x[j][1]);
+                            store4(py + other, x[j][2], x[j][3]);
+                        }
+                        py += S.y.head;
+                    }
+                } else {
+                    float dot[HB];
+                    float2 um[HB][4];
+#pragma unroll
+                    for (int j = 0; j < HB; ++j) {
+                        float2 g[4], v[2], d = both(0.f);
+                        these[j][2].get(v);
+                        g[0] = v[0]; g[1] = v[1];
+                        these[j][3].get(v);
+                        g[2] = v[0]; g[3] = v[1];
+                        const bool have = on && h + j < hi;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            um[j][i] = fma2(g[i], cosine[i], mul2(g[2 + i], sine[i]));
+                            um[j][2 + i] = fma2(g[2 + i], cosine[i], neg2(mul2(g[i], sine[i])));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (!have) um[j][i] = both(0.f);
+                            x[j][i] = mul2(x[j][i], both(r[j]));
+                            sum[s][i] = fma2(um[j][i], x[j][i], sum[s][i]);
+                            um[j][i] = mul2(um[j][i], w[i]);
+                            d = fma2(um[j][i], x[j][i], d);
+                        }
+                        dot[j] = d.x + d.y;
+                    }
+#pragma unroll
+                    for (int j = 0; j < HB; ++j) dot[j] = -group_sum(dot[j]) * per;
+#pragma unroll
+                    for (int j = 0; j < HB; ++j) {
+                        if (writes && h + j < hi) {
+                            float2 o[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = mul2(fma2(x[j][i], both(dot[j]), um[j][i]), both(r[j]));
+                            store4(py, o[0], o[1]);
+                            store4(py + other, o[2], o[3]);
+                        }
+                        py += S.y.head;
+                    }
                 }
             }
-            T* y = out_at<T>(A, U, s, h);
-            if (!y) continue;
-            store4(y + ca, out[0]);
-            store4(y + cb, out[1]);
         }
     }
     if constexpr (kBack) {
@@ -217,8 +288,8 @@ template <typename T, int LANES, bool kBack> __global__ void __launch_bounds__(k
             if (on) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    joined[group * 8 * LANES + ca + i] = sum[s][i];
-                    joined[group * 8 * LANES + cb + i] = sum[s][4 + i];
+                    joined[group * 8 * LANES + ca + i] = i & 1 ? sum[s][i / 2].y : sum[s][i / 2].x;
+                    joined[group * 8 * LANES + cb + i] = i & 1 ? sum[s][2 + i / 2].y : sum[s][2 + i / 2].x;
                 }
             }
             __syncthreads();
@@ -238,6 +309,12 @@ template <typename T, bool kBack> __global__ void __launch_bounds__(kThreads) ro
     constexpr int kCols = kMostDim / 32, kWarps = kThreads / 32;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, total = A.side[0].heads + A.side[1].heads + A.side[2].heads, n = A.pairs;
     const int64_t units = A.batch * A.tokens * A.chunks;
+    uint64_t freq[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) {
+        const int c = lane + 32 * i;
+        freq[i] = c < 2 * n ? turn_of(A.frequency[c < n ? c : c - n]) : 0;
+    }
     float sum[2][kCols];
 #pragma unroll
     for (int i = 0; i < kCols; ++i) sum[0][i] = sum[1][i] = 0.f;
@@ -247,7 +324,7 @@ template <typename T, bool kBack> __global__ void __launch_bounds__(kThreads) ro
 #pragma unroll
         for (int i = 0; i < kCols; ++i) {
             const int c = lane + 32 * i;
-            turn[i] = c < 2 * n ? turned(A.frequency[c < n ? c : c - n], U.pos) : make_float2(0.f, 1.f);
+            turn[i] = c < 2 * n ? turned(freq[i], U.pos) : make_float2(0.f, 1.f);
             if (c < n) turn[i].x = -turn[i].x;      // y_c = h_c cos + h_partner * (-sin or sin)
         }
         for (int hh = U.first; hh < U.last; ++hh) {
@@ -331,7 +408,7 @@ template <bool kBack> const void* rotary_fn(int dtype, int lanes) {
 bool packs4(int dtype, const Heads& h) { return heads_on(h, elem_size(dtype), 4 * elem_size(dtype)); }
 
 // CTAs of a backward that sums over all tokens: as many as stay on the SMs together.
-int64_t back_ctas(int64_t units, int groups) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), 4LL * sm_count())); }
+int64_t back_ctas(int64_t units, int groups) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), 6LL * sm_count())); }
 // Heads of a token that a group of lanes takes: as many as leave every SM 64 groups (a token's sines and cosines
 // are made once per group).
 int heads_at_once(int64_t tokens, int heads) {
