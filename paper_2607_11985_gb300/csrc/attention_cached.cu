@@ -235,20 +235,20 @@ __device__ __forceinline__ float power(float x) {
     return r;
 }
 // A stage: the pieces of 16 keys and values of a warp, each where the lane that copied it reads it.
-template <int DM> struct MmaShape {
+template <int DM, int W> struct MmaShape {
     static constexpr int NK = DM / 32, NV = DM / 64, kPieces = 2 * NK + 4 * NV, kStage = kPieces * 512, kDeep = DM == 64 ? 4 : 3;
-    static constexpr int kRing = kWarps * kDeep * kStage, kSums = kWarps * kRows * (DM + 4) * 4;
-    static constexpr int kSmem = (kRing > kSums ? kRing : kSums) + kWarps * kRows * 8;
+    static constexpr int kRing = W * kDeep * kStage, kSums = W * kRows * (DM + 4) * 4;
+    static constexpr int kSmem = (kRing > kSums ? kRing : kSums) + W * kRows * 8;
 };
 
-template <typename T, int DM> __global__ void __launch_bounds__(kThreads, DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
-    using L = MmaShape<DM>;
+template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W == 8 ? 1 : DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
+    using L = MmaShape<DM, W>;
     constexpr int NK = L::NK, NV = L::NV, kDeep = L::kDeep;      // pieces of 16 bytes of a lane: of a key, of a value
     constexpr float kShift = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value ? 6.f : 0.f;
     constexpr int P = DM + 4;
     extern __shared__ __align__(16) unsigned char shared[];
     float(*joined)[kRows][P] = reinterpret_cast<float(*)[kRows][P]>(shared);      // in the place of the ring, after it
-    float(*stats)[kRows][2] = reinterpret_cast<float(*)[kRows][2]>(shared + L::kSmem - kWarps * kRows * 8);
+    float(*stats)[kRows][2] = reinterpret_cast<float(*)[kRows][2]>(shared + L::kSmem - W * kRows * 8);
     stream_order();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     int64_t w = blockIdx.x;      // all groups of a chunk together: they read neighbouring memory
@@ -329,7 +329,7 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads, DM == 
         }
         copies_end();
     };
-    constexpr int kStep = 16 * kWarps;
+    constexpr int kStep = 16 * W;
     float o[8 * NV][4], followed[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 8 * NV; ++j)
@@ -437,15 +437,15 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads, DM == 
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < rows * (DM / 4); e += kThreads) {
+    for (int e = threadIdx.x; e < rows * (DM / 4); e += 32 * W) {
         const int r = e / (DM / 4), c = e % (DM / 4) * 4;
         if (c >= A.dim) continue;      // (dim is a multiple of 8)
         float most = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) most = fmaxf(most, stats[k][r][0]);
+        for (int k = 0; k < W; ++k) most = fmaxf(most, stats[k][r][0]);
         float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
+        for (int k = 0; k < W; ++k) {
             const float f = stats[k][r][0] == -INFINITY ? (stats[k][r][1] == 0.f ? 0.f : 1.f) : power(stats[k][r][0] - most);
             const float4 x = *reinterpret_cast<const float4*>(&joined[k][r][c]);
             sum += f * stats[k][r][1];
@@ -523,13 +523,15 @@ template <typename T, int DM, int RB> Chosen cached_fn(bool packs) {
 template <typename T> Chosen cached_fn(int dim, bool packs) {
     return dim <= 32 ? cached_fn<T, 32, 4>(packs) : dim <= 64 ? cached_fn<T, 64, 4>(packs) : dim <= 128 ? cached_fn<T, 128, 4>(packs) : cached_fn<T, 256, 2>(packs);
 }
-template <typename T> Chosen cached_mma_fn(int dim) {
-    if (dim <= 64) return {(const void*)cached_mma_kernel<T, 64>, MmaShape<64>::kSmem};
-    return {(const void*)cached_mma_kernel<T, 128>, MmaShape<128>::kSmem};
+template <typename T, int W> Chosen cached_mma_fn(int dim) {
+    if (dim <= 64) return {(const void*)cached_mma_kernel<T, 64, W>, MmaShape<64, W>::kSmem};
+    return {(const void*)cached_mma_kernel<T, 128, W>, MmaShape<128, W>::kSmem};
 }
+template <typename T> Chosen cached_mma_fn(int dim, bool one) { return one ? cached_mma_fn<T, 8>(dim) : cached_mma_fn<T, kWarps>(dim); }
 
 // How the keys are cut.  `most`: keys that can be in sight at once.  Chunks of 64 to 512 keys: short ones where
 // there are few rows, so that all SMs take part, long ones where the parts of the output would count.
+constexpr int kOne = 1024;
 struct Cut {
     int chunk, chunks, blocks;
     size_t part, stats;      // bytes
@@ -539,6 +541,12 @@ Cut cut_of(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t
     const int64_t most = window ? std::min(capacity, std::min(window, kMostTokens) + tokens - 1 + std::min(sinks, kMostTokens)) : capacity;
     c.blocks = (int)ceil_div(heads / groups * tokens, mma ? kRows : dim > 128 ? 2 : 4);
     const int64_t units = batch * groups * c.blocks, even = ceil_div(most * units, 6LL * sm_count());
+    // (A few keys are one CTA's of 8 warps: the second launch takes longer than 128 keys of a warp.)
+    if (mma && most <= kOne) {
+        c.chunk = kOne;
+        c.chunks = 1;
+        return c;
+    }
     c.chunk = (int)std::min<int64_t>(2048, std::max<int64_t>(64, ceil_div(even, 64) * 64));
     c.chunks = (int)std::max<int64_t>(1, ceil_div(most, c.chunk));
     if (c.chunks > 1) {
@@ -608,8 +616,8 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
         }
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         void* args[] = {&a};
-        const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim) : cached_mma_fn<__half>(a.dim)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
-        cudaError_t err = launch(fn.fn, dim3((unsigned)grid), kThreads, args, s, fn.shared);
+        const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim, c.chunks == 1) : cached_mma_fn<__half>(a.dim, c.chunks == 1)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
+        cudaError_t err = launch(fn.fn, dim3((unsigned)grid), mma && c.chunks == 1 ? 256 : kThreads, args, s, fn.shared);
         if (err == cudaSuccess && c.chunks > 1) {
             const void* join = dtype == VQC_F32 ? (const void*)join_kernel<float> : dtype == VQC_BF16 ? (const void*)join_kernel<__nv_bfloat16> : (const void*)join_kernel<__half>;
             err = launch(join, dim3((unsigned)rows), 256, args, s);

@@ -461,34 +461,39 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// Backward.  Both kernels have one shape: 128 resident rows (queries: Q and dO; keys: K and V) and units of 64 rows of
+// Backward.  Both kernels have one shape: 128 resident rows (queries: Q and dO; keys: K and V) and units of 128 rows of
 // the other side that stream by (X and Y: K and V, or Q and dO):
-//   S = R1 X^T, dP = R2 Y^T   (128 x 64, two buffers in tensor memory, one unit after the other)
-//   P = exp(scale S - lse), dS = P (dP - d), each put back as 16-bit elements where S and dP lay
-//   queries: dQ += dS X      keys: dK += dS X, dV += P Y
+//   S = R1 X^T, dP = R2 Y^T
+//   P = exp(scale S - lse), dS = P (dP - d), put back as 16-bit elements where S and dP lay
+//   queries: dQ += dS X      keys: dV += P Y, dK += dS X
 // With keys resident S is the transposed one, so that P and dS are the left operands of their products as they
-// lie in tensor memory; lse and d of the columns come with the unit.  Warps 4..7 work on the even units,
-// 8..11 on the odd ones.  P and dS are rounded to the operands' type.  float16 holds P times 2^14 and
+// lie in tensor memory; lse and d of the columns come with the unit.  Warps 4..7 work on a unit's first 64 columns,
+// 8..11 on the others.  One set of S and dP is enough (two would not fit beside dK and dV): while P is computed
+// the tensor cores multiply with the last unit's dS and make this unit's dP, and while dS is computed they multiply
+// with P and make the next unit's S:
+//   keys:    .. dV(u) S(u+1) | dK(u) dP(u+1) ..      queries: .. S(u+1) | dQ(u) dP(u+1) ..
+// P and dS are rounded to the operands' type.  float16 holds P times 2^14 and
 // dS times the power of two that keeps its largest possible value, 2 max|dO| max|V| (row norms), below 2^15: gradients
 // of any size keep their bits.
 //
 // Keys that stay visible through a window are seen by all later queries: their tiles' far queries are cut into
 // pieces, a CTA each, whose sums are joined in their order.
-constexpr int kUnit = 64;
-constexpr int kHalf = kUnit * 128;        // 64 rows of 64 elements
+constexpr int kUnit = N;
+constexpr float kBackShift = 14.f;         // of float16's P, in powers of two
 
 template <int C> struct BackShape {
-    static constexpr int kResident = 2 * C * kChunk, kStageX = C * kHalf, kStage = 2 * kStageX;
-    static constexpr int kStages = C == 2 ? 5 : 6;
-    static constexpr int kStats = kResident + kStages * kStage;      // lse and -d of 64 columns for each stage
-    static constexpr int kBars = kStats + kStages * 512;
+    static constexpr int kTile = C * kChunk;
+    static constexpr int kStagesX = C == 2 ? 3 : 4, kStagesY = C == 2 ? 2 : 3;
+    static constexpr int kX = 2 * kTile, kY = kX + kStagesX * kTile;
+    static constexpr int kLse = kY + kStagesY * kTile, kD = kLse + kStagesX * 512;      // of 128 columns for each stage
+    static constexpr int kBars = kD + kStagesY * 512;
     static constexpr int kSmem = kBars + 256;
 };
 
 struct TcBack {
     CUtensorMap q, k, v, g;
     View sight;
-    const float *lse, *d;        // [batch, heads, pitch]: log2 of the sum (infinity behind a sequence), and -d
+    const float *lse, *d;        // [batch, heads, pitch]: kBackShift - log2 of the sum (-infinity behind a sequence), and -d
     const float* most;           // float16: largest row norms of dO and V
     void *gq, *gk, *gv;          // dense; for keys' tiles that are cut:
     float* part;                 // [tile][piece][batch * groups][2][128][64 C]
@@ -512,27 +517,31 @@ __device__ __forceinline__ float float16_factor(const float* most) {
 
 template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThreads, 1) back_tc(const __grid_constant__ TcBack A) {
     using L = BackShape<C>;
-    constexpr int NS = L::kStages;
+    constexpr int NX = L::kStagesX, NY = L::kStagesY;
     constexpr bool kF16 = !std::is_same<T, __nv_bfloat16>::value;
-    constexpr float kShift = kF16 ? 14.f : 0.f;
     extern __shared__ __align__(1024) unsigned char sm[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::kBars);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, rfull = empty + 8 * NS, sfull = rfull + 8, ready = sfull + 16, done = ready + 16, drain = done + 8;
-    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 7);
-    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 8);
+    const uint32_t xfull = smem_u32(bars), xempty = xfull + 8 * NX, yfull = xempty + 8 * NX, yempty = yfull + 8 * NY, rfull = yempty + 8 * NY, sfull = rfull + 8,
+                   pready = sfull + 8, dpfull = pready + 8, dsready = dpfull + 8, done = dsready + 8, drain = done + 8;
+    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NX + 2 * NY + 7);
+    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NX + 2 * NY + 8);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = smem_u32(sm), ring = base + L::kResident;
+    const uint32_t base = smem_u32(sm);
 
     if (tid == 0) {
-        for (int i = 0; i < NS; ++i) {
-            mbar_init(full + 8 * i, 1);
-            mbar_init(empty + 8 * i, 1);
+        for (int i = 0; i < NX; ++i) {
+            mbar_init(xfull + 8 * i, 1);
+            mbar_init(xempty + 8 * i, 1);
+        }
+        for (int i = 0; i < NY; ++i) {
+            mbar_init(yfull + 8 * i, 1);
+            mbar_init(yempty + 8 * i, 1);
         }
         mbar_init(rfull, 1);
-        for (int h = 0; h < 2; ++h) {
-            mbar_init(sfull + 8 * h, 1);
-            mbar_init(ready + 8 * h, 4);
-        }
+        mbar_init(sfull, 1);
+        mbar_init(pready, 8);
+        mbar_init(dpfull, 1);
+        mbar_init(dsready, 8);
         mbar_init(done, 1);
         mbar_init(drain, 1);
         *gave_up = 0;
@@ -582,9 +591,10 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             from = first / kUnit;
             to = last > first ? (last + kUnit - 1) / kUnit : from;
         } else {
-            to = (min(r0 + N, length) + kUnit - 1) / kUnit;
-            from = max(0, r0 - A.sight.window + 1) / kUnit;
-            sinks = min((min(A.sight.sinks, A.sight.tokens) + kUnit - 1) / kUnit, from);
+            const Span keys = span_of(A.sight, r0, min(r0 + N, length));
+            sinks = keys.sinks;
+            from = keys.from;
+            to = keys.to;
         }
     }
     const int span = sinks + to - from, units = kKeys ? span * per : span;
@@ -598,83 +608,115 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
 
     const Roles R{gave_up, A.wait_ns};
     const bool issuer = elect_one();
-    uint32_t asked = 0;
+    uint32_t asked_x = 0, asked_y = 0;
     bool issued = false;
     if (warp == 0) {
         bool ok = true;
         if (units && issuer) {
-            mbar_expect(rfull, L::kResident);
+            mbar_expect(rfull, 2 * L::kTile);
             for (int o = 0; o < 2; ++o)
-                for (int c = 0; c < C; ++c)
-                    for (int j = 0; j < 2; ++j)
-                        tma_load4(base + (o * C + c) * kChunk + j * kHalf, kKeys ? (o ? &A.v : &A.k) : (o ? &A.g : &A.q), 64 * c, r0 + kUnit * j, own, b, rfull);
+                for (int c = 0; c < C; ++c) tma_load4(base + o * L::kTile + c * kChunk, kKeys ? (o ? &A.v : &A.k) : (o ? &A.g : &A.q), 64 * c, r0, own, b, rfull);
         }
-        Ring<NS> r;
+        Ring<NX> x;
+        Ring<NY> y;
         for (int u = 0; u < units; ++u) {
-            ok = R.wait(empty + 8 * r.slot, r.phase ^ 1);
+            const int row = row_of(u), head = head_of(u);
+            const int64_t at = ((int64_t)b * A.heads + head) * A.pitch + row;
+            ok = R.wait(xempty + 8 * x.slot, x.phase ^ 1);
             if (!ok) break;
             if (issuer) {
-                const uint32_t x = ring + r.slot * L::kStage, bar = full + 8 * r.slot;
-                const int row = row_of(u), head = head_of(u);
-                mbar_expect(bar, L::kStage + (kKeys ? 512 : 0));
-                for (int c = 0; c < C; ++c) tma_load4(x + c * kHalf, kKeys ? &A.q : &A.k, 64 * c, row, head, b, bar);
-                for (int c = 0; c < C; ++c) tma_load4(x + L::kStageX + c * kHalf, kKeys ? &A.g : &A.v, 64 * c, row, head, b, bar);
-                if (kKeys) {
-                    const int64_t at = ((int64_t)b * A.heads + head) * A.pitch + row;
-                    const uint32_t stats = base + L::kStats + r.slot * 512;
-                    bulk_load(stats, A.lse + at, 256, bar);
-                    bulk_load(stats + 256, A.d + at, 256, bar);
-                }
+                const uint32_t bar = xfull + 8 * x.slot;
+                mbar_expect(bar, L::kTile + (kKeys ? 512 : 0));
+                for (int c = 0; c < C; ++c) tma_load4(base + L::kX + x.slot * L::kTile + c * kChunk, kKeys ? &A.q : &A.k, 64 * c, row, head, b, bar);
+                if (kKeys) bulk_load(base + L::kLse + x.slot * 512, A.lse + at, 512, bar);
             }
-            ++asked;
-            r.next();
+            ++asked_x;
+            x.next();
+            ok = R.wait(yempty + 8 * y.slot, y.phase ^ 1);
+            if (!ok) break;
+            if (issuer) {
+                const uint32_t bar = yfull + 8 * y.slot;
+                mbar_expect(bar, L::kTile + (kKeys ? 512 : 0));
+                for (int c = 0; c < C; ++c) tma_load4(base + L::kY + y.slot * L::kTile + c * kChunk, kKeys ? &A.g : &A.v, 64 * c, row, head, b, bar);
+                if (kKeys) bulk_load(base + L::kD + y.slot * 512, A.d + at, 512, bar);
+            }
+            ++asked_y;
+            y.next();
         }
         let_next();
         if (!ok && issuer) give_up(gave_up, A.err);
     } else if (warp == 1) {
         constexpr uint32_t kType = kF16 ? 0u : 1u << 7 | 1u << 10;
-        const uint32_t scores = 1u << 4 | kType | (uint32_t)(kUnit >> 3) << 17 | (uint32_t)(N >> 4) << 24;
+        const uint32_t scores = 1u << 4 | kType | (uint32_t)(N >> 3) << 17 | (uint32_t)(N >> 4) << 24;
         const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
-        const uint64_t d1 = smem_desc(base, 0), d2 = smem_desc(base + C * kChunk, 0);
+        const uint64_t d1 = smem_desc(base, 0), d2 = smem_desc(base + L::kTile, 0);
         const uint32_t acc1 = tmem + 256, acc2 = tmem + 256 + 64 * C;
-        Ring<NS> now, then;      // the stages of units u and u - 2
-        bool ok = units == 0 || R.wait(rfull, 0);
-        for (int u = 0; ok && units && u < units + 2; ++u) {
-            const uint32_t buffer = tmem + (u & 1) * 128;
-            if (u >= 2) {
-                ok = R.wait(ready + 8 * (u & 1), (u - 2) >> 1 & 1);
-                if (!ok) break;
-                tc_fence_after();
-                if (issuer) {
-                    const uint64_t dx = smem_desc(ring + then.slot * L::kStage, kHalf), dy = smem_desc(ring + then.slot * L::kStage + L::kStageX, kHalf);
+        // 128 x 128 from a resident tile and a streaming one
+        auto score = [&](uint32_t to_cols, uint64_t da, uint32_t tile_at) {
+            const uint64_t db = smem_desc(tile_at, 0);
 #pragma unroll
-                    for (int j = 0; j < kUnit / 16; ++j) mma_rows(acc1, buffer + 64 + 8 * j, dx + j * (2048 >> 4), outputs, u > 2 || j > 0);
-                    if (kKeys) {
-#pragma unroll
-                        for (int j = 0; j < kUnit / 16; ++j) mma_rows(acc2, buffer + 8 * j, dy + j * (2048 >> 4), outputs, u > 2 || j > 0);
-                    }
-                    mma_commit<1>(empty + 8 * then.slot);
-                }
-                then.next();
+            for (int j = 0; j < 4 * C; ++j) {
+                const uint32_t step = (j / 4 * kChunk + j % 4 * 32) >> 4;
+                mma<1>(to_cols, da + step, db + step, scores, j > 0);
             }
-            if (u < units) {
-                ok = R.wait(full + 8 * now.slot, now.phase);
+        };
+        // += of 16-bit columns (first half at `a`, second 64 columns behind) and a streaming tile
+        auto product = [&](uint32_t acc, uint32_t a, uint32_t tile_at, bool first) {
+            const uint64_t db = smem_desc(tile_at, kChunk);
+#pragma unroll
+            for (int j = 0; j < kUnit / 16; ++j) mma_rows(acc, a + (j / 4) * 64 + (j % 4) * 8, db + j * (2048 >> 4), outputs, !first || j > 0);
+        };
+        // a streaming tile has come; rows behind the sequence: what they hold meets zeros in the products
+        auto arrived = [&](uint32_t bar, uint32_t phase, int offset, int u) {
+            if (!R.wait(bar, phase)) return false;
+            if (tail && row_of(u) == length - tail) clear_rows(sm + offset, C, kUnit, tail, lane);
+            return true;
+        };
+        Ring<NX> x, xu;      // the stages of units u + 1 and u
+        Ring<NY> y, yu;
+        bool ok = units == 0 || R.wait(rfull, 0);
+        for (int u = -1; ok && units && u < units; ++u) {
+            if (u >= 0) {
+                ok = R.wait(pready, u & 1);      // P (queries: S has been read)
                 if (!ok) break;
                 tc_fence_after();
-                // rows behind the sequence: what they hold meets zeros in the products
-                if (tail && row_of(u) == length - tail) clear_rows(sm + L::kResident + now.slot * L::kStage, 2 * C, kUnit, tail, lane);
+                if (kKeys) {
+                    if (issuer) {
+                        product(acc2, tmem, base + L::kY + yu.slot * L::kTile, u == 0);
+                        mma_commit<1>(yempty + 8 * yu.slot);
+                    }
+                    yu.next();
+                }
+            }
+            if (u + 1 < units) {
+                ok = arrived(xfull + 8 * x.slot, x.phase, L::kX + x.slot * L::kTile, u + 1);
+                if (!ok) break;
                 if (issuer) {
-                    const uint64_t dx = smem_desc(ring + now.slot * L::kStage, 0), dy = smem_desc(ring + now.slot * L::kStage + L::kStageX, 0);
-#pragma unroll
-                    for (int j = 0; j < 4 * C; ++j)
-                        mma<1>(buffer, d1 + ((j / 4 * kChunk + j % 4 * 32) >> 4), dx + ((j / 4 * kHalf + j % 4 * 32) >> 4), scores, j > 0);
-#pragma unroll
-                    for (int j = 0; j < 4 * C; ++j)
-                        mma<1>(buffer + 64, d2 + ((j / 4 * kChunk + j % 4 * 32) >> 4), dy + ((j / 4 * kHalf + j % 4 * 32) >> 4), scores, j > 0);
-                    mma_commit<1>(sfull + 8 * (u & 1));
+                    score(tmem, d1, base + L::kX + x.slot * L::kTile);
+                    mma_commit<1>(sfull);
                 }
                 issued = true;
-                now.next();
+                x.next();
+            }
+            if (u >= 0) {
+                ok = R.wait(dsready, u & 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (issuer) {
+                    product(acc1, tmem + 128, base + L::kX + xu.slot * L::kTile, u == 0);
+                    mma_commit<1>(xempty + 8 * xu.slot);
+                }
+                xu.next();
+            }
+            if (u + 1 < units) {
+                ok = arrived(yfull + 8 * y.slot, y.phase, L::kY + y.slot * L::kTile, u + 1);
+                if (!ok) break;
+                if (issuer) {
+                    score(tmem + 128, d2, base + L::kY + y.slot * L::kTile);
+                    mma_commit<1>(dpfull);
+                    if (!kKeys) mma_commit<1>(yempty + 8 * y.slot);
+                }
+                y.next();
             }
         }
         if (issuer) {
@@ -683,95 +725,116 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
         }
     } else if (warp >= 4) {
         const int h = (warp - 4) >> 2, quad = warp & 3, row0 = r0 + quad * 32, row = row0 + lane;
-        const uint32_t lanes = (uint32_t)(quad * 32) << 16, buffer = tmem + lanes + h * 128;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16, ts = tmem + lanes + 64 * h, tdp = ts + 128;
         const float factor = kF16 ? float16_factor(A.most) : 1.f;      // of dS
         const float2 scale = make_float2(A.scale2, A.scale2), times = make_float2(factor * 6.103515625e-05f, factor * 6.103515625e-05f);   // 2^-14
         float2 less, minus;       // of a resident query
         if (!kKeys) {
             const int64_t at = ((int64_t)b * A.heads + own) * A.pitch + row;
-            less.x = less.y = kShift - A.lse[at];
+            less.x = less.y = A.lse[at];
             minus.x = minus.y = A.d[at];
         }
         bool ok = true;
-        Ring<NS> r;
-        if (h) r.next();
-        for (int u = h; u < units; u += 2) {
+        Ring<NX> x;
+        Ring<NY> y;
+        for (int u = 0; u < units; ++u) {
+            const int c0 = row_of(u) + 64 * h;      // this thread's first column
             if (kKeys) {
-                ok = R.wait(full + 8 * r.slot, r.phase);      // lse and d
+                ok = R.wait(xfull + 8 * x.slot, x.phase);      // lse
                 if (!ok) break;
             }
-            ok = R.wait(sfull + 8 * h, u >> 1 & 1);
+            ok = R.wait(sfull, u & 1);
             if (!ok) break;
             tc_fence_after();
-            uint32_t s[kUnit], p[kUnit];
-            tmem_ld32(buffer, s);
-            tmem_ld32(buffer + 32, s + 32);
-            tmem_ld32(buffer + 64, p);
-            tmem_ld32(buffer + 96, p + 32);
+            uint32_t s[64];
+            tmem_ld32(ts, s);
+            tmem_ld32(ts + 32, s + 32);
             tmem_wait();
-            const int c0 = row_of(u);
+            if (!kKeys) {      // the next unit's S may come
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pready);
+            }
             uint32_t bits[2] = {~0u, ~0u};
-            bool some;        // of the unit is not seen by some row
+            bool some;        // of the columns are not seen by some row
             if (kKeys) {
-                some = r0 + N - 1 > c0 || !(c0 + kUnit - 1 - r0 < A.sight.window || r0 + N - 1 < A.sight.sinks) || c0 + kUnit > length;
+                some = r0 + N - 1 > c0 || !(c0 + 63 - r0 < A.sight.window || r0 + N - 1 < A.sight.sinks) || c0 + 64 > length;
                 if (some) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         bits[c] = ~low_bits(row - c0 - 32 * c) & low_bits(length - c0 - 32 * c) & (row < A.sight.sinks ? ~0u : low_bits(row - c0 - 32 * c + A.sight.window));
                 }
             } else {
-                some = c0 + kUnit - 1 > r0 || !(r0 + N - 1 - c0 < A.sight.window || c0 + kUnit - 1 < A.sight.sinks);
+                some = c0 + 63 > r0 || !(r0 + N - 1 - c0 < A.sight.window || c0 + 63 < A.sight.sinks);
                 if (some) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         bits[c] = low_bits(row + 1 - c0 - 32 * c) & (~low_bits(row - A.sight.window + 1 - c0 - 32 * c) | low_bits(A.sight.sinks - c0 - 32 * c));
                 }
             }
-            const float4* lse = reinterpret_cast<const float4*>(sm + L::kStats + r.slot * 512);
+            const float4* lse = reinterpret_cast<const float4*>(sm + L::kLse + x.slot * 512 + 256 * h);
 #pragma unroll
-            for (int c = 0; c < kUnit; c += 4) {
-                float4 l, d;
-                if (kKeys) {
-                    l = lse[c / 4];
-                    d = lse[16 + c / 4];
-                }
+            for (int c = 0; c < 64; c += 4) {
+                float4 l;
+                if (kKeys) l = lse[c / 4];
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    if (kKeys) {
-                        less = e ? make_float2(kShift - l.z, kShift - l.w) : make_float2(kShift - l.x, kShift - l.y);
-                        minus = e ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
-                    }
-                    float2 x = fma2(make_float2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, less);
-                    x.x = power(x.x);
-                    x.y = power(x.y);
-                    float2 y = mul2(kF16 ? mul2(x, times) : x, add2(make_float2(__uint_as_float(p[c + e]), __uint_as_float(p[c + e + 1])), minus));
-                    s[c + e] = __float_as_uint(x.x);
-                    s[c + e + 1] = __float_as_uint(x.y);
-                    p[c + e] = __float_as_uint(y.x);
-                    p[c + e + 1] = __float_as_uint(y.y);
+                    if (kKeys) less = e ? make_float2(l.z, l.w) : make_float2(l.x, l.y);
+                    const float2 v = fma2(make_float2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, less);
+                    s[c + e] = __float_as_uint(power(v.x));
+                    s[c + e + 1] = __float_as_uint(power(v.y));
                 }
             }
             if (some) {
 #pragma unroll
-                for (int c = 0; c < kUnit; ++c) {
-                    const bool seen = bits[c / 32] & 1u << c % 32;
-                    s[c] = seen ? s[c] : 0u;
-                    p[c] = seen ? p[c] : 0u;
+                for (int c = 0; c < 64; ++c) s[c] = bits[c / 32] & 1u << c % 32 ? s[c] : 0u;
+            }
+            if (kKeys) {
+                uint32_t p[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) p[c] = pack2<T>(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+                tmem_st32(ts, p);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pready);
+                ok = R.wait(yfull + 8 * y.slot, y.phase);      // d
+                if (!ok) break;
+            }
+            ok = R.wait(dpfull, u & 1);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t p[64];
+            tmem_ld32(tdp, p);
+            tmem_ld32(tdp + 32, p + 32);
+            tmem_wait();
+            const float4* d = reinterpret_cast<const float4*>(sm + L::kD + y.slot * 512 + 256 * h);
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                float4 m;
+                if (kKeys) m = d[c / 4];
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    if (kKeys) minus = e ? make_float2(m.z, m.w) : make_float2(m.x, m.y);
+                    const float2 v = make_float2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1]));
+                    const float2 w = mul2(kF16 ? mul2(v, times) : v, add2(make_float2(__uint_as_float(p[c + e]), __uint_as_float(p[c + e + 1])), minus));
+                    p[c + e] = __float_as_uint(w.x);
+                    p[c + e + 1] = __float_as_uint(w.y);
                 }
             }
+            if (some) {      // (dP of what is not seen may be anything)
 #pragma unroll
-            for (int c = 0; c < kUnit / 2; ++c) {
-                s[c] = pack2<T>(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
-                p[c] = pack2<T>(__uint_as_float(p[2 * c]), __uint_as_float(p[2 * c + 1]));
+                for (int c = 0; c < 64; ++c) p[c] = bits[c / 32] & 1u << c % 32 ? p[c] : 0u;
             }
-            if (kKeys) tmem_st32(buffer, s);
-            tmem_st32(buffer + 64, p);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) s[c] = pack2<T>(__uint_as_float(p[2 * c]), __uint_as_float(p[2 * c + 1]));
+            tmem_st32(tdp, s);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(ready + 8 * h);
-            r.next();
-            r.next();
+            if (lane == 0) mbar_arrive(dsready);
+            x.next();
+            y.next();
         }
         if (ok && units) ok = R.wait(done, 0);
         if (ok) {
@@ -780,7 +843,7 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             const bool values = kKeys && h, real = units && row < length;
             const float times_out = values ? (kF16 ? 6.103515625e-05f : 1.f) : A.scale / factor;
             const int rows = min(32, A.sight.tokens - row0);
-            unsigned char* stage = sm + L::kResident + (warp - 4) * 4096;      // all products are done: the ring is free
+            unsigned char* stage = sm + L::kX + (warp - 4) * 4096;      // all products are done: the rings are free
             T* to_rows = static_cast<T*>(kKeys ? (h ? A.gv : A.gk) : A.gq) + (((int64_t)b * A.sight.tokens + row0) * row_heads + own) * (int64_t)A.dim;
             const int64_t pitch = (int64_t)row_heads * A.dim;
             float* part = nullptr;
@@ -793,8 +856,8 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
                 tmem_wait();
 #pragma unroll
                 for (int e = 0; e < 64; ++e) o[e] = real ? __float_as_uint(__uint_as_float(o[e]) * times_out) : 0u;
+                uint32_t v[32];
                 if (cut) {
-                    uint32_t v[32];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -802,7 +865,6 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
                         rows_out(stage, v, reinterpret_cast<char*>(part + c + 32 * j), 64 * C * 4, 32, 64, lane);
                     }
                 } else {
-                    uint32_t v[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = pack2<T>(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
                     if (A.dim % 8 == 0) {
@@ -830,16 +892,18 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
     if (*gave_up) {
         if (warp == 0 && units) {
             mbar_wait(rfull, 0, kWaitNs, nullptr);
-            for (uint32_t a = asked > NS ? asked - NS : 0; a < asked; ++a)
-                if (!mbar_wait(full + 8 * (a % NS), a / NS & 1, kWaitNs, nullptr)) break;
+            for (uint32_t a = asked_x > NX ? asked_x - NX : 0; a < asked_x; ++a)
+                if (!mbar_wait(xfull + 8 * (a % NX), a / NX & 1, kWaitNs, nullptr)) break;
+            for (uint32_t a = asked_y > NY ? asked_y - NY : 0; a < asked_y; ++a)
+                if (!mbar_wait(yfull + 8 * (a % NY), a / NY & 1, kWaitNs, nullptr)) break;
         }
         __syncthreads();
     }
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// What the backward needs of each row: -g . o and lse in powers of two (infinity behind a sequence: no probability), 16
-// lanes a row, and for float16 the largest squared norms of g's and v's rows.  Bound by HBM.
+// What the backward needs of each row: -g . o and -lse in powers of two, with float16's shift of P (-infinity behind a
+// sequence: no probability), 16 lanes a row, and for float16 the largest squared norms of g's and v's rows.  Bound by HBM.
 struct RowArgs {
     Heads g, v;
     const void* o;
@@ -847,6 +911,7 @@ struct RowArgs {
     float *lse, *d, *most;       // most: [2], or NULL
     const int32_t* lengths;
     int64_t batch, tokens, pitch;
+    float shift;
     int heads, groups, dim, packs;
 };
 __device__ __forceinline__ float sum16(float v) {
@@ -893,7 +958,7 @@ template <typename T> __global__ void __launch_bounds__(256) rows_tc_kernel(cons
         if (A.most) most[0] = fmaxf(most[0], sum16(n));
         if (c == 0) {
             A.d[at] = in ? -s : 0.f;
-            A.lse[at] = in ? A.saved[(b * A.heads + h) * A.tokens + t] * 1.44269504088896341f : INFINITY;
+            A.lse[at] = in ? A.shift - A.saved[(b * A.heads + h) * A.tokens + t] * 1.44269504088896341f : -INFINITY;
         }
     }
     if (!A.most) return;
@@ -1116,7 +1181,7 @@ vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes,
     const int heads[4] = {a.heads, a.groups, a.groups, a.heads};
     CUtensorMap* map[4] = {&t.q, &t.k, &t.v, &t.g};
     char* at = static_cast<char*>(ws);
-    st = maps_of(a, from, heads, map, 4, kUnit, at, bytes, s);
+    st = maps_of(a, from, heads, map, 4, N, at, bytes, s);
     if (st != VQC_OK) return st;
     const BackSpace b = back_space(a.dtype, a.batch, a.sight.tokens, a.heads, a.groups, a.dim, a.sight.window, a.sight.sinks);
     if (2 * b.stats + b.most + b.part > bytes) return set_error(VQC_ERR_WORKSPACE, "attention: workspace too small");
@@ -1132,6 +1197,7 @@ vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes,
     r.lengths = a.sight.lengths;
     r.batch = a.batch; r.tokens = a.sight.tokens; r.pitch = b.pitch;
     r.heads = a.heads; r.groups = a.groups; r.dim = a.dim;
+    r.shift = a.dtype == VQC_F16 ? kBackShift : 0.f;
     r.packs = a.dim % 8 == 0 && heads_on(a.g, 2, 16) && heads_on(a.v, 2, 16);
     cudaError_t e = cudaSuccess;
     if (r.most) e = cudaMemsetAsync(r.most, 0, 8, s);

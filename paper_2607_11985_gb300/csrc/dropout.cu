@@ -54,7 +54,7 @@ __device__ __forceinline__ float dropped(float x, float res, uint32_t w, const D
 
 // V elements (16 bytes) of a row at a time; a row holds whole packs, but for the last one of a single row.
 // kState: seed and offset from memory (as arguments they stay out of the vector registers, with all the rounds' keys).
-template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(256, 5) drop_kernel(const __grid_constant__ DropArgs A) {
+template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(256, 6) drop_kernel(const __grid_constant__ DropArgs A) {
     constexpr int V = 16 / sizeof(T);
     stream_order();
     const uint64_t seed = kState ? A.state[0] : A.seed, offset = A.offset + (kState ? A.state[1] : 0);
@@ -66,17 +66,10 @@ template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(
         const int64_t r = A.rows == 1 ? 0 : packs >> 32 ? i / across : (int64_t)((uint32_t)i / (uint32_t)across);
         return r * ld + (i - r * across) * V;
     };
-    // the next pack is on the way while this one's words are drawn
-    uint4 xn = make_uint4(0, 0, 0, 0), rn = xn;
-    auto ask = [&](int64_t i) {
-        if (i >= packs) return;
-        xn = *reinterpret_cast<const uint4*>(x + at(i, A.ld_x));
-        if (kRes) rn = *reinterpret_cast<const uint4*>(res + at(i, A.ld_res));
-    };
-    ask(first);
     for (int64_t i = first; i < packs; i += step) {
-        const uint32_t xw[4] = {xn.x, xn.y, xn.z, xn.w}, rw[4] = {rn.x, rn.y, rn.z, rn.w};
-        ask(i + step);
+        const uint4 xv = *reinterpret_cast<const uint4*>(x + at(i, A.ld_x));
+        const uint4 rv = kRes ? *reinterpret_cast<const uint4*>(res + at(i, A.ld_res)) : make_uint4(0, 0, 0, 0);
+        const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, rw[4] = {rv.x, rv.y, rv.z, rv.w};
         uint32_t out[4];
 #pragma unroll
         for (int b = 0; b < V / 4; ++b) {
@@ -149,7 +142,7 @@ vqc_status dropout(const char* call, int dtype, int64_t rows, int64_t cols, cons
     const void* fn = dtype == VQC_F32 ? drop_fn<float>(packs, res, state) : dtype == VQC_BF16 ? drop_fn<__nv_bfloat16>(packs, res, state) : drop_fn<__half>(packs, res, state);
     const int64_t threads = ceil_div(rows * cols, packs ? v : 4);
     void* args[] = {&a};
-    const cudaError_t err = launch(fn, dim3((unsigned)std::min<int64_t>(std::max<int64_t>(1, ceil_div(threads, 256)), 5LL * sm_count())), 256, args,
+    const cudaError_t err = launch(fn, dim3((unsigned)std::min<int64_t>(std::max<int64_t>(1, ceil_div(threads, 256)), 30LL * sm_count())), 256, args,
                                    static_cast<cudaStream_t>(stream));
     return err == cudaSuccess ? VQC_OK : cuda_error(err, "dropout launch");
 }
