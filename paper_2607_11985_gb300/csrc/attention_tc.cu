@@ -472,6 +472,9 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
 // the tensor cores multiply with the last unit's dS and make this unit's dP, and while dS is computed they multiply
 // with P and make the next unit's S:
 //   keys:    .. dV(u) S(u+1) | dK(u) dP(u+1) ..      queries: .. S(u+1) | dQ(u) dP(u+1) ..
+// A 128 x 128 x 16 product takes 64 cycles with its left operand in tensor memory and about 100 with both in shared
+// memory, which the left one is read from once for every 64 columns.  So the resident rows lie in tensor memory
+// where there is room (queries, and keys of heads up to 64 elements; beside dK and dV of 128 there is none).
 // P and dS are rounded to the operands' type.  float16 holds P times 2^14 and
 // dS times the power of two that keeps its largest possible value, 2 max|dO| max|V| (row norms), below 2^15: gradients
 // of any size keep their bits.
@@ -481,10 +484,11 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
 constexpr int kUnit = N;
 constexpr float kBackShift = 14.f;         // of float16's P, in powers of two
 
-template <int C> struct BackShape {
+template <int C, bool kKeys> struct BackShape {
+    static constexpr bool kInTmem = !kKeys || C == 1;      // the resident rows
     static constexpr int kTile = C * kChunk;
     static constexpr int kStagesX = C == 2 ? 3 : 4, kStagesY = C == 2 ? 2 : 3;
-    static constexpr int kX = 2 * kTile, kY = kX + kStagesX * kTile;
+    static constexpr int kX = kInTmem ? 0 : 2 * kTile, kY = kX + kStagesX * kTile;
     static constexpr int kLse = kY + kStagesY * kTile, kD = kLse + kStagesX * 512;      // of 128 columns for each stage
     static constexpr int kBars = kD + kStagesY * 512;
     static constexpr int kSmem = kBars + 256;
@@ -492,6 +496,8 @@ template <int C> struct BackShape {
 
 struct TcBack {
     CUtensorMap q, k, v, g;
+    Heads rows[4];               // the same as they lie in memory: q, k, v, g
+    Heads resident[2];           // of them, those whose rows are resident
     View sight;
     const float *lse, *d;        // [batch, heads, pitch]: kBackShift - log2 of the sum (-infinity behind a sequence), and -d
     const float* most;           // float16: largest row norms of dO and V
@@ -501,9 +507,9 @@ struct TcBack {
     unsigned long long wait_ns;
     int64_t pitch;
     int tiles, planes;           // of 128 resident rows; heads (groups) of all sequences
-    int cut, pieces, piece;      // keys: tiles that are cut, pieces behind the first, queries of one
+    int cut, pieces, piece;      // keys: tiles that are cut, pieces behind the first, queries of one (0: even parts of all units)
     float scale, scale2;
-    int heads, groups, dim;
+    int heads, groups, dim, width;       // width: elements of a head in memory (copies: a multiple of 8)
 };
 
 // 2^k of float16's dS
@@ -516,15 +522,16 @@ __device__ __forceinline__ float float16_factor(const float* most) {
 }
 
 template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThreads, 1) back_tc(const __grid_constant__ TcBack A) {
-    using L = BackShape<C>;
+    using L = BackShape<C, kKeys>;
+    constexpr bool kInTmem = L::kInTmem;
     constexpr int NX = L::kStagesX, NY = L::kStagesY;
     constexpr bool kF16 = !std::is_same<T, __nv_bfloat16>::value;
     extern __shared__ __align__(1024) unsigned char sm[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::kBars);
     const uint32_t xfull = smem_u32(bars), xempty = xfull + 8 * NX, yfull = xempty + 8 * NX, yempty = yfull + 8 * NY, rfull = yempty + 8 * NY, sfull = rfull + 8,
                    pready = sfull + 8, dpfull = pready + 8, dsready = dpfull + 8, done = dsready + 8, drain = done + 8;
-    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NX + 2 * NY + 7);
-    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NX + 2 * NY + 8);
+    volatile int* gave_up = reinterpret_cast<volatile int*>(bars + 2 * NX + 2 * NY + 8);
+    uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + 2 * NX + 2 * NY + 9);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = smem_u32(sm);
 
@@ -537,7 +544,7 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             mbar_init(yfull + 8 * i, 1);
             mbar_init(yempty + 8 * i, 1);
         }
-        mbar_init(rfull, 1);
+        mbar_init(rfull, kInTmem ? 8 : 1);
         mbar_init(sfull, 1);
         mbar_init(pready, 8);
         mbar_init(dpfull, 1);
@@ -565,7 +572,10 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
     const int per = A.heads / A.groups, which = blockIdx.x % A.planes, row_heads = kKeys ? A.groups : A.heads;
     int tile = blockIdx.x / A.planes, piece = 0;
     if (kKeys) {
-        if (tile < A.cut * A.pieces) {
+        if (!A.piece && A.cut) {
+            piece = tile % (A.pieces + 1);
+            tile /= A.pieces + 1;
+        } else if (tile < A.cut * A.pieces) {
             piece = 1 + tile % A.pieces;
             tile /= A.pieces;
         } else {
@@ -582,9 +592,9 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
         if constexpr (kKeys) {
             // past the window of all, in whole units
             const int near = (int)min(((int64_t)r0 + N + min(A.sight.window, A.sight.tokens) + kUnit - 1) / kUnit * kUnit, (int64_t)1 << 30);
-            const bool all = (r0 < A.sight.sinks || A.sight.window > A.sight.tokens) && !cut;
-            int first = r0, last = all ? length : min(length, cut ? near : min(r0 + N, length) - 1 + A.sight.window);
-            if (piece) {
+            const bool far = cut && A.piece, all = (r0 < A.sight.sinks || A.sight.window > A.sight.tokens) && !far;
+            int first = r0, last = all ? length : min(length, far ? near : min(r0 + N, length) - 1 + A.sight.window);
+            if (piece && A.piece) {
                 first = near + (piece - 1) * A.piece;
                 last = min(length, first + A.piece);
             }
@@ -597,13 +607,18 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             to = keys.to;
         }
     }
-    const int span = sinks + to - from, units = kKeys ? span * per : span;
+    const int span = sinks + to - from;
+    int units = kKeys ? span * per : span, unit0 = 0;
+    if (cut && !A.piece) {
+        unit0 = (int)((int64_t)units * piece / (A.pieces + 1));
+        units = (int)((int64_t)units * (piece + 1) / (A.pieces + 1)) - unit0;
+    }
     // first row of a unit, and its head
     auto row_of = [&](int u) {
-        const int i = kKeys ? u % span : u;
+        const int i = kKeys ? (unit0 + u) % span : u;
         return (i < sinks ? i : from + i - sinks) * kUnit;
     };
-    auto head_of = [&](int u) { return kKeys ? own * per + u / span : own / per; };
+    auto head_of = [&](int u) { return kKeys ? own * per + (unit0 + u) / span : own / per; };
     const int tail = length < A.sight.tokens ? length % kUnit : 0;
 
     const Roles R{gave_up, A.wait_ns};
@@ -612,7 +627,7 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
     bool issued = false;
     if (warp == 0) {
         bool ok = true;
-        if (units && issuer) {
+        if (units && issuer && !kInTmem) {
             mbar_expect(rfull, 2 * L::kTile);
             for (int o = 0; o < 2; ++o)
                 for (int c = 0; c < C; ++c) tma_load4(base + o * L::kTile + c * kChunk, kKeys ? (o ? &A.v : &A.k) : (o ? &A.g : &A.q), 64 * c, r0, own, b, rfull);
@@ -651,13 +666,14 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
         const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
         const uint64_t d1 = smem_desc(base, 0), d2 = smem_desc(base + L::kTile, 0);
         const uint32_t acc1 = tmem + 256, acc2 = tmem + 256 + 64 * C;
-        // 128 x 128 from a resident tile and a streaming one
-        auto score = [&](uint32_t to_cols, uint64_t da, uint32_t tile_at) {
-            const uint64_t db = smem_desc(tile_at, 0);
+        // 128 x 128 from the resident rows (`which` of them) and a streaming tile
+        auto score = [&](uint32_t to_cols, int which, uint32_t tile_at) {
+            const uint64_t db = smem_desc(tile_at, 0), da = which ? d2 : d1;
 #pragma unroll
             for (int j = 0; j < 4 * C; ++j) {
                 const uint32_t step = (j / 4 * kChunk + j % 4 * 32) >> 4;
-                mma<1>(to_cols, da + step, db + step, scores, j > 0);
+                if (kInTmem) mma_rows(to_cols, tmem + 384 + 64 * which + 8 * j, db + step, scores, j > 0);
+                else mma<1>(to_cols, da + step, db + step, scores, j > 0);
             }
         };
         // += of 16-bit columns (first half at `a`, second 64 columns behind) and a streaming tile
@@ -675,6 +691,17 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
         Ring<NX> x, xu;      // the stages of units u + 1 and u
         Ring<NY> y, yu;
         bool ok = units == 0 || R.wait(rfull, 0);
+        tc_fence_after();
+        auto with_ds = [&](int u) {      // dK or dQ += dS X
+            if (!R.wait(dsready, u & 1)) return false;
+            tc_fence_after();
+            if (issuer) {
+                product(acc1, tmem + 128, base + L::kX + xu.slot * L::kTile, u == 0);
+                mma_commit<1>(xempty + 8 * xu.slot);
+            }
+            xu.next();
+            return true;
+        };
         for (int u = -1; ok && units && u < units; ++u) {
             if (u >= 0) {
                 ok = R.wait(pready, u & 1);      // P (queries: S has been read)
@@ -692,27 +719,18 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
                 ok = arrived(xfull + 8 * x.slot, x.phase, L::kX + x.slot * L::kTile, u + 1);
                 if (!ok) break;
                 if (issuer) {
-                    score(tmem, d1, base + L::kX + x.slot * L::kTile);
+                    score(tmem, 0, base + L::kX + x.slot * L::kTile);
                     mma_commit<1>(sfull);
                 }
                 issued = true;
                 x.next();
             }
-            if (u >= 0) {
-                ok = R.wait(dsready, u & 1);
-                if (!ok) break;
-                tc_fence_after();
-                if (issuer) {
-                    product(acc1, tmem + 128, base + L::kX + xu.slot * L::kTile, u == 0);
-                    mma_commit<1>(xempty + 8 * xu.slot);
-                }
-                xu.next();
-            }
+            if (u >= 0 && !(ok = with_ds(u))) break;
             if (u + 1 < units) {
                 ok = arrived(yfull + 8 * y.slot, y.phase, L::kY + y.slot * L::kTile, u + 1);
                 if (!ok) break;
                 if (issuer) {
-                    score(tmem + 128, d2, base + L::kY + y.slot * L::kTile);
+                    score(tmem + 128, 1, base + L::kY + y.slot * L::kTile);
                     mma_commit<1>(dpfull);
                     if (!kKeys) mma_commit<1>(yempty + 8 * y.slot);
                 }
@@ -735,14 +753,29 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             minus.x = minus.y = A.d[at];
         }
         bool ok = true;
+        if (kInTmem && units) {      // a row per lane, as the left operands of products lie there
+            const Heads& from_rows = A.resident[h];
+            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(from_rows.p) + (int64_t)b * from_rows.batch + (int64_t)row * from_rows.token + (int64_t)own * from_rows.head);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                uint32_t v[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 w = row < A.sight.tokens && 64 * c + 8 * i < A.width ? p[8 * c + i] : make_uint4(0, 0, 0, 0);
+                    v[4 * i] = w.x; v[4 * i + 1] = w.y; v[4 * i + 2] = w.z; v[4 * i + 3] = w.w;
+                }
+                tmem_st32(tmem + lanes + 384 + 64 * h + 32 * c, v);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(rfull);
+        }
         Ring<NX> x;
         Ring<NY> y;
         for (int u = 0; u < units; ++u) {
             const int c0 = row_of(u) + 64 * h;      // this thread's first column
-            if (kKeys) {
-                ok = R.wait(xfull + 8 * x.slot, x.phase);      // lse
-                if (!ok) break;
-            }
+            // (lse came with the unit's tile, which the scores were made of; d below as well)
             ok = R.wait(sfull, u & 1);
             if (!ok) break;
             tc_fence_after();
@@ -798,8 +831,6 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pready);
-                ok = R.wait(yfull + 8 * y.slot, y.phase);      // d
-                if (!ok) break;
             }
             ok = R.wait(dpfull, u & 1);
             if (!ok) break;
@@ -891,7 +922,7 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
     tc_fence_after();
     if (*gave_up) {
         if (warp == 0 && units) {
-            mbar_wait(rfull, 0, kWaitNs, nullptr);
+            if (!kInTmem) mbar_wait(rfull, 0, kWaitNs, nullptr);
             for (uint32_t a = asked_x > NX ? asked_x - NX : 0; a < asked_x; ++a)
                 if (!mbar_wait(xfull + 8 * (a % NX), a / NX & 1, kWaitNs, nullptr)) break;
             for (uint32_t a = asked_y > NY ? asked_y - NY : 0; a < asked_y; ++a)
@@ -1047,8 +1078,9 @@ bool in_place(const Heads& h, int64_t batch, int64_t tokens, int64_t heads, int6
 size_t copy_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t dim) { return align256((size_t)(batch * tokens * heads) * padded(dim) * 2); }
 
 // Maps of the operands, after copies of those that need one into `ws`.
+// (`placed`, where given: the operands as they are read.)
 vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* heads, CUtensorMap* const* map, int count, int box, char*& ws, size_t& bytes,
-                   cudaStream_t s) {
+                   Heads* placed, cudaStream_t s) {
     CopyJobs jobs{};
     jobs.tokens = a.sight.tokens;
     jobs.dim = a.dim;
@@ -1069,6 +1101,7 @@ vqc_status maps_of(const AttentionArgs& a, const Heads* const* from, const int* 
             ws += need;
             bytes -= need;
         }
+        if (placed) placed[i] = h;
         if (!make_map(map[i], h, a.dtype, a.batch, a.sight.tokens, heads[i], dim, box)) return set_error(VQC_ERR_CUDA, "attention: a tensor map was refused");
     }
     if (!copies) return VQC_OK;
@@ -1095,13 +1128,15 @@ template <typename T, int C> cudaError_t launch_forward(const TcAttention& t, un
 
 template <typename T, int C, bool kKeys> cudaError_t launch_back(const TcBack& t, cudaStream_t s) {
     void* args[] = {const_cast<TcBack*>(&t)};
-    const int64_t tiles = t.tiles + (kKeys ? (int64_t)t.cut * t.pieces : 0);
-    return launch((const void*)back_tc<T, C, kKeys>, dim3((unsigned)(tiles * t.planes)), kThreads, args, s, BackShape<C>::kSmem);
+    const int64_t tiles = t.tiles + (kKeys ? (int64_t)t.cut * t.pieces : 0);      // (even parts: tiles * (pieces + 1) as well)
+    return launch((const void*)back_tc<T, C, kKeys>, dim3((unsigned)(tiles * t.planes)), kThreads, args, s, BackShape<C, kKeys>::kSmem);
 }
 template <typename T, int C> cudaError_t run_back(TcBack& t, const AttentionArgs& a, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
     if (a.gk) {
         t.planes = (int)(a.batch * a.groups);
+        t.resident[0] = t.rows[1];
+        t.resident[1] = t.rows[2];
         e = launch_back<T, C, true>(t, s);
         if (e == cudaSuccess && t.cut) {
             int width = 64 * C;
@@ -1112,6 +1147,8 @@ template <typename T, int C> cudaError_t run_back(TcBack& t, const AttentionArgs
     }
     if (e == cudaSuccess && a.gq) {
         t.planes = (int)(a.batch * a.heads);
+        t.resident[0] = t.rows[0];
+        t.resident[1] = t.rows[3];
         e = launch_back<T, C, false>(t, s);
     }
     return e;
@@ -1128,6 +1165,15 @@ BackSpace back_space(int dtype, int64_t batch, int64_t tokens, int64_t heads, in
     b.pitch = ceil_div(tokens, N) * N;
     b.stats = align256((size_t)(batch * heads * b.pitch) * 4);
     b.most = dtype == VQC_F16 ? 256 : 0;
+    // Few tiles of keys leave SMs idle: each is cut into even parts of its units, of which every head has about half as
+    // many as there are tiles.  (1 x 1024 tokens, 16 heads over 4, bfloat16: 56 us in 32 CTAs, 25 in 128.)
+    const int64_t tiles = ceil_div(tokens, N), all = tiles * batch * groups, sms = sm_count();
+    if (2 * all <= sms) {
+        b.pieces = (int)std::min<int64_t>(std::min<int64_t>(sms / all, 8), std::max<int64_t>(1, heads / groups * (tiles + 1) / 4)) - 1;
+        b.cut = b.pieces ? (int)tiles : 0;
+        b.part = align256((size_t)b.cut * (b.pieces + 1) * batch * groups * 2 * N * (dim <= 64 ? 64 : 128) * 4);
+        return b;
+    }
     // Keys seen from behind the window: pieces as long as a window, 2048 queries at least (a piece writes its sums as floats).
     if (sinks > 0 && window < tokens) {
         b.piece = (int)std::max<int64_t>(2048, ceil_div(window + N, kUnit) * kUnit);
@@ -1161,7 +1207,7 @@ vqc_status attention_tc_forward(const AttentionArgs& a, void* ws, size_t bytes, 
     const int heads[3] = {a.heads, a.groups, a.groups};
     CUtensorMap* map[3] = {&t.q, &t.k, &t.v};
     char* at = static_cast<char*>(ws);
-    st = maps_of(a, from, heads, map, 3, N, at, bytes, s);
+    st = maps_of(a, from, heads, map, 3, N, at, bytes, nullptr, s);
     if (st != VQC_OK) return st;
     t.o = a.o;
     t.saved = a.saved;
@@ -1181,7 +1227,8 @@ vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes,
     const int heads[4] = {a.heads, a.groups, a.groups, a.heads};
     CUtensorMap* map[4] = {&t.q, &t.k, &t.v, &t.g};
     char* at = static_cast<char*>(ws);
-    st = maps_of(a, from, heads, map, 4, N, at, bytes, s);
+    st = maps_of(a, from, heads, map, 4, N, at, bytes, t.rows, s);
+    t.width = (int)padded(a.dim);
     if (st != VQC_OK) return st;
     const BackSpace b = back_space(a.dtype, a.batch, a.sight.tokens, a.heads, a.groups, a.dim, a.sight.window, a.sight.sinks);
     if (2 * b.stats + b.most + b.part > bytes) return set_error(VQC_ERR_WORKSPACE, "attention: workspace too small");
