@@ -467,15 +467,17 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
     }
 }
 
-// A row's chunks joined: a CTA per row, 8 warps take every 8th chunk.
-template <typename T> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ CachedArgs A) {
+// A row's chunks joined, in an order of their own: by a warp (kWarpsOfRow 1), or where there are many by 8 warps, which take every
+// 8th chunk.
+template <typename T, int kWarpsOfRow> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ CachedArgs A, int64_t rows) {
     stream_order();
     constexpr int kCols = kMostDim / 32;
     __shared__ float sums[8][kMostDim], weights[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row = blockIdx.x, t = row % A.tokens, h = row / A.tokens % A.heads, b = row / A.tokens / A.heads;
+    const int64_t row = kWarpsOfRow == 1 ? blockIdx.x * 8ll + warp : blockIdx.x, t = row % A.tokens, h = row / A.tokens % A.heads, b = row / A.tokens / A.heads;
+    if (row >= rows) return;
     const Keys K = keys_of(A, b);
-    const int chunks = (int)max((int64_t)1, (K.count + A.chunk - 1) / A.chunk);
+    const int chunks = (int)max((int64_t)1, (K.count + A.chunk - 1) / A.chunk), first = kWarpsOfRow == 1 ? 0 : warp;
     const float* stats = A.stats + 2 * row * A.chunks;
     float most = -INFINITY;
     for (int c = lane; c < chunks; c += 32) most = fmaxf(most, stats[2 * c]);
@@ -484,30 +486,39 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const _
     float out[kCols], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kCols; ++i) out[i] = 0.f;
-    for (int c = warp; c < chunks; c += 8) {
+#pragma unroll 4
+    for (int c = first; c < chunks; c += kWarpsOfRow) {
         const float m = stats[2 * c], l = stats[2 * c + 1];
-        if (m == -INFINITY && l == 0.f) continue;
-        const float f = exp2f(m - (most == -INFINITY ? 0.f : most));
+        const float f = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(m - most);
         sum += f * l;
         const float* p = A.part + (row * A.chunks + c) * A.dim;
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
             if (lane + 32 * i < A.dim) out[i] += f * p[lane + 32 * i];
     }
+    T* o = static_cast<T*>(A.o) + ((b * A.tokens + t) * A.heads + h) * A.dim;
+    if constexpr (kWarpsOfRow == 1) {
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int i = 0; i < kCols; ++i) sums[warp][lane + 32 * i] = out[i];
-    if (lane == 0) weights[warp] = sum;
-    __syncthreads();
-    for (int c = threadIdx.x; c < A.dim; c += 256) {
-        float v = 0.f, total = 0.f;
+        for (int i = 0; i < kCols; ++i)
+            if (lane + 32 * i < A.dim) o[lane + 32 * i] = from_f<T>(out[i] * f);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v += sums[i][c];
-            total += weights[i];
+        for (int i = 0; i < kCols; ++i) sums[warp][lane + 32 * i] = out[i];
+        if (lane == 0) weights[warp] = sum;
+        __syncthreads();
+        for (int c = threadIdx.x; c < A.dim; c += 256) {
+            float v = 0.f, total = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v += sums[i][c];
+                total += weights[i];
+            }
+            o[c] = from_f<T>(total == 0.f ? 0.f : v / total);
         }
-        static_cast<T*>(A.o)[((b * A.tokens + t) * A.heads + h) * A.dim + c] = from_f<T>(total == 0.f ? 0.f : v / total);
     }
 }
+template <typename T> const void* join_fn(bool wide) { return wide ? (const void*)join_kernel<T, 8> : (const void*)join_kernel<T, 1>; }
 
 // A kernel and its shared memory.
 struct Chosen {
@@ -529,25 +540,38 @@ template <typename T, int W> Chosen cached_mma_fn(int dim) {
 }
 template <typename T> Chosen cached_mma_fn(int dim, bool one) { return one ? cached_mma_fn<T, 8>(dim) : cached_mma_fn<T, kWarps>(dim); }
 
-// How the keys are cut.  `most`: keys that can be in sight at once.  Chunks of 64 to 512 keys: short ones where
-// there are few rows, so that all SMs take part, long ones where the parts of the output would count.
-constexpr int kOne = 1024;
+// How the keys are cut.  `most`: keys that can be in sight at once.  The chunks of one, two, .. waves of CTAs that the SMs
+// hold together are compared by their longest SM: its keys, and for each CTA the time of about 192 keys to begin and to
+// end.  Sequences of a batch have other lengths, which the host does not know: the same for two thirds of the
+// keys, dealt as SMs get free, counts twice.
 struct Cut {
     int chunk, chunks, blocks;
     size_t part, stats;      // bytes
 };
+constexpr int kOne = 1024;
 Cut cut_of(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity, int64_t window, int64_t sinks, bool mma) {
     Cut c{};
     const int64_t most = window ? std::min(capacity, std::min(window, kMostTokens) + tokens - 1 + std::min(sinks, kMostTokens)) : capacity;
     c.blocks = (int)ceil_div(heads / groups * tokens, mma ? kRows : dim > 128 ? 2 : 4);
-    const int64_t units = batch * groups * c.blocks, even = ceil_div(most * units, 6LL * sm_count());
     // (A few keys are one CTA's of 8 warps: the second launch takes longer than 128 keys of a warp.)
     if (mma && most <= kOne) {
         c.chunk = kOne;
         c.chunks = 1;
         return c;
     }
-    c.chunk = (int)std::min<int64_t>(2048, std::max<int64_t>(64, ceil_div(even, 64) * 64));
+    const int64_t units = batch * groups * c.blocks, wave = (int64_t)sm_count() * (mma && dim <= 64 ? 4 : 2), least = 64;
+    double best = 1e300;
+    for (int waves = 1; waves <= 16; ++waves) {
+        const int64_t chunks = std::max<int64_t>(1, std::min(ceil_div(most, least), waves * wave / units));
+        const int64_t chunk = std::max(least, ceil_div(ceil_div(most, chunks), 16) * 16);
+        const int64_t ctas = ceil_div(most, chunk) * units;
+        double cost = (double)ceil_div(ctas, wave) * (chunk + 192);
+        if (batch > 1) cost += 2 * (ctas <= wave ? chunk + 192.0 : 0.67 * ctas / wave * (chunk + 192) + 0.5 * chunk);
+        if (cost < best) {
+            best = cost;
+            c.chunk = (int)chunk;
+        }
+    }
     c.chunks = (int)std::max<int64_t>(1, ceil_div(most, c.chunk));
     if (c.chunks > 1) {
         const size_t rows = (size_t)batch * heads * tokens * c.chunks;
@@ -619,8 +643,11 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
         const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim, c.chunks == 1) : cached_mma_fn<__half>(a.dim, c.chunks == 1)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
         cudaError_t err = launch(fn.fn, dim3((unsigned)grid), mma && c.chunks == 1 ? 256 : kThreads, args, s, fn.shared);
         if (err == cudaSuccess && c.chunks > 1) {
-            const void* join = dtype == VQC_F32 ? (const void*)join_kernel<float> : dtype == VQC_BF16 ? (const void*)join_kernel<__nv_bfloat16> : (const void*)join_kernel<__half>;
-            err = launch(join, dim3((unsigned)rows), 256, args, s);
+            const bool wide = c.chunks > 4;
+            int64_t count = rows;
+            void* join_args[] = {&a, &count};
+            err = launch(dtype == VQC_F32 ? join_fn<float>(wide) : dtype == VQC_BF16 ? join_fn<__nv_bfloat16>(wide) : join_fn<__half>(wide),
+                         dim3((unsigned)(wide ? rows : ceil_div(rows, 8))), 256, join_args, s);
         }
         return err == cudaSuccess ? VQC_OK : cuda_error(err, "cached attention launch");
     } catch (...) {

@@ -1015,16 +1015,26 @@ template <typename T> __global__ void __launch_bounds__(256) rows_tc_kernel(cons
 // Sums of the pieces of cut tiles, in their order: keys and values [tiles * 128 rows] of every group.
 template <typename T> __global__ void __launch_bounds__(256) join_tc_kernel(const __grid_constant__ TcBack A, int width) {
     stream_order();
-    const int64_t rows = min((int64_t)A.cut * N, (int64_t)A.sight.tokens), count = (int64_t)A.planes * 2 * rows * width, step = (int64_t)gridDim.x * 256;
+    const int across = (A.dim + 3) / 4, rows = min(A.cut * N, A.sight.tokens);
+    const int64_t count = (int64_t)A.planes * 2 * rows * across, step = (int64_t)gridDim.x * 256, plane = (int64_t)A.planes * 2 * N * width;
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < count; e += step) {
-        const int c = (int)(e % width);
-        const int64_t row = e / width % rows, side = e / width / rows % 2, which = e / width / rows / 2, tile = row / N;
-        if (c >= A.dim) continue;
-        float s = 0.f;
-        for (int p = 0; p <= A.pieces; ++p)
-            s += A.part[((((tile * (A.pieces + 1) + p) * A.planes + which) * 2 + side) * N + row % N) * width + c];
+        const int64_t i = e / across, j = i / rows;
+        const int c = (int)(e - i * across) * 4, row = (int)(i - j * rows), side = (int)(j & 1), which = (int)(j >> 1), tile = row / N;
+        const float* p = A.part + (int64_t)tile * (A.pieces + 1) * plane + (((int64_t)which * 2 + side) * N + row % N) * width + c;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k <= A.pieces; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(p + k * plane);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
         const int64_t b = which / A.groups;
-        static_cast<T*>(side ? A.gv : A.gk)[((b * A.sight.tokens + row) * A.groups + which % A.groups) * A.dim + c] = from_f<T>(s);
+        T* to = static_cast<T*>(side ? A.gv : A.gk) + ((b * A.sight.tokens + row) * A.groups + which % A.groups) * A.dim + c;
+        if (A.dim % 4 == 0) {
+            *reinterpret_cast<uint2*>(to) = make_uint2(pack2<T>(s.x, s.y), pack2<T>(s.z, s.w));
+        } else {
+            const float v[4] = {s.x, s.y, s.z, s.w};
+            for (int k = 0; k < 4 && c + k < A.dim; ++k) to[k] = from_f<T>(v[k]);
+        }
     }
 }
 
@@ -1141,7 +1151,7 @@ template <typename T, int C> cudaError_t run_back(TcBack& t, const AttentionArgs
         if (e == cudaSuccess && t.cut) {
             int width = 64 * C;
             void* args[] = {&t, &width};
-            const int64_t count = (int64_t)t.planes * 2 * t.cut * N * width;
+            const int64_t count = (int64_t)t.planes * 2 * t.cut * N * (width / 4);
             e = launch((const void*)join_tc_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(count, 256), 8LL * sm_count())), 256, args, s);
         }
     }
