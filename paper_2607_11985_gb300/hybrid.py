@@ -12,7 +12,17 @@ complex64 circuit, and the float32 expectations go back into the residual
 stream in the features' type: the last steps of the products on both sides of
 the circuit.
 
-``python -m paper_2607_11985_gb300.hybrid`` trains one block on a synthetic task.
+``SequenceBlock`` stands before it where samples are tokens of sequences, [batch, tokens, width]:
+
+  q, k, v = W_q norm(h), W_k norm(h), W_v norm(h)      in heads; keys and values in fewer
+  q, k    = norms of each head, turned by their positions
+  h       = h + dropout(W_o attention(q, k, v))         causal, through a window and over the first tokens
+
+and then the two halves above.  In training a sequence goes through whole; ``step`` takes the next
+tokens of sequences whose keys and values lie in a cache.
+
+``python -m paper_2607_11985_gb300.hybrid`` trains one block on a synthetic task (``--tokens``: a
+sequence block).
 """
 from __future__ import annotations
 
@@ -71,6 +81,86 @@ class HybridBlock(torch.nn.Module):
         return layers.linear(a, self.w_down, residual=h)
 
 
+class SequenceBlock(torch.nn.Module):
+    """See the module's text.  ``heads`` of ``dim`` elements, ``groups`` of keys and values; ``window`` (None: every
+    earlier token) and ``sinks`` first tokens that stay visible; ``dropout`` of the attention's branch in
+    training, drawn anew in every forward pass (``draws``: seed and offset)."""
+
+    def __init__(self, width: int, heads: int, groups: int, dim: int, qubits: int, window=None, sinks: int = 0,
+                 dropout: float = 0.0, dtype=torch.float32, seed: int = 0, **rest):
+        super().__init__()
+        self.heads, self.groups, self.dim, self.window, self.sinks, self.dropout = heads, groups, dim, window, sinks, dropout
+        g = torch.Generator().manual_seed(seed + 1)
+
+        def matrix(rows, cols):
+            return torch.nn.Parameter((torch.randn(rows, cols, generator=g) * cols ** -0.5).to(dtype).cuda())
+
+        def ones(size):
+            return torch.nn.Parameter(torch.ones(size, dtype=dtype, device="cuda"))
+
+        self.norm_weight, self.norm_bias = ones(width), torch.nn.Parameter(torch.zeros(width, dtype=dtype, device="cuda"))
+        self.w_q, self.w_k, self.w_v = matrix(heads * dim, width), matrix(groups * dim, width), matrix(groups * dim, width)
+        self.w_o = matrix(width, heads * dim)
+        self.weight_q, self.weight_k = ones(dim), ones(dim)
+        self.register_buffer("frequencies", layers.rotary_frequencies(dim))
+        self.register_buffer("draws", torch.tensor([seed, 0], device="cuda"))
+        self.rest = HybridBlock(width, qubits, dtype=dtype, seed=seed, **rest)
+
+    def _heads(self, h):
+        a = layers.layer_norm(h, self.norm_weight, self.norm_bias)
+        return [layers.linear(a, w).unflatten(-1, (-1, self.dim)) for w in (self.w_q, self.w_k, self.w_v)]
+
+    def forward(self, h, lengths=None):
+        q, k, v = self._heads(h)
+        q, k = layers.norm_rotary(q, k, self.weight_q, self.weight_k, self.frequencies)
+        a = layers.attention(q, k, v, self.window, self.sinks, lengths=lengths).flatten(-2)
+        if self.training and self.dropout:
+            # a state of its own for every pass: its backward draws the same elements again
+            state = self.draws.clone()
+            self.draws[1] += 1
+            h = layers.dropout(layers.linear(a, self.w_o), self.dropout, state, residual=h)
+        else:
+            h = layers.linear(a, self.w_o, residual=h)
+        return self.rest(h)
+
+    def cache(self, batch, capacity):
+        """Keys and values of ``capacity`` tokens of each sequence."""
+        shape = (2, batch, capacity, self.groups, self.dim)
+        return torch.zeros(shape, dtype=self.w_q.dtype, device=self.w_q.device)
+
+    @torch.no_grad()
+    def step(self, h, cache, lengths):
+        """The next tokens h [batch, tokens, width] of sequences; lengths (int32 [batch]) counts them in."""
+        q, k, v = self._heads(h)
+        q = layers.norm_rotary_step(q, k, v, cache[0], cache[1], lengths, self.weight_q, self.weight_k, self.frequencies)
+        a = layers.attention_step(q, cache[0], cache[1], lengths, self.window, self.sinks).flatten(-2)
+        return self.rest(layers.linear(a, self.w_o, residual=h))
+
+
+def train_sequence(width=256, qubits=6, batch=16, tokens=64, steps=40, rate=0.02, dtype=torch.bfloat16, seed=0, window=16,
+                   sinks=2, dropout=0.1, say=print):
+    """Losses of ``steps`` steps on a synthetic task over sequences: a token's first feature is to follow the
+    product of two features of the token before it."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    block = SequenceBlock(width, 4, 2, 64, qubits, window, sinks, dropout, dtype, seed)
+    opt = torch.optim.SGD(block.parameters(), lr=rate, momentum=0.9)
+    x = torch.randn(batch, tokens, width, generator=g, device="cuda")
+    target = torch.tanh(x[:, :-1, 1] * x[:, :-1, 2])
+    x = x.to(dtype)
+    losses = []
+    for step in range(steps):
+        loss = (block(x)[:, 1:, 0].float() - target).square().mean()
+        opt.zero_grad(set_to_none=True)
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+    losses = [float(v) for v in losses]
+    B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
+    for step in sorted(set(range(0, steps, max(1, steps // 8))) | {steps - 1}):
+        say("step %3d  loss %.4f" % (step, losses[step]))
+    return losses
+
+
 def train(width=256, qubits=6, batch=512, steps=40, rate=0.02, dtype=torch.bfloat16, seed=0, say=print):
     """Losses of ``steps`` steps of gradient descent (momentum 0.9) on a synthetic
     regression: the block's first feature is to follow a product of two others."""
@@ -102,8 +192,14 @@ def main():
     ap.add_argument("--batch", type=int, default=512)
     ap.add_argument("--steps", type=int, default=40)
     ap.add_argument("--dtype", choices=("float32", "bfloat16", "float16"), default="bfloat16")
+    ap.add_argument("--tokens", type=int, default=0, help="tokens of a sequence: train a sequence block")
+    ap.add_argument("--window", type=int, default=16)
     a = ap.parse_args()
-    train(a.width, a.qubits, a.batch, a.steps, dtype=getattr(torch, a.dtype))
+    if a.tokens:
+        train_sequence(a.width, a.qubits, max(1, a.batch // a.tokens), a.tokens, a.steps, dtype=getattr(torch, a.dtype),
+                       window=a.window)
+    else:
+        train(a.width, a.qubits, a.batch, a.steps, dtype=getattr(torch, a.dtype))
 
 
 if __name__ == "__main__":
