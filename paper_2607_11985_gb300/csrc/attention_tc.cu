@@ -85,13 +85,18 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 struct Roles {
     const volatile int* gave_up;
     unsigned long long ns;
-    // (The bound is looked at after some tries, each of which waits by itself: reading the clock takes longer than
-    // most waits here.)
+    // False when the bound ran out or another role gave up.  (A bound of milliseconds is looked at after some tries, each of
+    // which waits by itself: reading the clock takes longer than most waits here.)
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
+        const int tries = ns >= 1000000 ? 32 : 0;
 #pragma unroll 1
-        for (int i = 0; i < 32; ++i)
+        for (int i = 0; i < tries; ++i)
             if (__all_sync(~0u, mbar_try(bar, parity))) return true;
-        return mbar_wait(bar, parity, ns, gave_up);
+        const unsigned long long end = now_ns() + ns;
+        for (;;) {
+            if (__all_sync(~0u, mbar_test(bar, parity))) return true;
+            if (__any_sync(~0u, *gave_up || now_ns() > end)) return false;
+        }
     }
 };
 __device__ __forceinline__ void give_up(volatile int* flag, unsigned* err) {
@@ -968,20 +973,23 @@ __device__ __forceinline__ float dot8(const float2 (&a)[4], const float2 (&b)[4]
 template <typename T> __global__ void __launch_bounds__(256) rows_tc_kernel(const __grid_constant__ RowArgs A) {
     stream_order();
     const int c = 8 * (threadIdx.x & 15);
-    const int64_t step = (int64_t)gridDim.x * 16, rows = A.batch * A.heads * A.pitch, values = A.most ? A.batch * A.tokens * A.groups : 0;
+    const int64_t step = (int64_t)gridDim.x * 16, rows = A.batch * A.pitch * A.heads, values = A.most ? A.batch * A.tokens * A.groups : 0;
     float most[2] = {0.f, 0.f};
-    // (a warp's two rows stay together: rows is a multiple of 128)
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < rows; i += step) {
-        // heads inside of tokens, so that neighbouring rows of a sequence lie together
-        const int64_t b = i / (A.pitch * A.heads), j = i - b * A.pitch * A.heads, t = j / A.heads;
-        const int h = (int)(j - t * A.heads);
-        const int64_t at = (b * A.heads + h) * A.pitch + t;
+    // Rows in the order of memory, [batch, pitch, heads]: a row's place moves on by a step without divisions.
+    // (A warp's two rows stay together: a pitch is a multiple of 128.)
+    int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), bt = i / A.heads, b = bt / A.pitch, t = bt - b * A.pitch;
+    int h = (int)(i - bt * A.heads);
+    const int64_t far = step / A.heads;
+    const int more = (int)(step - far * A.heads);
+    for (; i < rows; i += step) {
         const bool in = t < (A.lengths ? min(max((int64_t)A.lengths[b], (int64_t)0), A.tokens) : A.tokens);
-        float s = 0.f, n = 0.f;
+        const int64_t at = (b * A.heads + h) * A.pitch + t;
+        float s = 0.f, n = 0.f, l = 0.f;
         if (in) {
             float2 g[4], o[4];
             load8(static_cast<const T*>(A.g.p) + b * A.g.batch + t * A.g.token + h * A.g.head, c, A.dim, A.packs, g);
             load8(static_cast<const T*>(A.o) + ((b * A.tokens + t) * A.heads + h) * A.dim, c, A.dim, A.packs, o);
+            if (c == 0) l = A.saved[(b * A.heads + h) * A.tokens + t];
             s = dot8(g, o);
             n = dot8(g, g);
         }
@@ -989,7 +997,17 @@ template <typename T> __global__ void __launch_bounds__(256) rows_tc_kernel(cons
         if (A.most) most[0] = fmaxf(most[0], sum16(n));
         if (c == 0) {
             A.d[at] = in ? -s : 0.f;
-            A.lse[at] = in ? A.shift - A.saved[(b * A.heads + h) * A.tokens + t] * 1.44269504088896341f : -INFINITY;
+            A.lse[at] = in ? fmaf(l, -1.44269504088896341f, A.shift) : -INFINITY;
+        }
+        h += more;
+        t += far;
+        if (h >= A.heads) {
+            h -= A.heads;
+            ++t;
+        }
+        while (t >= A.pitch) {
+            t -= A.pitch;
+            ++b;
         }
     }
     if (!A.most) return;
@@ -1262,7 +1280,7 @@ vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes,
         void* args[] = {&r};
         const int64_t rows = a.batch * a.heads * b.pitch;
         e = launch(a.dtype == VQC_BF16 ? (const void*)rows_tc_kernel<__nv_bfloat16> : (const void*)rows_tc_kernel<__half>,
-                   dim3((unsigned)std::min<int64_t>(ceil_div(rows, 16), 16LL * sm_count())), 256, args, s);
+                   dim3((unsigned)std::min<int64_t>(ceil_div(rows, 16), 12LL * sm_count())), 256, args, s);
     }
     if (e != cudaSuccess) return cuda_error(e, "attention launch");
     t.lse = r.lse;

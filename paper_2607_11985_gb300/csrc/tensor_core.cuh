@@ -45,6 +45,16 @@ __device__ __forceinline__ bool mbar_try(uint32_t mbar, uint32_t parity) {
         : "memory");
     return done != 0;
 }
+// the same at once
+__device__ __forceinline__ bool mbar_test(uint32_t mbar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(mbar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 
 // Bounded wait for a phase; false when it ran out or another role gave up.  Lanes may see the end
 // at different times: the warp goes by what all of them saw.

@@ -1,7 +1,11 @@
 """The operators of a sequence on the GPU against their definitions in 64 bits (sequence_reference):
 types, head layouts, lengths from none to several tiles, windows that end inside tiles, strides, empty rows,
 values that are not finite in places that nothing sees, streams and captured calls."""
+import json
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -44,6 +48,13 @@ def heads(seed, batch, tokens, count, dim, dtype, stride=0, scale=1.0):
     """[batch, tokens, count, dim], a slice of rows that are `stride` elements longer"""
     wide = normal(seed, batch, tokens, count * dim + stride, dtype=dtype, scale=scale)
     return wide[..., :count * dim].unflatten(-1, (count, dim))
+
+
+def child(code, **env):
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                       env={**os.environ, **env}, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+    return json.loads(r.stdout.strip().splitlines()[-1])
 
 
 def wide(t):
@@ -404,6 +415,40 @@ def test_results_repeat(layers):
         now = (o, saved, *layers.attention_backward(g, q, k, v, o, saved, 300, 4))
         first = first or now
         assert all(torch.equal(a, b) for a, b in zip(first, now))
+
+
+LIMIT = """
+import json, torch
+from paper_2607_11985_gb300 import binding as B, layers
+def ran_out():
+    try:
+        B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
+        return False
+    except B.VQCError as e:
+        assert B.STATUS[e.status] == "VQC_ERR_DEVICE_CHECK" and "timed out" in str(e), e
+        return True
+seen = []
+for dtype, dim, window in ((torch.bfloat16, 128, None), (torch.float16, 64, 700), (torch.bfloat16, 40, None)):
+    q, k, v = (torch.ones(2, 4096, n, dim, dtype=dtype, device="cuda") for n in (8, 2, 2))
+    o, saved = torch.ones_like(q), torch.zeros(2, 8, 4096, device="cuda")
+    for call in (lambda: layers.attention_forward(q, k, v, window, 3), lambda: layers.attention_backward(q, q, k, v, o, saved, window, 3)):
+        for _ in range(4):
+            call()
+            seen.append(ran_out())
+            # the device and the library go on
+            assert float(q[:, 0].float().sum()) == 2 * 8 * dim
+            w = layers.attention_step(q[:, :1], k, v, torch.full((2,), 9, dtype=torch.int32, device="cuda"))
+            assert bool((w == 1).all()) and not ran_out()
+print(json.dumps(seen))
+"""
+
+
+def test_waits_that_run_out_end_the_kernel_and_are_reported(layers):
+    """With a limit of one microsecond the roles of the tensor-core kernels give up with copies and products in
+    flight: the kernel ends, the status says so, and the device can be used as before."""
+    seen = child(LIMIT, VQC_WAIT_NS="1000")
+    assert len(seen) == 24 and any(seen[:4]) and any(seen[4:8]), seen
+    assert not any(child(LIMIT, VQC_WAIT_NS="4000000000"))
 
 
 # -------------------------------------------------------------- refusals
