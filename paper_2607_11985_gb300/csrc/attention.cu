@@ -36,7 +36,7 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 template <int DM> struct Tile {
     static constexpr int R = DM > 128 ? 2 : 4, N = 16 * R;
     static constexpr int kPitch = DM + 4, kScores = N + 4;      // floats between rows: rows 16 apart fall on other banks
-    static constexpr int kSmemForward = (3 * N * kPitch + N * kScores) * 4;
+    static constexpr int kSmemForward = (2 * N * kPitch + N * kScores) * 4;      // keys and values in turn: two CTAs per SM
     static constexpr int kSmemQueries = (4 * N * kPitch + N * kScores + 2 * N) * 4;
     static constexpr int kSmemKeys = (4 * N * kPitch + 2 * N * kScores + 2 * N) * 4;
 };
@@ -52,10 +52,29 @@ __device__ __forceinline__ bool sees(const Sight& S, int64_t i, int64_t j, int64
 template <typename T, int DM, int N>
 __device__ __forceinline__ void load_tile(float* to, const Heads& x, int64_t b, int64_t head, int64_t first, int64_t rows, int dim) {
     const T* p = static_cast<const T*>(x.p) + b * x.batch + head * x.head;
+    if constexpr (sizeof(T) == 4) {
+        // floats on 16-byte boundaries: four at a time, straight to their places; all of a thread's are on the way together
+        if (dim % 4 == 0 && ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(x.token * 4)) & 15) == 0) {
+#pragma unroll
+            for (int e = threadIdx.x; e < N * (DM / 4); e += kThreads) {
+                const int r = e / (DM / 4), c = e % (DM / 4) * 4;
+                const bool in = first + r < rows && c < dim;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to + r * (DM + 4) + c)),
+                             "l"(in ? reinterpret_cast<const float*>(p) + (first + r) * x.token + c : reinterpret_cast<const float*>(p)), "r"(in ? 16 : 0)
+                             : "memory");
+            }
+            return;
+        }
+    }
     for (int e = threadIdx.x; e < N * DM; e += kThreads) {
         const int r = e / DM, c = e % DM;
         to[r * (DM + 4) + c] = first + r < rows && c < dim ? to_f(p[(first + r) * x.token + c]) : 0.f;
     }
+}
+// The tiles that have been asked for are there, for all threads.
+__device__ __forceinline__ void tiles_there() {
+    asm volatile("cp.async.wait_all;\n" ::: "memory");
+    __syncthreads();
 }
 // s[i][j] = rows ty R + i of a times rows tx + 16 j of b
 template <int DM, int R> __device__ __forceinline__ void scores(const float* a, const float* b, int ty, int tx, float (&s)[R][R]) {
@@ -162,12 +181,12 @@ __device__ __forceinline__ At tile_of(int64_t tiles, int64_t heads, bool last_fi
     return r;
 }
 
-template <typename T, int DM> __global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ AttentionArgs A, int64_t tiles) {
+template <typename T, int DM> __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_constant__ AttentionArgs A, int64_t tiles) {
     stream_order();
     using L = Tile<DM>;
     constexpr int R = L::R, N = L::N;
     extern __shared__ __align__(16) float sm[];
-    float *q = sm, *k = q + N * L::kPitch, *v = k + N * L::kPitch, *p = v + N * L::kPitch;
+    float *q = sm, *kv = q + N * L::kPitch, *p = kv + N * L::kPitch;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const At W = tile_of(tiles, A.heads, true);
     const int64_t length = length_of(A.sight, W.b), q0 = W.tile * N, q1 = min(q0 + N, length), group = W.head / (A.heads / A.groups);
@@ -184,11 +203,12 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) forwar
         const Span span = keys_of(A.sight, q0, q1, N);
         for (int64_t t = span.sinks ? 0 : span.from; t < span.to; t = t + 1 == span.sinks ? span.from : t + 1) {
             __syncthreads();
-            load_tile<T, DM, N>(k, A.k, W.b, group, t * N, length, A.dim);
-            load_tile<T, DM, N>(v, A.v, W.b, group, t * N, length, A.dim);
-            __syncthreads();
+            load_tile<T, DM, N>(kv, A.k, W.b, group, t * N, length, A.dim);
+            tiles_there();
             float s[R][R];
-            scores<DM, R>(q, k, ty, tx, s);
+            scores<DM, R>(q, kv, ty, tx, s);
+            __syncthreads();
+            load_tile<T, DM, N>(kv, A.v, W.b, group, t * N, length, A.dim);      // while the scores are worked on
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 float most = top[i];
@@ -212,8 +232,8 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) forwar
 #pragma unroll
                 for (int c = 0; c < kOut<DM>; ++c) o[i][c] *= shrink;
             }
-            __syncwarp();      // a row's scores are of one half of a warp
-            add_product<DM, R>(p, v, ty, tx, o);
+            tiles_there();
+            add_product<DM, R>(p, kv, ty, tx, o);
         }
     }
     const int64_t rows = min((int64_t)N, A.sight.tokens - q0);
@@ -281,7 +301,7 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) querie
             __syncthreads();
             load_tile<T, DM, N>(k, A.k, W.b, group, t * N, length, A.dim);
             load_tile<T, DM, N>(v, A.v, W.b, group, t * N, length, A.dim);
-            __syncthreads();
+            tiles_there();
             float s[R][R], dp[R][R];
             scores<DM, R>(q, k, ty, tx, s);
             scores<DM, R>(g, v, ty, tx, dp);
@@ -301,7 +321,8 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) querie
                          min((int64_t)N, A.sight.tokens - q0), A.dim, ty, tx);
 }
 
-// Gradients of a tile of keys and values: over the heads that share them and the queries that see them.
+// Gradients of a tile of keys and values: over the heads that share them and the queries that see them.  Where that leaves
+// SMs idle (A.part) a CTA takes one of the heads, and sums of the heads are joined in their order.
 template <typename T, int DM> __global__ void __launch_bounds__(kThreads) keys_kernel(const __grid_constant__ AttentionArgs A, int64_t tiles) {
     stream_order();
     using L = Tile<DM>;
@@ -310,8 +331,9 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) keys_k
     float *k = sm, *v = k + N * L::kPitch, *q = v + N * L::kPitch, *g = q + N * L::kPitch, *p = g + N * L::kPitch, *ds = p + N * L::kScores,
           *lse = ds + N * L::kScores, *d = lse + N;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const At W = tile_of(tiles, A.groups, false);
+    const At W = tile_of(tiles, A.part ? A.heads : A.groups, false);
     const int64_t length = length_of(A.sight, W.b), k0 = W.tile * N, k1 = min(k0 + N, length), per = A.heads / A.groups;
+    const int64_t group = A.part ? W.head / per : W.head, h0 = A.part ? W.head : W.head * per, h1 = A.part ? h0 + 1 : h0 + per;
     float gk[R][kOut<DM>], gv[R][kOut<DM>], factor[R], one[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -321,16 +343,16 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) keys_k
         for (int c = 0; c < kOut<DM>; ++c) gk[i][c] = gv[i][c] = 0.f;
     }
     if (k0 < length) {
-        load_tile<T, DM, N>(k, A.k, W.b, W.head, k0, length, A.dim);
-        load_tile<T, DM, N>(v, A.v, W.b, W.head, k0, length, A.dim);
+        load_tile<T, DM, N>(k, A.k, W.b, group, k0, length, A.dim);
+        load_tile<T, DM, N>(v, A.v, W.b, group, k0, length, A.dim);
         const int64_t end = (queries_end(A.sight, k0, k1, length) + N - 1) / N;
-        for (int64_t h = W.head * per; h < (W.head + 1) * per; ++h)
+        for (int64_t h = h0; h < h1; ++h)
             for (int64_t t = k0 / N; t < end; ++t) {
                 __syncthreads();
                 load_tile<T, DM, N>(q, A.q, W.b, h, t * N, length, A.dim);
                 load_tile<T, DM, N>(g, A.g, W.b, h, t * N, length, A.dim);
                 load_stats(lse, d, A, W, h, t * N, length, N);
-                __syncthreads();
+                tiles_there();
                 float s[R][R], dp[R][R];
                 scores<DM, R>(k, q, ty, tx, s);
                 scores<DM, R>(v, g, ty, tx, dp);
@@ -349,9 +371,31 @@ template <typename T, int DM> __global__ void __launch_bounds__(kThreads) keys_k
                 add_product<DM, R>(ds, q, ty, tx, gk);
             }
     }
-    const int64_t rows = min((int64_t)N, A.sight.tokens - k0), at = ((W.b * A.sight.tokens + k0) * A.groups + W.head) * A.dim, pitch = (int64_t)A.groups * A.dim;
+    const int64_t rows = min((int64_t)N, A.sight.tokens - k0);
+    if (A.part) {      // [2][batch, tokens, heads, dim]
+        const int64_t at = ((W.b * A.sight.tokens + k0) * A.heads + W.head) * A.dim, pitch = (int64_t)A.heads * A.dim;
+        store_rows<float, DM, R>(A.part, gk, factor, at, pitch, rows, A.dim, ty, tx);
+        store_rows<float, DM, R>(A.part + A.batch * A.sight.tokens * pitch, gv, one, at, pitch, rows, A.dim, ty, tx);
+        return;
+    }
+    const int64_t at = ((W.b * A.sight.tokens + k0) * A.groups + W.head) * A.dim, pitch = (int64_t)A.groups * A.dim;
     store_rows<T, DM, R>(A.gk, gk, factor, at, pitch, rows, A.dim, ty, tx);
     store_rows<T, DM, R>(A.gv, gv, one, at, pitch, rows, A.dim, ty, tx);
+}
+
+// The heads' sums of each group: [2][rows, heads, dim] to gk and gv [rows, groups, dim].
+template <typename T> __global__ void __launch_bounds__(kThreads) join_heads_kernel(const __grid_constant__ AttentionArgs A, int64_t rows) {
+    stream_order();
+    const int per = A.heads / A.groups;
+    const int64_t width = (int64_t)A.groups * A.dim, count = rows * width, step = (int64_t)gridDim.x * kThreads;
+    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < 2 * count; e += step) {
+        const int64_t side = e >= count, i = e - side * count, row = i / width;
+        const int c = (int)(i - row * width), group = c / A.dim;
+        const float* p = A.part + side * rows * A.heads * A.dim + (row * A.heads + (int64_t)group * per) * A.dim + (c - group * A.dim);
+        float s = 0.f;
+        for (int h = 0; h < per; ++h) s += p[(int64_t)h * A.dim];
+        static_cast<T*>(side ? A.gv : A.gk)[i] = from_f<T>(s);
+    }
 }
 
 template <typename T, int DM> struct Kernels {
@@ -371,7 +415,11 @@ template <typename T, int DM> struct Kernels {
         AttentionArgs a = a0;
         int64_t tiles = ceil_div(a.sight.tokens, Tile<DM>::N);
         void* args[] = {&a, &tiles};
-        return launch((const void*)keys_kernel<T, DM>, dim3((unsigned)(tiles * a.batch * a.groups)), kThreads, args, s, Tile<DM>::kSmemKeys);
+        const cudaError_t e = launch((const void*)keys_kernel<T, DM>, dim3((unsigned)(tiles * a.batch * (a.part ? a.heads : a.groups))), kThreads, args, s, Tile<DM>::kSmemKeys);
+        if (e != cudaSuccess || !a.part) return e;
+        int64_t rows = a.batch * a.sight.tokens;
+        void* join_args[] = {&a, &rows};
+        return launch((const void*)join_heads_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(2 * rows * a.groups * a.dim, kThreads), 16LL * sm_count())), kThreads, join_args, s);
     }
     static cudaError_t run(const AttentionArgs& a, int which, cudaStream_t s) { return which == 0 ? forward(a, s) : which == 1 ? queries(a, s) : keys(a, s); }
 };
@@ -414,6 +462,11 @@ AttentionArgs arguments(int dtype, int64_t batch, int64_t tokens, int64_t heads,
     a.scale2 = (float)scale * kLog2e;
     return a;
 }
+// Space of the heads' sums where the keys' tiles leave SMs idle.
+size_t part_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim) {
+    if (heads == groups || ceil_div(tokens, dim > 128 ? 32 : 64) * batch * groups >= 2LL * sm_count()) return 0;
+    return align256((size_t)(2 * batch * tokens) * heads * dim * 4);
+}
 size_t saved_bytes(int64_t batch, int64_t tokens, int64_t heads) { return align256((size_t)(batch * tokens) * heads * 4); }
 
 }  // namespace
@@ -432,7 +485,7 @@ size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch
     const Sight s = arguments(dtype, batch, tokens, heads, groups, dim, window, sinks, 1.0, nullptr).sight;
     if (attention_tc_takes(dtype, dim))
         return batch * tokens ? attention_tc_workspace(mode, dtype, batch, tokens, heads, groups, dim, s.window, s.sinks, aligned != 0) : 0;
-    return mode ? saved_bytes(batch, tokens, heads) : 0;
+    return mode ? saved_bytes(batch, tokens, heads) + part_bytes(batch, tokens, heads, groups, dim) : 0;
 }
 
 vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, const vqc_heads* q,
@@ -482,13 +535,14 @@ vqc_status vqc_attention_backward(vqc_real dtype, int64_t batch, int64_t tokens,
         if (!grid_ok(batch, tokens, heads, dim)) return set_error(VQC_ERR_INVALID_ARG, std::string(call) + ": sizes out of range");
         if (batch * tokens == 0 || (!grad_q && !grad_k)) return VQC_OK;
         const bool tc = attention_tc_takes(dtype, dim);
-        if (!workspace || (!tc && workspace_bytes < saved_bytes(batch, tokens, heads)))
+        if (!workspace || (!tc && workspace_bytes < saved_bytes(batch, tokens, heads) + part_bytes(batch, tokens, heads, groups, dim)))
             return set_error(VQC_ERR_WORKSPACE, std::string(call) + ": workspace too small");
         AttentionArgs a = arguments(dtype, batch, tokens, heads, groups, dim, window, sinks, scale, lengths);
         a.q = heads_of(*q); a.k = heads_of(*k); a.v = heads_of(*v); a.g = heads_of(*grad_o);
         a.o = const_cast<void*>(o);
         a.lse = saved;
         a.d = static_cast<float*>(workspace);
+        if (part_bytes(batch, tokens, heads, groups, dim)) a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + saved_bytes(batch, tokens, heads));
         a.gq = grad_q; a.gk = grad_k; a.gv = grad_v;
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         if (tc) {

@@ -20,6 +20,7 @@ struct AttentionArgs {
     const float* lse;            // backward
     float* d;                    // g . o of the rows, [batch, heads, tokens]
     void *gq, *gk, *gv;          // dense
+    float* part;                 // FP32 kernels: keys' sums of each head, or NULL
     int64_t batch;
     float scale, scale2;         // scale2: times log2(e)
     int heads, groups, dim, dtype;
