@@ -26,20 +26,21 @@ struct DropArgs {
     uint64_t seed, offset;
     uint32_t limit;              // words below it drop their element
     float scale;
+    uint32_t key[20];            // of the rounds, from `seed`
 };
 
-__device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t seed) {
+// kState: the rounds' keys from a seed in memory; else as they come with the arguments, where they cost no instruction
+// (with two additions a round the kernel took 42 us in the place of 37).
+template <bool kState> __device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t seed, const uint32_t* key) {
     uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
-    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);       // (the rounds' keys are the same in all threads)
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        const uint32_t k0 = kState ? (uint32_t)seed + r * 0x9E3779B9u : key[2 * r], k1 = kState ? (uint32_t)(seed >> 32) + r * 0xBB67AE85u : key[2 * r + 1];
         c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
         c1 = (uint32_t)b;
         c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
         c3 = (uint32_t)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
     }
     return make_uint4(c0, c1, c2, c3);
 }
@@ -53,8 +54,8 @@ __device__ __forceinline__ float dropped(float x, float res, uint32_t w, const D
 }
 
 // V elements (16 bytes) of a row at a time; a row holds whole packs, but for the last one of a single row.
-// kState: seed and offset from memory (as arguments they stay out of the vector registers, with all the rounds' keys).
-template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(256, 6) drop_kernel(const __grid_constant__ DropArgs A) {
+// kFlat: one row.
+template <typename T, bool kRes, bool kState, bool kFlat> __global__ void __launch_bounds__(256, 6) drop_kernel(const __grid_constant__ DropArgs A) {
     constexpr int V = 16 / sizeof(T);
     stream_order();
     const uint64_t seed = kState ? A.state[0] : A.seed, offset = A.offset + (kState ? A.state[1] : 0);
@@ -63,7 +64,8 @@ template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(
     T* y = static_cast<T*>(A.y);
     const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     auto at = [&](int64_t i, int64_t ld) {
-        const int64_t r = A.rows == 1 ? 0 : packs >> 32 ? i / across : (int64_t)((uint32_t)i / (uint32_t)across);
+        if (kFlat) return i * V;
+        const int64_t r = packs >> 32 ? i / across : (int64_t)((uint32_t)i / (uint32_t)across);
         return r * ld + (i - r * across) * V;
     };
     for (int64_t i = first; i < packs; i += step) {
@@ -73,7 +75,7 @@ template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(
         uint32_t out[4];
 #pragma unroll
         for (int b = 0; b < V / 4; ++b) {
-            const uint4 w = philox((uint64_t)i * (V / 4) + b, offset, seed);
+            const uint4 w = philox<kState>((uint64_t)i * (V / 4) + b, offset, seed, A.key);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if constexpr (sizeof(T) == 4) {
@@ -87,9 +89,9 @@ template <typename T, bool kRes, bool kState> __global__ void __launch_bounds__(
         }
         *reinterpret_cast<uint4*>(y + i * V) = make_uint4(out[0], out[1], out[2], out[3]);
     }
-    if (A.rows == 1 && first < A.cols - across * V) {
+    if (kFlat && first < A.cols - across * V) {
         const int64_t e = across * V + first;
-        y[e] = from_f<T>(dropped(to_f(x[e]), kRes ? to_f(res[e]) : 0.f, word(philox((uint64_t)e / 4, offset, seed), (int)(e & 3)), A));
+        y[e] = from_f<T>(dropped(to_f(x[e]), kRes ? to_f(res[e]) : 0.f, word(philox<kState>((uint64_t)e / 4, offset, seed, A.key), (int)(e & 3)), A));
     }
 }
 
@@ -100,7 +102,7 @@ template <typename T> __global__ void __launch_bounds__(256) drop_any_kernel(con
     const int64_t n = A.rows * A.cols, step = (int64_t)gridDim.x * blockDim.x;
     const T *x = static_cast<const T*>(A.x), *res = static_cast<const T*>(A.res);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; 4 * i < n; i += step) {
-        const uint4 w = philox((uint64_t)i, offset, seed);
+        const uint4 w = philox<true>((uint64_t)i, offset, seed, nullptr);
         int64_t r = n >> 32 ? 4 * i / A.cols : (int64_t)((uint32_t)(4 * i) / (uint32_t)A.cols), c = 4 * i - r * A.cols;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -115,10 +117,13 @@ template <typename T> __global__ void __launch_bounds__(256) drop_any_kernel(con
     }
 }
 
-template <typename T> const void* drop_fn(bool packs, bool res, bool state) {
+template <typename T, bool kRes, bool kState> const void* drop_fn(bool flat) {
+    return flat ? (const void*)drop_kernel<T, kRes, kState, true> : (const void*)drop_kernel<T, kRes, kState, false>;
+}
+template <typename T> const void* drop_fn(bool packs, bool res, bool state, bool flat) {
     if (!packs) return (const void*)drop_any_kernel<T>;
-    if (state) return res ? (const void*)drop_kernel<T, true, true> : (const void*)drop_kernel<T, false, true>;
-    return res ? (const void*)drop_kernel<T, true, false> : (const void*)drop_kernel<T, false, false>;
+    if (state) return res ? drop_fn<T, true, true>(flat) : drop_fn<T, false, true>(flat);
+    return res ? drop_fn<T, true, false>(flat) : drop_fn<T, false, false>(flat);
 }
 
 vqc_status dropout(const char* call, int dtype, int64_t rows, int64_t cols, const void* x, int64_t ld_x, const void* res, int64_t ld_res,
@@ -135,11 +140,15 @@ vqc_status dropout(const char* call, int dtype, int64_t rows, int64_t cols, cons
         ld_x = ld_res = cols;
         rows = 1;
     }
-    DropArgs a{x, res, y, rows, cols, ld_x, ld_res, state, seed, offset, 0, (float)(1.0 / (1.0 - p))};
+    DropArgs a{x, res, y, rows, cols, ld_x, ld_res, state, seed, offset, 0, (float)(1.0 / (1.0 - p)), {}};
+    for (int r = 0; r < 10; ++r) {
+        a.key[2 * r] = (uint32_t)seed + (uint32_t)r * 0x9E3779B9u;
+        a.key[2 * r + 1] = (uint32_t)(seed >> 32) + (uint32_t)r * 0xBB67AE85u;
+    }
     a.limit = (uint32_t)std::fmin(std::nearbyint(p * 4294967296.0), 4294967295.0);
     const int64_t v = 16 / (int64_t)e;
     const bool packs = aligned_to(x, 16) && aligned_to(res, 16) && (rows == 1 || (cols % v == 0 && ld_x % v == 0 && (!res || ld_res % v == 0)));
-    const void* fn = dtype == VQC_F32 ? drop_fn<float>(packs, res, state) : dtype == VQC_BF16 ? drop_fn<__nv_bfloat16>(packs, res, state) : drop_fn<__half>(packs, res, state);
+    const void* fn = dtype == VQC_F32 ? drop_fn<float>(packs, res, state, rows == 1) : dtype == VQC_BF16 ? drop_fn<__nv_bfloat16>(packs, res, state, rows == 1) : drop_fn<__half>(packs, res, state, rows == 1);
     const int64_t threads = ceil_div(rows * cols, packs ? v : 4);
     void* args[] = {&a};
     const cudaError_t err = launch(fn, dim3((unsigned)std::min<int64_t>(std::max<int64_t>(1, ceil_div(threads, 256)), 30LL * sm_count())), 256, args,
