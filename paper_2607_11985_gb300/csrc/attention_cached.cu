@@ -220,12 +220,12 @@ template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(k
 // copies, and what is on the way takes no registers (in registers 5.2 TB/s).
 constexpr int kRows = 16;
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -241,11 +241,12 @@ template <int DM, int W> struct MmaShape {
     static constexpr int kSmem = (kRing > kSums ? kRing : kSums) + W * kRows * 8;
 };
 
-template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W == 8 ? 1 : DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
+// kFew: 8 rows at most; the work for rows 8 to 15 is left out (and their operands are zeros).
+template <typename T, int DM, int W, bool kFew> __global__ void __launch_bounds__(32 * W, W == 8 ? 1 : DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
     using L = MmaShape<DM, W>;
     constexpr int NK = L::NK, NV = L::NV, kDeep = L::kDeep;      // pieces of 16 bytes of a lane: of a key, of a value
     constexpr float kShift = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value ? 6.f : 0.f;
-    constexpr int P = DM + 4;
+    constexpr int P = DM + 4, RN = kFew ? 1 : 2;      // rows of a lane
     extern __shared__ __align__(16) unsigned char shared[];
     float(*joined)[kRows][P] = reinterpret_cast<float(*)[kRows][P]>(shared);      // in the place of the ring, after it
     float(*stats)[kRows][2] = reinterpret_cast<float(*)[kRows][2]>(shared + L::kSmem - W * kRows * 8);
@@ -265,8 +266,12 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
     // this lane's rows: g and g + 8; their queries, and positions less the first key's
     uint32_t q[2 * NK][4];
     int at[2];
+    if (kFew) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+        for (int i = 0; i < 2 * NK; ++i) q[i][1] = q[i][3] = 0u;
+    }
+#pragma unroll
+    for (int r = 0; r < RN; ++r) {
         const int row = block * kRows + g + 8 * r, h = group * per + row / tokens, tok = row % tokens;
         const bool in = g + 8 * r < rows;
         at[r] = (int)(K.length - tokens) + tok;
@@ -343,26 +348,36 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
     for (int i = 16 * warp; i < count; i += kStep) {
         copies_wait<kDeep - 2>();
         const unsigned char* from = ring + stage * L::kStage;
+        // all of a stage's pieces at once: one by one, each before its products, their latencies took half of the time
+        uint4 kw[2][NK], vw[4][NV];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int c = 0; c < NK; ++c) kw[n][c] = *reinterpret_cast<const uint4*>(from + (n * NK + c) * 512);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int c = 0; c < NV; ++c) vw[n][c] = *reinterpret_cast<const uint4*>(from + (2 * NK + n * NV + c) * 512);
         ask(i + (kDeep - 1) * kStep, stage ? stage - 1 : kDeep - 1);
         stage = stage + 1 == kDeep ? 0 : stage + 1;
         float s[2][4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
 #pragma unroll
-            for (int c = 0; c < NK; ++c) {
-                const uint4 k = *reinterpret_cast<const uint4*>(from + (n * NK + c) * 512);
-                mma_16816(s[n], q[2 * c], k.x, k.y, T());
-                mma_16816(s[n], q[2 * c + 1], k.z, k.w, T());
+        for (int c = 0; c < NK; ++c)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {      // (the two sums go on side by side)
+                mma_16816(s[n], q[2 * c], kw[n][c].x, kw[n][c].y, T());
+                mma_16816(s[n], q[2 * c + 1], kw[n][c].z, kw[n][c].w, T());
             }
-        }
         // element e of s[n]: row g + 8 (e / 2), key i + 8 n + 2 t + e % 2
         if (tokens > 1 || i + 16 > count)
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 2 * RN; ++e) {
                 const int at_i = i + 8 * n + 2 * t + (e & 1);
                 bool seen = at_i < count;
                 if (tokens > 1) {      // (one token sees every key that is counted)
@@ -373,15 +388,15 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
             }
         float top[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < RN; ++r) {
             top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * A.scale2;
             top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
             top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
         }
         // the followed maximum moves when it has grown by more than 2^8
-        if (__any_sync(~0u, top[0] > followed[0] + 8.f || top[1] > followed[1] + 8.f)) {
+        if (__any_sync(~0u, top[0] > followed[0] + 8.f || (!kFew && top[1] > followed[1] + 8.f))) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < RN; ++r) {
                 const float now = fmaxf(followed[r], top[r]), shrink = power(followed[r] - (now == -INFINITY ? 0.f : now));
                 followed[r] = now;
                 total[r] *= shrink;
@@ -395,19 +410,19 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 2 * RN; ++e) {
                 const float f = followed[e >> 1];
                 s[n][e] = power(fmaf(s[n][e], A.scale2, f == -INFINITY ? 0.f : kShift - f));
                 total[e >> 1] += s[n][e];
             }
-        const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]), pack2<T>(s[1][2], s[1][3])};
+        const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), kFew ? 0u : pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]),
+                               kFew ? 0u : pack2<T>(s[1][2], s[1][3])};
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             uint32_t v[4][4];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const uint4 x = *reinterpret_cast<const uint4*>(from + (2 * NK + n * NV + c) * 512);
-                v[n][0] = x.x; v[n][1] = x.y; v[n][2] = x.z; v[n][3] = x.w;
+                v[n][0] = vw[n][c].x; v[n][1] = vw[n][c].y; v[n][2] = vw[n][c].z; v[n][3] = vw[n][c].w;
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -420,7 +435,7 @@ template <typename T, int DM, int W> __global__ void __launch_bounds__(32 * W, W
     __syncthreads();
     // a warp's sums to shared memory: row g + 8 r, element 64 c + 8 n + j of o[8 c + j][2 r + n % 2], n = 2 t, 2 t + 1
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < RN; ++r) {
         total[r] += __shfl_xor_sync(~0u, total[r], 1);
         total[r] += __shfl_xor_sync(~0u, total[r], 2);
 #pragma unroll
@@ -534,11 +549,14 @@ template <typename T, int DM, int RB> Chosen cached_fn(bool packs) {
 template <typename T> Chosen cached_fn(int dim, bool packs) {
     return dim <= 32 ? cached_fn<T, 32, 4>(packs) : dim <= 64 ? cached_fn<T, 64, 4>(packs) : dim <= 128 ? cached_fn<T, 128, 4>(packs) : cached_fn<T, 256, 2>(packs);
 }
-template <typename T, int W> Chosen cached_mma_fn(int dim) {
-    if (dim <= 64) return {(const void*)cached_mma_kernel<T, 64, W>, MmaShape<64, W>::kSmem};
-    return {(const void*)cached_mma_kernel<T, 128, W>, MmaShape<128, W>::kSmem};
+template <typename T, int W, bool kFew> Chosen cached_mma_fn(int dim) {
+    if (dim <= 64) return {(const void*)cached_mma_kernel<T, 64, W, kFew>, MmaShape<64, W>::kSmem};
+    return {(const void*)cached_mma_kernel<T, 128, W, kFew>, MmaShape<128, W>::kSmem};
 }
-template <typename T> Chosen cached_mma_fn(int dim, bool one) { return one ? cached_mma_fn<T, 8>(dim) : cached_mma_fn<T, kWarps>(dim); }
+template <typename T> Chosen cached_mma_fn(int dim, bool one, bool few) {
+    if (few) return one ? cached_mma_fn<T, 8, true>(dim) : cached_mma_fn<T, kWarps, true>(dim);
+    return one ? cached_mma_fn<T, 8, false>(dim) : cached_mma_fn<T, kWarps, false>(dim);
+}
 
 // How the keys are cut.  `most`: keys that can be in sight at once.  The chunks of one, two, .. waves of CTAs that the SMs
 // hold together are compared by their longest SM: its keys, and for each CTA the time of about 192 keys to begin and to
@@ -640,7 +658,8 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
         }
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         void* args[] = {&a};
-        const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim, c.chunks == 1) : cached_mma_fn<__half>(a.dim, c.chunks == 1)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
+        const bool few = heads / groups * tokens <= 8;
+        const Chosen fn = mma ? (dtype == VQC_BF16 ? cached_mma_fn<__nv_bfloat16>(a.dim, c.chunks == 1, few) : cached_mma_fn<__half>(a.dim, c.chunks == 1, few)) : dtype == VQC_F32 ? cached_fn<float>(a.dim, packs) : dtype == VQC_BF16 ? cached_fn<__nv_bfloat16>(a.dim, packs) : cached_fn<__half>(a.dim, packs);
         cudaError_t err = launch(fn.fn, dim3((unsigned)grid), mma && c.chunks == 1 ? 256 : kThreads, args, s, fn.shared);
         if (err == cudaSuccess && c.chunks > 1) {
             const bool wide = c.chunks > 4;
