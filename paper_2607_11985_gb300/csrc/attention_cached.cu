@@ -173,6 +173,7 @@ template <typename T, int DM, int V, int RB> __global__ void __launch_bounds__(k
         __syncwarp();
     }
     constexpr int P = DM + 2;
+    let_next();      // the join may be placed
     if (V > 1) copies_wait<0>();
     __syncthreads();
 #pragma unroll
@@ -229,6 +230,12 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// an 8 x 8 matrix of 16-bit elements (two neighbours of row g in lane 4 g + t), its rows for its columns
+__device__ __forceinline__ uint32_t turned8(uint32_t w) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
+    return r;
+}
 __device__ __forceinline__ float power(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -241,12 +248,15 @@ template <int DM, int W> struct MmaShape {
     static constexpr int kSmem = (kRing > kSums ? kRing : kSums) + W * kRows * 8;
 };
 
-// kFew: 8 rows at most; the work for rows 8 to 15 is left out (and their operands are zeros).
+// kFew: 8 rows at most.  The products are the transposed ones, S^T = K Q^T and O^T = V^T P^T, with 16 keys (16 elements of a
+// value) in the place of the 16 rows: half as many, and half the registers of the output; P^T is turned by movmatrix.  A
+// lane then has rows 2 t and 2 t + 1 of keys g and g + 8, and a row's maximum is looked for over the lanes only where
+// some key is above the followed one by 2^8.
 template <typename T, int DM, int W, bool kFew> __global__ void __launch_bounds__(32 * W, W == 8 ? 1 : DM == 64 ? 4 : 2) cached_mma_kernel(const __grid_constant__ CachedArgs A) {
     using L = MmaShape<DM, W>;
     constexpr int NK = L::NK, NV = L::NV, kDeep = L::kDeep;      // pieces of 16 bytes of a lane: of a key, of a value
     constexpr float kShift = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value ? 6.f : 0.f;
-    constexpr int P = DM + 4, RN = kFew ? 1 : 2;      // rows of a lane
+    constexpr int P = DM + 4;
     extern __shared__ __align__(16) unsigned char shared[];
     float(*joined)[kRows][P] = reinterpret_cast<float(*)[kRows][P]>(shared);      // in the place of the ring, after it
     float(*stats)[kRows][2] = reinterpret_cast<float(*)[kRows][2]>(shared + L::kSmem - W * kRows * 8);
@@ -263,34 +273,6 @@ template <typename T, int DM, int W, bool kFew> __global__ void __launch_bounds_
     if (i0 >= K.count && chunk > 0) return;
     const int count = (int)max((int64_t)0, min((int64_t)A.chunk, K.count - i0));
     const int per = A.heads / A.groups, tokens = (int)A.tokens, rows = min(kRows, per * tokens - block * kRows);
-    // this lane's rows: g and g + 8; their queries, and positions less the first key's
-    uint32_t q[2 * NK][4];
-    int at[2];
-    if (kFew) {
-#pragma unroll
-        for (int i = 0; i < 2 * NK; ++i) q[i][1] = q[i][3] = 0u;
-    }
-#pragma unroll
-    for (int r = 0; r < RN; ++r) {
-        const int row = block * kRows + g + 8 * r, h = group * per + row / tokens, tok = row % tokens;
-        const bool in = g + 8 * r < rows;
-        at[r] = (int)(K.length - tokens) + tok;
-        const T* p = static_cast<const T*>(A.q.p) + b * A.q.batch + tok * A.q.token + h * A.q.head;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            const int c = 32 * i + 8 * t;
-            uint32_t x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {      // (queries may have any alignment)
-                const uint32_t lo = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e] : 0u, hi = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e + 1] : 0u;
-                x[e] = lo | hi << 16;
-            }
-            q[2 * i][r] = x[0];
-            q[2 * i][2 + r] = x[1];
-            q[2 * i + 1][r] = x[2];
-            q[2 * i + 1][2 + r] = x[3];
-        }
-    }
     const T *kp = static_cast<const T*>(A.k.p) + b * A.k.batch + group * A.k.head, *vp = static_cast<const T*>(A.v.p) + b * A.v.batch + group * A.v.head;
     unsigned char* ring = shared + warp * kDeep * L::kStage + lane * 16;
     // keys and values of index i0 + i behind the first ones
@@ -335,15 +317,41 @@ template <typename T, int DM, int W, bool kFew> __global__ void __launch_bounds_
         copies_end();
     };
     constexpr int kStep = 16 * W;
-    float o[8 * NV][4], followed[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 8 * NV; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
     if (count) {
 #pragma unroll
         for (int d = 0; d < kDeep - 1; ++d) ask(16 * warp + d * kStep, d);
     }
+    // queries of rows g (and g + 8), while the first keys come; positions of the rows of this lane's scores
+    uint32_t q[2 * NK][4];
+    int at[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        at[r] = (int)(K.length - tokens) + (block * kRows + (kFew ? 2 * t + r : g + 8 * r)) % tokens;
+        if (kFew && r) break;
+        const int row = block * kRows + g + 8 * r, h = group * per + row / tokens, tok = row % tokens;
+        const bool in = g + 8 * r < rows;
+        const T* p = static_cast<const T*>(A.q.p) + b * A.q.batch + tok * A.q.token + h * A.q.head;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int c = 32 * i + 8 * t;
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {      // (queries may have any alignment)
+                const uint32_t lo = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e] : 0u, hi = in && c < A.dim ? reinterpret_cast<const uint16_t*>(p)[c + 2 * e + 1] : 0u;
+                x[e] = lo | hi << 16;
+            }
+            q[2 * i][r] = x[0];
+            q[2 * i][2 + r] = x[1];
+            q[2 * i + 1][r] = x[2];
+            q[2 * i + 1][2 + r] = x[3];
+        }
+    }
+    constexpr int NO = kFew ? 4 * NV : 8 * NV;
+    float o[NO][4], followed[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
     int stage = 0;
     for (int i = 16 * warp; i < count; i += kStep) {
         copies_wait<kDeep - 2>();
@@ -360,95 +368,173 @@ template <typename T, int DM, int W, bool kFew> __global__ void __launch_bounds_
             for (int c = 0; c < NV; ++c) vw[n][c] = *reinterpret_cast<const uint4*>(from + (2 * NK + n * NV + c) * 512);
         ask(i + (kDeep - 1) * kStep, stage ? stage - 1 : kDeep - 1);
         stage = stage + 1 == kDeep ? 0 : stage + 1;
-        float s[2][4];
+        if constexpr (kFew) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};      // two sums side by side
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-#pragma unroll
-        for (int c = 0; c < NK; ++c)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {      // (the two sums go on side by side)
-                mma_16816(s[n], q[2 * c], kw[n][c].x, kw[n][c].y, T());
-                mma_16816(s[n], q[2 * c + 1], kw[n][c].z, kw[n][c].w, T());
+            for (int c = 0; c < NK; ++c) {
+                const uint32_t a0[4] = {kw[0][c].x, kw[1][c].x, kw[0][c].y, kw[1][c].y}, a1[4] = {kw[0][c].z, kw[1][c].z, kw[0][c].w, kw[1][c].w};
+                mma_16816(s, a0, q[2 * c][0], q[2 * c][2], T());
+                mma_16816(s1, a1, q[2 * c + 1][0], q[2 * c + 1][2], T());
             }
-        // element e of s[n]: row g + 8 (e / 2), key i + 8 n + 2 t + e % 2
-        if (tokens > 1 || i + 16 > count)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+            for (int e = 0; e < 4; ++e) s[e] += s1[e];
+            // element e: key i + g + 8 (e / 2), row 2 t + e % 2
+            if (tokens > 1 || i + 16 > count) {
 #pragma unroll
-            for (int e = 0; e < 2 * RN; ++e) {
-                const int at_i = i + 8 * n + 2 * t + (e & 1);
-                bool seen = at_i < count;
-                if (tokens > 1) {      // (one token sees every key that is counted)
-                    const int64_t j = key_at(K, i0 + at_i), p = at[e >> 1];
-                    seen = seen && j <= p && (p - j < A.window || j < A.sinks);
-                }
-                if (!seen) s[n][e] = -INFINITY;
-            }
-        float top[2];
-#pragma unroll
-        for (int r = 0; r < RN; ++r) {
-            top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * A.scale2;
-            top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
-            top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
-        }
-        // the followed maximum moves when it has grown by more than 2^8
-        if (__any_sync(~0u, top[0] > followed[0] + 8.f || (!kFew && top[1] > followed[1] + 8.f))) {
-#pragma unroll
-            for (int r = 0; r < RN; ++r) {
-                const float now = fmaxf(followed[r], top[r]), shrink = power(followed[r] - (now == -INFINITY ? 0.f : now));
-                followed[r] = now;
-                total[r] *= shrink;
-#pragma unroll
-                for (int j = 0; j < 8 * NV; ++j) {
-                    o[j][2 * r] *= shrink;
-                    o[j][2 * r + 1] *= shrink;
+                for (int e = 0; e < 4; ++e) {
+                    const int at_i = i + g + 8 * (e >> 1);
+                    bool seen = at_i < count;
+                    if (tokens > 1) {      // (one token sees every key that is counted)
+                        const int64_t j = key_at(K, i0 + at_i), p = at[e & 1];
+                        seen = seen && j <= p && (p - j < A.window || j < A.sinks);
+                    }
+                    if (!seen) s[e] = -INFINITY;
                 }
             }
-        }
+            float top[2] = {fmaxf(s[0], s[2]) * A.scale2, fmaxf(s[1], s[3]) * A.scale2};
+            if (__any_sync(~0u, top[0] > followed[0] + 8.f || top[1] > followed[1] + 8.f)) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+                for (int r = 0; r < 2; ++r) {
 #pragma unroll
-            for (int e = 0; e < 2 * RN; ++e) {
-                const float f = followed[e >> 1];
-                s[n][e] = power(fmaf(s[n][e], A.scale2, f == -INFINITY ? 0.f : kShift - f));
-                total[e >> 1] += s[n][e];
-            }
-        const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), kFew ? 0u : pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]),
-                               kFew ? 0u : pack2<T>(s[1][2], s[1][3])};
+                    for (int x = 4; x < 32; x <<= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], x));
+                    const float now = fmaxf(followed[r], top[r]), shrink = power(followed[r] - (now == -INFINITY ? 0.f : now));
+                    followed[r] = now;
+                    total[r] *= shrink;
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            uint32_t v[4][4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                v[n][0] = vw[n][c].x; v[n][1] = vw[n][c].y; v[n][2] = vw[n][c].z; v[n][3] = vw[n][c].w;
+                    for (int j = 0; j < NO; ++j) {
+                        o[j][r] *= shrink;
+                        o[j][2 + r] *= shrink;
+                    }
+                }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t order = j & 1 ? 0x7632 : 0x5410;
-                mma_16816(o[8 * c + j], p, __byte_perm(v[0][j / 2], v[1][j / 2], order), __byte_perm(v[2][j / 2], v[3][j / 2], order), T());
+            for (int e = 0; e < 4; ++e) {
+                const float f = followed[e & 1];
+                s[e] = power(fmaf(s[e], A.scale2, f == -INFINITY ? 0.f : kShift - f));
+                total[e & 1] += s[e];
             }
-        }
-    }
-    copies_wait<0>();
-    __syncthreads();
-    // a warp's sums to shared memory: row g + 8 r, element 64 c + 8 n + j of o[8 c + j][2 r + n % 2], n = 2 t, 2 t + 1
+            const uint32_t p0 = turned8(pack2<T>(s[0], s[1])), p1 = turned8(pack2<T>(s[2], s[3]));
+            // block 4 c + j: elements 64 c + 8 g + 2 j (and the one behind it, as rows g + 8 of the left operand)
 #pragma unroll
-    for (int r = 0; r < RN; ++r) {
-        total[r] += __shfl_xor_sync(~0u, total[r], 1);
-        total[r] += __shfl_xor_sync(~0u, total[r], 2);
+            for (int c = 0; c < NV; ++c) {
+                const uint32_t v[4][4] = {{vw[0][c].x, vw[0][c].y, vw[0][c].z, vw[0][c].w}, {vw[1][c].x, vw[1][c].y, vw[1][c].z, vw[1][c].w},
+                                          {vw[2][c].x, vw[2][c].y, vw[2][c].z, vw[2][c].w}, {vw[3][c].x, vw[3][c].y, vw[3][c].z, vw[3][c].w}};
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t a[4] = {__byte_perm(v[0][j], v[1][j], 0x5410), __byte_perm(v[0][j], v[1][j], 0x7632), __byte_perm(v[2][j], v[3][j], 0x5410),
+                                           __byte_perm(v[2][j], v[3][j], 0x7632)};
+                    mma_16816(o[4 * c + j], a, p0, p1, T());
+                }
+            }
+        } else {
+            float s[2][4];
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int j = 0; j < 8; j += 4)
-                    *reinterpret_cast<float4*>(&joined[warp][g + 8 * r][64 * c + 16 * t + 8 * n + j]) =
-                        make_float4(o[8 * c + j][2 * r + n], o[8 * c + j + 1][2 * r + n], o[8 * c + j + 2][2 * r + n], o[8 * c + j + 3][2 * r + n]);
-        if (t == 0) {
-            stats[warp][g + 8 * r][0] = followed[r];
-            stats[warp][g + 8 * r][1] = total[r];
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NK; ++c)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {      // (the two sums go on side by side)
+                    mma_16816(s[n], q[2 * c], kw[n][c].x, kw[n][c].y, T());
+                    mma_16816(s[n], q[2 * c + 1], kw[n][c].z, kw[n][c].w, T());
+                }
+            // element e of s[n]: row g + 8 (e / 2), key i + 8 n + 2 t + e % 2
+            if (tokens > 1 || i + 16 > count)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at_i = i + 8 * n + 2 * t + (e & 1);
+                    bool seen = at_i < count;
+                    if (tokens > 1) {      // (one token sees every key that is counted)
+                        const int64_t j = key_at(K, i0 + at_i), p = at[e >> 1];
+                        seen = seen && j <= p && (p - j < A.window || j < A.sinks);
+                    }
+                    if (!seen) s[n][e] = -INFINITY;
+                }
+            float top[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * A.scale2;
+                top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
+                top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
+            }
+            // the followed maximum moves when it has grown by more than 2^8
+            if (__any_sync(~0u, top[0] > followed[0] + 8.f || top[1] > followed[1] + 8.f)) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float now = fmaxf(followed[r], top[r]), shrink = power(followed[r] - (now == -INFINITY ? 0.f : now));
+                    followed[r] = now;
+                    total[r] *= shrink;
+#pragma unroll
+                    for (int j = 0; j < 8 * NV; ++j) {
+                        o[j][2 * r] *= shrink;
+                        o[j][2 * r + 1] *= shrink;
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float f = followed[e >> 1];
+                    s[n][e] = power(fmaf(s[n][e], A.scale2, f == -INFINITY ? 0.f : kShift - f));
+                    total[e >> 1] += s[n][e];
+                }
+            const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]),
+                                   pack2<T>(s[1][2], s[1][3])};
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                uint32_t v[4][4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    v[n][0] = vw[n][c].x; v[n][1] = vw[n][c].y; v[n][2] = vw[n][c].z; v[n][3] = vw[n][c].w;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t order = j & 1 ? 0x7632 : 0x5410;
+                    mma_16816(o[8 * c + j], p, __byte_perm(v[0][j / 2], v[1][j / 2], order), __byte_perm(v[2][j / 2], v[3][j / 2], order), T());
+                }
+            }
+        }
+    }
+    let_next();      // the join may be placed
+    copies_wait<0>();
+    __syncthreads();
+    if constexpr (kFew) {      // row 2 t + r, element 64 c + 8 g + 2 j + k of o[4 c + j][2 k + r]
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) total[r] += __shfl_xor_sync(~0u, total[r], x);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; j += 2)
+                    *reinterpret_cast<float4*>(&joined[warp][2 * t + r][64 * c + 8 * g + 2 * j]) = make_float4(o[4 * c + j][r], o[4 * c + j][2 + r], o[4 * c + j + 1][r], o[4 * c + j + 1][2 + r]);
+            if (g == 0) {
+                stats[warp][2 * t + r][0] = followed[r];
+                stats[warp][2 * t + r][1] = total[r];
+            }
+        }
+    } else {
+        // a warp's sums to shared memory: row g + 8 r, element 64 c + 8 n + j of o[8 c + j][2 r + n % 2], n = 2 t, 2 t + 1
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            total[r] += __shfl_xor_sync(~0u, total[r], 1);
+            total[r] += __shfl_xor_sync(~0u, total[r], 2);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int j = 0; j < 8; j += 4)
+                        *reinterpret_cast<float4*>(&joined[warp][g + 8 * r][64 * c + 16 * t + 8 * n + j]) =
+                            make_float4(o[8 * c + j][2 * r + n], o[8 * c + j + 1][2 * r + n], o[8 * c + j + 2][2 * r + n], o[8 * c + j + 3][2 * r + n]);
+            if (t == 0) {
+                stats[warp][g + 8 * r][0] = followed[r];
+                stats[warp][g + 8 * r][1] = total[r];
+            }
         }
     }
     __syncthreads();
