@@ -580,7 +580,8 @@ vqc_status vqc_norm_rotary_backward(vqc_real dtype, int64_t batch, int64_t token
 /* The same for serving, into a cache: token t of a sequence stands at position lengths[b] - tokens + t
  * (lengths: device int32 [batch], tokens in the cache with the new ones); its normalised, turned key and
  * its value as it is are written at that place of cache_k and cache_v [batch, capacity, groups, dim], its query
- * to q_out (dense).  Places outside of the cache are not written.
+ * to q_out (dense).  Places outside of the cache are not written.  The caches' places lie apart from one another
+ * and from q, k and v.
  * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_CUDA. */
 vqc_status vqc_norm_rotary_step(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
                                 int64_t dim, int64_t capacity, const vqc_heads* q, const vqc_heads* k,
@@ -630,7 +631,8 @@ size_t vqc_attention_workspace_bytes(int32_t mode, vqc_real dtype, int64_t batch
  * lengths[b] - tokens + t and sees the keys of vqc_attention_forward at that position (lengths beyond
  * 0..capacity count as the nearest; a token at a negative position sees nothing: zeros).
  *   q [batch, tokens, heads, dim]; cache_k, cache_v [batch, capacity, groups, dim]; o dense.
- * Places of a cache from the length on are not read.  No backward.
+ * Places of a cache from the length on are not read.  With several tokens, keys and values that are not finite may
+ * make NaN of outputs of their sequence that do not see them.  No backward.
  * Errors: VQC_ERR_INVALID_ARG, VQC_ERR_WORKSPACE, VQC_ERR_CUDA. */
 vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int64_t heads, int64_t groups,
                               int64_t dim, int64_t capacity, const vqc_heads* q, const vqc_heads* cache_k,

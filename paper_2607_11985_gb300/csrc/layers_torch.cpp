@@ -16,6 +16,8 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstdint>
 #include <optional>
@@ -284,11 +286,38 @@ HeadRows cache_rows(const Tensor& given, const HeadRows& q, int64_t groups, int6
     if (r.code != q.code || r.size(0) != q.size(0) || (groups > 0 && r.size(2) != groups) || (capacity >= 0 && r.size(1) != capacity) || r.size(3) != q.size(3))
         throw Refused(std::string(name) + " does not fit: " + told(given) + " beside " + told(q.t));
     if (written) {
+        // axes by their strides, each of which has to step over all places of the shorter ones
+        std::array<std::pair<int64_t, int64_t>, 3> axes;
+        for (int i = 0; i < 3; ++i) axes[i] = {r.t.stride(i), r.t.size(i)};
+        std::sort(axes.begin(), axes.end());
         bool apart = r.t.is_same(given);
-        for (int i = 0; i < 3; ++i) apart = apart && (r.t.stride(i) != 0 || r.t.size(i) == 1);
+        int64_t last = r.size(3) - 1;
+        for (const auto& [stride, size] : axes) {
+            if (size < 2) continue;
+            apart = apart && stride > last;
+            last += (size - 1) * stride;
+        }
         if (!apart) throw Refused(std::string(name) + " is written: the elements of a head must be adjacent and no two places one (got " + told(given) + ")");
     }
     return r;
+}
+// The first and last places of two tensors' elements span memory that they share?
+bool shares(const Tensor& a, const Tensor& b) {
+    auto span = [](const Tensor& t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
+        const char* p = static_cast<const char*>(t.data_ptr());
+        return std::make_pair(p, p + (last + 1) * t.element_size());
+    };
+    if (!a.numel() || !b.numel()) return false;
+    const auto x = span(a), y = span(b);
+    return x.first < y.second && y.first < x.second;
+}
+// The forms for serving have no gradients: better an error than one that is lost.
+void without_gradient(std::initializer_list<const Tensor*> all) {
+    if (!at::GradMode::is_enabled()) return;
+    for (const Tensor* t : all)
+        if (t->defined() && t->requires_grad()) throw Refused("a step has no gradients: call it without recording (torch.no_grad) or on detached tensors");
 }
 Tensor int_rows(const Tensor& given, int64_t batch, int64_t tokens, const char* name) {      // tokens < 0: [batch]
     if (!given.defined()) return given;
@@ -378,6 +407,11 @@ void written(const Tensor& t) {
 Tensor rotary_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& ck, const Tensor& cv, const Tensor& lengths, const Turn& given) {
     const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v");
     const HeadRows kc = cache_rows(ck, a, b.size(2), -1, true, "cache_k"), vc = cache_rows(cv, a, b.size(2), kc.size(1), true, "cache_v");
+    without_gradient({&q, &k, &v, &given.wq, &given.wk});
+    // (views of one tensor that holds keys and values are fine: other places)
+    if (kc.t.numel() && kc.t.data_ptr() == vc.t.data_ptr()) throw Refused("cache_k and cache_v are written: they must be two");
+    for (const HeadRows* from : {&a, &b, &c})
+        if (shares(from->t, kc.t) || shares(from->t, vc.t)) throw Refused("the caches are written: q, k and v must lie elsewhere");
     const Turn t = turn_of(a, given);
     if (!lengths.defined()) throw Refused("lengths must be given");
     const Tensor n = int_rows(lengths, a.size(0), -1, "lengths");
@@ -442,6 +476,7 @@ variable_list attention_backward(const Tensor& go, const Tensor& q, const Tensor
 Tensor attention_step(const Tensor& q, const Tensor& ck, const Tensor& cv, const Sight& given) {
     const HeadRows a = head_rows(q, "q"), kc = cache_rows(ck, a, -1, -1, false, "cache_k"), vc = cache_rows(cv, a, kc.size(2), kc.size(1), false, "cache_v");
     if (!given.lengths.defined()) throw Refused("lengths must be given");
+    without_gradient({&q, &ck, &cv});
     const Sight s = sight_of(a, kc.size(2), given);
     Tensor o = dense(a, a.size(2));
     const size_t bytes = vqc_attention_step_workspace_bytes(a.size(0), a.size(1), a.size(2), kc.size(2), a.size(3), kc.size(1), s.window, s.sinks);

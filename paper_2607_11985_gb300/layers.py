@@ -162,7 +162,8 @@ def norm_rotary(q, k, weight_q=None, weight_k=None, frequencies=None, positions=
 def norm_rotary_step(q, k, v, cache_k, cache_v, lengths, weight_q=None, weight_k=None, frequencies=None, eps=1e-6):
     """q' of new tokens, whose k' and v are written into the caches [batch, capacity, groups, dim] in place:
     token t of a sequence stands at position lengths - tokens + t (lengths: int32 [batch], with the
-    new tokens); places outside of the cache are not written."""
+    new tokens); places outside of the cache are not written.  The caches must lie apart from q, k and v.  No
+    gradients: tensors that need one are refused while autograd records."""
     return _native.rotary_step(q, k, v, cache_k, cache_v, lengths, weight_q, weight_k, frequencies, eps)
 
 
@@ -187,5 +188,6 @@ def attention(q, k, v, window=None, sinks=0, scale=None, lengths=None):
 
 def attention_step(q, cache_k, cache_v, lengths, window=None, sinks=0, scale=None):
     """o of the last tokens of sequences over caches [batch, capacity, groups, dim]: token t stands at
-    position lengths - tokens + t (lengths: int32 [batch], the tokens in the cache) and sees what ``attention`` sees there."""
+    position lengths - tokens + t (lengths: int32 [batch], the tokens in the cache) and sees what ``attention`` sees
+    there.  No gradients: tensors that need one are refused while autograd records."""
     return _native.attention_step(q, cache_k, cache_v, window, sinks, scale, lengths)

@@ -370,6 +370,35 @@ def test_tokens_one_by_one_as_a_whole_sequence(layers, dtype):
     check(whole, cpu(want), dtype, 1.5, "whole")
 
 
+def test_step_refuses_shared_places(layers):
+    """A cache is written: its places have to lie apart; views of one tensor for both caches are fine."""
+    q, k, n = heads(2, 2, 1, 4, 8, F32), heads(3, 2, 1, 2, 8, F32), torch.tensor([3, 3], dtype=torch.int32, device="cuda")
+    ck, cv = torch.zeros(2, 5, 2, 8, device="cuda"), torch.zeros(2, 5, 2, 8, device="cuda")
+    over = torch.zeros(200, device="cuda")
+    bad = [
+        lambda: layers.norm_rotary_step(q, k, k, ck, ck, n), lambda: layers.norm_rotary_step(q, ck[:, 2:3], k, ck, cv, n),
+        lambda: layers.norm_rotary_step(q, k, cv[:, 2:3], ck, cv, n),
+        lambda: layers.norm_rotary_step(q, k, k, over.as_strided((2, 5, 2, 8), (64, 8, 8, 1)), cv, n),
+        lambda: layers.norm_rotary_step(q, k, k, over.as_strided((2, 5, 2, 8), (80, 16, 7, 1)), cv, n),
+        lambda: layers.norm_rotary_step(q.clone().requires_grad_(), k, k, ck, cv, n),
+        lambda: layers.norm_rotary_step(q, k, k, ck, cv, n, torch.ones(8, device="cuda", requires_grad=True)),
+        lambda: layers.attention_step(q.clone().requires_grad_(), ck, cv, n),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("call %d was not refused" % i)
+    assert not bool(ck.any()) and not bool(cv.any())
+    # keys beside values in one tensor; heads before places
+    both, turned = torch.zeros(2, 5, 2, 2, 8, device="cuda"), torch.zeros(2, 2, 2, 5, 8, device="cuda")
+    with torch.no_grad():
+        layers.norm_rotary_step(q.clone().requires_grad_(), k, k, ck, cv, n)
+    layers.norm_rotary_step(q, k, k, both[:, :, 0], both[:, :, 1], n)
+    layers.norm_rotary_step(q, k, k, turned[0].transpose(1, 2), turned[1].transpose(1, 2), n)
+    for a, b in ((both[:, :, 0], ck), (both[:, :, 1], cv), (turned[0].transpose(1, 2), ck), (turned[1].transpose(1, 2), cv)):
+        assert torch.equal(a, b)
+
+
 # -------------------------------------------------------------- streams, graphs, repeats
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
