@@ -703,8 +703,11 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
             if (issuer) {
                 product(acc1, tmem + 128, base + L::kX + xu.slot * L::kTile, u == 0);
                 mma_commit<1>(xempty + 8 * xu.slot);
+                // (not with dV: d, which lies beside the stage of Y, has been read by all only where dS is there)
+                if (kKeys) mma_commit<1>(yempty + 8 * yu.slot);
             }
             xu.next();
+            if (kKeys) yu.next();
             return true;
         };
         for (int u = -1; ok && units && u < units; ++u) {
@@ -713,11 +716,7 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
                 if (!ok) break;
                 tc_fence_after();
                 if (kKeys) {
-                    if (issuer) {
-                        product(acc2, tmem, base + L::kY + yu.slot * L::kTile, u == 0);
-                        mma_commit<1>(yempty + 8 * yu.slot);
-                    }
-                    yu.next();
+                    if (issuer) product(acc2, tmem, base + L::kY + yu.slot * L::kTile, u == 0);
                 }
             }
             if (u + 1 < units) {
