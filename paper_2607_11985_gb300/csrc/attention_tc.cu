@@ -9,6 +9,10 @@
 // more than 2^8: P and the row's sum are relative to the followed one, and O is rescaled in tensor memory
 // then (the product that last wrote it has ended: its scores' successor was committed after it).
 //
+// 4 x 4096 tokens, 16 heads over 4 of 128 elements, bfloat16: 176 us, 1560 TFLOP/s of visible pairs (16384 tokens: 610 us, 1800).
+// Bound by the products: a 128 x 128 x 16 one takes 64 cycles with its left operand in tensor memory (P V) and about 100
+// with both in shared memory (Q K^T).
+//
 // P is rounded to the operands' type (one rounding of a probability, whose error averages out over the keys
 // of a row), its sum is taken before.  float16 probabilities are held times 2^6: 2^-30 of the largest.
 //
@@ -496,6 +500,8 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
 // P and dS are rounded to the operands' type.  float16 holds P times 2^14 and
 // dS times the power of two that keeps its largest possible value, 2 max|dO| max|V| (row norms), below 2^15: gradients
 // of any size keep their bits.
+//
+// 4 x 4096 tokens as above: 662 us, 1040 TFLOP/s of five products (seven are made); tensor pipe active for 70%.
 //
 // Keys that stay visible through a window are seen by all later queries: their tiles' far queries are cut into
 // pieces, a CTA each, whose sums are joined in their order.

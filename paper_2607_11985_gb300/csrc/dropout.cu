@@ -5,9 +5,9 @@
 // (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) is at least
 // p 2^32, so that no mask is stored: the backward draws it again, in any order and launch shape.
 //
-// Bound by HBM: x (and the residual) once, y once.  A block of four words takes 10 rounds of two
-// 32 x 32 -> 64 bit products, about 70 instructions: 18 per element, half of what the SMs issue
-// while 6 bytes per element (16-bit x, residual and y) pass through HBM.
+// Bound by HBM (x and the residual once, y once) and nearly as much by the generator: 10 rounds of two 32 x 32 -> 64 bit
+// products and two exclusive ors for four elements.  8192 x 4096 bfloat16: forward with a residual 32 us (6.3 TB/s),
+// backward 30 us (4.4 TB/s: bound by the integer instructions).
 #include <algorithm>
 #include <cmath>
 
@@ -30,7 +30,7 @@ struct DropArgs {
 };
 
 // kState: the rounds' keys from a seed in memory; else as they come with the arguments, where they cost no instruction
-// (with two additions a round the kernel took 42 us in the place of 37).
+// (two additions a round: 5 us more at 8192 x 4096).
 template <bool kState> __device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t seed, const uint32_t* key) {
     uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
 #pragma unroll
