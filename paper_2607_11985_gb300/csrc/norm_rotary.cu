@@ -13,7 +13,7 @@
 // Bound by HBM (x once, y once; x and the gradient once, the result once).  A head's elements lie
 // in the registers of 4 to 32 lanes, each lane with 4 of the first half and their 4 partners, so that pairs meet
 // in a lane; a lane keeps its sines and cosines over the heads of its token.  8192 tokens of 32 + 8 heads of 128, bfloat16:
-// forward 37 us (4.6 TB/s), backward 60 (4.2 TB/s): a head's sums wait for its loads, of which the next heads' are on the way.
+// forward 34 us (4.9 TB/s), backward 54 (4.6 TB/s): a head's sums wait for its loads, of which the next heads' are on the way.
 #include <algorithm>
 #include <cmath>
 
@@ -408,13 +408,14 @@ template <bool kBack> const void* rotary_fn(int dtype, int lanes) {
 
 bool packs4(int dtype, const Heads& h) { return heads_on(h, elem_size(dtype), 4 * elem_size(dtype)); }
 
-// CTAs of a backward that sums over all tokens: as many as stay on the SMs together.
-int64_t back_ctas(int64_t units, int groups) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), 6LL * sm_count())); }
-// Heads of a token that a group of lanes takes: as many as leave every SM 64 groups (a token's sines and cosines
-// are made once per group).
+// CTAs of a backward that sums over all tokens: as many as stay on the SMs together (8192 tokens of 40 heads of 128: 54 us; with
+// six per SM, which take turns, 60).
+int64_t back_ctas(int64_t units, int groups) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), 2LL * sm_count())); }
+// Heads of a token that a group of lanes takes: as many as leave every SM 32 groups, which stay on it together (a token's sines and
+// cosines are made once per group; 64 groups: 37 us in the place of 34 for a forward of 8192 tokens, 128: 44).
 int heads_at_once(int64_t tokens, int heads) {
     int chunk = heads;
-    while (chunk > 1 && tokens * ceil_div(heads, chunk) < 64LL * sm_count()) chunk = (chunk + 1) / 2;
+    while (chunk > 1 && tokens * ceil_div(heads, chunk) < 32LL * sm_count()) chunk = (chunk + 1) / 2;
     return chunk;
 }
 
