@@ -86,7 +86,7 @@ __device__ __forceinline__ float power(float x) {
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
 // The end of a wait that was not over at the first look, out of line: in the place of every wait its code made a unit of the
-// backward last 900 cycles even without products and arithmetic, for instructions to be fetched (550 so), and a
+// backward last 900 cycles even without products and arithmetic, for instructions to be fetched (640 so), and a
 // forward of 4 x 4096 tokens, 16 heads, 208 us (194).
 static __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, unsigned long long ns, const volatile int* gave_up) {
     // (a bound of milliseconds is looked at after some tries, each of which waits by itself: reading the clock takes long)
