@@ -84,7 +84,7 @@ class HybridBlock(torch.nn.Module):
 class SequenceBlock(torch.nn.Module):
     """See the module's text.  ``heads`` of ``dim`` elements, ``groups`` of keys and values; ``window`` (None: every
     earlier token) and ``sinks`` first tokens that stay visible; ``dropout`` of the attention's branch in
-    training, drawn anew in every forward pass (``draws``: seed and offset)."""
+    training, drawn anew in every forward pass (``draws``: seed and offset, which counts the passes)."""
 
     def __init__(self, width: int, heads: int, groups: int, dim: int, qubits: int, window=None, sinks: int = 0,
                  dropout: float = 0.0, dtype=torch.float32, seed: int = 0, **rest):
@@ -110,15 +110,22 @@ class SequenceBlock(torch.nn.Module):
         a = layers.layer_norm(h, self.norm_weight, self.norm_bias)
         return [layers.linear(a, w).unflatten(-1, (-1, self.dim)) for w in (self.w_q, self.w_k, self.w_v)]
 
-    def forward(self, h, lengths=None):
+    def _next_draws(self):
+        """Seed and offset of a pass, in a tensor of their own: its backward draws the same elements again."""
+        if torch._C._current_graph_task_id() >= 0:      # inside of a backward pass
+            raise RuntimeError("a forward pass that is made again for its backward (activation checkpointing) would draw other "
+                               "elements than the first one: give the block its draws")
+        draws = self.draws.clone()
+        self.draws[1] += 1
+        return draws
+
+    def forward(self, h, lengths=None, draws=None):
+        """``draws``: seed and offset of the dropout, an int64 tensor on the device, in the place of the block's own."""
         q, k, v = self._heads(h)
         q, k = layers.norm_rotary(q, k, self.weight_q, self.weight_k, self.frequencies)
         a = layers.attention(q, k, v, self.window, self.sinks, lengths=lengths).flatten(-2)
         if self.training and self.dropout:
-            # a state of its own for every pass: its backward draws the same elements again
-            state = self.draws.clone()
-            self.draws[1] += 1
-            h = layers.dropout(layers.linear(a, self.w_o), self.dropout, state, residual=h)
+            h = layers.dropout(layers.linear(a, self.w_o), self.dropout, self._next_draws() if draws is None else draws, residual=h)
         else:
             h = layers.linear(a, self.w_o, residual=h)
         return self.rest(h)

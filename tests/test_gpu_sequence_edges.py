@@ -1,0 +1,78 @@
+"""Operators of a sequence and their block at the edges: an epsilon of nothing, gradients that have nowhere to go, strides of
+axes of one, prompts over a cache, blocks whose forward pass is made twice, stacked and converted blocks."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests import sequence_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+    torch.cuda.set_device(0)
+    from paper_2607_11985_gb300 import layers
+    return layers
+
+
+@pytest.fixture(autouse=True)
+def errors_are_reported(layers):
+    yield
+    from paper_2607_11985_gb300 import binding as B
+    torch.cuda.synchronize()
+    B.vqc_sync_check(torch.cuda.current_stream().cuda_stream)
+
+
+def normal(seed, *shape, dtype=F32):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def cpu(pair):
+    return tuple(t.cpu() for t in pair)
+
+
+# -------------------------------------------------------------- the block
+
+def blocks(count, dtype=F32, **given):
+    """Blocks whose hybrid half has a test of its own; what they drop is y == h."""
+    from paper_2607_11985_gb300.hybrid import SequenceBlock
+    made = [SequenceBlock(48, 4, 2, 24, 3, window=7, sinks=2, dropout=0.5, dtype=dtype, hidden=64, **given) for _ in range(count)]
+    for b in made:
+        b.rest = torch.nn.Identity()
+    return torch.nn.Sequential(*made)
+
+
+def gradients(model, call, h, gy):
+    model.zero_grad()
+    x = h.detach().requires_grad_()
+    y = call(x)
+    y.backward(gy)
+    return [y.detach(), x.grad] + [p.grad.clone() for p in model.parameters()]
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_checkpointed_block_that_counts_its_passes(layers, reentrant):
+    """Draws that are counted in the block would be others in the second pass: refused there, and given by the caller."""
+    from torch.utils.checkpoint import checkpoint
+    block, h, gy = blocks(1, seed=5)[0], normal(1, 2, 21, 48), normal(2, 2, 21, 48)
+    with pytest.raises(RuntimeError, match="draws"):
+        gradients(block, lambda x: checkpoint(block, x, use_reentrant=reentrant), h, gy)
+    state, other = torch.tensor([5, 40], device="cuda"), torch.tensor([5, 41], device="cuda")
+    count = block.draws.clone()
+    want = gradients(block, lambda x: block(x, None, state), h, gy)
+    got = gradients(block, lambda x: checkpoint(block, x, None, state, use_reentrant=reentrant), h, gy)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(block.draws, count)
+    kept = ref.kept(h.shape, 0.5, 5, 40).cuda()
+    assert torch.equal(want[0] == h, ~kept)
+    assert not torch.equal(block(h, None, other) == h, ~kept)
