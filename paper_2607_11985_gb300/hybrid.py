@@ -84,11 +84,13 @@ class HybridBlock(torch.nn.Module):
 class SequenceBlock(torch.nn.Module):
     """See the module's text.  ``heads`` of ``dim`` elements, ``groups`` of keys and values; ``window`` (None: every
     earlier token) and ``sinks`` first tokens that stay visible; ``dropout`` of the attention's branch in
-    training, drawn anew in every forward pass (``draws``: seed and offset, which counts the passes)."""
+    training, drawn anew in every forward pass: from torch's generator, or with a ``seed`` of its own from that and the
+    count of passes (``draws``)."""
 
     def __init__(self, width: int, heads: int, groups: int, dim: int, qubits: int, window=None, sinks: int = 0,
-                 dropout: float = 0.0, dtype=torch.float32, seed: int = 0, **rest):
+                 dropout: float = 0.0, dtype=torch.float32, seed: int | None = None, **rest):
         super().__init__()
+        self.counts, seed = seed is not None, seed or 0
         self.heads, self.groups, self.dim, self.window, self.sinks, self.dropout = heads, groups, dim, window, sinks, dropout
         g = torch.Generator().manual_seed(seed + 1)
 
@@ -111,10 +113,13 @@ class SequenceBlock(torch.nn.Module):
         return [layers.linear(a, w).unflatten(-1, (-1, self.dim)) for w in (self.w_q, self.w_k, self.w_v)]
 
     def _next_draws(self):
-        """Seed and offset of a pass, in a tensor of their own: its backward draws the same elements again."""
+        """Seed and offset of a pass, in a tensor of their own: its backward draws the same elements again.  (Torch's generator
+        is put back for a pass that is made again, and goes on in the replays of a captured one.)"""
+        if not self.counts:
+            return torch.empty_like(self.draws).random_()
         if torch._C._current_graph_task_id() >= 0:      # inside of a backward pass
             raise RuntimeError("a forward pass that is made again for its backward (activation checkpointing) would draw other "
-                               "elements than the first one: give the block its draws")
+                               "elements than the first one: give the block its draws, or no seed")
         draws = self.draws.clone()
         self.draws[1] += 1
         return draws

@@ -1,5 +1,6 @@
 """Operators of a sequence and their block at the edges: an epsilon of nothing, gradients that have nowhere to go, strides of
 axes of one, prompts over a cache, blocks whose forward pass is made twice, stacked and converted blocks."""
+import math
 
 import pytest
 
@@ -62,6 +63,19 @@ def gradients(model, call, h, gy):
 
 
 @pytest.mark.parametrize("reentrant", [False, True])
+def test_checkpointed_block(layers, reentrant):
+    """A forward pass that is made again for its backward draws what it has drawn: gradients are those of the plain block."""
+    from torch.utils.checkpoint import checkpoint
+    model, h, gy = blocks(2), normal(1, 2, 21, 48), normal(2, 2, 21, 48)
+    for seed in (1, 2):
+        torch.manual_seed(seed)
+        want = gradients(model, model, h, gy)
+        torch.manual_seed(seed)
+        got = gradients(model, lambda x: checkpoint(model, x, use_reentrant=reentrant), h, gy)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
 def test_checkpointed_block_that_counts_its_passes(layers, reentrant):
     """Draws that are counted in the block would be others in the second pass: refused there, and given by the caller."""
     from torch.utils.checkpoint import checkpoint
@@ -76,3 +90,52 @@ def test_checkpointed_block_that_counts_its_passes(layers, reentrant):
     kept = ref.kept(h.shape, 0.5, 5, 40).cuda()
     assert torch.equal(want[0] == h, ~kept)
     assert not torch.equal(block(h, None, other) == h, ~kept)
+
+
+def test_stacked_blocks_draw_apart(layers):
+    """Blocks without a seed draw from torch's generator: each its own, anew in every pass, again from the same seed."""
+    model, h = blocks(3), normal(1, 4, 40, 48)
+
+    def masks():
+        with torch.no_grad():
+            return [block(h) == h for block in model]
+    torch.manual_seed(3)
+    first, second = masks(), masks()
+    drawn = first + second
+    for i, a in enumerate(drawn):
+        assert abs(float(a.double().mean()) - 0.5) < 5 * 0.5 / math.sqrt(a.numel())
+        for b in drawn[:i]:          # independent draws agree in half of the places
+            assert abs(float((a == b).double().mean()) - 0.5) < 5 * 0.5 / math.sqrt(a.numel())
+    torch.manual_seed(3)
+    assert all(torch.equal(a, b) for a, b in zip(masks(), first))
+
+
+def test_captured_block_draws_anew(layers):
+    """Torch's generator goes on in the replays; a replay's backward draws what its forward has drawn."""
+    block, h, gy = blocks(1)[0], normal(1, 2, 21, 48), normal(2, 2, 21, 48)
+
+    def step():
+        x = h.detach().requires_grad_()
+        y = block(x)
+        branch, = torch.autograd.grad(y, block.w_o, gy)
+        return y.detach(), branch
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, branch = step()
+    seen = []
+    with torch.no_grad():
+        q, k, v = block._heads(h)
+        q, k = layers.norm_rotary(q, k, block.weight_q, block.weight_k, block.frequencies)
+        a = layers.attention(q, k, v, block.window, block.sinks).flatten(-2).reshape(-1, 96).double()
+    for _ in range(3):
+        graph.replay()
+        kept = (y != h)
+        seen.append(kept.clone())
+        want = torch.where(kept, 2 * gy, 0.0).reshape(-1, 48).double().t() @ a
+        assert float((branch.double() - want).norm() / want.norm()) < 1e-5        # sums of 42 terms of another mask: 1
+    assert not torch.equal(seen[0], seen[1]) and not torch.equal(seen[1], seen[2])
