@@ -217,7 +217,10 @@ template <typename T, int LANES, bool kBack> __global__ void __launch_bounds__(k
                     r[j] = ss.x + ss.y;
                 }
 #pragma unroll
-                for (int j = 0; j < HB; ++j) r[j] = rsqrtf(fmaf(group_sum(r[j]), per, A.eps));
+                for (int j = 0; j < HB; ++j) {
+                    r[j] = rsqrtf(fmaf(group_sum(r[j]), per, A.eps));
+                    if (kBack && h + j >= hi) r[j] = 0.f;      // no head: without an eps its zeros would be made NaN and counted in the sums
+                }
                 if constexpr (!kBack) {
 #pragma unroll
                     for (int j = 0; j < HB; ++j) {

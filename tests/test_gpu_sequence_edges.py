@@ -7,6 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import sequence_reference as ref
+from tests.layers_reference import check
 
 pytestmark = pytest.mark.gpu
 
@@ -39,8 +40,35 @@ def normal(seed, *shape, dtype=F32):
     return torch.randn(*shape, generator=g, device="cuda").to(dtype)
 
 
+def wide(t):
+    return None if t is None else t.detach().double()
+
+
 def cpu(pair):
     return tuple(t.cpu() for t in pair)
+
+
+def turns(dim):
+    return torch.tensor([10000.0 ** (-2 * i / dim) for i in range(dim // 2)], dtype=torch.float64, device="cuda")
+
+
+# -------------------------------------------------------------- norms and rotation
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("eps", [0.0, 1e-50])         # (the second is none as a float)
+@pytest.mark.parametrize("batch,tokens,count,groups,dim", [
+    (1, 1, 1, 1, 64), (2, 3, 3, 1, 64), (1, 5, 4, 2, 128), (2, 400, 3, 1, 64), (3, 700, 5, 3, 16), (2, 9, 3, 1, 33)])
+def test_norm_rotary_without_epsilon(layers, dtype, eps, batch, tokens, count, groups, dim):
+    """Heads in odd numbers, alone, many and few tokens; packs of elements and single ones."""
+    q, k, gq, gk = (normal(i, batch, tokens, n, dim, dtype=dtype) for i, n in ((1, count), (2, groups), (3, count), (4, groups)))
+    wq, wk, freq = normal(5, dim, dtype=dtype), normal(6, dim, dtype=dtype), turns(dim - dim % 2)
+    at = torch.arange(tokens).expand(batch, tokens)
+    y = layers.norm_rotary_forward(q, k, wq, wk, freq, eps=eps)
+    back = layers.norm_rotary_backward(gq, gk, q, k, wq, wk, freq, eps=eps)
+    for i, (x, w, g) in enumerate(((q, wq, gq), (k, wk, gk))):
+        want = ref.norm_rotary(wide(x).cpu(), wide(w).cpu(), freq.cpu(), at, eps, wide(g).cpu(), dtype)
+        for name, got in (("y", y[i]), ("gx", back[i]), ("gw", back[2 + i])):
+            check(got, want[name], dtype, 1, name + "qk"[i])
 
 
 # -------------------------------------------------------------- the block
