@@ -365,6 +365,7 @@ Turn turn_of(const HeadRows& q, const Turn& t) {
     if (r.frequencies.defined()) {
         if (r.frequencies.scalar_type() != at::kDouble || r.frequencies.dim() != 1 || 2 * r.frequencies.size(0) > dim || !here(r.frequencies))
             throw Refused("frequencies must be a CUDA float64 tensor of at most half as many elements as a head on the current device (got " + told(r.frequencies) + ")");
+        no_tangent(r.frequencies, "frequencies");
         r.frequencies = as_read(r.frequencies).contiguous();
     }
     if (!(t.eps >= 0)) throw Refused("eps must not be negative (got " + std::to_string(t.eps) + ")");
@@ -407,7 +408,7 @@ void written(const Tensor& t) {
 Tensor rotary_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& ck, const Tensor& cv, const Tensor& lengths, const Turn& given) {
     const HeadRows a = head_rows(q, "q"), b = head_rows(k, a, -1, "k"), c = head_rows(v, a, b.size(2), "v");
     const HeadRows kc = cache_rows(ck, a, b.size(2), -1, true, "cache_k"), vc = cache_rows(cv, a, b.size(2), kc.size(1), true, "cache_v");
-    without_gradient({&q, &k, &v, &given.wq, &given.wk});
+    without_gradient({&q, &k, &v, &given.wq, &given.wk, &given.frequencies});
     // (views of one tensor that holds keys and values are fine: other places)
     if (kc.t.numel() && kc.t.data_ptr() == vc.t.data_ptr()) throw Refused("cache_k and cache_v are written: they must be two");
     for (const HeadRows* from : {&a, &b, &c})
@@ -755,6 +756,7 @@ Tensor dropout(const Tensor& x, const Draw& d, const Tensor& res) {
                                 : dropout_run(x, d, res, false);
 }
 variable_list rotary(const Tensor& q, const Tensor& k, const Turn& t) {
+    if (recorded({&t.frequencies})) throw Refused("frequencies have no gradient: call it without recording (torch.no_grad) or on detached ones");
     return recorded({&q, &k, &t.wq, &t.wk}) ? RotaryFunction::apply(q, k, optional(t.wq), optional(t.wk), optional(t.frequencies), optional(t.positions), t.eps)
                                             : rotary_forward(q, k, t);
 }

@@ -155,7 +155,7 @@ def norm_rotary_backward(grad_q, grad_k, q, k, weight_q=None, weight_k=None, fre
 
 
 def norm_rotary(q, k, weight_q=None, weight_k=None, frequencies=None, positions=None, eps=1e-6):
-    """See ``norm_rotary_forward``; differentiable in q, k and the weights."""
+    """See ``norm_rotary_forward``; differentiable in q, k and the weights (frequencies that need a gradient are refused)."""
     return _native.rotary(q, k, weight_q, weight_k, frequencies, positions, eps)
 
 

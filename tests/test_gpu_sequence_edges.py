@@ -71,6 +71,24 @@ def test_norm_rotary_without_epsilon(layers, dtype, eps, batch, tokens, count, g
             check(got, want[name], dtype, 1, name + "qk"[i])
 
 
+def test_frequencies_have_no_gradient(layers):
+    """One that would be lost is refused, and a tangent."""
+    import torch.autograd.forward_ad as fwd
+    q, k, v, n = normal(1, 2, 3, 4, 8), normal(2, 2, 3, 2, 8), normal(3, 2, 3, 2, 8), torch.tensor([3, 3], dtype=torch.int32, device="cuda")
+    caches = torch.zeros(2, 2, 5, 2, 8, device="cuda")
+    learned = turns(8).requires_grad_()
+    for call in (lambda: layers.norm_rotary(q, k, None, None, learned), lambda: layers.norm_rotary(q.clone().requires_grad_(), k, None, None, learned),
+                 lambda: layers.norm_rotary_step(q, k, v, *caches, n, None, None, learned)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    assert torch.equal(layers.norm_rotary(q, k, None, None, learned.detach())[0], layers.norm_rotary_forward(q, k, None, None, learned)[0])
+    with fwd.dual_level():
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            layers.norm_rotary(q, k, None, None, fwd.make_dual(turns(8), turns(8)))
+
+
 # -------------------------------------------------------------- the block
 
 def blocks(count, dtype=F32, **given):
