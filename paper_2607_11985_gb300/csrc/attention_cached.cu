@@ -648,7 +648,7 @@ template <typename T> Chosen cached_mma_fn(int dim, bool one, bool few) {
 // How the keys are cut.  `most`: keys that can be in sight at once.  The chunks of one, two, .. waves of CTAs that the SMs
 // hold together are compared by their longest SM: its keys, and for each CTA the time of about 192 keys to begin and to
 // end.  Sequences of a batch have other lengths, which the host does not know: the same for two thirds of the
-// keys, dealt as SMs get free, counts twice.
+// keys, dealt as SMs get free, counts twice.  (There is a token at least.)
 struct Cut {
     int chunk, chunks, blocks;
     size_t part, stats;      // bytes
@@ -685,8 +685,11 @@ Cut cut_of(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t
     }
     return c;
 }
+// (Rows (b, head, token) within 31 bits: no more CTAs than that, as a block has a row at least, and cut_of makes no more chunks of blocks
+// than stay on the SMs in 16 waves.)
 bool sizes_ok(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity) {
-    return sequence_sizes_ok(batch, tokens, heads, groups) && heads % groups == 0 && dim >= 1 && dim <= kMostDim && capacity >= 0 && capacity <= kMostTokens;
+    return sequence_sizes_ok(batch, tokens, heads, groups) && heads % groups == 0 && batch * tokens * heads <= 0x7fffffff && dim >= 1 && dim <= kMostDim &&
+           capacity >= 0 && capacity <= kMostTokens;
 }
 
 }  // namespace
@@ -701,6 +704,7 @@ extern "C" {
 size_t vqc_attention_step_workspace_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t groups, int64_t dim, int64_t capacity, int64_t window,
                                           int64_t sinks) {
     if (!sizes_ok(batch, tokens, heads, groups, dim, capacity) || window < 0 || sinks < 0) return (size_t)-1;
+    if (batch * tokens == 0) return 0;
     // (the most of the two kernels, one of which the cache's alignment decides on)
     const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, false), m = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, true);
     return std::max(c.part + c.stats, m.part + m.stats);
@@ -728,7 +732,6 @@ vqc_status vqc_attention_step(vqc_real dtype, int64_t batch, int64_t tokens, int
         const Cut c = cut_of(batch, tokens, heads, groups, dim, capacity, window, sinks, mma);
         if (c.chunks > 1 && (!workspace || workspace_bytes < c.part + c.stats)) return set_error(VQC_ERR_WORKSPACE, call + ": workspace too small");
         const int64_t grid = batch * groups * c.blocks * c.chunks, rows = batch * heads * tokens;
-        if (grid > 0x7fffffff || rows > 0x7fffffff) return set_error(VQC_ERR_INVALID_ARG, call + ": sizes out of range");
         CachedArgs a{};
         a.q = heads_of(*q); a.k = heads_of(*cache_k); a.v = heads_of(*cache_v);
         a.lengths = lengths;
