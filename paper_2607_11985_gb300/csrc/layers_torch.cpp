@@ -278,6 +278,14 @@ HeadRows head_rows(const Tensor& given, const HeadRows& like, int64_t heads, con
         throw Refused(std::string(name) + " does not fit: " + told(given) + " beside " + told(like.t));
     return r;
 }
+// Sequences, places and heads of a cache by their strides, the shortest first: (stride, size).
+using Axes = std::array<std::pair<int64_t, int64_t>, 3>;
+Axes axes_of(const Tensor& t) {
+    Axes axes;
+    for (int i = 0; i < 3; ++i) axes[i] = {t.stride(i), t.size(i)};
+    std::sort(axes.begin(), axes.end());
+    return axes;
+}
 // A cache [batch, capacity, groups, dim], read or written in place.
 HeadRows cache_rows(const Tensor& given, const HeadRows& q, int64_t groups, int64_t capacity, bool written, const char* name) {
     if (written && given.defined() && (given.is_neg() || (at::GradMode::is_enabled() && given.requires_grad())))
@@ -286,13 +294,10 @@ HeadRows cache_rows(const Tensor& given, const HeadRows& q, int64_t groups, int6
     if (r.code != q.code || r.size(0) != q.size(0) || (groups > 0 && r.size(2) != groups) || (capacity >= 0 && r.size(1) != capacity) || r.size(3) != q.size(3))
         throw Refused(std::string(name) + " does not fit: " + told(given) + " beside " + told(q.t));
     if (written) {
-        // axes by their strides, each of which has to step over all places of the shorter ones
-        std::array<std::pair<int64_t, int64_t>, 3> axes;
-        for (int i = 0; i < 3; ++i) axes[i] = {r.t.stride(i), r.t.size(i)};
-        std::sort(axes.begin(), axes.end());
+        // each stride has to step over all places of the shorter ones
         bool apart = r.t.is_same(given);
         int64_t last = r.size(3) - 1;
-        for (const auto& [stride, size] : axes) {
+        for (const auto& [stride, size] : axes_of(r.t)) {
             if (size < 2) continue;
             apart = apart && stride > last;
             last += (size - 1) * stride;
@@ -312,6 +317,25 @@ bool shares(const Tensor& a, const Tensor& b) {
     if (!a.numel() || !b.numel()) return false;
     const auto x = span(a), y = span(b);
     return x.first < y.second && y.first < x.second;
+}
+// Is `rest` the distance of two elements of a cache, as a sum of steps along its axes up to the i-th and within a head?  Where each
+// stride steps over all places of the shorter ones, what those reach is less than it: a step or two of an axis can be meant.
+bool distance_within(const Axes& axes, int i, int64_t dim, int64_t rest) {
+    if (i < 0) return rest < dim && -rest < dim;
+    const auto [stride, size] = axes[i];
+    if (size < 2) return distance_within(axes, i - 1, dim, rest);
+    for (int64_t near = rest / stride, d = near - 1; d <= near + 1; ++d)
+        if (d < size && -d < size && distance_within(axes, i - 1, dim, rest - d * stride)) return true;
+    return false;
+}
+// Is a place of one cache one of the other, too?  (Caches as cache_rows takes them to be written; where their strides differ: may
+// one be?)
+bool caches_meet(const Tensor& a, const Tensor& b) {
+    if (!shares(a, b)) return false;
+    for (int i = 0; i < 3; ++i)
+        if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return true;
+    const int64_t bytes = static_cast<const char*>(b.data_ptr()) - static_cast<const char*>(a.data_ptr());
+    return bytes % a.element_size() || distance_within(axes_of(a), 2, a.size(3), bytes / a.element_size());
 }
 // The forms for serving have no gradients: better an error than one that is lost.
 void without_gradient(std::initializer_list<const Tensor*> all) {
@@ -410,7 +434,7 @@ Tensor rotary_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tens
     const HeadRows kc = cache_rows(ck, a, b.size(2), -1, true, "cache_k"), vc = cache_rows(cv, a, b.size(2), kc.size(1), true, "cache_v");
     without_gradient({&q, &k, &v, &given.wq, &given.wk, &given.frequencies});
     // (views of one tensor that holds keys and values are fine: other places)
-    if (kc.t.numel() && kc.t.data_ptr() == vc.t.data_ptr()) throw Refused("cache_k and cache_v are written: they must be two");
+    if (caches_meet(kc.t, vc.t)) throw Refused("cache_k and cache_v are written: no place of one may be one of the other (got " + told(ck) + " and " + told(cv) + ")");
     for (const HeadRows* from : {&a, &b, &c})
         if (shares(from->t, kc.t) || shares(from->t, vc.t)) throw Refused("the caches are written: q, k and v must lie elsewhere");
     const Turn t = turn_of(a, given);

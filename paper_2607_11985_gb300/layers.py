@@ -162,7 +162,8 @@ def norm_rotary(q, k, weight_q=None, weight_k=None, frequencies=None, positions=
 def norm_rotary_step(q, k, v, cache_k, cache_v, lengths, weight_q=None, weight_k=None, frequencies=None, eps=1e-6):
     """q' of new tokens, whose k' and v are written into the caches [batch, capacity, groups, dim] in place:
     token t of a sequence stands at position lengths - tokens + t (lengths: int32 [batch], with the
-    new tokens); places outside of the cache are not written.  The caches must lie apart from q, k and v.  No
+    new tokens); places outside of the cache are not written.  The caches must lie apart from
+    each other (views of one tensor that holds both are fine where their places are others) and from q, k and v.  No
     gradients: tensors that need one are refused while autograd records."""
     return _native.rotary_step(q, k, v, cache_k, cache_v, lengths, weight_q, weight_k, frequencies, eps)
 

@@ -89,6 +89,38 @@ def test_frequencies_have_no_gradient(layers):
             layers.norm_rotary(q, k, None, None, fwd.make_dual(turns(8), turns(8)))
 
 
+def test_step_refuses_caches_that_meet(layers):
+    """Two views of one tensor are taken where no place of one is one of the other: decided as by listing the places.  What is
+    written is what two tensors get (with the same strides and offsets: packs of elements are added in another order)."""
+    batch, capacity, groups, dim = 2, 3, 2, 8
+    q, k, v = normal(1, batch, 2, 4, dim), normal(2, batch, 2, groups, dim), normal(3, batch, 2, groups, dim)
+    n, memory = torch.tensor([2, 3], dtype=torch.int32, device="cuda"), torch.zeros(1000, device="cuda")
+    counts = [0, 0]
+    for strides in ((48, 16, 8), (96, 32, 8), (96, 16, 48), (100, 33, 9), (96, 32, 16), (16, 100, 8), (200, 16, 8)):
+        at = torch.as_strided(torch.arange(1000), (batch, capacity, groups, dim), (*strides, 1)).reshape(-1)
+        for shift in (-131, -96, -48, -33, -32, -16, -9, -8, -7, -1, 0, 1, 7, 8, 9, 10, 16, 17, 24, 32, 40, 47, 48, 64, 72, 96, 100, 104, 131, 300):
+            ck, cv = (memory.as_strided((batch, capacity, groups, dim), (*strides, 1), 300 + s) for s in (0, shift))
+            meet = bool(torch.isin(at, at + shift).any())
+            counts[meet] += 1
+            memory.zero_()
+            if meet:
+                with pytest.raises(ValueError, match="cache_k and cache_v"):
+                    layers.norm_rotary_step(q, k, v, ck, cv, n)
+                assert not bool(memory.any())
+            else:
+                layers.norm_rotary_step(q, k, v, ck, cv, n)
+                apart = [torch.zeros(1000, device="cuda").as_strided((batch, capacity, groups, dim), (*strides, 1), 300 + s) for s in (0, shift)]
+                layers.norm_rotary_step(q, k, v, *apart, n)
+                assert torch.equal(ck, apart[0]) and torch.equal(cv, apart[1])
+    assert min(counts) > 20, counts
+    # the capacity's last place left out of one and the first of the other; other strides
+    buffer = torch.zeros(batch, 4, groups, dim, device="cuda")
+    for ck, cv in ((buffer[:, :3], buffer[:, 1:]), (buffer[:, :3], buffer.view(batch, groups, 4, dim).transpose(1, 2)[:, :3])):
+        with pytest.raises(ValueError, match="cache_k and cache_v"):
+            layers.norm_rotary_step(q, k, v, ck, cv, n)
+    assert not bool(buffer.any())
+
+
 # -------------------------------------------------------------- the block
 
 def blocks(count, dtype=F32, **given):
