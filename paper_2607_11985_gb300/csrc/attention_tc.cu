@@ -1212,7 +1212,7 @@ BackSpace back_space(int dtype, int64_t batch, int64_t tokens, int64_t heads, in
     b.stats = align256((size_t)(batch * heads * b.pitch) * 4);
     b.most = dtype == VQC_F16 ? 256 : 0;
     // Few tiles of keys leave SMs idle: each is cut into even parts of its units, of which every head has about half as
-    // many as there are tiles.  (1 x 1024 tokens, 16 heads over 4, bfloat16: 56 us in 32 CTAs, 25 in 128.)
+    // many as there are tiles.  (1 x 2048 tokens, 8 heads over one, bfloat16: 172 us in one part, 98 in 2, 61 in 4, 43 in 8, 41 in 16.)
     const int64_t tiles = ceil_div(tokens, N), all = tiles * batch * groups, sms = sm_count();
     if (2 * all <= sms) {
         b.pieces = (int)std::min<int64_t>(std::min<int64_t>(sms / all, 8), std::max<int64_t>(1, heads / groups * (tiles + 1) / 4)) - 1;
@@ -1220,13 +1220,17 @@ BackSpace back_space(int dtype, int64_t batch, int64_t tokens, int64_t heads, in
         b.part = align256((size_t)b.cut * (b.pieces + 1) * batch * groups * 2 * N * (dim <= 64 ? 64 : 128) * 4);
         return b;
     }
-    // Keys seen from behind the window: pieces as long as a window, 2048 queries at least (a piece writes its sums as floats).
+    // Keys seen from behind the window: pieces as long as a window, 2048 queries at least (a piece writes its sums as floats), and no
+    // more of them than two CTAs for each SM: that evens the SMs out, and the sums need no more space than 4 such tiles for each (80 MB).
+    // (8 heads over 2 of 128, the keys' half, 32768 tokens, 16 first ones, window 256: pieces of 1024 182 us, 2048 174, 4096 264, one 1645.
+    // 4096 first tokens, window 1024: 837 us and 143 MB without the bound, 761 with it; over 8 groups, 16000 and 128: 2965 and 2.2 GB, 1783.)
     if (sinks > 0 && window < tokens) {
-        b.piece = (int)std::max<int64_t>(2048, ceil_div(window + N, kUnit) * kUnit);
-        b.pieces = (int)ceil_div(tokens - window, b.piece);
-        b.cut = (int)std::min(ceil_div(sinks, N), ceil_div(tokens, N));
+        const int64_t cut = std::min(ceil_div(sinks, N), tiles), most = 2 * sms / (cut * batch * groups);
         // (where most keys are such there is nothing to even out)
-        if (2 * b.cut > ceil_div(tokens, N)) b.cut = b.pieces = 0;
+        if (2 * cut > tiles || !most) return b;
+        b.cut = (int)cut;
+        b.piece = (int)std::max<int64_t>({2048, ceil_div(window + N, kUnit) * kUnit, ceil_div(ceil_div(tokens - window, most), kUnit) * kUnit});
+        b.pieces = (int)ceil_div(tokens - window, b.piece);
         b.part = align256((size_t)b.cut * (b.pieces + 1) * batch * groups * 2 * N * (dim <= 64 ? 64 : 128) * 4);
     }
     return b;

@@ -121,6 +121,25 @@ def test_step_refuses_caches_that_meet(layers):
     assert not bool(buffer.any())
 
 
+# -------------------------------------------------------------- attention
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("batch,tokens,count,groups,dim,window,sinks,lengths", [
+    (1, 9000, 8, 8, 64, 64, 1500, None), (1, 9000, 8, 8, 64, 300, 1500, [8800]), (3, 4400, 8, 8, 64, 100, 2176, [4400, 4000, 1]), (2, 7000, 4, 2, 128, 40, 3000, None)])
+def test_attention_with_many_first_tokens(layers, dtype, batch, tokens, count, groups, dim, window, sinks, lengths):
+    """So many that their queries are cut into fewer pieces than windows, or not at all."""
+    q, k, v, g = (normal(i, batch, tokens, n, dim, dtype=dtype) for i, n in ((1, count), (2, groups), (3, groups), (4, count)))
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    want = ref.attention(*(wide(t) for t in (q, k, v, g)), window, sinks, None, lengths, dtype)
+    o, saved = layers.attention_forward(q, k, v, window, sinks, lengths=n)
+    check(o, cpu(want["o"]), dtype, 1.5, "o")
+    grads = layers.attention_backward(g, q, k, v, o, saved, window, sinks, lengths=n)
+    for name, x in zip(("gq", "gk", "gv"), grads):
+        check(x, cpu(want[name]), dtype, 2, name)
+    for a, b in zip(layers.attention_backward(g, q, k, v, o, saved, window, sinks, lengths=n), grads):
+        assert torch.equal(a, b)
+
+
 # -------------------------------------------------------------- the block
 
 def blocks(count, dtype=F32, **given):

@@ -35,3 +35,20 @@ def test_workspaces_of_any_sizes():
         B.vqc_norm_rotary_workspace_bytes(batch, tokens, heads, groups, dim)
         for dtype in (B.VQC_F32, B.VQC_BF16, B.VQC_F16):
             B.vqc_attention_workspace_bytes(rng.randrange(2), dtype, batch, tokens, heads, groups, dim, window, sinks, rng.randrange(2))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,groups", [(8, 8), (8, 2), (16, 1)])
+def test_workspace_of_many_first_tokens(heads, groups, dim):
+    """The backward's sums of pieces of queries are bounded, whatever stays visible: by those of 4 tiles of keys (two matrices of 128 rows
+    of floats) for each of 152 SMs, beside two floats for each row of queries (in whole tiles) of every head."""
+    pieces = 4 * 152 * 2 * 128 * dim * 4
+    for batch, tokens, window, sinks in ((1, 32768, 4096, 16), (1, 32768, 128, 16000), (1, 131072, 1024, 4096), (1, 131072, 1024, 65000), (1, 262144, 1024, 65536),
+                                         (4, 65536, 512, 300), (64, 8192, 64, 100), (1, 1 << 22, 1 << 12, 1 << 20)):
+        for dtype in (B.VQC_BF16, B.VQC_F16):
+            with_them, without = (B.vqc_attention_workspace_bytes(1, dtype, batch, tokens, heads, groups, dim, window, s, 1) for s in (sinks, 0))
+            assert without <= 2 * 4 * batch * heads * tokens + 512
+            assert with_them - without <= pieces, (batch, tokens, window, sinks)
+    # few first tokens are cut as they were: one tile of each group, in pieces of the window and a tile
+    one = B.vqc_attention_workspace_bytes(1, B.VQC_BF16, 1, 32768, heads, groups, dim, 4096, 16, 1) - B.vqc_attention_workspace_bytes(1, B.VQC_BF16, 1, 32768, heads, groups, dim, 4096, 0, 1)
+    assert one == groups * (1 + -(-(32768 - 4096) // 4224)) * 2 * 128 * dim * 4
