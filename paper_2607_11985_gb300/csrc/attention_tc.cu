@@ -1116,10 +1116,14 @@ __global__ void __launch_bounds__(256) copy_heads_kernel(const __grid_constant__
 }
 
 int64_t padded(int64_t dim) { return (dim + 7) / 8 * 8; }
+// On 16-byte boundaries, all heads of all tokens (the stride of an axis of one is not used).
+bool on16(const Heads& h, int64_t batch, int64_t tokens, int64_t heads) {
+    return aligned_to(h.p, 16) && (batch == 1 || h.batch % 8 == 0) && (tokens == 1 || h.token % 8 == 0) && (heads == 1 || h.head % 8 == 0);
+}
 bool in_place(const Heads& h, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
     constexpr int64_t kMost = int64_t(1) << 38;      // elements: strides of maps have 40 bits of bytes
-    return dim % 8 == 0 && heads_on(h, 2, 16) && (tokens == 1 || h.token > 0) && (heads == 1 || h.head > 0) && (batch == 1 || h.batch > 0) && h.token < kMost &&
-           h.head < kMost && h.batch < kMost;
+    auto stride = [](int64_t size, int64_t s) { return size == 1 || (s > 0 && s < kMost); };
+    return dim % 8 == 0 && on16(h, batch, tokens, heads) && stride(batch, h.batch) && stride(tokens, h.token) && stride(heads, h.head);
 }
 size_t copy_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t dim) { return align256((size_t)(batch * tokens * heads) * padded(dim) * 2); }
 
@@ -1295,7 +1299,7 @@ vqc_status attention_tc_backward(const AttentionArgs& a, void* ws, size_t bytes,
     r.batch = a.batch; r.tokens = a.sight.tokens; r.pitch = b.pitch;
     r.heads = a.heads; r.groups = a.groups; r.dim = a.dim;
     r.shift = a.dtype == VQC_F16 ? kBackShift : 0.f;
-    r.packs = a.dim % 8 == 0 && heads_on(a.g, 2, 16) && heads_on(a.v, 2, 16);
+    r.packs = a.dim % 8 == 0 && on16(a.g, a.batch, a.sight.tokens, a.heads) && on16(a.v, a.batch, a.sight.tokens, a.groups);
     cudaError_t e = cudaSuccess;
     if (r.most) e = cudaMemsetAsync(r.most, 0, 8, s);
     if (e == cudaSuccess) {

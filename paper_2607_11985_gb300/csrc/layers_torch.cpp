@@ -466,7 +466,7 @@ Sight sight_of(const HeadRows& q, int64_t groups, const Sight& s) {
 bool on16(const HeadRows& r) {
     const int64_t n = r.code == VQC_F32 ? 4 : 8;
     bool on = aligned({r.h.data});
-    for (int i = 0; i < 3; ++i) on = on && r.t.stride(i) % n == 0 && (r.t.stride(i) > 0 || r.t.size(i) == 1);
+    for (int i = 0; i < 3; ++i) on = on && (r.t.size(i) == 1 || (r.t.stride(i) > 0 && r.t.stride(i) % n == 0));
     return on;
 }
 std::pair<Tensor, Tensor> attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Sight& given, bool save) {

@@ -1,5 +1,6 @@
 """Operators of a sequence and their block at the edges: an epsilon of nothing, gradients that have nowhere to go, strides of
 axes of one, prompts over a cache, blocks whose forward pass is made twice, stacked and converted blocks."""
+import ctypes
 import math
 
 import pytest
@@ -122,6 +123,43 @@ def test_step_refuses_caches_that_meet(layers):
 
 
 # -------------------------------------------------------------- attention
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("batch,tokens,count,groups,dim", [(1, 200, 4, 2, 64), (2, 140, 1, 1, 128), (3, 1, 2, 1, 64), (1, 1, 1, 1, 128)])
+def test_strides_of_axes_of_one_are_free(layers, dtype, batch, tokens, count, groups, dim):
+    """As the header says of `aligned`, whose workspace is then enough."""
+    from paper_2607_11985_gb300 import binding as B
+
+    def odd(seed, heads):
+        x = normal(seed, batch, tokens, heads, dim, dtype=dtype)
+        strides = [s if n > 1 else 8 * s + 3 for n, s in zip(x.shape[:3], x.stride()[:3])]
+        return x, torch.as_strided(x, x.shape, strides + [1])
+
+    def heads(x):
+        return ctypes.byref(B.vqc_heads(x.data_ptr(), *x.stride()[:3]))
+    plain, odd_ones = zip(*(odd(i, n) for i, n in ((1, count), (2, groups), (3, groups), (4, count))))
+    (q, k, v, g), (q1, k1, v1, g1) = plain, odd_ones
+    code, stream = {BF16: B.VQC_BF16, F16: B.VQC_F16}[dtype], torch.cuda.current_stream().cuda_stream
+    sizes = (batch, tokens, count, groups, dim)
+    o, saved = layers.attention_forward(q, k, v, 50, 2)
+    grads = layers.attention_backward(g, q, k, v, o, saved, 50, 2)
+    for mode in (0, 1):
+        need = B.vqc_attention_workspace_bytes(mode, code, *sizes, 50, 2, 1)
+        space = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        if mode == 0:
+            assert need == 0
+            out, lse = torch.empty_like(o), torch.empty_like(saved)
+            B.vqc_attention_forward(code, *sizes, heads(q1), heads(k1), heads(v1), 50, 2, dim ** -0.5, None, out.data_ptr(), lse.data_ptr(), None, 0, stream)
+            assert torch.equal(out, o) and torch.equal(lse, saved)
+        else:
+            got = [torch.empty_like(t) for t in grads]
+            B.vqc_attention_backward(code, *sizes, heads(g1), heads(q1), heads(k1), heads(v1), o.data_ptr(), saved.data_ptr(), 50, 2, dim ** -0.5, None,
+                                     *(t.data_ptr() for t in got), space.data_ptr(), need, stream)
+            assert all(torch.equal(a, b) for a, b in zip(got, grads))
+    o1, saved1 = layers.attention_forward(q1, k1, v1, 50, 2)
+    assert torch.equal(o1, o) and torch.equal(saved1, saved)
+    assert all(torch.equal(a, b) for a, b in zip(layers.attention_backward(g1, q1, k1, v1, o1, saved1, 50, 2), grads))
+
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("batch,tokens,count,groups,dim,window,sinks,lengths", [
