@@ -34,9 +34,26 @@ from . import binding as B, layers, workloads as wl
 from .circuit import Circuit
 
 
-class HybridBlock(torch.nn.Module):
+class _Block(torch.nn.Module):
+    """A module some of whose tensors (``own_types``) have types of their own beside the features', which stay theirs where the
+    module is converted to another one."""
+    own_types = ()
+
+    def _apply(self, fn, *args, **kwargs):
+        own = [getattr(self, n) for n in self.own_types]
+        own += [t.grad for t in own if t.grad is not None]
+        kept = {id(t) for t in own}
+
+        def moved(t):
+            r = fn(t)
+            return t.to(r.device) if id(t) in kept and r.dtype != t.dtype else r
+        return super()._apply(moved, *args, **kwargs)
+
+
+class HybridBlock(_Block):
     """See the module's text.  ``spec``: a circuit with one x angle per qubit
     (``workloads.CircuitSpec``), by default a layered ansatz of RY, RZ and CX."""
+    own_types = ("angles", "w_out", "b_out")      # float32, as the circuit
 
     def __init__(self, width: int, qubits: int, depth: int = 2, hidden: int = 0, dtype=torch.float32, spec=None,
                  seed: int = 0):
@@ -81,11 +98,12 @@ class HybridBlock(torch.nn.Module):
         return layers.linear(a, self.w_down, residual=h)
 
 
-class SequenceBlock(torch.nn.Module):
+class SequenceBlock(_Block):
     """See the module's text.  ``heads`` of ``dim`` elements, ``groups`` of keys and values; ``window`` (None: every
     earlier token) and ``sinks`` first tokens that stay visible; ``dropout`` of the attention's branch in
     training, drawn anew in every forward pass: from torch's generator, or with a ``seed`` of its own from that and the
     count of passes (``draws``)."""
+    own_types = ("frequencies",)                  # float64: angles of far positions
 
     def __init__(self, width: int, heads: int, groups: int, dim: int, qubits: int, window=None, sinks: int = 0,
                  dropout: float = 0.0, dtype=torch.float32, seed: int | None = None, **rest):

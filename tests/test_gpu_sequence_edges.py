@@ -274,3 +274,21 @@ def test_captured_block_draws_anew(layers):
         want = torch.where(kept, 2 * gy, 0.0).reshape(-1, 48).double().t() @ a
         assert float((branch.double() - want).norm() / want.norm()) < 1e-5        # sums of 42 terms of another mask: 1
     assert not torch.equal(seen[0], seen[1]) and not torch.equal(seen[1], seen[2])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_converted_block(layers, dtype):
+    """What has a type of its own in a block (the frequencies; the circuit's angles and the projection behind it) keeps it."""
+    from paper_2607_11985_gb300.hybrid import SequenceBlock
+    made = {"window": 7, "sinks": 2, "seed": 5, "hidden": 64}
+    block, other = SequenceBlock(48, 4, 2, 24, 3, **made).to(dtype), SequenceBlock(48, 4, 2, 24, 3, dtype=dtype, **made)
+    assert block.frequencies.dtype == torch.float64
+    for a, b in zip(block.state_dict().values(), other.state_dict().values()):
+        assert a.dtype == b.dtype and torch.equal(a, b)
+    h, gy = normal(1, 2, 21, 48, dtype=dtype), normal(2, 2, 21, 48, dtype=dtype)
+    assert torch.equal(block(h), other(h))
+    block(h).backward(gy)
+    again = block.to(F32)           # gradients go with their parameters
+    for p in again.parameters():
+        assert p.dtype == F32 and p.grad.dtype == F32
+    assert torch.equal(again.frequencies, other.frequencies) and bool(again(h.float()).isfinite().all())
