@@ -1,5 +1,5 @@
 // attention.cu -- causal attention through a window and over the first tokens: entry points,
-// kernels on the FP32 units for every type and head size.
+// kernels on the FP32 units for float32 and for 16-bit heads of more than 128 elements.
 //
 // Query i of a sequence sees key j where j <= i < length and (i - j < window or j < sinks):
 //   z_j = scale q . k_j,   lse = log sum_j exp z_j,   o = sum_j exp(z_j - lse) v_j
@@ -425,9 +425,12 @@ template <typename T, int DM> struct Kernels {
     static cudaError_t run(const AttentionArgs& a, int which, cudaStream_t s) { return which == 0 ? forward(a, s) : which == 1 ? queries(a, s) : keys(a, s); }
 };
 template <typename T> cudaError_t run_typed(const AttentionArgs& a, int which, cudaStream_t s) {
-    return a.dim <= 32 ? Kernels<T, 32>::run(a, which, s)
-         : a.dim <= 64 ? Kernels<T, 64>::run(a, which, s)
-         : a.dim <= 128 ? Kernels<T, 128>::run(a, which, s) : Kernels<T, 256>::run(a, which, s);
+    if constexpr (sizeof(T) == 4) {      // (16-bit heads of up to 128 elements are the tensor cores')
+        if (a.dim <= 32) return Kernels<T, 32>::run(a, which, s);
+        if (a.dim <= 64) return Kernels<T, 64>::run(a, which, s);
+        if (a.dim <= 128) return Kernels<T, 128>::run(a, which, s);
+    }
+    return Kernels<T, 256>::run(a, which, s);
 }
 cudaError_t run_plain(const AttentionArgs& a, int which, cudaStream_t s) {
     return a.dtype == VQC_F32 ? run_typed<float>(a, which, s) : a.dtype == VQC_BF16 ? run_typed<__nv_bfloat16>(a, which, s) : run_typed<__half>(a, which, s);

@@ -630,7 +630,8 @@ struct Chosen {
 template <typename T, int DM, int RB> Chosen cached_fn(bool packs) {
     constexpr int V = 16 / sizeof(T), W = DM / 8 >= V ? V : 1;
     constexpr size_t sums = 16 * RB * (DM + 2) * 4, ring = (size_t)kWarps * kDepth * 2 * (DM / 8 / W) * 512;
-    if (packs && W > 1) return {(const void*)cached_kernel<T, DM, W, RB>, std::max(sums, ring)};
+    if constexpr (W > 1 && (sizeof(T) == 4 || DM > 128))      // (packs of 16-bit heads of up to 128 elements are cached_mma_kernel's)
+        if (packs) return {(const void*)cached_kernel<T, DM, W, RB>, std::max(sums, ring)};
     return {(const void*)cached_kernel<T, DM, 1, RB>, sums};
 }
 template <typename T> Chosen cached_fn(int dim, bool packs) {
