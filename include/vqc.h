@@ -613,7 +613,9 @@ vqc_status vqc_attention_forward(vqc_real dtype, int64_t batch, int64_t tokens, 
 /* Gradients of vqc_attention_forward, from its o and saved: p = exp(z - saved), ds = p (grad_o . v -
  * grad_o . o), grad_v = sum p grad_o, grad_k = scale sum ds q, grad_q = scale sum ds k; grad_k and grad_v
  * summed over the queries of all heads that read the key, in a fixed order; p and ds rounded to
- * dtype before their products.  Rows from a sequence's length on are zero.
+ * dtype before their products, o as it was returned: what the values of a sequence have in common is lost in ds but for
+ * o's rounding, by which the error of grad_q and grad_k grows where that part is large beside their differences.  Rows from
+ * a sequence's length on are zero.
  *   grad_q, grad_k, grad_v  dense of dtype; grad_q or NULL, grad_k and grad_v both or neither.
  *   workspace vqc_attention_workspace_bytes(1, ...) bytes, 256-byte aligned.
  * Errors as vqc_attention_forward. */

@@ -650,6 +650,10 @@ template <typename T> Chosen cached_mma_fn(int dim, bool one, bool few) {
 // hold together are compared by their longest SM: its keys, and for each CTA the time of about 192 keys to begin and to
 // end.  Sequences of a batch have other lengths, which the host does not know: the same for two thirds of the
 // keys, dealt as SMs get free, counts twice.  (There is a token at least.)
+// What the numbers are worth, in us of a pass alone with flushed caches, sequences of up to 8192 keys of other lengths: without the 192 keys
+// 16 of 16 heads over 4 of 64 elements take 66 (38), with 384 of them 24 of 32 heads over 8 of 128 take 144 (124).  Without the half
+// chunk at the end those take 145, and 16 float32 ones of 8 heads of 128 188 (155).  Two thirds: a half is the same, the whole takes 169 for
+// the floats.  Other sizes change by less than 8%.
 struct Cut {
     int chunk, chunks, blocks;
     size_t part, stats;      // bytes

@@ -283,7 +283,8 @@ template <typename T, int C> __global__ void __launch_bounds__(kThreads, 1) forw
         if (!ok && issuer) give_up(gave_up, A.err);
     } else if (warp == 1) {
         // Strictly one half after the other: while one's scores are worked on, the other's are multiplied.  One thread
-        // issues all products: with a warp per half, committed products were seen unfinished.
+        // issues all products: products are ordered among those that one thread issues.  (A version with a warp per half, whose last
+        // commits nobody waited for, gave wrong outputs; which of the two was its fault was not found.)
         constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u << 7 | 1u << 10 : 0u;
         const uint32_t scores = 1u << 4 | kType | (uint32_t)(N >> 3) << 17 | (uint32_t)(N >> 4) << 24;
         const uint32_t outputs = 1u << 4 | kType | 1u << 16 | (uint32_t)(64 * C >> 3) << 17 | (uint32_t)(N >> 4) << 24;
@@ -958,6 +959,9 @@ template <typename T, int C, bool kKeys> __global__ void __launch_bounds__(kThre
 
 // What the backward needs of each row: -g . o and -lse in powers of two, with float16's shift of P (-infinity behind a
 // sequence: no probability), 16 lanes a row, and for float16 the largest squared norms of g's and v's rows.  Bound by HBM.
+// o is the rounded one: the sum of p (g . v) over the keys would have to be made by two more products.  Its rounding is one of dS where
+// values are about as large as their differences (bfloat16 dQ 0.0025 of its norm, with the unrounded o 0.0025; two keys a row 0.0038 and
+// 0.0035), and grows with a part that all values share, which dP - d loses: ten times as large, 0.027 and 0.007.
 struct RowArgs {
     Heads g, v;
     const void* o;

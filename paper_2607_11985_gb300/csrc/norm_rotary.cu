@@ -13,7 +13,8 @@
 // Bound by HBM (x once, y once; x and the gradient once, the result once).  A head's elements lie
 // in the registers of 4 to 32 lanes, each lane with 4 of the first half and their 4 partners, so that pairs meet
 // in a lane; a lane keeps its sines and cosines over the heads of its token.  8192 tokens of 32 + 8 heads of 128, bfloat16:
-// forward 34 us (4.9 TB/s), backward 54 (4.6 TB/s): a head's sums wait for its loads, of which the next heads' are on the way.
+// forward 33 us (5.1 TB/s), backward 54 (4.6 TB/s): a head's sums wait for its loads, of which the next heads' are on the way, and
+// 8192 units of work for the 4864 groups of lanes that stay on the SMs take the time of two rounds.  float32: 58 us (5.8 TB/s), 101 (5.0).
 #include <algorithm>
 #include <cmath>
 
@@ -411,8 +412,8 @@ template <bool kBack> const void* rotary_fn(int dtype, int lanes) {
 
 bool packs4(int dtype, const Heads& h) { return heads_on(h, elem_size(dtype), 4 * elem_size(dtype)); }
 
-// CTAs of a backward that sums over all tokens: as many as stay on the SMs together (8192 tokens of 40 heads of 128: 54 us; with
-// six per SM, which take turns, 60).
+// CTAs of a backward that sums over all tokens: as many as stay on the SMs together (8192 tokens of 40 heads of 128, bfloat16: 54 us; with
+// six per SM, which take turns, 60; float32, with 170 registers, has one of the two at a time).
 int64_t back_ctas(int64_t units, int groups) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), 2LL * sm_count())); }
 // Heads of a token that a group of lanes takes: as many as leave every SM 32 groups, which stay on it together (a token's sines and
 // cosines are made once per group; 64 groups: 37 us in the place of 34 for a forward of 8192 tokens, 128: 44).
