@@ -178,6 +178,44 @@ def test_attention_with_many_first_tokens(layers, dtype, batch, tokens, count, g
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,tokens,count,groups,dim,capacity,window,sinks,lengths", [
+    (2, 300, 4, 1, 64, 700, None, 0, [300, 555]), (1, 129, 6, 2, 128, 400, 60, 3, [390]), (2, 65, 2, 2, 80, 65, 17, 1, [65, 40]),
+    (1, 200, 4, 2, 33, 200, None, 0, [200]), (1, 70, 2, 1, 192, 1500, 1000, 2, [1400])])
+def test_prompt_over_a_cache(layers, dtype, batch, tokens, count, groups, dim, capacity, window, sinks, lengths):
+    """Many new tokens at once, into an empty and a filled cache; the first of them at no position."""
+    q, ck, cv = normal(1, batch, tokens, count, dim, dtype=dtype), normal(2, batch, capacity, groups, dim, dtype=dtype), normal(3, batch, capacity, groups, dim, dtype=dtype)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    want = ref.attention_step(wide(q), wide(ck), wide(cv), lengths, window, sinks, None, dtype)
+    for b, m in enumerate(lengths):
+        ck[b, m:], cv[b, m:] = math.nan, math.inf
+    check(layers.attention_step(q, ck, cv, n, window, sinks), cpu(want), dtype, 1.5, "o")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_captured_float16_backward(layers, dim):
+    """Its norms are set to zero between the kernels: captured, and replayed on new inputs."""
+    q, k, v, g = (normal(i, 2, 200, n, dim, dtype=F16) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+
+    def step():
+        o, saved = layers.attention_forward(q, k, v, 70, 1)
+        return (o, *layers.attention_backward(g, q, k, v, o, saved, 70, 1))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for scale in (1.0, 2.0 ** -8, 2.0 ** 4):
+        g.copy_(normal(9, 2, 200, 4, dim) * scale)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, step()):
+            assert torch.equal(a, b)
+
+
 # -------------------------------------------------------------- the block
 
 def blocks(count, dtype=F32, **given):
